@@ -424,6 +424,112 @@ sa_status sa_stca_bwd(const void* Xs, const void* q, const void* Wq, const void*
                       void* stream);
 
 /*
+ * The sketch cache: users' sketches kept between requests in 8 or 4 bits (the
+ * low-rank caching of the paper, whose sketches are read for an hour or more by
+ * every target of their user), written once per refresh and attended over where
+ * they lie.
+ *
+ * A cache is two caller-owned device arrays: n_slots slots of
+ * sa_cache_slot_bytes(k, D, format) bytes each (16-byte aligned), for sketches of up
+ * to k rows of D values, and rows [n_slots] int32, the valid rows of each slot, zero
+ * before the first write and from then on written by sa_cache_write alone (a caller
+ * may set one to zero, which empties the slot).  Which user has which slot is the
+ * caller's; a slot index outside [0, n_slots), such as -1, is a user without one (a
+ * miss): a write passes it over, a read gives zeros, an attention no rows.
+ *
+ * Format: a row's values in groups of 32 (the last may be short) share one power of
+ * two 2^e.  e is the least integer with amax <= L 2^e, amax the group's largest
+ * magnitude and L the largest that rounds to the type's largest value (7 for
+ * SA_CACHE_FP4, e2m1: 0 .5 1 1.5 2 3 4 6; 464 for SA_CACHE_FP8, e4m3 to 448), held to
+ * -100 <= e <= 125 (fp4) or 119 (fp8).  A value is stored as x / 2^e rounded to
+ * nearest, ties to even (past the largest value, where e is held: that one), and
+ * stands for exactly code 2^e, in bf16 as in fp32.  A group with an infinity or a NaN
+ * reads as NaN.  Per slot, with O = ceil(k / 8) and G = ceil(D / 32): the codes as
+ * [O][G][4][8 rows][8 values], 8 values in 4 (fp4) or 8 bytes with the first in the
+ * lowest bits, then the bytes e + 127 (255: NaN) as [O][G][8 rows], padded to a
+ * multiple of 128 bytes.
+ */
+typedef enum {
+    SA_CACHE_FP8 = 0, /* 8 bits a value and 8 for each 32: 1.03 bytes a value */
+    SA_CACHE_FP4 = 1  /* 4 bits a value and 8 for each 32: 0.53 bytes a value */
+} sa_cache_format;
+
+/* Bytes of one slot; 0 for invalid sizes (k, D >= 1, fewer than 2^31 values). */
+size_t sa_cache_slot_bytes(int32_t k, int32_t D, sa_cache_format format);
+
+/*
+ * Quantises sketches into their slots.
+ *
+ *   Xs          [B,k,D] sketches (dtype), for instance sa_block_fwd's out after the
+ *               adapter, or as it is ([B, H M, d])
+ *   slots       [B] int64 slot of each user.  Where two users of a call have the same
+ *               slot, the last one's sketch is what it holds afterwards
+ *   rows        [B] int32 valid rows of each sketch, clamped to [0, k]; NULL for k.
+ *               The slot's bytes for rows from there on are left as they were
+ *   cache, cache_rows   the cache; cache_rows[slot] becomes the user's rows
+ *
+ * Asynchronous on `stream`, without a workspace.  B = 0 and n_slots = 0 are no-ops.
+ */
+sa_status sa_cache_write(const void* Xs, sa_dtype dtype, const int64_t* slots, const int32_t* rows, int64_t B,
+                         int32_t k, int32_t D, sa_cache_format format, void* cache, int32_t* cache_rows,
+                         int64_t n_slots, void* stream);
+
+/*
+ * Reads slots back: out [B,k,D] (dtype) holds each user's valid rows, exactly the
+ * values that the codes stand for, and zeros from there on.  A slot may be read for
+ * several users.  Asynchronous on `stream`, without a workspace; B = 0 is a no-op.
+ */
+sa_status sa_cache_read(const void* cache, const int32_t* cache_rows, int64_t n_slots, const int64_t* slots,
+                        int64_t B, int32_t k, int32_t D, sa_cache_format format, void* out, sa_dtype dtype,
+                        void* stream);
+
+/* Bytes of workspace that sa_stca_cached_fwd needs for this shape. */
+size_t sa_stca_cached_fwd_workspace_size(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa_dtype dtype);
+
+/*
+ * sa_stca_fwd over cached sketches: each user's Xs is the valid rows of its slot, as
+ * sa_cache_read gives them.  A user without rows (a miss, an empty slot) gets out = 0
+ * and lse = -inf.  Several users may share a slot.
+ *
+ *   cache, cache_rows, n_slots, slots, k, D, format   as for sa_cache_read
+ *   q, Wq, Wk, Wv, R, h, scale, dtype, lse            as for sa_stca_fwd
+ *   out, out_dtype   [B,R,D] in out_dtype: SA_FP32, or SA_BF16 with dtype SA_BF16
+ *                    (rounded once from fp32)
+ *
+ * bf16 mode rounds q W_Q, u, the softmax weights and the aggregates to bf16, as
+ * sa_stca_fwd does, but not the logits; fp32 mode rounds nothing below fp32.  Errors,
+ * ownership and streams as for sa_sketch_fwd; B = 0 is a no-op.
+ */
+sa_status sa_stca_cached_fwd(const void* cache, const int32_t* cache_rows, int64_t n_slots, const int64_t* slots,
+                             sa_cache_format format, const void* q, const void* Wq, const void* Wk, const void* Wv,
+                             int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, float scale, sa_dtype dtype,
+                             void* out, sa_dtype out_dtype, float* lse, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
+/* Bytes of workspace that sa_stca_cached_bwd needs for this shape. */
+size_t sa_stca_cached_bwd_workspace_size(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa_dtype dtype);
+
+/*
+ * Backward of sa_stca_cached_fwd: sa_stca_bwd's gradients for the targets and the
+ * weights.  Cached sketches are constants (they come from an earlier step), so there
+ * is no dXs; a user without rows adds nothing.  The forward is replayed in the
+ * workspace.
+ *
+ *   dout                 [B,R,D] in grad_dtype
+ *   dq                   output [B,R,D] in grad_dtype
+ *   dWq, dWk, dWv        outputs [D,D] in grad_dtype, summed over every user and target
+ *   grad_dtype           SA_FP32, or SA_BF16 with dtype SA_BF16
+ *
+ * All outputs are overwritten.  B = 0 is SA_ERR_INVALID_ARG (nothing to write); other
+ * arguments as for sa_stca_cached_fwd.
+ */
+sa_status sa_stca_cached_bwd(const void* cache, const int32_t* cache_rows, int64_t n_slots, const int64_t* slots,
+                             sa_cache_format format, const void* q, const void* Wq, const void* Wk, const void* Wv,
+                             int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, float scale, sa_dtype dtype,
+                             const void* dout, void* dq, void* dWq, void* dWk, void* dWv, sa_dtype grad_dtype,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * The forward's ranges as a list of segments (the fused backward's work list),
  * exposed for exact testing.
  *

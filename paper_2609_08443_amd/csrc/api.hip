@@ -11,6 +11,7 @@
 #include <mutex>
 #include <vector>
 
+#include "cache.h"
 #include "sa_internal.h"
 
 namespace {
@@ -628,6 +629,165 @@ sa_status stca_forward(const void* Xs, const void* q, const void* Wq, const void
                              false}, stream);
     }
     if (e != hipSuccess) return hip_fail(e, "STCA forward launch");
+    return SA_OK;
+}
+
+// ---------------------------------------------------------------- the sketch cache
+int cache_bits(sa_cache_format format) { return format == SA_CACHE_FP4 ? 4 : 8; }
+
+sa_status check_cache(int64_t B, int32_t k, int32_t D, int64_t n_slots, sa_cache_format format) {
+    if (format != SA_CACHE_FP8 && format != SA_CACHE_FP4)
+        return fail(SA_ERR_INVALID_ARG, "unknown cache format %d", (int)format);
+    if (B < 0 || k < 1 || D < 1 || n_slots < 0)
+        return fail(SA_ERR_INVALID_ARG, "bad sizes B=%lld k=%d D=%d n_slots=%lld", (long long)B, k, D,
+                    (long long)n_slots);
+    // a slot's values, a row's padding included, are counted in 32 bits
+    if ((((int64_t)k + 7) / 8 * 8) * (((int64_t)D + 31) / 32 * 32) >= (int64_t(1) << 31))
+        return fail(SA_ERR_UNSUPPORTED, "k * D must be < 2^31");
+    if (B > 0 && (B + k >= (int64_t(1) << 31) - 1 || B * sa::cache_io_workgroups(k, D) >= (int64_t(1) << 31)))
+        return fail(SA_ERR_UNSUPPORTED, "sizes beyond the supported range");
+    return SA_OK;
+}
+
+sa::CacheView cache_view(const void* cache, const int32_t* rows, const int64_t* slots, int64_t n_slots, int32_t k,
+                         int32_t D, sa_cache_format format) {
+    sa::CacheView c;
+    c.data = reinterpret_cast<const uint8_t*>(cache);
+    c.rows = rows;
+    c.slots = slots;
+    c.n_slots = n_slots;
+    c.slot_bytes = (int64_t)sa_cache_slot_bytes(k, D, format);
+    c.k = k;
+    c.D = D;
+    c.G = (D + sa::cachefmt::kGroup - 1) / sa::cachefmt::kGroup;
+    c.scales_at = ((int64_t)k + 7) / 8 * c.G * sa::cachefmt::kGroup * cache_bits(format);
+    return c;
+}
+
+// STCA over cached sketches in separate products: [Xd | Qp | U | S (fp32) | alpha | C |
+// lse (fp32) | (bwd) dout in the operand dtype | dC | dalpha (fp32) | ds | dU | dQp];
+// Xd [B,k,D] are the sketches read from the cache, the rest as in StcaPlan.
+struct CachedPlan {
+    size_t off_xd = 0, off_qp = 0, off_u = 0, off_s = 0, off_al = 0, off_c = 0, off_lse = 0, off_dob = 0, off_dc = 0,
+           off_da = 0, off_ds = 0, off_du = 0, off_dqp = 0, total = 0;
+};
+
+CachedPlan plan_cached(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa_dtype dtype, bool bwd) {
+    CachedPlan p;
+    size_t off = 0;
+    auto carve = [&](size_t bytes) {
+        const size_t o = off;
+        off = align_up(off + bytes, 256);
+        return o;
+    };
+    const size_t el = dtype == SA_BF16 ? 2 : 4;
+    const size_t BR = (size_t)B * R, rows = BR * h;
+    p.off_xd = carve(el * B * k * D);
+    p.off_qp = carve(el * BR * D);
+    p.off_u = carve(el * rows * D);
+    p.off_s = carve(4 * rows * k);
+    p.off_al = carve(el * rows * k);
+    p.off_c = carve(el * rows * D);
+    p.off_lse = carve(4 * rows);
+    if (bwd) {
+        p.off_dob = carve(dtype == SA_BF16 ? el * BR * D : 0);
+        p.off_dc = carve(el * rows * D);
+        p.off_da = carve(4 * rows * k);
+        p.off_ds = carve(el * rows * k);
+        p.off_du = carve(el * rows * D);
+        p.off_dqp = carve(el * BR * D);
+    }
+    p.total = off;
+    return p;
+}
+
+struct CachedArgs {
+    sa::CacheView cache;
+    int bits;
+    const void *q, *Wq, *Wk, *Wv;
+    int64_t B;
+    int32_t R, k, D, h;
+    float scale;
+    bool bf;
+};
+
+// Qp, U and the attention over the cached rows: C [B,R,h,D] and lse
+sa_status cached_attention(const CachedArgs& a, float* lse, uint8_t* ws, const CachedPlan& p, hipStream_t stream) {
+    const bool bf = a.bf;
+    const int32_t BR = (int32_t)(a.B * a.R), D = a.D, k = a.k, dh = D / a.h, Rh = a.R * a.h;
+    const int64_t kD = (int64_t)k * D, RhD = (int64_t)Rh * D, Rhk = (int64_t)Rh * k;
+    void *Xd = ws + p.off_xd, *Qp = ws + p.off_qp, *U = ws + p.off_u, *Al = ws + p.off_al, *Cc = ws + p.off_c;
+    float* S = reinterpret_cast<float*>(ws + p.off_s);
+    hipError_t e;
+    {
+        sa::ProfScope ps("cached_read", stream);
+        e = sa::launch_cache_read(a.cache, a.bits, Xd, bf, a.B, stream);
+    }
+    if (e == hipSuccess) {
+        sa::ProfScope ps("cached_query_proj", stream);
+        e = sa::launch_gemm({a.q, bf, 0, D, 1, a.Wq, bf, 0, D, 1, Qp, bf, 0, D, BR, D, D, 1, 1.f, false}, stream);
+        if (e == hipSuccess)
+            e = sa::launch_gemm({Qp, bf, dh, D, 1, a.Wk, bf, dh, 1, D, U, bf, D, (int64_t)a.h * D, BR, D, dh, a.h, 1.f,
+                                 false}, stream);
+    }
+    if (e == hipSuccess) {
+        sa::ProfScope ps("cached_logits", stream);
+        e = sa::launch_gemm({U, bf, RhD, D, 1, Xd, bf, kD, 1, D, S, false, Rhk, k, Rh, k, D, (int32_t)a.B, a.scale,
+                             false}, stream);
+    }
+    if (e == hipSuccess) {
+        sa::ProfScope ps("cached_softmax", stream);
+        e = sa::launch_cached_softmax(a.cache, S, (int64_t)BR * a.h, Rh, bf, Al, lse, stream);
+    }
+    if (e == hipSuccess) {
+        sa::ProfScope ps("cached_aggregate", stream);
+        e = sa::launch_gemm({Al, bf, Rhk, k, 1, Xd, bf, kD, D, 1, Cc, bf, RhD, D, Rh, D, k, (int32_t)a.B, 1.f, false},
+                            stream);
+    }
+    if (e != hipSuccess) return hip_fail(e, "cached STCA launch");
+    return SA_OK;
+}
+
+// dU from C's gradient dC = dout W_V^T: the attention's backward towards its queries
+sa_status cached_attention_bwd(const CachedArgs& a, const float* lse, uint8_t* ws, const CachedPlan& p,
+                               hipStream_t stream) {
+    const bool bf = a.bf;
+    const int32_t D = a.D, k = a.k, Rh = a.R * a.h;
+    const int64_t kD = (int64_t)k * D, RhD = (int64_t)Rh * D, Rhk = (int64_t)Rh * k;
+    const void *Xd = ws + p.off_xd, *dC = ws + p.off_dc;
+    const float* S = reinterpret_cast<const float*>(ws + p.off_s);
+    float* dA = reinterpret_cast<float*>(ws + p.off_da);
+    void *ds = ws + p.off_ds, *dU = ws + p.off_du;
+    hipError_t e;
+    {
+        sa::ProfScope ps("cached_dalpha", stream);
+        e = sa::launch_gemm({dC, bf, RhD, D, 1, Xd, bf, kD, 1, D, dA, false, Rhk, k, Rh, k, D, (int32_t)a.B, 1.f, false},
+                            stream);
+    }
+    if (e == hipSuccess) {
+        sa::ProfScope ps("cached_softmax_bwd", stream);
+        e = sa::launch_cached_softmax_bwd(a.cache, S, lse, dA, a.B * Rh, Rh, a.scale, bf, ds, stream);
+    }
+    if (e == hipSuccess) {
+        sa::ProfScope ps("cached_query_side", stream);
+        e = sa::launch_gemm({ds, bf, Rhk, k, 1, Xd, bf, kD, D, 1, dU, bf, RhD, D, Rh, D, k, (int32_t)a.B, 1.f, false},
+                            stream);
+    }
+    if (e != hipSuccess) return hip_fail(e, "cached STCA backward launch");
+    return SA_OK;
+}
+
+// arguments shared by the two directions
+sa_status check_cached(const CachedArgs& a, const int64_t* slots, const void* cache, const int32_t* cache_rows,
+                       sa_dtype io_dtype) {
+    if (io_dtype != SA_FP32 && io_dtype != SA_BF16)
+        return fail(SA_ERR_INVALID_ARG, "unknown result dtype %d", (int)io_dtype);
+    if (io_dtype == SA_BF16 && !a.bf) return fail(SA_ERR_UNSUPPORTED, "SA_FP32 inputs have SA_FP32 results");
+    if (!slots || !a.q || !a.Wq || !a.Wk || !a.Wv || (a.cache.n_slots > 0 && (!cache || !cache_rows)))
+        return fail(SA_ERR_INVALID_ARG, "null pointer argument");
+    if (!aligned16(cache) || !aligned16(cache_rows) || !aligned16(slots) || !aligned16(a.q) || !aligned16(a.Wq) ||
+        !aligned16(a.Wk) || !aligned16(a.Wv))
+        return fail(SA_ERR_INVALID_ARG, "tensor arguments must be 16-byte aligned");
     return SA_OK;
 }
 
@@ -1521,6 +1681,160 @@ sa_status sa_stca_bwd(const void* Xs, const void* q, const void* Wq, const void*
             e = sa::launch_gemm({q, bf, 0, 1, D, dQp, bf, 0, D, 1, dWq, false, 0, D, D, D, BR, 1, 1.f, false}, stream);
     }
     if (e != hipSuccess) return hip_fail(e, "STCA backward launch");
+    return SA_OK;
+}
+
+size_t sa_cache_slot_bytes(int32_t k, int32_t D, sa_cache_format format) {
+    if (check_cache(0, k, D, 0, format) != SA_OK) return 0;
+    const size_t octets = ((size_t)k + 7) / 8, groups = ((size_t)D + sa::cachefmt::kGroup - 1) / sa::cachefmt::kGroup;
+    return align_up(octets * groups * (sa::cachefmt::kGroup * cache_bits(format) + 8), 128);
+}
+
+sa_status sa_cache_write(const void* Xs, sa_dtype dtype, const int64_t* slots, const int32_t* rows, int64_t B,
+                         int32_t k, int32_t D, sa_cache_format format, void* cache, int32_t* cache_rows,
+                         int64_t n_slots, void* stream_) {
+    g_last_error[0] = 0;
+    if (dtype != SA_BF16 && dtype != SA_FP32) return fail(SA_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+    sa_status st = check_cache(B, k, D, n_slots, format);
+    if (st != SA_OK) return st;
+    if (B == 0 || n_slots == 0) return SA_OK;
+    if (!Xs || !slots || !cache || !cache_rows) return fail(SA_ERR_INVALID_ARG, "null pointer argument");
+    if (!aligned16(Xs) || !aligned16(slots) || !aligned16(rows) || !aligned16(cache) || !aligned16(cache_rows))
+        return fail(SA_ERR_INVALID_ARG, "tensor arguments must be 16-byte aligned");
+    hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
+    sa::ProfScope ps("cache_write", stream);
+    hipError_t e = sa::launch_cache_write(cache_view(cache, cache_rows, slots, n_slots, k, D, format),
+                                          cache_bits(format), Xs, dtype == SA_BF16, rows, B, stream);
+    if (e != hipSuccess) return hip_fail(e, "cache write launch");
+    return SA_OK;
+}
+
+sa_status sa_cache_read(const void* cache, const int32_t* cache_rows, int64_t n_slots, const int64_t* slots, int64_t B,
+                        int32_t k, int32_t D, sa_cache_format format, void* out, sa_dtype dtype, void* stream_) {
+    g_last_error[0] = 0;
+    if (dtype != SA_BF16 && dtype != SA_FP32) return fail(SA_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+    sa_status st = check_cache(B, k, D, n_slots, format);
+    if (st != SA_OK) return st;
+    if (B == 0) return SA_OK;
+    if (!slots || !out || (n_slots > 0 && (!cache || !cache_rows)))
+        return fail(SA_ERR_INVALID_ARG, "null pointer argument");
+    if (!aligned16(slots) || !aligned16(out) || !aligned16(cache) || !aligned16(cache_rows))
+        return fail(SA_ERR_INVALID_ARG, "tensor arguments must be 16-byte aligned");
+    hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
+    sa::ProfScope ps("cache_read", stream);
+    hipError_t e = sa::launch_cache_read(cache_view(cache, cache_rows, slots, n_slots, k, D, format),
+                                         cache_bits(format), out, dtype == SA_BF16, B, stream);
+    if (e != hipSuccess) return hip_fail(e, "cache read launch");
+    return SA_OK;
+}
+
+size_t sa_stca_cached_fwd_workspace_size(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa_dtype dtype) {
+    if (check_stca(B, R, k, D, h, 1.0f, dtype) != SA_OK || check_cache(B, k, D, 0, SA_CACHE_FP8) != SA_OK) return 0;
+    return plan_cached(B, R, k, D, h, dtype, false).total;
+}
+
+sa_status sa_stca_cached_fwd(const void* cache, const int32_t* cache_rows, int64_t n_slots, const int64_t* slots,
+                             sa_cache_format format, const void* q, const void* Wq, const void* Wk, const void* Wv,
+                             int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, float scale, sa_dtype dtype,
+                             void* out, sa_dtype out_dtype, float* lse, void* workspace, size_t workspace_bytes,
+                             void* stream_) {
+    g_last_error[0] = 0;
+    sa_status st = check_stca(B, R, k, D, h, scale, dtype);
+    if (st == SA_OK) st = check_cache(B, k, D, n_slots, format);
+    if (st != SA_OK) return st;
+    const bool bf = dtype == SA_BF16;
+    const CachedArgs a{cache_view(cache, cache_rows, slots, n_slots, k, D, format), cache_bits(format), q, Wq, Wk, Wv,
+                       B, R, k, D, h, scale, bf};
+    if (B == 0) return SA_OK;
+    st = check_cached(a, slots, cache, cache_rows, out_dtype);
+    if (st != SA_OK) return st;
+    if (!out) return fail(SA_ERR_INVALID_ARG, "null pointer argument");
+    if (!aligned16(out) || !aligned16(lse))
+        return fail(SA_ERR_INVALID_ARG, "tensor arguments must be 16-byte aligned");
+    const CachedPlan p = plan_cached(B, R, k, D, h, dtype, false);
+    if (!workspace || workspace_bytes < p.total)
+        return fail(SA_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", p.total,
+                    workspace ? workspace_bytes : (size_t)0);
+    if (!aligned16(workspace)) return fail(SA_ERR_WORKSPACE, "workspace must be 16-byte aligned");
+    uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
+    hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
+    st = cached_attention(a, lse ? lse : reinterpret_cast<float*>(ws + p.off_lse), ws, p, stream);
+    if (st != SA_OK) return st;
+    const int32_t BR = (int32_t)(B * R), dh = D / h;
+    sa::ProfScope ps("cached_value_proj", stream);   // out[., head i] = C[., i] W_V^(i)
+    hipError_t e = sa::launch_gemm({ws + p.off_c, bf, D, (int64_t)h * D, 1, Wv, bf, dh, D, 1, out, out_dtype == SA_BF16,
+                                    dh, D, BR, dh, D, h, 1.f, false}, stream);
+    if (e != hipSuccess) return hip_fail(e, "cached STCA launch");
+    return SA_OK;
+}
+
+size_t sa_stca_cached_bwd_workspace_size(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa_dtype dtype) {
+    if (check_stca(B, R, k, D, h, 1.0f, dtype) != SA_OK || check_cache(B, k, D, 0, SA_CACHE_FP8) != SA_OK) return 0;
+    return plan_cached(B, R, k, D, h, dtype, true).total;
+}
+
+sa_status sa_stca_cached_bwd(const void* cache, const int32_t* cache_rows, int64_t n_slots, const int64_t* slots,
+                             sa_cache_format format, const void* q, const void* Wq, const void* Wk, const void* Wv,
+                             int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, float scale, sa_dtype dtype,
+                             const void* dout, void* dq, void* dWq, void* dWk, void* dWv, sa_dtype grad_dtype,
+                             void* workspace, size_t workspace_bytes, void* stream_) {
+    g_last_error[0] = 0;
+    sa_status st = check_stca(B, R, k, D, h, scale, dtype);
+    if (st == SA_OK) st = check_cache(B, k, D, n_slots, format);
+    if (st != SA_OK) return st;
+    if (B < 1) return fail(SA_ERR_INVALID_ARG, "B must be >= 1 for the backward");
+    const bool bf = dtype == SA_BF16, gb = grad_dtype == SA_BF16;
+    const CachedArgs a{cache_view(cache, cache_rows, slots, n_slots, k, D, format), cache_bits(format), q, Wq, Wk, Wv,
+                       B, R, k, D, h, scale, bf};
+    st = check_cached(a, slots, cache, cache_rows, grad_dtype);
+    if (st != SA_OK) return st;
+    if (!dout || !dq || !dWq || !dWk || !dWv) return fail(SA_ERR_INVALID_ARG, "null pointer argument");
+    if (!aligned16(dout) || !aligned16(dq) || !aligned16(dWq) || !aligned16(dWk) || !aligned16(dWv))
+        return fail(SA_ERR_INVALID_ARG, "tensor arguments must be 16-byte aligned");
+    const CachedPlan p = plan_cached(B, R, k, D, h, dtype, true);
+    if (!workspace || workspace_bytes < p.total)
+        return fail(SA_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", p.total,
+                    workspace ? workspace_bytes : (size_t)0);
+    if (!aligned16(workspace)) return fail(SA_ERR_WORKSPACE, "workspace must be 16-byte aligned");
+    uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
+    hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
+    float* lse = reinterpret_cast<float*>(ws + p.off_lse);
+    st = cached_attention(a, lse, ws, p, stream);   // Qp, U, lse and C once more
+    if (st != SA_OK) return st;
+    const int32_t BR = (int32_t)(B * R), dh = D / h;
+    const int64_t hD = (int64_t)h * D;
+    void *Qp = ws + p.off_qp, *Cc = ws + p.off_c, *dC = ws + p.off_dc, *dU = ws + p.off_du, *dQp = ws + p.off_dqp;
+    const void* dob = dout;
+    hipError_t e = hipSuccess;
+    {
+        sa::ProfScope ps("cached_value_grads", stream);
+        if (bf && !gb) {
+            dob = ws + p.off_dob;
+            e = sa::launch_to_bf16(reinterpret_cast<const float*>(dout), reinterpret_cast<uint16_t*>(ws + p.off_dob),
+                                   (int64_t)BR * D, stream);
+        }
+        // dC[., i] = dout[., head i] W_V^(i)T;  dW_V^(i) = sum over targets of C[., i]^T dout[., head i]
+        if (e == hipSuccess)
+            e = sa::launch_gemm({dob, bf, dh, D, 1, Wv, bf, dh, 1, D, dC, bf, D, hD, BR, D, dh, h, 1.f, false}, stream);
+        if (e == hipSuccess)
+            e = sa::launch_gemm({Cc, bf, D, 1, hD, dob, bf, dh, D, 1, dWv, gb, dh, D, D, dh, BR, h, 1.f, false}, stream);
+    }
+    if (e != hipSuccess) return hip_fail(e, "cached STCA backward launch");
+    st = cached_attention_bwd(a, lse, ws, p, stream);
+    if (st != SA_OK) return st;
+    {
+        sa::ProfScope ps("cached_query_grads", stream);
+        // dQp[., head i] = dU[., i] W_K^(i);  dW_K^(i) = sum dU[., i]^T Qp[., head i]
+        e = sa::launch_gemm({dU, bf, D, hD, 1, Wk, bf, dh, D, 1, dQp, bf, dh, D, BR, dh, D, h, 1.f, false}, stream);
+        if (e == hipSuccess)
+            e = sa::launch_gemm({dU, bf, D, 1, hD, Qp, bf, dh, D, 1, dWk, gb, dh, D, D, dh, BR, h, 1.f, false}, stream);
+        // dq = dQp W_Q^T;  dW_Q = q^T dQp
+        if (e == hipSuccess)
+            e = sa::launch_gemm({dQp, bf, 0, D, 1, Wq, bf, 0, 1, D, dq, gb, 0, D, BR, D, D, 1, 1.f, false}, stream);
+        if (e == hipSuccess)
+            e = sa::launch_gemm({q, bf, 0, 1, D, dQp, bf, 0, D, 1, dWq, gb, 0, D, D, D, BR, 1, 1.f, false}, stream);
+    }
+    if (e != hipSuccess) return hip_fail(e, "cached STCA backward launch");
     return SA_OK;
 }
 

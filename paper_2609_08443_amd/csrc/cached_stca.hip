@@ -1,0 +1,100 @@
+// STCA over the sketch cache (sa_stca_cached_fwd / sa_stca_cached_bwd): the row
+// kernels of the path in separate products, in which the cached sketches are read into
+// the workspace and the products run on the batched GEMM.
+//
+// A row is the k fp32 logits of one (user, target, head), of which the user's first n
+// count; one wave per row.  Weights past n are zero, and all of them where n = 0.
+#include "cache.h"
+
+namespace sa {
+
+namespace {
+
+__device__ inline float wave_max(float v) {
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) v = fmaxf(v, __shfl_xor(v, k, 64));
+    return v;
+}
+__device__ inline float wave_sum(float v) {
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) v += __shfl_xor(v, k, 64);
+    return v;
+}
+template <bool BF>
+__device__ inline void put(void* p, int64_t i, float v) {
+    if constexpr (BF) reinterpret_cast<uint16_t*>(p)[i] = tile::to_bf16(v);
+    else reinterpret_cast<float*>(p)[i] = v;
+}
+
+// lse = log sum_j exp(s_j), -inf for no rows; alpha_j = exp(s_j - max) / sum
+template <bool BF>
+__global__ __launch_bounds__(256) void cached_softmax_kernel(CacheView c, const float* __restrict__ S, int64_t rows,
+                                                             int32_t Rh, void* __restrict__ alpha,
+                                                             float* __restrict__ lse) {
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= rows) return;
+    int32_t n;
+    cache_slot(c, row / Rh, &n);
+    const int lane = threadIdx.x & 63;
+    const float* s = S + row * c.k;
+    float mx = -INFINITY;
+    for (int j = lane; j < n; j += 64) mx = fmaxf(mx, s[j]);
+    mx = wave_max(mx);
+    if (mx == -INFINITY) mx = 0.f;
+    float z = 0.f;
+    for (int j = lane; j < n; j += 64) z += __expf(s[j] - mx);
+    z = wave_sum(z);
+    const float inv = n ? 1.f / z : 0.f;
+    for (int j = lane; j < c.k; j += 64) put<BF>(alpha, row * c.k + j, j < n ? __expf(s[j] - mx) * inv : 0.f);
+    if (lane == 0) lse[row] = mx + __logf(z);
+}
+
+// ds_j = scale alpha_j (da_j - sum_i alpha_i da_i), alpha_j = exp(s_j - lse)
+template <bool BF>
+__global__ __launch_bounds__(256) void cached_softmax_bwd_kernel(CacheView c, const float* __restrict__ S,
+                                                                 const float* __restrict__ lse,
+                                                                 const float* __restrict__ dA, int64_t rows,
+                                                                 int32_t Rh, float scale, void* __restrict__ ds) {
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= rows) return;
+    int32_t n;
+    cache_slot(c, row / Rh, &n);
+    const int lane = threadIdx.x & 63;
+    const float *s = S + row * c.k, *da = dA + row * c.k;
+    const float l = lse[row];
+    float dot = 0.f, z = 0.f;
+    for (int j = lane; j < n; j += 64) {
+        const float p = __expf(s[j] - l);
+        dot = __builtin_fmaf(p, da[j], dot);
+        z += p;
+    }
+    // sum of the weights as they come out here, 1 up to rounding: the gradients' sum over a
+    // row then vanishes to the last bit for one row, and no worse than rounding otherwise
+    dot = wave_sum(dot) / wave_sum(z);
+    for (int j = lane; j < c.k; j += 64)
+        put<BF>(ds, row * c.k + j, j < n ? scale * __expf(s[j] - l) * (da[j] - dot) : 0.f);
+}
+
+}  // namespace
+
+hipError_t launch_cached_softmax(const CacheView& c, const float* S, int64_t rows, int32_t Rh, bool bf16, void* alpha,
+                                 float* lse, hipStream_t stream) {
+    if (rows <= 0) return hipSuccess;
+    const dim3 grid((unsigned)((rows + 3) / 4));
+    if (bf16) hipLaunchKernelGGL(cached_softmax_kernel<true>, grid, dim3(256), 0, stream, c, S, rows, Rh, alpha, lse);
+    else hipLaunchKernelGGL(cached_softmax_kernel<false>, grid, dim3(256), 0, stream, c, S, rows, Rh, alpha, lse);
+    return hipGetLastError();
+}
+
+hipError_t launch_cached_softmax_bwd(const CacheView& c, const float* S, const float* lse, const float* dA,
+                                     int64_t rows, int32_t Rh, float scale, bool bf16, void* ds, hipStream_t stream) {
+    if (rows <= 0) return hipSuccess;
+    const dim3 grid((unsigned)((rows + 3) / 4));
+    if (bf16)
+        hipLaunchKernelGGL(cached_softmax_bwd_kernel<true>, grid, dim3(256), 0, stream, c, S, lse, dA, rows, Rh, scale, ds);
+    else
+        hipLaunchKernelGGL(cached_softmax_bwd_kernel<false>, grid, dim3(256), 0, stream, c, S, lse, dA, rows, Rh, scale, ds);
+    return hipGetLastError();
+}
+
+}  // namespace sa

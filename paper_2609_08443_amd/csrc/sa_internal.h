@@ -215,6 +215,21 @@ hipError_t launch_stca_softmax_bwd(const void* S, bool s_bf16, const float* lse,
                                    int32_t k, float scale, bool bf16, void* ds, hipStream_t stream);
 hipError_t launch_to_bf16(const float* x, uint16_t* y, int64_t n, hipStream_t stream);
 
+// The sketch cache (cache.hip, cached_stca.hip; CacheView in cache.h).  bits: 4 or 8.
+struct CacheView;
+// workgroups a user of a write or a read takes
+int64_t cache_io_workgroups(int32_t k, int32_t D);
+// n: rows of each user [B], or null for k; c's data and rows are written
+hipError_t launch_cache_write(const CacheView& c, int bits, const void* Xs, bool bf16, const int32_t* n, int64_t B,
+                              hipStream_t stream);
+// out [B][k][D]; zeros past a slot's rows
+hipError_t launch_cache_read(const CacheView& c, int bits, void* out, bool bf16, int64_t B, hipStream_t stream);
+// softmax rows over each user's valid rows (rows = B Rh of k fp32 logits) and its backward
+hipError_t launch_cached_softmax(const CacheView& c, const float* S, int64_t rows, int32_t Rh, bool bf16, void* alpha,
+                                 float* lse, hipStream_t stream);
+hipError_t launch_cached_softmax_bwd(const CacheView& c, const float* S, const float* lse, const float* dA,
+                                     int64_t rows, int32_t Rh, float scale, bool bf16, void* ds, hipStream_t stream);
+
 // Stacked-SA refinement (block.hip).  add_ln: one row of d features per
 // (user, head, prototype): out[r] = LN(x[r mod x_rows] + y[r]) * gamma[h] + beta[h],
 // h = (r / M) % H; x fp32 or bf16 (the shared prototypes broadcast over users

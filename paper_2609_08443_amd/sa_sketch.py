@@ -10,12 +10,13 @@ from __future__ import annotations
 import ctypes
 import math
 import os
-from typing import Optional, Tuple
+from typing import Any, NamedTuple, Optional, Tuple
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsa_sketch.so")
 
 SA_BF16, SA_FP32 = 0, 1
+CACHE_FORMATS = {"fp8": 0, "fp4": 1}
 _STATUS = {0: "SA_OK", 1: "SA_ERR_INVALID_ARG", 2: "SA_ERR_UNSUPPORTED", 3: "SA_ERR_WORKSPACE",
            4: "SA_ERR_BAD_OFFSETS", 5: "SA_ERR_HIP"}
 ITEM_WORDS = 8
@@ -27,7 +28,10 @@ EXPORTS = ("sa_sketch_fwd_workspace_size", "sa_sketch_fwd", "sa_sketch_fwd_noall
            "sa_layer_bwd", "sa_block_fwd_workspace_size", "sa_block_fwd",
            "sa_block_saved_size", "sa_block_saved_offset", "sa_block_bwd_workspace_size", "sa_block_bwd",
            "sa_stca_fwd_workspace_size", "sa_stca_fwd",
-           "sa_stca_bwd_workspace_size", "sa_stca_bwd", "sa_gemm_tile_shapes", "sa_gemm_bf16",
+           "sa_stca_bwd_workspace_size", "sa_stca_bwd",
+           "sa_cache_slot_bytes", "sa_cache_write", "sa_cache_read",
+           "sa_stca_cached_fwd_workspace_size", "sa_stca_cached_fwd",
+           "sa_stca_cached_bwd_workspace_size", "sa_stca_cached_bwd", "sa_gemm_tile_shapes", "sa_gemm_bf16",
            "sa_profile_enable", "sa_kernel_times", "sa_status_string", "sa_last_error")
 
 
@@ -107,6 +111,20 @@ def lib() -> ctypes.CDLL:
     L.sa_stca_bwd.argtypes = [vp, vp, vp, vp, vp, i64, i32, i32, i32, i32, f32, c.c_int, vp, vp, vp, vp, vp, vp,
                               vp, sz, vp]
     L.sa_stca_bwd.restype = c.c_int
+    L.sa_cache_slot_bytes.argtypes = [i32, i32, c.c_int]
+    L.sa_cache_slot_bytes.restype = sz
+    L.sa_cache_write.argtypes = [vp, c.c_int, vp, vp, i64, i32, i32, c.c_int, vp, vp, i64, vp]
+    L.sa_cache_write.restype = c.c_int
+    L.sa_cache_read.argtypes = [vp, vp, i64, vp, i64, i32, i32, c.c_int, vp, c.c_int, vp]
+    L.sa_cache_read.restype = c.c_int
+    for nm in ("sa_stca_cached_fwd_workspace_size", "sa_stca_cached_bwd_workspace_size"):
+        getattr(L, nm).argtypes = [i64, i32, i32, i32, i32, c.c_int]
+        getattr(L, nm).restype = sz
+    cached = [vp, vp, i64, vp, c.c_int, vp, vp, vp, vp, i64, i32, i32, i32, i32, f32, c.c_int]
+    L.sa_stca_cached_fwd.argtypes = cached + [vp, c.c_int, vp, vp, sz, vp]
+    L.sa_stca_cached_fwd.restype = c.c_int
+    L.sa_stca_cached_bwd.argtypes = cached + [vp, vp, vp, vp, vp, c.c_int, vp, sz, vp]
+    L.sa_stca_cached_bwd.restype = c.c_int
     L.sa_build_worklist.argtypes = [vp, i64, i64, i32, i64, vp, i64, vp, vp]
     L.sa_build_worklist.restype = c.c_int
     L.sa_status_string.argtypes = [c.c_int]
@@ -571,6 +589,182 @@ def stca_bwd(Xs, q, Wq, Wk, Wv, h: int, dout, scale: Optional[float] = None, wor
     rc = lib().sa_stca_bwd(_ptr(Xs), _ptr(q), _ptr(Wq), _ptr(Wk), _ptr(Wv), B, R, k, D, h, float(scale), code,
                            _ptr(dout), _ptr(g["dXs"]), _ptr(g["dq"]), _ptr(g["dWq"]), _ptr(g["dWk"]),
                            _ptr(g["dWv"]), _ptr(ws), nbytes, _stream_handle(stream))
+    _check(rc)
+    return g
+
+
+class SketchCache(NamedTuple):
+    """Users' sketches in 8 or 4 bits: the caller's device tensors `data` uint8
+    [n_slots, cache_slot_bytes(k, D, fmt)] and `rows` int32 [n_slots], the valid rows of
+    each slot (zeros before the first cache_write), for sketches of up to k rows of D
+    values.  fmt: "fp8" or "fp4"."""
+    data: Any
+    rows: Any
+    k: int
+    D: int
+    fmt: str
+
+
+def cache_slot_bytes(k: int, D: int, fmt: str) -> int:
+    """Bytes of one slot of a cache for sketches of up to k rows of D values."""
+    return int(lib().sa_cache_slot_bytes(k, D, _cache_format(fmt)))
+
+
+def sketch_cache(n_slots: int, k: int, D: int, fmt: str = "fp8", device="cuda") -> SketchCache:
+    """An empty cache of n_slots slots on `device`."""
+    import torch
+    nbytes = cache_slot_bytes(k, D, fmt)
+    if nbytes == 0:
+        raise SAError(1, lib().sa_last_error().decode())
+    return SketchCache(torch.empty((n_slots, nbytes), dtype=torch.uint8, device=device),
+                       torch.zeros(n_slots, dtype=torch.int32, device=device), k, D, fmt)
+
+
+def _cache_format(fmt) -> int:
+    if fmt not in CACHE_FORMATS:
+        raise SAError(1, f"cache format {fmt!r}, expected one of {tuple(CACHE_FORMATS)}")
+    return CACHE_FORMATS[fmt]
+
+
+def _cache_args(cache: SketchCache, slots):
+    """(device, format code, n_slots, B) of a cache and the slots of a batch."""
+    import torch
+    code = _cache_format(cache.fmt)
+    dev = cache.data.device
+    if dev.type != "cuda":
+        raise SAError(1, f"the cache is on {dev}, expected a GPU")
+    n_slots = cache.data.shape[0]
+    _require(cache.data, "cache.data", (n_slots, cache_slot_bytes(cache.k, cache.D, cache.fmt)), torch.uint8, dev)
+    _require(cache.rows, "cache.rows", (n_slots,), torch.int32, dev)
+    if slots.dim() != 1:
+        raise SAError(1, f"slots has shape {tuple(slots.shape)}, expected one dimension")
+    _require(slots, "slots", slots.shape, torch.int64, dev)
+    return dev, code, n_slots, slots.shape[0]
+
+
+def _on_device(workspace, device):
+    """A workspace of the caller's (None: the call allocates one)."""
+    if workspace is not None and (workspace.device != device or not workspace.is_contiguous()):
+        raise SAError(3, f"the workspace must be contiguous on {device}")
+    return workspace
+
+
+class _on:
+    """The tensors' device and, where given, the caller's stream as the current ones, so
+    that what a call allocates belongs to the stream that it runs on."""
+
+    def __init__(self, device, stream):
+        import torch
+        self.ctx = torch.cuda.device(device) if stream is None else torch.cuda.stream(stream)
+
+    def __enter__(self):
+        self.ctx.__enter__()
+
+    def __exit__(self, *exc):
+        return self.ctx.__exit__(*exc)
+
+
+def cache_write(cache: SketchCache, Xs, slots, rows=None, stream=None) -> None:
+    """sa_cache_write on torch tensors: sketches Xs [B,k,D] (bf16 or fp32) into the slots
+    [B] int64 of the cache; rows [B] int32 are their valid rows (None: all k)."""
+    import torch
+    dev, fmt, n_slots, B = _cache_args(cache, slots)
+    code = _dtype_code(Xs)
+    _require(Xs, "Xs", (B, cache.k, cache.D), Xs.dtype, dev)
+    if rows is not None:
+        _require(rows, "rows", (B,), torch.int32, dev)
+    with _on(dev, stream):
+        rc = lib().sa_cache_write(_ptr(Xs), code, _ptr(slots), _ptr(rows), B, cache.k, cache.D, fmt, _ptr(cache.data),
+                                  _ptr(cache.rows), n_slots, _stream_handle(stream))
+    _check(rc)
+
+
+def cache_read(cache: SketchCache, slots, dtype=None, out=None, stream=None):
+    """sa_cache_read on torch tensors: [B,k,D] in `dtype` (or out's; bf16 by default) of
+    the slots [B], zeros past each one's rows and for slots outside the cache."""
+    import torch
+    dev, fmt, n_slots, B = _cache_args(cache, slots)
+    if dtype is None:
+        dtype = torch.bfloat16 if out is None else out.dtype
+    with _on(dev, stream):
+        if out is None:
+            out = torch.empty((B, cache.k, cache.D), dtype=dtype, device=dev)
+        _require(out, "out", (B, cache.k, cache.D), dtype, dev)
+        rc = lib().sa_cache_read(_ptr(cache.data), _ptr(cache.rows), n_slots, _ptr(slots), B, cache.k, cache.D, fmt,
+                                 _ptr(out), _dtype_code(out), _stream_handle(stream))
+    _check(rc)
+    return out
+
+
+def stca_cached_fwd_workspace_size(B, R, k, D, h, dtype_code) -> int:
+    return int(lib().sa_stca_cached_fwd_workspace_size(B, R, k, D, h, dtype_code))
+
+
+def stca_cached_bwd_workspace_size(B, R, k, D, h, dtype_code) -> int:
+    return int(lib().sa_stca_cached_bwd_workspace_size(B, R, k, D, h, dtype_code))
+
+
+def _cached_check(cache, slots, q, Wq, Wk, Wv):
+    dev, fmt, n_slots, B = _cache_args(cache, slots)
+    if q.dim() != 3:
+        raise SAError(1, f"q has shape {tuple(q.shape)}, expected [B, R, D]")
+    R, D, dt = q.shape[1], cache.D, q.dtype
+    _require(q, "q", (B, R, D), dt, dev)
+    for name, W in (("Wq", Wq), ("Wk", Wk), ("Wv", Wv)):
+        _require(W, name, (D, D), dt, dev)
+    return dev, fmt, n_slots, B, R, _dtype_code(q)
+
+
+def stca_cached_fwd(cache: SketchCache, slots, q, Wq, Wk, Wv, h: int, scale: Optional[float] = None, out=None,
+                    out_dtype=None, want_lse: bool = False, workspace=None, stream=None):
+    """sa_stca_cached_fwd on torch tensors: stca_fwd with each user's sketch read from its
+    slot [B] int64 of the cache.  Returns (out [B,R,D] in out_dtype (or out's; fp32 by
+    default), lse [B,R,h] or None)."""
+    import torch
+    dev, fmt, n_slots, B, R, code = _cached_check(cache, slots, q, Wq, Wk, Wv)
+    k, D = cache.k, cache.D
+    if h < 1:
+        raise SAError(1, f"h is {h}, expected at least 1")
+    if scale is None:
+        scale = 1.0 / math.sqrt(max(D // h, 1))
+    if out_dtype is None:
+        out_dtype = torch.float32 if out is None else out.dtype
+    with _on(dev, stream):
+        if out is None:
+            out = torch.empty((B, R, D), dtype=out_dtype, device=dev)
+        _require(out, "out", (B, R, D), out_dtype, dev)
+        lse = torch.empty((B, R, h), dtype=torch.float32, device=dev) if want_lse else None
+        ws, nbytes = _workspace(stca_cached_fwd_workspace_size(B, R, k, D, h, code), dev,
+                                _on_device(workspace, dev))
+        rc = lib().sa_stca_cached_fwd(_ptr(cache.data), _ptr(cache.rows), n_slots, _ptr(slots), fmt, _ptr(q), _ptr(Wq),
+                                      _ptr(Wk), _ptr(Wv), B, R, k, D, h, float(scale), code, _ptr(out),
+                                      _dtype_code(out), _ptr(lse), _ptr(ws), nbytes, _stream_handle(stream))
+    _check(rc)
+    return out, lse
+
+
+def stca_cached_bwd(cache: SketchCache, slots, q, Wq, Wk, Wv, h: int, dout, scale: Optional[float] = None,
+                    workspace=None, stream=None):
+    """sa_stca_cached_bwd on torch tensors: dict of the gradients dq, dWq, dWk, dWv in
+    dout's dtype (the cached sketches are constants)."""
+    import torch
+    dev, fmt, n_slots, B, R, code = _cached_check(cache, slots, q, Wq, Wk, Wv)
+    k, D = cache.k, cache.D
+    _require(dout, "dout", (B, R, D), dout.dtype, dev)
+    if h < 1:
+        raise SAError(1, f"h is {h}, expected at least 1")
+    if scale is None:
+        scale = 1.0 / math.sqrt(max(D // h, 1))
+    with _on(dev, stream):
+        gdt = dict(dtype=dout.dtype, device=dev)
+        g = {"dq": torch.empty((B, R, D), **gdt), "dWq": torch.empty((D, D), **gdt),
+             "dWk": torch.empty((D, D), **gdt), "dWv": torch.empty((D, D), **gdt)}
+        ws, nbytes = _workspace(stca_cached_bwd_workspace_size(B, R, k, D, h, code), dev,
+                                _on_device(workspace, dev))
+        rc = lib().sa_stca_cached_bwd(_ptr(cache.data), _ptr(cache.rows), n_slots, _ptr(slots), fmt, _ptr(q), _ptr(Wq),
+                                      _ptr(Wk), _ptr(Wv), B, R, k, D, h, float(scale), code, _ptr(dout),
+                                      _ptr(g["dq"]), _ptr(g["dWq"]), _ptr(g["dWk"]), _ptr(g["dWv"]),
+                                      _dtype_code(dout), _ptr(ws), nbytes, _stream_handle(stream))
     _check(rc)
     return g
 
