@@ -664,12 +664,15 @@ sa::CacheView cache_view(const void* cache, const int32_t* rows, const int64_t* 
     return c;
 }
 
-// STCA over cached sketches in separate products: [Xd | Qp | U | S (fp32) | alpha | C |
-// lse (fp32) | (bwd) dout in the operand dtype | dC | dalpha (fp32) | ds | dU | dQp];
-// Xd [B,k,D] are the sketches read from the cache, the rest as in StcaPlan.
+// STCA over cached sketches.  fused: the attention in one kernel, [Qp | U | C | lse
+// (fp32) | partial results of split keys].  Otherwise in separate products: [Xd | Qp | U
+// | S (fp32) | alpha | C | lse (fp32) | (bwd) dout in the operand dtype | dC | dalpha
+// (fp32) | ds | dU | dQp]; Xd [B,k,D] are the sketches read from the cache, the rest as
+// in StcaPlan.
 struct CachedPlan {
-    size_t off_xd = 0, off_qp = 0, off_u = 0, off_s = 0, off_al = 0, off_c = 0, off_lse = 0, off_dob = 0, off_dc = 0,
-           off_da = 0, off_ds = 0, off_du = 0, off_dqp = 0, total = 0;
+    bool fused = false;
+    size_t off_xd = 0, off_qp = 0, off_u = 0, off_s = 0, off_al = 0, off_c = 0, off_lse = 0, off_part = 0, off_dob = 0,
+           off_dc = 0, off_da = 0, off_ds = 0, off_du = 0, off_dqp = 0, total = 0;
 };
 
 CachedPlan plan_cached(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa_dtype dtype, bool bwd) {
@@ -682,13 +685,18 @@ CachedPlan plan_cached(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa
     };
     const size_t el = dtype == SA_BF16 ? 2 : 4;
     const size_t BR = (size_t)B * R, rows = BR * h;
-    p.off_xd = carve(el * B * k * D);
+    p.fused = dtype == SA_BF16 && sa::cached_attn_supported(D) && !bwd;
     p.off_qp = carve(el * BR * D);
     p.off_u = carve(el * rows * D);
-    p.off_s = carve(4 * rows * k);
-    p.off_al = carve(el * rows * k);
     p.off_c = carve(el * rows * D);
     p.off_lse = carve(4 * rows);
+    if (p.fused) {
+        p.off_part = carve(sa::cached_attn_workspace(B, R * h, k, D));
+    } else {
+        p.off_xd = carve(el * B * k * D);
+        p.off_s = carve(4 * rows * k);
+        p.off_al = carve(el * rows * k);
+    }
     if (bwd) {
         p.off_dob = carve(dtype == SA_BF16 ? el * BR * D : 0);
         p.off_dc = carve(el * rows * D);
@@ -718,8 +726,8 @@ sa_status cached_attention(const CachedArgs& a, float* lse, uint8_t* ws, const C
     const int64_t kD = (int64_t)k * D, RhD = (int64_t)Rh * D, Rhk = (int64_t)Rh * k;
     void *Xd = ws + p.off_xd, *Qp = ws + p.off_qp, *U = ws + p.off_u, *Al = ws + p.off_al, *Cc = ws + p.off_c;
     float* S = reinterpret_cast<float*>(ws + p.off_s);
-    hipError_t e;
-    {
+    hipError_t e = hipSuccess;
+    if (!p.fused) {
         sa::ProfScope ps("cached_read", stream);
         e = sa::launch_cache_read(a.cache, a.bits, Xd, bf, a.B, stream);
     }
@@ -729,6 +737,15 @@ sa_status cached_attention(const CachedArgs& a, float* lse, uint8_t* ws, const C
         if (e == hipSuccess)
             e = sa::launch_gemm({Qp, bf, dh, D, 1, a.Wk, bf, dh, 1, D, U, bf, D, (int64_t)a.h * D, BR, D, dh, a.h, 1.f,
                                  false}, stream);
+    }
+    if (p.fused) {
+        if (e == hipSuccess) {
+            sa::ProfScope ps("cached_attention", stream);
+            e = sa::launch_cached_attn(a.cache, a.bits, reinterpret_cast<const uint16_t*>(U),
+                                       reinterpret_cast<uint16_t*>(Cc), lse, ws + p.off_part, a.B, Rh, a.scale, stream);
+        }
+        if (e != hipSuccess) return hip_fail(e, "cached STCA launch");
+        return SA_OK;
     }
     if (e == hipSuccess) {
         sa::ProfScope ps("cached_logits", stream);

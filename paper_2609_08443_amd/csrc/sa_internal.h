@@ -224,6 +224,12 @@ hipError_t launch_cache_write(const CacheView& c, int bits, const void* Xs, bool
                               hipStream_t stream);
 // out [B][k][D]; zeros past a slot's rows
 hipError_t launch_cache_read(const CacheView& c, int bits, void* out, bool bf16, int64_t B, hipStream_t stream);
+// bf16 attention of N rows U [B][N][D] a user over its cached rows: C [B][N][D] bf16 and
+// lse [B][N]; part: cached_attn_workspace bytes (cached_attn.hip)
+bool cached_attn_supported(int32_t D);
+size_t cached_attn_workspace(int64_t B, int32_t N, int32_t k, int32_t D);
+hipError_t launch_cached_attn(const CacheView& c, int bits, const uint16_t* U, uint16_t* C, float* lse, void* part,
+                              int64_t B, int32_t N, float scale, hipStream_t stream);
 // softmax rows over each user's valid rows (rows = B Rh of k fp32 logits) and its backward
 hipError_t launch_cached_softmax(const CacheView& c, const float* S, int64_t rows, int32_t Rh, bool bf16, void* alpha,
                                  float* lse, hipStream_t stream);
