@@ -671,6 +671,7 @@ sa::CacheView cache_view(const void* cache, const int32_t* rows, const int64_t* 
 // in StcaPlan.
 struct CachedPlan {
     bool fused = false;
+    bool heads = false;   // fused with the projections around it: [Qp | lse]
     size_t off_xd = 0, off_qp = 0, off_u = 0, off_s = 0, off_al = 0, off_c = 0, off_lse = 0, off_part = 0, off_dob = 0,
            off_dc = 0, off_da = 0, off_ds = 0, off_du = 0, off_dqp = 0, total = 0;
 };
@@ -686,10 +687,15 @@ CachedPlan plan_cached(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa
     const size_t el = dtype == SA_BF16 ? 2 : 4;
     const size_t BR = (size_t)B * R, rows = BR * h;
     p.fused = dtype == SA_BF16 && sa::cached_attn_supported(D) && !bwd;
+    p.heads = p.fused && sa::cached_heads_supported(B, R, h, k, D);
     p.off_qp = carve(el * BR * D);
+    p.off_lse = carve(4 * rows);
+    if (p.heads) {
+        p.total = off;
+        return p;
+    }
     p.off_u = carve(el * rows * D);
     p.off_c = carve(el * rows * D);
-    p.off_lse = carve(4 * rows);
     if (p.fused) {
         p.off_part = carve(sa::cached_attn_workspace(B, R * h, k, D));
     } else {
@@ -1775,9 +1781,26 @@ sa_status sa_stca_cached_fwd(const void* cache, const int32_t* cache_rows, int64
     if (!aligned16(workspace)) return fail(SA_ERR_WORKSPACE, "workspace must be 16-byte aligned");
     uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
     hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
-    st = cached_attention(a, lse ? lse : reinterpret_cast<float*>(ws + p.off_lse), ws, p, stream);
-    if (st != SA_OK) return st;
     const int32_t BR = (int32_t)(B * R), dh = D / h;
+    if (!lse) lse = reinterpret_cast<float*>(ws + p.off_lse);
+    if (p.heads) {
+        uint16_t* Qp = reinterpret_cast<uint16_t*>(ws + p.off_qp);
+        hipError_t e;
+        {
+            sa::ProfScope ps("cached_query_proj", stream);
+            e = sa::launch_gemm({q, bf, 0, D, 1, Wq, bf, 0, D, 1, Qp, bf, 0, D, BR, D, D, 1, 1.f, false}, stream);
+        }
+        if (e == hipSuccess) {
+            sa::ProfScope ps("cached_heads", stream);
+            e = sa::launch_cached_heads(a.cache, a.bits, Qp, reinterpret_cast<const uint16_t*>(Wk),
+                                        reinterpret_cast<const uint16_t*>(Wv), out, out_dtype == SA_BF16, lse, B, R, h,
+                                        scale, stream);
+        }
+        if (e != hipSuccess) return hip_fail(e, "cached STCA launch");
+        return SA_OK;
+    }
+    st = cached_attention(a, lse, ws, p, stream);
+    if (st != SA_OK) return st;
     sa::ProfScope ps("cached_value_proj", stream);   // out[., head i] = C[., i] W_V^(i)
     hipError_t e = sa::launch_gemm({ws + p.off_c, bf, D, (int64_t)h * D, 1, Wv, bf, dh, D, 1, out, out_dtype == SA_BF16,
                                     dh, D, BR, dh, D, h, 1.f, false}, stream);

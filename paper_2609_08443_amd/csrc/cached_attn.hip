@@ -44,15 +44,29 @@ struct AttnArgs {
     int64_t B;
     int32_t N, row_tiles, splits, split_keys;   // split_keys a multiple of 32
     float scale2;        // scale log2(e)
+    // whole heads: the projections around the attention, too
+    const uint16_t *Qp, *Wk, *Wv;   // q W_Q [B][R][D]; [D][D]
+    void* out;                      // [B][R][D], bf16 or fp32
+    bool out_bf16;
+    int32_t R, h, dh;               // dh a multiple of 32; N = R h, row_tiles tiles of targets a head
 };
 
 // keys of a chunk: KT tiles of 16 a wave
 constexpr int chunk_keys(int KT, int waves) { return 16 * KT * waves; }
 
+// [rows u | weights (LOOP; else over the rows u) | maxima and sums of the waves | scales of the
+// waves' keys (HEADS: before them, 64 values of the targets)]
 template <int RM, int KT, bool LOOP>
-constexpr int lds_bytes(int waves) {
+constexpr int lds_tiles(int waves) {
     const int u = 16 * RM * 128 * waves * 2, p = 16 * RM * chunk_keys(KT, waves) * 2;
-    return (LOOP ? u + p : (u > p ? u : p)) + 16 * RM * 4 * 2 * waves;
+    return LOOP ? u + p : (u > p ? u : p);
+}
+// An octet of rows' scales in a wave's copy in LDS, padded so that octets lie in different banks
+constexpr int scale_stride(int waves) { return 4 * waves * 8 + 8; }
+template <int RM, int KT, bool LOOP, bool HEADS>
+constexpr int lds_bytes(int waves) {
+    const int s = waves * 8 * scale_stride(waves), t = HEADS ? 16 * RM * 64 * 2 : 0;
+    return lds_tiles<RM, KT, LOOP>(waves) + 16 * RM * 4 * 2 * waves + (s > t ? s : t);
 }
 
 // 16-byte chunk c of row r of an LDS tile of rows of `chunks` chunks (a multiple of 8):
@@ -84,73 +98,255 @@ __device__ inline void load_block(Block<BITS>& b, const uint8_t* codes, const ui
     b.s = *reinterpret_cast<const uint2*>(scales + sat);
 }
 
-// Logits of NT tiles of 16 keys (tile t at keys kb + t kstep) against the 16 RM rows u in LDS.
-// The next GB groups' codes are on their way while this batch's are multiplied.
-template <int BITS, int RM, int NT, int KT>
-__device__ inline void logits(const AttnArgs& a, const uint8_t* codes, const uint8_t* scales, const uint16_t* Ul, int chunks,
-                              int kb, int kstep, int last, int lane, f32x4 (&S)[KT][RM]) {
-    constexpr int kRegs = RM >= 2 && (RM == 2 || BITS == 8) ? 8 : 16;
-    constexpr int GB = kRegs / NT > 0 ? kRegs / NT : 1;
-    constexpr int W = BITS / 4;
+// Logits of NT tiles of 16 keys from kb on against the 16 RM rows u in LDS, into S[T0 ..].
+// The load path takes four lanes at a time and 64 bytes that lie together in one go:
+// NT = 4, 64 keys: lane l16's keys are 32 j + 2 l16 and the next, in tiles 2 j and 2 j + 1, so
+// that four lanes read one block of 8 rows x 8 values (with one key a lane, four lanes' rows,
+// it was the load path that bound this loop; with four keys a lane, whose octets lie apart,
+// more so), and the scales come through LDS, 256 bytes a row octet copied by the wave
+// beforehand.  A lane's results S[T0 + 2 j + s][.][i] are keys 32 j + 8 q + 2 i + s.
+// NT = 1: 16 keys, lane l16's the l16-th, results 4 q + i.
+// The codes of the next GB groups are on their way while a group is multiplied.  The
+// groups run to the end of the rows u in LDS (a multiple of 128 columns), which hold zeros
+// from 32 G on; the codes read there are the last group's.  Octets past the slot's last
+// valid one, olast, read that one.
+template <int BITS, int RM, int T0, int NT, int KT>
+__device__ __forceinline__ void logits(const AttnArgs& a, const uint8_t* codes, const uint8_t* scales, const uint16_t* Ul,
+                                       uint8_t* Sl, int chunks, int kb, int olast, int first, int lane, f32x4 (&S)[KT][RM]) {
+    static_assert(NT == 1 || NT == 4, "one key a lane, or four");
+    constexpr int GB = NT == 1 ? 16 : 4;
+    constexpr int NJ = NT == 1 ? 1 : 2;             // loads a group
+    constexpr int W = (NT == 1 ? 1 : 2) * BITS / 4;  // words of a load
     const int l16 = lane & 15, q = lane >> 4;
-    const int G = a.c.G;
-    uint32_t at[NT], sat[NT];
+    const int G = a.c.G, Gp = chunks / 4, stride = 8 * Gp + 8;
+    uint32_t at[NJ];
+    uint32_t sat = 0;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int key = min(kb + t * kstep + l16, last);   // rows past the last read that one
-        const uint32_t og = (uint32_t)(key >> 3) * (uint32_t)G;
-        at[t] = (og * 4 + q) * (8 * BITS) + (key & 7) * BITS;
-        sat[t] = og * 8 + (key & 7);
-#pragma unroll
-        for (int rm = 0; rm < RM; ++rm) S[t][rm] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < NJ; ++j) {
+        const int key = kb + (NT == 1 ? l16 : 32 * j + 2 * l16);
+        const uint32_t og = (uint32_t)min(key >> 3, olast) * (uint32_t)G;
+        at[j] = (og * 4 + q) * (8 * BITS) + (key & 7) * BITS;
+        if (NT == 1) sat = og * 8 + (key & 7);
     }
-    uint32_t w[2][GB][NT][W], sc[2][GB][NT];
-    auto fetch = [&](int buf, int g0) {
+    if constexpr (NT == 4) {
+        const int o = lane >> 3;
+        const uint8_t* from = scales + (uint32_t)min((kb >> 3) + o, olast) * (uint32_t)G * 8;
+        for (int g = lane & 7; g < G; g += 8)
+            *reinterpret_cast<uint2*>(Sl + o * stride + 8 * g) = *reinterpret_cast<const uint2*>(from + 8 * g);
+        tile::wave_lds_order();
+    }
+    const uint8_t* const sl = Sl + (l16 >> 2) * stride + 2 * (l16 & 3);
 #pragma unroll
-        for (int i = 0; i < GB; ++i) {
-            const uint32_t g = (uint32_t)min(g0 + i, G - 1);
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const uint8_t* p = codes + at[t] + g * (32 * BITS);
-                if constexpr (BITS == 4) {
-                    w[buf][i][t][0] = *reinterpret_cast<const uint32_t*>(p);
-                } else {
-                    const uint2 v = *reinterpret_cast<const uint2*>(p);
-                    w[buf][i][t][0] = v.x;
-                    w[buf][i][t][1] = v.y;
-                }
-                sc[buf][i][t] = scales[sat[t] + g * 8];
+        for (int rm = 0; rm < RM; ++rm) S[T0 + t][rm] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    uint32_t w[GB][NJ][W], sc[GB];
+    auto fetch = [&](int i, int g_) {
+        const uint32_t g = (uint32_t)min(g_ < Gp ? g_ : g_ - Gp, G - 1);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const uint8_t* p = codes + (at[j] + g * (32 * BITS));
+            if constexpr (W == 4) {
+                const uint4 v = *reinterpret_cast<const uint4*>(p);
+                w[i][j][0] = v.x; w[i][j][1] = v.y; w[i][j][2 % W] = v.z; w[i][j][3 % W] = v.w;
+            } else if constexpr (W == 2) {
+                const uint2 v = *reinterpret_cast<const uint2*>(p);
+                w[i][j][0] = v.x;
+                w[i][j][1 % W] = v.y;
+            } else {
+                w[i][j][0] = *reinterpret_cast<const uint32_t*>(p);
+            }
+        }
+        if constexpr (NT == 1) sc[i] = scales[sat + g * 8];
+    };
+    // the lane's chunk of row l16 in groups of even and odd number; two groups on, 128 bytes
+    const uint16_t* const u0 = Ul + at16(l16, q, chunks);
+    const uint16_t* const u1 = Ul + at16(l16, 4 + q, chunks);
+    auto multiply = [&](int i, int g) {
+        if (g >= Gp) g -= Gp;
+        bf16x8 u[RM];
+#pragma unroll
+        for (int rm = 0; rm < RM; ++rm)
+            u[rm] = tile::lds_b128((i & 1) ? u1 : u0, rm * 16 * chunks * 8 + (g >> 1) * 64);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            uint32_t s2;
+            if constexpr (NT == 1) s2 = sc[i];
+            else s2 = *reinterpret_cast<const uint16_t*>(sl + j * 4 * stride + 8 * min(g, G - 1));
+#pragma unroll
+            for (int t = 0; t < NT / NJ; ++t) {
+                uint32_t c[BITS / 4];
+#pragma unroll
+                for (int x = 0; x < BITS / 4; ++x) c[x] = w[i][j][t * (BITS / 4) + x];
+                const bf16x8 x = __builtin_bit_cast(bf16x8, decode8<BITS>(c, scale_float((s2 >> (8 * t)) & 255u)));
+#pragma unroll
+                for (int rm = 0; rm < RM; ++rm)
+                    S[T0 + 2 * j + t][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, u[rm], S[T0 + 2 * j + t][rm], 0, 0, 0);
             }
         }
     };
-    auto multiply = [&](int buf, int g0) {
+#pragma unroll
+    for (int i = 0; i < GB; ++i) fetch(i, first + i);
+    int g0 = 0;
+    for (; g0 + GB <= Gp; g0 += GB) {
 #pragma unroll
         for (int i = 0; i < GB; ++i) {
-            if (g0 + i >= G) return;
-            bf16x8 u[RM];
+            multiply(i, first + g0 + i);
+            const int next = g0 + GB + i;
+            fetch(i, first + (next < Gp ? next : 0));
+        }
+    }
+    if constexpr (GB > 4) {   // (Gp is a multiple of 4)
 #pragma unroll
-            for (int rm = 0; rm < RM; ++rm) u[rm] = tile::lds_b128(Ul, at16(rm * 16 + l16, (g0 + i) * 4 + q, chunks));
+        for (int i = 0; i < GB; ++i)
+            if (g0 + i < Gp) multiply(i, first + g0 + i);
+    }
+}
+
+// Rows u of one head's targets into LDS: U = Qp_i W_K^(i)T, a wave its 128 columns.  Columns
+// of u are the result's rows, so that a lane writes four neighbouring ones.  The targets'
+// 64 values at a time come through LDS once for all waves (each wave loading them for
+// itself, in rows of 64 bytes, took as long as W_K); W_K's loads are all on their way by then.
+template <int RM>
+__device__ __forceinline__ void project_rows(const uint16_t* Qp, const uint16_t* Wk, int D, int dh, int rows, int wave,
+                                             int lane, uint16_t* Ul, int chunks, uint16_t* Ql) {
+    const int l16 = lane & 15, q = lane >> 4;
+    f32x4 u[8][RM];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const bf16x8 x = __builtin_bit_cast(bf16x8, decode8<BITS>(w[buf][i][t], scale_float(sc[buf][i][t])));
+    for (int e = 0; e < 8; ++e)
 #pragma unroll
-                for (int rm = 0; rm < RM; ++rm)
-                    S[t][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, u[rm], S[t][rm], 0, 0, 0);
-            }
+        for (int rm = 0; rm < RM; ++rm) u[e][rm] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < dh; k += 64) {
+        const bool two = k + 32 < dh;   // (a width that ends at 32 multiplies zeros there)
+        bf16x8 w[2][8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            // columns past D (zeros below) read the last's; D D values are counted in 32 bits
+            const uint16_t* wk = Wk + (uint32_t)(min(128 * wave + 16 * e + l16, D - 1) * D + 8 * q + k);
+            w[0][e] = tile::lds_b128(wk, 0);
+            w[1][e] = two ? tile::lds_b128(wk, 32) : (bf16x8){};
+        }
+        if (k) __syncthreads();   // the last 64 have been read
+        for (int i = threadIdx.x; i < 16 * RM * 8; i += blockDim.x) {
+            const int r = i >> 3, c = i & 7;
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (k + 8 * c < dh) v = *reinterpret_cast<const uint4*>(Qp + (int64_t)min(r, rows - 1) * D + k + 8 * c);
+            *reinterpret_cast<uint4*>(Ql + at16(r, c, 8)) = v;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            bf16x8 x[RM];
+#pragma unroll
+            for (int rm = 0; rm < RM; ++rm) x[rm] = tile::lds_b128(Ql, at16(rm * 16 + l16, 4 * i + q, 8));
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int rm = 0; rm < RM; ++rm) u[e][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[i][e], x[rm], u[e][rm], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int rm = 0; rm < RM; ++rm)
+            *reinterpret_cast<uint2*>(Ul + at16(rm * 16 + l16, 16 * wave + 2 * e + (q >> 1), chunks) + 4 * (q & 1)) =
+                128 * wave + 16 * e + 4 * q < D
+                    ? make_uint2(tile::pack_bf16x2(u[e][rm][0], u[e][rm][1]), tile::pack_bf16x2(u[e][rm][2], u[e][rm][3]))
+                    : make_uint2(0u, 0u);
+}
+
+// out = c W of one head, c [16 RM][128 waves] in accumulators (rows rm 16 + 4 q + i, columns
+// 8 (16 wave + l16) + j): each wave multiplies its own 128 columns of c, through its own part
+// of LDS into operand order, with their rows of W [D][dh of D], 64 columns of out at a time;
+// the waves' sums meet in LDS.  W's operands are blocks of 8 rows x 4 columns, paired by byte
+// permutes as the codes are.  All waves have left LDS before.
+template <int RM>
+__device__ __forceinline__ void project_out(const AttnArgs& a, const f32x4 (&acc)[8][RM], const float (&inv)[RM][4],
+                                   const uint16_t* W, int rows, int64_t row0, int head, int waves, int wave, int lane,
+                                   uint16_t* lds) {
+    const int l16 = lane & 15, q = lane >> 4, D = a.c.D;
+    uint16_t* const mine = lds + wave * (16 * RM * 128);
+    const bool in = 8 * (16 * wave + l16) < D;
+    // two 32-row steps of W ahead, the first two before c is turned (W's bytes from its head's
+    // first column on are counted in 32 bits: D is at most 1024)
+    uint2 w[2][8];
+    auto fetch = [&](int k, int j0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {   // (rows past D meet c's zero columns; the last one's values are as good as any)
+            const uint32_t at = (uint32_t)(min(128 * wave + 32 * k + 8 * q + e, D - 1) * D + min(j0 + 4 * l16, a.dh - 4));
+            w[k & 1][e] = *reinterpret_cast<const uint2*>(W + at);
         }
     };
     fetch(0, 0);
-    for (int g0 = 0; g0 < G; g0 += 2 * GB) {
-        fetch(1, g0 + GB);
-        multiply(0, g0);
-        if (g0 + GB < G) {
-            fetch(0, g0 + 2 * GB);
-            multiply(1, g0 + GB);
+    fetch(1, 0);
+#pragma unroll
+    for (int rm = 0; rm < RM; ++rm)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = in ? acc[j][rm][i] * inv[rm][i] : 0.f;
+            *reinterpret_cast<uint4*>(mine + at16(rm * 16 + 4 * q + i, l16, 16)) = __builtin_bit_cast(uint4, tile::pack8(v));
+        }
+    tile::wave_lds_order();
+    bf16x8 c[4][RM];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int rm = 0; rm < RM; ++rm) c[k][rm] = tile::lds_b128(mine, at16(rm * 16 + l16, 4 * k + q, 16));
+    tile::wave_lds_order();
+    for (int j0 = 0; j0 < a.dh; j0 += 64) {
+        f32x4 o[4][RM];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int rm = 0; rm < RM; ++rm) o[j][rm] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint2(&x)[8] = w[k & 1];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    p[e] = __builtin_amdgcn_perm(j < 2 ? x[2 * e + 1].x : x[2 * e + 1].y, j < 2 ? x[2 * e].x : x[2 * e].y,
+                                                 (j & 1) ? 0x07060302u : 0x05040100u);
+                const bf16x8 b = __builtin_bit_cast(bf16x8, make_uint4(p[0], p[1], p[2], p[3]));
+#pragma unroll
+                for (int rm = 0; rm < RM; ++rm) o[j][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c[k][rm], b, o[j][rm], 0, 0, 0);
+            }
+            if (k < 2) fetch(k + 2, j0);
+            else if (j0 + 64 < a.dh) fetch(k - 2, j0 + 64);
+        }
+        if (j0) __syncthreads();   // the last 64 columns' sums have been read
+        float* const part = reinterpret_cast<float*>(mine);   // [row][64]
+#pragma unroll
+        for (int rm = 0; rm < RM; ++rm)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<float4*>(part + (rm * 16 + 4 * q + i) * 64 + 4 * l16) =
+                    make_float4(o[0][rm][i], o[1][rm][i], o[2][rm][i], o[3][rm][i]);
+        __syncthreads();
+        for (int i = threadIdx.x; i < rows * 16; i += blockDim.x) {
+            const int r = i >> 4, cc = 4 * (i & 15);
+            if (j0 + cc >= a.dh) continue;
+            const float* from = reinterpret_cast<const float*>(lds) + r * 64 + cc;
+            float4 s = *reinterpret_cast<const float4*>(from);
+            for (int v = 1; v < waves; ++v) {
+                const float4 x = *reinterpret_cast<const float4*>(from + v * (16 * RM * 64));
+                s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+            }
+            const int64_t to = (row0 + r) * D + head * a.dh + j0 + cc;
+            if (a.out_bf16)
+                *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + to) =
+                    make_uint2(tile::pack_bf16x2(s.x, s.y), tile::pack_bf16x2(s.z, s.w));
+            else
+                *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + to) = s;
         }
     }
 }
 
-template <int BITS, int RM, int KT, bool LOOP>
+template <int BITS, int RM, int KT, bool LOOP, bool HEADS>
 __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
     extern __shared__ uint4 smem[];
     const int waves = blockDim.x >> 6, chunks = 16 * waves, KC = chunk_keys(KT, waves);
@@ -158,24 +354,42 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
     const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
     uint16_t* const Ul = reinterpret_cast<uint16_t*>(smem);
     uint16_t* const Pl = LOOP ? Ul + 16 * RM * 128 * waves : Ul;
-    float* const wmax = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(smem) +
-                                                 (lds_bytes<RM, KT, LOOP>(waves) - 16 * RM * 4 * 2 * waves));
+    float* const wmax = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(smem) + lds_tiles<RM, KT, LOOP>(waves));
     float* const wsum = wmax + 16 * RM * waves;      // [wave][row], as wmax
 
-    const int64_t id = tile::xcd_range(blockIdx.x, gridDim.x);
-    const int rt = (int)(id % a.row_tiles);
-    const int sp = (int)(id / a.row_tiles % a.splits);
-    const int64_t b = id / a.row_tiles / a.splits;
+    uint8_t* const Sl = reinterpret_cast<uint8_t*>(wsum + 16 * RM * waves) + wave * 8 * (32 * waves + 8);
+    const uint32_t id = (uint32_t)tile::xcd_range(blockIdx.x, gridDim.x);
+    const int D = a.c.D, N = a.N;
+    int64_t b;
+    int sp = 0, head = 0, row0, rows;   // rows u of this workgroup: from row0 on, of the user or of the head's targets
+    if constexpr (HEADS) {
+        const uint32_t bh = id / (uint32_t)a.row_tiles;
+        row0 = (int)(id - bh * (uint32_t)a.row_tiles) * 16 * RM;
+        b = bh / (uint32_t)a.h;
+        head = (int)(bh - (uint32_t)b * (uint32_t)a.h);
+        rows = min(16 * RM, a.R - row0);
+    } else {
+        const uint32_t bs = id / (uint32_t)a.row_tiles;
+        row0 = (int)(id - bs * (uint32_t)a.row_tiles) * 16 * RM;
+        b = bs / (uint32_t)a.splits;
+        sp = (int)(bs - (uint32_t)b * (uint32_t)a.splits);
+        rows = min(16 * RM, N - row0);
+    }
     int32_t n;
     const uint8_t* const codes = cache_slot(a.c, b, &n);
     const uint8_t* const scales = codes + a.c.scales_at;
-    const int D = a.c.D, N = a.N, row0 = rt * 16 * RM;
     const int k0 = sp * a.split_keys, k1 = min(n, k0 + a.split_keys);
-    const int rows = min(16 * RM, N - row0);
     const int64_t prow = ((int64_t)sp * a.B + b) * N + row0;   // partial results' rows
-    const int64_t urow = b * N + row0;
+    const int64_t urow = HEADS ? b * a.R + row0 : b * N + row0;
     if (k1 <= k0) {
-        if (a.splits > 1) {
+        if constexpr (HEADS) {
+            for (int r = threadIdx.x; r < rows; r += blockDim.x) a.lse[(urow + r) * a.h + head] = -INFINITY;
+            for (int i = threadIdx.x; i < rows * a.dh; i += blockDim.x) {
+                const int64_t to = (urow + i / a.dh) * D + head * a.dh + i % a.dh;
+                if (a.out_bf16) reinterpret_cast<uint16_t*>(a.out)[to] = 0;
+                else reinterpret_cast<float*>(a.out)[to] = 0.f;
+            }
+        } else if (a.splits > 1) {
             for (int r = threadIdx.x; r < rows; r += blockDim.x) a.part_ml[prow + r] = make_float2(-INFINITY, 0.f);
         } else {
             for (int r = threadIdx.x; r < rows; r += blockDim.x) a.lse[urow + r] = -INFINITY;
@@ -184,22 +398,31 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
         return;
     }
 
-    // rows u: chunks of 8 values, zeros past D (the codes there are zeros, but 0 NaN is none);
-    // rows past the last repeat it
-    if (D % 32 == 0) {
-        const int per = D / 8;   // straight into LDS, each lane the chunk that belongs at its place
+    if constexpr (HEADS) {
+        project_rows<RM>(a.Qp + urow * D + head * a.dh, a.Wk + head * a.dh, D, a.dh, rows, wave, lane, Ul, chunks,
+                         reinterpret_cast<uint16_t*>(wsum + 16 * RM * waves));
+    } else if (D % 128 == 0) {
+        // rows u straight into LDS, each lane the chunk that belongs at its place; rows past the
+        // last repeat it
         for (int i = wave * 64; i < 16 * RM * chunks; i += waves * 64) {
             const int r = (i + lane) / chunks, c = ((i + lane) % chunks) ^ (r & 7);
-            tile::load_lds16(a.U + (urow + min(r, rows - 1)) * D + 8 * min(c, per - 1), Ul + (int64_t)i * 8);
+            tile::load_lds16(a.U + (urow + min(r, rows - 1)) * D + 8 * c, Ul + (int64_t)i * 8);
         }
         tile::wait_vmem();
-    } else {
+    } else {   // zeros past D
         for (int i = threadIdx.x; i < 16 * RM * chunks; i += blockDim.x) {
             const int r = i / chunks, c = i % chunks;
             const uint16_t* from = a.U + (urow + min(r, rows - 1)) * D + 8 * c;
             uint32_t v[4] = {0u, 0u, 0u, 0u};
-            for (int j = 0; j < 8; ++j)
-                if (8 * c + j < D) v[j / 2] |= (uint32_t)from[j] << (16 * (j & 1));
+            if (D % 8 == 0) {
+                if (8 * c < D) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(from);
+                    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+                }
+            } else {
+                for (int j = 0; j < 8; ++j)
+                    if (8 * c + j < D) v[j / 2] |= (uint32_t)from[j] << (16 * (j & 1));
+            }
             *reinterpret_cast<uint4*>(Ul + at16(r, c, chunks)) = make_uint4(v[0], v[1], v[2], v[3]);
         }
     }
@@ -220,25 +443,44 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
     for (int c0 = k0; c0 < k1; c0 += KC) {
         const int kend = min(k1, c0 + KC);
         const int nk = (kend - c0 + 31) / 32 * 32;
-        // ---- logits of this wave's key tiles
+        // ---- logits of this wave's keys: wide, up to two runs of 64; or, where that would leave
+        // waves without keys, two of 16
         f32x4 S[KT][RM];
-        const int kb = c0 + 16 * wave, kstep = 16 * waves;
-        const int nt = nk > 16 * wave ? (nk - 16 * wave + kstep - 1) / kstep : 0;
-        if (nt > KT / 2) logits<BITS, RM, KT, KT>(a, codes, scales, Ul, chunks, kb, kstep, n - 1, lane, S);
-        else if (nt > KT / 4) logits<BITS, RM, KT / 2, KT>(a, codes, scales, Ul, chunks, kb, kstep, n - 1, lane, S);
-        else if (nt > 0) logits<BITS, RM, KT / 4, KT>(a, codes, scales, Ul, chunks, kb, kstep, n - 1, lane, S);
-        // ---- softmax: the maximum over the chunk's keys, of all waves
-#pragma unroll
-        for (int rm = 0; rm < RM; ++rm) {
-            float mx = -INFINITY;
+        static_assert(KT == 8, "two runs of four tiles");
+        const bool wide = nk > 32 * waves;
+        const int run = wide ? 64 : 16;
+        const int kb = run * wave, kstep = run * waves;   // in the chunk
+        const int nt = nk > kb ? min((nk - kb + kstep - 1) / kstep, 2) : 0;
+        const int olast = (n - 1) >> 3;
+        // each wave starts at a group of its own: octets of rows lie a power of two of bytes apart
+        // (D = 1024), so that one group of all of them is in one channel of the L2
+        const int first = 2 * (int)((uint32_t)(3 * wave + 5 * id) % (uint32_t)(chunks / 8));
+        if (nt > 0) {
+            if (wide) logits<BITS, RM, 0, 4, KT>(a, codes, scales, Ul, Sl, chunks, c0 + kb, olast, first, lane, S);
+            else logits<BITS, RM, 0, 1, KT>(a, codes, scales, Ul, Sl, chunks, c0 + kb, olast, first, lane, S);
+        }
+        if (nt > 1) {
+            if (wide) logits<BITS, RM, 4, 4, KT>(a, codes, scales, Ul, Sl, chunks, c0 + kb + kstep, olast, first, lane, S);
+            else logits<BITS, RM, 4, 1, KT>(a, codes, scales, Ul, Sl, chunks, c0 + kb + kstep, olast, first, lane, S);
+        }
+        // ---- softmax: the maximum over the chunk's keys, of all waves.  (scale2 > 0: the largest
+        // logit has the largest product.)  Only waves without a full share of keys mask.
+        if (!wide || nt < 2 || c0 + kb + kstep + run > kend) {
 #pragma unroll
             for (int t = 0; t < KT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const bool in = t < nt && kb + t * kstep + 4 * q + i < kend;
-                    S[t][rm][i] = in ? S[t][rm][i] * a.scale2 : -INFINITY;
-                    mx = fmaxf(mx, S[t][rm][i]);
+                    const int key = kb + (t >> 2) * kstep + (wide ? 16 * (t & 2) + 8 * q + 2 * i + (t & 1) : 4 * q + i);
+                    const bool in = (t >> 2) < nt && (wide || (t & 3) == 0) && c0 + key < kend;
+#pragma unroll
+                    for (int rm = 0; rm < RM; ++rm) S[t][rm][i] = in ? S[t][rm][i] : -INFINITY;
                 }
+        }
+#pragma unroll
+        for (int rm = 0; rm < RM; ++rm) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < KT; ++t) mx = fmaxf(fmaxf(fmaxf(mx, S[t][rm][0]), fmaxf(S[t][rm][1], S[t][rm][2])), S[t][rm][3]);
             mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
             if (q == 0) wmax[wave * 16 * RM + rm * 16 + l16] = mx;
@@ -249,23 +491,33 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
         for (int rm = 0; rm < RM; ++rm) {
             float mx = wmax[rm * 16 + l16];
             for (int v = 1; v < waves; ++v) mx = fmaxf(mx, wmax[v * 16 * RM + rm * 16 + l16]);
+            mx *= a.scale2;
             if constexpr (LOOP) mx = fmaxf(mx, m[rm]);
             const float base = mx == -INFINITY ? 0.f : mx;   // (logits that are all -inf)
             if constexpr (LOOP) cor[rm] = exp2f(m[rm] - base);
             m[rm] = mx;
             float sum = 0.f;
 #pragma unroll
-            for (int t = 0; t < KT; ++t) {
-                if (t < nt) {
-                    float p[4];
+            for (int t = 0; t < KT; t += 4) {
+                if ((t >> 2) >= nt) break;
+                float p[4][4];   // [i][tile]
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        p[i] = __builtin_amdgcn_exp2f(S[t][rm][i] - base);
-                        sum += p[i];
-                    }
-                    const int key = 16 * wave + t * kstep + 4 * q;   // in the chunk
-                    *reinterpret_cast<uint2*>(Pl + at16(rm * 16 + l16, key >> 3, KC >> 3) + (key & 7)) =
-                        make_uint2(tile::pack_bf16x2(p[0], p[1]), tile::pack_bf16x2(p[2], p[3]));
+                for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        p[i][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t + j][rm][i], a.scale2, -base));
+                    sum += (p[i][0] + p[i][1]) + (p[i][2] + p[i][3]);
+                }
+                const int c = (kb + (t >> 2) * kstep) >> 3;   // in chunks of 8 keys
+                if (wide) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+                        *reinterpret_cast<uint4*>(Pl + at16(rm * 16 + l16, c + 4 * x + q, KC >> 3)) =
+                            make_uint4(tile::pack_bf16x2(p[0][2 * x], p[0][2 * x + 1]), tile::pack_bf16x2(p[1][2 * x], p[1][2 * x + 1]),
+                                       tile::pack_bf16x2(p[2][2 * x], p[2][2 * x + 1]), tile::pack_bf16x2(p[3][2 * x], p[3][2 * x + 1]));
+                } else {
+                    *reinterpret_cast<uint2*>(Pl + at16(rm * 16 + l16, c + (q >> 1), KC >> 3) + 4 * (q & 1)) =
+                        make_uint2(tile::pack_bf16x2(p[0][0], p[1][0]), tile::pack_bf16x2(p[2][0], p[3][0]));
                 }
             }
             sum += __shfl_xor(sum, 16, 64);
@@ -299,24 +551,23 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
 #pragma unroll
                 for (int rm = 0; rm < RM; ++rm) acc[j][rm] = (f32x4){0.f, 0.f, 0.f, 0.f};
         }
-        const int olast = (n - 1) >> 3;
-        auto place = [&](int kk, uint32_t& at, uint32_t& sat) {
-            const int o = min((c0 >> 3) + kk * 4 + q, olast);
-            const uint32_t og = (uint32_t)o * (uint32_t)a.c.G;
-            at = (og * 4 + dj) * (8 * BITS);
-            sat = (og + (dj >> 2)) * 8;
-            return o;
+        const int steps = nk / 32, tail = steps - 1;
+        // A lane's block of a step lies a fixed number of bytes behind the last step's (the steps
+        // move in scalar registers), but in the last step, where octets past the slot's last one
+        // read that one
+        const uint32_t G = (uint32_t)a.c.G;
+        const int otail = min((c0 >> 3) + 4 * tail + q, (n - 1) >> 3);
+        const uint32_t oq = (uint32_t)((c0 >> 3) + q) * G, ot = (uint32_t)otail * G - (uint32_t)(4 * tail) * G;
+        const uint32_t at0 = (oq * 4 + dj) * (8 * BITS), at1 = (ot * 4 + dj) * (8 * BITS);
+        const uint32_t sat0 = (oq + (dj >> 2)) * 8, sat1 = (ot + (dj >> 2)) * 8;
+        Block<BITS> b0, b1;
+        auto fetch = [&](Block<BITS>& to, int kk) {   // (past the last step: that one, not used)
+            kk = min(kk, tail);
+            const uint32_t at = kk == tail ? at1 : at0, sat = kk == tail ? sat1 : sat0;
+            const uint32_t step = (uint32_t)(4 * kk) * G;
+            load_block<BITS>(to, codes + step * (32 * BITS), scales + step * 8, at, sat);
         };
-        const int steps = nk / 32;
-        Block<BITS> cur, nxt;
-        uint32_t at, sat;
-        int o = place(0, at, sat), onext = o;
-        load_block<BITS>(cur, codes, scales, at, sat);
-        for (int kk = 0; kk < steps; ++kk) {
-            if (kk + 1 < steps) {
-                onext = place(kk + 1, at, sat);
-                load_block<BITS>(nxt, codes, scales, at, sat);
-            }
+        auto multiply = [&](const Block<BITS>& from, int kk) {
             bf16x8 p[RM];
 #pragma unroll
             for (int rm = 0; rm < RM; ++rm) p[rm] = tile::lds_b128(Pl, at16(rm * 16 + l16, kk * 4 + q, KC >> 3));
@@ -324,15 +575,15 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
             float sc[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const uint32_t* words = reinterpret_cast<const uint32_t*>(cur.w);
+                const uint32_t* words = reinterpret_cast<const uint32_t*>(from.w);
 #pragma unroll
                 for (int x = 0; x < BITS / 4; ++x) raw[j][x] = words[j * (BITS / 4) + x];
-                const uint32_t s = j < 4 ? cur.s.x : cur.s.y;
+                const uint32_t s = j < 4 ? from.s.x : from.s.y;
                 sc[j] = scale_float((s >> (8 * (j & 3))) & 255u);
             }
             if (c0 + kk * 32 + 32 > (n & ~7)) {
                 // bytes behind the slot's last row may be anything: their weights are zero, and so are they
-                const int in = n - 8 * o;
+                const int in = n - 8 * otail;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
                     if (j >= in) {
@@ -355,9 +606,16 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
             columns(std::integral_constant<int, 1>{});
             columns(std::integral_constant<int, 2>{});
             columns(std::integral_constant<int, 3>{});
-            cur = nxt;
-            o = onext;
+        };
+        fetch(b0, 0);
+        int kk = 0;
+        for (; kk + 1 < steps; kk += 2) {
+            fetch(b1, kk + 1);
+            multiply(b0, kk);
+            fetch(b0, kk + 2);
+            multiply(b1, kk + 1);
         }
+        if (kk < steps) multiply(b0, kk);
         if constexpr (!LOOP) break;   // all keys are in one chunk
     }
     // ---- results: rows rm 16 + 4 q + i, this lane's columns 8 (16 wave + l16) ..+7
@@ -366,10 +624,21 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
         for (int rm = 0; rm < RM; ++rm) {
             const int r = rm * 16 + l16;
             if (r < rows) {
-                if (a.splits > 1) a.part_ml[prow + r] = make_float2(m[rm], l[rm]);
+                if (HEADS) a.lse[(urow + r) * a.h + head] = (m[rm] + __builtin_amdgcn_logf(l[rm])) * 0.6931471805599453f;
+                else if (a.splits > 1) a.part_ml[prow + r] = make_float2(m[rm], l[rm]);
                 else a.lse[urow + r] = (m[rm] + __builtin_amdgcn_logf(l[rm])) * 0.6931471805599453f;
             }
         }
+    }
+    if constexpr (HEADS) {
+        float inv[RM][4];
+#pragma unroll
+        for (int rm = 0; rm < RM; ++rm)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) inv[rm][i] = 1.f / __shfl(l[rm], 4 * q + i, 64);
+        __syncthreads();   // the weights in LDS have been read
+        project_out<RM>(a, acc, inv, a.Wv + head * a.dh, rows, urow, head, waves, wave, lane, reinterpret_cast<uint16_t*>(smem));
+        return;
     }
     const int col = 8 * (wave * 16 + l16);
 #pragma unroll
@@ -450,14 +719,14 @@ __global__ __launch_bounds__(256) void cached_join_kernel(AttnArgs a) {
     }
 }
 
-template <int BITS, int RM, int KT, bool LOOP>
+template <int BITS, int RM, int KT, bool LOOP, bool HEADS>
 hipError_t launch_instance(const AttnArgs& a, hipStream_t stream) {
     const int waves = (a.c.D + 127) / 128;
-    const int lds = lds_bytes<RM, KT, LOOP>(waves);
-    auto kern = cached_attn_kernel<BITS, RM, KT, LOOP>;
+    const int lds = lds_bytes<RM, KT, LOOP, HEADS>(waves);
+    auto kern = cached_attn_kernel<BITS, RM, KT, LOOP, HEADS>;
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
-    const int64_t blocks = a.B * a.row_tiles * a.splits;
+    const int64_t blocks = a.B * a.row_tiles * (HEADS ? a.h : a.splits);
     hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(64 * waves), lds, stream, a);
     return hipGetLastError();
 }
@@ -487,7 +756,61 @@ AttnPlan attn_plan(int64_t B, int32_t N, int32_t k, int32_t D) {
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
+// Rows u of a workgroup (in 16s) where workgroups take one head's targets, or 0 where
+// they do not.
+int heads_tiles(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
+    if (D % h != 0 || (D / h) % 32 != 0) return 0;
+#ifdef SA_EXPERIMENT
+    if (getenv("SA_H")) return atoi(getenv("SA_H"));
+#endif
+    if (R < 12 || B * h * ((R + 63) / 64) < device_cus() / 2) return 0;
+    const bool one = k <= chunk_keys(8, (D + 127) / 128);
+    int best = 0;
+    int64_t cost = 0;
+    for (int rm = 2; rm <= (one ? 4 : 2); ++rm) {
+        const int64_t wgs = B * h * ((R + 16 * rm - 1) / (16 * rm));
+        const int64_t c = (wgs + device_cus() - 1) / device_cus() * (rm + 1);
+        if (best == 0 || c <= cost) best = rm, cost = c;
+    }
+    return best;
+}
+
 }  // namespace
+
+bool cached_heads_supported(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) { return heads_tiles(B, R, h, k, D) > 0; }
+
+hipError_t launch_cached_heads(const CacheView& c, int bits, const uint16_t* Qp, const uint16_t* Wk, const uint16_t* Wv,
+                               void* out, bool out_bf16, float* lse, int64_t B, int32_t R, int32_t h, float scale,
+                               hipStream_t stream) {
+    const int rm = heads_tiles(B, R, h, c.k, c.D);
+    AttnArgs a{};
+    a.c = c;
+    a.lse = lse;
+    a.B = B;
+    a.N = R * h;
+    a.row_tiles = (R + 16 * rm - 1) / (16 * rm);
+    a.splits = 1;
+    a.split_keys = (c.k + 31) / 32 * 32;
+    a.scale2 = scale * tile::kLog2e;
+    a.Qp = Qp;
+    a.Wk = Wk;
+    a.Wv = Wv;
+    a.out = out;
+    a.out_bf16 = out_bf16;
+    a.R = R;
+    a.h = h;
+    a.dh = c.D / h;
+    if (bits == 4) {
+        if (rm == 2) return launch_instance<4, 2, 8, true, true>(a, stream);
+        if (rm == 3) return launch_instance<4, 3, 8, false, true>(a, stream);
+        if (rm == 4) return launch_instance<4, 4, 8, false, true>(a, stream);
+    } else {
+        if (rm == 2) return launch_instance<8, 2, 8, true, true>(a, stream);
+        if (rm == 3) return launch_instance<8, 3, 8, false, true>(a, stream);
+        if (rm == 4) return launch_instance<8, 4, 8, false, true>(a, stream);
+    }
+    return hipErrorInvalidValue;
+}
 
 bool cached_attn_supported(int32_t D) { return D <= 1024; }
 
@@ -516,13 +839,13 @@ hipError_t launch_cached_attn(const CacheView& c, int bits, const uint16_t* U, u
     a.scale2 = scale * tile::kLog2e;
     hipError_t e = hipErrorInvalidValue;
     if (bits == 4) {
-        if (p.variant == 0) e = launch_instance<4, 1, 8, true>(a, stream);
-        else if (p.variant == 1) e = launch_instance<4, 2, 8, true>(a, stream);
-        else e = launch_instance<4, 4, 8, false>(a, stream);
+        if (p.variant == 0) e = launch_instance<4, 1, 8, true, false>(a, stream);
+        else if (p.variant == 1) e = launch_instance<4, 2, 8, true, false>(a, stream);
+        else e = launch_instance<4, 4, 8, false, false>(a, stream);
     } else {
-        if (p.variant == 0) e = launch_instance<8, 1, 8, true>(a, stream);
-        else if (p.variant == 1) e = launch_instance<8, 2, 8, true>(a, stream);
-        else e = launch_instance<8, 4, 8, false>(a, stream);
+        if (p.variant == 0) e = launch_instance<8, 1, 8, true, false>(a, stream);
+        else if (p.variant == 1) e = launch_instance<8, 2, 8, true, false>(a, stream);
+        else e = launch_instance<8, 4, 8, false, false>(a, stream);
     }
     if (e != hipSuccess || p.splits == 1) return e;
     const int64_t threads = B * N * ((c.D + 7) / 8);

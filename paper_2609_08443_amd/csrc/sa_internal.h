@@ -230,6 +230,12 @@ bool cached_attn_supported(int32_t D);
 size_t cached_attn_workspace(int64_t B, int32_t N, int32_t k, int32_t D);
 hipError_t launch_cached_attn(const CacheView& c, int bits, const uint16_t* U, uint16_t* C, float* lse, void* part,
                               int64_t B, int32_t N, float scale, hipStream_t stream);
+// the same with the projections around it, workgroups taking a head's targets: from Qp = q W_Q
+// [B][R][D] to out [B][R][D] (bf16 or fp32) and lse [B][R][h]
+bool cached_heads_supported(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D);
+hipError_t launch_cached_heads(const CacheView& c, int bits, const uint16_t* Qp, const uint16_t* Wk, const uint16_t* Wv,
+                               void* out, bool out_bf16, float* lse, int64_t B, int32_t R, int32_t h, float scale,
+                               hipStream_t stream);
 // softmax rows over each user's valid rows (rows = B Rh of k fp32 logits) and its backward
 hipError_t launch_cached_softmax(const CacheView& c, const float* S, int64_t rows, int32_t Rh, bool bf16, void* alpha,
                                  float* lse, hipStream_t stream);

@@ -267,6 +267,25 @@ STCA_CASES = [
 ]
 
 
+def many(B, k, empty=True):
+    """Rows and slots of a batch: full and short sketches, some empty, a miss."""
+    g = rng_of(B, k, 5)
+    rows = np.minimum(g.integers(1, 2 * k, B), k)
+    if empty:
+        rows[1::5] = 0
+    slots = g.permutation(B)
+    slots[2] = -1
+    return rows.tolist(), slots.tolist()
+
+
+# batches large enough for workgroups of one head's targets: heads of 32, 64, 96 and 128,
+# one to four 16s of targets, one chunk of keys and several
+HEAD_CASES = [(43, 12, 24, 96, 3), (32, 13, 33, 256, 4), (32, 20, 300, 256, 4), (65, 12, 20, 256, 2),
+              (45, 17, 100, 288, 3), (11, 40, 150, 384, 12), (11, 64, 384, 384, 12), (9, 70, 130, 512, 16),
+              (9, 33, 1030, 1024, 16)]
+STCA_CASES += [c + many(c[0], c[2]) for c in HEAD_CASES]
+
+
 @pytest.mark.parametrize("fmt", ["fp4", "fp8"])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("B,R,k,D,h,rows,slots", STCA_CASES)
