@@ -55,7 +55,7 @@ struct AttnArgs {
 constexpr int chunk_keys(int KT, int waves) { return 16 * KT * waves; }
 
 // [rows u | weights (LOOP; else over the rows u) | maxima and sums of the waves | scales of the
-// waves' keys (HEADS: before them, 64 values of the targets)]
+// waves' keys]; before that (HEADS) [64 values of W_K's rows | of the targets]
 template <int RM, int KT, bool LOOP>
 constexpr int lds_tiles(int waves) {
     const int u = 16 * RM * 128 * waves * 2, p = 16 * RM * chunk_keys(KT, waves) * 2;
@@ -65,8 +65,9 @@ constexpr int lds_tiles(int waves) {
 constexpr int scale_stride(int waves) { return 4 * waves * 8 + 8; }
 template <int RM, int KT, bool LOOP, bool HEADS>
 constexpr int lds_bytes(int waves) {
-    const int s = waves * 8 * scale_stride(waves), t = HEADS ? 16 * RM * 64 * 2 : 0;
-    return lds_tiles<RM, KT, LOOP>(waves) + 16 * RM * 4 * 2 * waves + (s > t ? s : t);
+    const int s = lds_tiles<RM, KT, LOOP>(waves) + 16 * RM * 4 * 2 * waves + waves * 8 * scale_stride(waves);
+    const int t = HEADS ? waves * 128 * 64 * 2 + 16 * RM * 64 * 2 : 0;
+    return s > t ? s : t;
 }
 
 // 16-byte chunk c of row r of an LDS tile of rows of `chunks` chunks (a multiple of 8):
@@ -203,36 +204,40 @@ __device__ __forceinline__ void logits(const AttnArgs& a, const uint8_t* codes, 
     }
 }
 
-// Rows u of one head's targets into LDS: U = Qp_i W_K^(i)T, a wave its 128 columns.  Columns
-// of u are the result's rows, so that a lane writes four neighbouring ones.  The targets'
-// 64 values at a time come through LDS once for all waves (each wave loading them for
-// itself, in rows of 64 bytes, took as long as W_K); W_K's loads are all on their way by then.
+// Rows u of one head's targets into LDS: U = Qp_i W_K^(i)T, a wave its 128 columns, 64 of the
+// head's width at a time.  W_K's rows come through LDS in whole lines, wave by wave in the
+// place that the rows u take afterwards (loaded as operands, 16 rows a load, they took four
+// times the load path's time: 15,000 of 147,000 cycles of a workgroup of 64 rows and 1,024
+// keys), and the targets' values once for all waves.  Columns of u are the result's rows, so
+// that a lane writes four neighbouring ones; those past D are zeros.
 template <int RM>
 __device__ __forceinline__ void project_rows(const uint16_t* Qp, const uint16_t* Wk, int D, int dh, int rows, int wave,
                                              int lane, uint16_t* Ul, int chunks, uint16_t* Ql) {
     const int l16 = lane & 15, q = lane >> 4;
+    uint16_t* const mine = Ul + wave * (128 * 64);
     f32x4 u[8][RM];
 #pragma unroll
     for (int e = 0; e < 8; ++e)
 #pragma unroll
         for (int rm = 0; rm < RM; ++rm) u[e][rm] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    const int r8 = lane >> 3, c8 = lane & 7;
     for (int k = 0; k < dh; k += 64) {
-        const bool two = k + 32 < dh;   // (a width that ends at 32 multiplies zeros there)
-        bf16x8 w[2][8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            // columns past D (zeros below) read the last's; D D values are counted in 32 bits
-            const uint16_t* wk = Wk + (uint32_t)(min(128 * wave + 16 * e + l16, D - 1) * D + 8 * q + k);
-            w[0][e] = tile::lds_b128(wk, 0);
-            w[1][e] = two ? tile::lds_b128(wk, 32) : (bf16x8){};
-        }
+        // (a width that ends at 32 repeats W_K's first 32 there and multiplies them by zeros;
+        // columns past D read the last's; D D values are counted in 32 bits)
         if (k) __syncthreads();   // the last 64 have been read
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int e = 8 * i + r8, c = c8 ^ (e & 7);
+            tile::load_lds16(Wk + (uint32_t)(min(128 * wave + e, D - 1) * D + k + (k + 8 * c < dh ? 8 * c : 8 * c - 32)),
+                             mine + i * 512);
+        }
         for (int i = threadIdx.x; i < 16 * RM * 8; i += blockDim.x) {
             const int r = i >> 3, c = i & 7;
             uint4 v = make_uint4(0u, 0u, 0u, 0u);
             if (k + 8 * c < dh) v = *reinterpret_cast<const uint4*>(Qp + (int64_t)min(r, rows - 1) * D + k + 8 * c);
             *reinterpret_cast<uint4*>(Ql + at16(r, c, 8)) = v;
         }
+        tile::wait_vmem();
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -240,11 +245,14 @@ __device__ __forceinline__ void project_rows(const uint16_t* Qp, const uint16_t*
 #pragma unroll
             for (int rm = 0; rm < RM; ++rm) x[rm] = tile::lds_b128(Ql, at16(rm * 16 + l16, 4 * i + q, 8));
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
+            for (int e = 0; e < 8; ++e) {
+                const bf16x8 w = tile::lds_b128(mine, at16(16 * e + l16, 4 * i + q, 8));
 #pragma unroll
-                for (int rm = 0; rm < RM; ++rm) u[e][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[i][e], x[rm], u[e][rm], 0, 0, 0);
+                for (int rm = 0; rm < RM; ++rm) u[e][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[rm], u[e][rm], 0, 0, 0);
+            }
         }
     }
+    __syncthreads();
 #pragma unroll
     for (int e = 0; e < 8; ++e)
 #pragma unroll
@@ -400,7 +408,7 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
 
     if constexpr (HEADS) {
         project_rows<RM>(a.Qp + urow * D + head * a.dh, a.Wk + head * a.dh, D, a.dh, rows, wave, lane, Ul, chunks,
-                         reinterpret_cast<uint16_t*>(wsum + 16 * RM * waves));
+                         Ul + waves * 128 * 64);
     } else if (D % 128 == 0) {
         // rows u straight into LDS, each lane the chunk that belongs at its place; rows past the
         // last repeat it
