@@ -671,7 +671,7 @@ sa::CacheView cache_view(const void* cache, const int32_t* rows, const int64_t* 
 // in StcaPlan.
 struct CachedPlan {
     bool fused = false;
-    bool heads = false;   // fused with the projections around it: [Qp | lse]
+    bool heads = false;   // fused with the projections around it: [Qp | lse | (bwd) dout in bf16 | C | dU | dQp]
     size_t off_xd = 0, off_qp = 0, off_u = 0, off_s = 0, off_al = 0, off_c = 0, off_lse = 0, off_part = 0, off_dob = 0,
            off_dc = 0, off_da = 0, off_ds = 0, off_du = 0, off_dqp = 0, total = 0;
 };
@@ -687,10 +687,17 @@ CachedPlan plan_cached(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa
     const size_t el = dtype == SA_BF16 ? 2 : 4;
     const size_t BR = (size_t)B * R, rows = BR * h;
     p.fused = dtype == SA_BF16 && sa::cached_attn_supported(D) && !bwd;
-    p.heads = p.fused && sa::cached_heads_supported(B, R, h, k, D);
+    p.heads = dtype == SA_BF16 && (bwd ? sa::cached_heads_bwd_supported(B, R, h, k, D)
+                                       : p.fused && sa::cached_heads_supported(B, R, h, k, D));
     p.off_qp = carve(el * BR * D);
     p.off_lse = carve(4 * rows);
     if (p.heads) {
+        if (bwd) {
+            p.off_dob = carve(el * BR * D);
+            p.off_c = carve(el * rows * D);
+            p.off_du = carve(el * rows * D);
+            p.off_dqp = carve(el * BR * D);
+        }
         p.total = off;
         return p;
     }
@@ -1839,38 +1846,54 @@ sa_status sa_stca_cached_bwd(const void* cache, const int32_t* cache_rows, int64
     uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
     hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
     float* lse = reinterpret_cast<float*>(ws + p.off_lse);
-    st = cached_attention(a, lse, ws, p, stream);   // Qp, U, lse and C once more
-    if (st != SA_OK) return st;
     const int32_t BR = (int32_t)(B * R), dh = D / h;
     const int64_t hD = (int64_t)h * D;
     void *Qp = ws + p.off_qp, *Cc = ws + p.off_c, *dC = ws + p.off_dc, *dU = ws + p.off_du, *dQp = ws + p.off_dqp;
     const void* dob = dout;
     hipError_t e = hipSuccess;
-    {
-        sa::ProfScope ps("cached_value_grads", stream);
-        if (bf && !gb) {
-            dob = ws + p.off_dob;
-            e = sa::launch_to_bf16(reinterpret_cast<const float*>(dout), reinterpret_cast<uint16_t*>(ws + p.off_dob),
-                                   (int64_t)BR * D, stream);
-        }
-        // dC[., i] = dout[., head i] W_V^(i)T;  dW_V^(i) = sum over targets of C[., i]^T dout[., head i]
-        if (e == hipSuccess)
-            e = sa::launch_gemm({dob, bf, dh, D, 1, Wv, bf, dh, 1, D, dC, bf, D, hD, BR, D, dh, h, 1.f, false}, stream);
-        if (e == hipSuccess)
-            e = sa::launch_gemm({Cc, bf, D, 1, hD, dob, bf, dh, D, 1, dWv, gb, dh, D, D, dh, BR, h, 1.f, false}, stream);
+    if (bf && !gb) {
+        sa::ProfScope ps("cached_round_dout", stream);
+        dob = ws + p.off_dob;
+        e = sa::launch_to_bf16(reinterpret_cast<const float*>(dout), reinterpret_cast<uint16_t*>(ws + p.off_dob),
+                               (int64_t)BR * D, stream);
     }
-    if (e != hipSuccess) return hip_fail(e, "cached STCA backward launch");
-    st = cached_attention_bwd(a, lse, ws, p, stream);
-    if (st != SA_OK) return st;
-    {
-        sa::ProfScope ps("cached_query_grads", stream);
-        // dQp[., head i] = dU[., i] W_K^(i);  dW_K^(i) = sum dU[., i]^T Qp[., head i]
-        e = sa::launch_gemm({dU, bf, D, hD, 1, Wk, bf, dh, D, 1, dQp, bf, dh, D, BR, dh, D, h, 1.f, false}, stream);
+    if (p.heads) {   // Qp; C, dU and dQp
+        if (e == hipSuccess) {
+            sa::ProfScope ps("cached_query_proj", stream);
+            e = sa::launch_gemm({q, bf, 0, D, 1, Wq, bf, 0, D, 1, Qp, bf, 0, D, BR, D, D, 1, 1.f, false}, stream);
+        }
+        if (e == hipSuccess) {
+            sa::ProfScope ps("cached_heads_bwd", stream);
+            e = sa::launch_cached_heads_bwd(a.cache, a.bits, reinterpret_cast<const uint16_t*>(Qp),
+                                            reinterpret_cast<const uint16_t*>(dob), reinterpret_cast<const uint16_t*>(Wk),
+                                            reinterpret_cast<const uint16_t*>(Wv), reinterpret_cast<uint16_t*>(Cc),
+                                            reinterpret_cast<uint16_t*>(dU), reinterpret_cast<uint16_t*>(dQp), B, R, h,
+                                            scale, stream);
+        }
+    } else {
+        if (e == hipSuccess) {
+            st = cached_attention(a, lse, ws, p, stream);   // Qp, U, lse and C once more
+            if (st != SA_OK) return st;
+            sa::ProfScope ps("cached_value_side", stream);   // dC[., i] = dout[., head i] W_V^(i)T
+            e = sa::launch_gemm({dob, bf, dh, D, 1, Wv, bf, dh, 1, D, dC, bf, D, hD, BR, D, dh, h, 1.f, false}, stream);
+        }
+        if (e == hipSuccess) {
+            st = cached_attention_bwd(a, lse, ws, p, stream);
+            if (st != SA_OK) return st;
+            sa::ProfScope ps("cached_key_side", stream);   // dQp[., head i] = dU[., i] W_K^(i)
+            e = sa::launch_gemm({dU, bf, D, hD, 1, Wk, bf, dh, D, 1, dQp, bf, dh, D, BR, dh, D, h, 1.f, false}, stream);
+        }
+    }
+    if (e == hipSuccess) {
+        sa::ProfScope ps("cached_weight_grads", stream);
+        // dW_V^(i) = sum over targets of C[., i]^T dout[., head i];  dW_K^(i) = sum dU[., i]^T Qp[., head i]
+        e = sa::launch_gemm({Cc, bf, D, 1, hD, dob, bf, dh, D, 1, dWv, gb, dh, D, D, dh, BR, h, 1.f, false}, stream);
         if (e == hipSuccess)
             e = sa::launch_gemm({dU, bf, D, 1, hD, Qp, bf, dh, D, 1, dWk, gb, dh, D, D, dh, BR, h, 1.f, false}, stream);
-        // dq = dQp W_Q^T;  dW_Q = q^T dQp
-        if (e == hipSuccess)
-            e = sa::launch_gemm({dQp, bf, 0, D, 1, Wq, bf, 0, 1, D, dq, gb, 0, D, BR, D, D, 1, 1.f, false}, stream);
+    }
+    if (e == hipSuccess) {
+        sa::ProfScope ps("cached_query_grads", stream);   // dq = dQp W_Q^T;  dW_Q = q^T dQp
+        e = sa::launch_gemm({dQp, bf, 0, D, 1, Wq, bf, 0, 1, D, dq, gb, 0, D, BR, D, D, 1, 1.f, false}, stream);
         if (e == hipSuccess)
             e = sa::launch_gemm({q, bf, 0, 1, D, dQp, bf, 0, D, 1, dWq, gb, 0, D, D, D, BR, 1, 1.f, false}, stream);
     }

@@ -49,6 +49,10 @@ struct AttnArgs {
     void* out;                      // [B][R][D], bf16 or fp32
     bool out_bf16;
     int32_t R, h, dh;               // dh a multiple of 32; N = R h, row_tiles tiles of targets a head
+    // backward: out is dQp (bf16), C is written too
+    const uint16_t* dout;           // [B][R][D]
+    uint16_t* dU;                   // [B][N][D]
+    float scale;
 };
 
 // keys of a chunk: KT tiles of 16 a wave
@@ -354,6 +358,144 @@ __device__ __forceinline__ void project_out(const AttnArgs& a, const f32x4 (&acc
     }
 }
 
+// The keys of a chunk that a wave's logits are of: up to KT / 4 runs of 64 (wide), or, where that
+// would leave waves without keys, of 16; the first at kb of the chunk, the next kstep on.
+struct Keys {
+    int c0, kend, nk;   // the chunk's first and last key; their number in whole 32s
+    bool wide;
+    int run, kb, kstep, nt;
+};
+template <int KT>
+__device__ inline Keys wave_keys(int c0, int kend, int waves, int wave) {
+    Keys k;
+    k.c0 = c0;
+    k.kend = kend;
+    k.nk = (kend - c0 + 31) / 32 * 32;
+    k.wide = k.nk > 4 * KT * waves;
+    k.run = k.wide ? 64 : 16;
+    k.kb = k.run * wave;
+    k.kstep = k.run * waves;
+    k.nt = k.nk > k.kb ? min((k.nk - k.kb + k.kstep - 1) / k.kstep, KT / 4) : 0;
+    return k;
+}
+
+// A wave's logits of its keys; `fill` where there is none
+template <int BITS, int RM, int KT>
+__device__ __forceinline__ void wave_logits(const AttnArgs& a, const uint8_t* codes, const uint8_t* scales,
+                                            const uint16_t* Ul, uint8_t* Sl, int chunks, const Keys& k, int n, int first,
+                                            int lane, float fill, f32x4 (&S)[KT][RM]) {
+    static_assert(KT == 4 || KT == 8, "one or two runs of four tiles");
+    const int q = lane >> 4, olast = (n - 1) >> 3, at = k.c0 + k.kb;
+    if (k.nt > 0) {
+        if (k.wide) logits<BITS, RM, 0, 4, KT>(a, codes, scales, Ul, Sl, chunks, at, olast, first, lane, S);
+        else logits<BITS, RM, 0, 1, KT>(a, codes, scales, Ul, Sl, chunks, at, olast, first, lane, S);
+    }
+    if constexpr (KT == 8) {
+        if (k.nt > 1) {
+            if (k.wide) logits<BITS, RM, 4, 4, KT>(a, codes, scales, Ul, Sl, chunks, at + k.kstep, olast, first, lane, S);
+            else logits<BITS, RM, 4, 1, KT>(a, codes, scales, Ul, Sl, chunks, at + k.kstep, olast, first, lane, S);
+        }
+    }
+    if (k.wide && k.nt == KT / 4 && at + (k.nt - 1) * k.kstep + 64 <= k.kend) return;   // a full share
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int key = at + (t >> 2) * k.kstep + (k.wide ? 16 * (t & 2) + 8 * q + 2 * i + (t & 1) : 4 * q + i);
+            const bool in = (t >> 2) < k.nt && (k.wide || (t & 3) == 0) && key < k.kend;
+#pragma unroll
+            for (int rm = 0; rm < RM; ++rm) S[t][rm][i] = in ? S[t][rm][i] : fill;
+        }
+}
+
+// A run's values p[i][tile] of row r into LDS as bf16, keys in order
+__device__ __forceinline__ void put_run(uint16_t* Pl, int r, int run, const Keys& k, int KC, int q, const float (&p)[4][4]) {
+    const int c = (k.kb + run * k.kstep) >> 3;   // in chunks of 8 keys
+    if (k.wide) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+            *reinterpret_cast<uint4*>(Pl + at16(r, c + 4 * x + q, KC >> 3)) =
+                make_uint4(tile::pack_bf16x2(p[0][2 * x], p[0][2 * x + 1]), tile::pack_bf16x2(p[1][2 * x], p[1][2 * x + 1]),
+                           tile::pack_bf16x2(p[2][2 * x], p[2][2 * x + 1]), tile::pack_bf16x2(p[3][2 * x], p[3][2 * x + 1]));
+    } else {
+        *reinterpret_cast<uint2*>(Pl + at16(r, c + (q >> 1), KC >> 3) + 4 * (q & 1)) =
+            make_uint2(tile::pack_bf16x2(p[0][0], p[1][0]), tile::pack_bf16x2(p[2][0], p[3][0]));
+    }
+}
+
+// acc += P X over the chunk's keys: a wave its 128 columns (dj: the lane's octet of them)
+template <int BITS, int RM>
+__device__ __forceinline__ void weighted_sum(const AttnArgs& a, const uint8_t* codes, const uint8_t* scales,
+                                             const uint16_t* Pl, int KC, int c0, int nk, int n, int dj, int lane,
+                                             f32x4 (&acc)[8][RM]) {
+    const int l16 = lane & 15, q = lane >> 4;
+    const int steps = nk / 32, tail = steps - 1;
+    // A lane's block of a step lies a fixed number of bytes behind the last step's (the steps
+    // move in scalar registers), but in the last step, where octets past the slot's last one
+    // read that one
+    const uint32_t G = (uint32_t)a.c.G;
+    const int otail = min((c0 >> 3) + 4 * tail + q, (n - 1) >> 3);
+    const uint32_t oq = (uint32_t)((c0 >> 3) + q) * G, ot = (uint32_t)otail * G - (uint32_t)(4 * tail) * G;
+    const uint32_t at0 = (oq * 4 + dj) * (8 * BITS), at1 = (ot * 4 + dj) * (8 * BITS);
+    const uint32_t sat0 = (oq + (dj >> 2)) * 8, sat1 = (ot + (dj >> 2)) * 8;
+    Block<BITS> b0, b1;
+    auto fetch = [&](Block<BITS>& to, int kk) {   // (past the last step: that one, not used)
+        kk = min(kk, tail);
+        const uint32_t at = kk == tail ? at1 : at0, sat = kk == tail ? sat1 : sat0;
+        const uint32_t step = (uint32_t)(4 * kk) * G;
+        load_block<BITS>(to, codes + step * (32 * BITS), scales + step * 8, at, sat);
+    };
+    auto multiply = [&](const Block<BITS>& from, int kk) {
+        bf16x8 p[RM];
+#pragma unroll
+        for (int rm = 0; rm < RM; ++rm) p[rm] = tile::lds_b128(Pl, at16(rm * 16 + l16, kk * 4 + q, KC >> 3));
+        uint32_t raw[8][BITS / 4];
+        float sc[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t* words = reinterpret_cast<const uint32_t*>(from.w);
+#pragma unroll
+            for (int x = 0; x < BITS / 4; ++x) raw[j][x] = words[j * (BITS / 4) + x];
+            const uint32_t s = j < 4 ? from.s.x : from.s.y;
+            sc[j] = scale_float((s >> (8 * (j & 3))) & 255u);
+        }
+        if (c0 + kk * 32 + 32 > (n & ~7)) {
+            // bytes behind the slot's last row may be anything: their weights are zero, and so are they
+            const int in = n - 8 * otail;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j >= in) {
+#pragma unroll
+                    for (int x = 0; x < BITS / 4; ++x) raw[j][x] = 0u;
+                    sc[j] = 1.f;
+                }
+        }
+        auto columns = [&](auto I) {
+            constexpr int i = decltype(I)::value;
+            uint4 lo, hi;
+            turn<BITS, i>(raw, sc, lo, hi);
+#pragma unroll
+            for (int rm = 0; rm < RM; ++rm) {
+                acc[2 * i][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[rm], __builtin_bit_cast(bf16x8, lo), acc[2 * i][rm], 0, 0, 0);
+                acc[2 * i + 1][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[rm], __builtin_bit_cast(bf16x8, hi), acc[2 * i + 1][rm], 0, 0, 0);
+            }
+        };
+        columns(std::integral_constant<int, 0>{});
+        columns(std::integral_constant<int, 1>{});
+        columns(std::integral_constant<int, 2>{});
+        columns(std::integral_constant<int, 3>{});
+    };
+    fetch(b0, 0);
+    int kk = 0;
+    for (; kk + 1 < steps; kk += 2) {
+        fetch(b1, kk + 1);
+        multiply(b0, kk);
+        fetch(b0, kk + 2);
+        multiply(b1, kk + 1);
+    }
+    if (kk < steps) multiply(b0, kk);
+}
+
 template <int BITS, int RM, int KT, bool LOOP, bool HEADS>
 __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
     extern __shared__ uint4 smem[];
@@ -365,7 +507,7 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
     float* const wmax = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(smem) + lds_tiles<RM, KT, LOOP>(waves));
     float* const wsum = wmax + 16 * RM * waves;      // [wave][row], as wmax
 
-    uint8_t* const Sl = reinterpret_cast<uint8_t*>(wsum + 16 * RM * waves) + wave * 8 * (32 * waves + 8);
+    uint8_t* const Sl = reinterpret_cast<uint8_t*>(wsum + 16 * RM * waves) + wave * 8 * scale_stride(waves);
     const uint32_t id = (uint32_t)tile::xcd_range(blockIdx.x, gridDim.x);
     const int D = a.c.D, N = a.N;
     int64_t b;
@@ -448,42 +590,15 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
         }
     }
     const int dj = min(wave * 16 + l16, a.c.G * 4 - 1);   // this lane's octet of columns
+    // each wave starts its logits at a group of its own: octets of rows lie a power of two of bytes
+    // apart (D = 1024), so that one group of all of them is in one channel of the L2
+    const int first = 2 * (int)((uint32_t)(3 * wave + 5 * id) % (uint32_t)(chunks / 8));
     for (int c0 = k0; c0 < k1; c0 += KC) {
-        const int kend = min(k1, c0 + KC);
-        const int nk = (kend - c0 + 31) / 32 * 32;
-        // ---- logits of this wave's keys: wide, up to two runs of 64; or, where that would leave
-        // waves without keys, two of 16
+        const Keys keys = wave_keys<KT>(c0, min(k1, c0 + KC), waves, wave);
         f32x4 S[KT][RM];
-        static_assert(KT == 8, "two runs of four tiles");
-        const bool wide = nk > 32 * waves;
-        const int run = wide ? 64 : 16;
-        const int kb = run * wave, kstep = run * waves;   // in the chunk
-        const int nt = nk > kb ? min((nk - kb + kstep - 1) / kstep, 2) : 0;
-        const int olast = (n - 1) >> 3;
-        // each wave starts at a group of its own: octets of rows lie a power of two of bytes apart
-        // (D = 1024), so that one group of all of them is in one channel of the L2
-        const int first = 2 * (int)((uint32_t)(3 * wave + 5 * id) % (uint32_t)(chunks / 8));
-        if (nt > 0) {
-            if (wide) logits<BITS, RM, 0, 4, KT>(a, codes, scales, Ul, Sl, chunks, c0 + kb, olast, first, lane, S);
-            else logits<BITS, RM, 0, 1, KT>(a, codes, scales, Ul, Sl, chunks, c0 + kb, olast, first, lane, S);
-        }
-        if (nt > 1) {
-            if (wide) logits<BITS, RM, 4, 4, KT>(a, codes, scales, Ul, Sl, chunks, c0 + kb + kstep, olast, first, lane, S);
-            else logits<BITS, RM, 4, 1, KT>(a, codes, scales, Ul, Sl, chunks, c0 + kb + kstep, olast, first, lane, S);
-        }
-        // ---- softmax: the maximum over the chunk's keys, of all waves.  (scale2 > 0: the largest
-        // logit has the largest product.)  Only waves without a full share of keys mask.
-        if (!wide || nt < 2 || c0 + kb + kstep + run > kend) {
-#pragma unroll
-            for (int t = 0; t < KT; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int key = kb + (t >> 2) * kstep + (wide ? 16 * (t & 2) + 8 * q + 2 * i + (t & 1) : 4 * q + i);
-                    const bool in = (t >> 2) < nt && (wide || (t & 3) == 0) && c0 + key < kend;
-#pragma unroll
-                    for (int rm = 0; rm < RM; ++rm) S[t][rm][i] = in ? S[t][rm][i] : -INFINITY;
-                }
-        }
+        wave_logits<BITS, RM, KT>(a, codes, scales, Ul, Sl, chunks, keys, n, first, lane, -INFINITY, S);
+        // ---- softmax: the maximum over the chunk's keys, of all waves (scale2 > 0: the largest
+        // logit has the largest product)
 #pragma unroll
         for (int rm = 0; rm < RM; ++rm) {
             float mx = -INFINITY;
@@ -507,7 +622,7 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
             float sum = 0.f;
 #pragma unroll
             for (int t = 0; t < KT; t += 4) {
-                if ((t >> 2) >= nt) break;
+                if ((t >> 2) >= keys.nt) break;
                 float p[4][4];   // [i][tile]
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -516,17 +631,7 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
                         p[i][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t + j][rm][i], a.scale2, -base));
                     sum += (p[i][0] + p[i][1]) + (p[i][2] + p[i][3]);
                 }
-                const int c = (kb + (t >> 2) * kstep) >> 3;   // in chunks of 8 keys
-                if (wide) {
-#pragma unroll
-                    for (int x = 0; x < 2; ++x)
-                        *reinterpret_cast<uint4*>(Pl + at16(rm * 16 + l16, c + 4 * x + q, KC >> 3)) =
-                            make_uint4(tile::pack_bf16x2(p[0][2 * x], p[0][2 * x + 1]), tile::pack_bf16x2(p[1][2 * x], p[1][2 * x + 1]),
-                                       tile::pack_bf16x2(p[2][2 * x], p[2][2 * x + 1]), tile::pack_bf16x2(p[3][2 * x], p[3][2 * x + 1]));
-                } else {
-                    *reinterpret_cast<uint2*>(Pl + at16(rm * 16 + l16, c + (q >> 1), KC >> 3) + 4 * (q & 1)) =
-                        make_uint2(tile::pack_bf16x2(p[0][0], p[1][0]), tile::pack_bf16x2(p[2][0], p[3][0]));
-                }
+                put_run(Pl, rm * 16 + l16, t >> 2, keys, KC, q, p);
             }
             sum += __shfl_xor(sum, 16, 64);
             sum += __shfl_xor(sum, 32, 64);
@@ -559,71 +664,7 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
 #pragma unroll
                 for (int rm = 0; rm < RM; ++rm) acc[j][rm] = (f32x4){0.f, 0.f, 0.f, 0.f};
         }
-        const int steps = nk / 32, tail = steps - 1;
-        // A lane's block of a step lies a fixed number of bytes behind the last step's (the steps
-        // move in scalar registers), but in the last step, where octets past the slot's last one
-        // read that one
-        const uint32_t G = (uint32_t)a.c.G;
-        const int otail = min((c0 >> 3) + 4 * tail + q, (n - 1) >> 3);
-        const uint32_t oq = (uint32_t)((c0 >> 3) + q) * G, ot = (uint32_t)otail * G - (uint32_t)(4 * tail) * G;
-        const uint32_t at0 = (oq * 4 + dj) * (8 * BITS), at1 = (ot * 4 + dj) * (8 * BITS);
-        const uint32_t sat0 = (oq + (dj >> 2)) * 8, sat1 = (ot + (dj >> 2)) * 8;
-        Block<BITS> b0, b1;
-        auto fetch = [&](Block<BITS>& to, int kk) {   // (past the last step: that one, not used)
-            kk = min(kk, tail);
-            const uint32_t at = kk == tail ? at1 : at0, sat = kk == tail ? sat1 : sat0;
-            const uint32_t step = (uint32_t)(4 * kk) * G;
-            load_block<BITS>(to, codes + step * (32 * BITS), scales + step * 8, at, sat);
-        };
-        auto multiply = [&](const Block<BITS>& from, int kk) {
-            bf16x8 p[RM];
-#pragma unroll
-            for (int rm = 0; rm < RM; ++rm) p[rm] = tile::lds_b128(Pl, at16(rm * 16 + l16, kk * 4 + q, KC >> 3));
-            uint32_t raw[8][BITS / 4];
-            float sc[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t* words = reinterpret_cast<const uint32_t*>(from.w);
-#pragma unroll
-                for (int x = 0; x < BITS / 4; ++x) raw[j][x] = words[j * (BITS / 4) + x];
-                const uint32_t s = j < 4 ? from.s.x : from.s.y;
-                sc[j] = scale_float((s >> (8 * (j & 3))) & 255u);
-            }
-            if (c0 + kk * 32 + 32 > (n & ~7)) {
-                // bytes behind the slot's last row may be anything: their weights are zero, and so are they
-                const int in = n - 8 * otail;
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (j >= in) {
-#pragma unroll
-                        for (int x = 0; x < BITS / 4; ++x) raw[j][x] = 0u;
-                        sc[j] = 1.f;
-                    }
-            }
-            auto columns = [&](auto I) {
-                constexpr int i = decltype(I)::value;
-                uint4 lo, hi;
-                turn<BITS, i>(raw, sc, lo, hi);
-#pragma unroll
-                for (int rm = 0; rm < RM; ++rm) {
-                    acc[2 * i][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[rm], __builtin_bit_cast(bf16x8, lo), acc[2 * i][rm], 0, 0, 0);
-                    acc[2 * i + 1][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[rm], __builtin_bit_cast(bf16x8, hi), acc[2 * i + 1][rm], 0, 0, 0);
-                }
-            };
-            columns(std::integral_constant<int, 0>{});
-            columns(std::integral_constant<int, 1>{});
-            columns(std::integral_constant<int, 2>{});
-            columns(std::integral_constant<int, 3>{});
-        };
-        fetch(b0, 0);
-        int kk = 0;
-        for (; kk + 1 < steps; kk += 2) {
-            fetch(b1, kk + 1);
-            multiply(b0, kk);
-            fetch(b0, kk + 2);
-            multiply(b1, kk + 1);
-        }
-        if (kk < steps) multiply(b0, kk);
+        weighted_sum<BITS, RM>(a, codes, scales, Pl, KC, c0, keys.nk, n, dj, lane, acc);
         if constexpr (!LOOP) break;   // all keys are in one chunk
     }
     // ---- results: rows rm 16 + 4 q + i, this lane's columns 8 (16 wave + l16) ..+7
@@ -682,6 +723,177 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
             }
         }
     }
+}
+
+// The backward of one head's targets towards its queries, everything around the attention that
+// needs no sum over users: with U = Qp_i W_K^(i)T and dC = dout_i W_V^(i)T (in LDS one after the
+// other)
+//   alpha = softmax(scale U X^T),  C = alpha X,
+//   dA = dC X^T,  ds = scale alpha (dA - sum alpha dA),  dU = ds X,  dQp_i = dU W_K^(i),
+// C and dU left in memory for the weights' gradients.  All keys in one chunk: the weights wait in
+// registers, fp32, while C is summed and dA computed.  Four products of the forward's kind, each
+// decoding the codes once.
+template <int BITS, int RM, int KT>
+__global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
+    extern __shared__ uint4 smem[];
+    const int waves = blockDim.x >> 6, chunks = 16 * waves, KC = chunk_keys(KT, waves);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
+    uint16_t* const Ul = reinterpret_cast<uint16_t*>(smem);
+    uint16_t* const Pl = Ul;
+    float* const wmax = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(smem) + lds_tiles<RM, KT, false>(waves));
+    float* const wsum = wmax + 16 * RM * waves;      // [wave][row], as wmax
+    uint8_t* const Sl = reinterpret_cast<uint8_t*>(wsum + 16 * RM * waves) + wave * 8 * scale_stride(waves);
+    const uint32_t id = (uint32_t)tile::xcd_range(blockIdx.x, gridDim.x);
+    const int D = a.c.D;
+    const uint32_t bh = id / (uint32_t)a.row_tiles;
+    const int row0 = (int)(id - bh * (uint32_t)a.row_tiles) * 16 * RM;
+    const int64_t b = bh / (uint32_t)a.h;
+    const int head = (int)(bh - (uint32_t)b * (uint32_t)a.h), rows = min(16 * RM, a.R - row0);
+    int32_t n;
+    const uint8_t* const codes = cache_slot(a.c, b, &n);
+    const uint8_t* const scales = codes + a.c.scales_at;
+    const int64_t urow = b * a.R + row0;
+    const int col = 8 * (wave * 16 + l16);   // this lane's columns of C and dU (D is a multiple of 32)
+    if (n <= 0) {
+        for (int i = threadIdx.x; i < rows * (D / 8); i += blockDim.x) {
+            const int64_t to = ((urow + i / (D / 8)) * a.h + head) * D + 8 * (i % (D / 8));
+            *reinterpret_cast<uint4*>(a.C + to) = make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4*>(a.dU + to) = make_uint4(0u, 0u, 0u, 0u);
+        }
+        for (int i = threadIdx.x; i < rows * a.dh; i += blockDim.x)
+            reinterpret_cast<uint16_t*>(a.out)[(urow + i / a.dh) * D + head * a.dh + i % a.dh] = 0;
+        return;
+    }
+    const int first = 2 * (int)((uint32_t)(3 * wave + 5 * id) % (uint32_t)(chunks / 8));
+    const int dj = min(wave * 16 + l16, a.c.G * 4 - 1);
+    const Keys keys = wave_keys<KT>(0, n, waves, wave);
+    uint16_t* const Ql = Ul + waves * 128 * 64;
+
+    project_rows<RM>(a.Qp + urow * D + head * a.dh, a.Wk + head * a.dh, D, a.dh, rows, wave, lane, Ul, chunks, Ql);
+    __syncthreads();
+    f32x4 S[KT][RM];   // logits, then weights before their division by the sum
+    wave_logits<BITS, RM, KT>(a, codes, scales, Ul, Sl, chunks, keys, n, first, lane, -INFINITY, S);
+#pragma unroll
+    for (int rm = 0; rm < RM; ++rm) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < KT; ++t) mx = fmaxf(fmaxf(fmaxf(mx, S[t][rm][0]), fmaxf(S[t][rm][1], S[t][rm][2])), S[t][rm][3]);
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        if (q == 0) wmax[wave * 16 * RM + rm * 16 + l16] = mx;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rm = 0; rm < RM; ++rm) {
+        float mx = wmax[rm * 16 + l16];
+        for (int v = 1; v < waves; ++v) mx = fmaxf(mx, wmax[v * 16 * RM + rm * 16 + l16]);
+        if (mx == -INFINITY) mx = 0.f;
+        float sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < KT; t += 4) {
+            float p[4][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    {
+                    // (the difference first: the largest weight is 1 exactly, and a row alone has no gradient)
+                    p[i][j] = __builtin_amdgcn_exp2f((S[t + j][rm][i] - mx) * a.scale2);
+                    S[t + j][rm][i] = p[i][j];
+                }
+                sum += (p[i][0] + p[i][1]) + (p[i][2] + p[i][3]);
+            }
+            if ((t >> 2) < keys.nt) put_run(Pl, rm * 16 + l16, t >> 2, keys, KC, q, p);
+        }
+        sum += __shfl_xor(sum, 16, 64);
+        sum += __shfl_xor(sum, 32, 64);
+        if (q == 0) wsum[wave * 16 * RM + rm * 16 + l16] = sum;
+    }
+    __syncthreads();
+    float inv[RM];   // 1 / sum of row l16
+#pragma unroll
+    for (int rm = 0; rm < RM; ++rm) {
+        float sum = wsum[rm * 16 + l16];
+        for (int v = 1; v < waves; ++v) sum += wsum[v * 16 * RM + rm * 16 + l16];
+        inv[rm] = 1.f / sum;
+    }
+    f32x4 acc[8][RM];
+    auto clear = [&] {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int rm = 0; rm < RM; ++rm) acc[j][rm] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    };
+    // accumulators, times their rows' factors, as bf16
+    auto store = [&](uint16_t* to, const float (&f)[RM][4]) {
+#pragma unroll
+        for (int rm = 0; rm < RM; ++rm)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = rm * 16 + 4 * q + i;
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = acc[j][rm][i] * f[rm][i];
+                if (r < rows && col < D)
+                    *reinterpret_cast<uint4*>(to + ((urow + r) * a.h + head) * D + col) = __builtin_bit_cast(uint4, tile::pack8(v));
+            }
+    };
+    clear();
+    weighted_sum<BITS, RM>(a, codes, scales, Pl, KC, 0, keys.nk, n, dj, lane, acc);
+    {
+        float f[RM][4];
+#pragma unroll
+        for (int rm = 0; rm < RM; ++rm)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[rm][i] = __shfl(inv[rm], 4 * q + i, 64);
+        store(a.C, f);
+    }
+    __syncthreads();   // the weights in LDS have been read
+    project_rows<RM>(a.dout + urow * D + head * a.dh, a.Wv + head * a.dh, D, a.dh, rows, wave, lane, Ul, chunks, Ql);
+    __syncthreads();
+    f32x4 T[KT][RM];   // gradients of the weights
+    wave_logits<BITS, RM, KT>(a, codes, scales, Ul, Sl, chunks, keys, n, first, lane, 0.f, T);
+#pragma unroll
+    for (int rm = 0; rm < RM; ++rm) {
+        float dot = 0.f;
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dot = __builtin_fmaf(S[t][rm][i], T[t][rm][i], dot);
+        dot += __shfl_xor(dot, 16, 64);
+        dot += __shfl_xor(dot, 32, 64);
+        if (q == 0) wmax[wave * 16 * RM + rm * 16 + l16] = dot;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rm = 0; rm < RM; ++rm) {
+        float dot = wmax[rm * 16 + l16];
+        for (int v = 1; v < waves; ++v) dot += wmax[v * 16 * RM + rm * 16 + l16];
+        dot *= inv[rm];
+        const float f = a.scale * inv[rm];
+#pragma unroll
+        for (int t = 0; t < KT; t += 4) {
+            if ((t >> 2) >= keys.nt) break;
+            float p[4][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) p[i][j] = f * S[t + j][rm][i] * (T[t + j][rm][i] - dot);
+            put_run(Pl, rm * 16 + l16, t >> 2, keys, KC, q, p);
+        }
+    }
+    __syncthreads();
+    clear();
+    weighted_sum<BITS, RM>(a, codes, scales, Pl, KC, 0, keys.nk, n, dj, lane, acc);
+    float one[RM][4];
+#pragma unroll
+    for (int rm = 0; rm < RM; ++rm)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) one[rm][i] = 1.f;
+    store(a.dU, one);
+    __syncthreads();
+    project_out<RM>(a, acc, one, a.Wk + head * a.dh, rows, urow, head, waves, wave, lane, Ul);
 }
 
 // Joins the splits of each row: their sums and accumulators, each scaled to the common
@@ -816,6 +1028,78 @@ hipError_t launch_cached_heads(const CacheView& c, int bits, const uint16_t* Qp,
         if (rm == 2) return launch_instance<8, 2, 8, true, true>(a, stream);
         if (rm == 3) return launch_instance<8, 3, 8, false, true>(a, stream);
         if (rm == 4) return launch_instance<8, 4, 8, false, true>(a, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+namespace {
+
+// The backward's rows of a workgroup (in 16s) and tiles of 16 keys a wave; 0 rows where it does
+// not take the shape: all keys have to fit a chunk.
+int heads_bwd_tiles(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
+    if (D > 1024 || D % h != 0 || (D / h) % 32 != 0) return 0;
+    const int waves = (D + 127) / 128;
+    if (k > chunk_keys(8, waves)) return 0;
+#ifdef SA_EXPERIMENT
+    if (getenv("SA_HB")) return atoi(getenv("SA_HB"));
+#endif
+    int best = 0;
+    int64_t cost = 0;
+    for (int rm = 1; rm <= (k <= chunk_keys(4, waves) ? 3 : 2); ++rm) {
+        const int64_t wgs = B * h * ((R + 16 * rm - 1) / (16 * rm));
+        const int64_t c = (wgs + device_cus() - 1) / device_cus() * (rm + 1);
+        if (best == 0 || c <= cost) best = rm, cost = c;
+    }
+    return best;
+}
+
+template <int BITS, int RM, int KT>
+hipError_t launch_bwd_instance(const AttnArgs& a, hipStream_t stream) {
+    const int waves = (a.c.D + 127) / 128;
+    const int lds = lds_bytes<RM, KT, false, true>(waves);
+    auto kern = cached_attn_bwd_kernel<BITS, RM, KT>;
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(a.B * a.row_tiles * a.h)), dim3(64 * waves), lds, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+bool cached_heads_bwd_supported(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
+    return heads_bwd_tiles(B, R, h, k, D) > 0;
+}
+
+hipError_t launch_cached_heads_bwd(const CacheView& c, int bits, const uint16_t* Qp, const uint16_t* dout,
+                                   const uint16_t* Wk, const uint16_t* Wv, uint16_t* C, uint16_t* dU, uint16_t* dQp,
+                                   int64_t B, int32_t R, int32_t h, float scale, hipStream_t stream) {
+    const int rm = heads_bwd_tiles(B, R, h, c.k, c.D);
+    AttnArgs a{};
+    a.c = c;
+    a.C = C;
+    a.B = B;
+    a.N = R * h;
+    a.row_tiles = (R + 16 * rm - 1) / (16 * rm);
+    a.scale2 = scale * tile::kLog2e;
+    a.Qp = Qp;
+    a.Wk = Wk;
+    a.Wv = Wv;
+    a.out = dQp;
+    a.out_bf16 = true;
+    a.R = R;
+    a.h = h;
+    a.dh = c.D / h;
+    a.dout = dout;
+    a.dU = dU;
+    a.scale = scale;
+    if (bits == 4) {
+        if (rm == 1) return launch_bwd_instance<4, 1, 8>(a, stream);
+        if (rm == 2) return launch_bwd_instance<4, 2, 8>(a, stream);
+        if (rm == 3) return launch_bwd_instance<4, 3, 4>(a, stream);
+    } else {
+        if (rm == 1) return launch_bwd_instance<8, 1, 8>(a, stream);
+        if (rm == 2) return launch_bwd_instance<8, 2, 8>(a, stream);
+        if (rm == 3) return launch_bwd_instance<8, 3, 4>(a, stream);
     }
     return hipErrorInvalidValue;
 }

@@ -236,6 +236,11 @@ bool cached_heads_supported(int64_t B, int32_t R, int32_t h, int32_t k, int32_t 
 hipError_t launch_cached_heads(const CacheView& c, int bits, const uint16_t* Qp, const uint16_t* Wk, const uint16_t* Wv,
                                void* out, bool out_bf16, float* lse, int64_t B, int32_t R, int32_t h, float scale,
                                hipStream_t stream);
+// its backward: C and dU [B][R][h][D] and dQp [B][R][D], bf16
+bool cached_heads_bwd_supported(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D);
+hipError_t launch_cached_heads_bwd(const CacheView& c, int bits, const uint16_t* Qp, const uint16_t* dout,
+                                   const uint16_t* Wk, const uint16_t* Wv, uint16_t* C, uint16_t* dU, uint16_t* dQp,
+                                   int64_t B, int32_t R, int32_t h, float scale, hipStream_t stream);
 // softmax rows over each user's valid rows (rows = B Rh of k fp32 logits) and its backward
 hipError_t launch_cached_softmax(const CacheView& c, const float* S, int64_t rows, int32_t Rh, bool bf16, void* alpha,
                                  float* lse, hipStream_t stream);
