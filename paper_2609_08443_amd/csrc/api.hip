@@ -664,14 +664,16 @@ sa::CacheView cache_view(const void* cache, const int32_t* rows, const int64_t* 
     return c;
 }
 
-// STCA over cached sketches.  fused: the attention in one kernel, [Qp | U | C | lse
-// (fp32) | partial results of split keys].  Otherwise in separate products: [Xd | Qp | U
-// | S (fp32) | alpha | C | lse (fp32) | (bwd) dout in the operand dtype | dC | dalpha
-// (fp32) | ds | dU | dQp]; Xd [B,k,D] are the sketches read from the cache, the rest as
-// in StcaPlan.
+// STCA over cached sketches; operand buffers in the input dtype, as in StcaPlan.
+//   kCachedHeads   workgroups take a head's targets, projections and all:
+//                  [Qp | lse | (bwd) dout in bf16 | C | dU | dQp]
+//   kCachedRows    the attention alone in one kernel:
+//                  [Qp | lse | U | C | partial results of split keys | (bwd) dout | dC | dU | dQp]
+//   kCachedProducts  in separate products over sketches read into the workspace, Xd [B,k,D]:
+//                  [Qp | lse | U | C | Xd | S (fp32) | alpha | (bwd) dout | dC | dU | dQp | dalpha (fp32) | ds]
+enum CachedKind { kCachedProducts = 0, kCachedRows = 1, kCachedHeads = 2 };
 struct CachedPlan {
-    bool fused = false;
-    bool heads = false;   // fused with the projections around it: [Qp | lse | (bwd) dout in bf16 | C | dU | dQp]
+    CachedKind kind = kCachedProducts;
     size_t off_xd = 0, off_qp = 0, off_u = 0, off_s = 0, off_al = 0, off_c = 0, off_lse = 0, off_part = 0, off_dob = 0,
            off_dc = 0, off_da = 0, off_ds = 0, off_du = 0, off_dqp = 0, total = 0;
 };
@@ -686,37 +688,27 @@ CachedPlan plan_cached(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa
     };
     const size_t el = dtype == SA_BF16 ? 2 : 4;
     const size_t BR = (size_t)B * R, rows = BR * h;
-    p.fused = dtype == SA_BF16 && sa::cached_attn_supported(D) && !bwd;
-    p.heads = dtype == SA_BF16 && (bwd ? sa::cached_heads_bwd_supported(B, R, h, k, D)
-                                       : p.fused && sa::cached_heads_supported(B, R, h, k, D));
+    if (dtype == SA_BF16)
+        p.kind = (CachedKind)(bwd ? sa::cached_bwd_kind(B, R, h, k, D) : sa::cached_attn_kind(B, R, h, k, D));
     p.off_qp = carve(el * BR * D);
     p.off_lse = carve(4 * rows);
-    if (p.heads) {
-        if (bwd) {
-            p.off_dob = carve(el * BR * D);
-            p.off_c = carve(el * rows * D);
-            p.off_du = carve(el * rows * D);
-            p.off_dqp = carve(el * BR * D);
-        }
-        p.total = off;
-        return p;
-    }
-    p.off_u = carve(el * rows * D);
-    p.off_c = carve(el * rows * D);
-    if (p.fused) {
-        p.off_part = carve(sa::cached_attn_workspace(B, R * h, k, D));
-    } else {
+    if (p.kind != kCachedHeads) p.off_u = carve(el * rows * D);
+    if (p.kind != kCachedHeads || bwd) p.off_c = carve(el * rows * D);
+    if (p.kind == kCachedRows && !bwd) p.off_part = carve(sa::cached_attn_workspace(B, R, h, k, D));
+    if (p.kind == kCachedProducts) {
         p.off_xd = carve(el * B * k * D);
         p.off_s = carve(4 * rows * k);
         p.off_al = carve(el * rows * k);
     }
     if (bwd) {
         p.off_dob = carve(dtype == SA_BF16 ? el * BR * D : 0);
-        p.off_dc = carve(el * rows * D);
-        p.off_da = carve(4 * rows * k);
-        p.off_ds = carve(el * rows * k);
+        if (p.kind != kCachedHeads) p.off_dc = carve(el * rows * D);
         p.off_du = carve(el * rows * D);
         p.off_dqp = carve(el * BR * D);
+        if (p.kind == kCachedProducts) {
+            p.off_da = carve(4 * rows * k);
+            p.off_ds = carve(el * rows * k);
+        }
     }
     p.total = off;
     return p;
@@ -732,33 +724,33 @@ struct CachedArgs {
     bool bf;
 };
 
-// Qp, U and the attention over the cached rows: C [B,R,h,D] and lse
-sa_status cached_attention(const CachedArgs& a, float* lse, uint8_t* ws, const CachedPlan& p, hipStream_t stream) {
+// Qp = q W_Q [B,R,D]
+hipError_t cached_query(const CachedArgs& a, uint8_t* ws, const CachedPlan& p, hipStream_t stream) {
+    const int32_t BR = (int32_t)(a.B * a.R), D = a.D;
+    sa::ProfScope ps("cached_query_proj", stream);
+    return sa::launch_gemm({a.q, a.bf, 0, D, 1, a.Wq, a.bf, 0, D, 1, ws + p.off_qp, a.bf, 0, D, BR, D, D, 1, 1.f, false},
+                           stream);
+}
+// U[., i] = Qp[., head i] W_K^(i)T [B,R,h,D] (from Qp), or dC from dout and W_V
+hipError_t cached_head_rows(const CachedArgs& a, const void* rows, const void* W, void* to, const char* name,
+                            hipStream_t stream) {
+    const int32_t BR = (int32_t)(a.B * a.R), D = a.D, dh = D / a.h;
+    sa::ProfScope ps(name, stream);
+    return sa::launch_gemm({rows, a.bf, dh, D, 1, W, a.bf, dh, 1, D, to, a.bf, D, (int64_t)a.h * D, BR, D, dh, a.h, 1.f,
+                            false}, stream);
+}
+
+// in separate products: alpha, C [B,R,h,D] and lse of U
+hipError_t cached_products(const CachedArgs& a, float* lse, uint8_t* ws, const CachedPlan& p, hipStream_t stream) {
     const bool bf = a.bf;
-    const int32_t BR = (int32_t)(a.B * a.R), D = a.D, k = a.k, dh = D / a.h, Rh = a.R * a.h;
+    const int32_t D = a.D, k = a.k, Rh = a.R * a.h;
     const int64_t kD = (int64_t)k * D, RhD = (int64_t)Rh * D, Rhk = (int64_t)Rh * k;
-    void *Xd = ws + p.off_xd, *Qp = ws + p.off_qp, *U = ws + p.off_u, *Al = ws + p.off_al, *Cc = ws + p.off_c;
+    void *Xd = ws + p.off_xd, *U = ws + p.off_u, *Al = ws + p.off_al, *Cc = ws + p.off_c;
     float* S = reinterpret_cast<float*>(ws + p.off_s);
-    hipError_t e = hipSuccess;
-    if (!p.fused) {
+    hipError_t e;
+    {
         sa::ProfScope ps("cached_read", stream);
         e = sa::launch_cache_read(a.cache, a.bits, Xd, bf, a.B, stream);
-    }
-    if (e == hipSuccess) {
-        sa::ProfScope ps("cached_query_proj", stream);
-        e = sa::launch_gemm({a.q, bf, 0, D, 1, a.Wq, bf, 0, D, 1, Qp, bf, 0, D, BR, D, D, 1, 1.f, false}, stream);
-        if (e == hipSuccess)
-            e = sa::launch_gemm({Qp, bf, dh, D, 1, a.Wk, bf, dh, 1, D, U, bf, D, (int64_t)a.h * D, BR, D, dh, a.h, 1.f,
-                                 false}, stream);
-    }
-    if (p.fused) {
-        if (e == hipSuccess) {
-            sa::ProfScope ps("cached_attention", stream);
-            e = sa::launch_cached_attn(a.cache, a.bits, reinterpret_cast<const uint16_t*>(U),
-                                       reinterpret_cast<uint16_t*>(Cc), lse, ws + p.off_part, a.B, Rh, a.scale, stream);
-        }
-        if (e != hipSuccess) return hip_fail(e, "cached STCA launch");
-        return SA_OK;
     }
     if (e == hipSuccess) {
         sa::ProfScope ps("cached_logits", stream);
@@ -767,19 +759,18 @@ sa_status cached_attention(const CachedArgs& a, float* lse, uint8_t* ws, const C
     }
     if (e == hipSuccess) {
         sa::ProfScope ps("cached_softmax", stream);
-        e = sa::launch_cached_softmax(a.cache, S, (int64_t)BR * a.h, Rh, bf, Al, lse, stream);
+        e = sa::launch_cached_softmax(a.cache, S, a.B * Rh, Rh, bf, Al, lse, stream);
     }
     if (e == hipSuccess) {
         sa::ProfScope ps("cached_aggregate", stream);
         e = sa::launch_gemm({Al, bf, Rhk, k, 1, Xd, bf, kD, D, 1, Cc, bf, RhD, D, Rh, D, k, (int32_t)a.B, 1.f, false},
                             stream);
     }
-    if (e != hipSuccess) return hip_fail(e, "cached STCA launch");
-    return SA_OK;
+    return e;
 }
 
-// dU from C's gradient dC = dout W_V^T: the attention's backward towards its queries
-sa_status cached_attention_bwd(const CachedArgs& a, const float* lse, uint8_t* ws, const CachedPlan& p,
+// in separate products: dU from C's gradient dC
+hipError_t cached_products_bwd(const CachedArgs& a, const float* lse, uint8_t* ws, const CachedPlan& p,
                                hipStream_t stream) {
     const bool bf = a.bf;
     const int32_t D = a.D, k = a.k, Rh = a.R * a.h;
@@ -803,8 +794,7 @@ sa_status cached_attention_bwd(const CachedArgs& a, const float* lse, uint8_t* w
         e = sa::launch_gemm({ds, bf, Rhk, k, 1, Xd, bf, kD, D, 1, dU, bf, RhD, D, Rh, D, k, (int32_t)a.B, 1.f, false},
                             stream);
     }
-    if (e != hipSuccess) return hip_fail(e, "cached STCA backward launch");
-    return SA_OK;
+    return e;
 }
 
 // arguments shared by the two directions
@@ -1790,27 +1780,24 @@ sa_status sa_stca_cached_fwd(const void* cache, const int32_t* cache_rows, int64
     hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
     const int32_t BR = (int32_t)(B * R), dh = D / h;
     if (!lse) lse = reinterpret_cast<float*>(ws + p.off_lse);
-    if (p.heads) {
-        uint16_t* Qp = reinterpret_cast<uint16_t*>(ws + p.off_qp);
-        hipError_t e;
-        {
-            sa::ProfScope ps("cached_query_proj", stream);
-            e = sa::launch_gemm({q, bf, 0, D, 1, Wq, bf, 0, D, 1, Qp, bf, 0, D, BR, D, D, 1, 1.f, false}, stream);
-        }
-        if (e == hipSuccess) {
-            sa::ProfScope ps("cached_heads", stream);
-            e = sa::launch_cached_heads(a.cache, a.bits, Qp, reinterpret_cast<const uint16_t*>(Wk),
-                                        reinterpret_cast<const uint16_t*>(Wv), out, out_dtype == SA_BF16, lse, B, R, h,
-                                        scale, stream);
-        }
-        if (e != hipSuccess) return hip_fail(e, "cached STCA launch");
-        return SA_OK;
+    hipError_t e = cached_query(a, ws, p, stream);
+    if (e == hipSuccess && p.kind != kCachedHeads)
+        e = cached_head_rows(a, ws + p.off_qp, Wk, ws + p.off_u, "cached_query_rows", stream);
+    if (e == hipSuccess && p.kind != kCachedProducts) {
+        sa::ProfScope ps("cached_attention", stream);
+        auto b16 = [](const void* x) { return reinterpret_cast<const uint16_t*>(x); };
+        e = sa::launch_cached_attn(a.cache, a.bits,
+                                   {b16(ws + p.off_u), reinterpret_cast<uint16_t*>(ws + p.off_c), ws + p.off_part,
+                                    b16(ws + p.off_qp), b16(Wk), b16(Wv), out, out_dtype == SA_BF16, lse, B, R, h, scale},
+                                   stream);
+    } else if (e == hipSuccess) {
+        e = cached_products(a, lse, ws, p, stream);
     }
-    st = cached_attention(a, lse, ws, p, stream);
-    if (st != SA_OK) return st;
-    sa::ProfScope ps("cached_value_proj", stream);   // out[., head i] = C[., i] W_V^(i)
-    hipError_t e = sa::launch_gemm({ws + p.off_c, bf, D, (int64_t)h * D, 1, Wv, bf, dh, D, 1, out, out_dtype == SA_BF16,
-                                    dh, D, BR, dh, D, h, 1.f, false}, stream);
+    if (e == hipSuccess && p.kind != kCachedHeads) {
+        sa::ProfScope ps("cached_value_proj", stream);   // out[., head i] = C[., i] W_V^(i)
+        e = sa::launch_gemm({ws + p.off_c, bf, D, (int64_t)h * D, 1, Wv, bf, dh, D, 1, out, out_dtype == SA_BF16, dh, D,
+                             BR, dh, D, h, 1.f, false}, stream);
+    }
     if (e != hipSuccess) return hip_fail(e, "cached STCA launch");
     return SA_OK;
 }
@@ -1857,32 +1844,25 @@ sa_status sa_stca_cached_bwd(const void* cache, const int32_t* cache_rows, int64
         e = sa::launch_to_bf16(reinterpret_cast<const float*>(dout), reinterpret_cast<uint16_t*>(ws + p.off_dob),
                                (int64_t)BR * D, stream);
     }
-    if (p.heads) {   // Qp; C, dU and dQp
-        if (e == hipSuccess) {
-            sa::ProfScope ps("cached_query_proj", stream);
-            e = sa::launch_gemm({q, bf, 0, D, 1, Wq, bf, 0, D, 1, Qp, bf, 0, D, BR, D, D, 1, 1.f, false}, stream);
-        }
-        if (e == hipSuccess) {
-            sa::ProfScope ps("cached_heads_bwd", stream);
-            e = sa::launch_cached_heads_bwd(a.cache, a.bits, reinterpret_cast<const uint16_t*>(Qp),
-                                            reinterpret_cast<const uint16_t*>(dob), reinterpret_cast<const uint16_t*>(Wk),
-                                            reinterpret_cast<const uint16_t*>(Wv), reinterpret_cast<uint16_t*>(Cc),
-                                            reinterpret_cast<uint16_t*>(dU), reinterpret_cast<uint16_t*>(dQp), B, R, h,
-                                            scale, stream);
-        }
-    } else {
-        if (e == hipSuccess) {
-            st = cached_attention(a, lse, ws, p, stream);   // Qp, U, lse and C once more
-            if (st != SA_OK) return st;
-            sa::ProfScope ps("cached_value_side", stream);   // dC[., i] = dout[., head i] W_V^(i)T
-            e = sa::launch_gemm({dob, bf, dh, D, 1, Wv, bf, dh, 1, D, dC, bf, D, hD, BR, D, dh, h, 1.f, false}, stream);
-        }
-        if (e == hipSuccess) {
-            st = cached_attention_bwd(a, lse, ws, p, stream);
-            if (st != SA_OK) return st;
-            sa::ProfScope ps("cached_key_side", stream);   // dQp[., head i] = dU[., i] W_K^(i)
-            e = sa::launch_gemm({dU, bf, D, hD, 1, Wk, bf, dh, D, 1, dQp, bf, dh, D, BR, dh, D, h, 1.f, false}, stream);
-        }
+    if (e == hipSuccess) e = cached_query(a, ws, p, stream);
+    if (p.kind != kCachedHeads) {
+        if (e == hipSuccess) e = cached_head_rows(a, Qp, Wk, ws + p.off_u, "cached_query_rows", stream);
+        if (e == hipSuccess) e = cached_head_rows(a, dob, Wv, dC, "cached_value_rows", stream);
+    }
+    if (p.kind == kCachedProducts) {
+        if (e == hipSuccess) e = cached_products(a, lse, ws, p, stream);
+        if (e == hipSuccess) e = cached_products_bwd(a, lse, ws, p, stream);
+    } else if (e == hipSuccess) {
+        sa::ProfScope ps("cached_attention_bwd", stream);
+        auto b16 = [](const void* x) { return reinterpret_cast<const uint16_t*>(x); };
+        e = sa::launch_cached_bwd(a.cache, a.bits,
+                                  {b16(ws + p.off_u), b16(dC), b16(Qp), b16(dob), b16(Wk), b16(Wv),
+                                   reinterpret_cast<uint16_t*>(Cc), reinterpret_cast<uint16_t*>(dU),
+                                   reinterpret_cast<uint16_t*>(dQp), B, R, h, scale}, stream);
+    }
+    if (e == hipSuccess && p.kind != kCachedHeads) {
+        sa::ProfScope ps("cached_key_side", stream);   // dQp[., head i] = dU[., i] W_K^(i)
+        e = sa::launch_gemm({dU, bf, D, hD, 1, Wk, bf, dh, D, 1, dQp, bf, dh, D, BR, dh, D, h, 1.f, false}, stream);
     }
     if (e == hipSuccess) {
         sa::ProfScope ps("cached_weight_grads", stream);

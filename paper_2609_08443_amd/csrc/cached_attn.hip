@@ -21,7 +21,6 @@
 // The running maximum, the sum and both accumulators are fp32; the weights are rounded to
 // bf16 as matrix-core operands, the result once.
 #include <algorithm>
-#include <cstdlib>
 #include <type_traits>
 
 #include "cache.h"
@@ -50,7 +49,8 @@ struct AttnArgs {
     bool out_bf16;
     int32_t R, h, dh;               // dh a multiple of 32; N = R h, row_tiles tiles of targets a head
     // backward: out is dQp (bf16), C is written too
-    const uint16_t* dout;           // [B][R][D]
+    const uint16_t* dout;           // [B][R][D] (whole heads)
+    const uint16_t* dC;             // [B][N][D] (else)
     uint16_t* dU;                   // [B][N][D]
     float scale;
 };
@@ -265,6 +265,35 @@ __device__ __forceinline__ void project_rows(const uint16_t* Qp, const uint16_t*
                 128 * wave + 16 * e + 4 * q < D
                     ? make_uint2(tile::pack_bf16x2(u[e][rm][0], u[e][rm][1]), tile::pack_bf16x2(u[e][rm][2], u[e][rm][3]))
                     : make_uint2(0u, 0u);
+}
+
+// 16 RM rows of D values into LDS, zeros past D; rows past the last repeat it
+template <int RM>
+__device__ __forceinline__ void load_rows(const uint16_t* U, int D, int rows, int waves, int wave, int lane, uint16_t* Ul,
+                                          int chunks) {
+    if (D % 128 == 0) {   // straight into LDS, each lane the chunk that belongs at its place
+        for (int i = wave * 64; i < 16 * RM * chunks; i += waves * 64) {
+            const int r = (i + lane) / chunks, c = ((i + lane) % chunks) ^ (r & 7);
+            tile::load_lds16(U + (int64_t)min(r, rows - 1) * D + 8 * c, Ul + (int64_t)i * 8);
+        }
+        tile::wait_vmem();
+        return;
+    }
+    for (int i = threadIdx.x; i < 16 * RM * chunks; i += blockDim.x) {
+        const int r = i / chunks, c = i % chunks;
+        const uint16_t* from = U + (int64_t)min(r, rows - 1) * D + 8 * c;
+        uint32_t v[4] = {0u, 0u, 0u, 0u};
+        if (D % 8 == 0) {
+            if (8 * c < D) {
+                const uint4 x = *reinterpret_cast<const uint4*>(from);
+                v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+            }
+        } else {
+            for (int j = 0; j < 8; ++j)
+                if (8 * c + j < D) v[j / 2] |= (uint32_t)from[j] << (16 * (j & 1));
+        }
+        *reinterpret_cast<uint4*>(Ul + at16(r, c, chunks)) = make_uint4(v[0], v[1], v[2], v[3]);
+    }
 }
 
 // out = c W of one head, c [16 RM][128 waves] in accumulators (rows rm 16 + 4 q + i, columns
@@ -551,30 +580,8 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
     if constexpr (HEADS) {
         project_rows<RM>(a.Qp + urow * D + head * a.dh, a.Wk + head * a.dh, D, a.dh, rows, wave, lane, Ul, chunks,
                          Ul + waves * 128 * 64);
-    } else if (D % 128 == 0) {
-        // rows u straight into LDS, each lane the chunk that belongs at its place; rows past the
-        // last repeat it
-        for (int i = wave * 64; i < 16 * RM * chunks; i += waves * 64) {
-            const int r = (i + lane) / chunks, c = ((i + lane) % chunks) ^ (r & 7);
-            tile::load_lds16(a.U + (urow + min(r, rows - 1)) * D + 8 * c, Ul + (int64_t)i * 8);
-        }
-        tile::wait_vmem();
-    } else {   // zeros past D
-        for (int i = threadIdx.x; i < 16 * RM * chunks; i += blockDim.x) {
-            const int r = i / chunks, c = i % chunks;
-            const uint16_t* from = a.U + (urow + min(r, rows - 1)) * D + 8 * c;
-            uint32_t v[4] = {0u, 0u, 0u, 0u};
-            if (D % 8 == 0) {
-                if (8 * c < D) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(from);
-                    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-                }
-            } else {
-                for (int j = 0; j < 8; ++j)
-                    if (8 * c + j < D) v[j / 2] |= (uint32_t)from[j] << (16 * (j & 1));
-            }
-            *reinterpret_cast<uint4*>(Ul + at16(r, c, chunks)) = make_uint4(v[0], v[1], v[2], v[3]);
-        }
+    } else {
+        load_rows<RM>(a.U + urow * D, D, rows, waves, wave, lane, Ul, chunks);
     }
     __syncthreads();
 
@@ -725,15 +732,15 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
     }
 }
 
-// The backward of one head's targets towards its queries, everything around the attention that
-// needs no sum over users: with U = Qp_i W_K^(i)T and dC = dout_i W_V^(i)T (in LDS one after the
+// The attention's backward: of rows u and their aggregates' gradients dC (in LDS one after the
 // other)
 //   alpha = softmax(scale U X^T),  C = alpha X,
-//   dA = dC X^T,  ds = scale alpha (dA - sum alpha dA),  dU = ds X,  dQp_i = dU W_K^(i),
-// C and dU left in memory for the weights' gradients.  All keys in one chunk: the weights wait in
-// registers, fp32, while C is summed and dA computed.  Four products of the forward's kind, each
-// decoding the codes once.
-template <int BITS, int RM, int KT>
+//   dA = dC X^T,  ds = scale alpha (dA - sum alpha dA),  dU = ds X,
+// C and dU for the weights' gradients.  All keys in one chunk: the weights wait in registers,
+// fp32, while C is summed and dA computed.  Four products of the forward's kind, each decoding
+// the codes once.  HEADS: the rows are one head's targets, and the workgroup makes
+// U = Qp_i W_K^(i)T and dC = dout_i W_V^(i)T itself, and dQp_i = dU W_K^(i).
+template <int BITS, int RM, int KT, bool HEADS>
 __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
     extern __shared__ uint4 smem[];
     const int waves = blockDim.x >> 6, chunks = 16 * waves, KC = chunk_keys(KT, waves);
@@ -748,21 +755,25 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
     const int D = a.c.D;
     const uint32_t bh = id / (uint32_t)a.row_tiles;
     const int row0 = (int)(id - bh * (uint32_t)a.row_tiles) * 16 * RM;
-    const int64_t b = bh / (uint32_t)a.h;
-    const int head = (int)(bh - (uint32_t)b * (uint32_t)a.h), rows = min(16 * RM, a.R - row0);
+    const int64_t b = HEADS ? bh / (uint32_t)a.h : bh;
+    const int head = HEADS ? (int)(bh - (uint32_t)b * (uint32_t)a.h) : 0;
+    const int rows = min(16 * RM, (HEADS ? a.R : a.N) - row0);
     int32_t n;
     const uint8_t* const codes = cache_slot(a.c, b, &n);
     const uint8_t* const scales = codes + a.c.scales_at;
-    const int64_t urow = b * a.R + row0;
-    const int col = 8 * (wave * 16 + l16);   // this lane's columns of C and dU (D is a multiple of 32)
+    const int64_t urow = b * (HEADS ? a.R : a.N) + row0;
+    // row r of C and dU, [B][R][h][D]
+    auto place = [&](int r) { return (HEADS ? (urow + r) * a.h + head : urow + r) * D; };
+    const int col = 8 * (wave * 16 + l16);   // this lane's columns of C and dU
     if (n <= 0) {
-        for (int i = threadIdx.x; i < rows * (D / 8); i += blockDim.x) {
-            const int64_t to = ((urow + i / (D / 8)) * a.h + head) * D + 8 * (i % (D / 8));
-            *reinterpret_cast<uint4*>(a.C + to) = make_uint4(0u, 0u, 0u, 0u);
-            *reinterpret_cast<uint4*>(a.dU + to) = make_uint4(0u, 0u, 0u, 0u);
+        for (int i = threadIdx.x; i < rows * D; i += blockDim.x) {
+            const int64_t to = place(i / D) + i % D;
+            a.C[to] = 0;
+            a.dU[to] = 0;
         }
-        for (int i = threadIdx.x; i < rows * a.dh; i += blockDim.x)
-            reinterpret_cast<uint16_t*>(a.out)[(urow + i / a.dh) * D + head * a.dh + i % a.dh] = 0;
+        if constexpr (HEADS)
+            for (int i = threadIdx.x; i < rows * a.dh; i += blockDim.x)
+                reinterpret_cast<uint16_t*>(a.out)[(urow + i / a.dh) * D + head * a.dh + i % a.dh] = 0;
         return;
     }
     const int first = 2 * (int)((uint32_t)(3 * wave + 5 * id) % (uint32_t)(chunks / 8));
@@ -770,7 +781,10 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
     const Keys keys = wave_keys<KT>(0, n, waves, wave);
     uint16_t* const Ql = Ul + waves * 128 * 64;
 
-    project_rows<RM>(a.Qp + urow * D + head * a.dh, a.Wk + head * a.dh, D, a.dh, rows, wave, lane, Ul, chunks, Ql);
+    if constexpr (HEADS)
+        project_rows<RM>(a.Qp + urow * D + head * a.dh, a.Wk + head * a.dh, D, a.dh, rows, wave, lane, Ul, chunks, Ql);
+    else
+        load_rows<RM>(a.U + urow * D, D, rows, waves, wave, lane, Ul, chunks);
     __syncthreads();
     f32x4 S[KT][RM];   // logits, then weights before their division by the sum
     wave_logits<BITS, RM, KT>(a, codes, scales, Ul, Sl, chunks, keys, n, first, lane, -INFINITY, S);
@@ -835,8 +849,14 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
                 float v[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = acc[j][rm][i] * f[rm][i];
-                if (r < rows && col < D)
-                    *reinterpret_cast<uint4*>(to + ((urow + r) * a.h + head) * D + col) = __builtin_bit_cast(uint4, tile::pack8(v));
+                if (r >= rows || col >= D) continue;
+                if (HEADS || D % 8 == 0) {
+                    *reinterpret_cast<uint4*>(to + place(r) + col) = __builtin_bit_cast(uint4, tile::pack8(v));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (col + j < D) to[place(r) + col + j] = tile::to_bf16(v[j]);
+                }
             }
     };
     clear();
@@ -850,7 +870,10 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
         store(a.C, f);
     }
     __syncthreads();   // the weights in LDS have been read
-    project_rows<RM>(a.dout + urow * D + head * a.dh, a.Wv + head * a.dh, D, a.dh, rows, wave, lane, Ul, chunks, Ql);
+    if constexpr (HEADS)
+        project_rows<RM>(a.dout + urow * D + head * a.dh, a.Wv + head * a.dh, D, a.dh, rows, wave, lane, Ul, chunks, Ql);
+    else
+        load_rows<RM>(a.dC + urow * D, D, rows, waves, wave, lane, Ul, chunks);
     __syncthreads();
     f32x4 T[KT][RM];   // gradients of the weights
     wave_logits<BITS, RM, KT>(a, codes, scales, Ul, Sl, chunks, keys, n, first, lane, 0.f, T);
@@ -892,6 +915,7 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) one[rm][i] = 1.f;
     store(a.dU, one);
+    if constexpr (!HEADS) return;
     __syncthreads();
     project_out<RM>(a, acc, one, a.Wk + head * a.dh, rows, urow, head, waves, wave, lane, Ul);
 }
@@ -951,198 +975,211 @@ hipError_t launch_instance(const AttnArgs& a, hipStream_t stream) {
     return hipGetLastError();
 }
 
+// The forward's workgroups: 16 rm rows u, of one head's targets (heads; rm 1 to 4) or of all of a
+// user's (rm 1, 2 or 4, and splits of its keys where workgroups would be too few).  rm above 2
+// takes all keys in one chunk.
 struct AttnPlan {
-    int variant;   // 0: 16 rows u a workgroup, 1: 32, 2: 64 with all keys in one chunk
-    int row_tiles, splits, split_keys;
+    bool heads = false;
+    int rm = 0, row_tiles = 0, splits = 1, split_keys = 0;
 };
 
-AttnPlan attn_plan(int64_t B, int32_t N, int32_t k, int32_t D) {
-    AttnPlan p;
+// By estimated time (us).  Measured at k = 512, D = 1024, h = 16, fp4, whole calls: heads in 16,
+// 32, 48, 64 rows / all rows in 16, 32, 64:
+//   R = 1,   B = 1      31   36   40   47 /  34   36   42
+//   R = 1,   B = 64    105  125  140  165 /  41   43   48
+//   R = 4,   B = 64    105  125  141  165 /  44   55   65
+//   R = 8,   B = 64    105  126  141  165 /  68   53   78
+//   R = 16,  B = 16     35   40   44   50 /  47   55   64
+//   R = 16,  B = 64    105  126  141  166 / 107   83   68
+//   R = 40,  B = 32    146  126   78   91 / 129  108  103
+//   R = 300, B = 1      55   38   43   49 /  66   52   73
+//   R = 300, B = 4     122   94   76   88 / 127  107  103
+// that is, heads: 9 and a round of workgroups 5 + 2.5 rm and 13.5 + 2.7 rm for 512 keys (at
+// k = 1024 40, 46, 54, 63 a round); all rows: 27, 3 and the partial sums' bytes to join splits, and a round 5 and 15, 22 or
+// 33 for 512 keys.  Widths below 1024 scale both, not below a half: latency.
+AttnPlan attn_plan(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
     const int waves = (D + 127) / 128;
-    p.variant = N <= 16 ? 0 : N > 32 && k <= chunk_keys(8, waves) ? 2 : 1;
-#ifdef SA_EXPERIMENT
-    if (getenv("SA_V")) p.variant = atoi(getenv("SA_V"));
-#endif
-    const int rows = 16 << p.variant;
-    p.row_tiles = (N + rows - 1) / rows;
-    const int64_t wgs = B * p.row_tiles;
-    int64_t most = std::max<int64_t>(1, device_cus() / std::max<int64_t>(wgs, 1));
-    const int least = 16 * waves < 32 ? 32 : 16 * waves;   // keys that give every wave a tile
-    int64_t keys = std::max<int64_t>(least, (k + most - 1) / most);
-    p.split_keys = (int)((keys + 31) / 32 * 32);
-    p.splits = (k + p.split_keys - 1) / p.split_keys;
+    const int64_t slots = (int64_t)device_cus() * std::max(1, 8 / waves);   // eight waves a compute unit
+    const double width = std::max(0.5, D / 1024.0);
+    B = std::max<int64_t>(B, 1);
+    const bool one = k <= chunk_keys(8, waves);
+    AttnPlan p;
+    double best = 0;
+    auto consider = [&](AttnPlan c, double cost) {
+        if (p.rm == 0 || cost < best) p = c, best = cost;
+    };
+    if (D % h == 0 && (D / h) % 32 == 0) {
+        for (int rm = 1; rm <= (one ? 4 : 2); ++rm) {
+            AttnPlan c;
+            c.heads = true;
+            c.rm = rm;
+            c.row_tiles = (R + 16 * rm - 1) / (16 * rm);
+            c.split_keys = (k + 31) / 32 * 32;
+            const int64_t rounds = (B * h * c.row_tiles + slots - 1) / slots;
+            consider(c, 9 + rounds * width * (5 + 2.5 * rm + (13.5 + 2.7 * rm) * k / 512));
+        }
+    }
+    const int64_t N = (int64_t)R * h;
+    for (int rm = 1; rm <= (one ? 4 : 2); rm *= 2) {
+        AttnPlan c;
+        c.rm = rm;
+        c.row_tiles = (int)((N + 16 * rm - 1) / (16 * rm));
+        const int64_t wgs = B * c.row_tiles, most = std::max<int64_t>(1, slots / wgs);
+        const int least = std::max(32, 16 * waves);   // keys that give every wave a tile
+        const int64_t keys = std::max<int64_t>(least, (k + most - 1) / most);
+        c.split_keys = (int)((keys + 31) / 32 * 32);
+        c.splits = (k + c.split_keys - 1) / c.split_keys;
+        const int64_t rounds = (wgs * c.splits + slots - 1) / slots;
+        const double key = rm == 1 ? 15 : rm == 2 ? 22 : 33;
+        const double join = c.splits > 1 ? 3 + 8.0 * c.splits * B * N * D / 5e6 : 0;   // written and read at 5 TB/s
+        consider(c, 27 + join + rounds * width * (5 + key * std::min(k, c.split_keys) / 512));
+    }
     return p;
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
-// Rows u of a workgroup (in 16s) where workgroups take one head's targets, or 0 where
-// they do not.
-int heads_tiles(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
-    if (D % h != 0 || (D / h) % 32 != 0) return 0;
-#ifdef SA_EXPERIMENT
-    if (getenv("SA_H")) return atoi(getenv("SA_H"));
-#endif
-    if (R < 12 || B * h * ((R + 63) / 64) < device_cus() / 2) return 0;
-    const bool one = k <= chunk_keys(8, (D + 127) / 128);
-    int best = 0;
-    int64_t cost = 0;
-    for (int rm = 2; rm <= (one ? 4 : 2); ++rm) {
-        const int64_t wgs = B * h * ((R + 16 * rm - 1) / (16 * rm));
-        const int64_t c = (wgs + device_cus() - 1) / device_cus() * (rm + 1);
-        if (best == 0 || c <= cost) best = rm, cost = c;
+template <int BITS>
+hipError_t launch_plan(const AttnPlan& p, const AttnArgs& a, hipStream_t stream) {
+    if (p.heads) {
+        if (p.rm == 1) return launch_instance<BITS, 1, 8, true, true>(a, stream);
+        if (p.rm == 2) return launch_instance<BITS, 2, 8, true, true>(a, stream);
+        if (p.rm == 3) return launch_instance<BITS, 3, 8, false, true>(a, stream);
+        return launch_instance<BITS, 4, 8, false, true>(a, stream);
     }
-    return best;
+    if (p.rm == 1) return launch_instance<BITS, 1, 8, true, false>(a, stream);
+    if (p.rm == 2) return launch_instance<BITS, 2, 8, true, false>(a, stream);
+    return launch_instance<BITS, 4, 8, false, false>(a, stream);
 }
 
 }  // namespace
 
-bool cached_heads_supported(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) { return heads_tiles(B, R, h, k, D) > 0; }
+int cached_attn_kind(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
+    if (D > 1024) return 0;
+    return attn_plan(B, R, h, k, D).heads ? 2 : 1;
+}
 
-hipError_t launch_cached_heads(const CacheView& c, int bits, const uint16_t* Qp, const uint16_t* Wk, const uint16_t* Wv,
-                               void* out, bool out_bf16, float* lse, int64_t B, int32_t R, int32_t h, float scale,
-                               hipStream_t stream) {
-    const int rm = heads_tiles(B, R, h, c.k, c.D);
+size_t cached_attn_workspace(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
+    const AttnPlan p = attn_plan(B, R, h, k, D);
+    if (p.splits <= 1) return 0;
+    const size_t rows = (size_t)p.splits * B * R * h;
+    return up256(rows * sizeof(float2)) + rows * D * 4;
+}
+
+hipError_t launch_cached_attn(const CacheView& c, int bits, const CachedAttnArgs& f, hipStream_t stream) {
+    const AttnPlan p = attn_plan(f.B, f.R, f.h, c.k, c.D);
     AttnArgs a{};
     a.c = c;
-    a.lse = lse;
-    a.B = B;
-    a.N = R * h;
-    a.row_tiles = (R + 16 * rm - 1) / (16 * rm);
-    a.splits = 1;
-    a.split_keys = (c.k + 31) / 32 * 32;
-    a.scale2 = scale * tile::kLog2e;
-    a.Qp = Qp;
-    a.Wk = Wk;
-    a.Wv = Wv;
-    a.out = out;
-    a.out_bf16 = out_bf16;
-    a.R = R;
-    a.h = h;
-    a.dh = c.D / h;
-    if (bits == 4) {
-        if (rm == 2) return launch_instance<4, 2, 8, true, true>(a, stream);
-        if (rm == 3) return launch_instance<4, 3, 8, false, true>(a, stream);
-        if (rm == 4) return launch_instance<4, 4, 8, false, true>(a, stream);
-    } else {
-        if (rm == 2) return launch_instance<8, 2, 8, true, true>(a, stream);
-        if (rm == 3) return launch_instance<8, 3, 8, false, true>(a, stream);
-        if (rm == 4) return launch_instance<8, 4, 8, false, true>(a, stream);
-    }
-    return hipErrorInvalidValue;
+    a.U = f.U;
+    a.C = f.C;
+    a.lse = f.lse;
+    a.B = f.B;
+    a.R = f.R;
+    a.h = f.h;
+    a.N = f.R * f.h;
+    a.row_tiles = p.row_tiles;
+    a.splits = p.splits;
+    a.split_keys = p.split_keys;
+    a.scale2 = f.scale * tile::kLog2e;
+    a.part_ml = reinterpret_cast<float2*>(f.part);
+    a.part_c = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(f.part) + up256((size_t)p.splits * f.B * a.N * sizeof(float2)));
+    a.Qp = f.Qp;
+    a.Wk = f.Wk;
+    a.Wv = f.Wv;
+    a.out = f.out;
+    a.out_bf16 = f.out_bf16;
+    a.dh = c.D / f.h;
+    const hipError_t e = bits == 4 ? launch_plan<4>(p, a, stream) : launch_plan<8>(p, a, stream);
+    if (e != hipSuccess || p.splits == 1) return e;
+    const int64_t threads = f.B * a.N * ((c.D + 7) / 8);
+    hipLaunchKernelGGL(cached_join_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, a);
+    return hipGetLastError();
 }
 
 namespace {
 
-// The backward's rows of a workgroup (in 16s) and tiles of 16 keys a wave; 0 rows where it does
-// not take the shape: all keys have to fit a chunk.
-int heads_bwd_tiles(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
-    if (D > 1024 || D % h != 0 || (D / h) % 32 != 0) return 0;
+// The backward's workgroups: rm 16s of rows, of one head's targets (heads) or of all of a
+// user's; rm = 0 where it does not take the shape (all keys have to fit a chunk).
+struct BwdPlan {
+    int rm = 0;
+    bool heads = false;
+};
+BwdPlan bwd_plan(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
+    BwdPlan p;
     const int waves = (D + 127) / 128;
-    if (k > chunk_keys(8, waves)) return 0;
-#ifdef SA_EXPERIMENT
-    if (getenv("SA_HB")) return atoi(getenv("SA_HB"));
-#endif
-    int best = 0;
-    int64_t cost = 0;
-    for (int rm = 1; rm <= (k <= chunk_keys(4, waves) ? 3 : 2); ++rm) {
-        const int64_t wgs = B * h * ((R + 16 * rm - 1) / (16 * rm));
-        const int64_t c = (wgs + device_cus() - 1) / device_cus() * (rm + 1);
-        if (best == 0 || c <= cost) best = rm, cost = c;
+    if (D > 1024 || k > chunk_keys(8, waves)) return p;
+    // Microseconds: rounds of workgroups, each 12.5 for every 16 rows at k = 512, D = 1024, and 22
+    // (heads: 26) for the rest at D = 1024; 15 for the three products around the rows' form.
+    // Measured there, heads in 16, 32, 48 rows / rows in 16, 32, 48 (us a call):
+    //   R = 1,  B = 16     71   82   89 /  74   82   88
+    //   R = 1,  B = 128   342  430  477 /  79   87   94
+    //   R = 8,  B = 64    199  242  267 / 129  111  115
+    //   R = 16, B = 32    122  143  156 / 129  110  114
+    //   R = 40, B = 32    287  260  179 / 245  221  194
+    //   R = 100, B = 8    261  211  224 / 264  225  240
+    const double rest = D / 1024.0, row16 = 12.5 * rest * (k / 512.0);
+    double best = 0;
+    for (int heads = 0; heads < 2; ++heads) {
+        if (heads && (D % h != 0 || (D / h) % 32 != 0)) continue;
+        for (int rm = 1; rm <= (k <= chunk_keys(4, waves) ? 3 : 2); ++rm) {
+            const int64_t wgs = heads ? B * h * ((R + 16 * rm - 1) / (16 * rm)) : B * (((int64_t)R * h + 16 * rm - 1) / (16 * rm));
+            const double rounds = (double)((wgs + device_cus() - 1) / device_cus());
+            const double cost = rounds * (rm * row16 + (heads ? 26 : 22) * rest) + (heads ? 0 : 15);
+            if (p.rm == 0 || cost <= best) p.rm = rm, p.heads = heads != 0, best = cost;
+        }
     }
-    return best;
+    return p;
 }
 
-template <int BITS, int RM, int KT>
+template <int BITS, int RM, int KT, bool HEADS>
 hipError_t launch_bwd_instance(const AttnArgs& a, hipStream_t stream) {
     const int waves = (a.c.D + 127) / 128;
-    const int lds = lds_bytes<RM, KT, false, true>(waves);
-    auto kern = cached_attn_bwd_kernel<BITS, RM, KT>;
+    const int lds = lds_bytes<RM, KT, false, HEADS>(waves);
+    auto kern = cached_attn_bwd_kernel<BITS, RM, KT, HEADS>;
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(a.B * a.row_tiles * a.h)), dim3(64 * waves), lds, stream, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(a.B * a.row_tiles * (HEADS ? a.h : 1))), dim3(64 * waves), lds, stream, a);
     return hipGetLastError();
+}
+template <int BITS, bool HEADS>
+hipError_t launch_bwd_rows(const AttnArgs& a, int rm, hipStream_t stream) {
+    if (rm == 1) return launch_bwd_instance<BITS, 1, 8, HEADS>(a, stream);
+    if (rm == 2) return launch_bwd_instance<BITS, 2, 8, HEADS>(a, stream);
+    if (rm == 3) return launch_bwd_instance<BITS, 3, 4, HEADS>(a, stream);
+    return hipErrorInvalidValue;
 }
 
 }  // namespace
 
-bool cached_heads_bwd_supported(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
-    return heads_bwd_tiles(B, R, h, k, D) > 0;
+int cached_bwd_kind(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
+    const BwdPlan p = bwd_plan(B, R, h, k, D);
+    return p.rm == 0 ? 0 : p.heads ? 2 : 1;
 }
 
-hipError_t launch_cached_heads_bwd(const CacheView& c, int bits, const uint16_t* Qp, const uint16_t* dout,
-                                   const uint16_t* Wk, const uint16_t* Wv, uint16_t* C, uint16_t* dU, uint16_t* dQp,
-                                   int64_t B, int32_t R, int32_t h, float scale, hipStream_t stream) {
-    const int rm = heads_bwd_tiles(B, R, h, c.k, c.D);
+hipError_t launch_cached_bwd(const CacheView& c, int bits, const CachedBwdArgs& f, hipStream_t stream) {
+    const BwdPlan p = bwd_plan(f.B, f.R, f.h, c.k, c.D);
     AttnArgs a{};
     a.c = c;
-    a.C = C;
-    a.B = B;
-    a.N = R * h;
-    a.row_tiles = (R + 16 * rm - 1) / (16 * rm);
-    a.scale2 = scale * tile::kLog2e;
-    a.Qp = Qp;
-    a.Wk = Wk;
-    a.Wv = Wv;
-    a.out = dQp;
+    a.U = f.U;
+    a.C = f.C;
+    a.B = f.B;
+    a.N = f.R * f.h;
+    a.row_tiles = ((p.heads ? f.R : a.N) + 16 * p.rm - 1) / (16 * p.rm);
+    a.scale2 = f.scale * tile::kLog2e;
+    a.Qp = f.Qp;
+    a.Wk = f.Wk;
+    a.Wv = f.Wv;
+    a.out = f.dQp;
     a.out_bf16 = true;
-    a.R = R;
-    a.h = h;
-    a.dh = c.D / h;
-    a.dout = dout;
-    a.dU = dU;
-    a.scale = scale;
-    if (bits == 4) {
-        if (rm == 1) return launch_bwd_instance<4, 1, 8>(a, stream);
-        if (rm == 2) return launch_bwd_instance<4, 2, 8>(a, stream);
-        if (rm == 3) return launch_bwd_instance<4, 3, 4>(a, stream);
-    } else {
-        if (rm == 1) return launch_bwd_instance<8, 1, 8>(a, stream);
-        if (rm == 2) return launch_bwd_instance<8, 2, 8>(a, stream);
-        if (rm == 3) return launch_bwd_instance<8, 3, 4>(a, stream);
-    }
-    return hipErrorInvalidValue;
-}
-
-bool cached_attn_supported(int32_t D) { return D <= 1024; }
-
-size_t cached_attn_workspace(int64_t B, int32_t N, int32_t k, int32_t D) {
-    const AttnPlan p = attn_plan(B, N, k, D);
-    if (p.splits <= 1) return 0;
-    return up256((size_t)p.splits * B * N * sizeof(float2)) + (size_t)p.splits * B * N * D * 4;
-}
-
-hipError_t launch_cached_attn(const CacheView& c, int bits, const uint16_t* U, uint16_t* C, float* lse, void* part,
-                              int64_t B, int32_t N, float scale, hipStream_t stream) {
-    if (B <= 0 || N <= 0) return hipSuccess;
-    const AttnPlan p = attn_plan(B, N, c.k, c.D);
-    AttnArgs a;
-    a.c = c;
-    a.U = U;
-    a.C = C;
-    a.lse = lse;
-    a.part_ml = reinterpret_cast<float2*>(part);
-    a.part_c = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(part) + up256((size_t)p.splits * B * N * sizeof(float2)));
-    a.B = B;
-    a.N = N;
-    a.row_tiles = p.row_tiles;
-    a.splits = p.splits;
-    a.split_keys = p.split_keys;
-    a.scale2 = scale * tile::kLog2e;
-    hipError_t e = hipErrorInvalidValue;
-    if (bits == 4) {
-        if (p.variant == 0) e = launch_instance<4, 1, 8, true, false>(a, stream);
-        else if (p.variant == 1) e = launch_instance<4, 2, 8, true, false>(a, stream);
-        else e = launch_instance<4, 4, 8, false, false>(a, stream);
-    } else {
-        if (p.variant == 0) e = launch_instance<8, 1, 8, true, false>(a, stream);
-        else if (p.variant == 1) e = launch_instance<8, 2, 8, true, false>(a, stream);
-        else e = launch_instance<8, 4, 8, false, false>(a, stream);
-    }
-    if (e != hipSuccess || p.splits == 1) return e;
-    const int64_t threads = B * N * ((c.D + 7) / 8);
-    hipLaunchKernelGGL(cached_join_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, a);
-    return hipGetLastError();
+    a.R = f.R;
+    a.h = f.h;
+    a.dh = c.D / f.h;
+    a.dout = f.dout;
+    a.dC = f.dC;
+    a.dU = f.dU;
+    a.scale = f.scale;
+    if (bits == 4) return p.heads ? launch_bwd_rows<4, true>(a, p.rm, stream) : launch_bwd_rows<4, false>(a, p.rm, stream);
+    return p.heads ? launch_bwd_rows<8, true>(a, p.rm, stream) : launch_bwd_rows<8, false>(a, p.rm, stream);
 }
 
 }  // namespace sa

@@ -224,23 +224,37 @@ hipError_t launch_cache_write(const CacheView& c, int bits, const void* Xs, bool
                               hipStream_t stream);
 // out [B][k][D]; zeros past a slot's rows
 hipError_t launch_cache_read(const CacheView& c, int bits, void* out, bool bf16, int64_t B, hipStream_t stream);
-// bf16 attention of N rows U [B][N][D] a user over its cached rows: C [B][N][D] bf16 and
-// lse [B][N]; part: cached_attn_workspace bytes (cached_attn.hip)
-bool cached_attn_supported(int32_t D);
-size_t cached_attn_workspace(int64_t B, int32_t N, int32_t k, int32_t D);
-hipError_t launch_cached_attn(const CacheView& c, int bits, const uint16_t* U, uint16_t* C, float* lse, void* part,
-                              int64_t B, int32_t N, float scale, hipStream_t stream);
-// the same with the projections around it, workgroups taking a head's targets: from Qp = q W_Q
-// [B][R][D] to out [B][R][D] (bf16 or fp32) and lse [B][R][h]
-bool cached_heads_supported(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D);
-hipError_t launch_cached_heads(const CacheView& c, int bits, const uint16_t* Qp, const uint16_t* Wk, const uint16_t* Wv,
-                               void* out, bool out_bf16, float* lse, int64_t B, int32_t R, int32_t h, float scale,
-                               hipStream_t stream);
-// its backward: C and dU [B][R][h][D] and dQp [B][R][D], bf16
-bool cached_heads_bwd_supported(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D);
-hipError_t launch_cached_heads_bwd(const CacheView& c, int bits, const uint16_t* Qp, const uint16_t* dout,
-                                   const uint16_t* Wk, const uint16_t* Wv, uint16_t* C, uint16_t* dU, uint16_t* dQp,
-                                   int64_t B, int32_t R, int32_t h, float scale, hipStream_t stream);
+// The bf16 attention in one kernel (cached_attn.hip; D up to 1024).  Kind 1: U [B][R][h][D] to C
+// [B][R][h][D], part holding cached_attn_workspace bytes; kind 2, with the projections around it:
+// Qp = q W_Q [B][R][D] to out [B][R][D] (bf16 or fp32); 0 where it does not take the width.
+struct CachedAttnArgs {
+    const uint16_t* U;                // kind 1
+    uint16_t* C;
+    void* part;
+    const uint16_t *Qp, *Wk, *Wv;     // kind 2
+    void* out;
+    bool out_bf16;
+    float* lse;                       // [B][R][h]
+    int64_t B;
+    int32_t R, h;
+    float scale;
+};
+int cached_attn_kind(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D);
+size_t cached_attn_workspace(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D);
+hipError_t launch_cached_attn(const CacheView& c, int bits, const CachedAttnArgs& f, hipStream_t stream);
+// The attention's backward in one kernel: C and dU [B][R][h][D], bf16.  Kind 1: from U and dC
+// [B][R][h][D]; kind 2: from Qp and dout [B][R][D], with dQp [B][R][D]; 0 where it does not
+// take the shape.
+struct CachedBwdArgs {
+    const uint16_t *U, *dC;              // kind 1
+    const uint16_t *Qp, *dout, *Wk, *Wv; // kind 2
+    uint16_t *C, *dU, *dQp;
+    int64_t B;
+    int32_t R, h;
+    float scale;
+};
+int cached_bwd_kind(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D);
+hipError_t launch_cached_bwd(const CacheView& c, int bits, const CachedBwdArgs& f, hipStream_t stream);
 // softmax rows over each user's valid rows (rows = B Rh of k fp32 logits) and its backward
 hipError_t launch_cached_softmax(const CacheView& c, const float* S, int64_t rows, int32_t Rh, bool bf16, void* alpha,
                                  float* lse, hipStream_t stream);
