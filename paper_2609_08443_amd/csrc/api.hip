@@ -666,7 +666,7 @@ sa::CacheView cache_view(const void* cache, const int32_t* rows, const int64_t* 
 
 // STCA over cached sketches; operand buffers in the input dtype, as in StcaPlan.
 //   kCachedHeads   workgroups take a head's targets, projections and all:
-//                  [Qp | lse | (bwd) dout in bf16 | C | dU | dQp]
+//                  [Qp | lse | (bwd) Qp in fp32 | dout in bf16 | C | dU | dQp]
 //   kCachedRows    the attention alone in one kernel:
 //                  [Qp | lse | U | C | partial results of split keys | (bwd) dout | dC | dU | dQp]
 //   kCachedProducts  in separate products over sketches read into the workspace, Xd [B,k,D]:
@@ -675,7 +675,7 @@ enum CachedKind { kCachedProducts = 0, kCachedRows = 1, kCachedHeads = 2 };
 struct CachedPlan {
     CachedKind kind = kCachedProducts;
     size_t off_xd = 0, off_qp = 0, off_u = 0, off_s = 0, off_al = 0, off_c = 0, off_lse = 0, off_part = 0, off_dob = 0,
-           off_dc = 0, off_da = 0, off_ds = 0, off_du = 0, off_dqp = 0, total = 0;
+           off_dc = 0, off_da = 0, off_ds = 0, off_du = 0, off_dqp = 0, off_qf = 0, total = 0;
 };
 
 CachedPlan plan_cached(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa_dtype dtype, bool bwd) {
@@ -701,6 +701,7 @@ CachedPlan plan_cached(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa
         p.off_al = carve(el * rows * k);
     }
     if (bwd) {
+        if (p.kind == kCachedHeads) p.off_qf = carve(4 * BR * D);
         p.off_dob = carve(dtype == SA_BF16 ? el * BR * D : 0);
         if (p.kind != kCachedHeads) p.off_dc = carve(el * rows * D);
         p.off_du = carve(el * rows * D);
@@ -724,12 +725,11 @@ struct CachedArgs {
     bool bf;
 };
 
-// Qp = q W_Q [B,R,D]
-hipError_t cached_query(const CachedArgs& a, uint8_t* ws, const CachedPlan& p, hipStream_t stream) {
+// Qp = q W_Q [B,R,D], in the operand dtype or fp32
+hipError_t cached_query(const CachedArgs& a, void* Qp, bool bf, hipStream_t stream) {
     const int32_t BR = (int32_t)(a.B * a.R), D = a.D;
     sa::ProfScope ps("cached_query_proj", stream);
-    return sa::launch_gemm({a.q, a.bf, 0, D, 1, a.Wq, a.bf, 0, D, 1, ws + p.off_qp, a.bf, 0, D, BR, D, D, 1, 1.f, false},
-                           stream);
+    return sa::launch_gemm({a.q, a.bf, 0, D, 1, a.Wq, a.bf, 0, D, 1, Qp, bf, 0, D, BR, D, D, 1, 1.f, false}, stream);
 }
 // U[., i] = Qp[., head i] W_K^(i)T [B,R,h,D] (from Qp), or dC from dout and W_V
 hipError_t cached_head_rows(const CachedArgs& a, const void* rows, const void* W, void* to, const char* name,
@@ -1780,7 +1780,7 @@ sa_status sa_stca_cached_fwd(const void* cache, const int32_t* cache_rows, int64
     hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
     const int32_t BR = (int32_t)(B * R), dh = D / h;
     if (!lse) lse = reinterpret_cast<float*>(ws + p.off_lse);
-    hipError_t e = cached_query(a, ws, p, stream);
+    hipError_t e = cached_query(a, ws + p.off_qp, bf, stream);
     if (e == hipSuccess && p.kind != kCachedHeads)
         e = cached_head_rows(a, ws + p.off_qp, Wk, ws + p.off_u, "cached_query_rows", stream);
     if (e == hipSuccess && p.kind != kCachedProducts) {
@@ -1844,7 +1844,8 @@ sa_status sa_stca_cached_bwd(const void* cache, const int32_t* cache_rows, int64
         e = sa::launch_to_bf16(reinterpret_cast<const float*>(dout), reinterpret_cast<uint16_t*>(ws + p.off_dob),
                                (int64_t)BR * D, stream);
     }
-    if (e == hipSuccess) e = cached_query(a, ws, p, stream);
+    const bool heads = p.kind == kCachedHeads;
+    if (e == hipSuccess) e = cached_query(a, heads ? ws + p.off_qf : Qp, bf && !heads, stream);
     if (p.kind != kCachedHeads) {
         if (e == hipSuccess) e = cached_head_rows(a, Qp, Wk, ws + p.off_u, "cached_query_rows", stream);
         if (e == hipSuccess) e = cached_head_rows(a, dob, Wv, dC, "cached_value_rows", stream);
@@ -1854,11 +1855,11 @@ sa_status sa_stca_cached_bwd(const void* cache, const int32_t* cache_rows, int64
         if (e == hipSuccess) e = cached_products_bwd(a, lse, ws, p, stream);
     } else if (e == hipSuccess) {
         sa::ProfScope ps("cached_attention_bwd", stream);
-        auto b16 = [](const void* x) { return reinterpret_cast<const uint16_t*>(x); };
+        auto b16 = [](void* x) { return reinterpret_cast<uint16_t*>(x); };
+        auto c16 = [](const void* x) { return reinterpret_cast<const uint16_t*>(x); };
         e = sa::launch_cached_bwd(a.cache, a.bits,
-                                  {b16(ws + p.off_u), b16(dC), b16(Qp), b16(dob), b16(Wk), b16(Wv),
-                                   reinterpret_cast<uint16_t*>(Cc), reinterpret_cast<uint16_t*>(dU),
-                                   reinterpret_cast<uint16_t*>(dQp), B, R, h, scale}, stream);
+                                  {c16(ws + p.off_u), c16(dC), reinterpret_cast<const float*>(ws + p.off_qf), c16(dob),
+                                   c16(Wk), c16(Wv), b16(Qp), b16(dQp), b16(Cc), b16(dU), B, R, h, scale}, stream);
     }
     if (e == hipSuccess && p.kind != kCachedHeads) {
         sa::ProfScope ps("cached_key_side", stream);   // dQp[., head i] = dU[., i] W_K^(i)

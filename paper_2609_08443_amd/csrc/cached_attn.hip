@@ -49,7 +49,9 @@ struct AttnArgs {
     bool out_bf16;
     int32_t R, h, dh;               // dh a multiple of 32; N = R h, row_tiles tiles of targets a head
     // backward: out is dQp (bf16), C is written too
-    const uint16_t* dout;           // [B][R][D] (whole heads)
+    const uint16_t* dout;           // [B][R][D] (whole heads; with Qp in fp32, which is left in Qb as bf16)
+    const float* Qf;
+    uint16_t* Qb;
     const uint16_t* dC;             // [B][N][D] (else)
     uint16_t* dU;                   // [B][N][D]
     float scale;
@@ -70,7 +72,7 @@ constexpr int scale_stride(int waves) { return 4 * waves * 8 + 8; }
 template <int RM, int KT, bool LOOP, bool HEADS>
 constexpr int lds_bytes(int waves) {
     const int s = lds_tiles<RM, KT, LOOP>(waves) + 16 * RM * 4 * 2 * waves + waves * 8 * scale_stride(waves);
-    const int t = HEADS ? waves * 128 * 64 * 2 + 16 * RM * 64 * 2 : 0;
+    const int t = HEADS ? waves * 128 * 64 * 2 + 16 * RM * 64 * 2 * 2 : 0;   // (targets in two parts)
     return s > t ? s : t;
 }
 
@@ -213,10 +215,12 @@ __device__ __forceinline__ void logits(const AttnArgs& a, const uint8_t* codes, 
 // place that the rows u take afterwards (loaded as operands, 16 rows a load, they took four
 // times the load path's time: 15,000 of 147,000 cycles of a workgroup of 64 rows and 1,024
 // keys), and the targets' values once for all waves.  Columns of u are the result's rows, so
-// that a lane writes four neighbouring ones; those past D are zeros.
-template <int RM>
-__device__ __forceinline__ void project_rows(const uint16_t* Qp, const uint16_t* Wk, int D, int dh, int rows, int wave,
-                                             int lane, uint16_t* Ul, int chunks, uint16_t* Ql) {
+// that a lane writes four neighbouring ones; those past D are zeros.  fp32 targets go in as two
+// bf16 parts, v = hi + lo to 2^-17 of v, and hi is left in Qb for a later product.
+template <int RM, typename T>
+__device__ __forceinline__ void project_rows(const T* Qp, const uint16_t* Wk, int D, int dh, int rows, int wave, int lane,
+                                             uint16_t* Ul, int chunks, uint16_t* Ql, uint16_t* Qb = nullptr) {
+    constexpr bool SPLIT = sizeof(T) == 4;
     const int l16 = lane & 15, q = lane >> 4;
     uint16_t* const mine = Ul + wave * (128 * 64);
     f32x4 u[8][RM];
@@ -238,21 +242,41 @@ __device__ __forceinline__ void project_rows(const uint16_t* Qp, const uint16_t*
         for (int i = threadIdx.x; i < 16 * RM * 8; i += blockDim.x) {
             const int r = i >> 3, c = i & 7;
             uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (k + 8 * c < dh) v = *reinterpret_cast<const uint4*>(Qp + (int64_t)min(r, rows - 1) * D + k + 8 * c);
+            const int64_t at = (int64_t)min(r, rows - 1) * D + k + 8 * c;
+            if constexpr (SPLIT) {
+                uint4 lo = v;
+                if (k + 8 * c < dh) {
+                    const float4 x = *reinterpret_cast<const float4*>(Qp + at), y = *reinterpret_cast<const float4*>(Qp + at + 4);
+                    v = make_uint4(tile::pack_bf16x2(x.x, x.y), tile::pack_bf16x2(x.z, x.w), tile::pack_bf16x2(y.x, y.y),
+                                   tile::pack_bf16x2(y.z, y.w));
+                    auto rest = [](uint32_t h, float a, float b) { return tile::pack_bf16x2(a - tile::bf16_lo(h), b - tile::bf16_hi(h)); };
+                    lo = make_uint4(rest(v.x, x.x, x.y), rest(v.y, x.z, x.w), rest(v.z, y.x, y.y), rest(v.w, y.z, y.w));
+                    if (r < rows) *reinterpret_cast<uint4*>(Qb + at) = v;
+                }
+                *reinterpret_cast<uint4*>(Ql + 16 * RM * 64 + at16(r, c, 8)) = lo;
+            } else if (k + 8 * c < dh) {
+                v = *reinterpret_cast<const uint4*>(Qp + at);
+            }
             *reinterpret_cast<uint4*>(Ql + at16(r, c, 8)) = v;
         }
         tile::wait_vmem();
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            bf16x8 x[RM];
+            bf16x8 x[RM], lo[RM];
 #pragma unroll
-            for (int rm = 0; rm < RM; ++rm) x[rm] = tile::lds_b128(Ql, at16(rm * 16 + l16, 4 * i + q, 8));
+            for (int rm = 0; rm < RM; ++rm) {
+                x[rm] = tile::lds_b128(Ql, at16(rm * 16 + l16, 4 * i + q, 8));
+                if constexpr (SPLIT) lo[rm] = tile::lds_b128(Ql + 16 * RM * 64, at16(rm * 16 + l16, 4 * i + q, 8));
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const bf16x8 w = tile::lds_b128(mine, at16(16 * e + l16, 4 * i + q, 8));
 #pragma unroll
-                for (int rm = 0; rm < RM; ++rm) u[e][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[rm], u[e][rm], 0, 0, 0);
+                for (int rm = 0; rm < RM; ++rm) {
+                    if constexpr (SPLIT) u[e][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, lo[rm], u[e][rm], 0, 0, 0);
+                    u[e][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[rm], u[e][rm], 0, 0, 0);
+                }
             }
         }
     }
@@ -300,8 +324,9 @@ __device__ __forceinline__ void load_rows(const uint16_t* U, int D, int rows, in
 // 8 (16 wave + l16) + j): each wave multiplies its own 128 columns of c, through its own part
 // of LDS into operand order, with their rows of W [D][dh of D], 64 columns of out at a time;
 // the waves' sums meet in LDS.  W's operands are blocks of 8 rows x 4 columns, paired by byte
-// permutes as the codes are.  All waves have left LDS before.
-template <int RM>
+// permutes as the codes are.  All waves have left LDS before.  SPLIT: c goes in as two bf16
+// parts, its leading 8 bits and the next.
+template <int RM, bool SPLIT>
 __device__ __forceinline__ void project_out(const AttnArgs& a, const f32x4 (&acc)[8][RM], const float (&inv)[RM][4],
                                    const uint16_t* W, int rows, int64_t row0, int head, int waves, int wave, int lane,
                                    uint16_t* lds) {
@@ -320,22 +345,28 @@ __device__ __forceinline__ void project_out(const AttnArgs& a, const f32x4 (&acc
     };
     fetch(0, 0);
     fetch(1, 0);
+    bf16x8 c[SPLIT ? 2 : 1][4][RM];
 #pragma unroll
-    for (int rm = 0; rm < RM; ++rm)
+    for (int part = 0; part < (SPLIT ? 2 : 1); ++part) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float v[8];
+        for (int rm = 0; rm < RM; ++rm)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = in ? acc[j][rm][i] * inv[rm][i] : 0.f;
-            *reinterpret_cast<uint4*>(mine + at16(rm * 16 + 4 * q + i, l16, 16)) = __builtin_bit_cast(uint4, tile::pack8(v));
-        }
-    tile::wave_lds_order();
-    bf16x8 c[4][RM];
+            for (int i = 0; i < 4; ++i) {
+                float v[8];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+                for (int j = 0; j < 8; ++j) {
+                    v[j] = in ? acc[j][rm][i] * inv[rm][i] : 0.f;
+                    if (part == 1) v[j] -= tile::bf16_lo(tile::to_bf16(v[j]));
+                }
+                *reinterpret_cast<uint4*>(mine + at16(rm * 16 + 4 * q + i, l16, 16)) = __builtin_bit_cast(uint4, tile::pack8(v));
+            }
+        tile::wave_lds_order();
 #pragma unroll
-        for (int rm = 0; rm < RM; ++rm) c[k][rm] = tile::lds_b128(mine, at16(rm * 16 + l16, 4 * k + q, 16));
-    tile::wave_lds_order();
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int rm = 0; rm < RM; ++rm) c[part][k][rm] = tile::lds_b128(mine, at16(rm * 16 + l16, 4 * k + q, 16));
+        tile::wave_lds_order();
+    }
     for (int j0 = 0; j0 < a.dh; j0 += 64) {
         f32x4 o[4][RM];
 #pragma unroll
@@ -354,7 +385,10 @@ __device__ __forceinline__ void project_out(const AttnArgs& a, const f32x4 (&acc
                                                  (j & 1) ? 0x07060302u : 0x05040100u);
                 const bf16x8 b = __builtin_bit_cast(bf16x8, make_uint4(p[0], p[1], p[2], p[3]));
 #pragma unroll
-                for (int rm = 0; rm < RM; ++rm) o[j][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c[k][rm], b, o[j][rm], 0, 0, 0);
+                for (int rm = 0; rm < RM; ++rm) {
+                    if constexpr (SPLIT) o[j][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c[1][k][rm], b, o[j][rm], 0, 0, 0);
+                    o[j][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c[0][k][rm], b, o[j][rm], 0, 0, 0);
+                }
             }
             if (k < 2) fetch(k + 2, j0);
             else if (j0 + 64 < a.dh) fetch(k - 2, j0 + 64);
@@ -693,7 +727,7 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) inv[rm][i] = 1.f / __shfl(l[rm], 4 * q + i, 64);
         __syncthreads();   // the weights in LDS have been read
-        project_out<RM>(a, acc, inv, a.Wv + head * a.dh, rows, urow, head, waves, wave, lane, reinterpret_cast<uint16_t*>(smem));
+        project_out<RM, false>(a, acc, inv, a.Wv + head * a.dh, rows, urow, head, waves, wave, lane, reinterpret_cast<uint16_t*>(smem));
         return;
     }
     const int col = 8 * (wave * 16 + l16);
@@ -739,7 +773,10 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
 // C and dU for the weights' gradients.  All keys in one chunk: the weights wait in registers,
 // fp32, while C is summed and dA computed.  Four products of the forward's kind, each decoding
 // the codes once.  HEADS: the rows are one head's targets, and the workgroup makes
-// U = Qp_i W_K^(i)T and dC = dout_i W_V^(i)T itself, and dQp_i = dU W_K^(i).
+// U = Qp_i W_K^(i)T and dC = dout_i W_V^(i)T itself, and dQp_i = dU W_K^(i).  Roundings to bf16 in
+// the way to dq: U, dC, ds, dQp and the result, as operands of products too large to run twice;
+// Qp and dU, of small ones, go in as two parts (with them rounded, single targets' gradients were
+// up to 0.5% off by 2-norm, now 0.4%).
 template <int BITS, int RM, int KT, bool HEADS>
 __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
     extern __shared__ uint4 smem[];
@@ -772,8 +809,11 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
             a.dU[to] = 0;
         }
         if constexpr (HEADS)
-            for (int i = threadIdx.x; i < rows * a.dh; i += blockDim.x)
-                reinterpret_cast<uint16_t*>(a.out)[(urow + i / a.dh) * D + head * a.dh + i % a.dh] = 0;
+            for (int i = threadIdx.x; i < rows * a.dh; i += blockDim.x) {
+                const int64_t at = (urow + i / a.dh) * D + head * a.dh + i % a.dh;
+                reinterpret_cast<uint16_t*>(a.out)[at] = 0;
+                a.Qb[at] = tile::to_bf16(a.Qf[at]);
+            }
         return;
     }
     const int first = 2 * (int)((uint32_t)(3 * wave + 5 * id) % (uint32_t)(chunks / 8));
@@ -782,7 +822,8 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
     uint16_t* const Ql = Ul + waves * 128 * 64;
 
     if constexpr (HEADS)
-        project_rows<RM>(a.Qp + urow * D + head * a.dh, a.Wk + head * a.dh, D, a.dh, rows, wave, lane, Ul, chunks, Ql);
+        project_rows<RM>(a.Qf + urow * D + head * a.dh, a.Wk + head * a.dh, D, a.dh, rows, wave, lane, Ul, chunks, Ql,
+                         a.Qb + urow * D + head * a.dh);
     else
         load_rows<RM>(a.U + urow * D, D, rows, waves, wave, lane, Ul, chunks);
     __syncthreads();
@@ -917,7 +958,7 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
     store(a.dU, one);
     if constexpr (!HEADS) return;
     __syncthreads();
-    project_out<RM>(a, acc, one, a.Wk + head * a.dh, rows, urow, head, waves, wave, lane, Ul);
+    project_out<RM, true>(a, acc, one, a.Wk + head * a.dh, rows, urow, head, waves, wave, lane, Ul);
 }
 
 // Joins the splits of each row: their sums and accumulators, each scaled to the common
@@ -1166,7 +1207,8 @@ hipError_t launch_cached_bwd(const CacheView& c, int bits, const CachedBwdArgs& 
     a.N = f.R * f.h;
     a.row_tiles = ((p.heads ? f.R : a.N) + 16 * p.rm - 1) / (16 * p.rm);
     a.scale2 = f.scale * tile::kLog2e;
-    a.Qp = f.Qp;
+    a.Qf = f.Qf;
+    a.Qb = f.Qb;
     a.Wk = f.Wk;
     a.Wv = f.Wv;
     a.out = f.dQp;

@@ -243,12 +243,14 @@ int cached_attn_kind(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D);
 size_t cached_attn_workspace(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D);
 hipError_t launch_cached_attn(const CacheView& c, int bits, const CachedAttnArgs& f, hipStream_t stream);
 // The attention's backward in one kernel: C and dU [B][R][h][D], bf16.  Kind 1: from U and dC
-// [B][R][h][D]; kind 2: from Qp and dout [B][R][D], with dQp [B][R][D]; 0 where it does not
-// take the shape.
+// [B][R][h][D]; kind 2: from fp32 Qp and dout [B][R][D], with dQp [B][R][D] and Qp in bf16 (Qb);
+// 0 where it does not take the shape.
 struct CachedBwdArgs {
     const uint16_t *U, *dC;              // kind 1
-    const uint16_t *Qp, *dout, *Wk, *Wv; // kind 2
-    uint16_t *C, *dU, *dQp;
+    const float* Qf;                     // kind 2
+    const uint16_t *dout, *Wk, *Wv;
+    uint16_t *Qb, *dQp;
+    uint16_t *C, *dU;
     int64_t B;
     int32_t R, h;
     float scale;
