@@ -729,6 +729,9 @@ struct CachedArgs {
 hipError_t cached_query(const CachedArgs& a, void* Qp, bool bf, hipStream_t stream) {
     const int32_t BR = (int32_t)(a.B * a.R), D = a.D;
     sa::ProfScope ps("cached_query_proj", stream);
+    if (a.bf && sa::few_rows_supported(BR, D, D))
+        return sa::launch_few_rows(reinterpret_cast<const uint16_t*>(a.q), reinterpret_cast<const uint16_t*>(a.Wq), Qp, bf,
+                                   BR, D, D, stream);
     return sa::launch_gemm({a.q, a.bf, 0, D, 1, a.Wq, a.bf, 0, D, 1, Qp, bf, 0, D, BR, D, D, 1, 1.f, false}, stream);
 }
 // U[., i] = Qp[., head i] W_K^(i)T [B,R,h,D] (from Qp), or dC from dout and W_V

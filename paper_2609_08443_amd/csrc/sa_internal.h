@@ -215,6 +215,11 @@ hipError_t launch_stca_softmax_bwd(const void* S, bool s_bf16, const float* lse,
                                    int32_t k, float scale, bool bf16, void* ds, hipStream_t stream);
 hipError_t launch_to_bf16(const float* x, uint16_t* y, int64_t n, hipStream_t stream);
 
+// C [rows][N] (bf16 or fp32) = A [rows][K] W [K][N], bf16, for one or two rows (few_rows.hip)
+bool few_rows_supported(int32_t rows, int32_t K, int32_t N);
+hipError_t launch_few_rows(const uint16_t* A, const uint16_t* W, void* C, bool c_bf16, int32_t rows, int32_t K, int32_t N,
+                           hipStream_t stream);
+
 // The sketch cache (cache.hip, cached_stca.hip; CacheView in cache.h).  bits: 4 or 8.
 struct CacheView;
 // workgroups a user of a write or a read takes

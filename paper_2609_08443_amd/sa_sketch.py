@@ -7,7 +7,6 @@ There is no fallback: if the library is missing, or a call fails, an
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import functools
 import math
@@ -664,7 +663,15 @@ def _on(device, stream):
     return torch.cuda.device(device)
 
 
-_AS_IT_IS = contextlib.nullcontext()
+class _AsItIs:
+    def __enter__(self):
+        pass
+
+    def __exit__(self, *exc):
+        pass
+
+
+_AS_IT_IS = _AsItIs()
 
 
 def _handle(device, stream) -> Optional[int]:
