@@ -5,7 +5,10 @@
 // octet of rows by 64 values at a time, lane l row l % 8 and values 8 (l / 8) ..+7:
 // each lane's values are whole 16-byte pieces, each row of the wave a run of 128
 // (bf16) or 256 bytes, the codes of the wave 256 or 512 contiguous bytes, and the four
-// lanes of a group's values find its largest magnitude in two exchanges.
+// lanes of a group's values find its largest magnitude in two exchanges.  Measured: 128
+// sketches of 512 x 1024 from bf16 to 8 bits 46 us (203 MB, 4.4 TB/s) and back 33 us, 64
+// of 1024 x 1024 from 4 bits to bf16 28 us (170 MB, 6.1 TB/s: the codes from the cache
+// behind the L2); a copy of 1 GB runs at 5.0 TB/s.
 #include "cache.h"
 
 namespace sa {
@@ -31,13 +34,13 @@ struct IoArgs {
 };
 
 // 8 values of a row from column c (columns from D on: zeros).  VEC: D is a multiple
-// of 8 (bf16) or 4 (fp32), so that pieces are aligned.
+// of 8 (bf16) or 4 (fp32), so that pieces are aligned.  Read once, and not kept in the
+// caches that the codes go into (128 sketches of 512 x 1024 bf16: write 58 -> 46 us).
 template <bool BF, bool VEC>
 __device__ inline void load8(const void* p, int64_t at, int c, int D, float (&v)[8]) {
     if constexpr (BF && VEC) {
-        uint4 q = make_uint4(0, 0, 0, 0);
-        if (c < D) q = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p) + at + c);
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        tile::u32x4 w = {0u, 0u, 0u, 0u};
+        if (c < D) w = __builtin_nontemporal_load(reinterpret_cast<const tile::u32x4*>(reinterpret_cast<const uint16_t*>(p) + at + c));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             v[2 * i] = tile::bf16_lo(w[i]);
@@ -46,9 +49,11 @@ __device__ inline void load8(const void* p, int64_t at, int c, int D, float (&v)
     } else if constexpr (VEC) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (c + 4 * i < D) q = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p) + at + c + 4 * i);
-            v[4 * i] = q.x; v[4 * i + 1] = q.y; v[4 * i + 2] = q.z; v[4 * i + 3] = q.w;
+            tile::u32x4 q = {0u, 0u, 0u, 0u};
+            if (c + 4 * i < D)
+                q = __builtin_nontemporal_load(reinterpret_cast<const tile::u32x4*>(reinterpret_cast<const float*>(p) + at + c + 4 * i));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[4 * i + j] = __uint_as_float(q[j]);
         }
     } else {
 #pragma unroll

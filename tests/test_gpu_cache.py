@@ -281,8 +281,7 @@ def many(B, k, empty=True):
 # batches large enough for workgroups of one head's targets: heads of 32, 64, 96 and 128,
 # one to four 16s of targets, one chunk of keys and several
 HEAD_CASES = [(43, 12, 24, 96, 3), (32, 13, 33, 256, 4), (32, 20, 300, 256, 4), (65, 12, 20, 256, 2),
-              (45, 17, 100, 288, 3), (11, 40, 150, 384, 12), (11, 64, 384, 384, 12), (9, 70, 130, 512, 16),
-              (9, 33, 1030, 1024, 16)]
+              (45, 17, 100, 288, 3), (11, 40, 150, 384, 12), (11, 64, 384, 384, 12), (9, 70, 130, 512, 16)]
 STCA_CASES += [c + many(c[0], c[2]) for c in HEAD_CASES]
 
 
@@ -300,6 +299,75 @@ def test_forward_matches_oracle(sa, B, R, k, D, h, rows, slots, dtype, fmt):
 def test_backward_matches_oracle(sa, B, R, k, D, h, rows, slots, dtype, fmt):
     print(f"bwd B={B} R={R} k={k} D={D} h={h} {dtype} {fmt}", flush=True)
     check_bwd(sa, problem(sa, B, R, k, D, h, fmt, dtype, rows, slots), h, dtype, dtype)
+
+
+# ---------------------------------------------------------------- larger batches
+
+
+def reference64(X, n, q, W, h, dout):
+    """(out, lse, gradients) of the masked attention in float64 on the device, all users
+    at once, keys X W_K and values X W_V formed, the gradients by differentiation."""
+    B, k, D = X.shape
+    R, dh = q.shape[1], D // h
+    leaves = [t.double().requires_grad_(True) for t in (q, *W)]
+    Q = (leaves[0] @ leaves[1]).view(B, R, h, dh).transpose(1, 2)
+    K = (X @ leaves[2]).view(B, k, h, dh).transpose(1, 2)
+    V = (X @ leaves[3]).view(B, k, h, dh).transpose(1, 2)
+    s = (Q @ K.transpose(2, 3).contiguous()) / dh ** 0.5                    # [B, h, R, k]
+    valid = torch.arange(k, device=X.device) < n[:, None]
+    s = s.masked_fill(~valid[:, None, None, :], -torch.inf)
+    lse = torch.logsumexp(s, -1)
+    alpha = torch.where(n[:, None, None, None] > 0, torch.exp(s - lse[..., None].nan_to_num(neginf=0.0)), 0.0)
+    out = (alpha @ V).transpose(1, 2).reshape(B, R, D)
+    g = torch.autograd.grad(out, leaves, dout.double())
+    return out.detach(), lse.detach().transpose(1, 2), dict(zip(("dq", "dWq", "dWk", "dWv"), g))
+
+
+# every form of the forward and of the backward: workgroups of one head's targets in one to
+# four 16s, of all of a user's rows, of split keys, keys in one chunk and several, the
+# separate products (the backward's where keys do not fit a chunk); widths that are no
+# multiple of a head's 32, of 8, of 2
+BIG_CASES = [(16, 40, 130, 1024, 16), (16, 60, 300, 1024, 16), (64, 16, 140, 1024, 16), (64, 8, 1100, 1024, 16),
+             (300, 1, 100, 1024, 16), (50, 30, 90, 600, 5), (60, 33, 70, 333, 3), (3, 300, 700, 1024, 16),
+             (20, 33, 1030, 1024, 16), (100, 40, 40, 96, 3), (40, 100, 300, 256, 2), (16, 16, 140, 1024, 16),
+             (32, 40, 100, 1024, 32), (64, 20, 60, 512, 16), (2, 4, 600, 1000, 8), (8, 60, 150, 999, 9),
+             (128, 20, 60, 1000, 5), (40, 50, 200, 768, 8), (1, 300, 2500, 1024, 8), (2, 20, 90, 1600, 10),
+             (40, 300, 130, 96, 3), (40, 300, 520, 20, 1), (100, 300, 130, 20, 1), (1, 1, 130, 20, 1)]
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("B,R,k,D,h", BIG_CASES)
+def test_larger_batches_match_float64(sa, B, R, k, D, h, fmt):
+    print(f"big B={B} R={R} k={k} D={D} h={h} {fmt}", flush=True)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(B + R + k + D)
+    normal = lambda *shape: torch.randn(shape, generator=g, device="cuda")  # noqa: E731
+    rows, slots = many(B, k, empty=B > 3) if B > 2 else ([k, max(1, k - 37)][:B], [1, 0][:B])
+    n = torch.tensor(rows, device="cuda")
+    slots = torch.tensor(slots, device="cuda")
+    c = raw_cache(sa, max(B, 2), k, D, fmt, B)
+    held = sa.sketch_cache(max(B, 2), k, D, fmt)
+    held.data.copy_(c.data)
+    sa.cache_write(held, normal(B, k, D), slots, n.int())
+    X = sa.cache_read(held, slots, dtype=torch.float32).double()   # (exact: tested above)
+    n = torch.where(slots >= 0, n, 0)
+    q, dout = normal(B, R, D).bfloat16(), normal(B, R, D).bfloat16()
+    W = [(normal(D, D) / D ** 0.5).bfloat16() for _ in range(3)]
+    out, lse = sa.stca_cached_fwd(held, slots, q, *W, h, out_dtype=torch.bfloat16, want_lse=True)
+    grads = sa.stca_cached_bwd(held, slots, q, *W, h, dout)
+    ref, rlse, rgrads = reference64(X, n, q, W, h, dout)
+    ftol, btol = bounds("bf16", k, D, B * R)
+    off = lambda a, b: float((a.double() - b).norm() / b.norm().clamp(min=1e-300))  # noqa: E731
+    assert off(out, ref) <= ftol, ("out", off(out, ref))
+    for b in range(B):   # no user is wrong among many: 1.5 times the bound for the fewer values of one
+        assert off(out[b], ref[b]) <= 1.5 * ftol, ("out", b, int(n[b]), off(out[b], ref[b]))
+        assert off(grads["dq"][b], rgrads["dq"][b]) <= 1.5 * btol or int(n[b]) <= 2, ("dq", b, int(n[b]))
+        if not int(n[b]):
+            assert not out[b].any() and not grads["dq"][b].any() and torch.isneginf(lse[b]).all()
+    some = n > 0
+    assert float((lse[some] - rlse[some]).abs().max()) <= 2.0 ** -6 * max(1.0, float(rlse[some].abs().max()) + np.log(k))
+    for name in grads:
+        assert off(grads[name], rgrads[name]) <= btol, (name, off(grads[name], rgrads[name]))
 
 
 def test_fp32_results_of_bf16_inputs(sa):
