@@ -80,6 +80,22 @@ constexpr int lds_bytes(int waves) {
 // eight neighbouring rows' chunks lie in different banks
 __device__ inline int at16(int r, int c, int chunks) { return (r * chunks + (c ^ (r & 7))) * 8; }
 
+// A user's codes and scale bytes as buffers: a lane's offset in a vector register, the step's in a
+// scalar one (as sums of pointers they took two thirds of the logits' vector instructions
+// besides the decoding), and nothing outside the slot is read.
+struct Slot {
+    __amdgpu_buffer_rsrc_t codes, scales;
+};
+__device__ inline __amdgpu_buffer_rsrc_t buffer_of(const uint8_t* p, int64_t bytes) {
+    const uint64_t u = reinterpret_cast<uint64_t>(p);
+    const uint64_t v = (uint64_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 |
+                       (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)u);
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(v), 0, (int)bytes, 0x00027000);
+}
+__device__ inline Slot slot_of(const CacheView& c, const uint8_t* codes) {
+    return {buffer_of(codes, c.scales_at), buffer_of(codes + c.scales_at, c.slot_bytes - c.scales_at)};
+}
+
 // 8 rows x 8 columns of codes with their rows' scales: the operand words of column 2 I
 // and 2 I + 1, keys in pairs
 template <int BITS, int I>
@@ -99,10 +115,11 @@ struct Block {   // 8 keys x 8 columns of codes, and the keys' scale bytes
     uint2 s;
 };
 template <int BITS>
-__device__ inline void load_block(Block<BITS>& b, const uint8_t* codes, const uint8_t* scales, uint32_t at, uint32_t sat) {
+__device__ inline void load_block(Block<BITS>& b, const Slot& x, uint32_t at, uint32_t step, uint32_t sat, uint32_t sstep) {
 #pragma unroll
-    for (int i = 0; i < BITS / 2; ++i) b.w[i] = *reinterpret_cast<const uint4*>(codes + at + 16 * i);
-    b.s = *reinterpret_cast<const uint2*>(scales + sat);
+    for (int i = 0; i < BITS / 2; ++i)
+        b.w[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(x.codes, at + 16 * i, step, 0));
+    b.s = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(x.scales, sat, sstep, 0));
 }
 
 // Logits of NT tiles of 16 keys from kb on against the 16 RM rows u in LDS, into S[T0 ..].
@@ -118,8 +135,8 @@ __device__ inline void load_block(Block<BITS>& b, const uint8_t* codes, const ui
 // from 32 G on; the codes read there are the last group's.  Octets past the slot's last
 // valid one, olast, read that one.
 template <int BITS, int RM, int T0, int NT, int KT>
-__device__ __forceinline__ void logits(const AttnArgs& a, const uint8_t* codes, const uint8_t* scales, const uint16_t* Ul,
-                                       uint8_t* Sl, int chunks, int kb, int olast, int first, int lane, f32x4 (&S)[KT][RM]) {
+__device__ __forceinline__ void logits(const AttnArgs& a, const Slot& x, const uint16_t* Ul, uint8_t* Sl, int chunks, int kb,
+                                       int olast, int first, int lane, f32x4 (&S)[KT][RM]) {
     static_assert(NT == 1 || NT == 4, "one key a lane, or four");
     constexpr int GB = NT == 1 ? 16 : 4;
     constexpr int NJ = NT == 1 ? 1 : 2;             // loads a group
@@ -137,9 +154,10 @@ __device__ __forceinline__ void logits(const AttnArgs& a, const uint8_t* codes, 
     }
     if constexpr (NT == 4) {
         const int o = lane >> 3;
-        const uint8_t* from = scales + (uint32_t)min((kb >> 3) + o, olast) * (uint32_t)G * 8;
-        for (int g = lane & 7; g < G; g += 8)
-            *reinterpret_cast<uint2*>(Sl + o * stride + 8 * g) = *reinterpret_cast<const uint2*>(from + 8 * g);
+        const uint32_t from = (uint32_t)min((kb >> 3) + o, olast) * (uint32_t)G * 8;
+        for (int g = lane & 7; g < Gp; g += 8)
+            *reinterpret_cast<uint2*>(Sl + o * stride + 8 * g) =
+                __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(x.scales, from + 8 * min(g, G - 1), 0, 0));
         tile::wave_lds_order();
     }
     const uint8_t* const sl = Sl + (l16 >> 2) * stride + 2 * (l16 & 3);
@@ -148,65 +166,78 @@ __device__ __forceinline__ void logits(const AttnArgs& a, const uint8_t* codes, 
 #pragma unroll
         for (int rm = 0; rm < RM; ++rm) S[T0 + t][rm] = (f32x4){0.f, 0.f, 0.f, 0.f};
     uint32_t w[GB][NJ][W], sc[GB];
-    auto fetch = [&](int i, int g_) {
-        const uint32_t g = (uint32_t)min(g_ < Gp ? g_ : g_ - Gp, G - 1);
+    auto fetch = [&](int i, int g) {
+        g = min(g, G - 1);
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
-            const uint8_t* p = codes + (at[j] + g * (32 * BITS));
+            const uint32_t step = (uint32_t)g * (32 * BITS);
             if constexpr (W == 4) {
-                const uint4 v = *reinterpret_cast<const uint4*>(p);
+                const uint4 v = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(x.codes, at[j], step, 0));
                 w[i][j][0] = v.x; w[i][j][1] = v.y; w[i][j][2 % W] = v.z; w[i][j][3 % W] = v.w;
             } else if constexpr (W == 2) {
-                const uint2 v = *reinterpret_cast<const uint2*>(p);
+                const uint2 v = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(x.codes, at[j], step, 0));
                 w[i][j][0] = v.x;
                 w[i][j][1 % W] = v.y;
             } else {
-                w[i][j][0] = *reinterpret_cast<const uint32_t*>(p);
+                w[i][j][0] = __builtin_amdgcn_raw_buffer_load_b32(x.codes, at[j], step, 0);
             }
         }
-        if constexpr (NT == 1) sc[i] = scales[sat + g * 8];
+        if constexpr (NT == 1) sc[i] = __builtin_amdgcn_raw_buffer_load_b8(x.scales, sat, (uint32_t)g * 8, 0);
     };
-    // the lane's chunk of row l16 in groups of even and odd number; two groups on, 128 bytes
-    const uint16_t* const u0 = Ul + at16(l16, q, chunks);
-    const uint16_t* const u1 = Ul + at16(l16, 4 + q, chunks);
-    auto multiply = [&](int i, int g) {
-        if (g >= Gp) g -= Gp;
-        bf16x8 u[RM];
+    // the lane's chunk of rows rm 16 + l16 in groups of even and odd number; two groups on, 128 bytes
+    const uint16_t* u[2][RM];
 #pragma unroll
-        for (int rm = 0; rm < RM; ++rm)
-            u[rm] = tile::lds_b128((i & 1) ? u1 : u0, rm * 16 * chunks * 8 + (g >> 1) * 64);
+    for (int rm = 0; rm < RM; ++rm) {
+        u[0][rm] = Ul + at16(l16, q, chunks) + rm * 16 * chunks * 8;
+        u[1][rm] = Ul + at16(l16, 4 + q, chunks) + rm * 16 * chunks * 8;
+    }
+    // group base + i, base a multiple of four
+    auto multiply = [&](int i, int base) {
+        bf16x8 y[RM];
+#pragma unroll
+        for (int rm = 0; rm < RM; ++rm) y[rm] = tile::lds_b128(u[i & 1][rm] + (base >> 1) * 64, (i >> 1) * 64);
+        const uint8_t* const sg = sl + 8 * base;
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
             uint32_t s2;
             if constexpr (NT == 1) s2 = sc[i];
-            else s2 = *reinterpret_cast<const uint16_t*>(sl + j * 4 * stride + 8 * min(g, G - 1));
+            else s2 = *reinterpret_cast<const uint16_t*>(sg + j * 4 * stride + 8 * i);
 #pragma unroll
             for (int t = 0; t < NT / NJ; ++t) {
                 uint32_t c[BITS / 4];
 #pragma unroll
-                for (int x = 0; x < BITS / 4; ++x) c[x] = w[i][j][t * (BITS / 4) + x];
-                const bf16x8 x = __builtin_bit_cast(bf16x8, decode8<BITS>(c, scale_float((s2 >> (8 * t)) & 255u)));
+                for (int v = 0; v < BITS / 4; ++v) c[v] = w[i][j][t * (BITS / 4) + v];
+                const bf16x8 z = __builtin_bit_cast(bf16x8, decode8<BITS>(c, scale_float((s2 >> (8 * t)) & 255u)));
 #pragma unroll
                 for (int rm = 0; rm < RM; ++rm)
-                    S[T0 + 2 * j + t][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, u[rm], S[T0 + 2 * j + t][rm], 0, 0, 0);
+                    S[T0 + 2 * j + t][rm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(z, y[rm], S[T0 + 2 * j + t][rm], 0, 0, 0);
             }
         }
     };
+    if constexpr (NT == 4) {
+        // from group `first` (a multiple of four, as Gp) round to it again
 #pragma unroll
-    for (int i = 0; i < GB; ++i) fetch(i, first + i);
-    int g0 = 0;
-    for (; g0 + GB <= Gp; g0 += GB) {
+        for (int i = 0; i < 4; ++i) fetch(i, first + i);
+        int base = first;
+        for (int g0 = 0; g0 < Gp; g0 += 4) {
+            const int next = base + 4 < Gp ? base + 4 : 0;
 #pragma unroll
-        for (int i = 0; i < GB; ++i) {
-            multiply(i, first + g0 + i);
-            const int next = g0 + GB + i;
-            fetch(i, first + (next < Gp ? next : 0));
+            for (int i = 0; i < 4; ++i) {
+                multiply(i, base);
+                fetch(i, next + i);
+            }
+            base = next;
         }
-    }
-    if constexpr (GB > 4) {   // (Gp is a multiple of 4)
+    } else {
 #pragma unroll
-        for (int i = 0; i < GB; ++i)
-            if (g0 + i < Gp) multiply(i, first + g0 + i);
+        for (int i = 0; i < GB; ++i) fetch(i, i);
+        for (int g0 = 0; g0 < Gp; g0 += GB) {
+#pragma unroll
+            for (int i = 0; i < GB; ++i) {
+                if (g0 + i < Gp) multiply(i, g0);
+                fetch(i, g0 + GB + i);
+            }
+        }
     }
 }
 
@@ -444,19 +475,18 @@ __device__ inline Keys wave_keys(int c0, int kend, int waves, int wave) {
 
 // A wave's logits of its keys; `fill` where there is none
 template <int BITS, int RM, int KT>
-__device__ __forceinline__ void wave_logits(const AttnArgs& a, const uint8_t* codes, const uint8_t* scales,
-                                            const uint16_t* Ul, uint8_t* Sl, int chunks, const Keys& k, int n, int first,
+__device__ __forceinline__ void wave_logits(const AttnArgs& a, const Slot& x, const uint16_t* Ul, uint8_t* Sl, int chunks, const Keys& k, int n, int first,
                                             int lane, float fill, f32x4 (&S)[KT][RM]) {
     static_assert(KT == 4 || KT == 8, "one or two runs of four tiles");
     const int q = lane >> 4, olast = (n - 1) >> 3, at = k.c0 + k.kb;
     if (k.nt > 0) {
-        if (k.wide) logits<BITS, RM, 0, 4, KT>(a, codes, scales, Ul, Sl, chunks, at, olast, first, lane, S);
-        else logits<BITS, RM, 0, 1, KT>(a, codes, scales, Ul, Sl, chunks, at, olast, first, lane, S);
+        if (k.wide) logits<BITS, RM, 0, 4, KT>(a, x, Ul, Sl, chunks, at, olast, first, lane, S);
+        else logits<BITS, RM, 0, 1, KT>(a, x, Ul, Sl, chunks, at, olast, first, lane, S);
     }
     if constexpr (KT == 8) {
         if (k.nt > 1) {
-            if (k.wide) logits<BITS, RM, 4, 4, KT>(a, codes, scales, Ul, Sl, chunks, at + k.kstep, olast, first, lane, S);
-            else logits<BITS, RM, 4, 1, KT>(a, codes, scales, Ul, Sl, chunks, at + k.kstep, olast, first, lane, S);
+            if (k.wide) logits<BITS, RM, 4, 4, KT>(a, x, Ul, Sl, chunks, at + k.kstep, olast, first, lane, S);
+            else logits<BITS, RM, 4, 1, KT>(a, x, Ul, Sl, chunks, at + k.kstep, olast, first, lane, S);
         }
     }
     if (k.wide && k.nt == KT / 4 && at + (k.nt - 1) * k.kstep + 64 <= k.kend) return;   // a full share
@@ -488,8 +518,7 @@ __device__ __forceinline__ void put_run(uint16_t* Pl, int r, int run, const Keys
 
 // acc += P X over the chunk's keys: a wave its 128 columns (dj: the lane's octet of them)
 template <int BITS, int RM>
-__device__ __forceinline__ void weighted_sum(const AttnArgs& a, const uint8_t* codes, const uint8_t* scales,
-                                             const uint16_t* Pl, int KC, int c0, int nk, int n, int dj, int lane,
+__device__ __forceinline__ void weighted_sum(const AttnArgs& a, const Slot& x, const uint16_t* Pl, int KC, int c0, int nk, int n, int dj, int lane,
                                              f32x4 (&acc)[8][RM]) {
     const int l16 = lane & 15, q = lane >> 4;
     const int steps = nk / 32, tail = steps - 1;
@@ -506,7 +535,7 @@ __device__ __forceinline__ void weighted_sum(const AttnArgs& a, const uint8_t* c
         kk = min(kk, tail);
         const uint32_t at = kk == tail ? at1 : at0, sat = kk == tail ? sat1 : sat0;
         const uint32_t step = (uint32_t)(4 * kk) * G;
-        load_block<BITS>(to, codes + step * (32 * BITS), scales + step * 8, at, sat);
+        load_block<BITS>(to, x, at, step * (32 * BITS), sat, step * 8);
     };
     auto multiply = [&](const Block<BITS>& from, int kk) {
         bf16x8 p[RM];
@@ -590,7 +619,7 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
     }
     int32_t n;
     const uint8_t* const codes = cache_slot(a.c, b, &n);
-    const uint8_t* const scales = codes + a.c.scales_at;
+    const Slot x = slot_of(a.c, codes);
     const int k0 = sp * a.split_keys, k1 = min(n, k0 + a.split_keys);
     const int64_t prow = ((int64_t)sp * a.B + b) * N + row0;   // partial results' rows
     const int64_t urow = HEADS ? b * a.R + row0 : b * N + row0;
@@ -633,11 +662,11 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
     const int dj = min(wave * 16 + l16, a.c.G * 4 - 1);   // this lane's octet of columns
     // each wave starts its logits at a group of its own: octets of rows lie a power of two of bytes
     // apart (D = 1024), so that one group of all of them is in one channel of the L2
-    const int first = 2 * (int)((uint32_t)(3 * wave + 5 * id) % (uint32_t)(chunks / 8));
+    const int first = 4 * (int)((uint32_t)(3 * wave + 5 * id) % (uint32_t)(chunks / 16));
     for (int c0 = k0; c0 < k1; c0 += KC) {
         const Keys keys = wave_keys<KT>(c0, min(k1, c0 + KC), waves, wave);
         f32x4 S[KT][RM];
-        wave_logits<BITS, RM, KT>(a, codes, scales, Ul, Sl, chunks, keys, n, first, lane, -INFINITY, S);
+        wave_logits<BITS, RM, KT>(a, x, Ul, Sl, chunks, keys, n, first, lane, -INFINITY, S);
         // ---- softmax: the maximum over the chunk's keys, of all waves (scale2 > 0: the largest
         // logit has the largest product)
 #pragma unroll
@@ -705,7 +734,7 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
 #pragma unroll
                 for (int rm = 0; rm < RM; ++rm) acc[j][rm] = (f32x4){0.f, 0.f, 0.f, 0.f};
         }
-        weighted_sum<BITS, RM>(a, codes, scales, Pl, KC, c0, keys.nk, n, dj, lane, acc);
+        weighted_sum<BITS, RM>(a, x, Pl, KC, c0, keys.nk, n, dj, lane, acc);
         if constexpr (!LOOP) break;   // all keys are in one chunk
     }
     // ---- results: rows rm 16 + 4 q + i, this lane's columns 8 (16 wave + l16) ..+7
@@ -797,7 +826,7 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
     const int rows = min(16 * RM, (HEADS ? a.R : a.N) - row0);
     int32_t n;
     const uint8_t* const codes = cache_slot(a.c, b, &n);
-    const uint8_t* const scales = codes + a.c.scales_at;
+    const Slot x = slot_of(a.c, codes);
     const int64_t urow = b * (HEADS ? a.R : a.N) + row0;
     // row r of C and dU, [B][R][h][D]
     auto place = [&](int r) { return (HEADS ? (urow + r) * a.h + head : urow + r) * D; };
@@ -816,7 +845,7 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
             }
         return;
     }
-    const int first = 2 * (int)((uint32_t)(3 * wave + 5 * id) % (uint32_t)(chunks / 8));
+    const int first = 4 * (int)((uint32_t)(3 * wave + 5 * id) % (uint32_t)(chunks / 16));
     const int dj = min(wave * 16 + l16, a.c.G * 4 - 1);
     const Keys keys = wave_keys<KT>(0, n, waves, wave);
     uint16_t* const Ql = Ul + waves * 128 * 64;
@@ -828,7 +857,7 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
         load_rows<RM>(a.U + urow * D, D, rows, waves, wave, lane, Ul, chunks);
     __syncthreads();
     f32x4 S[KT][RM];   // logits, then weights before their division by the sum
-    wave_logits<BITS, RM, KT>(a, codes, scales, Ul, Sl, chunks, keys, n, first, lane, -INFINITY, S);
+    wave_logits<BITS, RM, KT>(a, x, Ul, Sl, chunks, keys, n, first, lane, -INFINITY, S);
 #pragma unroll
     for (int rm = 0; rm < RM; ++rm) {
         float mx = -INFINITY;
@@ -901,7 +930,7 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
             }
     };
     clear();
-    weighted_sum<BITS, RM>(a, codes, scales, Pl, KC, 0, keys.nk, n, dj, lane, acc);
+    weighted_sum<BITS, RM>(a, x, Pl, KC, 0, keys.nk, n, dj, lane, acc);
     {
         float f[RM][4];
 #pragma unroll
@@ -917,7 +946,7 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
         load_rows<RM>(a.dC + urow * D, D, rows, waves, wave, lane, Ul, chunks);
     __syncthreads();
     f32x4 T[KT][RM];   // gradients of the weights
-    wave_logits<BITS, RM, KT>(a, codes, scales, Ul, Sl, chunks, keys, n, first, lane, 0.f, T);
+    wave_logits<BITS, RM, KT>(a, x, Ul, Sl, chunks, keys, n, first, lane, 0.f, T);
 #pragma unroll
     for (int rm = 0; rm < RM; ++rm) {
         float dot = 0.f;
@@ -949,7 +978,7 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
     }
     __syncthreads();
     clear();
-    weighted_sum<BITS, RM>(a, codes, scales, Pl, KC, 0, keys.nk, n, dj, lane, acc);
+    weighted_sum<BITS, RM>(a, x, Pl, KC, 0, keys.nk, n, dj, lane, acc);
     float one[RM][4];
 #pragma unroll
     for (int rm = 0; rm < RM; ++rm)
