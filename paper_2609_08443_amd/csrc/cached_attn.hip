@@ -795,6 +795,48 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
     }
 }
 
+// a user without rows: no C, dU and dQp (and Qp in bf16 as ever)
+template <bool HEADS>
+__device__ inline void no_rows(const AttnArgs& a, int64_t urow, int head, int rows) {
+    const int D = a.c.D;
+    for (int i = threadIdx.x; i < rows * D; i += blockDim.x) {
+        const int64_t to = (HEADS ? (urow + i / D) * a.h + head : urow + i / D) * D + i % D;
+        a.C[to] = 0;
+        a.dU[to] = 0;
+    }
+    if constexpr (HEADS)
+        for (int i = threadIdx.x; i < rows * a.dh; i += blockDim.x) {
+            const int64_t at = (urow + i / a.dh) * D + head * a.dh + i % a.dh;
+            reinterpret_cast<uint16_t*>(a.out)[at] = 0;
+            a.Qb[at] = tile::to_bf16(a.Qf[at]);
+        }
+}
+
+// accumulators times their rows' factors to [B][R][h][D], bf16
+template <int RM, bool HEADS>
+__device__ __forceinline__ void store_rows(const AttnArgs& a, uint16_t* to, const f32x4 (&acc)[8][RM], const float (&f)[RM][4],
+                                           int64_t urow, int head, int rows, int wave, int lane) {
+    const int l16 = lane & 15, q = lane >> 4, D = a.c.D, col = 8 * (wave * 16 + l16);
+#pragma unroll
+    for (int rm = 0; rm < RM; ++rm)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = rm * 16 + 4 * q + i;
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = acc[j][rm][i] * f[rm][i];
+            if (r >= rows || col >= D) continue;
+            const int64_t at = (HEADS ? (urow + r) * a.h + head : urow + r) * D + col;
+            if (HEADS || D % 8 == 0) {
+                *reinterpret_cast<uint4*>(to + at) = __builtin_bit_cast(uint4, tile::pack8(v));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (col + j < D) to[at + j] = tile::to_bf16(v[j]);
+            }
+        }
+}
+
 // The attention's backward: of rows u and their aggregates' gradients dC (in LDS one after the
 // other)
 //   alpha = softmax(scale U X^T),  C = alpha X,
@@ -828,21 +870,8 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
     const uint8_t* const codes = cache_slot(a.c, b, &n);
     const Slot x = slot_of(a.c, codes);
     const int64_t urow = b * (HEADS ? a.R : a.N) + row0;
-    // row r of C and dU, [B][R][h][D]
-    auto place = [&](int r) { return (HEADS ? (urow + r) * a.h + head : urow + r) * D; };
-    const int col = 8 * (wave * 16 + l16);   // this lane's columns of C and dU
     if (n <= 0) {
-        for (int i = threadIdx.x; i < rows * D; i += blockDim.x) {
-            const int64_t to = place(i / D) + i % D;
-            a.C[to] = 0;
-            a.dU[to] = 0;
-        }
-        if constexpr (HEADS)
-            for (int i = threadIdx.x; i < rows * a.dh; i += blockDim.x) {
-                const int64_t at = (urow + i / a.dh) * D + head * a.dh + i % a.dh;
-                reinterpret_cast<uint16_t*>(a.out)[at] = 0;
-                a.Qb[at] = tile::to_bf16(a.Qf[at]);
-            }
+        no_rows<HEADS>(a, urow, head, rows);
         return;
     }
     const int first = 4 * (int)((uint32_t)(3 * wave + 5 * id) % (uint32_t)(chunks / 16));
@@ -909,26 +938,6 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
 #pragma unroll
             for (int rm = 0; rm < RM; ++rm) acc[j][rm] = (f32x4){0.f, 0.f, 0.f, 0.f};
     };
-    // accumulators, times their rows' factors, as bf16
-    auto store = [&](uint16_t* to, const float (&f)[RM][4]) {
-#pragma unroll
-        for (int rm = 0; rm < RM; ++rm)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = rm * 16 + 4 * q + i;
-                float v[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = acc[j][rm][i] * f[rm][i];
-                if (r >= rows || col >= D) continue;
-                if (HEADS || D % 8 == 0) {
-                    *reinterpret_cast<uint4*>(to + place(r) + col) = __builtin_bit_cast(uint4, tile::pack8(v));
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (col + j < D) to[place(r) + col + j] = tile::to_bf16(v[j]);
-                }
-            }
-    };
     clear();
     weighted_sum<BITS, RM>(a, x, Pl, KC, 0, keys.nk, n, dj, lane, acc);
     {
@@ -937,7 +946,7 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
         for (int rm = 0; rm < RM; ++rm)
 #pragma unroll
             for (int i = 0; i < 4; ++i) f[rm][i] = __shfl(inv[rm], 4 * q + i, 64);
-        store(a.C, f);
+        store_rows<RM, HEADS>(a, a.C, acc, f, urow, head, rows, wave, lane);
     }
     __syncthreads();   // the weights in LDS have been read
     if constexpr (HEADS)
@@ -984,10 +993,182 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
     for (int rm = 0; rm < RM; ++rm)
 #pragma unroll
         for (int i = 0; i < 4; ++i) one[rm][i] = 1.f;
-    store(a.dU, one);
+    store_rows<RM, HEADS>(a, a.dU, acc, one, urow, head, rows, wave, lane);
     if constexpr (!HEADS) return;
     __syncthreads();
     project_out<RM, true>(a, acc, one, a.Wk + head * a.dh, rows, urow, head, waves, wave, lane, Ul);
+}
+
+// The same where the keys fill several chunks, in two passes over them: the first carries the
+// maximum, the sum, sum alpha dA and C from chunk to chunk, the second has the final ones and sums
+// dU.  Logits and dA are computed in both, six products instead of four, and U and dC stay in LDS
+// side by side: 16 or 32 rows a workgroup.
+template <int BITS, int RM, int KT, bool HEADS>
+__global__ __launch_bounds__(512) void cached_attn_bwd_loop_kernel(AttnArgs a) {
+    extern __shared__ uint4 smem[];
+    const int waves = blockDim.x >> 6, chunks = 16 * waves, KC = chunk_keys(KT, waves);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
+    uint16_t* const Ul = reinterpret_cast<uint16_t*>(smem);
+    uint16_t* const Dl = Ul + 16 * RM * 128 * waves;
+    uint16_t* const Pl = Dl + 16 * RM * 128 * waves;
+    float* const wmax = reinterpret_cast<float*>(Pl + 16 * RM * KC);
+    float* const wsum = wmax + 16 * RM * waves;      // [wave][row], all three
+    float* const wdot = wsum + 16 * RM * waves;
+    uint8_t* const Sl = reinterpret_cast<uint8_t*>(wdot + 16 * RM * waves) + wave * 8 * scale_stride(waves);
+    const uint32_t id = (uint32_t)tile::xcd_range(blockIdx.x, gridDim.x);
+    const int D = a.c.D;
+    const uint32_t bh = id / (uint32_t)a.row_tiles;
+    const int row0 = (int)(id - bh * (uint32_t)a.row_tiles) * 16 * RM;
+    const int64_t b = HEADS ? bh / (uint32_t)a.h : bh;
+    const int head = HEADS ? (int)(bh - (uint32_t)b * (uint32_t)a.h) : 0;
+    const int rows = min(16 * RM, (HEADS ? a.R : a.N) - row0);
+    int32_t n;
+    const uint8_t* const codes = cache_slot(a.c, b, &n);
+    const Slot x = slot_of(a.c, codes);
+    const int64_t urow = b * (HEADS ? a.R : a.N) + row0;
+    if (n <= 0) {
+        no_rows<HEADS>(a, urow, head, rows);
+        return;
+    }
+    const int first = 4 * (int)((uint32_t)(3 * wave + 5 * id) % (uint32_t)(chunks / 16));
+    const int dj = min(wave * 16 + l16, a.c.G * 4 - 1);
+    if constexpr (HEADS) {   // (W_K's and W_V's rows pass through LDS behind what is there already)
+        project_rows<RM>(a.Qf + urow * D + head * a.dh, a.Wk + head * a.dh, D, a.dh, rows, wave, lane, Ul, chunks,
+                         Ul + waves * 128 * 64, a.Qb + urow * D + head * a.dh);
+        __syncthreads();
+        project_rows<RM>(a.dout + urow * D + head * a.dh, a.Wv + head * a.dh, D, a.dh, rows, wave, lane, Dl, chunks,
+                         Dl + waves * 128 * 64);
+    } else {
+        load_rows<RM>(a.U + urow * D, D, rows, waves, wave, lane, Ul, chunks);
+        load_rows<RM>(a.dC + urow * D, D, rows, waves, wave, lane, Dl, chunks);
+    }
+    __syncthreads();
+
+    f32x4 acc[8][RM];
+    float m[RM], l[RM], dot[RM];   // of row l16: maximum, sum of weights, of weights times dA
+    auto clear = [&] {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int rm = 0; rm < RM; ++rm) acc[j][rm] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    };
+    clear();
+#pragma unroll
+    for (int rm = 0; rm < RM; ++rm) m[rm] = -INFINITY, l[rm] = 0.f, dot[rm] = 0.f;
+    for (int c0 = 0; c0 < n; c0 += KC) {
+        const Keys keys = wave_keys<KT>(c0, min(n, c0 + KC), waves, wave);
+        f32x4 S[KT][RM], T[KT][RM];
+        wave_logits<BITS, RM, KT>(a, x, Ul, Sl, chunks, keys, n, first, lane, -INFINITY, S);
+        wave_logits<BITS, RM, KT>(a, x, Dl, Sl, chunks, keys, n, first, lane, 0.f, T);
+#pragma unroll
+        for (int rm = 0; rm < RM; ++rm) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < KT; ++t) mx = fmaxf(fmaxf(fmaxf(mx, S[t][rm][0]), fmaxf(S[t][rm][1], S[t][rm][2])), S[t][rm][3]);
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            if (q == 0) wmax[wave * 16 * RM + rm * 16 + l16] = mx;
+        }
+        __syncthreads();   // the last chunk's weights have been read, too
+        float cor[RM];
+#pragma unroll
+        for (int rm = 0; rm < RM; ++rm) {
+            float mx = m[rm];
+            for (int v = 0; v < waves; ++v) mx = fmaxf(mx, wmax[v * 16 * RM + rm * 16 + l16]);
+            const float base = mx == -INFINITY ? 0.f : mx;
+            cor[rm] = __builtin_amdgcn_exp2f((m[rm] - base) * a.scale2);
+            m[rm] = mx;
+            float sum = 0.f, d = 0.f;
+#pragma unroll
+            for (int t = 0; t < KT; t += 4) {
+                if ((t >> 2) >= keys.nt) break;
+                float p[4][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        p[i][j] = __builtin_amdgcn_exp2f((S[t + j][rm][i] - base) * a.scale2);
+                        d = __builtin_fmaf(p[i][j], T[t + j][rm][i], d);
+                    }
+                    sum += (p[i][0] + p[i][1]) + (p[i][2] + p[i][3]);
+                }
+                put_run(Pl, rm * 16 + l16, t >> 2, keys, KC, q, p);
+            }
+            sum += __shfl_xor(sum, 16, 64);
+            sum += __shfl_xor(sum, 32, 64);
+            d += __shfl_xor(d, 16, 64);
+            d += __shfl_xor(d, 32, 64);
+            if (q == 0) {
+                wsum[wave * 16 * RM + rm * 16 + l16] = sum;
+                wdot[wave * 16 * RM + rm * 16 + l16] = d;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int rm = 0; rm < RM; ++rm) {
+            float sum = 0.f, d = 0.f;
+            for (int v = 0; v < waves; ++v) {
+                sum += wsum[v * 16 * RM + rm * 16 + l16];
+                d += wdot[v * 16 * RM + rm * 16 + l16];
+            }
+            l[rm] = l[rm] * cor[rm] + sum;
+            dot[rm] = dot[rm] * cor[rm] + d;
+            if (c0 > 0) {
+                float f[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f[i] = __shfl(cor[rm], 4 * q + i, 64);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[j][rm][i] *= f[i];
+            }
+        }
+        weighted_sum<BITS, RM>(a, x, Pl, KC, c0, keys.nk, n, dj, lane, acc);
+    }
+    float f[RM][4], inv[RM];
+#pragma unroll
+    for (int rm = 0; rm < RM; ++rm) {
+        inv[rm] = 1.f / l[rm];
+        dot[rm] *= inv[rm];
+        if (m[rm] == -INFINITY) m[rm] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[rm][i] = __shfl(inv[rm], 4 * q + i, 64);
+    }
+    store_rows<RM, HEADS>(a, a.C, acc, f, urow, head, rows, wave, lane);
+    clear();
+    for (int c0 = 0; c0 < n; c0 += KC) {
+        const Keys keys = wave_keys<KT>(c0, min(n, c0 + KC), waves, wave);
+        f32x4 S[KT][RM], T[KT][RM];
+        wave_logits<BITS, RM, KT>(a, x, Ul, Sl, chunks, keys, n, first, lane, -INFINITY, S);
+        wave_logits<BITS, RM, KT>(a, x, Dl, Sl, chunks, keys, n, first, lane, 0.f, T);
+        __syncthreads();   // the last weights have been read
+#pragma unroll
+        for (int rm = 0; rm < RM; ++rm) {
+            const float g = a.scale * inv[rm];
+#pragma unroll
+            for (int t = 0; t < KT; t += 4) {
+                if ((t >> 2) >= keys.nt) break;
+                float p[4][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        p[i][j] = g * __builtin_amdgcn_exp2f((S[t + j][rm][i] - m[rm]) * a.scale2) * (T[t + j][rm][i] - dot[rm]);
+                put_run(Pl, rm * 16 + l16, t >> 2, keys, KC, q, p);
+            }
+        }
+        __syncthreads();
+        weighted_sum<BITS, RM>(a, x, Pl, KC, c0, keys.nk, n, dj, lane, acc);
+    }
+#pragma unroll
+    for (int rm = 0; rm < RM; ++rm)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[rm][i] = 1.f;
+    store_rows<RM, HEADS>(a, a.dU, acc, f, urow, head, rows, wave, lane);
+    if constexpr (!HEADS) return;
+    __syncthreads();
+    project_out<RM, true>(a, acc, f, a.Wk + head * a.dh, rows, urow, head, waves, wave, lane, Ul);
 }
 
 // Joins the splits of each row: their sums and accumulators, each scaled to the common
@@ -1169,15 +1350,33 @@ hipError_t launch_cached_attn(const CacheView& c, int bits, const CachedAttnArgs
 namespace {
 
 // The backward's workgroups: rm 16s of rows, of one head's targets (heads) or of all of a
-// user's; rm = 0 where it does not take the shape (all keys have to fit a chunk).
+// user's; rm = 0 where it does not take the shape.  Keys that do not fit a chunk go in chunks
+// (loop), in as many rows as LDS holds twice.
 struct BwdPlan {
     int rm = 0;
-    bool heads = false;
+    bool heads = false, loop = false;
 };
+template <int RM, int KT, bool HEADS>
+constexpr int bwd_loop_lds(int waves) {
+    const int s = 2 * 16 * RM * 128 * waves * 2 + 16 * RM * chunk_keys(KT, waves) * 2 + 3 * 16 * RM * 4 * waves +
+                  waves * 8 * scale_stride(waves);
+    const int t = HEADS ? 16 * RM * 128 * waves * 2 + waves * 128 * 64 * 2 + 16 * RM * 64 * 2 * 2 : 0;
+    return s > t ? s : t;
+}
+// (up to half the width all of them fit)
+static_assert(bwd_loop_lds<2, 4, true>(4) <= 160 * 1024 && bwd_loop_lds<1, 8, true>(4) <= 160 * 1024, "LDS");
 BwdPlan bwd_plan(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
     BwdPlan p;
     const int waves = (D + 127) / 128;
-    if (D > 1024 || k > chunk_keys(8, waves)) return p;
+    if (D > 1024) return p;
+    // Chunks of keys one after the other, up to 16 and at half the width; elsewhere the separate
+    // products are faster.  In chunks / in products (us a call):
+    //   D = 256:  16 users, R = 20, k = 512    61 /  70;  10 users, R = 60, k = 3000  316 / 464
+    //   D = 512:  20 users, R = 30, k = 1024  135 / 150;  64 users, R = 8, k = 2048   163 / 240
+    //   D = 1024: 14 users, R = 1, k = 2048   201 / 142;  4 users, R = 100, k = 2048  392 / 334
+    //   D = 64, 24 chunks: 2 users, R = 2, k = 3000  244 / 193
+    p.loop = k > chunk_keys(8, waves);
+    if (p.loop && (D > 512 || k > 16 * chunk_keys(8, waves))) return p;
     // Microseconds: rounds of workgroups, each 12.5 for every 16 rows at k = 512, D = 1024, and 22
     // (heads: 26) for the rest at D = 1024; 15 for the three products around the rows' form.
     // Measured there, heads in 16, 32, 48 rows / rows in 16, 32, 48 (us a call):
@@ -1187,7 +1386,8 @@ BwdPlan bwd_plan(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
     //   R = 16, B = 32    122  143  156 / 129  110  114
     //   R = 40, B = 32    287  260  179 / 245  221  194
     //   R = 100, B = 8    261  211  224 / 264  225  240
-    const double rest = D / 1024.0, row16 = 12.5 * rest * (k / 512.0);
+    // (loop: six products for four)
+    const double rest = D / 1024.0, row16 = (p.loop ? 18.75 : 12.5) * rest * (k / 512.0);
     double best = 0;
     for (int heads = 0; heads < 2; ++heads) {
         if (heads && (D % h != 0 || (D / h) % 32 != 0)) continue;
@@ -1211,8 +1411,18 @@ hipError_t launch_bwd_instance(const AttnArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL(kern, dim3((unsigned)(a.B * a.row_tiles * (HEADS ? a.h : 1))), dim3(64 * waves), lds, stream, a);
     return hipGetLastError();
 }
+template <int BITS, int RM, int KT, bool HEADS>
+hipError_t launch_bwd_loop(const AttnArgs& a, hipStream_t stream) {
+    const int waves = (a.c.D + 127) / 128, lds = bwd_loop_lds<RM, KT, HEADS>(waves);
+    auto kern = cached_attn_bwd_loop_kernel<BITS, RM, KT, HEADS>;
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(a.B * a.row_tiles * (HEADS ? a.h : 1))), dim3(64 * waves), lds, stream, a);
+    return hipGetLastError();
+}
 template <int BITS, bool HEADS>
-hipError_t launch_bwd_rows(const AttnArgs& a, int rm, hipStream_t stream) {
+hipError_t launch_bwd_rows(const AttnArgs& a, int rm, bool loop, hipStream_t stream) {
+    if (loop) return rm == 1 ? launch_bwd_loop<BITS, 1, 8, HEADS>(a, stream) : launch_bwd_loop<BITS, 2, 4, HEADS>(a, stream);
     if (rm == 1) return launch_bwd_instance<BITS, 1, 8, HEADS>(a, stream);
     if (rm == 2) return launch_bwd_instance<BITS, 2, 8, HEADS>(a, stream);
     if (rm == 3) return launch_bwd_instance<BITS, 3, 4, HEADS>(a, stream);
@@ -1249,8 +1459,8 @@ hipError_t launch_cached_bwd(const CacheView& c, int bits, const CachedBwdArgs& 
     a.dC = f.dC;
     a.dU = f.dU;
     a.scale = f.scale;
-    if (bits == 4) return p.heads ? launch_bwd_rows<4, true>(a, p.rm, stream) : launch_bwd_rows<4, false>(a, p.rm, stream);
-    return p.heads ? launch_bwd_rows<8, true>(a, p.rm, stream) : launch_bwd_rows<8, false>(a, p.rm, stream);
+    if (bits == 4) return p.heads ? launch_bwd_rows<4, true>(a, p.rm, p.loop, stream) : launch_bwd_rows<4, false>(a, p.rm, p.loop, stream);
+    return p.heads ? launch_bwd_rows<8, true>(a, p.rm, p.loop, stream) : launch_bwd_rows<8, false>(a, p.rm, p.loop, stream);
 }
 
 }  // namespace sa

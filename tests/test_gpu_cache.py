@@ -325,14 +325,15 @@ def reference64(X, n, q, W, h, dout):
 
 # every form of the forward and of the backward: workgroups of one head's targets in one to
 # four 16s, of all of a user's rows, of split keys, keys in one chunk and several, the
-# separate products (the backward's where keys do not fit a chunk); widths that are no
+# separate products (the backward's for many keys at the widest, too); widths that are no
 # multiple of a head's 32, of 8, of 2
 BIG_CASES = [(16, 40, 130, 1024, 16), (16, 60, 300, 1024, 16), (64, 16, 140, 1024, 16), (64, 8, 1100, 1024, 16),
              (300, 1, 100, 1024, 16), (50, 30, 90, 600, 5), (60, 33, 70, 333, 3), (3, 300, 700, 1024, 16),
              (20, 33, 1030, 1024, 16), (100, 40, 40, 96, 3), (40, 100, 300, 256, 2), (16, 16, 140, 1024, 16),
              (32, 40, 100, 1024, 32), (64, 20, 60, 512, 16), (2, 4, 600, 1000, 8), (8, 60, 150, 999, 9),
              (128, 20, 60, 1000, 5), (40, 50, 200, 768, 8), (1, 300, 2500, 1024, 8), (2, 20, 90, 1600, 10),
-             (40, 300, 130, 96, 3), (40, 300, 520, 20, 1), (100, 300, 130, 20, 1), (1, 1, 130, 20, 1)]
+             (40, 300, 130, 96, 3), (40, 300, 520, 20, 1), (100, 300, 130, 20, 1), (1, 1, 130, 20, 1),
+             (20, 9, 1100, 512, 4), (7, 30, 900, 288, 3), (6, 5, 1500, 500, 5), (3, 2, 4096, 256, 2), (100, 20, 600, 480, 5)]
 
 
 @pytest.mark.parametrize("fmt", ["fp4", "fp8"])
