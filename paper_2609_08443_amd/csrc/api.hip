@@ -644,7 +644,12 @@ sa_status check_cache(int64_t B, int32_t k, int32_t D, int64_t n_slots, sa_cache
     // a slot's values, a row's padding included, are counted in 32 bits
     if ((((int64_t)k + 7) / 8 * 8) * (((int64_t)D + 31) / 32 * 32) >= (int64_t(1) << 31))
         return fail(SA_ERR_UNSUPPORTED, "k * D must be < 2^31");
-    if (B > 0 && (B + k >= (int64_t(1) << 31) - 1 || B * sa::cache_io_workgroups(k, D) >= (int64_t(1) << 31)))
+    if (B + k >= (int64_t(1) << 31) - 1) return fail(SA_ERR_UNSUPPORTED, "sizes beyond the supported range");
+    return SA_OK;
+}
+// a launch has fewer than 2^32 threads
+sa_status check_cache_io(int64_t B, int32_t k, int32_t D) {
+    if (B * sa::cache_io_workgroups(k, D) >= (int64_t(1) << 24))
         return fail(SA_ERR_UNSUPPORTED, "sizes beyond the supported range");
     return SA_OK;
 }
@@ -798,6 +803,13 @@ hipError_t cached_products_bwd(const CachedArgs& a, const float* lse, uint8_t* w
                             stream);
     }
     return e;
+}
+
+// whether the plan's kernels take that many users and rows
+sa_status check_cached_plan(const CachedPlan& p, int64_t B, int32_t R, int32_t k, int32_t D, int32_t h) {
+    if (p.kind != kCachedProducts) return SA_OK;   // (their plans are of launches that fit)
+    if (B * R * h >= (int64_t(1) << 26)) return fail(SA_ERR_UNSUPPORTED, "sizes beyond the supported range");
+    return check_cache_io(B, k, D);
 }
 
 // arguments shared by the two directions
@@ -1719,6 +1731,7 @@ sa_status sa_cache_write(const void* Xs, sa_dtype dtype, const int64_t* slots, c
     g_last_error[0] = 0;
     if (dtype != SA_BF16 && dtype != SA_FP32) return fail(SA_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
     sa_status st = check_cache(B, k, D, n_slots, format);
+    if (st == SA_OK) st = check_cache_io(B, k, D);
     if (st != SA_OK) return st;
     if (B == 0 || n_slots == 0) return SA_OK;
     if (!Xs || !slots || !cache || !cache_rows) return fail(SA_ERR_INVALID_ARG, "null pointer argument");
@@ -1737,6 +1750,7 @@ sa_status sa_cache_read(const void* cache, const int32_t* cache_rows, int64_t n_
     g_last_error[0] = 0;
     if (dtype != SA_BF16 && dtype != SA_FP32) return fail(SA_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
     sa_status st = check_cache(B, k, D, n_slots, format);
+    if (st == SA_OK) st = check_cache_io(B, k, D);
     if (st != SA_OK) return st;
     if (B == 0) return SA_OK;
     if (!slots || !out || (n_slots > 0 && (!cache || !cache_rows)))
@@ -1753,7 +1767,8 @@ sa_status sa_cache_read(const void* cache, const int32_t* cache_rows, int64_t n_
 
 size_t sa_stca_cached_fwd_workspace_size(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa_dtype dtype) {
     if (check_stca(B, R, k, D, h, 1.0f, dtype) != SA_OK || check_cache(B, k, D, 0, SA_CACHE_FP8) != SA_OK) return 0;
-    return plan_cached(B, R, k, D, h, dtype, false).total;
+    const CachedPlan p = plan_cached(B, R, k, D, h, dtype, false);
+    return check_cached_plan(p, B, R, k, D, h) == SA_OK ? p.total : 0;
 }
 
 sa_status sa_stca_cached_fwd(const void* cache, const int32_t* cache_rows, int64_t n_slots, const int64_t* slots,
@@ -1775,6 +1790,8 @@ sa_status sa_stca_cached_fwd(const void* cache, const int32_t* cache_rows, int64
     if (!aligned16(out) || !aligned16(lse))
         return fail(SA_ERR_INVALID_ARG, "tensor arguments must be 16-byte aligned");
     const CachedPlan p = plan_cached(B, R, k, D, h, dtype, false);
+    st = check_cached_plan(p, B, R, k, D, h);
+    if (st != SA_OK) return st;
     if (!workspace || workspace_bytes < p.total)
         return fail(SA_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", p.total,
                     workspace ? workspace_bytes : (size_t)0);
@@ -1807,7 +1824,8 @@ sa_status sa_stca_cached_fwd(const void* cache, const int32_t* cache_rows, int64
 
 size_t sa_stca_cached_bwd_workspace_size(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa_dtype dtype) {
     if (check_stca(B, R, k, D, h, 1.0f, dtype) != SA_OK || check_cache(B, k, D, 0, SA_CACHE_FP8) != SA_OK) return 0;
-    return plan_cached(B, R, k, D, h, dtype, true).total;
+    const CachedPlan p = plan_cached(B, R, k, D, h, dtype, true);
+    return check_cached_plan(p, B, R, k, D, h) == SA_OK ? p.total : 0;
 }
 
 sa_status sa_stca_cached_bwd(const void* cache, const int32_t* cache_rows, int64_t n_slots, const int64_t* slots,
@@ -1829,6 +1847,8 @@ sa_status sa_stca_cached_bwd(const void* cache, const int32_t* cache_rows, int64
     if (!aligned16(dout) || !aligned16(dq) || !aligned16(dWq) || !aligned16(dWk) || !aligned16(dWv))
         return fail(SA_ERR_INVALID_ARG, "tensor arguments must be 16-byte aligned");
     const CachedPlan p = plan_cached(B, R, k, D, h, dtype, true);
+    st = check_cached_plan(p, B, R, k, D, h);
+    if (st != SA_OK) return st;
     if (!workspace || workspace_bytes < p.total)
         return fail(SA_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", p.total,
                     workspace ? workspace_bytes : (size_t)0);

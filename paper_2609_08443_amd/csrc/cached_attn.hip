@@ -1226,6 +1226,9 @@ hipError_t launch_instance(const AttnArgs& a, hipStream_t stream) {
     return hipGetLastError();
 }
 
+// (a launch has fewer than 2^32 threads)
+bool fits_a_grid(int64_t workgroups, int waves) { return workgroups * 64 * waves < (int64_t(1) << 32); }
+
 // The forward's workgroups: 16 rm rows u, of one head's targets (heads; rm 1 to 4) or of all of a
 // user's (rm 1, 2 or 4, and splits of its keys where workgroups would be too few).  rm above 2
 // takes all keys in one chunk.
@@ -1256,8 +1259,8 @@ AttnPlan attn_plan(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
     const bool one = k <= chunk_keys(8, waves);
     AttnPlan p;
     double best = 0;
-    auto consider = [&](AttnPlan c, double cost) {
-        if (p.rm == 0 || cost < best) p = c, best = cost;
+    auto consider = [&](AttnPlan c, int64_t wgs, double cost) {
+        if (fits_a_grid(wgs, waves) && (p.rm == 0 || cost < best)) p = c, best = cost;
     };
     if (D % h == 0 && (D / h) % 32 == 0) {
         for (int rm = 1; rm <= (one ? 4 : 2); ++rm) {
@@ -1266,8 +1269,8 @@ AttnPlan attn_plan(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
             c.rm = rm;
             c.row_tiles = (R + 16 * rm - 1) / (16 * rm);
             c.split_keys = (k + 31) / 32 * 32;
-            const int64_t rounds = (B * h * c.row_tiles + slots - 1) / slots;
-            consider(c, 9 + rounds * width * (5 + 2.5 * rm + (13.5 + 2.7 * rm) * k / 512));
+            const int64_t wgs = B * h * c.row_tiles, rounds = (wgs + slots - 1) / slots;
+            consider(c, wgs, 9 + rounds * width * (5 + 2.5 * rm + (13.5 + 2.7 * rm) * k / 512));
         }
     }
     const int64_t N = (int64_t)R * h;
@@ -1283,7 +1286,7 @@ AttnPlan attn_plan(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
         const int64_t rounds = (wgs * c.splits + slots - 1) / slots;
         const double key = rm == 1 ? 15 : rm == 2 ? 22 : 33;
         const double join = c.splits > 1 ? 3 + 8.0 * c.splits * B * N * D / 5e6 : 0;   // written and read at 5 TB/s
-        consider(c, 27 + join + rounds * width * (5 + key * std::min(k, c.split_keys) / 512));
+        consider(c, wgs * c.splits, 27 + join + rounds * width * (5 + key * std::min(k, c.split_keys) / 512));
     }
     return p;
 }
@@ -1307,7 +1310,8 @@ hipError_t launch_plan(const AttnPlan& p, const AttnArgs& a, hipStream_t stream)
 
 int cached_attn_kind(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
     if (D > 1024) return 0;
-    return attn_plan(B, R, h, k, D).heads ? 2 : 1;
+    const AttnPlan p = attn_plan(B, R, h, k, D);
+    return p.rm == 0 ? 0 : p.heads ? 2 : 1;
 }
 
 size_t cached_attn_workspace(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
@@ -1395,7 +1399,7 @@ BwdPlan bwd_plan(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
             const int64_t wgs = heads ? B * h * ((R + 16 * rm - 1) / (16 * rm)) : B * (((int64_t)R * h + 16 * rm - 1) / (16 * rm));
             const double rounds = (double)((wgs + device_cus() - 1) / device_cus());
             const double cost = rounds * (rm * row16 + (heads ? 26 : 22) * rest) + (heads ? 0 : 15);
-            if (p.rm == 0 || cost <= best) p.rm = rm, p.heads = heads != 0, best = cost;
+            if (fits_a_grid(wgs, waves) && (p.rm == 0 || cost <= best)) p.rm = rm, p.heads = heads != 0, best = cost;
         }
     }
     return p;

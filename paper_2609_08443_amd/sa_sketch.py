@@ -657,6 +657,8 @@ def _on(device, stream):
     that what a call allocates belongs to the stream that it runs on."""
     import torch
     if stream is not None:
+        if stream.device != device:
+            raise SAError(1, f"the stream is on {stream.device}, the tensors on {device}")
         return torch.cuda.stream(stream)
     if device.index == torch.cuda.current_device():
         return _AS_IT_IS

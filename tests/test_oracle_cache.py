@@ -198,6 +198,27 @@ def test_cached_stca_rejects_bad_arguments(fwd):
     assert size(2, 3, 64, 128, 3, 0) == 0 and size(2, 0, 64, 128, 2, 0) == 0
 
 
+@pytest.mark.parametrize("fwd", [True, False])
+def test_sizes_past_a_launch_are_refused(fwd):
+    """a launch holds fewer than 2^32 threads"""
+    L = sa.lib()
+    io = (P, P, 1 << 20, P)
+    assert L.sa_cache_read(*io, 1 << 24, 1, 32, 0, P, 0, None) == 2      # one workgroup a user
+    assert L.sa_cache_write(P, 0, P, None, 1 << 24, 1, 32, 0, P, P, 1 << 20, None) == 2
+    size = sa.stca_cached_fwd_workspace_size if fwd else sa.stca_cached_bwd_workspace_size
+    assert cached_call(fwd, B=65535, R=256, h=8, k=1, D=8, dt=1, odt=1) == 2   # 2^27 rows of the softmax
+    assert size(65535, 256, 1, 8, 8, 1) == 0 and size(65535, 64, 1, 8, 8, 1) > 0
+    # bf16: workgroups of more rows instead
+    assert size(65535, 300, 4, 1024, 16, 0) > 0
+
+
+def test_binding_refuses_a_stream_of_another_device():
+    class Stream:
+        device, cuda_stream = torch.device("cuda", 1), 0
+    with pytest.raises(sa.SAError):
+        sa._on(torch.device("cuda", 0), Stream())
+
+
 def test_binding_refuses_what_is_not_a_cache():
     rows = torch.zeros(4, dtype=torch.int32)
     data = torch.zeros((4, sa.cache_slot_bytes(8, 64, "fp4")), dtype=torch.uint8)
