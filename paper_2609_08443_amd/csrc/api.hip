@@ -671,16 +671,18 @@ sa::CacheView cache_view(const void* cache, const int32_t* rows, const int64_t* 
 
 // STCA over cached sketches; operand buffers in the input dtype, as in StcaPlan.
 //   kCachedHeads   workgroups take a head's targets, projections and all:
-//                  [Qp | lse | (bwd) Qp in fp32 | dout in bf16 | C | dU | dQp]
+//                  [Qp | lse | (bwd) Qp in fp32 | dout in bf16 | C | dU | dQp | tail]
 //   kCachedRows    the attention alone in one kernel:
-//                  [Qp | lse | U | C | partial results of split keys | (bwd) dout | dC | dU | dQp]
+//                  [Qp | lse | U | C | partial results of split keys | (bwd) dout | dC | dU | dQp | tail]
 //   kCachedProducts  in separate products over sketches read into the workspace, Xd [B,k,D]:
-//                  [Qp | lse | U | C | Xd | S (fp32) | alpha | (bwd) dout | dC | dU | dQp | dalpha (fp32) | ds]
+//                  [Qp | lse | U | C | Xd | S (fp32) | alpha | (bwd) dout | dC | dU | dQp | tail |
+//                   dalpha (fp32) | ds]
 enum CachedKind { kCachedProducts = 0, kCachedRows = 1, kCachedHeads = 2 };
 struct CachedPlan {
     CachedKind kind = kCachedProducts;
     size_t off_xd = 0, off_qp = 0, off_u = 0, off_s = 0, off_al = 0, off_c = 0, off_lse = 0, off_part = 0, off_dob = 0,
-           off_dc = 0, off_da = 0, off_ds = 0, off_du = 0, off_dqp = 0, off_qf = 0, total = 0;
+           off_dc = 0, off_da = 0, off_ds = 0, off_du = 0, off_dqp = 0, off_qf = 0, off_tail = 0, total = 0;
+    bool tail = false;   // the weights' gradients sum over a number of targets that is no multiple of 64
 };
 
 CachedPlan plan_cached(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa_dtype dtype, bool bwd) {
@@ -711,6 +713,12 @@ CachedPlan plan_cached(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa
         if (p.kind != kCachedHeads) p.off_dc = carve(el * rows * D);
         p.off_du = carve(el * rows * D);
         p.off_dqp = carve(el * BR * D);
+        // The bf16 product takes 64 targets at a time: the last BR % 64 are copied with zeros up to
+        // 64, one launch for six operands, instead of three products in fp32.  With / without (us
+        // a call): 100 targets, D = 1024 67 / 77; 250, D = 256 39 / 46; 1,000, D = 1024 181 / 255;
+        // 2,460, D = 512 142 / 210.
+        p.tail = dtype == SA_BF16 && BR > 64 && BR % 64 != 0 && D / h % 8 == 0;
+        if (p.tail) p.off_tail = carve(64 * el * (2 * (size_t)h + 4) * D);
         if (p.kind == kCachedProducts) {
             p.off_da = carve(4 * rows * k);
             p.off_ds = carve(el * rows * k);
@@ -1888,18 +1896,30 @@ sa_status sa_stca_cached_bwd(const void* cache, const int32_t* cache_rows, int64
         sa::ProfScope ps("cached_key_side", stream);   // dQp[., head i] = dU[., i] W_K^(i)
         e = sa::launch_gemm({dU, bf, D, hD, 1, Wk, bf, dh, D, 1, dQp, bf, dh, D, BR, dh, D, h, 1.f, false}, stream);
     }
+    // the targets' last BR % 64 rows of the weights' gradients' operands [C | dU | dout | Qp | dQp | q]
+    const uint16_t* tail = reinterpret_cast<const uint16_t*>(ws + p.off_tail);
+    const uint16_t *dUt = tail + 64 * hD, *dot = dUt + 64 * hD, *Qpt = dot + 64 * D, *dQpt = Qpt + 64 * D, *qt = dQpt + 64 * D;
+    if (e == hipSuccess && p.tail) {
+        sa::ProfScope ps("cached_tail_rows", stream);
+        auto c16 = [](const void* x) { return reinterpret_cast<const uint16_t*>(x); };
+        e = sa::launch_tail_rows({{c16(Cc), c16(dU), c16(dob), c16(Qp), c16(dQp), c16(q)}, {(int32_t)hD, (int32_t)hD, D, D, D, D}},
+                                 BR, reinterpret_cast<uint16_t*>(ws + p.off_tail), stream);
+    }
+    auto over_targets = [&](const sa::GemmDesc& d, const uint16_t* A2, const uint16_t* B2) {
+        return p.tail ? sa::launch_gemm_tail(d, A2, B2, stream) : sa::launch_gemm(d, stream);
+    };
     if (e == hipSuccess) {
         sa::ProfScope ps("cached_weight_grads", stream);
         // dW_V^(i) = sum over targets of C[., i]^T dout[., head i];  dW_K^(i) = sum dU[., i]^T Qp[., head i]
-        e = sa::launch_gemm({Cc, bf, D, 1, hD, dob, bf, dh, D, 1, dWv, gb, dh, D, D, dh, BR, h, 1.f, false}, stream);
+        e = over_targets({Cc, bf, D, 1, hD, dob, bf, dh, D, 1, dWv, gb, dh, D, D, dh, BR, h, 1.f, false}, tail, dot);
         if (e == hipSuccess)
-            e = sa::launch_gemm({dU, bf, D, 1, hD, Qp, bf, dh, D, 1, dWk, gb, dh, D, D, dh, BR, h, 1.f, false}, stream);
+            e = over_targets({dU, bf, D, 1, hD, Qp, bf, dh, D, 1, dWk, gb, dh, D, D, dh, BR, h, 1.f, false}, dUt, Qpt);
     }
     if (e == hipSuccess) {
         sa::ProfScope ps("cached_query_grads", stream);   // dq = dQp W_Q^T;  dW_Q = q^T dQp
         e = sa::launch_gemm({dQp, bf, 0, D, 1, Wq, bf, 0, 1, D, dq, gb, 0, D, BR, D, D, 1, 1.f, false}, stream);
         if (e == hipSuccess)
-            e = sa::launch_gemm({q, bf, 0, 1, D, dQp, bf, 0, D, 1, dWq, gb, 0, D, D, D, BR, 1, 1.f, false}, stream);
+            e = over_targets({q, bf, 0, 1, D, dQp, bf, 0, D, 1, dWq, gb, 0, D, D, D, BR, 1, 1.f, false}, qt, dQpt);
     }
     if (e != hipSuccess) return hip_fail(e, "cached STCA backward launch");
     return SA_OK;

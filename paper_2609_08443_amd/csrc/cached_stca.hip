@@ -75,7 +75,31 @@ __global__ __launch_bounds__(256) void cached_softmax_bwd_kernel(CacheView c, co
         put<BF>(ds, row * c.k + j, j < n ? scale * __expf(s[j] - l) * (da[j] - dot) : 0.f);
 }
 
+// one thread per 8 columns of a row, the matrices one after the other
+__global__ __launch_bounds__(256) void tail_rows_kernel(TailRows t, int32_t rows, uint16_t* __restrict__ to) {
+    int i = blockIdx.x * 256 + threadIdx.x, at = 0;
+#pragma unroll
+    for (int m = 0; m < 6; ++m) {
+        const int per = t.width[m] / 8, n = 64 * per;
+        if (i >= 0 && i < n) {
+            const int64_t row = (int64_t)(rows & ~63) + i / per;
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (row < rows) v = reinterpret_cast<const uint4*>(t.from[m])[row * per + i % per];
+            reinterpret_cast<uint4*>(to)[at + i] = v;
+        }
+        i -= n;
+        at += n;
+    }
+}
+
 }  // namespace
+
+hipError_t launch_tail_rows(const TailRows& t, int32_t rows, uint16_t* to, hipStream_t stream) {
+    int64_t n = 0;
+    for (int m = 0; m < 6; ++m) n += 64 * (int64_t)(t.width[m] / 8);
+    hipLaunchKernelGGL(tail_rows_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, t, rows, to);
+    return hipGetLastError();
+}
 
 hipError_t launch_cached_softmax(const CacheView& c, const float* S, int64_t rows, int32_t Rh, bool bf16, void* alpha,
                                  float* lse, hipStream_t stream) {

@@ -607,9 +607,12 @@ hipError_t lt_launch(MgArgs g, bool c_bf16, int64_t batch, hipStream_t stream) {
     const int64_t blocks = (int64_t)g.tm * g.tn * batch;
     if (g.A2) {
         if constexpr (!A_KC && !B_KC && NS > 1) {
-            if (c_bf16) return hipErrorInvalidValue;
-            hipLaunchKernelGGL((mfma_gemm_lt_kernel<FM, FN, PM, PN, false, false, false, NS, true>), dim3((unsigned)blocks),
-                               dim3(256), 0, stream, g);
+            if (c_bf16)
+                hipLaunchKernelGGL((mfma_gemm_lt_kernel<FM, FN, PM, PN, false, false, true, NS, true>), dim3((unsigned)blocks),
+                                   dim3(256), 0, stream, g);
+            else
+                hipLaunchKernelGGL((mfma_gemm_lt_kernel<FM, FN, PM, PN, false, false, false, NS, true>), dim3((unsigned)blocks),
+                                   dim3(256), 0, stream, g);
             return hipGetLastError();
         } else {
             return hipErrorInvalidValue;
@@ -816,6 +819,22 @@ hipError_t launch_gemm_pair(const GemmDesc& d, const void* A2, const void* B2, h
     second.B = B2;
     second.accumulate = true;
     return launch_gemm(second, stream);
+}
+
+hipError_t launch_gemm_tail(const GemmDesc& d, const void* A2, const void* B2, hipStream_t stream) {
+    if (d.batch <= 0 || d.M <= 0 || d.N <= 0) return hipSuccess;
+    GemmDesc whole = d;
+    whole.K = (d.K + GBK - 1) / GBK * GBK;
+    if (d.a_k == 1 || d.b_k == 1 || d.K <= GBK || !d.a_bf16 || !d.b_bf16 || !gemm_on_matrix_cores(whole) || !al16(A2) ||
+        !al16(B2))
+        return launch_gemm(d, stream);
+    const int shape = choose_lt(whole, false, false);
+    if (shape < 0) return launch_gemm(d, stream);
+    MgArgs g = make_args(whole);
+    g.A2 = A2;
+    g.B2 = B2;
+    g.k1_slabs = d.K / GBK;
+    return lt_run(shape, g, false, false, d.c_bf16, d.batch, stream);
 }
 
 int gemm_tile_shapes() { return (int)(sizeof(kLtShapes) / sizeof(kLtShapes[0])); }

@@ -204,6 +204,10 @@ hipError_t launch_gemm(const GemmDesc& d, hipStream_t stream);
 // C = alpha (A B + A2 B2) (+ C), A2 and B2 with the strides and types of A and B: one
 // product over both contractions where the bf16 kernel takes it, else two.
 hipError_t launch_gemm_pair(const GemmDesc& d, const void* A2, const void* B2, hipStream_t stream);
+// launch_gemm of bf16 operands that are both contiguous along their rows, for a K that is no
+// multiple of 64 and more than that: A2 and B2 hold the last K % 64 of k, with zeros up to 64, in
+// A's and B's strides.
+hipError_t launch_gemm_tail(const GemmDesc& d, const void* A2, const void* B2, hipStream_t stream);
 hipError_t launch_small_gemm_general(const GemmDesc& d, hipStream_t stream);
 
 // Reordered single-query STCA rows (stca.hip), over [rows][k] fp32 logits already
@@ -260,6 +264,13 @@ struct CachedBwdArgs {
     int32_t R, h;
     float scale;
 };
+// The last rows % 64 rows of up to six bf16 matrices [rows][width], zeros up to 64, each into
+// [64][width] of `to`, one after the other.  Widths: multiples of 8.
+struct TailRows {
+    const uint16_t* from[6];
+    int32_t width[6];
+};
+hipError_t launch_tail_rows(const TailRows& t, int32_t rows, uint16_t* to, hipStream_t stream);
 int cached_bwd_kind(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D);
 hipError_t launch_cached_bwd(const CacheView& c, int bits, const CachedBwdArgs& f, hipStream_t stream);
 // softmax rows over each user's valid rows (rows = B Rh of k fp32 logits) and its backward

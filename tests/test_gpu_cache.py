@@ -371,6 +371,33 @@ def test_larger_batches_match_float64(sa, B, R, k, D, h, fmt):
         assert off(grads[name], rgrads[name]) <= btol, (name, off(grads[name], rgrads[name]))
 
 
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,R,D,h", [(13, 5, 24, 3), (65, 1, 128, 4), (9, 71, 64, 1), (3, 64, 40, 1), (127, 1, 72, 3),
+                                     (40, 125, 256, 4)])
+def test_weight_gradients_over_any_number_of_targets(sa, B, R, D, h, dt):
+    """sums over one target to many, around the multiples of 64 that the products take at a time,
+    with gradients in either type"""
+    k = 20
+    print(f"targets B={B} R={R} D={D} h={h} {dt}", flush=True)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(B + R + D)
+    normal = lambda *shape: torch.randn(shape, generator=g, device="cuda")  # noqa: E731
+    c = sa.sketch_cache(B, k, D, "fp8")
+    slots = torch.arange(B, device="cuda")
+    sa.cache_write(c, normal(B, k, D), slots)
+    X = sa.cache_read(c, slots, dtype=torch.float32).double()
+    q, dout = normal(B, R, D).bfloat16(), normal(B, R, D).to(dt)
+    W = [(normal(D, D) / D ** 0.5).bfloat16() for _ in range(3)]
+    grads = sa.stca_cached_bwd(c, slots, q, *W, h, dout)
+    n = torch.full((B,), k, device="cuda")
+    _, _, ref = reference64(X, n, q, W, h, dout)
+    _, btol = bounds("bf16", k, D, B * R)
+    for name, want in ref.items():
+        assert grads[name].dtype == dt
+        off = float((grads[name].double() - want).norm() / want.norm())
+        assert off <= btol, (name, off)
+
+
 def test_fp32_results_of_bf16_inputs(sa):
     p = problem(sa, 3, 6, 70, 128, 2, "fp8", "bf16", [70, 0, 41], [0, 1, 2])
     check_fwd(sa, p, 2, "bf16", "fp32")
