@@ -671,18 +671,20 @@ sa::CacheView cache_view(const void* cache, const int32_t* rows, const int64_t* 
 
 // STCA over cached sketches; operand buffers in the input dtype, as in StcaPlan.
 //   kCachedHeads   workgroups take a head's targets, projections and all:
-//                  [Qp | lse | (bwd) Qp in fp32 | dout in bf16 | C | dU | dQp | tail]
+//                  [Qp | lse | (bwd) Qp in fp32 | dout in bf16 | C | dU | dQp | tail | parts]
 //   kCachedRows    the attention alone in one kernel:
-//                  [Qp | lse | U | C | partial results of split keys | (bwd) dout | dC | dU | dQp | tail]
+//                  [Qp | lse | U | C | partial results of split keys | (bwd) dout | dC | dU | dQp | tail | parts]
 //   kCachedProducts  in separate products over sketches read into the workspace, Xd [B,k,D]:
 //                  [Qp | lse | U | C | Xd | S (fp32) | alpha | (bwd) dout | dC | dU | dQp | tail |
-//                   dalpha (fp32) | ds]
+//                   parts | dalpha (fp32) | ds]
 enum CachedKind { kCachedProducts = 0, kCachedRows = 1, kCachedHeads = 2 };
 struct CachedPlan {
     CachedKind kind = kCachedProducts;
     size_t off_xd = 0, off_qp = 0, off_u = 0, off_s = 0, off_al = 0, off_c = 0, off_lse = 0, off_part = 0, off_dob = 0,
-           off_dc = 0, off_da = 0, off_ds = 0, off_du = 0, off_dqp = 0, off_qf = 0, off_tail = 0, total = 0;
-    bool tail = false;   // the weights' gradients sum over a number of targets that is no multiple of 64
+           off_dc = 0, off_da = 0, off_ds = 0, off_du = 0, off_dqp = 0, off_qf = 0, off_tail = 0, off_parts = 0, total = 0;
+    // the weights' gradients: over a number of targets that is no multiple of 64, and in parts
+    bool tail = false;
+    int32_t splits = 1;
 };
 
 CachedPlan plan_cached(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa_dtype dtype, bool bwd) {
@@ -717,7 +719,18 @@ CachedPlan plan_cached(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa
         // 64, one launch for six operands, instead of three products in fp32.  With / without (us
         // a call): 100 targets, D = 1024 67 / 77; 250, D = 256 39 / 46; 1,000, D = 1024 181 / 255;
         // 2,460, D = 512 142 / 210.
-        p.tail = dtype == SA_BF16 && BR > 64 && BR % 64 != 0 && D / h % 8 == 0;
+        const bool in64s = dtype == SA_BF16 && BR > 64 && BR < (int64_t(1) << 31) && D / h % 8 == 0;
+        p.tail = in64s && BR % 64 != 0;
+        // Narrow matrices over many targets: too few tiles of 64 x 64 for the compute units, so the
+        // targets in parts of at least 8 of their 64s, whose sums are added up.  In parts / whole (us
+        // a call): 1,000 targets, D = 256 54 / 59; 10,000, D = 256 100 / 245; 1,024, D = 512 66 / 69;
+        // 2,460, D = 512 118 / 141; 2,400, D = 640 161 / 173.
+        if (in64s) {
+            const int64_t slabs = (int64_t)(BR + 63) / 64, tiles = (int64_t)(D + 63) / 64 * ((D + 63) / 64);
+            const int64_t parts = std::min<int64_t>(sa::device_cus() / tiles, slabs / 8);
+            if (parts > 1) p.splits = (int32_t)((slabs + (slabs + parts - 1) / parts - 1) / ((slabs + parts - 1) / parts));
+            if (p.splits > 1) p.off_parts = carve(3 * 4 * (size_t)p.splits * D * D);
+        }
         if (p.tail) p.off_tail = carve(64 * el * (2 * (size_t)h + 4) * D);
         if (p.kind == kCachedProducts) {
             p.off_da = carve(4 * rows * k);
@@ -1905,21 +1918,35 @@ sa_status sa_stca_cached_bwd(const void* cache, const int32_t* cache_rows, int64
         e = sa::launch_tail_rows({{c16(Cc), c16(dU), c16(dob), c16(Qp), c16(dQp), c16(q)}, {(int32_t)hD, (int32_t)hD, D, D, D, D}},
                                  BR, reinterpret_cast<uint16_t*>(ws + p.off_tail), stream);
     }
-    auto over_targets = [&](const sa::GemmDesc& d, const uint16_t* A2, const uint16_t* B2) {
-        return p.tail ? sa::launch_gemm_tail(d, A2, B2, stream) : sa::launch_gemm(d, stream);
+    // sums over the targets, into dW [D,D] or the m-th matrix's parts
+    float* const parts = reinterpret_cast<float*>(ws + p.off_parts);
+    const int64_t DD = (int64_t)D * D;
+    auto over_targets = [&](sa::GemmDesc d, const uint16_t* A2, const uint16_t* B2, int m) {
+        if (!p.tail && p.splits == 1) return sa::launch_gemm(d, stream);
+        if (p.splits > 1) {
+            d.C = parts + m * p.splits * DD;
+            d.c_bf16 = false;
+        } else if (!sa::gemm_parts_supported(d)) {
+            return sa::launch_gemm(d, stream);
+        }
+        return sa::launch_gemm_parts(d, A2, B2, p.splits, DD, stream);
     };
     if (e == hipSuccess) {
         sa::ProfScope ps("cached_weight_grads", stream);
         // dW_V^(i) = sum over targets of C[., i]^T dout[., head i];  dW_K^(i) = sum dU[., i]^T Qp[., head i]
-        e = over_targets({Cc, bf, D, 1, hD, dob, bf, dh, D, 1, dWv, gb, dh, D, D, dh, BR, h, 1.f, false}, tail, dot);
+        e = over_targets({Cc, bf, D, 1, hD, dob, bf, dh, D, 1, dWv, gb, dh, D, D, dh, BR, h, 1.f, false}, tail, dot, 0);
         if (e == hipSuccess)
-            e = over_targets({dU, bf, D, 1, hD, Qp, bf, dh, D, 1, dWk, gb, dh, D, D, dh, BR, h, 1.f, false}, dUt, Qpt);
+            e = over_targets({dU, bf, D, 1, hD, Qp, bf, dh, D, 1, dWk, gb, dh, D, D, dh, BR, h, 1.f, false}, dUt, Qpt, 1);
     }
     if (e == hipSuccess) {
         sa::ProfScope ps("cached_query_grads", stream);   // dq = dQp W_Q^T;  dW_Q = q^T dQp
         e = sa::launch_gemm({dQp, bf, 0, D, 1, Wq, bf, 0, 1, D, dq, gb, 0, D, BR, D, D, 1, 1.f, false}, stream);
         if (e == hipSuccess)
-            e = over_targets({q, bf, 0, 1, D, dQp, bf, 0, D, 1, dWq, gb, 0, D, D, D, BR, 1, 1.f, false}, qt, dQpt);
+            e = over_targets({q, bf, 0, 1, D, dQp, bf, 0, D, 1, dWq, gb, 0, D, D, D, BR, 1, 1.f, false}, qt, dQpt, 2);
+    }
+    if (e == hipSuccess && p.splits > 1) {
+        sa::ProfScope ps("cached_sum_parts", stream);
+        e = sa::launch_sum_parts({parts, {dWv, dWk, dWq}, DD, p.splits, gb}, stream);
     }
     if (e != hipSuccess) return hip_fail(e, "cached STCA backward launch");
     return SA_OK;

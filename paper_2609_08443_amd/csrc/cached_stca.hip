@@ -1,6 +1,6 @@
-// STCA over the sketch cache (sa_stca_cached_fwd / sa_stca_cached_bwd): the row
-// kernels of the path in separate products, in which the cached sketches are read into
-// the workspace and the products run on the batched GEMM.
+// STCA over the sketch cache (sa_stca_cached_fwd / sa_stca_cached_bwd): the small kernels around
+// the weights' gradients, and the row kernels of the path in separate products, in which
+// the cached sketches are read into the workspace and the products run on the batched GEMM.
 //
 // A row is the k fp32 logits of one (user, target, head), of which the user's first n
 // count; one wave per row.  Weights past n are zero, and all of them where n = 0.
@@ -92,7 +92,27 @@ __global__ __launch_bounds__(256) void tail_rows_kernel(TailRows t, int32_t rows
     }
 }
 
+__global__ __launch_bounds__(256) void sum_parts_kernel(SumParts s) {
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    const int m = blockIdx.y;
+    if (i >= s.n) return;
+    const float* from = s.parts + (int64_t)m * s.splits * s.n + i;
+    float4 v = *reinterpret_cast<const float4*>(from);
+    for (int p = 1; p < s.splits; ++p) {
+        const float4 x = *reinterpret_cast<const float4*>(from + p * s.n);
+        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+    }
+    void* const to = m == 0 ? s.to[0] : m == 1 ? s.to[1] : s.to[2];
+    if (s.bf16) *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(to) + i) = make_uint2(tile::pack_bf16x2(v.x, v.y), tile::pack_bf16x2(v.z, v.w));
+    else *reinterpret_cast<float4*>(reinterpret_cast<float*>(to) + i) = v;
+}
+
 }  // namespace
+
+hipError_t launch_sum_parts(const SumParts& s, hipStream_t stream) {
+    hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)((s.n / 4 + 255) / 256), 3), dim3(256), 0, stream, s);
+    return hipGetLastError();
+}
 
 hipError_t launch_tail_rows(const TailRows& t, int32_t rows, uint16_t* to, hipStream_t stream) {
     int64_t n = 0;

@@ -48,6 +48,9 @@ struct MgArgs {
     // pair's k1_slabs (bf16 kernel only): C = alpha (A B + A2 B2)
     const void *A2 = nullptr, *B2 = nullptr;
     int32_t k1_slabs = 0x7fffffff;
+    // with it: k in `splits` parts of `per` slabs (the last may be short), each part's C at c_s
+    int32_t splits = 1, per = 0x7fffffff;
+    int64_t c_s = 0;
 };
 
 // One thread's share of a [128 rows][64 k] slab: four 16-byte pieces of 8 bf16,
@@ -442,7 +445,7 @@ __device__ __forceinline__ bf16x8 lt_frag(const uint8_t* lds, int first, int ks,
     }
 }
 
-// PAIR: a second pair of operands follows the first (MgArgs)
+// PAIR: a second pair of operands follows the first, and k may be split (MgArgs)
 template <int FM, int FN, int PM, int PN, bool A_KC, bool B_KC, bool C_BF16, int NS, bool PAIR = false>
 __global__ __launch_bounds__(256, (LtCfg<FM, FN, PM, PN, NS>::OCC)) void mfma_gemm_lt_kernel(MgArgs g) {
     using C = LtCfg<FM, FN, PM, PN, NS>;
@@ -451,12 +454,19 @@ __global__ __launch_bounds__(256, (LtCfg<FM, FN, PM, PN, NS>::OCC)) void mfma_ge
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t tiles = (int64_t)g.tm * g.tn;
     const int64_t id = xcd_range(blockIdx.x, gridDim.x);
-    const int64_t z = id / tiles;
+    int64_t z = id / tiles;
+    int k0 = 0;   // this workgroup's first slab
+    if constexpr (PAIR) {
+        const int s = __builtin_amdgcn_readfirstlane((int)((uint32_t)z % (uint32_t)g.splits));
+        z = __builtin_amdgcn_readfirstlane((int)((uint32_t)z / (uint32_t)g.splits));
+        k0 = s * g.per;
+        g.C = reinterpret_cast<uint8_t*>(g.C) + s * g.c_s * (C_BF16 ? 2 : 4);
+    }
     const int tt = (int)(id % tiles);
     const int m0 = (tt / g.tn) * C::BM, n0 = (tt % g.tn) * C::BN;
     const uint16_t* Ab = reinterpret_cast<const uint16_t*>(g.A) + z * g.a_z;
     const uint16_t* Bb = reinterpret_cast<const uint16_t*>(g.B) + (g.b_mod > 0 ? z % g.b_mod : z) * g.b_z;
-    const int nk = g.K / GBK;
+    const int nk = PAIR ? min(g.per, g.K / GBK - k0) : g.K / GBK;
     LtOperand<C::BM, A_KC> opa;
     LtOperand<C::BN, B_KC> opb;
     const uint16_t* Ab2 = PAIR ? reinterpret_cast<const uint16_t*>(g.A2) + z * g.a_z : Ab;
@@ -467,8 +477,8 @@ __global__ __launch_bounds__(256, (LtCfg<FM, FN, PM, PN, NS>::OCC)) void mfma_ge
     // slab kt into the stage of slab position pos
     auto issue = [&](int kt, int pos) __attribute__((always_inline)) {
         uint8_t* st = stage(pos);
-        opa.template issue<PAIR>(kt, g.k1_slabs, st, w);
-        opb.template issue<PAIR>(kt, g.k1_slabs, st + C::A_BYTES, w);
+        opa.template issue<PAIR>(k0 + kt, g.k1_slabs, st, w);
+        opb.template issue<PAIR>(k0 + kt, g.k1_slabs, st + C::A_BYTES, w);
     };
 
     f32x16 acc[FM][FN];
@@ -604,7 +614,7 @@ hipError_t lt_launch(MgArgs g, bool c_bf16, int64_t batch, hipStream_t stream) {
     using C = LtCfg<FM, FN, PM, PN, NS>;
     g.tm = (g.M + C::BM - 1) / C::BM;
     g.tn = (g.N + C::BN - 1) / C::BN;
-    const int64_t blocks = (int64_t)g.tm * g.tn * batch;
+    const int64_t blocks = (int64_t)g.tm * g.tn * batch * g.splits;
     if (g.A2) {
         if constexpr (!A_KC && !B_KC && NS > 1) {
             if (c_bf16)
@@ -821,19 +831,31 @@ hipError_t launch_gemm_pair(const GemmDesc& d, const void* A2, const void* B2, h
     return launch_gemm(second, stream);
 }
 
-hipError_t launch_gemm_tail(const GemmDesc& d, const void* A2, const void* B2, hipStream_t stream) {
-    if (d.batch <= 0 || d.M <= 0 || d.N <= 0) return hipSuccess;
+bool gemm_parts_supported(const GemmDesc& d) {
     GemmDesc whole = d;
     whole.K = (d.K + GBK - 1) / GBK * GBK;
-    if (d.a_k == 1 || d.b_k == 1 || d.K <= GBK || !d.a_bf16 || !d.b_bf16 || !gemm_on_matrix_cores(whole) || !al16(A2) ||
-        !al16(B2))
-        return launch_gemm(d, stream);
-    const int shape = choose_lt(whole, false, false);
-    if (shape < 0) return launch_gemm(d, stream);
+    return d.a_bf16 && d.b_bf16 && d.a_k != 1 && d.b_k != 1 && d.K > GBK && gemm_on_matrix_cores(whole) &&
+           choose_lt(whole, false, false) >= 0;
+}
+
+hipError_t launch_gemm_parts(const GemmDesc& d, const void* A2, const void* B2, int32_t splits, int64_t c_s,
+                             hipStream_t stream) {
+    if (d.batch <= 0 || d.M <= 0 || d.N <= 0) return hipSuccess;
+    const int32_t slabs = (d.K + GBK - 1) / GBK, per = (slabs + splits - 1) / splits;
+    if (!gemm_parts_supported(d) || splits < 1 || (slabs + per - 1) / per != splits) return hipErrorInvalidValue;
+    GemmDesc whole = d;
+    whole.K = slabs * GBK;
     MgArgs g = make_args(whole);
-    g.A2 = A2;
-    g.B2 = B2;
+    g.A2 = d.K % GBK ? A2 : d.A;   // (the first pair alone)
+    g.B2 = d.K % GBK ? B2 : d.B;
+    if (!al16(g.A2) || !al16(g.B2)) return hipErrorInvalidValue;
     g.k1_slabs = d.K / GBK;
+    g.splits = splits;
+    g.per = per;
+    g.c_s = c_s;
+    whole.batch *= splits;   // the shape for that many tiles
+    const int shape = choose_lt(whole, false, false);
+    if (shape < 0) return hipErrorInvalidValue;
     return lt_run(shape, g, false, false, d.c_bf16, d.batch, stream);
 }
 

@@ -204,10 +204,13 @@ hipError_t launch_gemm(const GemmDesc& d, hipStream_t stream);
 // C = alpha (A B + A2 B2) (+ C), A2 and B2 with the strides and types of A and B: one
 // product over both contractions where the bf16 kernel takes it, else two.
 hipError_t launch_gemm_pair(const GemmDesc& d, const void* A2, const void* B2, hipStream_t stream);
-// launch_gemm of bf16 operands that are both contiguous along their rows, for a K that is no
-// multiple of 64 and more than that: A2 and B2 hold the last K % 64 of k, with zeros up to 64, in
-// A's and B's strides.
-hipError_t launch_gemm_tail(const GemmDesc& d, const void* A2, const void* B2, hipStream_t stream);
+// launch_gemm of bf16 operands that are both contiguous along their rows, for any K of more than
+// 64.  A2 and B2 hold the last K % 64 of k (if any), with zeros up to 64, in A's and B's strides.
+// splits > 1: the sum over k in that many parts of whole 64s, all of the same number but the last
+// (splits = ceil(slabs / ceil(slabs / splits))), each part's result c_s values after the one before.
+bool gemm_parts_supported(const GemmDesc& d);
+hipError_t launch_gemm_parts(const GemmDesc& d, const void* A2, const void* B2, int32_t splits, int64_t c_s,
+                             hipStream_t stream);
 hipError_t launch_small_gemm_general(const GemmDesc& d, hipStream_t stream);
 
 // Reordered single-query STCA rows (stca.hip), over [rows][k] fp32 logits already
@@ -271,6 +274,15 @@ struct TailRows {
     int32_t width[6];
 };
 hipError_t launch_tail_rows(const TailRows& t, int32_t rows, uint16_t* to, hipStream_t stream);
+// Three matrices of n values (a multiple of 4), each the sum of its parts [3][splits][n]
+struct SumParts {
+    const float* parts;
+    void* to[3];
+    int64_t n;
+    int32_t splits;
+    bool bf16;
+};
+hipError_t launch_sum_parts(const SumParts& s, hipStream_t stream);
 int cached_bwd_kind(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D);
 hipError_t launch_cached_bwd(const CacheView& c, int bits, const CachedBwdArgs& f, hipStream_t stream);
 // softmax rows over each user's valid rows (rows = B Rh of k fp32 logits) and its backward
