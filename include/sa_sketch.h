@@ -512,8 +512,8 @@ size_t sa_stca_cached_bwd_workspace_size(int64_t B, int32_t R, int32_t k, int32_
 /*
  * Backward of sa_stca_cached_fwd: sa_stca_bwd's gradients for the targets and the
  * weights.  Cached sketches are constants (they come from an earlier step), so there
- * is no dXs; a user without rows adds nothing.  The forward is replayed in the
- * workspace.
+ * is no dXs; a user without rows adds nothing, whatever its q and dout hold (NaN and
+ * infinities too).  The forward is replayed in the workspace.
  *
  *   dout                 [B,R,D] in grad_dtype
  *   dq                   output [B,R,D] in grad_dtype

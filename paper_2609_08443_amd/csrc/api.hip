@@ -671,17 +671,19 @@ sa::CacheView cache_view(const void* cache, const int32_t* rows, const int64_t* 
 
 // STCA over cached sketches; operand buffers in the input dtype, as in StcaPlan.
 //   kCachedHeads   workgroups take a head's targets, projections and all:
-//                  [Qp | lse | (bwd) Qp in fp32 | dout in bf16 | C | dU | dQp | tail | parts]
+//                  [Qp | lse | C (bwd) | (bwd) Qp in fp32 | dout | q | dU | dQp | parts | tail]
 //   kCachedRows    the attention alone in one kernel:
-//                  [Qp | lse | U | C | partial results of split keys | (bwd) dout | dC | dU | dQp | tail | parts]
+//                  [Qp | lse | U | C | partial results of split keys | (bwd) dout | q | dC | dU | dQp | parts | tail]
 //   kCachedProducts  in separate products over sketches read into the workspace, Xd [B,k,D]:
-//                  [Qp | lse | U | C | Xd | S (fp32) | alpha | (bwd) dout | dC | dU | dQp | tail |
-//                   parts | dalpha (fp32) | ds]
+//                  [Qp | lse | U | C | Xd | S (fp32) | alpha | (bwd) dout | q | dC | dU | dQp | parts |
+//                   tail | dalpha (fp32) | ds]
+// dout and q here are those that the weights' gradients sum over: zeros for users without rows.
 enum CachedKind { kCachedProducts = 0, kCachedRows = 1, kCachedHeads = 2 };
 struct CachedPlan {
     CachedKind kind = kCachedProducts;
     size_t off_xd = 0, off_qp = 0, off_u = 0, off_s = 0, off_al = 0, off_c = 0, off_lse = 0, off_part = 0, off_dob = 0,
-           off_dc = 0, off_da = 0, off_ds = 0, off_du = 0, off_dqp = 0, off_qf = 0, off_tail = 0, off_parts = 0, total = 0;
+           off_q0 = 0, off_dc = 0, off_da = 0, off_ds = 0, off_du = 0, off_dqp = 0, off_qf = 0, off_tail = 0,
+           off_parts = 0, total = 0;
     // the weights' gradients: over a number of targets that is no multiple of 64, and in parts
     bool tail = false;
     int32_t splits = 1;
@@ -711,7 +713,8 @@ CachedPlan plan_cached(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa
     }
     if (bwd) {
         if (p.kind == kCachedHeads) p.off_qf = carve(4 * BR * D);
-        p.off_dob = carve(dtype == SA_BF16 ? el * BR * D : 0);
+        p.off_dob = carve(el * BR * D);
+        p.off_q0 = carve(el * BR * D);
         if (p.kind != kCachedHeads) p.off_dc = carve(el * rows * D);
         p.off_du = carve(el * rows * D);
         p.off_dqp = carve(el * BR * D);
@@ -799,7 +802,7 @@ hipError_t cached_products(const CachedArgs& a, float* lse, uint8_t* ws, const C
 }
 
 // in separate products: dU from C's gradient dC
-hipError_t cached_products_bwd(const CachedArgs& a, const float* lse, uint8_t* ws, const CachedPlan& p,
+hipError_t cached_products_bwd(const CachedArgs& a, const void* dout, const float* lse, uint8_t* ws, const CachedPlan& p,
                                hipStream_t stream) {
     const bool bf = a.bf;
     const int32_t D = a.D, k = a.k, Rh = a.R * a.h;
@@ -816,7 +819,8 @@ hipError_t cached_products_bwd(const CachedArgs& a, const float* lse, uint8_t* w
     }
     if (e == hipSuccess) {
         sa::ProfScope ps("cached_softmax_bwd", stream);
-        e = sa::launch_cached_softmax_bwd(a.cache, S, lse, dA, a.B * Rh, Rh, a.scale, bf, ds, stream);
+        e = sa::launch_cached_softmax_bwd(a.cache, S, lse, dA, a.B * Rh, Rh, a.scale, bf, ds,
+                                          {a.q, dout, ws + p.off_q0, ws + p.off_dob, ws + p.off_qp, D / a.h}, stream);
     }
     if (e == hipSuccess) {
         sa::ProfScope ps("cached_query_side", stream);
@@ -1896,26 +1900,28 @@ sa_status sa_stca_cached_bwd(const void* cache, const int32_t* cache_rows, int64
     }
     if (p.kind == kCachedProducts) {
         if (e == hipSuccess) e = cached_products(a, lse, ws, p, stream);
-        if (e == hipSuccess) e = cached_products_bwd(a, lse, ws, p, stream);
+        if (e == hipSuccess) e = cached_products_bwd(a, dob, lse, ws, p, stream);
     } else if (e == hipSuccess) {
         sa::ProfScope ps("cached_attention_bwd", stream);
         auto b16 = [](void* x) { return reinterpret_cast<uint16_t*>(x); };
         auto c16 = [](const void* x) { return reinterpret_cast<const uint16_t*>(x); };
         e = sa::launch_cached_bwd(a.cache, a.bits,
-                                  {c16(ws + p.off_u), c16(dC), reinterpret_cast<const float*>(ws + p.off_qf), c16(dob),
-                                   c16(Wk), c16(Wv), b16(Qp), b16(dQp), b16(Cc), b16(dU), B, R, h, scale}, stream);
+                                  {c16(ws + p.off_u), c16(dC), reinterpret_cast<const float*>(ws + p.off_qf), c16(q),
+                                   c16(dob), c16(Wk), c16(Wv), b16(Qp), b16(ws + p.off_q0), b16(ws + p.off_dob), b16(dQp),
+                                   b16(Cc), b16(dU), B, R, h, scale}, stream);
     }
     if (e == hipSuccess && p.kind != kCachedHeads) {
         sa::ProfScope ps("cached_key_side", stream);   // dQp[., head i] = dU[., i] W_K^(i)
         e = sa::launch_gemm({dU, bf, D, hD, 1, Wk, bf, dh, D, 1, dQp, bf, dh, D, BR, dh, D, h, 1.f, false}, stream);
     }
+    const void *q0 = ws + p.off_q0, *do0 = ws + p.off_dob;
     // the targets' last BR % 64 rows of the weights' gradients' operands [C | dU | dout | Qp | dQp | q]
     const uint16_t* tail = reinterpret_cast<const uint16_t*>(ws + p.off_tail);
     const uint16_t *dUt = tail + 64 * hD, *dot = dUt + 64 * hD, *Qpt = dot + 64 * D, *dQpt = Qpt + 64 * D, *qt = dQpt + 64 * D;
     if (e == hipSuccess && p.tail) {
         sa::ProfScope ps("cached_tail_rows", stream);
         auto c16 = [](const void* x) { return reinterpret_cast<const uint16_t*>(x); };
-        e = sa::launch_tail_rows({{c16(Cc), c16(dU), c16(dob), c16(Qp), c16(dQp), c16(q)}, {(int32_t)hD, (int32_t)hD, D, D, D, D}},
+        e = sa::launch_tail_rows({{c16(Cc), c16(dU), c16(do0), c16(Qp), c16(dQp), c16(q0)}, {(int32_t)hD, (int32_t)hD, D, D, D, D}},
                                  BR, reinterpret_cast<uint16_t*>(ws + p.off_tail), stream);
     }
     // sums over the targets, into dW [D,D] or the m-th matrix's parts
@@ -1934,7 +1940,7 @@ sa_status sa_stca_cached_bwd(const void* cache, const int32_t* cache_rows, int64
     if (e == hipSuccess) {
         sa::ProfScope ps("cached_weight_grads", stream);
         // dW_V^(i) = sum over targets of C[., i]^T dout[., head i];  dW_K^(i) = sum dU[., i]^T Qp[., head i]
-        e = over_targets({Cc, bf, D, 1, hD, dob, bf, dh, D, 1, dWv, gb, dh, D, D, dh, BR, h, 1.f, false}, tail, dot, 0);
+        e = over_targets({Cc, bf, D, 1, hD, do0, bf, dh, D, 1, dWv, gb, dh, D, D, dh, BR, h, 1.f, false}, tail, dot, 0);
         if (e == hipSuccess)
             e = over_targets({dU, bf, D, 1, hD, Qp, bf, dh, D, 1, dWk, gb, dh, D, D, dh, BR, h, 1.f, false}, dUt, Qpt, 1);
     }
@@ -1942,7 +1948,7 @@ sa_status sa_stca_cached_bwd(const void* cache, const int32_t* cache_rows, int64
         sa::ProfScope ps("cached_query_grads", stream);   // dq = dQp W_Q^T;  dW_Q = q^T dQp
         e = sa::launch_gemm({dQp, bf, 0, D, 1, Wq, bf, 0, 1, D, dq, gb, 0, D, BR, D, D, 1, 1.f, false}, stream);
         if (e == hipSuccess)
-            e = over_targets({q, bf, 0, 1, D, dQp, bf, 0, D, 1, dWq, gb, 0, D, D, D, BR, 1, 1.f, false}, qt, dQpt, 2);
+            e = over_targets({q0, bf, 0, 1, D, dQp, bf, 0, D, 1, dWq, gb, 0, D, D, D, BR, 1, 1.f, false}, qt, dQpt, 2);
     }
     if (e == hipSuccess && p.splits > 1) {
         sa::ProfScope ps("cached_sum_parts", stream);

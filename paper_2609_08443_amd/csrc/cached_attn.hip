@@ -49,9 +49,9 @@ struct AttnArgs {
     bool out_bf16;
     int32_t R, h, dh;               // dh a multiple of 32; N = R h, row_tiles tiles of targets a head
     // backward: out is dQp (bf16), C is written too
-    const uint16_t* dout;           // [B][R][D] (whole heads; with Qp in fp32, which is left in Qb as bf16)
-    const float* Qf;
-    uint16_t* Qb;
+    const uint16_t *q, *dout;       // [B][R][D]
+    const float* Qf;                // Qp (whole heads), left in Qb as bf16
+    uint16_t *Qb, *q0, *dout0;      // [B][R][D]: Qp, q and dout, zeros for users without rows
     const uint16_t* dC;             // [B][N][D] (else)
     uint16_t* dU;                   // [B][N][D]
     float scale;
@@ -795,7 +795,39 @@ __global__ __launch_bounds__(512) void cached_attn_kernel(AttnArgs a) {
     }
 }
 
-// a user without rows: no C, dU and dQp (and Qp in bf16 as ever)
+// The rows' part of q and dout, copied for the weights' gradients, which sum over the targets of
+// all users: those of users without rows (a padded batch's) may be NaN or infinite, and their zeros
+// in C, dU and dQp times those are NaN.  They go in as zeros, and so does their Qp.
+template <bool HEADS>
+__device__ inline void keep_targets(const AttnArgs& a, int64_t urow, int head, int rows, bool any) {
+    const int D = a.c.D, dh = a.dh;
+    // (a row u's dh values, wherever its row of [B][R][h] is)
+    const int64_t first = HEADS ? urow * D + head * dh : urow * dh, next = HEADS ? D : dh;
+    if (HEADS || dh % 8 == 0) {
+        const int per = dh / 8;
+        for (int i = threadIdx.x; i < rows * per; i += blockDim.x) {
+            const int64_t at = first + i / per * next + 8 * (i % per);
+            uint4 q = make_uint4(0u, 0u, 0u, 0u), d = q;
+            if (any) {
+                q = *reinterpret_cast<const uint4*>(a.q + at);
+                d = *reinterpret_cast<const uint4*>(a.dout + at);
+            } else {
+                *reinterpret_cast<uint4*>(a.Qb + at) = q;
+            }
+            *reinterpret_cast<uint4*>(a.q0 + at) = q;
+            *reinterpret_cast<uint4*>(a.dout0 + at) = d;
+        }
+        return;
+    }
+    for (int i = threadIdx.x; i < rows * dh; i += blockDim.x) {
+        const int64_t at = first + i;
+        a.q0[at] = any ? a.q[at] : (uint16_t)0;
+        a.dout0[at] = any ? a.dout[at] : (uint16_t)0;
+        if (!any) a.Qb[at] = 0;
+    }
+}
+
+// a user without rows: no C, dU and dQp
 template <bool HEADS>
 __device__ inline void no_rows(const AttnArgs& a, int64_t urow, int head, int rows) {
     const int D = a.c.D;
@@ -808,8 +840,8 @@ __device__ inline void no_rows(const AttnArgs& a, int64_t urow, int head, int ro
         for (int i = threadIdx.x; i < rows * a.dh; i += blockDim.x) {
             const int64_t at = (urow + i / a.dh) * D + head * a.dh + i % a.dh;
             reinterpret_cast<uint16_t*>(a.out)[at] = 0;
-            a.Qb[at] = tile::to_bf16(a.Qf[at]);
         }
+    keep_targets<HEADS>(a, urow, head, rows, false);
 }
 
 // accumulators times their rows' factors to [B][R][h][D], bf16
@@ -948,6 +980,7 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_kernel(AttnArgs a) {
             for (int i = 0; i < 4; ++i) f[rm][i] = __shfl(inv[rm], 4 * q + i, 64);
         store_rows<RM, HEADS>(a, a.C, acc, f, urow, head, rows, wave, lane);
     }
+    keep_targets<HEADS>(a, urow, head, rows, true);
     __syncthreads();   // the weights in LDS have been read
     if constexpr (HEADS)
         project_rows<RM>(a.dout + urow * D + head * a.dh, a.Wv + head * a.dh, D, a.dh, rows, wave, lane, Ul, chunks, Ql);
@@ -1136,6 +1169,7 @@ __global__ __launch_bounds__(512) void cached_attn_bwd_loop_kernel(AttnArgs a) {
         for (int i = 0; i < 4; ++i) f[rm][i] = __shfl(inv[rm], 4 * q + i, 64);
     }
     store_rows<RM, HEADS>(a, a.C, acc, f, urow, head, rows, wave, lane);
+    keep_targets<HEADS>(a, urow, head, rows, true);
     clear();
     for (int c0 = 0; c0 < n; c0 += KC) {
         const Keys keys = wave_keys<KT>(c0, min(n, c0 + KC), waves, wave);
@@ -1450,6 +1484,9 @@ hipError_t launch_cached_bwd(const CacheView& c, int bits, const CachedBwdArgs& 
     a.N = f.R * f.h;
     a.row_tiles = ((p.heads ? f.R : a.N) + 16 * p.rm - 1) / (16 * p.rm);
     a.scale2 = f.scale * tile::kLog2e;
+    a.q = f.q;
+    a.q0 = f.q0;
+    a.dout0 = f.dout0;
     a.Qf = f.Qf;
     a.Qb = f.Qb;
     a.Wk = f.Wk;

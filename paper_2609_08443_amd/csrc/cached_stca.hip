@@ -4,6 +4,8 @@
 //
 // A row is the k fp32 logits of one (user, target, head), of which the user's first n
 // count; one wave per row.  Weights past n are zero, and all of them where n = 0.
+#include <type_traits>
+
 #include "cache.h"
 
 namespace sa {
@@ -49,12 +51,16 @@ __global__ __launch_bounds__(256) void cached_softmax_kernel(CacheView c, const 
     if (lane == 0) lse[row] = mx + __logf(z);
 }
 
-// ds_j = scale alpha_j (da_j - sum_i alpha_i da_i), alpha_j = exp(s_j - lse)
+// ds_j = scale alpha_j (da_j - sum_i alpha_i da_i), alpha_j = exp(s_j - lse); and the row's part of the
+// targets for the weights' gradients, zeros where n = 0 (what stands there may be NaN or
+// infinite, and times the zeros of C, dU and dQp it would be NaN in every sum)
 template <bool BF>
 __global__ __launch_bounds__(256) void cached_softmax_bwd_kernel(CacheView c, const float* __restrict__ S,
                                                                  const float* __restrict__ lse,
                                                                  const float* __restrict__ dA, int64_t rows,
-                                                                 int32_t Rh, float scale, void* __restrict__ ds) {
+                                                                 int32_t Rh, float scale, void* __restrict__ ds,
+                                                                 CachedTargets t) {
+    using T = std::conditional_t<BF, uint16_t, float>;
     const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= rows) return;
     int32_t n;
@@ -73,6 +79,12 @@ __global__ __launch_bounds__(256) void cached_softmax_bwd_kernel(CacheView c, co
     dot = wave_sum(dot) / wave_sum(z);
     for (int j = lane; j < c.k; j += 64)
         put<BF>(ds, row * c.k + j, j < n ? scale * __expf(s[j] - l) * (da[j] - dot) : 0.f);
+    for (int j = lane; j < t.dh; j += 64) {
+        const int64_t at = row * t.dh + j;
+        reinterpret_cast<T*>(t.q0)[at] = n ? reinterpret_cast<const T*>(t.q)[at] : T(0);
+        reinterpret_cast<T*>(t.dout0)[at] = n ? reinterpret_cast<const T*>(t.dout)[at] : T(0);
+        if (!n) reinterpret_cast<T*>(t.Qp)[at] = T(0);
+    }
 }
 
 // one thread per 8 columns of a row, the matrices one after the other
@@ -131,13 +143,14 @@ hipError_t launch_cached_softmax(const CacheView& c, const float* S, int64_t row
 }
 
 hipError_t launch_cached_softmax_bwd(const CacheView& c, const float* S, const float* lse, const float* dA,
-                                     int64_t rows, int32_t Rh, float scale, bool bf16, void* ds, hipStream_t stream) {
+                                     int64_t rows, int32_t Rh, float scale, bool bf16, void* ds, const CachedTargets& t,
+                                     hipStream_t stream) {
     if (rows <= 0) return hipSuccess;
     const dim3 grid((unsigned)((rows + 3) / 4));
     if (bf16)
-        hipLaunchKernelGGL(cached_softmax_bwd_kernel<true>, grid, dim3(256), 0, stream, c, S, lse, dA, rows, Rh, scale, ds);
+        hipLaunchKernelGGL(cached_softmax_bwd_kernel<true>, grid, dim3(256), 0, stream, c, S, lse, dA, rows, Rh, scale, ds, t);
     else
-        hipLaunchKernelGGL(cached_softmax_bwd_kernel<false>, grid, dim3(256), 0, stream, c, S, lse, dA, rows, Rh, scale, ds);
+        hipLaunchKernelGGL(cached_softmax_bwd_kernel<false>, grid, dim3(256), 0, stream, c, S, lse, dA, rows, Rh, scale, ds, t);
     return hipGetLastError();
 }
 

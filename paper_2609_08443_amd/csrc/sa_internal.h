@@ -256,12 +256,13 @@ size_t cached_attn_workspace(int64_t B, int32_t R, int32_t h, int32_t k, int32_t
 hipError_t launch_cached_attn(const CacheView& c, int bits, const CachedAttnArgs& f, hipStream_t stream);
 // The attention's backward in one kernel: C and dU [B][R][h][D], bf16.  Kind 1: from U and dC
 // [B][R][h][D]; kind 2: from fp32 Qp and dout [B][R][D], with dQp [B][R][D] and Qp in bf16 (Qb);
-// 0 where it does not take the shape.
+// 0 where it does not take the shape.  q0, dout0 (which may be dout) and Qb afterwards hold q, dout
+// and Qp with zeros for users without rows.
 struct CachedBwdArgs {
     const uint16_t *U, *dC;              // kind 1
     const float* Qf;                     // kind 2
-    const uint16_t *dout, *Wk, *Wv;
-    uint16_t *Qb, *dQp;
+    const uint16_t *q, *dout, *Wk, *Wv;
+    uint16_t *Qb, *q0, *dout0, *dQp;
     uint16_t *C, *dU;
     int64_t B;
     int32_t R, h;
@@ -288,8 +289,16 @@ hipError_t launch_cached_bwd(const CacheView& c, int bits, const CachedBwdArgs& 
 // softmax rows over each user's valid rows (rows = B Rh of k fp32 logits) and its backward
 hipError_t launch_cached_softmax(const CacheView& c, const float* S, int64_t rows, int32_t Rh, bool bf16, void* alpha,
                                  float* lse, hipStream_t stream);
+// Targets [B][R][D] = [rows][dh] in the operand type: q0, dout0 (which may be dout) and Qp are left
+// holding q, dout and Qp with zeros for users without rows
+struct CachedTargets {
+    const void *q, *dout;
+    void *q0, *dout0, *Qp;
+    int32_t dh;
+};
 hipError_t launch_cached_softmax_bwd(const CacheView& c, const float* S, const float* lse, const float* dA,
-                                     int64_t rows, int32_t Rh, float scale, bool bf16, void* ds, hipStream_t stream);
+                                     int64_t rows, int32_t Rh, float scale, bool bf16, void* ds, const CachedTargets& t,
+                                     hipStream_t stream);
 
 // Stacked-SA refinement (block.hip).  add_ln: one row of d features per
 // (user, head, prototype): out[r] = LN(x[r mod x_rows] + y[r]) * gamma[h] + beta[h],

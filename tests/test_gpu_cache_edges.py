@@ -1,0 +1,85 @@
+"""GPU tests of the sketch cache and of the attention over it at the edges of what a call
+may hold: targets of users without rows, sketches of one or two rows, sharp logits, row
+counts that no write has left, bytes at every rounding border, sizes past 32 bits.
+
+Tolerances.  A rounding to bf16 is off by at most half a step, 2^-8 of the value
+(finfo.eps / 2), so n independent ones in a chain add up to at most sqrt(n) 2^-8 by
+2-norm; how many stands at each test.  Everything else is compared bit by bit.
+"""
+import numpy as np
+import pytest
+
+from oracle import cache as oc
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def sa():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2609_08443_amd import sa_sketch
+    sa_sketch.lib()
+    return sa_sketch
+
+
+def generator(*key):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(8443 + sum(p * int(x) for p, x in zip((1, 3, 7, 11, 13), key)))
+    return lambda *shape: torch.randn(shape, generator=g, device="cuda")
+
+
+def off(a, b):
+    return float((a.double() - b).norm() / b.norm())
+
+
+# B, R, k, D, h: one head's targets a workgroup and all of a user's rows, keys in one chunk and in
+# several, heads of odd width, separate products (wider than 1024; the widest with many keys), sums over
+# whole 64s of targets and not
+FORMS = [(11, 40, 150, 384, 12), (32, 40, 100, 1024, 16), (9, 70, 130, 512, 16), (300, 1, 100, 1024, 16),
+         (60, 33, 70, 333, 3), (100, 40, 40, 96, 3), (12, 5, 200, 256, 4), (20, 9, 1100, 512, 4), (6, 5, 1500, 500, 5),
+         (7, 2, 4096, 256, 2), (6, 2, 60, 1100, 11), (10, 16, 1100, 1024, 16)]
+
+
+def batch(sa, B, R, k, D, h, rows, dt=BF, fmt="fp8"):
+    """A written cache, slots, targets, weights and upstream gradients; the last user has no slot."""
+    normal = generator(B, R, k, D, h)
+    c = sa.sketch_cache(B + 1, k, D, fmt)
+    slots = torch.randperm(B, device="cuda")
+    sa.cache_write(c, normal(B, k, D), slots, torch.tensor(rows, dtype=torch.int32, device="cuda"))
+    slots[-1] = -1
+    q, dout = normal(B, R, D).to(dt), normal(B, R, D).to(dt)
+    W = [(normal(D, D) / D ** 0.5).to(dt) for _ in range(3)]
+    return c, slots, q, W, dout
+
+
+# ---------------------------------------------------------------- users without rows
+
+
+@pytest.mark.parametrize("dt,gdt", [(BF, BF), (BF, F32), (F32, F32)])
+@pytest.mark.parametrize("B,R,k,D,h", FORMS)
+def test_targets_of_users_without_rows_may_hold_anything(sa, B, R, k, D, h, dt, gdt):
+    """A padded batch: misses and empty slots, whose q and dout are NaN and infinities, give and
+    add nothing, as if they were zeros."""
+    print(f"no rows B={B} R={R} k={k} D={D} h={h} {dt} {gdt}", flush=True)
+    rows = [k if b % 3 else 0 for b in range(B)]
+    c, slots, q, W, dout = batch(sa, B, R, k, D, h, rows, dt)
+    slots[1] = c.data.shape[0] + 5                      # outside the cache
+    none = torch.tensor([b % 3 == 0 or b in (1, B - 1) for b in range(B)], device="cuda")
+    dout = dout.to(gdt)
+    q[none], dout[none] = 0, 0
+    out, lse = sa.stca_cached_fwd(c, slots, q, *W, h, want_lse=True)
+    want = sa.stca_cached_bwd(c, slots, q, *W, h, dout)
+    assert not out[none].any() and torch.isneginf(lse[none]).all() and not want["dq"][none].any()
+    assert all(torch.isfinite(g).all() and g.any() for g in want.values())
+    for bad in (float("nan"), float("inf")):
+        q[none], dout[none] = bad, bad
+        q[none, :, ::3] = -bad
+        got, glse = sa.stca_cached_fwd(c, slots, q, *W, h, want_lse=True)
+        assert torch.equal(got, out) and torch.equal(glse, lse)
+        grads = sa.stca_cached_bwd(c, slots, q, *W, h, dout)
+        for name in want:
+            assert torch.equal(grads[name], want[name]), (name, bad)
