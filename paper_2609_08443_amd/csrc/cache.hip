@@ -129,13 +129,17 @@ __global__ __launch_bounds__(256) void cache_write_kernel(IoArgs a) {
     }
 }
 
-// Batches of more than kClaimUsers users: rows[] of a slot first takes the number of
-// its last writer, above every count of rows, and its count once the rows are written.
+// Batches of more than kClaimUsers users: rows[] of a slot, cleared of what it held (a
+// count past k would outdo a writer's number), first takes the number of its last writer,
+// above every count of rows, and its count once the rows are written.
+template <bool CLEAR>
 __global__ __launch_bounds__(256) void cache_claim_kernel(IoArgs a) {
     const int64_t b = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (b >= a.B) return;
     const int64_t slot = a.slots[b];
-    if (slot >= 0 && slot < a.n_slots) atomicMax(a.rows + slot, a.k + 1 + (int32_t)b);
+    if (slot < 0 || slot >= a.n_slots) return;
+    if constexpr (CLEAR) a.rows[slot] = 0;
+    else atomicMax(a.rows + slot, a.k + 1 + (int32_t)b);
 }
 __global__ __launch_bounds__(256) void cache_settle_kernel(IoArgs a) {
     const int64_t b = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -247,7 +251,10 @@ hipError_t launch_cache_write(const CacheView& c, int bits, const void* Xs, bool
     a.n = n;
     a.claimed = B > kClaimUsers;
     const dim3 grid((unsigned)(B * a.per_user)), users((unsigned)((B + 255) / 256));
-    if (a.claimed) hipLaunchKernelGGL(cache_claim_kernel, users, dim3(256), 0, stream, a);
+    if (a.claimed) {
+        hipLaunchKernelGGL(cache_claim_kernel<true>, users, dim3(256), 0, stream, a);
+        hipLaunchKernelGGL(cache_claim_kernel<false>, users, dim3(256), 0, stream, a);
+    }
     const bool vec = c.D % (bf16 ? 8 : 4) == 0;
 #define SA_LAUNCH(BITS, BF, VEC)                \
     if (bits == BITS && bf16 == BF && vec == VEC) \

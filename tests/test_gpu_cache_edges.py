@@ -83,3 +83,31 @@ def test_targets_of_users_without_rows_may_hold_anything(sa, B, R, k, D, h, dt, 
         grads = sa.stca_cached_bwd(c, slots, q, *W, h, dout)
         for name in want:
             assert torch.equal(grads[name], want[name]), (name, bad)
+
+
+# ---------------------------------------------------------------- row counts
+
+
+@pytest.mark.parametrize("B", [5, 1024, 1025, 3000])
+def test_a_write_takes_any_row_count(sa, B):
+    """Counts past k (of a cache of longer sketches, or memory that nobody has cleared) read as k
+    rows, and a write to their slots is a write, whatever the batch's size."""
+    k, D, n_slots = 3, 40, 6000
+    normal = generator(B)
+    c = sa.sketch_cache(n_slots, k, D, "fp8")
+    c.data.fill_(255)
+    left = torch.tensor([k + 1, 100, B + k, B + 5000, 2 ** 31 - 1, -1, -2 ** 31, k + 1 + B // 2], dtype=torch.int32)
+    c.rows.copy_(left.repeat(n_slots // 8 + 1)[:n_slots])
+    before = c.rows.clone()
+    slots = torch.randperm(n_slots, device="cuda")[:B]
+    slots[B // 2] = slots[B - 1]                        # the last of the two stays
+    n = torch.randint(0, k + 1, (B,), device="cuda", dtype=torch.int32)
+    x = normal(B, k, D)
+    sa.cache_write(c, x, slots, n)
+    want = before.clone()
+    want[slots[B // 2 + 1:]], want[slots[:B // 2]] = n[B // 2 + 1:], n[:B // 2]
+    assert torch.equal(c.rows, want)
+    clean = sa.sketch_cache(n_slots, k, D, "fp8")
+    for at in range(0, B, 512):
+        sa.cache_write(clean, x[at:at + 512].contiguous(), slots[at:at + 512].clone(), n[at:at + 512].clone())
+    assert torch.equal(sa.cache_read(c, slots), sa.cache_read(clean, slots))
