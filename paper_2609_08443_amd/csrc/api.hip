@@ -833,7 +833,8 @@ hipError_t cached_products_bwd(const CachedArgs& a, const void* dout, const floa
 // whether the plan's kernels take that many users and rows
 sa_status check_cached_plan(const CachedPlan& p, int64_t B, int32_t R, int32_t k, int32_t D, int32_t h) {
     if (p.kind != kCachedProducts) return SA_OK;   // (their plans are of launches that fit)
-    if (B * R * h >= (int64_t(1) << 26)) return fail(SA_ERR_UNSUPPORTED, "sizes beyond the supported range");
+    // (the softmax: four rows a workgroup of 256 threads)
+    if ((B * R * h + 3) / 4 >= (int64_t(1) << 24)) return fail(SA_ERR_UNSUPPORTED, "sizes beyond the supported range");
     return check_cache_io(B, k, D);
 }
 
