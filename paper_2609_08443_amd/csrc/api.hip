@@ -723,7 +723,8 @@ CachedPlan plan_cached(int64_t B, int32_t R, int32_t k, int32_t D, int32_t h, sa
         // a call): 100 targets, D = 1024 67 / 77; 250, D = 256 39 / 46; 1,000, D = 1024 181 / 255;
         // 2,460, D = 512 142 / 210.
         const bool in64s = dtype == SA_BF16 && BR > 64 && BR < (int64_t(1) << 31) && D / h % 8 == 0;
-        p.tail = in64s && BR % 64 != 0;
+        // (counted in 32 bits, in pieces of 8 values)
+        p.tail = in64s && BR % 64 != 0 && 8 * (2 * (int64_t)h + 4) * D < (int64_t(1) << 31);
         // Narrow matrices over many targets: too few tiles of 64 x 64 for the compute units, so the
         // targets in parts of at least 8 of their 64s, whose sums are added up.  In parts / whole (us
         // a call): 1,000 targets, D = 256 54 / 59; 10,000, D = 256 100 / 245; 1,024, D = 512 66 / 69;
