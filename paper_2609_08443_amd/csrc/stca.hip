@@ -7,6 +7,8 @@
 // alpha from the same rounded logits).  One wave per row.  With k a multiple of 4 and at most 1024, a row is read once into
 // registers (16 bytes per lane per 256 columns) and every pass runs on them;
 // otherwise lanes stride the row in each pass.
+#include <algorithm>
+
 #include "sa_internal.h"
 #include "tile_ops.h"
 
@@ -222,10 +224,11 @@ __global__ __launch_bounds__(256) void stca_softmax_b8_kernel(const uint16_t* __
     }
     if (lane == 0) lse[row] = mx + __logf(z);
 }
+// (a launch has fewer than 2^32 threads, and there may be more values)
 __global__ __launch_bounds__(256) void to_bf16_kernel(const float* __restrict__ x, uint16_t* __restrict__ y,
                                                       int64_t n) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) y[i] = tile::to_bf16(x[i]);
+    const int64_t threads = (int64_t)gridDim.x * 256;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += threads) y[i] = tile::to_bf16(x[i]);
 }
 
 }  // namespace
@@ -304,7 +307,8 @@ hipError_t launch_stca_softmax_bwd(const void* S, bool s_bf16, const float* lse,
 }
 hipError_t launch_to_bf16(const float* x, uint16_t* y, int64_t n, hipStream_t stream) {
     if (n <= 0) return hipSuccess;
-    hipLaunchKernelGGL(to_bf16_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, x, y, n);
+    const int64_t blocks = std::min<int64_t>((n + 255) / 256, 1 << 22);
+    hipLaunchKernelGGL(to_bf16_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, x, y, n);
     return hipGetLastError();
 }
 

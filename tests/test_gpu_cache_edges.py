@@ -111,3 +111,36 @@ def test_a_write_takes_any_row_count(sa, B):
     for at in range(0, B, 512):
         sa.cache_write(clean, x[at:at + 512].contiguous(), slots[at:at + 512].clone(), n[at:at + 512].clone())
     assert torch.equal(sa.cache_read(c, slots), sa.cache_read(clean, slots))
+
+
+# ---------------------------------------------------------------- sizes past 32 bits
+
+
+def test_more_than_four_giga_values_of_targets(sa):
+    """4.26 million targets at D = 1024, 2^32 + 67 million values: gradients asked for in fp32 are,
+    rounded, those asked for in bf16 of the same dout bit for bit, and the last user's are a small
+    call's (by 2-norm the eight roundings of the gradients)."""
+    B, R, k, D = 65535, 65, 4, 1024
+    if torch.cuda.mem_get_info()[0] < 170 << 30:
+        pytest.skip("needs 170 GB")
+    assert B * R * D > 1 << 32
+    normal = generator(B, R)
+    c = sa.sketch_cache(3, k, D, "fp8")
+    sa.cache_write(c, normal(3, k, D), torch.arange(3, device="cuda"))
+    slots = torch.arange(B, device="cuda") % 3
+    W = [(normal(D, D) / 32).to(BF) for _ in range(3)]
+    q, dout = (torch.empty((B, R, D), dtype=BF, device="cuda") for _ in range(2))
+    for at in range(0, B, 4096):                     # (other targets everywhere)
+        m = min(4096, B - at)
+        q[at:at + m], dout[at:at + m] = normal(m, R, D), normal(m, R, D)
+    ws = torch.empty(sa.stca_cached_bwd_workspace_size(B, R, k, D, 1, sa.SA_BF16), dtype=torch.uint8, device="cuda")
+    half = sa.stca_cached_bwd(c, slots, q, *W, 1, dout, workspace=ws)
+    single = sa.stca_cached_bwd(c, slots[-1:].clone(), q[-1:].contiguous(), *W, 1, dout[-1:].contiguous())
+    assert off(half["dq"][-1:], single["dq"].double()) <= 8 ** 0.5 * 2.0 ** -8
+    full = sa.stca_cached_bwd(c, slots, q, *W, 1, dout.float(), workspace=ws)
+    for name in full:
+        assert full[name].dtype == F32 and bool(half[name].any())
+        a, b = full[name].view(-1, D), half[name].view(-1, D)
+        assert all(torch.equal(a[at:at + (1 << 20)].to(BF), b[at:at + (1 << 20)]) for at in range(0, a.shape[0], 1 << 20))
+    del ws, half, full, q, dout
+    torch.cuda.empty_cache()
