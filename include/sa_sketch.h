@@ -498,7 +498,8 @@ size_t sa_stca_cached_fwd_workspace_size(int64_t B, int32_t R, int32_t k, int32_
  *
  * bf16 mode rounds q W_Q, u, the softmax weights and the aggregates to bf16, as
  * sa_stca_fwd does, but not the logits; fp32 mode rounds nothing below fp32.  Errors,
- * ownership and streams as for sa_sketch_fwd; B = 0 is a no-op.
+ * ownership and streams as for sa_sketch_fwd; B = 0 is a no-op.  SA_ERR_UNSUPPORTED as
+ * well for B > 65,535 and for B R h or R h k from 2^31 on.
  */
 sa_status sa_stca_cached_fwd(const void* cache, const int32_t* cache_rows, int64_t n_slots, const int64_t* slots,
                              sa_cache_format format, const void* q, const void* Wq, const void* Wk, const void* Wv,

@@ -6,9 +6,10 @@
 // each lane's values are whole 16-byte pieces, each row of the wave a run of 128
 // (bf16) or 256 bytes, the codes of the wave 256 or 512 contiguous bytes, and the four
 // lanes of a group's values find its largest magnitude in two exchanges.  Measured: 128
-// sketches of 512 x 1024 from bf16 to 8 bits 46 us (203 MB, 4.4 TB/s) and back 33 us, 64
-// of 1024 x 1024 from 4 bits to bf16 28 us (170 MB, 6.1 TB/s: the codes from the cache
-// behind the L2); a copy of 1 GB runs at 5.0 TB/s.
+// sketches of 512 x 1024 from bf16 to 8 bits 43 us (203 MB, 4.7 TB/s) and back 32 us (the
+// codes from the cache behind the L2), 64 of 1024 x 1024 from 4 bits to bf16 35 us (170 MB,
+// 4.8 TB/s; 27 into the same 134 MB again and again, which that cache then holds); a copy
+// of 1 GB runs at 5.0 TB/s.
 #include "cache.h"
 
 namespace sa {

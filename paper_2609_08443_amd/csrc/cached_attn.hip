@@ -18,8 +18,13 @@
 // together), decodes it along the columns and pairs neighbouring keys with byte
 // permutes, which makes the block eight operands of 8 keys each: no code passes LDS.
 //
-// The running maximum, the sum and both accumulators are fp32; the weights are rounded to
-// bf16 as matrix-core operands, the result once.
+// The running maximum, the sum and both accumulators are fp32.  Operands of the matrix cores
+// are bf16, each rounded once: q W_Q, the rows u, the weights, the aggregates, and the result
+// where it is asked for so.  Off by 0.36 to 0.39% by 2-norm with full sketches, a bf16 result
+// alone by 0.17%.  In two bf16 parts u and the weights would double both contractions, and two
+// parts of 48 rows u do not fit LDS; with q W_Q in two parts the result is off by 0.30 to 0.32%
+// and a call takes 2% longer (one target, 16 users with 300, 32 with 40), with the aggregates
+// besides 0.27% and 4 to 11%.
 #include <algorithm>
 #include <type_traits>
 
@@ -1284,7 +1289,8 @@ struct AttnPlan {
 //   R = 300, B = 4     122   94   76   88 / 127  107  103
 // that is, heads: 9 and a round of workgroups 5 + 2.5 rm and 13.5 + 2.7 rm for 512 keys (at
 // k = 1024 40, 46, 54, 63 a round); all rows: 27, 3 and the partial sums' bytes to join splits, and a round 5 and 15, 22 or
-// 33 for 512 keys.  Widths below 1024 scale both, not below a half: latency.
+// 33 for 512 keys.  Widths below 1024 scale both, not below a half: latency.  (fp8 counts as fp4, and
+// every slot as k rows: the host does not know how many it holds.)
 AttnPlan attn_plan(int64_t B, int32_t R, int32_t h, int32_t k, int32_t D) {
     const int waves = (D + 127) / 128;
     const int64_t slots = (int64_t)device_cus() * std::max(1, 8 / waves);   // eight waves a compute unit
