@@ -531,6 +531,90 @@ sa_status sa_stca_cached_bwd(const void* cache, const int32_t* cache_rows, int64
                              void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Attention of targets over their users' recent histories, as they lie in the packed
+ * batch: the recent branch of two-time-scale reasoning (section 3.4), beside the STCA over
+ * the sketch.  Per user, target i and head (query head y reads key head y / (h / hk)), over
+ * the tokens j of the user's history that the target sees:
+ *
+ *   s_j = scale <q_i, K_j>;   with cap > 0: s_j = cap tanh(s_j / cap);
+ *   with slopes: s_j -= slopes[y] (e_i - 1 - j)       (nearer tokens preferred)
+ *   lse = log sum_j exp(s_j),  out = sum_j exp(s_j - lse) V_j
+ *
+ * Target i sees the tokens [max(0, e_i - window), e_i) of its own user's, e_i = ends[i] held
+ * to [0, the user's tokens], or all of them without ends; window = 0: no limit.  (ends are the
+ * request-aware masks of section 4.2: a target sees what came before its request.)  A target
+ * that sees no token, or whose scores are all -inf, gets out = 0 and lse = -inf.
+ *
+ *   q                [N,h,d] queries of the targets, user by user (dtype)
+ *   K, V             [T,hk,d] keys and values of the tokens, user by user (dtype)
+ *   q_stride, ...    elements from a target's (token's) first head to the next one's, and from
+ *                    head to head; the d values of a head lie together.  0: as packed
+ *                    (h d and d; hk d and d)
+ *   targets          [B+1] int64 CSR offsets of the users' targets, offsets [B+1] of their tokens
+ *   ends             [N] int32 or NULL;  slopes [h] fp32, or NULL for none
+ *   B, T, N, h, hk, d    h a multiple of hk, d in {64, 128}
+ *   window           tokens, >= 0;  cap >= 0, finite (0: none);  scale finite and > 0
+ *
+ * Targets behind the last user's (from targets[B] on) see nothing; tokens behind the last
+ * user's (from offsets[B] on) are seen by none.  A NaN or infinity in a token reaches the
+ * targets that see it, and no others.
+ */
+typedef struct {
+    const void *q, *K, *V;
+    int64_t q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride;
+    const int64_t *offsets, *targets;
+    const int32_t* ends;
+    const float* slopes;
+    int64_t B, T, N;
+    int32_t h, hk, d, window;
+    float scale, cap;
+    sa_dtype dtype;
+} sa_recent_attn;
+
+/* Bytes of workspace that sa_recent_attn_fwd needs (sizes and dtype of the call). */
+size_t sa_recent_attn_fwd_workspace_size(const sa_recent_attn* a);
+
+/*
+ * Forward.
+ *
+ *   out      output [N,h,d] (dtype), packed;  lse output [N,h] fp32, or NULL (the backward
+ *            needs it)
+ *
+ * bf16 mode rounds the softmax weights and the result to bf16 and sums in fp32; fp32 mode
+ * rounds nothing below fp32.  Base addresses and strides must be multiples of 16 bytes;
+ * targets' (tokens') strides, and the heads of one, span less than 2^24 elements.  N = 0 is a
+ * no-op.  SA_ERR_UNSUPPORTED for more than 65,536 heads, and for T, N h or B + T / 128 from
+ * 2^31 on.  Errors, ownership and streams as for sa_sketch_fwd.
+ */
+sa_status sa_recent_attn_fwd(const sa_recent_attn* a, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
+/* Bytes of workspace that sa_recent_attn_bwd needs (sizes and dtype of the call). */
+size_t sa_recent_attn_bwd_workspace_size(const sa_recent_attn* a);
+
+/* The gradients of a call of sa_recent_attn_bwd, with strides like those of q, K and V: a
+ * projection's gradient may hold them side by side. */
+typedef struct {
+    void *dq, *dK, *dV;
+    int64_t dq_stride, dq_head_stride, dk_stride, dk_head_stride, dv_stride, dv_head_stride;
+} sa_recent_attn_grads;
+
+/*
+ * Backward: gradients of <dout, out> for q, K and V (slopes, cap and ends are constants).
+ *
+ *   out, lse     what sa_recent_attn_fwd wrote for the same inputs
+ *   dout         [N,h,d] (dtype), packed
+ *   grads        dq, dK, dV (dtype), overwritten; zeros for targets that see nothing and for
+ *                tokens that no target sees, those behind the last user's too
+ *
+ * A target that sees nothing adds nothing, whatever its q and dout hold.  bf16 mode rounds
+ * the softmax weights, their gradients and the results to bf16 and sums in fp32.  N = 0 and
+ * T = 0 leave only zeros to write.  Other arguments and errors as for sa_recent_attn_fwd.
+ */
+sa_status sa_recent_attn_bwd(const sa_recent_attn* a, const void* out, const float* lse, const void* dout,
+                             const sa_recent_attn_grads* grads, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * The forward's ranges as a list of segments (the fused backward's work list),
  * exposed for exact testing.
  *

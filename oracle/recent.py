@@ -1,0 +1,121 @@
+"""Attention over recent histories in fp64 numpy, by its formulas, with how far a result in
+lower precision may be off.  TEST INFRASTRUCTURE ONLY: used by tests/, never by the library.
+
+A rounding to bf16 is off by at most 2^-8 of the value (finfo.eps / 2), a single-precision
+operation by at most U = 2^-23 of its result, whichever way it rounds; a sum of n terms by at
+most n U of the sum of their magnitudes.  The bounds follow these through the formulas to first
+order, element by element:
+
+  score    scale (d + 2) U sum |q||K|, + 4 U cap (tanh), + 3 U slope (distance + 36)
+  weight p, relative    the score's, + 6 U (|s| + |lse| + 4) (change of base, exponent, exp)
+  out      sum p |V| (p's, + its mean over the row, + a rounding of p, + (keys + 8) U) + a rounding
+  lse      the mean over the row of p's, + (keys + 8) U, + 2 U |lse|
+  backward: delta = <dout, out> with out as given (one rounding), dP = dout V^T,
+  ds = scale p c (dP - delta), c = 1 - tanh^2, and one rounding of p and of ds before the sums.
+"""
+from __future__ import annotations
+
+import numpy as np
+
+U = 2.0 ** -23
+HALF = {"bf16": 2.0 ** -8, "fp32": U}   # of a value held in the operands' type
+
+
+def visible(L, ends, window):
+    """[R, L]: token j is in [max(0, e - window), e), e held to [0, L]."""
+    e = np.clip(np.asarray(ends, np.int64), 0, L)
+    j = np.arange(L)
+    lo = np.maximum(0, e - window) if window else np.zeros_like(e)
+    return (j >= lo[:, None]) & (j < e[:, None]), e[:, None] - 1 - j
+
+
+def _scores(q, K, see, dist, scale, cap, slope):
+    """One head: s [R, L] (masked), tanh or None, and how far s may be off."""
+    x = scale * (q @ K.T)
+    err = scale * (q.shape[1] + 2) * U * (np.abs(q) @ np.abs(K).T)
+    t = None
+    if cap:
+        t = np.tanh(x / cap)
+        x = cap * t
+        err = err + 4 * U * cap
+    if slope is not None:
+        x = x - slope * dist
+        err = err + 3 * U * abs(slope) * (np.abs(dist) + 36)
+    return np.where(see, x, -np.inf), t, err
+
+
+def _lse(s):
+    top = s.max(1, initial=-np.inf)
+    safe = np.where(np.isfinite(top), top, 0.0)
+    with np.errstate(divide="ignore"):
+        return safe + np.log(np.exp(s - safe[:, None]).sum(1))
+
+
+def _walk(offsets, targets, h, hk):
+    for b in range(len(offsets) - 1):
+        for y in range(h):
+            yield slice(offsets[b], offsets[b + 1]), slice(targets[b], targets[b + 1]), y, y // (h // hk)
+
+
+def _weights(q, K, toks, rows, y, x, ends, window, slopes, scale, cap):
+    L = toks.stop - toks.start
+    e = np.full(rows.stop - rows.start, L) if ends is None else ends[rows]
+    see, dist = visible(L, e, window)
+    s, t, es = _scores(q[rows, y], K[toks, x], see, dist, scale, cap, None if slopes is None else float(slopes[y]))
+    lse = _lse(s)
+    fine = np.isfinite(lse)
+    with np.errstate(invalid="ignore"):
+        p = np.where(see & fine[:, None], np.exp(s - np.where(fine, lse, 0.0)[:, None]), 0.0)
+        off = np.where(see & fine[:, None], es + 6 * U * (np.abs(np.where(see, s, 0.0)) + np.abs(np.where(fine, lse, 0.0))[:, None] + 4), 0.0)
+    return p, t, lse, off, es
+
+
+def fwd(q, K, V, offsets, targets, ends=None, window=0, slopes=None, scale=None, cap=0.0, dtype="bf16"):
+    """out, lse and how far each may be off."""
+    q, K, V = (np.asarray(x, np.float64) for x in (q, K, V))
+    N, h, d = q.shape
+    scale = d ** -0.5 if scale is None else scale
+    half = HALF[dtype]
+    out, lse = np.zeros((N, h, d)), np.full((N, h), -np.inf)
+    o_off, l_off = np.zeros((N, h, d)), np.zeros((N, h))
+    for toks, rows, y, x in _walk(offsets, targets, h, K.shape[1]):
+        p, _, z, off, _ = _weights(q, K, toks, rows, y, x, ends, window, slopes, scale, cap)
+        n, v = p.shape[1], np.abs(V[toks, x])
+        mean = (p * off).sum(1)
+        out[rows, y], lse[rows, y] = p @ V[toks, x], z
+        o_off[rows, y] = (p * (off + mean[:, None] + (half if dtype == "bf16" else 0) + (n + 8) * U)) @ v
+        o_off[rows, y] += half * np.abs(out[rows, y])
+        l_off[rows, y] = mean + (n + 8) * U + 2 * U * np.abs(np.where(np.isfinite(z), z, 0.0))
+    return out, lse, o_off, l_off
+
+
+def bwd(q, K, V, offsets, targets, dout, ends=None, window=0, slopes=None, scale=None, cap=0.0, dtype="bf16"):
+    """{"dq", "dK", "dV"} and how far each may be off, for out and lse as fwd gives them, rounded."""
+    q, K, V, dout = (np.asarray(x, np.float64) for x in (q, K, V, dout))
+    N, h, d = q.shape
+    scale = d ** -0.5 if scale is None else scale
+    half = HALF[dtype]
+    low = half if dtype == "bf16" else 0.0
+    g = {"dq": np.zeros(q.shape), "dK": np.zeros(K.shape), "dV": np.zeros(V.shape)}
+    e = {k: np.zeros(v.shape) for k, v in g.items()}
+    for toks, rows, y, x in _walk(offsets, targets, h, K.shape[1]):
+        p, t, z, off, es = _weights(q, K, toks, rows, y, x, ends, window, slopes, scale, cap)
+        R, L = p.shape
+        off = off + 2 * U * np.abs(np.where(np.isfinite(z), z, 0.0))[:, None]
+        do, k, v, qq = dout[rows, y], K[toks, x], V[toks, x], q[rows, y]
+        o = p @ v
+        delta, d_off = (do * o).sum(1), (np.abs(do) * np.abs(o)).sum(1) * (half + (d + 2) * U)
+        dp, dp_off = do @ v.T, (d + 2) * U * (np.abs(do) @ np.abs(v).T)
+        c, c_off = (1.0, 0.0) if t is None else (1 - t * t, 2 * np.abs(t) * (es / cap + 4 * U) + 2 * U)
+        rest = dp - delta[:, None]
+        ds = scale * p * c * rest
+        ds_off = scale * p * (c * (dp_off + d_off[:, None]) + np.abs(rest) * (c * (off + 4 * U) + c_off)) + low * np.abs(ds)
+        g["dq"][rows, y] += ds @ k
+        g["dK"][toks, x] += ds.T @ qq
+        g["dV"][toks, x] += p.T @ do
+        e["dq"][rows, y] += (ds_off + np.abs(ds) * (L + 8) * U) @ np.abs(k)
+        # (a shared head's sums run over all rows that read it)
+        rr = (R * (h // K.shape[1]) + 8) * U
+        e["dK"][toks, x] += (ds_off + np.abs(ds) * rr).T @ np.abs(qq)
+        e["dV"][toks, x] += (p * (off + low + rr)).T @ np.abs(do)
+    return g, {k: v + half * np.abs(g[k]) for k, v in e.items()}

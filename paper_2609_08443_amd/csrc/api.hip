@@ -1009,6 +1009,15 @@ sa_status run_bwd(const void* K, const void* V, const void* P, const int64_t* of
 
 namespace sa {
 
+sa_status api_fail(sa_status st, const char* fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_last_error, sizeof(g_last_error), fmt, ap);
+    va_end(ap);
+    return st;
+}
+void api_clear() { g_last_error[0] = 0; }
+
 // per-device constant: number of compute units (read once per device)
 static constexpr int kMaxCuDevices = 64;
 static std::once_flag g_cu_once[kMaxCuDevices];

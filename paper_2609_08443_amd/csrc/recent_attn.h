@@ -1,0 +1,309 @@
+// Attention of targets over the recent tokens of their users' packed histories: what its
+// kernels share (recent_attn.hip, recent_attn_rows.h, recent_attn_keys.hip).
+//
+// A "row" is one target's query of one head.  The g = h / hk query heads that read key head
+// kv stand side by side: row r of a user and key head is target r / g, head kv g + r % g, so
+// that shared heads fill a tile's rows together and read their keys once.
+#pragma once
+
+#include "sa_internal.h"
+#include "tile_ops.h"
+
+namespace sa {
+namespace attn {
+
+using namespace tile;
+
+// What a call reads (sa_recent_attn), strides in elements.
+struct View {
+    const void *q, *K, *V;
+    const int64_t *offsets, *targets;
+    const int32_t* ends;
+    const float* slopes;
+    int64_t B, T, N;
+    int32_t h, hk, g, window;
+    float scale, cap;
+    int64_t q_t, q_h, k_t, k_h, v_t, v_h;
+};
+
+// The forward pass and the queries' gradients go over tiles of `bq` rows of one user (all key
+// heads alike), a tile's keys in units of `unit` of them.
+struct TileRec {
+    int32_t user, row0;   // user B: the targets behind the last user's
+    int32_t klo, khi;     // the tokens that any of the tile's targets sees
+};
+struct Plan {
+    const TileRec* recs;      // [tiles]
+    const int64_t* prefix;    // [tiles + 1] units before each tile (at least one a tile with rows)
+    int64_t tiles;
+    int32_t min_units;        // fewest units a workgroup takes
+};
+
+// The whole work is hk times the tiles' units, key head by key head, in equal pieces.
+__device__ inline int64_t pieces(const Plan& p, int32_t hk, int64_t grid, int64_t* total) {
+    const int64_t X = p.prefix[p.tiles] * hk;
+    *total = X;
+    const int64_t most = X / p.min_units;
+    return most < 1 ? 1 : most < grid ? most : grid;
+}
+
+// the last tile that begins at or before a key head's unit
+__device__ inline int64_t tile_at(const Plan& p, int64_t unit) {
+    int64_t lo = 0, hi = p.tiles;
+    while (hi - lo > 1) {
+        const int64_t m = (lo + hi) / 2;
+        if (p.prefix[m] <= unit) lo = m;
+        else hi = m;
+    }
+    return lo;
+}
+
+struct User {
+    int64_t t0, tok0;   // first target, first token
+    int32_t n, L;       // targets, tokens
+};
+// User b of B, or b = B: the targets behind the last one's, which see no token.
+__device__ inline User user_at(const View& a, int64_t b) {
+    auto cut = [](int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; };
+    User u;
+    u.t0 = cut(a.targets[b], 0, a.N);
+    u.n = (int32_t)((b < a.B ? cut(a.targets[b + 1], u.t0, a.N) : a.N) - u.t0);
+    u.tok0 = cut(a.offsets[b], 0, a.T);
+    u.L = b < a.B ? (int32_t)(cut(a.offsets[b + 1], u.tok0, a.T) - u.tok0) : 0;
+    return u;
+}
+
+// The user whose tiles include tile t, where user b's begin at first[b] per / size + b: one tile more
+// than its rows take at most, so that the tiles of all users number rows / size + B + 1
+// without a look at the offsets.  Also its first tile.
+__device__ inline int64_t user_of_tile(const int64_t* first, int64_t B, int64_t most, int32_t per, int32_t size, int64_t t,
+                                       int64_t* tile0) {
+    auto base = [&](int64_t b) {
+        const int64_t v = first[b] < 0 ? 0 : first[b] > most ? most : first[b];
+        return v * per / size + b;
+    };
+    int64_t lo = 0, hi = B + 1;
+    while (hi - lo > 1) {
+        const int64_t m = (lo + hi) / 2;
+        if (base(m) <= t) lo = m;
+        else hi = m;
+    }
+    *tile0 = base(lo);
+    return lo;
+}
+
+// Tokens [lo, hi) of the user's that its target i (of the whole batch) sees
+__device__ inline void seen(const View& a, const User& u, int64_t i, int32_t* lo, int32_t* hi) {
+    int32_t e = u.L;
+    if (a.ends) {
+        e = a.ends[i];
+        e = e < 0 ? 0 : e > u.L ? u.L : e;
+    }
+    *hi = e;
+    *lo = a.window > 0 && e > a.window ? e - a.window : 0;
+}
+
+// Direct global -> LDS copy of 16 bytes a lane from base + off (base wave-uniform) to LDS bytes
+// [lds + 16 lane, + 16), as inline assembly: for the builtin the compiler makes the transposing
+// LDS reads wait for every such load in flight, the next unit's included.  Awaited by explicit
+// vmcnt waits.  M0, which holds the LDS address, is reserved: saved and restored.
+__device__ __forceinline__ void dma16(const char* base, uint32_t off, const void* lds) {
+    const uint32_t l = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)lds;
+    uint32_t saved;
+    asm volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %3\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dwordx4 %1, %2\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "v"(off), "s"(base), "s"(l)
+        : "memory");
+}
+// at most N of this wave's loads still in flight; no LDS operation
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (0 << 8) | ((N >> 4) << 14));
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ __forceinline__ void barrier() {
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ inline float swap_halves(float v, float (*f)(float, float)) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float add_(float a, float b) { return a + b; }
+__device__ inline float max_(float a, float b) { return fmaxf(a, b); }
+
+// Products of a 32-row tile in LDS, [32][D] of T, 16-byte chunks swizzled within each row, with
+// operands that hold 32 columns one a lane (l % 32; k over the halves).
+//   with_rows   C(m, n) += sum_k tile(m, k) f(k, n), f held as Frag
+//   with_cols   C(m, n) += sum_k tile(k, m) p(k, n), m over D, p as a result of with_rows has it
+template <typename T, int D>
+struct Tile32;
+
+template <int D>
+struct Tile32<uint16_t, D> {
+    static constexpr int CHUNKS = D / 8;   // 16-byte chunks a row
+    struct Frag {
+        bf16x8 v[D / 16];
+    };
+    struct Cols {
+        bf16x8 v[2];
+    };
+    __device__ static int chunk_at(int row, int pos) { return pos ^ swz_x<D>(row); }
+    // lane l: 8 values each of row `p` at columns 16 i + 8 (l / 32)
+    __device__ static void load(Frag& f, const uint16_t* p, bool ok, int hl) {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+            f.v[i] = ok ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(p + 16 * i + 8 * hl)) : bf16x8{};
+    }
+    __device__ static float dot(const Frag& a, const Frag& b) {   // this half's part
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s = __builtin_fmaf((float)a.v[i][e], (float)b.v[i][e], s);
+        return s;
+    }
+    __device__ static void with_rows(f32x16& c, const uint16_t* tile, const Frag& f, int lane) {
+        const int l32 = lane & 31, hl = lane >> 5;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+            c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_b128(tile, swz<D>(l32, 2 * i + hl)), f.v[i], c, 0, 0, 0);
+    }
+    __device__ static Cols cols(const f32x16& p) {
+        Cols o;
+        float e[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) e[r] = p[r];
+        o.v[0] = pack8(e);
+        o.v[1] = pack8(e + 8);
+        return o;
+    }
+    __device__ static void with_cols(f32x16 (&c)[D / 32], const uint16_t* tile, const Cols& p, int lane) {
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int h2 = 0; h2 < 2; ++h2)
+                c[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_tr_tokens<D>(tile, lane, i, h2), p.v[h2], c[i], 0, 0, 0);
+    }
+    // values 4 j .. 4 j + 3 of a row
+    __device__ static void store4(uint16_t* p, const float* v) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    }
+};
+
+template <int D>
+struct Tile32<float, D> {
+    static constexpr int CHUNKS = D / 4;
+    struct Frag {
+        float4 v[D / 8];
+    };
+    struct Cols {
+        f32x16 v;
+    };
+    __device__ static int chunk_at(int row, int pos) { return pos ^ (row & 15); }
+    __device__ static int at(int row, int chunk) { return row * D + 4 * chunk_at(row, chunk); }
+    __device__ static void load(Frag& f, const float* p, bool ok, int hl) {
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i)
+            f.v[i] = ok ? *reinterpret_cast<const float4*>(p + 8 * i + 4 * hl) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    __device__ static float dot(const Frag& a, const Frag& b) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+            s = __builtin_fmaf(a.v[i].x, b.v[i].x, s);
+            s = __builtin_fmaf(a.v[i].y, b.v[i].y, s);
+            s = __builtin_fmaf(a.v[i].z, b.v[i].z, s);
+            s = __builtin_fmaf(a.v[i].w, b.v[i].w, s);
+        }
+        return s;
+    }
+    __device__ static void with_rows(f32x16& c, const float* tile, const Frag& f, int lane) {
+        const int l32 = lane & 31, hl = lane >> 5;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+            const float4 a = *reinterpret_cast<const float4*>(tile + at(l32, 2 * i + hl));
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, f.v[i].x, c, 0, 0, 0);
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, f.v[i].y, c, 0, 0, 0);
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, f.v[i].z, c, 0, 0, 0);
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, f.v[i].w, c, 0, 0, 0);
+        }
+    }
+    __device__ static Cols cols(const f32x16& p) { return Cols{p}; }
+    __device__ static void with_cols(f32x16 (&c)[D / 32], const float* tile, const Cols& p, int lane) {
+        const int l32 = lane & 31, hl = lane >> 5;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = srow(r, hl);
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i)
+                c[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(tile[at(row, 8 * i + (l32 >> 2)) + (l32 & 3)], p.v[r], c[i], 0, 0, 0);
+        }
+    }
+    __device__ static void store4(float* p, const float* v) {
+        *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    }
+};
+
+// A capped score (in units of log 2) and, for the backward, the cap's derivative:
+//   cap tanh(x / cap) = cap (1 - 2 / (1 + exp(2 x / cap))).
+// That form's error is of the order of cap 2^-24 whatever x is; single precision takes tanh itself,
+// as exact for small scores as for large ones.
+template <typename T>
+__device__ inline float capped(float s, float to_exp, float inv_cap, float cap2, float* slope) {
+    float t;
+    if constexpr (sizeof(T) == 4) t = tanhf(s * inv_cap);
+    else t = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + exp2_(s * to_exp)), 1.f);
+    if (slope) *slope = __builtin_fmaf(-t, t, 1.f);
+    return cap2 * t;
+}
+
+// Kernels over tiles of rows: the forward, and the queries' gradients
+struct RowsArgs {
+    View a;
+    Plan p;
+    void* out;               // forward: [N,h,d]; else dq, at dq_t, dq_h
+    float* lse;              // [N,h]; the backward's input
+    const void *o, *dout;    // backward: [N,h,d]
+    float* delta;            // backward: <dout, out> of every row, written
+    int64_t dq_t, dq_h;
+    float* parts;            // [2 grid][bq][d + 2]: results of pieces that are not whole tiles
+    int32_t grid;
+};
+struct RowsShape {
+    int32_t bq, unit, per_cu;   // rows of a tile, keys of a unit, workgroups a CU holds
+};
+RowsShape rows_shape(bool bf16, int32_t d, bool wide, bool bwd);
+hipError_t launch_rows_fwd(const RowsArgs& f, bool bf16, int32_t d, bool wide, hipStream_t stream);
+hipError_t launch_rows_dq(const RowsArgs& f, bool bf16, int32_t d, bool wide, hipStream_t stream);
+
+// The keys' side of the backward
+struct KeysArgs {
+    View a;
+    const void* dout;             // [N,h,d]
+    const float *lse, *delta;     // [N,h]
+    void *dK, *dV;
+    int64_t dk_t, dk_h, dv_t, dv_h;
+    int64_t tiles;                // key_tiles
+};
+int64_t key_tiles(int64_t B, int64_t T);
+hipError_t launch_keys(const KeysArgs& f, bool bf16, int32_t d, hipStream_t stream);
+
+hipError_t launch_plan(const View& a, const RowsShape& s, int64_t tiles, TileRec* recs, int64_t* prefix,
+                       hipStream_t stream);
+hipError_t launch_join(const RowsArgs& f, bool bf16, int32_t d, int32_t bq, bool bwd, hipStream_t stream);
+
+}  // namespace attn
+}  // namespace sa

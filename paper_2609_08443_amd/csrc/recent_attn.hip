@@ -1,0 +1,177 @@
+// Attention of targets over their users' recent histories: the plan of the kernels over tiles
+// of rows (recent_attn_rows.h) and the join of tiles that several workgroups share.
+//
+// Where a user's targets and tokens lie is on the device alone, so the plan is made there: every
+// tile's keys, and the units of keys before it.  The units of all tiles and key heads, one after
+// the other, are cut into equal pieces, one a workgroup: users with few and many tokens, targets
+// that see little or everything, cost what they have to read, and no workgroup more.  A tile cut
+// by a piece's border leaves partial results, added up in the pieces' order.
+#include "recent_attn.h"
+
+namespace sa {
+namespace attn {
+
+namespace {
+
+constexpr int kPlanThreads = 1024;
+
+// tile t's record and its units
+__device__ int32_t plan_tile(const View& a, int32_t bq, int32_t unit, int64_t t, TileRec* rec) {
+    int64_t tile0;
+    const int64_t b = user_of_tile(a.targets, a.B, a.N, a.g, bq, t, &tile0);
+    const User us = user_at(a, b);
+    const int64_t row0 = (t - tile0) * bq, rows = (int64_t)us.n * a.g;
+    rec->user = (int32_t)b;
+    rec->row0 = (int32_t)row0;
+    rec->klo = rec->khi = (int32_t)us.tok0;
+    if (row0 >= rows) return 0;
+    int32_t lo = us.L, hi = 0;
+    if (!a.ends) {
+        seen(a, us, 0, &lo, &hi);
+    } else {
+        const int64_t i1 = us.t0 + (min(row0 + bq, rows) - 1) / a.g;
+        for (int64_t i = us.t0 + row0 / a.g; i <= i1; ++i) {
+            int32_t l, h;
+            seen(a, us, i, &l, &h);
+            if (h > l) {
+                lo = min(lo, l);
+                hi = max(hi, h);
+            }
+        }
+    }
+    if (hi <= lo) return 1;
+    rec->klo += lo;
+    rec->khi += hi;
+    return (hi - lo + unit - 1) / unit;
+}
+
+// Inclusive sums over the workgroup's threads
+__device__ inline int64_t scan(int64_t v, int64_t* sums) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+        const int64_t o = __shfl_up(v, s, 64);
+        if (lane >= s) v += o;
+    }
+    if (lane == 63) sums[w] = v;
+    __syncthreads();
+    for (int i = 0; i < w; ++i) v += sums[i];
+    __syncthreads();
+    return v;
+}
+
+// Few tiles: records and sums by one workgroup, a thread a tile.  Else every tile's units by the
+// grid first (into prefix[t + 1]), then their sums.
+enum PlanStep { kAll, kTiles, kSums };
+template <PlanStep STEP>
+__global__ __launch_bounds__(STEP == kTiles ? 256 : kPlanThreads) void plan_kernel(View a, int32_t bq, int32_t unit,
+                                                                                    int64_t tiles, TileRec* recs,
+                                                                                    int64_t* prefix) {
+    if constexpr (STEP == kTiles) {
+        const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+        if (t < tiles) prefix[t + 1] = plan_tile(a, bq, unit, t, recs + t);
+    } else {
+        __shared__ int64_t sums[kPlanThreads / 64];
+        __shared__ int64_t carry;
+        if (threadIdx.x == 0) {
+            carry = 0;
+            prefix[0] = 0;
+        }
+        __syncthreads();
+        for (int64_t t0 = 0; t0 < tiles; t0 += kPlanThreads) {
+            const int64_t t = t0 + threadIdx.x;
+            int64_t v = 0;
+            if (t < tiles) v = STEP == kAll ? plan_tile(a, bq, unit, t, recs + t) : prefix[t + 1];
+            v = scan(v, sums) + carry;
+            if (t < tiles) prefix[t + 1] = v;
+            __syncthreads();
+            if (threadIdx.x == kPlanThreads - 1) carry = v;
+            __syncthreads();
+        }
+    }
+}
+
+// Workgroup w: the tile that piece w's border cuts, if none before cuts it too.
+template <typename T, int D, bool BWD>
+__global__ __launch_bounds__(256) void join_kernel(RowsArgs f, int32_t bq) {
+    const View& a = f.a;
+    int64_t X;
+    const int64_t P = pieces(f.p, a.hk, f.grid, &X), W = f.p.prefix[f.p.tiles], w = blockIdx.x + 1;
+    if (w >= P) return;
+    const int64_t at = w * X / P, kv = at / W, tile = tile_at(f.p, at - kv * W);
+    const int64_t t0 = kv * W + f.p.prefix[tile], t1 = kv * W + f.p.prefix[tile + 1];
+    if (at <= t0 || (w - 1) * X / P > t0) return;
+    int64_t last = w;   // the last piece with a part of it
+    while (last + 1 < P && (last + 1) * X / P < t1) ++last;
+    const TileRec rec = f.p.recs[tile];
+    const User us = user_at(a, rec.user);
+    const int32_t rows = min(bq, us.n * a.g - rec.row0);
+    const int64_t stride = (int64_t)bq * (D + 2);
+    // piece w - 1 began the tile; piece v's part of a tile that it goes on with is at 2 v
+    const float* first = f.parts + (2 * (w - 1) + 1) * stride;
+    for (int32_t x = threadIdx.x; x < rows * (D / 4); x += 256) {
+        const int32_t r = x / (D / 4), d = 4 * (x % (D / 4));
+        const int32_t row = rec.row0 + r;
+        const int64_t target = us.t0 + row / a.g;
+        const int32_t head = (int32_t)kv * a.g + row % a.g;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        float m = -__builtin_inff(), l = 0.f;
+        if constexpr (!BWD) {
+            m = first[bq * D + r];
+            for (int64_t p = w; p <= last; ++p) m = fmaxf(m, f.parts[2 * p * stride + bq * D + r]);
+        }
+        const float ms = m == -__builtin_inff() ? 0.f : m;
+        auto add = [&](const float* part) {
+            const float4 o = *reinterpret_cast<const float4*>(part + r * D + d);
+            float fac = 1.f;
+            if constexpr (!BWD) {
+                fac = exp2_(part[bq * D + r] - ms);
+                l = __builtin_fmaf(part[bq * D + bq + r], fac, l);
+            }
+            v[0] = __builtin_fmaf(o.x, fac, v[0]);
+            v[1] = __builtin_fmaf(o.y, fac, v[1]);
+            v[2] = __builtin_fmaf(o.z, fac, v[2]);
+            v[3] = __builtin_fmaf(o.w, fac, v[3]);
+        };
+        add(first);
+        for (int64_t p = w; p <= last; ++p) add(f.parts + 2 * p * stride);
+        const float inv = BWD ? a.scale : l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] *= inv;
+        T* o = BWD ? reinterpret_cast<T*>(f.out) + target * f.dq_t + head * f.dq_h
+                   : reinterpret_cast<T*>(f.out) + (target * a.h + head) * D;
+        Tile32<T, D>::store4(o + d, v);
+        if (!BWD && f.lse && d == 0) f.lse[target * a.h + head] = (m + __builtin_amdgcn_logf(l)) / kLog2e;
+    }
+}
+
+template <typename T, int D>
+hipError_t launch_join_t(const RowsArgs& f, int32_t bq, bool bwd, hipStream_t stream) {
+    const dim3 grid((unsigned)(f.grid - 1));
+    if (bwd) hipLaunchKernelGGL((join_kernel<T, D, true>), grid, dim3(256), 0, stream, f, bq);
+    else hipLaunchKernelGGL((join_kernel<T, D, false>), grid, dim3(256), 0, stream, f, bq);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_plan(const View& a, const RowsShape& s, int64_t tiles, TileRec* recs, int64_t* prefix,
+                       hipStream_t stream) {
+    if (tiles <= 4 * kPlanThreads) {
+        hipLaunchKernelGGL(plan_kernel<kAll>, dim3(1), dim3(kPlanThreads), 0, stream, a, s.bq, s.unit, tiles, recs, prefix);
+    } else {
+        hipLaunchKernelGGL(plan_kernel<kTiles>, dim3((unsigned)((tiles + 255) / 256)), dim3(256), 0, stream, a, s.bq,
+                           s.unit, tiles, recs, prefix);
+        hipLaunchKernelGGL(plan_kernel<kSums>, dim3(1), dim3(kPlanThreads), 0, stream, a, s.bq, s.unit, tiles, recs, prefix);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_join(const RowsArgs& f, bool bf16, int32_t d, int32_t bq, bool bwd, hipStream_t stream) {
+    if (f.grid < 2) return hipSuccess;
+    if (bf16) return d == 64 ? launch_join_t<uint16_t, 64>(f, bq, bwd, stream) : launch_join_t<uint16_t, 128>(f, bq, bwd, stream);
+    return d == 64 ? launch_join_t<float, 64>(f, bq, bwd, stream) : launch_join_t<float, 128>(f, bq, bwd, stream);
+}
+
+}  // namespace attn
+}  // namespace sa

@@ -1,0 +1,246 @@
+// The keys' and values' gradients of the attention over recent histories.
+//
+// A workgroup holds 128 keys of one user and key head, 32 a wave and one a lane of each half, and
+// takes all rows that may see them, 32 at a time through LDS: S = q K^T and dP = dout V^T leave a
+// key's scores in its own two lanes, from where p = exp(s - lse) goes into dV^T += dout^T p and
+// ds = p (dP - delta), times the cap's derivative, into dK^T += q^T ds.  Every sum is one
+// workgroup's, in the rows' order: nothing is added up in memory.
+#include "recent_attn.h"
+
+namespace sa {
+namespace attn {
+
+namespace {
+
+constexpr int kKeys = 128, kRows = 32;
+
+template <typename T, int D>
+struct KeysCfg {
+    static constexpr int EL = sizeof(T), TILE = kRows * D * EL;
+    static constexpr int STAGE = 2 * TILE;   // q and dout
+    static constexpr int LOADS = TILE / 1024 / 4;   // a wave's, of each
+    static constexpr int PER_CU = EL == 2 ? (D == 64 ? 3 : 2) : 1;
+};
+
+// a row's statistics in LDS
+struct RowStats {
+    float lse2[kRows], delta[kRows], slope2[kRows];
+    int32_t lo[kRows], hi[kRows];   // absolute; hi = lo: sees nothing
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, (KeysCfg<T, D>::PER_CU)) void keys_kernel(KeysArgs f) {
+    using C = KeysCfg<T, D>;
+    using M = Tile32<T, D>;
+    __shared__ __attribute__((aligned(16))) uint8_t smem[2 * C::STAGE];
+    __shared__ __attribute__((aligned(16))) RowStats stats[2];
+    const View& a = f.a;
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hl = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const float inv_cap = a.cap > 0.f ? a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e, to_exp = 2.f * kLog2e * inv_cap;
+    for (int64_t v = blockIdx.x; v < f.tiles * a.hk; v += gridDim.x) {
+        const int64_t id = xcd_range(v, f.tiles * a.hk), tile = id / a.hk;
+        const int32_t kv = (int32_t)(id % a.hk);
+        int64_t tile0;
+        const int64_t b = user_of_tile(a.offsets, a.B, a.T, 1, kKeys, tile, &tile0);
+        User us = user_at(a, b);
+        if (b == a.B) {   // tokens behind the last user's
+            us.n = 0;
+            us.L = (int32_t)(a.T - us.tok0);
+        }
+        const int64_t first = (tile - tile0) * kKeys;
+        if (first >= us.L) continue;
+        const int32_t nk = (int32_t)min((int64_t)kKeys, us.L - first);
+        const int64_t key0 = us.tok0 + first + 32 * w;   // the wave's first
+        const int32_t mine = nk - 32 * w;                // how many it has
+        const bool ok = l32 < mine;
+        typename M::Frag kf, vf;
+        M::load(kf, reinterpret_cast<const T*>(a.K) + (key0 + (ok ? l32 : 0)) * a.k_t + kv * a.k_h, ok, hl);
+        M::load(vf, reinterpret_cast<const T*>(a.V) + (key0 + (ok ? l32 : 0)) * a.v_t + kv * a.v_h, ok, hl);
+        f32x16 dk[D / 32], dv[D / 32];
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = f32x16{};
+
+        const int32_t rows = us.n * a.g, units = (rows + kRows - 1) / kRows;
+        const T* qp = reinterpret_cast<const T*>(a.q) + us.t0 * a.q_t + (int64_t)kv * a.g * a.q_h;
+        const T* dp = reinterpret_cast<const T*>(f.dout) + (us.t0 * a.h + (int64_t)kv * a.g) * D;
+        auto issue = [&](int32_t u, int stage) __attribute__((always_inline)) {
+            uint8_t* to = smem + stage * C::STAGE;
+            const int32_t r0 = u * kRows, t0 = r0 / a.g;
+            const char* qb = reinterpret_cast<const char*>(qp + (int64_t)t0 * a.q_t);
+            const char* db = reinterpret_cast<const char*>(dp + (int64_t)t0 * a.h * D);
+#pragma unroll
+            for (int i = 0; i < C::LOADS; ++i) {
+                const int q = w + 4 * i, pos = q * 64 + lane, r = pos / M::CHUNKS;
+                const uint32_t chunk = 16u * M::chunk_at(r, pos % M::CHUNKS);
+                const uint32_t row = (uint32_t)min(r0 + r, rows - 1);
+                uint32_t t = row, gi = 0;
+                if (a.g > 1) {
+                    t = row / (uint32_t)a.g;
+                    gi = row - t * (uint32_t)a.g;
+                }
+                t -= (uint32_t)t0;
+                dma16(qb, t * (uint32_t)(a.q_t * C::EL) + gi * (uint32_t)(a.q_h * C::EL) + chunk, to + q * 1024);
+                dma16(db, (t * (uint32_t)a.h + gi) * (uint32_t)(D * C::EL) + chunk, to + C::TILE + q * 1024);
+            }
+        };
+        // the statistics of unit u's rows, by the first 32 threads
+        struct Stat {
+            float lse2, delta, slope2;
+            int32_t lo, hi;
+        };
+        auto stat = [&](int32_t u) {
+            Stat s;
+            const int32_t row = u * kRows + l32;
+            const bool in = row < rows;
+            const int64_t target = us.t0 + (in ? row / a.g : 0);
+            const int32_t head = kv * a.g + (in ? row % a.g : 0);
+            seen(a, us, target, &s.lo, &s.hi);
+            if (!in) s.hi = s.lo;
+            s.lo += (int32_t)us.tok0;
+            s.hi += (int32_t)us.tok0;
+            const int64_t o = target * a.h + head;
+            const float lse = f.lse[o];
+            s.lse2 = s.hi > s.lo && lse != -__builtin_inff() ? lse * kLog2e : __builtin_inff();
+            s.delta = s.hi > s.lo ? f.delta[o] : 0.f;
+            s.slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.f;
+            return s;
+        };
+        auto put = [&](const Stat& s, int stage) {
+            RowStats& st = stats[stage];
+            st.lse2[l32] = s.lse2;
+            st.delta[l32] = s.delta;
+            st.slope2[l32] = s.slope2;
+            st.lo[l32] = s.lo;
+            st.hi[l32] = s.hi;
+        };
+        auto multiply = [&](int stage) __attribute__((always_inline)) {
+            T* qt = reinterpret_cast<T*>(smem + stage * C::STAGE);
+            T* dt = reinterpret_cast<T*>(smem + stage * C::STAGE + C::TILE);
+            const RowStats& st = stats[stage];
+            const int32_t lo = st.lo[l32], hi = st.hi[l32];
+            const uint32_t dead = (uint32_t)__builtin_amdgcn_ballot_w64(hi <= lo);
+            if (dead) {   // rows that see nothing: zeros, whatever they hold (the same in every wave)
+                for (int x = tid; x < kRows * M::CHUNKS; x += 256)
+                    if ((dead >> (x / M::CHUNKS)) & 1u) {
+                        reinterpret_cast<uint4*>(qt)[x] = make_uint4(0, 0, 0, 0);
+                        reinterpret_cast<uint4*>(dt)[x] = make_uint4(0, 0, 0, 0);
+                    }
+                lds_barrier();
+            }
+            if (mine <= 0) return;
+            const int32_t k0 = (int32_t)key0, kn = k0 + min(mine, 32);
+            const bool live = hi > lo;
+            if (!__builtin_amdgcn_ballot_w64(live && lo < kn && hi > k0)) return;
+            const bool whole = __builtin_amdgcn_ballot_w64(live && (lo > k0 || hi < kn)) == 0;
+            f32x16 s = f32x16{}, ds = f32x16{};
+            M::with_rows(s, qt, kf, lane);
+            M::with_rows(ds, dt, vf, lane);
+            float cc = a.scale * kLog2e;
+            float slope[16];
+            const bool cap = a.cap > 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 de = *reinterpret_cast<const float4*>(&st.delta[8 * j + 4 * hl]);
+                ds[4 * j] -= de.x;
+                ds[4 * j + 1] -= de.y;
+                ds[4 * j + 2] -= de.z;
+                ds[4 * j + 3] -= de.w;
+            }
+            if (cap) {
+                cc = 1.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[r] = capped<T>(s[r], to_exp, inv_cap, cap2, &slope[r]);
+                    ds[r] *= slope[r];
+                }
+            }
+            if (a.slopes) {
+                const int32_t key = k0 + l32;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int row = srow(r, hl);
+                    s[r] = __builtin_fmaf(s[r], cc, st.slope2[row] * (float)(key + 1 - st.hi[row]));
+                }
+                cc = 1.f;
+            }
+            if (!whole) {
+                const int32_t key = k0 + l32;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int row = srow(r, hl);
+                    const bool in = key >= st.lo[row] && key < st.hi[row];
+                    s[r] = in ? s[r] : -__builtin_inff();
+                    ds[r] = in ? ds[r] : 0.f;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 ls = *reinterpret_cast<const float4*>(&st.lse2[8 * j + 4 * hl]);
+                const float lv[4] = {ls.x, ls.y, ls.z, ls.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[4 * j + e] = exp2_(__builtin_fmaf(s[4 * j + e], cc, -lv[e]));
+                    ds[4 * j + e] *= s[4 * j + e];
+                }
+            }
+            M::with_cols(dv, dt, M::cols(s), lane);
+            M::with_cols(dk, qt, M::cols(ds), lane);
+        };
+
+        if (units > 0) {
+            lds_barrier();   // the last tile's rows are read
+            issue(0, 0);
+            if (tid < 32) put(stat(0), 0);
+            wait_loads<0>();
+            lds_barrier();
+            for (int32_t u = 0; u < units; ++u) {
+                Stat next;
+                if (u + 1 < units) {
+                    if (tid < 32) next = stat(u + 1);
+                    issue(u + 1, (u + 1) & 1);
+                }
+                multiply(u & 1);
+                if (u + 1 < units && tid < 32) put(next, (u + 1) & 1);
+                wait_loads<0>();
+                lds_barrier();
+            }
+        }
+        if (ok) {
+            T* ko = reinterpret_cast<T*>(f.dK) + (key0 + l32) * f.dk_t + kv * f.dk_h;
+            T* vo = reinterpret_cast<T*>(f.dV) + (key0 + l32) * f.dv_t + kv * f.dv_h;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float x[4], y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[e] = dk[i][4 * j + e] * a.scale;
+                        y[e] = dv[i][4 * j + e];
+                    }
+                    M::store4(ko + 32 * i + 8 * j + 4 * hl, x);
+                    M::store4(vo + 32 * i + 8 * j + 4 * hl, y);
+                }
+        }
+    }
+}
+
+template <typename T, int D>
+hipError_t launch_keys_t(const KeysArgs& f, hipStream_t stream) {
+    const int64_t most = int64_t(1) << 22, n = f.tiles * f.a.hk;
+    hipLaunchKernelGGL((keys_kernel<T, D>), dim3((unsigned)(n < most ? n : most)), dim3(256), 0, stream, f);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t key_tiles(int64_t B, int64_t T) { return T / kKeys + B + 1; }
+
+hipError_t launch_keys(const KeysArgs& f, bool bf16, int32_t d, hipStream_t stream) {
+    if (bf16) return d == 64 ? launch_keys_t<uint16_t, 64>(f, stream) : launch_keys_t<uint16_t, 128>(f, stream);
+    return d == 64 ? launch_keys_t<float, 64>(f, stream) : launch_keys_t<float, 128>(f, stream);
+}
+
+}  // namespace attn
+}  // namespace sa

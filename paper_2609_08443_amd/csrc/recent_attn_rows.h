@@ -1,0 +1,389 @@
+// The kernels over tiles of rows: the forward pass, and the queries' gradients (BWD).
+//
+// A wave holds 32 rows of one user and key head, one a lane of each half, and takes 32 keys at a
+// time: S^T = K q^T on the matrix cores leaves a row's scores in its own two lanes, so that its
+// softmax needs no exchange but one between the halves, and p goes into V^T p^T (or K^T ds^T)
+// from the registers it is in.  One pass over the keys with the running maximum and sum; the
+// maximum is followed only where it rose by more than 8 (in powers of two), so that the results
+// are rarely scaled anew, and p is at most 2^8.
+#pragma once
+
+#include "recent_attn.h"
+
+namespace sa {
+namespace attn {
+
+// WIDE: tiles of 128 rows, 32 a wave, all waves the same keys.  Else tiles of 32 rows (single
+// targets), each wave its own quarter of the keys; their results are joined at the end.
+template <typename T, int D, bool WIDE, bool BWD>
+struct RowsCfg {
+    static constexpr int EL = sizeof(T);
+    static constexpr int BQ = WIDE ? 128 : 32;
+    static constexpr int NT = WIDE && EL == 2 ? 2 : 1;   // tiles of 32 keys a wave takes at a time
+    static constexpr int UNIT = WIDE ? 32 * NT : 128;
+    static constexpr int TILE = 32 * D * EL;
+    static constexpr int STAGE = 2 * NT * TILE;          // keys and values
+    static constexpr int OWNERS = WIDE ? 1 : 4;
+    static constexpr int STAGES = OWNERS * STAGE <= 64 * 1024 ? 2 : 1;
+    static constexpr int JOIN = WIDE ? 0 : 4 * 32 * (D + 2) * 4;
+    static constexpr int RING = OWNERS * STAGES * STAGE;
+    static constexpr int LDS = RING > JOIN ? RING : JOIN;
+    static constexpr int LOADS = STAGE / (WIDE ? 4 : 1) / 1024;   // a wave's loads of a unit
+    static constexpr int BY_LDS = 160 * 1024 / LDS;
+    static constexpr int PER_CU = BY_LDS < (D == 64 && EL == 2 ? 3 : 2) ? BY_LDS : (D == 64 && EL == 2 ? 3 : 2);
+    static_assert(PER_CU >= 1 && LDS <= 160 * 1024, "LDS");
+};
+
+template <typename T, int D, bool WIDE, bool BWD>
+__global__ __launch_bounds__(256, (RowsCfg<T, D, WIDE, BWD>::PER_CU)) void rows_kernel(RowsArgs f) {
+    using C = RowsCfg<T, D, WIDE, BWD>;
+    using M = Tile32<T, D>;
+    using Frag = typename M::Frag;
+    constexpr int NT = C::NT;
+    __shared__ __attribute__((aligned(16))) uint8_t smem[C::LDS];
+    const View& a = f.a;
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hl = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int64_t X;
+    const int64_t P = pieces(f.p, a.hk, f.grid, &X);
+    if (blockIdx.x >= P) return;
+    const int64_t id = xcd_range(blockIdx.x, P), W = f.p.prefix[f.p.tiles];
+    int64_t at = id * X / P;
+    const int64_t end = (id + 1) * X / P;
+    int32_t kv = (int32_t)(at / W);
+    int64_t rem = at - kv * W;   // of the key head's units
+    int64_t tile = tile_at(f.p, rem);
+    const T* Kp = reinterpret_cast<const T*>(a.K);
+    const T* Vp = reinterpret_cast<const T*>(a.V);
+    uint8_t* const ring = smem + (WIDE ? 0 : w * C::STAGES * C::STAGE);
+    const float cap2 = a.cap * kLog2e, inv_cap = a.cap > 0.f ? a.scale / a.cap : 0.f, to_exp = 2.f * kLog2e * inv_cap;
+
+    while (at < end) {
+        const int64_t first = f.p.prefix[tile], cost = f.p.prefix[tile + 1] - first;
+        if (rem >= f.p.prefix[tile + 1]) {   // (a tile without rows has no units)
+            if (++tile == f.p.tiles) {
+                tile = 0;
+                rem = 0;
+                ++kv;
+            }
+            continue;
+        }
+        const int64_t k0 = rem - first, k1 = min(cost, k0 + (end - at));
+        const TileRec rec = f.p.recs[tile];
+        const User us = user_at(a, rec.user);
+        const int32_t nrows = us.n * a.g;
+        // the lane's row
+        const int32_t row = rec.row0 + (WIDE ? 32 * w : 0) + l32;
+        const bool ok = row < nrows;
+        const int64_t target = us.t0 + (ok ? row / a.g : 0);
+        const int32_t head = kv * a.g + (ok ? row % a.g : 0);
+        int32_t lo, hi;
+        seen(a, us, target, &lo, &hi);
+        lo += (int32_t)us.tok0;
+        hi += (int32_t)us.tok0;
+        if (!ok) hi = lo;
+        const bool live = hi > lo;
+        // of the wave's rows that see something: the keys that all see, that any sees
+        int32_t all_lo = live ? lo : 0, all_hi = live ? hi : 0x7fffffff;
+        int32_t any_lo = live ? lo : 0x7fffffff, any_hi = live ? hi : 0;
+#pragma unroll
+        for (int s = 1; s < 32; s *= 2) {
+            all_lo = max(all_lo, __shfl_xor(all_lo, s, 64));
+            all_hi = min(all_hi, __shfl_xor(all_hi, s, 64));
+            any_lo = min(any_lo, __shfl_xor(any_lo, s, 64));
+            any_hi = max(any_hi, __shfl_xor(any_hi, s, 64));
+        }
+        all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+        all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+        any_lo = __builtin_amdgcn_readfirstlane(any_lo);
+        any_hi = __builtin_amdgcn_readfirstlane(any_hi);
+        const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.f;
+
+        Frag qf, df;
+        M::load(qf, reinterpret_cast<const T*>(a.q) + target * a.q_t + head * a.q_h, live, hl);
+        float lse2 = 0.f, delta = 0.f;
+        if constexpr (BWD) {
+            const int64_t o = (target * a.h + head) * D;
+            M::load(df, reinterpret_cast<const T*>(f.dout) + o, live, hl);
+            Frag of;
+            M::load(of, reinterpret_cast<const T*>(f.o) + o, live, hl);
+            delta = swap_halves(M::dot(df, of), add_);
+            lse2 = live ? f.lse[target * a.h + head] * kLog2e : __builtin_inff();
+            if (lse2 == -__builtin_inff()) lse2 = __builtin_inff();
+            if (k0 == 0 && ok && hl == 0 && (WIDE || w == 0)) f.delta[target * a.h + head] = delta;
+        }
+
+        // keys [klo + UNIT u, ...) of unit u, rows past the last key repeating it
+        const int32_t klo = rec.klo, nkeys = rec.khi - rec.klo;
+        auto first_key = [&](int64_t u) { return (int32_t)(u * C::UNIT) + (WIDE ? 0 : 32 * w); };
+        auto issue = [&](int64_t u, int stage) __attribute__((always_inline)) {
+            const int32_t k = first_key(u), left = nkeys - 1 - k;
+            const char* kb = reinterpret_cast<const char*>(Kp + (int64_t)(klo + k) * a.k_t + kv * a.k_h);
+            const char* vb = reinterpret_cast<const char*>(Vp + (int64_t)(klo + k) * a.v_t + kv * a.v_h);
+            uint8_t* to = ring + stage * C::STAGE;
+            constexpr int Q = C::LOADS / 2;
+#pragma unroll
+            for (int i = 0; i < Q; ++i) {
+                const int q = WIDE ? w + 4 * i : i, pos = q * 64 + lane;
+                const int r = pos / M::CHUNKS, chunk = M::chunk_at(r & 31, pos % M::CHUNKS);
+                const uint32_t rr = (uint32_t)min(r, left);
+                dma16(kb, rr * (uint32_t)(a.k_t * C::EL) + 16u * chunk, to + q * 1024);
+                dma16(vb, rr * (uint32_t)(a.v_t * C::EL) + 16u * chunk, to + NT * C::TILE + q * 1024);
+            }
+        };
+
+        f32x16 acc[D / 32];
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
+        float m = -__builtin_inff(), l = 0.f;   // l: this half's part
+
+        auto multiply = [&](int64_t u, int stage) __attribute__((always_inline)) {
+            const T* kt = reinterpret_cast<const T*>(ring + stage * C::STAGE);
+            const T* vt = reinterpret_cast<const T*>(ring + stage * C::STAGE + NT * C::TILE);
+            const int32_t key0 = klo + first_key(u);   // (a tile's last keys may lie past khi: seen by none)
+            if (key0 >= any_hi || key0 + 32 * NT <= any_lo) return;
+            const bool whole = key0 >= all_lo && key0 + 32 * NT <= all_hi;
+            f32x16 s[NT], ds[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                s[t] = f32x16{};
+                M::with_rows(s[t], kt + t * 32 * D, qf, lane);
+                if constexpr (BWD) {
+                    ds[t] = f32x16{};
+                    M::with_rows(ds[t], vt + t * 32 * D, df, lane);
+                }
+            }
+            float cc = a.scale * kLog2e;
+            if (BWD) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) ds[t][r] -= delta;
+            }
+            if (a.cap > 0.f) {
+                cc = 1.f;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        float slope;
+                        s[t][r] = capped<T>(s[t][r], to_exp, inv_cap, cap2, BWD ? &slope : nullptr);
+                        if (BWD) ds[t][r] *= slope;
+                    }
+            }
+            if (a.slopes) {   // - slope (hi - 1 - key), from the unit's first key on
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const float b0 = slope2 * (float)(key0 + 32 * t + 4 * hl + 1 - hi);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        s[t][r] = __builtin_fmaf(s[t][r], cc, __builtin_fmaf(slope2, (float)(8 * (r >> 2) + (r & 3)), b0));
+                }
+                cc = 1.f;
+            }
+            if (!whole) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const uint32_t rel = (uint32_t)(key0 + 32 * t + 4 * hl - lo), len = (uint32_t)(hi - lo);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const bool in = rel + (uint32_t)(8 * (r >> 2) + (r & 3)) < len;
+                        s[t][r] = in ? s[t][r] : -__builtin_inff();
+                        if (BWD) ds[t][r] = in ? ds[t][r] : 0.f;
+                    }
+                }
+            }
+            if constexpr (BWD) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) ds[t][r] *= exp2_(__builtin_fmaf(s[t][r], cc, -lse2));
+                    M::with_cols(acc, kt + t * 32 * D, M::cols(ds[t]), lane);
+                }
+            } else {
+                float mx = s[0][0];
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
+                mx = swap_halves(mx, max_) * cc;
+                const bool rise = mx > m + 8.f;
+                if (__builtin_amdgcn_ballot_w64(rise)) {
+                    const float fac = rise ? exp2_(m - mx) : 1.f;
+                    m = rise ? mx : m;
+                    l *= fac;
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[i][r] *= fac;
+                }
+                const float ms = m == -__builtin_inff() ? 0.f : m;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        s[t][r] = exp2_(__builtin_fmaf(s[t][r], cc, -ms));
+                        l += s[t][r];
+                    }
+                    // (p in bf16 for bf16 inputs: as far off as the result's own rounding)
+                    M::with_cols(acc, vt + t * 32 * D, M::cols(s[t]), lane);
+                }
+            }
+        };
+
+        if constexpr (WIDE) {
+            if (nkeys > 0) {
+                issue(k0, 0);
+                wait_loads<0>();
+                barrier();
+                for (int64_t u = k0; u < k1; ++u) {
+                    const int st = (int)(u - k0) & 1;
+                    if (C::STAGES == 2 && u + 1 < k1) issue(u + 1, st ^ 1);
+                    multiply(u, C::STAGES == 2 ? st : 0);
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    if (C::STAGES == 1) {
+                        barrier();
+                        if (u + 1 < k1) issue(u + 1, 0);
+                    }
+                    wait_loads<0>();
+                    barrier();
+                }
+            }
+        } else {
+            if (k0 < k1 && first_key(k0) < nkeys) issue(k0, 0);
+            for (int64_t u = k0; u < k1; ++u) {
+                if (first_key(u) >= nkeys) break;
+                const int st = C::STAGES == 2 ? (int)(u - k0) & 1 : 0;
+                const bool more = u + 1 < k1 && first_key(u + 1) < nkeys;
+                if (C::STAGES == 2 && more) {
+                    issue(u + 1, st ^ 1);
+                    wait_loads<C::LOADS>();
+                } else {
+                    wait_loads<0>();
+                }
+                multiply(u, st);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before it is written again
+                if (C::STAGES == 1 && more) issue(u + 1, 0);
+            }
+        }
+
+        // results
+        const bool is_whole = k0 == 0 && k1 == cost;
+        float* part = f.parts + (2 * id + (k0 == 0 ? 1 : 0)) * C::BQ * (D + 2);
+        if constexpr (!BWD) l = swap_halves(l, add_);
+        if constexpr (WIDE) {
+            if (!live) {
+                m = -__builtin_inff();
+                l = 0.f;
+            }
+            if (ok && is_whole) {
+                const float inv = BWD ? (live ? a.scale : 0.f) : l > 0.f || l != l ? 1.f / l : 0.f;
+                T* o = BWD ? reinterpret_cast<T*>(f.out) + target * f.dq_t + head * f.dq_h
+                           : reinterpret_cast<T*>(f.out) + (target * a.h + head) * D;
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float v[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = live ? acc[i][4 * j + e] * inv : 0.f;
+                        M::store4(o + 32 * i + 8 * j + 4 * hl, v);
+                    }
+                if (!BWD && f.lse && hl == 0) f.lse[target * a.h + head] = (m + __builtin_amdgcn_logf(l)) / kLog2e;
+            } else if (ok) {
+                const int r32 = 32 * w + l32;
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        *reinterpret_cast<float4*>(part + r32 * D + 32 * i + 8 * j + 4 * hl) =
+                            live ? make_float4(acc[i][4 * j], acc[i][4 * j + 1], acc[i][4 * j + 2], acc[i][4 * j + 3])
+                                 : make_float4(0.f, 0.f, 0.f, 0.f);
+                if (!BWD && hl == 0) {
+                    part[C::BQ * D + r32] = m;
+                    part[C::BQ * D + C::BQ + r32] = l;
+                }
+            }
+        } else {
+            // the waves' results: [4][D][32] and their maxima and sums [4][32] in LDS
+            float* js = reinterpret_cast<float*>(smem);
+            float* jm = js + 4 * 32 * D;
+            if (!live) {
+                m = -__builtin_inff();
+                l = 0.f;
+            }
+            __syncthreads();
+            if (!BWD && hl == 0) {
+                jm[32 * w + l32] = m;
+                jm[128 + 32 * w + l32] = l;
+            }
+            __syncthreads();
+            float fac = 1.f;
+            if constexpr (!BWD) {
+                float top = m;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) top = fmaxf(top, jm[32 * v + l32]);
+                const float ts = top == -__builtin_inff() ? 0.f : top;
+                fac = exp2_(m - ts);
+                l = 0.f;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) l = __builtin_fmaf(jm[128 + 32 * v + l32], exp2_(jm[32 * v + l32] - ts), l);
+                m = top;
+            }
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) js[(w * D + 32 * i + srow(r, hl)) * 32 + l32] = live ? acc[i][r] * fac : 0.f;
+            __syncthreads();
+            constexpr int PER = D / 8;   // consecutive values a thread
+            const int d0 = (w * 2 + hl) * PER;
+            if (ok) {
+                float v[PER];
+#pragma unroll
+                for (int e = 0; e < PER; ++e) {
+                    const float* x = js + (d0 + e) * 32 + l32;
+                    v[e] = (x[0] + x[32 * D]) + (x[2 * 32 * D] + x[3 * 32 * D]);
+                }
+                if (is_whole) {
+                    const float inv = BWD ? a.scale : l > 0.f || l != l ? 1.f / l : 0.f;
+                    T* o = BWD ? reinterpret_cast<T*>(f.out) + target * f.dq_t + head * f.dq_h
+                               : reinterpret_cast<T*>(f.out) + (target * a.h + head) * D;
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) v[e] *= inv;
+#pragma unroll
+                    for (int e = 0; e < PER; e += 4) M::store4(o + d0 + e, v + e);
+                    if (!BWD && f.lse && tid < 32) f.lse[target * a.h + head] = (m + __builtin_amdgcn_logf(l)) / kLog2e;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < PER; e += 4)
+                        *reinterpret_cast<float4*>(part + l32 * D + d0 + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                    if (!BWD && tid < 32) {
+                        part[C::BQ * D + l32] = m;
+                        part[C::BQ * D + C::BQ + l32] = l;
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        at += k1 - k0;
+        rem += k1 - k0;
+    }
+}
+
+template <typename T, int D, bool WIDE, bool BWD>
+hipError_t launch_rows_t(const RowsArgs& f, hipStream_t stream) {
+    hipLaunchKernelGGL((rows_kernel<T, D, WIDE, BWD>), dim3((unsigned)f.grid), dim3(256), 0, stream, f);
+    return hipGetLastError();
+}
+template <bool BWD>
+hipError_t launch_rows(const RowsArgs& f, bool bf16, int32_t d, bool wide, hipStream_t stream) {
+    if (bf16) {
+        if (d == 64) return wide ? launch_rows_t<uint16_t, 64, true, BWD>(f, stream) : launch_rows_t<uint16_t, 64, false, BWD>(f, stream);
+        return wide ? launch_rows_t<uint16_t, 128, true, BWD>(f, stream) : launch_rows_t<uint16_t, 128, false, BWD>(f, stream);
+    }
+    if (d == 64) return wide ? launch_rows_t<float, 64, true, BWD>(f, stream) : launch_rows_t<float, 64, false, BWD>(f, stream);
+    return wide ? launch_rows_t<float, 128, true, BWD>(f, stream) : launch_rows_t<float, 128, false, BWD>(f, stream);
+}
+
+}  // namespace attn
+}  // namespace sa

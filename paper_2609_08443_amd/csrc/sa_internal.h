@@ -16,6 +16,10 @@ namespace sa {
 enum : int { IT_B = 0, IT_H = 1, IT_T0 = 2, IT_T1 = 3, IT_RANGE = 4, IT_SPLIT = 5,
              IT_PAIR_FIRST = 6, IT_WORDS = 8 };
 
+// An entry point's error, kept for sa_last_error (printf-like; returns st), and none
+sa_status api_fail(sa_status st, const char* fmt, ...);
+void api_clear();
+
 constexpr int kTileTokens = 32;     // tokens per MFMA tile (rows of the 32x32 output)
 constexpr int kWorklistThreads = 1024;
 constexpr int64_t kMergeWgs = 8192;   // most workgroups of a split-L merge while pairs share them

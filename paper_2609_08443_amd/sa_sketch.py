@@ -32,7 +32,9 @@ EXPORTS = ("sa_sketch_fwd_workspace_size", "sa_sketch_fwd", "sa_sketch_fwd_noall
            "sa_stca_bwd_workspace_size", "sa_stca_bwd",
            "sa_cache_slot_bytes", "sa_cache_write", "sa_cache_read",
            "sa_stca_cached_fwd_workspace_size", "sa_stca_cached_fwd",
-           "sa_stca_cached_bwd_workspace_size", "sa_stca_cached_bwd", "sa_gemm_tile_shapes", "sa_gemm_bf16",
+           "sa_stca_cached_bwd_workspace_size", "sa_stca_cached_bwd",
+           "sa_recent_attn_fwd_workspace_size", "sa_recent_attn_fwd",
+           "sa_recent_attn_bwd_workspace_size", "sa_recent_attn_bwd", "sa_gemm_tile_shapes", "sa_gemm_bf16",
            "sa_profile_enable", "sa_kernel_times", "sa_status_string", "sa_last_error")
 
 
@@ -41,6 +43,24 @@ class SAError(RuntimeError):
         self.status = status
         self.status_name = _STATUS.get(status, str(status))
         super().__init__(f"{self.status_name}: {detail}")
+
+
+class _RecentAttn(ctypes.Structure):
+    """sa_recent_attn"""
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "K", "V")]
+                + [(n, ctypes.c_int64) for n in ("q_stride", "q_head_stride", "k_stride", "k_head_stride", "v_stride",
+                                                 "v_head_stride")]
+                + [(n, ctypes.c_void_p) for n in ("offsets", "targets", "ends", "slopes")]
+                + [(n, ctypes.c_int64) for n in ("B", "T", "N")]
+                + [(n, ctypes.c_int32) for n in ("h", "hk", "d", "window")]
+                + [("scale", ctypes.c_float), ("cap", ctypes.c_float), ("dtype", ctypes.c_int)])
+
+
+class _RecentAttnGrads(ctypes.Structure):
+    """sa_recent_attn_grads"""
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("dq", "dK", "dV")]
+                + [(n, ctypes.c_int64) for n in ("dq_stride", "dq_head_stride", "dk_stride", "dk_head_stride", "dv_stride",
+                                                 "dv_head_stride")])
 
 
 _lib = None
@@ -126,6 +146,14 @@ def lib() -> ctypes.CDLL:
     L.sa_stca_cached_fwd.restype = c.c_int
     L.sa_stca_cached_bwd.argtypes = cached + [vp, vp, vp, vp, vp, c.c_int, vp, sz, vp]
     L.sa_stca_cached_bwd.restype = c.c_int
+    recent = c.POINTER(_RecentAttn)
+    for nm in ("sa_recent_attn_fwd_workspace_size", "sa_recent_attn_bwd_workspace_size"):
+        getattr(L, nm).argtypes = [recent]
+        getattr(L, nm).restype = sz
+    L.sa_recent_attn_fwd.argtypes = [recent, vp, vp, vp, sz, vp]
+    L.sa_recent_attn_fwd.restype = c.c_int
+    L.sa_recent_attn_bwd.argtypes = [recent, vp, vp, vp, c.POINTER(_RecentAttnGrads), vp, sz, vp]
+    L.sa_recent_attn_bwd.restype = c.c_int
     L.sa_build_worklist.argtypes = [vp, i64, i64, i32, i64, vp, i64, vp, vp]
     L.sa_build_worklist.restype = c.c_int
     L.sa_status_string.argtypes = [c.c_int]
@@ -786,6 +814,94 @@ def stca_cached_bwd(cache: SketchCache, slots, q, Wq, Wk, Wv, h: int, dout, scal
                                       _ptr(Wk), _ptr(Wv), B, R, k, D, h, float(scale), code, _ptr(dout),
                                       _ptr(g["dq"]), _ptr(g["dWq"]), _ptr(g["dWk"]), _ptr(g["dWv"]),
                                       _dtype_code(dout), _ptr(ws), nbytes, _handle(dev, stream))
+    _check(rc)
+    return g
+
+
+def _heads_view(t, name, shape, dtype, device):
+    """(elements from row to row, from head to head) of a [rows, heads, d] tensor whose heads
+    may lie in wider rows, as slices of one projection do."""
+    if t.shape != tuple(shape):
+        raise SAError(1, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype != dtype:
+        raise SAError(1, f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.device != device:
+        raise SAError(1, f"{name} is on {t.device}, expected {device}")
+    n, heads, d = shape
+    row, head, one = t.stride()
+    if one != 1 and d > 1:
+        raise SAError(1, f"{name}: the values of a head must lie together")
+    # (strides along dimensions of one say nothing)
+    return (row if n > 1 else 0), (head if heads > 1 else 0)
+
+
+def _recent_args(q, K, V, offsets, targets, ends, window, slopes, scale, cap):
+    """(device, the call's sa_recent_attn) of a batch."""
+    import torch
+    dev, dt = q.device, q.dtype
+    if dev.type != "cuda":
+        raise SAError(1, f"q is on {dev}, expected a GPU")
+    if q.dim() != 3 or K.dim() != 3:
+        raise SAError(1, f"q and K have shapes {tuple(q.shape)} and {tuple(K.shape)}, expected [N, h, d] and [T, hk, d]")
+    N, h, d = q.shape
+    T, hk = K.shape[:2]
+    code = _dtype_code(q)
+    strides = (*_heads_view(q, "q", (N, h, d), dt, dev), *_heads_view(K, "K", (T, hk, d), dt, dev),
+               *_heads_view(V, "V", (T, hk, d), dt, dev))
+    if offsets.dim() != 1 or offsets.shape[0] < 1:
+        raise SAError(1, f"offsets has shape {tuple(offsets.shape)}, expected [B + 1]")
+    B = offsets.shape[0] - 1
+    _require(offsets, "offsets", (B + 1,), torch.int64, dev)
+    _require(targets, "targets", (B + 1,), torch.int64, dev)
+    if ends is not None:
+        _require(ends, "ends", (N,), torch.int32, dev)
+    if slopes is not None:
+        _require(slopes, "slopes", (h,), torch.float32, dev)
+    if scale is None:
+        scale = 1.0 / math.sqrt(max(d, 1))
+    return dev, _RecentAttn(_ptr(q), _ptr(K), _ptr(V), *strides, _ptr(offsets), _ptr(targets), _ptr(ends), _ptr(slopes),
+                            B, T, N, h, hk, d, window, scale, cap, code)
+
+
+def recent_attn_fwd(q, K, V, offsets, targets, ends=None, window: int = 0, slopes=None, scale: Optional[float] = None,
+                    cap: float = 0.0, out=None, want_lse: bool = True, workspace=None, stream=None):
+    """sa_recent_attn_fwd on torch tensors: targets' queries q [N,h,d] over their users' recent
+    tokens K, V [T,hk,d] (views of wider rows are fine), packed by user as `targets` and
+    `offsets` [B+1] say; `ends` [N] int32 and `window` limit what a target sees, `slopes` [h]
+    prefer nearer tokens, `cap` bounds the scores.  Returns (out [N,h,d] in q's dtype, lse
+    [N,h] fp32 or None)."""
+    import torch
+    dev, a = _recent_args(q, K, V, offsets, targets, ends, window, slopes, scale, cap)
+    with _on(dev, stream):
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        _require(out, "out", q.shape, q.dtype, dev)
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=dev) if want_lse else None
+        ws, nbytes = _workspace(int(lib().sa_recent_attn_fwd_workspace_size(a)), dev, _on_device(workspace, dev))
+        rc = lib().sa_recent_attn_fwd(a, _ptr(out), _ptr(lse), _ptr(ws), nbytes, _handle(dev, stream))
+    _check(rc)
+    return out, lse
+
+
+def recent_attn_bwd(q, K, V, offsets, targets, out, lse, dout, ends=None, window: int = 0, slopes=None,
+                    scale: Optional[float] = None, cap: float = 0.0, dq=None, dK=None, dV=None, workspace=None,
+                    stream=None):
+    """sa_recent_attn_bwd on torch tensors: dict of the gradients dq, dK, dV in q's dtype, from
+    the forward's out and lse.  dq, dK and dV may be given, as views of wider rows too."""
+    import torch
+    dev, a = _recent_args(q, K, V, offsets, targets, ends, window, slopes, scale, cap)
+    _require(out, "out", q.shape, q.dtype, dev)
+    _require(dout, "dout", q.shape, q.dtype, dev)
+    _require(lse, "lse", q.shape[:2], torch.float32, dev)
+    with _on(dev, stream):
+        g, strides = {}, []
+        for name, t, like in (("dq", dq, q), ("dK", dK, K), ("dV", dV, V)):
+            g[name] = torch.empty(like.shape, dtype=q.dtype, device=dev) if t is None else t
+            strides += _heads_view(g[name], name, like.shape, q.dtype, dev)
+        ws, nbytes = _workspace(int(lib().sa_recent_attn_bwd_workspace_size(a)), dev, _on_device(workspace, dev))
+        rc = lib().sa_recent_attn_bwd(a, _ptr(out), _ptr(lse), _ptr(dout),
+                                      _RecentAttnGrads(_ptr(g["dq"]), _ptr(g["dK"]), _ptr(g["dV"]), *strides), _ptr(ws),
+                                      nbytes, _handle(dev, stream))
     _check(rc)
     return g
 
