@@ -615,6 +615,102 @@ sa_status sa_recent_attn_bwd(const sa_recent_attn* a, const void* out, const flo
                              const sa_recent_attn_grads* grads, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Layer norm of rows: the norms in front of a layer's products (the block's own are part of
+ * sa_block_fwd).
+ *
+ *   y = (x - mean) rstd gamma + beta,   rstd = 1 / sqrt(var + eps)
+ *
+ * with the mean and the (biased) variance of a row's D values.
+ *
+ *   x            [N,D] (dtype), x_stride elements from row to row (0: D), at any alignment that
+ *                the dtype has
+ *   gamma, beta  [D] (dtype);  eps finite and >= 0
+ *   y            output [N,D] (dtype), packed
+ *   stats        output [N,2] fp32: mean and rstd of each row, or NULL (the backward needs them)
+ *
+ * Sums and statistics in fp32, y rounded once.  N = 0 is a no-op; 1 <= D <= 2^24.  No
+ * workspace.  y may be x (with x_stride 0 or D).  Errors, ownership and streams as for
+ * sa_sketch_fwd, but that pointers need their dtype's alignment alone (stats: 8 bytes).
+ */
+sa_status sa_layer_norm_fwd(const void* x, int64_t x_stride, const void* gamma, const void* beta, int64_t N, int32_t D,
+                            float eps, sa_dtype dtype, void* y, float* stats, void* stream);
+
+/* Bytes of workspace that sa_layer_norm_bwd needs for this shape. */
+size_t sa_layer_norm_bwd_workspace_size(int64_t N, int32_t D, sa_dtype dtype);
+
+/*
+ * Backward of sa_layer_norm_fwd: with xh = (x - mean) rstd and g = dy gamma,
+ *
+ *   dx = rstd (g - mean(g) - xh mean(g xh)),   dgamma = sum over rows of dy xh,   dbeta = sum of dy
+ *
+ *   stats          what the forward wrote for the same x
+ *   dy             [N,D] (dtype), packed
+ *   dx             output [N,D] (dtype), packed; it may be dy
+ *   dgamma, dbeta  outputs [D] fp32
+ *
+ * All outputs are overwritten; N = 0 leaves zeros in dgamma and dbeta.
+ */
+sa_status sa_layer_norm_bwd(const void* x, int64_t x_stride, const void* gamma, const float* stats, const void* dy,
+                            int64_t N, int32_t D, sa_dtype dtype, void* dx, float* dgamma, float* dbeta, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Activations of a linear layer; gelu with erf. */
+typedef enum {
+    SA_ACT_NONE = 0,
+    SA_ACT_RELU = 1,
+    SA_ACT_GELU = 2,
+    SA_ACT_SILU = 3,
+    SA_ACT_SWIGLU = 4 /* W and bias have 2 F columns: y = silu(z[:, :F]) * z[:, F:] */
+} sa_activation;
+
+/* Bytes of workspace that sa_linear_fwd needs for this shape (0 is possible). */
+size_t sa_linear_fwd_workspace_size(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype);
+
+/*
+ * A linear layer with bias, activation and residual after its product: the projections, the
+ * feed-forward networks and the action-side fusion x + FFN([x; a]) around the attention
+ * (sections 2.3 and 3.4, Appendix D).
+ *
+ *   z = x W + bias,   y = act(z) + residual
+ *
+ *   x         [N,K] (dtype), x_stride elements from row to row (0: K)
+ *   W         [K,C] (dtype), row = input feature, C = F (swiglu: 2 F);  bias [C] (dtype) or NULL
+ *   residual  [N,F] (dtype), packed, or NULL
+ *   y         output [N,F] (dtype), packed; it may be residual
+ *   pre       output [N,C] (dtype), packed: z, for the backward, or NULL
+ *
+ * Sums in fp32, y and z rounded once each (y from the unrounded z).  N = 0 is a no-op; K, F >= 1.
+ * SA_ERR_UNSUPPORTED for N from 2^29 on, K or C above 2^20, K C from 2^31 on, and more than 2^35
+ * values in x, y or z.
+ * Errors, ownership and streams as for sa_sketch_fwd.
+ */
+sa_status sa_linear_fwd(const void* x, int64_t x_stride, const void* W, const void* bias, const void* residual, int64_t N,
+                        int32_t K, int32_t F, sa_activation act, sa_dtype dtype, void* y, void* pre, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that sa_linear_bwd needs for this shape (0 is possible). */
+size_t sa_linear_bwd_workspace_size(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype);
+
+/*
+ * Backward of sa_linear_fwd: with dz = dy act'(pre),
+ *
+ *   dx = dz W^T,   dW = x^T dz,   dbias = sum over rows of dz
+ *
+ * (the residual's gradient is dy itself).
+ *
+ *   pre              what the forward wrote; NULL for SA_ACT_NONE, which has no need of it
+ *   dy               [N,F] (dtype), packed
+ *   dx, dW, dbias    outputs [N,K], [K,C], [C], packed; dx in dtype, dW and dbias in weight_dtype:
+ *                    SA_FP32, or SA_BF16 with dtype SA_BF16.  NULL: not wanted
+ *
+ * bf16 mode rounds dz to bf16 before the products (dbias sums it unrounded).  All outputs are
+ * overwritten; N = 0 leaves zeros in dW and dbias.
+ */
+sa_status sa_linear_bwd(const void* x, int64_t x_stride, const void* W, const void* pre, const void* dy, int64_t N,
+                        int32_t K, int32_t F, sa_activation act, sa_dtype dtype, void* dx, void* dW, void* dbias,
+                        sa_dtype weight_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * The forward's ranges as a list of segments (the fused backward's work list),
  * exposed for exact testing.
  *

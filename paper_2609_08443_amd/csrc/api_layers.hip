@@ -1,9 +1,11 @@
-// Host side of the C ABI (include/sa_sketch.h): the attention over recent histories.
+// Host side of the C ABI (include/sa_sketch.h): the attention over recent histories, layer norm
+// and linear layers.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cmath>
 
+#include "linear.h"
 #include "recent_attn.h"
 #include "sa_internal.h"
 
@@ -132,9 +134,198 @@ hipError_t run_rows(const sa::attn::RowsArgs& f, const AttnPlan& p, const sa_rec
     return e;
 }
 
+// ---------------------------------------------------------------- layer norm, linear layers
+bool aligned_to(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+sa_status check_norm(int64_t N, int32_t D, sa_dtype dtype) {
+    if (dtype != SA_BF16 && dtype != SA_FP32) return api_fail(SA_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+    if (N < 0 || D < 1) return api_fail(SA_ERR_INVALID_ARG, "bad sizes N=%lld D=%d", (long long)N, D);
+    if (D > 1 << 24 || N >= int64_t(1) << 40) return api_fail(SA_ERR_UNSUPPORTED, "sizes beyond the supported range");
+    return SA_OK;
+}
+
+int32_t columns(int32_t F, sa_activation act) { return act == SA_ACT_SWIGLU ? 2 * F : F; }
+
+sa_status check_linear(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype) {
+    if (dtype != SA_BF16 && dtype != SA_FP32) return api_fail(SA_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+    if (act < SA_ACT_NONE || act > SA_ACT_SWIGLU) return api_fail(SA_ERR_INVALID_ARG, "unknown activation %d", (int)act);
+    if (N < 0 || K < 1 || F < 1) return api_fail(SA_ERR_INVALID_ARG, "bad sizes N=%lld K=%d F=%d", (long long)N, K, F);
+    // (launches have fewer than 2^32 threads, tiles at least 32 rows and columns)
+    const int64_t C = act == SA_ACT_SWIGLU ? 2 * (int64_t)F : F;
+    if (N >= int64_t(1) << 29 || K > 1 << 20 || C > 1 << 20 || C * K >= int64_t(1) << 31 || N * std::max<int64_t>(C, K) > int64_t(1) << 35)
+        return api_fail(SA_ERR_UNSUPPORTED, "sizes beyond the supported range");
+    return SA_OK;
+}
+
+size_t linear_fwd_workspace(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype) {
+    // z in fp32, where it does not fit into the result
+    return dtype == SA_FP32 && act != SA_ACT_SWIGLU ? 0 : 4 * (size_t)N * columns(F, act);
+}
+
+struct LinearBwdPlan {
+    size_t off_dz = 0, off_sums = 0, total = 0;
+};
+LinearBwdPlan plan_linear_bwd(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype) {
+    LinearBwdPlan p;
+    const size_t el = dtype == SA_BF16 ? 2 : 4, C = columns(F, act);
+    p.off_sums = act == SA_ACT_NONE ? 0 : align_up(el * (size_t)N * C, 256);
+    p.total = p.off_sums + 4 * (size_t)sa::linear::act_bwd_parts(N, F, dtype == SA_BF16) * C;
+    return p;
+}
+
 }  // namespace
 
 extern "C" {
+
+sa_status sa_layer_norm_fwd(const void* x, int64_t x_stride, const void* gamma, const void* beta, int64_t N, int32_t D,
+                            float eps, sa_dtype dtype, void* y, float* stats, void* stream_) {
+    sa::api_clear();
+    sa_status st = check_norm(N, D, dtype);
+    if (st != SA_OK) return st;
+    if (!(std::isfinite(eps) && eps >= 0.f)) return api_fail(SA_ERR_INVALID_ARG, "eps must be finite and >= 0");
+    if (x_stride == 0) x_stride = D;
+    if (x_stride < 0) return api_fail(SA_ERR_INVALID_ARG, "x_stride must be >= 0");
+    if (N == 0) return SA_OK;
+    if (!x || !gamma || !beta || !y) return api_fail(SA_ERR_INVALID_ARG, "null pointer argument");
+    const size_t el = dtype == SA_BF16 ? 2 : 4;
+    if (!aligned_to(x, el) || !aligned_to(gamma, el) || !aligned_to(beta, el) || !aligned_to(y, el) || !aligned_to(stats, 8))
+        return api_fail(SA_ERR_INVALID_ARG, "misaligned tensor argument");
+    sa::NormArgs a{};
+    a.x = x;
+    a.x_ld = x_stride;
+    a.gamma = gamma;
+    a.beta = beta;
+    a.N = N;
+    a.D = D;
+    a.eps = eps;
+    a.y = y;
+    a.stats = reinterpret_cast<float2*>(stats);
+    hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
+    sa::ProfScope ps("layer_norm_fwd", stream);
+    const hipError_t e = sa::launch_norm_fwd(a, dtype == SA_BF16, stream);
+    if (e != hipSuccess) return hip_fail(e, "layer norm launch");
+    return SA_OK;
+}
+
+size_t sa_layer_norm_bwd_workspace_size(int64_t N, int32_t D, sa_dtype dtype) {
+    if (check_norm(N, D, dtype) != SA_OK) return 0;
+    return 8 * (size_t)sa::norm_parts(N, D, dtype == SA_BF16) * D;
+}
+
+sa_status sa_layer_norm_bwd(const void* x, int64_t x_stride, const void* gamma, const float* stats, const void* dy,
+                            int64_t N, int32_t D, sa_dtype dtype, void* dx, float* dgamma, float* dbeta, void* workspace,
+                            size_t workspace_bytes, void* stream_) {
+    sa::api_clear();
+    sa_status st = check_norm(N, D, dtype);
+    if (st != SA_OK) return st;
+    if (x_stride == 0) x_stride = D;
+    if (x_stride < 0) return api_fail(SA_ERR_INVALID_ARG, "x_stride must be >= 0");
+    if (!gamma || !dgamma || !dbeta || (N > 0 && (!x || !stats || !dy || !dx)))
+        return api_fail(SA_ERR_INVALID_ARG, "null pointer argument");
+    const size_t el = dtype == SA_BF16 ? 2 : 4;
+    if (!aligned_to(x, el) || !aligned_to(gamma, el) || !aligned_to(dy, el) || !aligned_to(dx, el) || !aligned_to(stats, 8) ||
+        !aligned_to(dgamma, 4) || !aligned_to(dbeta, 4))
+        return api_fail(SA_ERR_INVALID_ARG, "misaligned tensor argument");
+    st = check_workspace(workspace, workspace_bytes, sa_layer_norm_bwd_workspace_size(N, D, dtype));
+    if (st != SA_OK) return st;
+    sa::NormArgs a{};
+    a.x = x;
+    a.x_ld = x_stride;
+    a.gamma = gamma;
+    a.dy = dy;
+    a.N = N;
+    a.D = D;
+    a.y = dx;
+    a.stats = reinterpret_cast<float2*>(const_cast<float*>(stats));
+    a.dgamma = dgamma;
+    a.dbeta = dbeta;
+    a.sums = reinterpret_cast<float*>(workspace);
+    hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
+    sa::ProfScope ps("layer_norm_bwd", stream);
+    const hipError_t e = sa::launch_norm_bwd(a, dtype == SA_BF16, stream);
+    if (e != hipSuccess) return hip_fail(e, "layer norm backward launch");
+    return SA_OK;
+}
+
+size_t sa_linear_fwd_workspace_size(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype) {
+    return check_linear(N, K, F, act, dtype) == SA_OK ? linear_fwd_workspace(N, K, F, act, dtype) : 0;
+}
+
+sa_status sa_linear_fwd(const void* x, int64_t x_stride, const void* W, const void* bias, const void* residual, int64_t N,
+                        int32_t K, int32_t F, sa_activation act, sa_dtype dtype, void* y, void* pre, void* workspace,
+                        size_t workspace_bytes, void* stream_) {
+    sa::api_clear();
+    sa_status st = check_linear(N, K, F, act, dtype);
+    if (st != SA_OK) return st;
+    if (x_stride == 0) x_stride = K;
+    if (x_stride < 0) return api_fail(SA_ERR_INVALID_ARG, "x_stride must be >= 0");
+    if (N == 0) return SA_OK;
+    if (!x || !W || !y) return api_fail(SA_ERR_INVALID_ARG, "null pointer argument");
+    if (!aligned16(x) || !aligned16(W) || !aligned16(bias) || !aligned16(residual) || !aligned16(y) || !aligned16(pre))
+        return api_fail(SA_ERR_INVALID_ARG, "tensor arguments must be 16-byte aligned");
+    const size_t need = linear_fwd_workspace(N, K, F, act, dtype);
+    if (need > 0) {
+        st = check_workspace(workspace, workspace_bytes, need);
+        if (st != SA_OK) return st;
+    }
+    hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
+    const bool bf = dtype == SA_BF16;
+    const int32_t C = columns(F, act);
+    float* z = reinterpret_cast<float*>(need > 0 ? workspace : y);
+    sa::ProfScope ps("linear_fwd", stream);
+    hipError_t e = sa::launch_gemm({x, bf, 0, x_stride, 1, W, bf, 0, C, 1, z, false, 0, C, (int32_t)N, C, K, 1, 1.f, false}, stream);
+    if (e == hipSuccess)
+        e = sa::linear::launch_epilogue(z, {bias, residual, (int)act, pre}, N, F, bf, y, stream);
+    if (e != hipSuccess) return hip_fail(e, "linear layer launch");
+    return SA_OK;
+}
+
+size_t sa_linear_bwd_workspace_size(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype) {
+    return check_linear(N, K, F, act, dtype) == SA_OK ? plan_linear_bwd(N, K, F, act, dtype).total : 0;
+}
+
+sa_status sa_linear_bwd(const void* x, int64_t x_stride, const void* W, const void* pre, const void* dy, int64_t N,
+                        int32_t K, int32_t F, sa_activation act, sa_dtype dtype, void* dx, void* dW, void* dbias,
+                        sa_dtype weight_dtype, void* workspace, size_t workspace_bytes, void* stream_) {
+    sa::api_clear();
+    sa_status st = check_linear(N, K, F, act, dtype);
+    if (st != SA_OK) return st;
+    if (weight_dtype != SA_FP32 && weight_dtype != SA_BF16)
+        return api_fail(SA_ERR_INVALID_ARG, "unknown weight dtype %d", (int)weight_dtype);
+    if (weight_dtype == SA_BF16 && dtype != SA_BF16)
+        return api_fail(SA_ERR_UNSUPPORTED, "SA_FP32 inputs have SA_FP32 gradients");
+    if (x_stride == 0) x_stride = K;
+    if (x_stride < 0) return api_fail(SA_ERR_INVALID_ARG, "x_stride must be >= 0");
+    if (N > 0 && (!dy || (dW && !x) || (dx && !W) || (act != SA_ACT_NONE && !pre)))
+        return api_fail(SA_ERR_INVALID_ARG, "null pointer argument");
+    if (!aligned16(x) || !aligned16(W) || !aligned16(pre) || !aligned16(dy) || !aligned16(dx) || !aligned16(dW) ||
+        !aligned16(dbias))
+        return api_fail(SA_ERR_INVALID_ARG, "tensor arguments must be 16-byte aligned");
+    const LinearBwdPlan p = plan_linear_bwd(N, K, F, act, dtype);
+    st = check_workspace(workspace, workspace_bytes, p.total);
+    if (st != SA_OK) return st;
+    uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
+    hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
+    const bool bf = dtype == SA_BF16, wb = weight_dtype == SA_BF16;
+    const int32_t C = columns(F, act);
+    hipError_t e = hipSuccess;
+    const void* dz = act == SA_ACT_NONE ? dy : ws + p.off_dz;
+    if (act != SA_ACT_NONE || dbias) {
+        sa::ProfScope ps("linear_act_bwd", stream);
+        e = sa::linear::launch_act_bwd({dy, pre, N, F, (int)act, ws + p.off_dz, dbias, wb, reinterpret_cast<float*>(ws + p.off_sums)},
+                                       bf, stream);
+    }
+    if (e == hipSuccess && dx) {
+        sa::ProfScope ps("linear_dx", stream);
+        e = sa::launch_gemm({dz, bf, 0, C, 1, W, bf, 0, 1, C, dx, bf, 0, K, (int32_t)N, K, C, 1, 1.f, false}, stream);
+    }
+    if (e == hipSuccess && dW) {
+        sa::ProfScope ps("linear_dw", stream);
+        e = sa::launch_gemm({x, bf, 0, 1, x_stride, dz, bf, 0, C, 1, dW, wb, 0, C, K, C, (int32_t)N, 1, 1.f, false}, stream);
+    }
+    if (e != hipSuccess) return hip_fail(e, "linear layer backward launch");
+    return SA_OK;
+}
 
 size_t sa_recent_attn_fwd_workspace_size(const sa_recent_attn* a) {
     return check_attn_sizes(a) == SA_OK ? plan_attn(*a, false).total : 0;

@@ -1,0 +1,74 @@
+// The linear layer's kernels around its products (linear.hip) and its activations.
+#pragma once
+
+#include "sa_internal.h"
+#include "tile_ops.h"
+
+namespace sa {
+namespace linear {
+
+// 1 / (1 + exp(-z)); EXACT: to the last bits, for single-precision results
+template <bool EXACT>
+__device__ inline float sigmoid(float z) {
+    if constexpr (EXACT) return 1.f / (1.f + expf(-z));
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-z * tile::kLog2e));
+}
+constexpr float kSqrtHalf = 0.70710678f, kInvSqrt2Pi = 0.39894228f;
+
+// act(z), or the gated silu(z) u
+template <bool EXACT>
+__device__ inline float activate(float z, float u, int act) {
+    switch (act) {
+        case SA_ACT_RELU: return z < 0.f ? 0.f : z;
+        case SA_ACT_GELU: return 0.5f * z * (1.f + erff(z * kSqrtHalf));
+        case SA_ACT_SILU: return z * sigmoid<EXACT>(z);
+        case SA_ACT_SWIGLU: return z * sigmoid<EXACT>(z) * u;
+        default: return z;
+    }
+}
+// dy act'(z); gated: dy u silu'(z), and dy silu(z) to du
+template <bool EXACT>
+__device__ inline float activate_bwd(float z, float u, float dy, int act, float* du) {
+    switch (act) {
+        case SA_ACT_RELU: return z > 0.f ? dy : 0.f;
+        case SA_ACT_GELU:
+            return dy * (0.5f * (1.f + erff(z * kSqrtHalf)) + z * kInvSqrt2Pi * (EXACT ? expf(-0.5f * z * z) : __builtin_amdgcn_exp2f(-0.5f * tile::kLog2e * z * z)));
+        case SA_ACT_SILU: {
+            const float s = sigmoid<EXACT>(z);
+            return dy * s * (1.f + z * (1.f - s));
+        }
+        case SA_ACT_SWIGLU: {
+            const float s = sigmoid<EXACT>(z);
+            *du = dy * z * s;
+            return dy * u * s * (1.f + z * (1.f - s));
+        }
+        default: return dy;
+    }
+}
+
+// what follows a product z = x W of F columns (2 F: swiglu)
+struct Epilogue {
+    const void *bias, *res;   // [columns of W], [N][F], or null
+    int act;
+    void* pre;                // [N][columns of W]: z + bias, or null
+};
+// y [N][F] of z fp32; y may be z (fp32, no swiglu)
+hipError_t launch_epilogue(const float* z, const Epilogue& e, int64_t N, int32_t F, bool bf16, void* y, hipStream_t stream);
+
+// dz = dy act'(pre) (not written for SA_ACT_NONE), and its column sums db, through sums
+// [act_bwd_parts][columns]
+struct ActBwd {
+    const void *dy, *pre;
+    int64_t N;
+    int32_t F;
+    int act;
+    void* dz;
+    void* db;   // or null
+    bool db_bf16;
+    float* sums;
+};
+int64_t act_bwd_parts(int64_t N, int32_t F, bool bf16);
+hipError_t launch_act_bwd(const ActBwd& a, bool bf16, hipStream_t stream);
+
+}  // namespace linear
+}  // namespace sa

@@ -1,0 +1,176 @@
+// Around the products of a linear layer, y = act(x W + b) + residual: what the product's own
+// epilogue does not take, and the gradient of the activation.
+//
+//   forward   z = x W (fp32) -> z + b (kept for the backward, if wanted), y
+//   backward  dz = dy act'(z) in the operands' type, db = sum over rows of dz
+//
+// swiglu: z has 2 F columns, y = silu(z1) z2, dz1 = dy z2 silu'(z1), dz2 = dy silu(z1), with
+// silu(z) = z s, silu'(z) = s (1 + z (1 - s)), s = 1 / (1 + exp(-z)).
+// Bound by memory: every value read and written once, 16 bytes at a time.  db's sums run down the
+// rows in registers, a workgroup's parts in LDS, and over the workgroups in a second launch, in
+// order.
+#include "linear.h"
+
+#include <algorithm>
+
+#include "vec_rows.h"
+
+namespace sa {
+namespace linear {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void epilogue_kernel(const float* z, const T* __restrict__ bias,
+                                                            const T* __restrict__ res, int64_t N, int F, int act,
+                                                            T* __restrict__ pre, T* y) {
+    constexpr int V = vec::Piece<T>::N;
+    const int64_t per = (F + V - 1) / V, n = N * per;
+    const int C = act == SA_ACT_SWIGLU ? 2 * F : F;
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) {
+        const int64_t row = i / per;
+        const int c = (int)(i % per) * V;
+        float a[V], b[V], t[V], o[V];
+        const float* zr = z + row * C;
+        auto part = [&](float* v, int first) __attribute__((always_inline)) {
+            vec::load<(V > 4 ? 8 : 4)>(zr + first, c, F, v);
+            if (bias) {
+                vec::load<V>(bias + first, c, F, t);
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] += t[e];
+            }
+            if (pre) vec::store<V>(pre + row * C + first, c, F, v);
+        };
+        part(a, 0);
+        if (act == SA_ACT_SWIGLU) part(b, F);
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = activate<sizeof(T) == 4>(a[e], act == SA_ACT_SWIGLU ? b[e] : 0.f, act);
+        if (res) {
+            vec::load<V>(res + row * F, c, F, t);
+#pragma unroll
+            for (int e = 0; e < V; ++e) o[e] += t[e];
+        }
+        vec::store<V>(y + row * F, c, F, o);
+    }
+}
+
+// dz of 64 rows' worth of columns a workgroup at a time: 32 threads side by side, 8 rows at once
+constexpr int kAcross = 32, kDown = kThreads / kAcross;
+template <typename T>
+__global__ __launch_bounds__(kThreads) void act_bwd_kernel(const T* __restrict__ dy, const T* __restrict__ pre, int64_t N,
+                                                           int F, int act, T* __restrict__ dz, float* __restrict__ sums) {
+    constexpr int V = vec::Piece<T>::N;
+    __shared__ float part[kDown][kAcross * V];
+    const int tx = threadIdx.x % kAcross, ty = threadIdx.x / kAcross, c = (blockIdx.x * kAcross + tx) * V;
+    const bool gated = act == SA_ACT_SWIGLU;
+    const int C = gated ? 2 * F : F;
+    float s1[V], s2[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) s1[e] = s2[e] = 0.f;
+    if (c < F)
+        for (int64_t row = (int64_t)blockIdx.y * kDown + ty; row < N; row += (int64_t)gridDim.y * kDown) {
+            float g[V], a[V], b[V], d2[V];
+            vec::load<V>(dy + row * F, c, F, g);
+            if (act != SA_ACT_NONE) {
+                vec::load<V>(pre + row * C, c, F, a);
+                if (gated) vec::load<V>(pre + row * C + F, c, F, b);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    d2[e] = 0.f;
+                    g[e] = activate_bwd<sizeof(T) == 4>(a[e], gated ? b[e] : 0.f, g[e], act, &d2[e]);
+                }
+                vec::store<V>(dz + row * C, c, F, g);
+                if (gated) vec::store<V>(dz + row * C + F, c, F, d2);
+            }
+            if (sums) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    s1[e] += g[e];
+                    if (gated) s2[e] += d2[e];
+                }
+            }
+        }
+    if (!sums) return;
+    for (int half = 0; half < (gated ? 2 : 1); ++half) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < V; ++e) part[ty][tx * V + e] = half ? s2[e] : s1[e];
+        __syncthreads();
+        for (int x = threadIdx.x; x < kAcross * V; x += kThreads) {
+            const int col = blockIdx.x * kAcross * V + x;
+            float s = 0.f;
+#pragma unroll
+            for (int r = 0; r < kDown; ++r) s += part[r][x];
+            if (col < F) sums[(int64_t)blockIdx.y * C + half * F + col] = s;
+        }
+    }
+}
+
+template <typename TO>
+__global__ __launch_bounds__(kThreads) void bias_sum_kernel(const float* __restrict__ sums, int n, int C, TO* __restrict__ db) {
+    __shared__ float acc[8][33];
+    const int c = blockIdx.x * 32 + threadIdx.x % 32, p = threadIdx.x / 32;
+    float s = 0.f;
+    if (c < C)
+        for (int i = p; i < n; i += 8) s += sums[(int64_t)i * C + c];
+    acc[p][threadIdx.x % 32] = s;
+    __syncthreads();
+    if (p == 0 && c < C) {
+        s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += acc[i][threadIdx.x];
+        vec::store(db + c, s);
+    }
+}
+
+template <typename T>
+hipError_t act_bwd(const ActBwd& a, hipStream_t stream) {
+    constexpr int V = vec::Piece<T>::N;
+    const int64_t parts = act_bwd_parts(a.N, a.F, sizeof(T) == 2);
+    const dim3 grid((unsigned)cdiv(a.F, kAcross * V), (unsigned)parts);
+    hipLaunchKernelGGL(act_bwd_kernel<T>, grid, dim3(kThreads), 0, stream, reinterpret_cast<const T*>(a.dy),
+                       reinterpret_cast<const T*>(a.pre), a.N, a.F, a.act, reinterpret_cast<T*>(a.dz), a.db ? a.sums : nullptr);
+    if (a.db) {
+        const int C = a.act == SA_ACT_SWIGLU ? 2 * a.F : a.F;
+        const dim3 g((unsigned)cdiv(C, 32));
+        if (a.db_bf16)
+            hipLaunchKernelGGL(bias_sum_kernel<uint16_t>, g, dim3(kThreads), 0, stream, a.sums, (int)parts, C,
+                               reinterpret_cast<uint16_t*>(a.db));
+        else
+            hipLaunchKernelGGL(bias_sum_kernel<float>, g, dim3(kThreads), 0, stream, a.sums, (int)parts, C,
+                               reinterpret_cast<float*>(a.db));
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t act_bwd_parts(int64_t N, int32_t F, bool bf16) {
+    const int64_t across = cdiv(F, kAcross * (bf16 ? 8 : 4));
+    return std::max<int64_t>(1, std::min<int64_t>(cdiv(N, kDown), cdiv(8 * (int64_t)device_cus(), across)));
+}
+
+hipError_t launch_act_bwd(const ActBwd& a, bool bf16, hipStream_t stream) {
+    return bf16 ? act_bwd<uint16_t>(a, stream) : act_bwd<float>(a, stream);
+}
+
+hipError_t launch_epilogue(const float* z, const Epilogue& e, int64_t N, int32_t F, bool bf16, void* y, hipStream_t stream) {
+    const int64_t n = N * cdiv(F, bf16 ? 8 : 4);
+    const dim3 grid((unsigned)std::min<int64_t>(cdiv(n, kThreads), 1 << 20));
+    if (bf16)
+        hipLaunchKernelGGL(epilogue_kernel<uint16_t>, grid, dim3(kThreads), 0, stream, z, reinterpret_cast<const uint16_t*>(e.bias),
+                           reinterpret_cast<const uint16_t*>(e.res), N, F, e.act, reinterpret_cast<uint16_t*>(e.pre),
+                           reinterpret_cast<uint16_t*>(y));
+    else
+        hipLaunchKernelGGL(epilogue_kernel<float>, grid, dim3(kThreads), 0, stream, z, reinterpret_cast<const float*>(e.bias),
+                           reinterpret_cast<const float*>(e.res), N, F, e.act, reinterpret_cast<float*>(e.pre),
+                           reinterpret_cast<float*>(y));
+    return hipGetLastError();
+}
+
+}  // namespace linear
+}  // namespace sa

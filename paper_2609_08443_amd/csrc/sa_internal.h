@@ -304,6 +304,21 @@ hipError_t launch_cached_softmax_bwd(const CacheView& c, const float* S, const f
                                      int64_t rows, int32_t Rh, float scale, bool bf16, void* ds, const CachedTargets& t,
                                      hipStream_t stream);
 
+// Layer norm of rows (layer_norm.hip): forward y, stats; backward y (= dx), dgamma, dbeta from dy
+// and stats, with `sums` [norm_parts][2][D].  x has x_ld values from row to row; y and dy are packed.
+struct NormArgs {
+    const void *x, *gamma, *beta, *dy;
+    int64_t x_ld, N;
+    int32_t D;
+    float eps;
+    void* y;
+    float2* stats;   // [N] mean, 1 / sqrt(var + eps); forward: or null
+    float *dgamma, *dbeta, *sums;
+};
+int64_t norm_parts(int64_t N, int32_t D, bool bf16);
+hipError_t launch_norm_fwd(const NormArgs& a, bool bf16, hipStream_t stream);
+hipError_t launch_norm_bwd(const NormArgs& a, bool bf16, hipStream_t stream);
+
 // Stacked-SA refinement (block.hip).  add_ln: one row of d features per
 // (user, head, prototype): out[r] = LN(x[r mod x_rows] + y[r]) * gamma[h] + beta[h],
 // h = (r / M) % H; x fp32 or bf16 (the shared prototypes broadcast over users

@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libsa_sketch.so")
 
 SA_BF16, SA_FP32 = 0, 1
 CACHE_FORMATS = {"fp8": 0, "fp4": 1}
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "swiglu": 4}
 _STATUS = {0: "SA_OK", 1: "SA_ERR_INVALID_ARG", 2: "SA_ERR_UNSUPPORTED", 3: "SA_ERR_WORKSPACE",
            4: "SA_ERR_BAD_OFFSETS", 5: "SA_ERR_HIP"}
 ITEM_WORDS = 8
@@ -34,7 +35,10 @@ EXPORTS = ("sa_sketch_fwd_workspace_size", "sa_sketch_fwd", "sa_sketch_fwd_noall
            "sa_stca_cached_fwd_workspace_size", "sa_stca_cached_fwd",
            "sa_stca_cached_bwd_workspace_size", "sa_stca_cached_bwd",
            "sa_recent_attn_fwd_workspace_size", "sa_recent_attn_fwd",
-           "sa_recent_attn_bwd_workspace_size", "sa_recent_attn_bwd", "sa_gemm_tile_shapes", "sa_gemm_bf16",
+           "sa_recent_attn_bwd_workspace_size", "sa_recent_attn_bwd",
+           "sa_layer_norm_fwd", "sa_layer_norm_bwd_workspace_size", "sa_layer_norm_bwd",
+           "sa_linear_fwd_workspace_size", "sa_linear_fwd", "sa_linear_bwd_workspace_size", "sa_linear_bwd",
+           "sa_gemm_tile_shapes", "sa_gemm_bf16",
            "sa_profile_enable", "sa_kernel_times", "sa_status_string", "sa_last_error")
 
 
@@ -154,6 +158,19 @@ def lib() -> ctypes.CDLL:
     L.sa_recent_attn_fwd.restype = c.c_int
     L.sa_recent_attn_bwd.argtypes = [recent, vp, vp, vp, c.POINTER(_RecentAttnGrads), vp, sz, vp]
     L.sa_recent_attn_bwd.restype = c.c_int
+    L.sa_layer_norm_fwd.argtypes = [vp, i64, vp, vp, i64, i32, f32, c.c_int, vp, vp, vp]
+    L.sa_layer_norm_fwd.restype = c.c_int
+    L.sa_layer_norm_bwd_workspace_size.argtypes = [i64, i32, c.c_int]
+    L.sa_layer_norm_bwd_workspace_size.restype = sz
+    L.sa_layer_norm_bwd.argtypes = [vp, i64, vp, vp, vp, i64, i32, c.c_int, vp, vp, vp, vp, sz, vp]
+    L.sa_layer_norm_bwd.restype = c.c_int
+    for nm in ("sa_linear_fwd_workspace_size", "sa_linear_bwd_workspace_size"):
+        getattr(L, nm).argtypes = [i64, i32, i32, c.c_int, c.c_int]
+        getattr(L, nm).restype = sz
+    L.sa_linear_fwd.argtypes = [vp, i64, vp, vp, vp, i64, i32, i32, c.c_int, c.c_int, vp, vp, vp, sz, vp]
+    L.sa_linear_fwd.restype = c.c_int
+    L.sa_linear_bwd.argtypes = [vp, i64, vp, vp, vp, i64, i32, i32, c.c_int, c.c_int, vp, vp, vp, c.c_int, vp, sz, vp]
+    L.sa_linear_bwd.restype = c.c_int
     L.sa_build_worklist.argtypes = [vp, i64, i64, i32, i64, vp, i64, vp, vp]
     L.sa_build_worklist.restype = c.c_int
     L.sa_status_string.argtypes = [c.c_int]
@@ -902,6 +919,128 @@ def recent_attn_bwd(q, K, V, offsets, targets, out, lse, dout, ends=None, window
         rc = lib().sa_recent_attn_bwd(a, _ptr(out), _ptr(lse), _ptr(dout),
                                       _RecentAttnGrads(_ptr(g["dq"]), _ptr(g["dK"]), _ptr(g["dV"]), *strides), _ptr(ws),
                                       nbytes, _handle(dev, stream))
+    _check(rc)
+    return g
+
+
+def _rows_view(t, name, width=None):
+    """(rows, width, elements from row to row) of a [rows, width] tensor whose rows may lie in
+    wider ones."""
+    if t.dim() != 2 or (width is not None and t.shape[1] != width):
+        raise SAError(1, f"{name} has shape {tuple(t.shape)}, expected [rows, {'width' if width is None else width}]")
+    if t.device.type != "cuda":
+        raise SAError(1, f"{name} is on {t.device}, expected a GPU")
+    n, D = t.shape
+    row, one = t.stride()
+    if one != 1 and D > 1:
+        raise SAError(1, f"{name}: the values of a row must lie together")
+    return n, D, (row if n > 1 else D)
+
+
+def layer_norm_fwd(x, gamma, beta, eps: float = 1e-5, y=None, want_stats: bool = True, stream=None):
+    """sa_layer_norm_fwd on torch tensors: rows x [N,D] (a view of wider rows is fine) with
+    weights gamma, beta [D].  Returns (y [N,D], stats [N,2] fp32: mean and 1 / sqrt(var + eps),
+    or None)."""
+    import torch
+    N, D, ld = _rows_view(x, "x")
+    dev, dt = x.device, x.dtype
+    code = _dtype_code(x)
+    _require(gamma, "gamma", (D,), dt, dev)
+    _require(beta, "beta", (D,), dt, dev)
+    with _on(dev, stream):
+        if y is None:
+            y = torch.empty((N, D), dtype=dt, device=dev)
+        _require(y, "y", (N, D), dt, dev)
+        stats = torch.empty((N, 2), dtype=torch.float32, device=dev) if want_stats else None
+        rc = lib().sa_layer_norm_fwd(_ptr(x), ld, _ptr(gamma), _ptr(beta), N, D, float(eps), code, _ptr(y), _ptr(stats),
+                                     _handle(dev, stream))
+    _check(rc)
+    return y, stats
+
+
+def layer_norm_bwd(x, gamma, stats, dy, dx=None, workspace=None, stream=None):
+    """sa_layer_norm_bwd on torch tensors: dict of dx [N,D] in x's dtype and dgamma, dbeta [D]
+    fp32, from the forward's stats."""
+    import torch
+    N, D, ld = _rows_view(x, "x")
+    dev, dt = x.device, x.dtype
+    code = _dtype_code(x)
+    _require(gamma, "gamma", (D,), dt, dev)
+    _require(stats, "stats", (N, 2), torch.float32, dev)
+    _require(dy, "dy", (N, D), dt, dev)
+    with _on(dev, stream):
+        g = {"dx": torch.empty((N, D), dtype=dt, device=dev) if dx is None else dx,
+             "dgamma": torch.empty(D, dtype=torch.float32, device=dev),
+             "dbeta": torch.empty(D, dtype=torch.float32, device=dev)}
+        _require(g["dx"], "dx", (N, D), dt, dev)
+        ws, nbytes = _workspace(int(lib().sa_layer_norm_bwd_workspace_size(N, D, code)), dev, _on_device(workspace, dev))
+        rc = lib().sa_layer_norm_bwd(_ptr(x), ld, _ptr(gamma), _ptr(stats), _ptr(dy), N, D, code, _ptr(g["dx"]),
+                                     _ptr(g["dgamma"]), _ptr(g["dbeta"]), _ptr(ws), nbytes, _handle(dev, stream))
+    _check(rc)
+    return g
+
+
+def _activation(act) -> int:
+    if act not in ACTIVATIONS:
+        raise SAError(1, f"activation {act!r}, expected one of {tuple(ACTIVATIONS)}")
+    return ACTIVATIONS[act]
+
+
+def _linear_args(x, W, act):
+    """(N, K, F, x's row stride, W's columns, activation, dtype code, device) of a linear layer."""
+    N, K, ld = _rows_view(x, "x")
+    code = _activation(act)
+    if W.dim() != 2 or (act == "swiglu" and W.shape[1] % 2):
+        raise SAError(1, f"W has shape {tuple(W.shape)}, expected [{K}, {'2 F' if act == 'swiglu' else 'F'}]")
+    C = W.shape[1]
+    _require(W, "W", (K, C), x.dtype, x.device)
+    return N, K, C // 2 if act == "swiglu" else C, ld, C, code, _dtype_code(x), x.device
+
+
+def linear_fwd(x, W, bias=None, act: str = "none", residual=None, y=None, want_pre: bool = False, workspace=None,
+               stream=None):
+    """sa_linear_fwd on torch tensors: y = act(x W + bias) + residual, x [N,K] (a view of wider
+    rows is fine), W [K,F], or [K,2F] for act "swiglu" (the gated half first).  Returns (y [N,F],
+    pre [N, W's columns], what the backward needs of an activation, or None)."""
+    import torch
+    N, K, F, ld, C, acode, code, dev = _linear_args(x, W, act)
+    dt = x.dtype
+    if bias is not None:
+        _require(bias, "bias", (C,), dt, dev)
+    if residual is not None:
+        _require(residual, "residual", (N, F), dt, dev)
+    with _on(dev, stream):
+        if y is None:
+            y = torch.empty((N, F), dtype=dt, device=dev)
+        _require(y, "y", (N, F), dt, dev)
+        pre = torch.empty((N, C), dtype=dt, device=dev) if want_pre else None
+        ws, nbytes = _workspace(int(lib().sa_linear_fwd_workspace_size(N, K, F, acode, code)), dev, _on_device(workspace, dev))
+        rc = lib().sa_linear_fwd(_ptr(x), ld, _ptr(W), _ptr(bias), _ptr(residual), N, K, F, acode, code, _ptr(y), _ptr(pre),
+                                 _ptr(ws), nbytes, _handle(dev, stream))
+    _check(rc)
+    return y, pre
+
+
+def linear_bwd(x, W, dy, bias: bool = False, act: str = "none", pre=None, weight_dtype=None, workspace=None, stream=None):
+    """sa_linear_bwd on torch tensors: dict of the gradients dx [N,K] in x's dtype, dW and, with
+    bias, db in weight_dtype (x's by default), from the forward's `pre` (act "none" needs none).
+    The residual's gradient is dy."""
+    import torch
+    N, K, F, ld, C, acode, code, dev = _linear_args(x, W, act)
+    dt = x.dtype
+    _require(dy, "dy", (N, F), dt, dev)
+    if act != "none":
+        if pre is None:
+            raise SAError(1, f"activation {act!r} needs the forward's pre")
+        _require(pre, "pre", (N, C), dt, dev)
+    with _on(dev, stream):
+        wdt = dict(dtype=dt if weight_dtype is None else weight_dtype, device=dev)
+        g = {"dx": torch.empty((N, K), dtype=dt, device=dev), "dW": torch.empty((K, C), **wdt)}
+        if bias:
+            g["db"] = torch.empty(C, **wdt)
+        ws, nbytes = _workspace(int(lib().sa_linear_bwd_workspace_size(N, K, F, acode, code)), dev, _on_device(workspace, dev))
+        rc = lib().sa_linear_bwd(_ptr(x), ld, _ptr(W), _ptr(pre), _ptr(dy), N, K, F, acode, code, _ptr(g["dx"]), _ptr(g["dW"]),
+                                 _ptr(g.get("db")), _dtype_code(g["dW"]), _ptr(ws), nbytes, _handle(dev, stream))
     _check(rc)
     return g
 

@@ -1,0 +1,160 @@
+"""GPU tests of layer norm and linear layers (sa_layer_norm_*, sa_linear_*) against the fp64
+oracle, element by element within the bounds that oracle/layers.py derives."""
+import numpy as np
+import pytest
+
+from oracle import layers as ol
+from oracle.recent import HALF
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def sa():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2609_08443_amd import sa_sketch
+    sa_sketch.lib()
+    return sa_sketch
+
+
+def values(dtype, shape, seed, sd=1.0, mean=0.0):
+    g = np.random.default_rng([8443, seed, *shape])
+    return torch.from_numpy((g.standard_normal(shape) * sd + mean).astype(np.float32)).to(DT[dtype])
+
+
+def f8(t):
+    return t.double().numpy()
+
+
+def within(got, ref, off, what):
+    got = got.detach().double().cpu().numpy()
+    assert got.shape == ref.shape, what
+    assert np.all(np.isfinite(got)), f"{what}: not finite"
+    worst = np.max(np.abs(got - ref) / np.maximum(off, 1e-30), initial=0.0)
+    assert worst <= 1.0, f"{what}: {worst:.3g} of the bound"
+
+
+NORM = [(1, 1), (1, 64), (3, 63), (130, 64), (65, 100), (33, 128), (17, 129), (40, 256), (9, 500), (50, 512), (70, 1024),
+        (5, 1023), (300, 1024), (7, 2048), (3, 2050), (5, 4096), (6, 5001), (4, 8192), (3, 9001), (2, 20000)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("N,D", NORM)
+def test_norm(sa, N, D, dtype):
+    print(f"norm {N}x{D} {dtype}", flush=True)
+    x = values(dtype, (N, D), 1, 1.5, 0.7)
+    gamma, beta, dy = values(dtype, (D,), 2, 0.1, 1.0), values(dtype, (D,), 3, 0.1), values(dtype, (N, D), 4)
+    y, stats = sa.layer_norm_fwd(x.cuda(), gamma.cuda(), beta.cuda(), eps=1e-5)
+    ry, rs, ey, es = ol.norm_fwd(f8(x), f8(gamma), f8(beta), 1e-5, dtype)
+    assert y.dtype == DT[dtype] and stats.dtype == torch.float32
+    within(y, ry, ey, "y")
+    within(stats, rs, es, "stats")
+    given = torch.from_numpy(rs.astype(np.float32))
+    got = sa.layer_norm_bwd(x.cuda(), gamma.cuda(), given.cuda(), dy.cuda())
+    ref, off = ol.norm_bwd(f8(x), f8(gamma), f8(given), f8(dy), dtype)
+    assert got["dx"].dtype == DT[dtype] and got["dgamma"].dtype == got["dbeta"].dtype == torch.float32
+    for k in ref:
+        within(got[k], ref[k], off[k], k)
+
+
+def test_norm_of_rows_far_from_zero(sa):
+    """The squares are summed around the mean."""
+    x = values("fp32", (40, 1000), 5, 1e-2, 1000.0)
+    one, zero = torch.ones(1000), torch.zeros(1000)
+    y, stats = sa.layer_norm_fwd(x.cuda(), one.cuda(), zero.cuda(), eps=0.0)
+    ry, rs, ey, es = ol.norm_fwd(f8(x), f8(one), f8(zero), 0.0, "fp32")
+    within(y, ry, ey, "y")
+    within(stats, rs, es, "stats")
+
+
+def test_norm_of_equal_values(sa):
+    x = torch.full((3, 777), 2.5, dtype=torch.bfloat16)
+    gamma, beta = values("bf16", (777,), 6), values("bf16", (777,), 7)
+    y, stats = sa.layer_norm_fwd(x.cuda(), gamma.cuda(), beta.cuda(), eps=1e-5)
+    assert torch.equal(y.cpu(), beta.expand(3, -1))
+    np.testing.assert_allclose(stats.cpu().numpy()[:, 1], 1e-5 ** -0.5, rtol=1e-6)
+
+
+@pytest.mark.parametrize("D", [64, 100, 1024])
+def test_norm_of_strided_rows_in_place(sa, D):
+    """Rows inside wider ones, y and dx in their inputs' place, a row with a NaN beside the others."""
+    wide = values("bf16", (37, D + 24), 8).cuda()
+    x = wide[:, 8:8 + D]
+    gamma, beta = values("bf16", (D,), 9).cuda(), values("bf16", (D,), 10).cuda()
+    y, stats = sa.layer_norm_fwd(x, gamma, beta)
+    y2, _ = sa.layer_norm_fwd(x.contiguous(), gamma, beta)
+    assert torch.equal(y, y2)
+    z = x.contiguous()
+    sa.layer_norm_fwd(z, gamma, beta, y=z)
+    assert torch.equal(y, z)
+    dy = values("bf16", (37, D), 11).cuda()
+    ref = sa.layer_norm_bwd(x, gamma, stats, dy)
+    d2 = dy.clone()
+    got = sa.layer_norm_bwd(x, gamma, stats, d2, dx=d2)
+    for k in ref:
+        assert torch.equal(got[k], ref[k]), k
+    z = x.contiguous()
+    z[5, 3] = float("nan")
+    y3, _ = sa.layer_norm_fwd(z, gamma, beta)
+    assert torch.isnan(y3[5]).all() and torch.equal(torch.cat([y3[:5], y3[6:]]), torch.cat([y[:5], y[6:]]))
+
+
+def test_norm_without_rows(sa):
+    for D in (64, 20000):
+        x, w = torch.empty(0, D, dtype=torch.bfloat16, device="cuda"), torch.ones(D, dtype=torch.bfloat16, device="cuda")
+        y, stats = sa.layer_norm_fwd(x, w, w)
+        assert y.shape == (0, D) and stats.shape == (0, 2)
+        g = sa.layer_norm_bwd(x, w, stats, y)
+        assert not g["dgamma"].any() and not g["dbeta"].any()
+
+
+LINEAR = [(1, 1, 1), (1, 64, 64), (1, 1024, 1024), (2, 256, 512), (5, 200, 331), (64, 64, 64), (100, 128, 96), (130, 72, 40),
+          (257, 320, 264), (300, 512, 1024), (1000, 63, 65), (77, 1030, 128), (16, 192, 8), (3, 4096, 24)]
+ACTS = ["none", "relu", "gelu", "silu", "swiglu"]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("N,K,F", LINEAR)
+def test_linear_forward(sa, N, K, F, act, dtype):
+    print(f"linear {N}x{K}x{F} {act} {dtype}", flush=True)
+    C = 2 * F if act == "swiglu" else F
+    x, W, b = values(dtype, (N, K), 1), values(dtype, (K, C), 2, K ** -0.5), values(dtype, (C,), 3)
+    res = values(dtype, (N, F), 4)
+    for bias, residual, want in ((b, res, True), (None, None, False), (None, res, True), (b, None, False)):
+        y, pre = sa.linear_fwd(x.cuda(), W.cuda(), bias=None if bias is None else bias.cuda(), act=act,
+                               residual=None if residual is None else residual.cuda(), want_pre=want)
+        ry, rz, ey, ez = ol.linear_fwd(f8(x), f8(W), None if bias is None else f8(bias), act,
+                                       None if residual is None else f8(residual), dtype)
+        assert y.dtype == DT[dtype]
+        within(y, ry, ey, "y")
+        if want:
+            assert pre.dtype == DT[dtype]
+            within(pre, rz, ez, "pre")
+        else:
+            assert pre is None
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("N,K,F", LINEAR)
+def test_linear_backward(sa, N, K, F, act, dtype):
+    print(f"linear_bwd {N}x{K}x{F} {act} {dtype}", flush=True)
+    C = 2 * F if act == "swiglu" else F
+    x, W, pre, dy = values(dtype, (N, K), 1), values(dtype, (K, C), 2, K ** -0.5), values(dtype, (N, C), 3, 2.0), values(dtype, (N, F), 4)
+    ref, off = ol.linear_bwd(f8(x), f8(W), f8(pre), f8(dy), act, dtype)
+    for wdt in ([None] if dtype == "fp32" else [None, torch.float32]):
+        got = sa.linear_bwd(x.cuda(), W.cuda(), dy.cuda(), bias=True, act=act, pre=None if act == "none" else pre.cuda(),
+                            weight_dtype=wdt)
+        assert set(got) == {"dx", "dW", "db"}
+        for k in got:
+            want = DT[dtype] if k == "dx" or wdt is None else wdt
+            assert got[k].dtype == want
+            half = HALF["bf16"] if want == torch.bfloat16 else HALF["fp32"]
+            within(got[k], ref[k], off[k] + half * np.abs(ref[k]), k)
+    got = sa.linear_bwd(x.cuda(), W.cuda(), dy.cuda(), act=act, pre=None if act == "none" else pre.cuda())
+    assert set(got) == {"dx", "dW"}
