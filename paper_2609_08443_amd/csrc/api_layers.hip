@@ -4,8 +4,10 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 
 #include "linear.h"
+#include "linear_gemm.h"
 #include "recent_attn.h"
 #include "sa_internal.h"
 
@@ -19,6 +21,9 @@ sa_status hip_fail(hipError_t e, const char* what) { return api_fail(SA_ERR_HIP,
 
 // ---------------------------------------------------------------- attention over recent histories
 struct AttnPlan {
+    bool fused = false, rest = true;   // backward: users with few rows in one kernel; others there may be
+    int32_t chunk = 256;
+    size_t off_dq = 0;
     bool wide = false;
     sa::attn::RowsShape shape;
     int64_t tiles = 0;
@@ -43,6 +48,20 @@ AttnPlan plan_attn(const sa_recent_attn& a, bool bwd) {
         off = align_up(off + bytes, 256);
         return o;
     };
+    if (bwd) {
+        // users with few rows on average: one pass over the keys for those with no more than it takes
+        const int32_t few = sa::attn::fused_rows(bf, a.d);
+        p.fused = few > 0 && rows <= few * a.B;
+        p.rest = !p.fused || rows > few;
+        if (p.fused) {
+            p.chunk = sa::attn::fused_chunk(a.B, a.T, a.hk);
+            p.off_dq = carve(sizeof(float) * (size_t)sa::attn::fused_slots(a.T, p.chunk) * a.hk * few * a.d);
+        }
+        if (!p.rest) {
+            p.total = off;
+            return p;
+        }
+    }
     p.off_recs = carve(sizeof(sa::attn::TileRec) * (size_t)p.tiles);
     p.off_prefix = carve(sizeof(int64_t) * ((size_t)p.tiles + 1));
     p.off_parts = carve(sizeof(float) * 2 * (size_t)p.grid * p.shape.bq * (a.d + 2));
@@ -157,19 +176,44 @@ sa_status check_linear(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dt
     return SA_OK;
 }
 
+int g_shape() { const char* e = getenv("SA_SHAPE"); return e ? atoi(e) : 0; }
+// the bf16 products of a layer; pointers of its operands where they are known, any aligned ones else
+const void* const kAny = reinterpret_cast<const void*>(256);
+sa::linear::Product fwd_product(const void* x, int64_t x_ld, const void* W, int64_t N, int32_t K, int32_t C,
+                                const sa::linear::Epilogue* epi, void* y) {
+    return {x, W, x_ld, 1, C, 1, (int32_t)N, C, K, 0, C, y, true, epi};
+}
+sa::linear::Product dx_product(const void* dz, const void* W, int64_t N, int32_t K, int32_t C, void* dx) {
+    return {dz, W, C, 1, 1, C, (int32_t)N, K, C, 0, 0, dx, true, nullptr};
+}
+sa::linear::Product dw_product(const void* x, int64_t x_ld, const void* dz, int64_t N, int32_t K, int32_t C, void* dW, bool bf) {
+    return {x, dz, 1, x_ld, C, 1, K, C, (int32_t)N, K, C, dW, bf, nullptr};
+}
+
+// z in fp32, where the product has no epilogue and z does not fit into the result
 size_t linear_fwd_workspace(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype) {
-    // z in fp32, where it does not fit into the result
     return dtype == SA_FP32 && act != SA_ACT_SWIGLU ? 0 : 4 * (size_t)N * columns(F, act);
 }
 
 struct LinearBwdPlan {
-    size_t off_dz = 0, off_sums = 0, total = 0;
+    int32_t splits = 1, per = 0x7fffffff;   // dW's sum over the rows
+    size_t off_dz = 0, off_sums = 0, off_parts = 0, total = 0;
 };
 LinearBwdPlan plan_linear_bwd(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype) {
     LinearBwdPlan p;
     const size_t el = dtype == SA_BF16 ? 2 : 4, C = columns(F, act);
     p.off_sums = act == SA_ACT_NONE ? 0 : align_up(el * (size_t)N * C, 256);
-    p.total = p.off_sums + 4 * (size_t)sa::linear::act_bwd_parts(N, F, dtype == SA_BF16) * C;
+    p.off_parts = align_up(p.off_sums + 4 * (size_t)sa::linear::act_bwd_parts(N, F, dtype == SA_BF16) * C, 256);
+    p.total = p.off_parts;
+    if (dtype == SA_BF16) {
+        const int64_t slabs = (N + 63) / 64, tiles = (int64_t)((K + 255) / 256) * ((C + 255) / 256);
+        const int64_t most = std::min<int64_t>(sa::device_cus() / tiles, slabs / 8);
+        if (most > 1) {
+            p.per = (int32_t)((slabs + most - 1) / most);
+            p.splits = (int32_t)((slabs + p.per - 1) / p.per);
+            p.total += 4 * (size_t)p.splits * K * C;
+        }
+    }
     return p;
 }
 
@@ -273,7 +317,15 @@ sa_status sa_linear_fwd(const void* x, int64_t x_stride, const void* W, const vo
     const int32_t C = columns(F, act);
     float* z = reinterpret_cast<float*>(need > 0 ? workspace : y);
     sa::ProfScope ps("linear_fwd", stream);
-    hipError_t e = sa::launch_gemm({x, bf, 0, x_stride, 1, W, bf, 0, C, 1, z, false, 0, C, (int32_t)N, C, K, 1, 1.f, false}, stream);
+    const sa::linear::Epilogue epi{bias, residual, (int)act, pre};
+    const sa::linear::Product prod = fwd_product(x, x_stride, W, N, K, C, &epi, y);
+    hipError_t e;
+    if (bf && sa::linear::product_supported(prod)) {
+        e = sa::linear::launch_product(prod, stream, g_shape());
+        if (e != hipSuccess) return hip_fail(e, "linear layer launch");
+        return SA_OK;
+    }
+    e = sa::launch_gemm({x, bf, 0, x_stride, 1, W, bf, 0, C, 1, z, false, 0, C, (int32_t)N, C, K, 1, 1.f, false}, stream);
     if (e == hipSuccess)
         e = sa::linear::launch_epilogue(z, {bias, residual, (int)act, pre}, N, F, bf, y, stream);
     if (e != hipSuccess) return hip_fail(e, "linear layer launch");
@@ -317,11 +369,24 @@ sa_status sa_linear_bwd(const void* x, int64_t x_stride, const void* W, const vo
     }
     if (e == hipSuccess && dx) {
         sa::ProfScope ps("linear_dx", stream);
-        e = sa::launch_gemm({dz, bf, 0, C, 1, W, bf, 0, 1, C, dx, bf, 0, K, (int32_t)N, K, C, 1, 1.f, false}, stream);
+        const sa::linear::Product prod = dx_product(dz, W, N, K, C, dx);
+        if (bf && sa::linear::product_supported(prod)) e = sa::linear::launch_product(prod, stream, g_shape());
+        else e = sa::launch_gemm({dz, bf, 0, C, 1, W, bf, 0, 1, C, dx, bf, 0, K, (int32_t)N, K, C, 1, 1.f, false}, stream);
     }
     if (e == hipSuccess && dW) {
         sa::ProfScope ps("linear_dw", stream);
-        e = sa::launch_gemm({x, bf, 0, 1, x_stride, dz, bf, 0, C, 1, dW, wb, 0, C, K, C, (int32_t)N, 1, 1.f, false}, stream);
+        sa::linear::Product prod = dw_product(x, x_stride, dz, N, K, C, dW, wb);
+        if (p.splits > 1) {
+            prod.y = ws + p.off_parts;
+            prod.y_bf16 = false;
+            prod.splits = p.splits;
+            prod.per = p.per;
+        }
+        if (bf && sa::linear::product_supported(prod)) {
+            e = sa::linear::launch_product(prod, stream, g_shape());
+            if (e == hipSuccess && p.splits > 1)
+                e = sa::linear::launch_sum_splits(reinterpret_cast<const float*>(ws + p.off_parts), p.splits, (int64_t)K * C, dW, wb, stream);
+        } else e = sa::launch_gemm({x, bf, 0, 1, x_stride, dz, bf, 0, C, 1, dW, wb, 0, C, K, C, (int32_t)N, 1, 1.f, false}, stream);
     }
     if (e != hipSuccess) return hip_fail(e, "linear layer backward launch");
     return SA_OK;
@@ -386,7 +451,15 @@ sa_status sa_recent_attn_bwd(const sa_recent_attn* a, const void* out, const flo
     hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
     float* delta = reinterpret_cast<float*>(ws + p.off_delta);
     hipError_t e = hipSuccess;
-    if (a->N > 0) {
+    if (p.fused) {
+        sa::ProfScope ps("recent_attn_bwd", stream);
+        sa::attn::FusedArgs f{v, out, dout, lse, gr.dq, gr.dK, gr.dV, gr.dq_stride, gr.dq_head_stride, gr.dk_stride,
+                              gr.dk_head_stride, gr.dv_stride, gr.dv_head_stride,
+                              sa::attn::fused_items(a->B, a->T, p.chunk), p.chunk, reinterpret_cast<float*>(ws + p.off_dq)};
+        e = sa::attn::launch_fused(f, bf, a->d, stream);
+        v.skip = sa::attn::fused_rows(bf, a->d);
+    }
+    if (e == hipSuccess && p.rest && a->N > 0) {
         sa::attn::RowsArgs f = rows_args(v, p, ws);
         f.out = gr.dq;
         f.dq_t = gr.dq_stride;
@@ -397,7 +470,7 @@ sa_status sa_recent_attn_bwd(const sa_recent_attn* a, const void* out, const flo
         f.delta = delta;
         e = run_rows(f, p, *a, true, ws, stream);
     }
-    if (e == hipSuccess && a->T > 0) {
+    if (e == hipSuccess && p.rest && a->T > 0) {
         sa::ProfScope ps("recent_attn_keys", stream);
         sa::attn::KeysArgs f{v, dout, lse, delta, gr.dK, gr.dV, gr.dk_stride, gr.dk_head_stride, gr.dv_stride,
                              gr.dv_head_stride, sa::attn::key_tiles(a->B, a->T)};

@@ -22,6 +22,7 @@
 // share that L2.  Products whose shapes or strides do not fit (k not a multiple of
 // 64, unaligned strides, fp32 operands without that permission) run on the
 // fp32 product of layer.hip.
+#include "gemm_tiles.h"
 #include "sa_internal.h"
 #include "tile_ops.h"
 
@@ -31,7 +32,7 @@ namespace {
 
 using namespace tile;
 
-constexpr int GBM = 128, GBN = 128, GBK = 64;
+constexpr int GBM = 128, GBN = 128;
 
 struct MgArgs {
     const void* A;
@@ -310,28 +311,6 @@ struct LtCfg {
     static_assert(LOADS < 64, "vmcnt range");
 };
 
-// Direct global -> LDS copy of 16 bytes per lane (global_load_lds_dwordx4) from
-// base + off (base wave-uniform) to LDS bytes [lds + 16 lane, + 16), written as
-// inline assembly: the compiler cannot tell which LDS bytes such a load writes,
-// so for the builtin it makes the transposing LDS reads wait for every load in
-// flight, the next slabs' included.  Completion is awaited by the explicit
-// vmcnt waits of lt_barrier (and the vmcnt(0) before the epilogue).
-// M0 (which holds the load's LDS address) is a reserved register, so the block
-// saves and restores it instead of declaring it clobbered.
-__device__ __forceinline__ void lt_dma16(const char* base, uint32_t off, const uint8_t* lds) {
-    const uint32_t l = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)lds;
-    uint32_t saved;
-    asm volatile(
-        "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %3\n\t"
-        "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %1, %2\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(saved)
-        : "v"(off), "s"(base), "s"(l)
-        : "memory");
-}
-
 template <int N>
 __device__ __forceinline__ void lt_barrier() {
     static_assert(N >= 0 && N < 64, "vmcnt range");
@@ -370,20 +349,9 @@ struct LtOperand<R, true> {
     __device__ __forceinline__ void issue(int kt, int k1, uint8_t* lds, int w) {
         const char* p = (!PAIR || kt < k1 ? base : base2) + kt * step;
 #pragma unroll
-        for (int i = 0; i < Q; ++i) lt_dma16(p, off[i], lds + (w + 4 * i) * 1024);
+        for (int i = 0; i < Q; ++i) dma16(p, off[i], lds + (w + 4 * i) * 1024);
     }
 };
-
-// 16-byte chunk swizzle of an m- (n-) contiguous slab ([64 k][R] bf16, LPR = R / 8
-// chunks per row): the eight k rows one transposing read touches (64 bytes of rows
-// k0 + 0..3 and k0 + 8..11) fall in four different 64-byte windows of the 256
-// bytes of banks instead of one.  Rows of 256 bytes or more start on the same
-// bank, so row k moves by (k mod 4) windows; 128-byte rows alternate between the
-// two halves, so row k moves by one window when bit 1 of k is set.  Measured: 8%
-// less time on a product with both operands transposed, 2% on one.
-__device__ __forceinline__ int tr_swizzle(int k, int lpr) {
-    return lpr >= 16 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
-}
 
 // m- (n-) contiguous operand: the slab is kept as it lies in memory, [64 k][R] (rows
 // of R bf16), its 16-byte chunks permuted within each row by tr_swizzle.  Lane l of
@@ -416,34 +384,9 @@ struct LtOperand<R, false> {
     __device__ __forceinline__ void issue(int kt, int k1, uint8_t* lds, int w) {
         const char* p = (!PAIR || kt < k1 ? base : base2) + kt * step;
 #pragma unroll
-        for (int i = 0; i < Q; ++i) lt_dma16(p, off[i], lds + (w + 4 * i) * 1024);
+        for (int i = 0; i < Q; ++i) dma16(p, off[i], lds + (w + 4 * i) * 1024);
     }
 };
-
-// fragment (32 rows or columns from `first`, k step ks) of an operand slab in LDS:
-// k-contiguous: ds_read_b128 of the swizzled rows; otherwise two transposing
-// reads: inside each 16-lane group, lane i receives element i % 4 of the 8-byte
-// pieces addressed by lanes 4 e + i / 4 (e < 4), so lane 4 e + j addresses k row
-// e (then e + 4) and columns 4 j .. 4 j + 3 of its group's 16 columns.
-template <int R, bool KC>
-__device__ __forceinline__ bf16x8 lt_frag(const uint8_t* lds, int first, int ks, int lane) {
-    const int l32 = lane & 31, hl = lane >> 5;
-    if constexpr (KC) {
-        return lds_b128(reinterpret_cast<const uint16_t*>(lds), swz<64>(first + l32, 2 * ks + hl));
-    } else {
-        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-        const int s = lane & 15, g = (lane >> 4) & 1;
-        const int k = 16 * ks + 8 * hl + (s >> 2), col = first + 16 * g + 4 * (s & 3);
-        typedef __attribute__((address_space(3))) short lds_short;
-        constexpr int LPR = R / 8;
-        lds_short* base = (lds_short*)(const_cast<uint8_t*>(lds));
-        lds_short* p = base + k * R + 8 * ((col >> 3) ^ tr_swizzle(k, LPR)) + (col & 7);
-        lds_short* q = base + (k + 4) * R + 8 * ((col >> 3) ^ tr_swizzle(k + 4, LPR)) + (col & 7);
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)q);
-        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    }
-}
 
 // PAIR: a second pair of operands follows the first, and k may be split (MgArgs)
 template <int FM, int FN, int PM, int PN, bool A_KC, bool B_KC, bool C_BF16, int NS, bool PAIR = false>

@@ -127,6 +127,22 @@ __global__ __launch_bounds__(kThreads) void bias_sum_kernel(const float* __restr
     }
 }
 
+// n values (a multiple of 4), each the sum of its parts [splits][n] in order
+template <typename TO>
+__global__ __launch_bounds__(kThreads) void sum_splits_kernel(const float* __restrict__ parts, int splits, int64_t n,
+                                                              TO* __restrict__ to) {
+    for (int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * kThreads * 4) {
+        float4 v = *reinterpret_cast<const float4*>(parts + i);
+        for (int p = 1; p < splits; ++p) {
+            const float4 x = *reinterpret_cast<const float4*>(parts + p * n + i);
+            v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+        }
+        if constexpr (sizeof(TO) == 2)
+            *reinterpret_cast<uint2*>(to + i) = make_uint2(tile::pack_bf16x2(v.x, v.y), tile::pack_bf16x2(v.z, v.w));
+        else *reinterpret_cast<float4*>(to + i) = v;
+    }
+}
+
 template <typename T>
 hipError_t act_bwd(const ActBwd& a, hipStream_t stream) {
     constexpr int V = vec::Piece<T>::N;
@@ -156,6 +172,15 @@ int64_t act_bwd_parts(int64_t N, int32_t F, bool bf16) {
 
 hipError_t launch_act_bwd(const ActBwd& a, bool bf16, hipStream_t stream) {
     return bf16 ? act_bwd<uint16_t>(a, stream) : act_bwd<float>(a, stream);
+}
+
+hipError_t launch_sum_splits(const float* parts, int32_t splits, int64_t n, void* to, bool bf16, hipStream_t stream) {
+    const dim3 grid((unsigned)std::min<int64_t>(cdiv(n, 4 * kThreads), 1 << 20));
+    if (bf16)
+        hipLaunchKernelGGL(sum_splits_kernel<uint16_t>, grid, dim3(kThreads), 0, stream, parts, splits, n, reinterpret_cast<uint16_t*>(to));
+    else
+        hipLaunchKernelGGL(sum_splits_kernel<float>, grid, dim3(kThreads), 0, stream, parts, splits, n, reinterpret_cast<float*>(to));
+    return hipGetLastError();
 }
 
 hipError_t launch_epilogue(const float* z, const Epilogue& e, int64_t N, int32_t F, bool bf16, void* y, hipStream_t stream) {

@@ -1,0 +1,521 @@
+// Products of a linear layer on the matrix cores, bf16 with fp32 sums:
+//
+//   y = act(x W + b) + residual   (A = x, B = W, epilogue on the results where they are)
+//   dx = dz W^T   (B k-contiguous),   dW = x^T dz   (A and B contiguous along their rows, any K)
+//
+// A wave takes (32 FM) x (32 FN) outputs as FM x FN v_mfma_f32_32x32x16_bf16 of W's columns by x's rows: a
+// lane then holds four consecutive columns of a row, where the epilogue is done; the results go through a
+// wave's own part of LDS and out in whole rows.  k goes by in slabs of 64, STAGES of both operands in LDS,
+// loaded straight into it STAGES - 1 slabs ahead; the first slabs of a workgroup's next tile are on their
+// way while the results of the last one are written.
+#include "linear_gemm.h"
+
+#include <algorithm>
+
+#include "gemm_tiles.h"
+
+namespace sa {
+namespace linear {
+
+namespace {
+
+using namespace tile;
+
+__device__ __attribute__((aligned(16))) const uint32_t kZeros[4] = {0, 0, 0, 0};
+
+struct Args {
+    const uint16_t *A, *B;
+    int64_t a_m, a_k, b_k, b_n;
+    int32_t M, N, K, F;     // F: columns of y, N those of pre
+    int32_t ma, nb;         // rows of A, columns of B to load, where they are contiguous along them
+    int32_t tm, tn, splits, per;
+    void* y;
+    const uint16_t *bias, *res;
+    uint16_t* pre;
+    int32_t act;
+};
+
+// what becomes of the results
+enum Out { kF32, kBf16, kGated, kEpi };   // kEpi + activation: one instance each, without branches at every value
+
+// Loads of an operand's slabs, R rows.  k-contiguous: load q of a slab fills LDS rows 8 q .. 8 q + 7, lane l
+// row 8 q + l / 8 and the chunk whose swizzled position is l % 8.
+template <int R, int WAVES, bool KC, bool GATED>
+struct Operand;
+template <int R, int WAVES, bool GATED>
+struct Operand<R, WAVES, true, GATED> {
+    static constexpr int Q = R / 8 / WAVES;
+    const char* base;
+    uint32_t off[Q];
+    int64_t step;
+    int chunk_k[Q];
+    __device__ __forceinline__ void init(const uint16_t* p, int64_t s_row, int64_t, int row0, int nrows, int w, int lane) {
+        base = reinterpret_cast<const char*>(p + (int64_t)row0 * s_row);
+        step = 2 * GBK;
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            const int row = 8 * (w + WAVES * i) + (lane >> 3), c = (lane & 7) ^ swz_x<64>(row);
+            off[i] = (uint32_t)min(row, nrows - 1 - row0) * (uint32_t)(2 * s_row) + 16u * c;
+            chunk_k[i] = 8 * c;
+        }
+    }
+    // slab kt, `left` of its k in the operand (64 or more: all)
+    __device__ __forceinline__ void issue(int kt, int left, uint8_t* lds, int w) const {
+        const char* p = base + kt * step;
+        if (left >= GBK) {
+#pragma unroll
+            for (int i = 0; i < Q; ++i) dma16(p, off[i], lds + (w + WAVES * i) * 1024);
+        } else {
+#pragma unroll
+            for (int i = 0; i < Q; ++i)
+                dma16(chunk_k[i] < left ? p + off[i] : reinterpret_cast<const char*>(kZeros), lds + (w + WAVES * i) * 1024);
+        }
+    }
+};
+// Contiguous along its rows: as it lies in memory, [64 k][R], chunks permuted within a row of LDS by
+// tr_swizzle.  GATED: column c of the tile is column 32 (c / 64) + c % 32 of one half of the matrix,
+// the second for odd c / 32.
+template <int R, int WAVES, bool GATED>
+struct Operand<R, WAVES, false, GATED> {
+    static constexpr int Q = R / 8 / WAVES, LPR = R / 8;
+    const char* base;
+    uint32_t off[Q];
+    int64_t step;
+    int row_k[Q];
+    __device__ __forceinline__ void init(const uint16_t* p, int64_t, int64_t s_k, int col0, int ncols, int w, int lane) {
+        base = reinterpret_cast<const char*>(p);
+        step = 2 * GBK * s_k;
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            const int idx = (w + WAVES * i) * 64 + lane, k = idx / LPR, c = 8 * ((idx % LPR) ^ tr_swizzle(k, LPR));
+            int col;
+            if constexpr (GATED) {
+                const int half = ncols / 2;
+                col = min(col0 / 2 + 32 * (c / 64) + c % 32, half - 8) + ((c / 32) & 1) * half;
+            } else {
+                col = min(col0 + c, ncols - 8);
+            }
+            off[i] = (uint32_t)k * (uint32_t)(2 * s_k) + 2u * (uint32_t)col;
+            row_k[i] = k;
+        }
+    }
+    __device__ __forceinline__ void issue(int kt, int left, uint8_t* lds, int w) const {
+        const char* p = base + kt * step;
+        if (left >= GBK) {
+#pragma unroll
+            for (int i = 0; i < Q; ++i) dma16(p, off[i], lds + (w + WAVES * i) * 1024);
+        } else {
+#pragma unroll
+            for (int i = 0; i < Q; ++i)
+                dma16(row_k[i] < left ? p + off[i] : reinterpret_cast<const char*>(kZeros), lds + (w + WAVES * i) * 1024);
+        }
+    }
+};
+
+// BM x BN outputs by PM x PN waves, NS stages
+template <int BM, int BN, int PM, int PN, int NS>
+struct Cfg {
+    static constexpr int WAVES = PM * PN, THREADS = 64 * WAVES;
+    static constexpr int FM = BM / PM / 32, FN = BN / PN / 32;   // 32 x 32 products of a wave
+    static constexpr int A_BYTES = BM * GBK * 2, STAGE = (BM + BN) * GBK * 2, LDS = NS * STAGE;
+    static constexpr int LOADS = (BM + BN) / 8 / WAVES;           // a wave's of a slab
+    static constexpr int OUT_BYTES = 32 * 32 * FN * 2;            // a wave's 32 rows of results
+    static constexpr int PER_CU = 160 * 1024 / LDS > 2 ? 2 : 160 * 1024 / LDS;
+    static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && FM >= 1 && FN >= 1, "whole loads and products");
+    static_assert(WAVES * OUT_BYTES <= STAGE, "results go through a stage");
+    static_assert(LOADS * (NS - 1) < 60, "vmcnt range");
+};
+
+// four values from p, `left` of them there, added to v (at any alignment)
+struct __attribute__((packed, aligned(2))) Four {
+    uint16_t v[4];
+};
+__device__ __forceinline__ void add4(const uint16_t* p, int left, float* v) {
+    Four x;
+    if (left >= 4) {
+        __builtin_memcpy(&x, p, 8);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x.v[e] = e < left ? p[e] : 0;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += __uint_as_float((uint32_t)x.v[e] << 16);
+}
+struct __attribute__((packed, aligned(2))) Eight {
+    uint16_t v[8];
+};
+__device__ __forceinline__ void put8(uint16_t* p, int left, const uint4& x) {
+    if (left >= 8) {
+        __builtin_memcpy(p, &x, 16);
+    } else {
+        Eight y;
+        __builtin_memcpy(&y, &x, 16);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) p[e] = y.v[e];
+    }
+}
+struct __attribute__((packed, aligned(4))) FourF {
+    float v[4];
+};
+
+// A wave's 32 rows of 32 NF columns through LDS: lane (row l32) puts columns 32 i + 8 q + 4 hl .. + 3, and takes
+// eight of a row, 4 NF lanes side by side.  16-byte chunks are permuted within a row so that rows spread over
+// the banks.
+template <int NF>
+struct Rows {
+    uint8_t* lds;
+    __device__ static int at(int row, int chunk) {
+        return row * 64 * NF + 16 * (chunk ^ (NF == 2 ? (row >> 1) & 7 : (row >> 2) & 3));
+    }
+    __device__ __forceinline__ void put(int row, int i, int q, int hl, const float* v) const {
+        *reinterpret_cast<uint2*>(lds + at(row, 4 * i + q) + 8 * hl) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    }
+    // to(row, first column, eight values) for all of them
+    template <typename F>
+    __device__ __forceinline__ void take(int lane, F to) const {
+        wave_lds_order();
+#pragma unroll
+        for (int p = 0; p < 2 * NF; ++p) {
+            const int row = p * (16 / NF) + lane / (4 * NF), chunk = lane % (4 * NF);
+            to(row, 8 * chunk, *reinterpret_cast<const uint4*>(lds + at(row, chunk)));
+        }
+        wave_lds_order();
+    }
+};
+
+template <int BM, int BN, int PM, int PN, int NS, bool A_KC, bool B_KC, int OUT>
+__global__ __launch_bounds__(64 * PM * PN, (Cfg<BM, BN, PM, PN, NS>::PER_CU * PM * PN / 4)) void product_kernel(Args g) {
+    using C = Cfg<BM, BN, PM, PN, NS>;
+    constexpr bool GATED = OUT == kGated;
+    static_assert(!GATED || C::FN == 2, "a wave holds both halves of its columns");
+    __shared__ __attribute__((aligned(16))) uint8_t smem[C::LDS];
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hl = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w % PM, wn = w / PM;
+    const int total = g.tm * g.tn * g.splits;   // (the host: fewer than 2^24)
+    const int slabs = (g.K + GBK - 1) / GBK;
+
+    Operand<BM, C::WAVES, A_KC, false> oa;
+    Operand<BN, C::WAVES, B_KC, GATED> ob;
+    struct Place {
+        int m0, n0, s0, nk;   // first row, column, slab, and the slabs
+        int64_t part;
+    };
+    // tiles go to the XCDs in runs of consecutive ones, eight rows of tiles by column after column: the
+    // workgroups of one XCD share rows of x and columns of W in its L2
+    auto place = [&](int v) {
+        Place p;
+        const int id = (int)xcd_range(v, total);
+        const int s = id / (g.tm * g.tn), t = id % (g.tm * g.tn);
+        const int band = t / (8 * g.tn), rows = min(8, g.tm - 8 * band), r = t - band * 8 * g.tn;
+        p.m0 = (8 * band + r % rows) * BM;
+        p.n0 = r / rows * BN;
+        p.s0 = s * g.per;
+        p.nk = min(g.per, slabs - p.s0);
+        p.part = (int64_t)s * g.M * g.N;
+        return p;
+    };
+    auto init = [&](const Place& p) __attribute__((always_inline)) {
+        oa.init(g.A, g.a_m, g.a_k, p.m0, A_KC ? g.M : g.ma, w, lane);
+        ob.init(g.B, g.b_n, g.b_k, p.n0, B_KC ? g.N : g.nb, w, lane);
+    };
+    auto issue = [&](int kt, int stage) __attribute__((always_inline)) {
+        uint8_t* st = smem + stage * C::STAGE;
+        const int left = g.K - kt * GBK;
+        oa.issue(kt, left, st, w);
+        ob.issue(kt, left, st + C::A_BYTES, w);
+    };
+
+    f32x16 acc[C::FN][C::FM];
+    auto zero = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < C::FN; ++i)
+#pragma unroll
+            for (int j = 0; j < C::FM; ++j) acc[i][j] = f32x16{};
+    };
+    auto mul = [&](int stage) __attribute__((always_inline)) {
+        const uint8_t* As = smem + stage * C::STAGE;
+        const uint8_t* Bs = As + C::A_BYTES;
+        bf16x8 a[2][C::FM], b[2][C::FN];
+        auto rd = [&](int ks, bf16x8(&ao)[C::FM], bf16x8(&bo)[C::FN]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < C::FN; ++i) bo[i] = lt_frag<BN, B_KC>(Bs, 32 * (C::FN * wn + i), ks, lane);
+#pragma unroll
+            for (int j = 0; j < C::FM; ++j) ao[j] = lt_frag<BM, A_KC>(As, 32 * (C::FM * wm + j), ks, lane);
+        };
+        rd(0, a[0], b[0]);
+#pragma unroll
+        for (int ks = 0; ks < GBK / 16; ++ks) {
+            if (ks + 1 < GBK / 16) rd(ks + 1, a[(ks + 1) & 1], b[(ks + 1) & 1]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < C::FM; ++j)
+#pragma unroll
+                for (int i = 0; i < C::FN; ++i)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[ks & 1][i], a[ks & 1][j], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // lane: row m of the rows' block j, four consecutive n for each quarter of the registers
+    auto write = [&](const Place& p, uint8_t* lds) __attribute__((always_inline)) {
+        const Rows<C::FN> wide{lds + w * C::OUT_BYTES};
+        const Rows<1> narrow{lds + w * C::OUT_BYTES};
+#pragma unroll
+        for (int j = 0; j < C::FM; ++j) {
+            const int m0 = p.m0 + 32 * (C::FM * wm + j), m = m0 + l32;
+            if constexpr (OUT == kF32) {
+                if (m >= g.M) continue;
+#pragma unroll
+                for (int i = 0; i < C::FN; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int n = p.n0 + 32 * (C::FN * wn + i) + 8 * q + 4 * hl;
+                        float* to = reinterpret_cast<float*>(g.y) + p.part + (int64_t)m * g.N + n;
+                        if (n + 4 <= g.N) {
+                            FourF x{{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]}};
+                            __builtin_memcpy(to, &x, 16);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (n + e < g.N) to[e] = acc[i][j][4 * q + e];
+                        }
+                    }
+            } else if constexpr (GATED) {
+                const int nw = p.n0 / 2 + 32 * wn;   // the wave's first column of each half
+                if (g.bias) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int n = nw + 8 * q + 4 * hl;
+                            float z[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) z[e] = acc[i][j][4 * q + e];
+                            add4(g.bias + i * g.F + n, g.F - n, z);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = z[e];
+                        }
+                }
+                if (g.pre) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            float z[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) z[e] = acc[i][j][4 * q + e];
+                            wide.put(l32, i, q, hl, z);
+                        }
+                    wide.take(lane, [&](int r, int c, const uint4& x) __attribute__((always_inline)) {
+                        const int n = nw + c % 32;
+                        if (m0 + r < g.M && n < g.F) put8(g.pre + (int64_t)(m0 + r) * g.N + c / 32 * g.F + n, g.F - n, x);
+                    });
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int n = nw + 8 * q + 4 * hl;
+                    float z[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[e] = activate<false>(acc[0][j][4 * q + e], acc[1][j][4 * q + e], SA_ACT_SWIGLU);
+                    if (g.res && m < g.M) add4(g.res + (int64_t)m * g.F + n, g.F - n, z);
+                    narrow.put(l32, 0, q, hl, z);
+                }
+                narrow.take(lane, [&](int r, int c, const uint4& x) __attribute__((always_inline)) {
+                    const int n = nw + c;
+                    if (m0 + r < g.M && n < g.F) put8(reinterpret_cast<uint16_t*>(g.y) + (int64_t)(m0 + r) * g.F + n, g.F - n, x);
+                });
+            } else {
+                const int nw = p.n0 + 32 * C::FN * wn;
+                auto out = [&](uint16_t* to) __attribute__((always_inline)) {
+                    wide.take(lane, [&](int r, int c, const uint4& x) __attribute__((always_inline)) {
+                        const int n = nw + c;
+                        if (m0 + r < g.M && n < g.N) put8(to + (int64_t)(m0 + r) * g.N + n, g.N - n, x);
+                    });
+                };
+                if (OUT >= kEpi && g.bias) {
+#pragma unroll
+                    for (int i = 0; i < C::FN; ++i)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int n = nw + 32 * i + 8 * q + 4 * hl;
+                            float z[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) z[e] = acc[i][j][4 * q + e];
+                            add4(g.bias + n, g.N - n, z);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = z[e];
+                        }
+                }
+                if (OUT >= kEpi && g.pre) {
+#pragma unroll
+                    for (int i = 0; i < C::FN; ++i)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            float z[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) z[e] = acc[i][j][4 * q + e];
+                            wide.put(l32, i, q, hl, z);
+                        }
+                    out(g.pre);
+                }
+#pragma unroll
+                for (int i = 0; i < C::FN; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int n = nw + 32 * i + 8 * q + 4 * hl;
+                        float z[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) z[e] = acc[i][j][4 * q + e];
+                        if constexpr (OUT >= kEpi) {
+                            if constexpr (OUT != kEpi + SA_ACT_NONE) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) z[e] = activate<false>(z[e], 0.f, OUT - kEpi);
+                            }
+                            if (g.res && m < g.M) add4(g.res + (int64_t)m * g.N + n, g.N - n, z);
+                        }
+                        wide.put(l32, i, q, hl, z);
+                    }
+                out(reinterpret_cast<uint16_t*>(g.y));
+            }
+        }
+    };
+
+    // The workgroup's slabs, tile after tile: (vi, ki) is the next one to load, (p, kt) the one multiplied.
+    int vi = blockIdx.x, ki = 0;
+    if (vi >= total) return;
+    Place pi = place(vi), p = pi;
+    init(pi);
+    int loaded = 0;   // slabs on their way or there, this one included
+    auto load_next = [&](int stage) __attribute__((always_inline)) {
+        if (vi >= total) return;
+        issue(pi.s0 + ki, stage);
+        ++loaded;
+        if (++ki == pi.nk) {
+            ki = 0;
+            vi += gridDim.x;
+            if (vi < total) {
+                pi = place(vi);
+                init(pi);
+            }
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s) load_next(s);
+    if (NS > 2 && loaded == NS - 1) wait_loads<(NS - 2) * C::LOADS>();
+    else wait_loads<0>();
+    barrier();
+    zero();
+    int v = blockIdx.x, kt = 0, stage = 0;
+    for (;;) {
+        load_next(stage == 0 ? NS - 1 : stage - 1);
+        mul(stage);
+        --loaded;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        // the next slab's loads (before the results' stores, which need not be done for it)
+        if (NS > 2 && loaded == NS - 1) wait_loads<(NS - 2) * C::LOADS>();
+        else wait_loads<0>();
+        if (++kt == p.nk) {
+            if (OUT != kF32) barrier();   // every wave is done with the stage that the results go through
+            write(p, smem + stage * C::STAGE);
+            v += gridDim.x;
+            if (v >= total) break;
+            p = place(v);
+            kt = 0;
+            zero();
+            if (OUT != kF32) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+        stage = stage == NS - 1 ? 0 : stage + 1;
+        barrier();
+    }
+}
+
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+template <int BM, int BN, int PM, int PN, int NS>
+hipError_t launch_t(const Product& p, hipStream_t stream) {
+    using C = Cfg<BM, BN, PM, PN, NS>;
+    Args g;
+    g.A = reinterpret_cast<const uint16_t*>(p.A);
+    g.B = reinterpret_cast<const uint16_t*>(p.B);
+    g.a_m = p.a_m; g.a_k = p.a_k; g.b_k = p.b_k; g.b_n = p.b_n;
+    g.M = p.M; g.N = p.N; g.K = p.K;
+    g.ma = p.ma; g.nb = p.nb;
+    const bool gated = p.epi && p.epi->act == SA_ACT_SWIGLU;
+    g.F = gated ? p.N / 2 : p.N;
+    g.tm = (int32_t)cdiv(p.M, BM);
+    g.tn = (int32_t)(gated ? cdiv(g.F, BN / 2) : cdiv(p.N, BN));
+    g.splits = p.splits;
+    g.per = p.per;
+    g.y = p.y;
+    g.bias = p.epi ? reinterpret_cast<const uint16_t*>(p.epi->bias) : nullptr;
+    g.res = p.epi ? reinterpret_cast<const uint16_t*>(p.epi->res) : nullptr;
+    g.pre = p.epi ? reinterpret_cast<uint16_t*>(p.epi->pre) : nullptr;
+    g.act = p.epi ? p.epi->act : SA_ACT_NONE;
+    const dim3 grid((unsigned)std::min<int64_t>((int64_t)g.tm * g.tn * g.splits, (int64_t)device_cus() * C::PER_CU));
+    const bool a_kc = p.a_k == 1, b_kc = p.b_k == 1;
+#define SA_RUN(AK, BK, OUT) \
+    hipLaunchKernelGGL((product_kernel<BM, BN, PM, PN, NS, AK, BK, OUT>), grid, dim3(C::THREADS), 0, stream, g)
+    if (p.epi) {
+        if (gated) {
+            if constexpr (C::FN == 2) SA_RUN(true, false, kGated);
+            else return hipErrorInvalidValue;
+        } else {
+            switch (g.act) {
+                case SA_ACT_RELU: SA_RUN(true, false, kEpi + SA_ACT_RELU); break;
+                case SA_ACT_GELU: SA_RUN(true, false, kEpi + SA_ACT_GELU); break;
+                case SA_ACT_SILU: SA_RUN(true, false, kEpi + SA_ACT_SILU); break;
+                default: SA_RUN(true, false, kEpi + SA_ACT_NONE);
+            }
+        }
+    } else if (a_kc && b_kc) {
+        SA_RUN(true, true, kBf16);
+    } else if constexpr (BM % 64 != 0 || BM == 192) {   // (rows of LDS that tr_swizzle permutes: powers of two)
+        return hipErrorInvalidValue;
+    } else if (p.y_bf16) {
+        SA_RUN(false, false, kBf16);
+    } else {
+        SA_RUN(false, false, kF32);
+    }
+#undef SA_RUN
+    return hipGetLastError();
+}
+
+}  // namespace
+
+bool product_supported(const Product& p) {
+    const bool a_kc = p.a_k == 1, b_kc = p.b_k == 1;
+    if (!al16(p.A) || !al16(p.B) || p.M < 1 || p.N < 1 || p.K < 1) return false;
+    if ((a_kc ? p.a_m : p.a_k) % 8 != 0 || (b_kc ? p.b_n : p.b_k) % 8 != 0) return false;
+    if ((a_kc || b_kc) && p.K % 8 != 0) return false;
+    if (!a_kc && (p.a_m != 1 || p.ma % 8 != 0 || p.ma < 8)) return false;
+    if (!b_kc && (p.b_n != 1 || p.nb % 8 != 0 || p.nb < 8)) return false;
+    if (p.epi) {
+        if (!a_kc || b_kc || (p.epi->act == SA_ACT_SWIGLU && p.nb % 16 != 0)) return false;
+    } else if (a_kc != b_kc || (a_kc && !p.y_bf16)) {
+        return false;
+    }
+    // a lane's offsets within a tile's slab are 32-bit bytes: 256 rows, or 64 k and all columns
+    auto fits = [](bool kc, int64_t rows, int64_t s_row, int64_t s_k) {
+        return kc ? 256 * s_row * 2 + 128 < (int64_t(1) << 32) : 64 * s_k * 2 + 2 * rows < (int64_t(1) << 32);
+    };
+    return fits(a_kc, p.ma, p.a_m, p.a_k) && fits(b_kc, p.nb, p.b_n, p.b_k) &&
+           cdiv(p.M, 64) * cdiv(p.N, 64) * p.splits < (int64_t(1) << 24);
+}
+
+int product_shapes() { return 6; }
+
+hipError_t launch_product(const Product& p, hipStream_t stream, int shape) {
+    if (!product_supported(p)) return hipErrorInvalidValue;
+    switch (shape) {
+        case 0: return launch_t<256, 256, 2, 4, 2>(p, stream);
+        case 1: return launch_t<192, 256, 2, 4, 2>(p, stream);
+        case 2: return launch_t<128, 256, 2, 4, 3>(p, stream);
+        case 3: return launch_t<256, 128, 4, 2, 3>(p, stream);
+        case 4: return launch_t<128, 128, 4, 2, 2>(p, stream);
+        default: return launch_t<64, 64, 2, 1, 4>(p, stream);
+    }
+}
+
+}  // namespace linear
+}  // namespace sa

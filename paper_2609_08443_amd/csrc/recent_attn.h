@@ -24,6 +24,7 @@ struct View {
     int32_t h, hk, g, window;
     float scale, cap;
     int64_t q_t, q_h, k_t, k_h, v_t, v_h;
+    int32_t skip = -1;   // backward: users with at most this many rows a key head are not this kernel's
 };
 
 // The forward pass and the queries' gradients go over tiles of `bq` rows of one user (all key
@@ -76,19 +77,36 @@ __device__ inline User user_at(const View& a, int64_t b) {
 // The user whose tiles include tile t, where user b's begin at first[b] per / size + b: one tile more
 // than its rows take at most, so that the tiles of all users number rows / size + B + 1
 // without a look at the offsets.  Also its first tile.
+__device__ inline int64_t first_tile(const int64_t* first, int64_t b, int64_t most, int32_t per, int32_t size) {
+    const int64_t v = first[b] < 0 ? 0 : first[b] > most ? most : first[b];
+    return v * per / size + b;
+}
 __device__ inline int64_t user_of_tile(const int64_t* first, int64_t B, int64_t most, int32_t per, int32_t size, int64_t t,
                                        int64_t* tile0) {
-    auto base = [&](int64_t b) {
-        const int64_t v = first[b] < 0 ? 0 : first[b] > most ? most : first[b];
-        return v * per / size + b;
-    };
     int64_t lo = 0, hi = B + 1;
     while (hi - lo > 1) {
         const int64_t m = (lo + hi) / 2;
-        if (base(m) <= t) lo = m;
+        if (first_tile(first, m, most, per, size) <= t) lo = m;
         else hi = m;
     }
-    *tile0 = base(lo);
+    *tile0 = first_tile(first, lo, most, per, size);
+    return lo;
+}
+// the same by a whole wave, 64 users at a time
+__device__ inline int64_t user_of_tile_wave(const int64_t* first, int64_t B, int64_t most, int32_t per, int32_t size,
+                                            int64_t t, int64_t* tile0) {
+    const int lane = threadIdx.x & 63;
+    int64_t lo = 0, hi = B + 1;
+    while (hi - lo > 1) {
+        const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const uint64_t le = __builtin_amdgcn_ballot_w64(at < hi && first_tile(first, at < hi ? at : lo, most, per, size) <= t);
+        // (user lo's is: lane 0's bit is set)
+        const int64_t n = lo + (63 - __builtin_clzll(le | 1)) * step;
+        hi = n + step < hi ? n + step : hi;
+        lo = n;
+    }
+    lo = ((int64_t)__builtin_amdgcn_readfirstlane((int32_t)(lo >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)lo);
+    *tile0 = first_tile(first, lo, most, per, size);
     return lo;
 }
 
@@ -101,39 +119,6 @@ __device__ inline void seen(const View& a, const User& u, int64_t i, int32_t* lo
     }
     *hi = e;
     *lo = a.window > 0 && e > a.window ? e - a.window : 0;
-}
-
-// Direct global -> LDS copy of 16 bytes a lane from base + off (base wave-uniform) to LDS bytes
-// [lds + 16 lane, + 16), as inline assembly: for the builtin the compiler makes the transposing
-// LDS reads wait for every such load in flight, the next unit's included.  Awaited by explicit
-// vmcnt waits.  M0, which holds the LDS address, is reserved: saved and restored.
-__device__ __forceinline__ void dma16(const char* base, uint32_t off, const void* lds) {
-    const uint32_t l = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)lds;
-    uint32_t saved;
-    asm volatile(
-        "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %3\n\t"
-        "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %1, %2\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(saved)
-        : "v"(off), "s"(base), "s"(l)
-        : "memory");
-}
-// at most N of this wave's loads still in flight; no LDS operation
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-    static_assert(N >= 0 && N < 64, "vmcnt range");
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (0 << 8) | ((N >> 4) << 14));
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-}
-
-__device__ __forceinline__ void barrier() {
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
 }
 
 __device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -167,6 +152,13 @@ struct Tile32<uint16_t, D> {
         for (int i = 0; i < D / 16; ++i)
             f.v[i] = ok ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(p + 16 * i + 8 * hl)) : bf16x8{};
     }
+    // the same of row l % 32 of a tile in LDS
+    __device__ static void load_tile(Frag& f, const uint16_t* tile, int lane) {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) f.v[i] = lds_b128(tile, swz<D>(lane & 31, 2 * i + (lane >> 5)));
+    }
+    // where column d (a multiple of 4) of a row of a tile is
+    __device__ static int place(int row, int d) { return swz<D>(row, d >> 3) + (d & 7); }
     __device__ static float dot(const Frag& a, const Frag& b) {   // this half's part
         float s = 0.f;
 #pragma unroll
@@ -219,6 +211,11 @@ struct Tile32<float, D> {
         for (int i = 0; i < D / 8; ++i)
             f.v[i] = ok ? *reinterpret_cast<const float4*>(p + 8 * i + 4 * hl) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
+    __device__ static void load_tile(Frag& f, const float* tile, int lane) {
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) f.v[i] = *reinterpret_cast<const float4*>(tile + at(lane & 31, 2 * i + (lane >> 5)));
+    }
+    __device__ static int place(int row, int d) { return at(row, d >> 2); }
     __device__ static float dot(const Frag& a, const Frag& b) {
         float s = 0.f;
 #pragma unroll
@@ -256,6 +253,32 @@ struct Tile32<float, D> {
         *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
     }
 };
+
+// <a, b> of n values in memory, 16 bytes at a time
+__device__ inline float dot_of(const uint16_t* a, const uint16_t* b, int n) {
+    float s = 0.f;
+    for (int i = 0; i < n; i += 8) {
+        const uint4 x = *reinterpret_cast<const uint4*>(a + i), y = *reinterpret_cast<const uint4*>(b + i);
+        const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            s = __builtin_fmaf(bf16_lo(xw[e]), bf16_lo(yw[e]), s);
+            s = __builtin_fmaf(bf16_hi(xw[e]), bf16_hi(yw[e]), s);
+        }
+    }
+    return s;
+}
+__device__ inline float dot_of(const float* a, const float* b, int n) {
+    float s = 0.f;
+    for (int i = 0; i < n; i += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(a + i), y = *reinterpret_cast<const float4*>(b + i);
+        s = __builtin_fmaf(x.x, y.x, s);
+        s = __builtin_fmaf(x.y, y.y, s);
+        s = __builtin_fmaf(x.z, y.z, s);
+        s = __builtin_fmaf(x.w, y.w, s);
+    }
+    return s;
+}
 
 // A capped score (in units of log 2) and, for the backward, the cap's derivative:
 //   cap tanh(x / cap) = cap (1 - 2 / (1 + exp(2 x / cap))).
@@ -300,6 +323,23 @@ struct KeysArgs {
 };
 int64_t key_tiles(int64_t B, int64_t T);
 hipError_t launch_keys(const KeysArgs& f, bool bf16, int32_t d, hipStream_t stream);
+
+// The whole backward of users with at most fused_rows rows a key head (0: no instance)
+struct FusedArgs {
+    View a;
+    const void *o, *dout;    // [N,h,d]
+    const float* lse;        // [N,h]
+    void *dq, *dK, *dV;
+    int64_t dq_t, dq_h, dk_t, dk_h, dv_t, dv_h;
+    int64_t items;           // chunks of keys: fused_items
+    int32_t chunk;           // keys of one, at most (a multiple of 128, at least 256)
+    float* parts;            // [fused_slots][hk][fused_rows][d]: dq of users with several chunks
+};
+int32_t fused_rows(bool bf16, int32_t d);
+int32_t fused_chunk(int64_t B, int64_t T, int32_t hk);
+int64_t fused_items(int64_t B, int64_t T, int32_t chunk);
+int64_t fused_slots(int64_t T, int32_t chunk);
+hipError_t launch_fused(const FusedArgs& f, bool bf16, int32_t d, hipStream_t stream);
 
 hipError_t launch_plan(const View& a, const RowsShape& s, int64_t tiles, TileRec* recs, int64_t* prefix,
                        hipStream_t stream);

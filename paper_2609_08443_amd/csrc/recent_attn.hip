@@ -24,7 +24,7 @@ __device__ int32_t plan_tile(const View& a, int32_t bq, int32_t unit, int64_t t,
     rec->user = (int32_t)b;
     rec->row0 = (int32_t)row0;
     rec->klo = rec->khi = (int32_t)us.tok0;
-    if (row0 >= rows) return 0;
+    if (row0 >= rows || rows <= a.skip) return 0;
     int32_t lo = us.L, hi = 0;
     if (!a.ends) {
         seen(a, us, 0, &lo, &hi);

@@ -1,0 +1,404 @@
+// The backward of the attention over recent histories for users with few rows (at most 64 a key
+// head, 32 at d = 128: 40 targets in training), all three gradients in one pass over the keys, which is what
+// bounds it: K and V read once, dK and dV written once.
+//
+// A workgroup holds a user's rows (q, dout and their statistics) in LDS and takes a chunk of the
+// keys of one key head, its waves 32 of every 128 in turn, each at its own pace.  S = q K^T and
+// dP = dout V^T leave a key's scores in its own two lanes, from where p goes into dV^T += dout^T p
+// and ds into dK^T += q^T ds; ds goes through LDS once, transposed, for dq^T += K^T ds^T, which a
+// wave keeps over all its keys.  dq of users with several chunks is added up in a second launch,
+// in the chunks' order.
+#include <algorithm>
+
+#include "recent_attn.h"
+
+namespace sa {
+namespace attn {
+
+namespace {
+
+template <typename T, int D>
+struct FusedCfg {
+    static constexpr int EL = sizeof(T), TILE = 32 * D * EL;
+    static constexpr int kTiles = D == 64 ? 2 : 1;        // tiles of rows
+    static constexpr int kFusedRows = 32 * kTiles;
+    static constexpr int ROWS = 2 * kTiles * TILE;        // q and dout
+    static constexpr int RING = 4 * 3 * TILE;             // a wave's keys, two stages, and its values
+    static constexpr int DS = 4 * 32 * 32 * EL;           // a wave's ds
+    static constexpr int LDS = ROWS + RING + DS;
+    static constexpr int LOADS = TILE / 1024;             // a wave's of 32 keys
+    static constexpr int PER_CU = EL == 2 && D == 64 ? 2 : 1;
+    static_assert(4 * 32 * 32 * 4 <= RING, "dq is joined there");
+};
+
+struct FusedStats {
+    float lse2[64], delta[64], slope2[64];
+    int32_t lo[64], hi[64];   // absolute; hi = lo: sees nothing
+};
+
+// A user's chunks: tokens in 32s, dealt out evenly to as few chunks as hold them.  Chunks of users with
+// several are longer than chunk / 2 - 32 keys, so that their first keys, over that length, number them apart.
+__device__ inline int32_t chunks_of(int32_t L, int32_t chunk) { return (int32_t)(((int64_t)L + chunk - 1) / chunk); }
+__device__ inline int32_t chunk_begin(int32_t L, int32_t n, int32_t i) {
+    const int64_t u = ((int64_t)L + 31) / 32;
+    return (int32_t)min((int64_t)L, 32 * (u * i / n));
+}
+__device__ inline int64_t slot_of(int64_t first, int32_t chunk) { return first / (chunk / 2 - 32); }
+
+// the transposed ds: [32 keys][32 rows] in LDS
+template <typename T>
+struct Turn;
+template <>
+struct Turn<uint16_t> {
+    typedef bf16x8 Half;
+    __device__ static void put(uint16_t* t, const f32x16& ds, int l32, int hl) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<uint2*>(t + swz<32>(l32, j) + 4 * hl) =
+                make_uint2(pack_bf16x2(ds[4 * j], ds[4 * j + 1]), pack_bf16x2(ds[4 * j + 2], ds[4 * j + 3]));
+    }
+    // c(d, row) += sum over keys of tile(key, d) ds(key, row)
+    template <int D>
+    __device__ static void add(f32x16 (&c)[D / 32], const uint16_t* tile, const uint16_t* t, int lane) {
+        const bf16x8 b0 = lds_tr_tokens<32>(t, lane, 0, 0), b1 = lds_tr_tokens<32>(t, lane, 0, 1);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            c[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_tr_tokens<D>(tile, lane, i, 0), b0, c[i], 0, 0, 0);
+            c[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_tr_tokens<D>(tile, lane, i, 1), b1, c[i], 0, 0, 0);
+        }
+    }
+};
+// x, which the compiler may not work out ahead of its use: addresses that come from it are computed where
+// they are needed, not kept in registers over the whole loop (without: 75 spilled registers at D = 64)
+__device__ __forceinline__ int anew(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, (FusedCfg<T, D>::PER_CU)) void fused_kernel(FusedArgs f) {
+    using C = FusedCfg<T, D>;
+    using M = Tile32<T, D>;
+    constexpr int kTiles = C::kTiles, kFusedRows = C::kFusedRows;
+    __shared__ __attribute__((aligned(16))) uint8_t smem[C::LDS];
+    __shared__ __attribute__((aligned(16))) FusedStats st;
+    const View& a = f.a;
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hl = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    T* const rows_q = reinterpret_cast<T*>(smem);
+    T* const rows_d = reinterpret_cast<T*>(smem + C::ROWS / 2);
+    uint8_t* const ring = smem + C::ROWS + w * 3 * C::TILE;
+    T* const vt = reinterpret_cast<T*>(ring + 2 * C::TILE);
+    T* const turn = reinterpret_cast<T*>(smem + C::ROWS + C::RING + w * 32 * 32 * C::EL);
+    const float inv_cap = a.cap > 0.f ? a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e, to_exp = 2.f * kLog2e * inv_cap;
+
+    for (int64_t v = blockIdx.x; v < f.items * a.hk; v += gridDim.x) {
+        const int64_t id = xcd_range(v, f.items * a.hk), item = id / a.hk;
+        const int32_t kv = (int32_t)(id % a.hk);
+        int64_t item0;
+        const int64_t b = user_of_tile_wave(a.offsets, a.B, a.T, 1, f.chunk, item, &item0);
+        User us = user_at(a, b);
+        if (b == a.B) {   // tokens behind the last user's
+            us.n = 0;
+            us.L = (int32_t)(a.T - us.tok0);
+        }
+        const int32_t n_chunks = chunks_of(us.L, f.chunk), ci = (int32_t)(item - item0);
+        if (ci >= n_chunks || (int64_t)us.n * a.g > kFusedRows) continue;
+        const int32_t rows = us.n * a.g;
+        const int32_t c0 = chunk_begin(us.L, n_chunks, ci), c1 = chunk_begin(us.L, n_chunks, ci + 1);
+        const int32_t first = (int32_t)us.tok0 + c0, last = (int32_t)us.tok0 + c1;   // the chunk's keys
+        const T* Kp = reinterpret_cast<const T*>(a.K) + kv * a.k_h;
+        const T* Vp = reinterpret_cast<const T*>(a.V) + kv * a.v_h;
+        // 32 keys or values from token k0 on, rows past the chunk repeating its last
+        auto issue = [&](const T* base, int64_t s_t, int32_t k0, void* to) __attribute__((always_inline)) {
+            const char* kb = reinterpret_cast<const char*>(base + (int64_t)k0 * s_t);
+            const int32_t left = last - 1 - k0;
+            const int lane = anew(tid) & 63;
+#pragma unroll
+            for (int i = 0; i < C::LOADS; ++i) {
+                const int pos = i * 64 + lane, r = pos / M::CHUNKS;
+                dma16(kb, (uint32_t)min(r, left) * (uint32_t)(s_t * C::EL) + 16u * M::chunk_at(r, pos % M::CHUNKS),
+                      reinterpret_cast<uint8_t*>(to) + i * 1024);
+            }
+        };
+        const int32_t mine = first + 32 * w;   // the wave's first keys, then every 128th
+        __syncthreads();                       // the last item's rows are read
+        if (rows > 0 && mine < last) {
+            issue(Kp, a.k_t, mine, ring);
+            issue(Vp, a.v_t, mine, vt);
+        }
+
+        // the rows: q and dout as they are, zeros for those that see nothing
+        if (rows > 0) {
+            for (int x = tid; x < kFusedRows * M::CHUNKS; x += 256) {
+                const int r = x / M::CHUNKS, pos = x % M::CHUNKS, chunk = M::chunk_at(r & 31, pos);
+                uint4 qv = make_uint4(0, 0, 0, 0), dv = qv;
+                if (r < rows) {
+                    const int64_t target = us.t0 + r / a.g;
+                    const int32_t head = kv * a.g + r % a.g;
+                    int32_t lo, hi;
+                    seen(a, us, target, &lo, &hi);
+                    if (hi > lo) {
+                        qv = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.q) + target * a.q_t + head * a.q_h + chunk * (16 / C::EL));
+                        dv = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(f.dout) + (target * a.h + head) * D + chunk * (16 / C::EL));
+                    }
+                }
+                reinterpret_cast<uint4*>(rows_q)[x] = qv;
+                reinterpret_cast<uint4*>(rows_d)[x] = dv;
+            }
+            // statistics, four threads a row (of 64)
+            const int r = tid >> 2, part = tid & 3;
+            float lse2 = __builtin_inff(), delta = 0.f, slope2 = 0.f;
+            int32_t lo = 0, hi = 0;
+            if (r < rows) {
+                const int64_t target = us.t0 + r / a.g;
+                const int32_t head = kv * a.g + r % a.g;
+                seen(a, us, target, &lo, &hi);
+                lo += (int32_t)us.tok0;
+                hi += (int32_t)us.tok0;
+                if (hi > lo) {
+                    const int64_t o = target * a.h + head;
+                    const T* op = reinterpret_cast<const T*>(f.o) + o * D + part * (D / 4);
+                    const T* dp = reinterpret_cast<const T*>(f.dout) + o * D + part * (D / 4);
+                    delta = dot_of(op, dp, D / 4);
+                    const float lse = f.lse[o];
+                    if (lse != -__builtin_inff()) lse2 = lse * kLog2e;
+                    if (a.slopes) slope2 = a.slopes[head] * kLog2e;
+                }
+            }
+            delta += __shfl_xor(delta, 1, 64);
+            delta += __shfl_xor(delta, 2, 64);
+            if (part == 0) {
+                st.lse2[r] = lse2;
+                st.delta[r] = delta;
+                st.slope2[r] = slope2;
+                st.lo[r] = lo;
+                st.hi[r] = hi;
+            }
+        }
+        __syncthreads();
+
+        f32x16 dq[kTiles][D / 32];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) dq[t][i] = f32x16{};
+        int stage = 0;
+        for (int32_t k0 = mine; k0 < last; k0 += 128) {
+            f32x16 dk[D / 32], dv[D / 32];
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = f32x16{};
+            T* const kt = reinterpret_cast<T*>(ring + stage * C::TILE);
+            if (rows > 0) {
+                wait_loads<0>();
+                typename M::Frag kf, vf;
+                M::load_tile(kf, kt, lane);
+                M::load_tile(vf, vt, lane);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before it is written again
+                if (k0 + 128 < last) {
+                    issue(Kp, a.k_t, k0 + 128, ring + (stage ^ 1) * C::TILE);
+                    issue(Vp, a.v_t, k0 + 128, vt);
+                }
+                const int32_t kn = min(k0 + 32, last), key = k0 + l32;
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    if (32 * t >= rows) break;
+                    const int32_t lo = st.lo[32 * t + l32], hi = st.hi[32 * t + l32];
+                    const bool live = hi > lo;
+                    if (!__builtin_amdgcn_ballot_w64(live && lo < kn && hi > k0)) continue;
+                    const bool whole = __builtin_amdgcn_ballot_w64((live && (lo > k0 || hi < kn)) || kn != k0 + 32) == 0;
+                    const T* qt = rows_q + t * 32 * D;
+                    const T* dt = rows_d + t * 32 * D;
+                    f32x16 s = f32x16{}, ds = f32x16{};
+                    M::with_rows(s, qt, kf, lane);
+                    M::with_rows(ds, dt, vf, lane);
+                    float cc = a.scale * kLog2e;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float4 de = *reinterpret_cast<const float4*>(&st.delta[32 * t + 8 * j + 4 * hl]);
+                        ds[4 * j] -= de.x;
+                        ds[4 * j + 1] -= de.y;
+                        ds[4 * j + 2] -= de.z;
+                        ds[4 * j + 3] -= de.w;
+                    }
+                    if (a.cap > 0.f) {
+                        cc = 1.f;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            float slope;
+                            s[r] = capped<T>(s[r], to_exp, inv_cap, cap2, &slope);
+                            ds[r] *= slope;
+                        }
+                    }
+                    if (a.slopes) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int row = 32 * t + srow(r, hl);
+                            s[r] = __builtin_fmaf(s[r], cc, st.slope2[row] * (float)(key + 1 - st.hi[row]));
+                        }
+                        cc = 1.f;
+                    }
+                    if (!whole) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int row = 32 * t + srow(r, hl);
+                            const bool in = key >= st.lo[row] && key < st.hi[row] && key < last;
+                            s[r] = in ? s[r] : -__builtin_inff();
+                            ds[r] = in ? ds[r] : 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float4 ls = *reinterpret_cast<const float4*>(&st.lse2[32 * t + 8 * j + 4 * hl]);
+                        const float lv[4] = {ls.x, ls.y, ls.z, ls.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            s[4 * j + e] = exp2_(__builtin_fmaf(s[4 * j + e], cc, -lv[e]));
+                            ds[4 * j + e] *= s[4 * j + e];
+                        }
+                    }
+                    Turn<T>::put(turn, ds, l32, hl);
+                    __builtin_amdgcn_sched_barrier(0);   // (one after the other: the registers are full)
+                    M::with_cols(dv, dt, M::cols(s), lane);
+                    __builtin_amdgcn_sched_barrier(0);
+                    M::with_cols(dk, qt, M::cols(ds), lane);
+                    wave_lds_order();
+                    __builtin_amdgcn_sched_barrier(0);
+                    Turn<T>::template add<D>(dq[t], kt, turn, lane);
+                    wave_lds_order();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            // dK and dV of the 32 keys, in whole rows through the keys' own place
+            auto put = [&](f32x16 (&x)[D / 32], void* base, int64_t s_t, int64_t s_h, float scale) __attribute__((always_inline)) {
+                const int lane = anew(tid) & 63, l32 = lane & 31, hl = lane >> 5;
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float y[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[e] = x[i][4 * j + e] * scale;
+                        M::store4(kt + M::place(l32, 32 * i + 8 * j + 4 * hl), y);
+                    }
+                wave_lds_order();
+                T* to = reinterpret_cast<T*>(base) + kv * s_h;
+#pragma unroll
+                for (int i = 0; i < C::LOADS; ++i) {
+                    const int pos = i * 64 + lane, r = pos / M::CHUNKS;
+                    const uint4 y = reinterpret_cast<const uint4*>(kt)[pos];
+                    if (k0 + r < last)
+                        *reinterpret_cast<uint4*>(to + (int64_t)(k0 + r) * s_t + M::chunk_at(r, pos % M::CHUNKS) * (16 / C::EL)) = y;
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            };
+            put(dk, f.dK, f.dk_t, f.dk_h, a.scale);
+            put(dv, f.dV, f.dv_t, f.dv_h, 1.f);
+            stage ^= 1;
+        }
+        if (rows == 0) continue;
+
+        // dq: the waves' sums, 32 rows by 32 values at a time
+        float* const join = reinterpret_cast<float*>(smem + C::ROWS);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            if (32 * t >= rows) break;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                __syncthreads();
+#pragma unroll
+                for (int r = 0; r < 16; ++r) join[(32 * w + srow(r, hl)) * 32 + l32] = dq[t][i][r];
+                __syncthreads();
+                const int row = tid & 31, d0 = 4 * (tid >> 5), rr = 32 * t + row;
+                float y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float* x = join + (d0 + e) * 32 + row;
+                    y[e] = ((x[0] + x[32 * 32]) + (x[2 * 32 * 32] + x[3 * 32 * 32]));
+                }
+                if (rr < rows) {
+                    if (n_chunks == 1) {
+                        const int64_t target = us.t0 + rr / a.g;
+                        const int32_t head = kv * a.g + rr % a.g;
+                        const bool live = st.hi[rr] > st.lo[rr];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[e] = live ? y[e] * a.scale : 0.f;
+                        M::store4(reinterpret_cast<T*>(f.dq) + target * f.dq_t + head * f.dq_h + 32 * i + d0, y);
+                    } else {
+                        float* to = f.parts + ((slot_of(first, f.chunk) * a.hk + kv) * kFusedRows + rr) * D + 32 * i + d0;
+                        *reinterpret_cast<float4*>(to) = make_float4(y[0], y[1], y[2], y[3]);
+                    }
+                }
+            }
+        }
+    }
+}
+
+// dq of users with several chunks, or none
+template <typename T, int D>
+__global__ __launch_bounds__(256) void fused_sum_kernel(FusedArgs f) {
+    const View& a = f.a;
+    constexpr int kFusedRows = FusedCfg<T, D>::kFusedRows;
+    for (int64_t v = blockIdx.x; v < (a.B + 1) * a.hk; v += gridDim.x) {
+        const int64_t b = v / a.hk;
+        const int32_t kv = (int32_t)(v % a.hk);
+        const User us = user_at(a, b);
+        const int64_t rows = (int64_t)us.n * a.g;
+        const int32_t n = b < a.B ? chunks_of(us.L, f.chunk) : 0;
+        if (n == 1 || (rows > kFusedRows && n > 0)) continue;
+        for (int64_t x = threadIdx.x; x < rows * (D / 4); x += 256) {
+            const int64_t r = x / (D / 4);
+            const int32_t d = 4 * (int32_t)(x % (D / 4));
+            const int64_t target = us.t0 + r / a.g;
+            const int32_t head = kv * a.g + (int32_t)(r % a.g);
+            int32_t lo, hi;
+            seen(a, us, target, &lo, &hi);
+            float y[4] = {0.f, 0.f, 0.f, 0.f};
+            if (hi > lo) {
+                for (int32_t i = 0; i < n; ++i) {
+                    const int64_t first = us.tok0 + chunk_begin(us.L, n, i);
+                    const float4 p = *reinterpret_cast<const float4*>(f.parts + ((slot_of(first, f.chunk) * a.hk + kv) * kFusedRows + r) * D + d);
+                    y[0] += p.x;
+                    y[1] += p.y;
+                    y[2] += p.z;
+                    y[3] += p.w;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] *= a.scale;
+            Tile32<T, D>::store4(reinterpret_cast<T*>(f.dq) + target * f.dq_t + head * f.dq_h + d, y);
+        }
+    }
+}
+
+template <typename T, int D>
+hipError_t launch_fused_t(const FusedArgs& f, hipStream_t stream) {
+    const int64_t most = int64_t(1) << 22;
+    if (f.a.T > 0)
+        hipLaunchKernelGGL((fused_kernel<T, D>), dim3((unsigned)std::min(f.items * f.a.hk, most)), dim3(256), 0, stream, f);
+    if (f.a.N > 0)
+        hipLaunchKernelGGL((fused_sum_kernel<T, D>), dim3((unsigned)std::min((f.a.B + 1) * f.a.hk, most)), dim3(256), 0, stream, f);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int32_t fused_rows(bool bf16, int32_t d) {
+    return !bf16 ? 0 : d == 64 ? FusedCfg<uint16_t, 64>::kFusedRows : FusedCfg<uint16_t, 128>::kFusedRows;
+}
+
+int32_t fused_chunk(int64_t B, int64_t T, int32_t hk) {
+    // enough chunks for the compute units, and few enough that their rows cost little
+    const int64_t want = T * hk / (4 * (int64_t)device_cus());
+    return (int32_t)std::min<int64_t>(2048, std::max<int64_t>(256, want / 128 * 128));
+}
+int64_t fused_items(int64_t B, int64_t T, int32_t chunk) { return T / chunk + B + 1; }
+int64_t fused_slots(int64_t T, int32_t chunk) { return T / (chunk / 2 - 32) + 1; }
+
+hipError_t launch_fused(const FusedArgs& f, bool bf16, int32_t d, hipStream_t stream) {
+    if (!bf16) return hipErrorInvalidValue;
+    return d == 64 ? launch_fused_t<uint16_t, 64>(f, stream) : launch_fused_t<uint16_t, 128>(f, stream);
+}
+
+}  // namespace attn
+}  // namespace sa

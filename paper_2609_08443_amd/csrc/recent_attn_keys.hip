@@ -42,14 +42,14 @@ __global__ __launch_bounds__(256, (KeysCfg<T, D>::PER_CU)) void keys_kernel(Keys
         const int64_t id = xcd_range(v, f.tiles * a.hk), tile = id / a.hk;
         const int32_t kv = (int32_t)(id % a.hk);
         int64_t tile0;
-        const int64_t b = user_of_tile(a.offsets, a.B, a.T, 1, kKeys, tile, &tile0);
+        const int64_t b = user_of_tile_wave(a.offsets, a.B, a.T, 1, kKeys, tile, &tile0);
         User us = user_at(a, b);
         if (b == a.B) {   // tokens behind the last user's
             us.n = 0;
             us.L = (int32_t)(a.T - us.tok0);
         }
         const int64_t first = (tile - tile0) * kKeys;
-        if (first >= us.L) continue;
+        if (first >= us.L || (int64_t)us.n * a.g <= a.skip) continue;
         const int32_t nk = (int32_t)min((int64_t)kKeys, us.L - first);
         const int64_t key0 = us.tok0 + first + 32 * w;   // the wave's first
         const int32_t mine = nk - 32 * w;                // how many it has

@@ -100,6 +100,56 @@ __device__ inline void load_lds16(const void* src, void* lds_base) {
 }
 __device__ inline void wait_vmem() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// Direct global -> LDS copy of 16 bytes per lane (global_load_lds_dwordx4) from
+// base + off (base wave-uniform) to LDS bytes [lds + 16 lane, + 16), written as
+// inline assembly: the compiler cannot tell which LDS bytes such a load writes,
+// so for the builtin it makes the transposing LDS reads wait for every load in
+// flight, later slabs' included.  Completion is awaited by explicit vmcnt waits.
+// M0 (which holds the load's LDS address) is a reserved register, so the block
+// saves and restores it instead of declaring it clobbered.
+__device__ __forceinline__ void dma16(const char* base, uint32_t off, const void* lds) {
+    const uint32_t l = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)lds;
+    uint32_t saved;
+    asm volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %3\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dwordx4 %1, %2\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "v"(off), "s"(base), "s"(l)
+        : "memory");
+}
+// the same from an address of each lane's own
+__device__ __forceinline__ void dma16(const char* from, const void* lds) {
+    const uint32_t l = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)lds;
+    uint32_t saved;
+    asm volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %2\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dwordx4 %1, off\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "v"(from), "s"(l)
+        : "memory");
+}
+// At most N of this wave's vector memory operations still in flight; LDS operations go on.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+// Workgroup barrier alone, no waits
+__device__ __forceinline__ void barrier() {
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // Workgroup barrier for LDS traffic only: waits for this wave's LDS operations,
 // then s_barrier.  Unlike __syncthreads(), which also waits for every
 // outstanding global load (vmcnt(0)), loads issued into registers ahead of time

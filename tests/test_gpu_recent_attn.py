@@ -126,6 +126,11 @@ CASES = {
     # rows and tokens behind the last user's
     "tail": dict(tokens=[30, 70], targets=[3, 60], h=2, hk=2, tail=(37, 150)),
     "tail_single": dict(tokens=[30, 70], targets=[1, 1], h=2, hk=2, tail=(200, 5)),
+    # rows around what one pass over the keys takes (64, or 32 at d = 128), beside users with more; several chunks
+    "few_rows": dict(tokens=[700, 31, 1500, 256, 4], targets=[32, 33, 64, 63, 1], h=1, hk=1, ends="random"),
+    "few_and_many": dict(tokens=[513, 2100, 65, 0, 300], targets=[65, 3, 200, 5, 0], h=2, hk=2, ends="random"),
+    "few_shared": dict(tokens=[600, 1030], targets=[8, 9], h=8, hk=2, cap=5.0, window=300),
+    "chunks": dict(tokens=[255, 256, 257, 3000, 1, 511, 513], targets=[2, 1, 2, 40, 1, 3, 1], h=2, hk=1),
     # no user at all
     "no_users": dict(tokens=[], targets=[], h=2, hk=2, tail=(5, 3)),
     "ends_out_of_range": dict(tokens=[20, 9], targets=[3, 2], h=1, hk=1, ends=[-5, 21, 2 ** 31 - 1, 0, 9]),
