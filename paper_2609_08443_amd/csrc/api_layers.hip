@@ -4,7 +4,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
 
 #include "linear.h"
 #include "linear_gemm.h"
@@ -28,7 +27,7 @@ struct AttnPlan {
     sa::attn::RowsShape shape;
     int64_t tiles = 0;
     int32_t grid = 1;
-    size_t off_recs = 0, off_prefix = 0, off_parts = 0, off_delta = 0, total = 0;
+    size_t off_recs = 0, off_prefix = 0, off_keys = 0, off_parts = 0, off_delta = 0, total = 0;
 };
 
 AttnPlan plan_attn(const sa_recent_attn& a, bool bwd) {
@@ -65,6 +64,7 @@ AttnPlan plan_attn(const sa_recent_attn& a, bool bwd) {
     p.off_recs = carve(sizeof(sa::attn::TileRec) * (size_t)p.tiles);
     p.off_prefix = carve(sizeof(int64_t) * ((size_t)p.tiles + 1));
     p.off_parts = carve(sizeof(float) * 2 * (size_t)p.grid * p.shape.bq * (a.d + 2));
+    if (bwd) p.off_keys = carve(sizeof(int64_t) * ((size_t)a.B + 2));
     if (bwd) p.off_delta = carve(sizeof(float) * (size_t)a.N * a.h);
     p.total = off;
     return p;
@@ -133,16 +133,16 @@ sa::attn::RowsArgs rows_args(const sa::attn::View& v, const AttnPlan& p, uint8_t
     return f;
 }
 
-hipError_t run_rows(const sa::attn::RowsArgs& f, const AttnPlan& p, const sa_recent_attn& a, bool bwd, uint8_t* ws,
-                    hipStream_t stream) {
+hipError_t run_plan(const sa::attn::RowsArgs& f, const AttnPlan& p, bool bwd, uint8_t* ws, hipStream_t stream) {
+    sa::ProfScope ps("recent_attn_plan", stream);
+    return sa::attn::launch_plan(f.a, p.shape, p.tiles, reinterpret_cast<sa::attn::TileRec*>(ws + p.off_recs),
+                                 reinterpret_cast<int64_t*>(ws + p.off_prefix),
+                                 bwd ? reinterpret_cast<int64_t*>(ws + p.off_keys) : nullptr, stream);
+}
+hipError_t run_rows(const sa::attn::RowsArgs& f, const AttnPlan& p, const sa_recent_attn& a, bool bwd, hipStream_t stream) {
     const bool bf = a.dtype == SA_BF16;
-    hipError_t e;
+    hipError_t e = hipSuccess;
     {
-        sa::ProfScope ps("recent_attn_plan", stream);
-        e = sa::attn::launch_plan(f.a, p.shape, p.tiles, reinterpret_cast<sa::attn::TileRec*>(ws + p.off_recs),
-                                  reinterpret_cast<int64_t*>(ws + p.off_prefix), stream);
-    }
-    if (e == hipSuccess) {
         sa::ProfScope ps(bwd ? "recent_attn_dq" : "recent_attn_fwd", stream);
         e = bwd ? sa::attn::launch_rows_dq(f, bf, a.d, p.wide, stream) : sa::attn::launch_rows_fwd(f, bf, a.d, p.wide, stream);
     }
@@ -176,9 +176,7 @@ sa_status check_linear(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dt
     return SA_OK;
 }
 
-int g_shape() { const char* e = getenv("SA_SHAPE"); return e ? atoi(e) : 0; }
-// the bf16 products of a layer; pointers of its operands where they are known, any aligned ones else
-const void* const kAny = reinterpret_cast<const void*>(256);
+// the bf16 products of a layer;
 sa::linear::Product fwd_product(const void* x, int64_t x_ld, const void* W, int64_t N, int32_t K, int32_t C,
                                 const sa::linear::Epilogue* epi, void* y) {
     return {x, W, x_ld, 1, C, 1, (int32_t)N, C, K, 0, C, y, true, epi};
@@ -206,13 +204,11 @@ LinearBwdPlan plan_linear_bwd(int64_t N, int32_t K, int32_t F, sa_activation act
     p.off_parts = align_up(p.off_sums + 4 * (size_t)sa::linear::act_bwd_parts(N, F, dtype == SA_BF16) * C, 256);
     p.total = p.off_parts;
     if (dtype == SA_BF16) {
-        const int64_t slabs = (N + 63) / 64, tiles = (int64_t)((K + 255) / 256) * ((C + 255) / 256);
-        const int64_t most = std::min<int64_t>(sa::device_cus() / tiles, slabs / 8);
-        if (most > 1) {
-            p.per = (int32_t)((slabs + most - 1) / most);
-            p.splits = (int32_t)((slabs + p.per - 1) / p.per);
-            p.total += 4 * (size_t)p.splits * K * C;
-        }
+        sa::linear::Product prod = dw_product(nullptr, K, nullptr, N, K, columns(F, act), nullptr, false);
+        sa::linear::choose_splits(&prod);
+        p.splits = prod.splits;
+        p.per = prod.per;
+        if (p.splits > 1) p.total += 4 * (size_t)p.splits * K * C;
     }
     return p;
 }
@@ -321,7 +317,7 @@ sa_status sa_linear_fwd(const void* x, int64_t x_stride, const void* W, const vo
     const sa::linear::Product prod = fwd_product(x, x_stride, W, N, K, C, &epi, y);
     hipError_t e;
     if (bf && sa::linear::product_supported(prod)) {
-        e = sa::linear::launch_product(prod, stream, g_shape());
+        e = sa::linear::launch_product(prod, stream);
         if (e != hipSuccess) return hip_fail(e, "linear layer launch");
         return SA_OK;
     }
@@ -370,7 +366,7 @@ sa_status sa_linear_bwd(const void* x, int64_t x_stride, const void* W, const vo
     if (e == hipSuccess && dx) {
         sa::ProfScope ps("linear_dx", stream);
         const sa::linear::Product prod = dx_product(dz, W, N, K, C, dx);
-        if (bf && sa::linear::product_supported(prod)) e = sa::linear::launch_product(prod, stream, g_shape());
+        if (bf && sa::linear::product_supported(prod)) e = sa::linear::launch_product(prod, stream);
         else e = sa::launch_gemm({dz, bf, 0, C, 1, W, bf, 0, 1, C, dx, bf, 0, K, (int32_t)N, K, C, 1, 1.f, false}, stream);
     }
     if (e == hipSuccess && dW) {
@@ -383,7 +379,7 @@ sa_status sa_linear_bwd(const void* x, int64_t x_stride, const void* W, const vo
             prod.per = p.per;
         }
         if (bf && sa::linear::product_supported(prod)) {
-            e = sa::linear::launch_product(prod, stream, g_shape());
+            e = sa::linear::launch_product(prod, stream);
             if (e == hipSuccess && p.splits > 1)
                 e = sa::linear::launch_sum_splits(reinterpret_cast<const float*>(ws + p.off_parts), p.splits, (int64_t)K * C, dW, wb, stream);
         } else e = sa::launch_gemm({x, bf, 0, 1, x_stride, dz, bf, 0, C, 1, dW, wb, 0, C, K, C, (int32_t)N, 1, 1.f, false}, stream);
@@ -415,7 +411,8 @@ sa_status sa_recent_attn_fwd(const sa_recent_attn* a, void* out, float* lse, voi
     sa::attn::RowsArgs f = rows_args(v, p, ws);
     f.out = out;
     f.lse = lse;
-    const hipError_t e = run_rows(f, p, *a, false, ws, stream);
+    hipError_t e = run_plan(f, p, false, ws, stream);
+    if (e == hipSuccess) e = run_rows(f, p, *a, false, stream);
     if (e != hipSuccess) return hip_fail(e, "recent attention launch");
     return SA_OK;
 }
@@ -459,22 +456,24 @@ sa_status sa_recent_attn_bwd(const sa_recent_attn* a, const void* out, const flo
         e = sa::attn::launch_fused(f, bf, a->d, stream);
         v.skip = sa::attn::fused_rows(bf, a->d);
     }
-    if (e == hipSuccess && p.rest && a->N > 0) {
-        sa::attn::RowsArgs f = rows_args(v, p, ws);
-        f.out = gr.dq;
-        f.dq_t = gr.dq_stride;
-        f.dq_h = gr.dq_head_stride;
-        f.lse = const_cast<float*>(lse);
-        f.o = out;
-        f.dout = dout;
-        f.delta = delta;
-        e = run_rows(f, p, *a, true, ws, stream);
-    }
-    if (e == hipSuccess && p.rest && a->T > 0) {
-        sa::ProfScope ps("recent_attn_keys", stream);
-        sa::attn::KeysArgs f{v, dout, lse, delta, gr.dK, gr.dV, gr.dk_stride, gr.dk_head_stride, gr.dv_stride,
-                             gr.dv_head_stride, sa::attn::key_tiles(a->B, a->T)};
-        e = sa::attn::launch_keys(f, bf, a->d, stream);
+    if (e == hipSuccess && p.rest) {
+        sa::attn::RowsArgs r = rows_args(v, p, ws);
+        r.out = gr.dq;
+        r.dq_t = gr.dq_stride;
+        r.dq_h = gr.dq_head_stride;
+        r.lse = const_cast<float*>(lse);
+        r.o = out;
+        r.dout = dout;
+        r.delta = delta;
+        e = run_plan(r, p, true, ws, stream);
+        if (e == hipSuccess && a->N > 0) e = run_rows(r, p, *a, true, stream);
+        if (e == hipSuccess && a->T > 0) {
+            sa::ProfScope ps("recent_attn_keys", stream);
+            sa::attn::KeysArgs f{v, dout, lse, delta, gr.dK, gr.dV, gr.dk_stride, gr.dk_head_stride, gr.dv_stride,
+                                 gr.dv_head_stride, reinterpret_cast<const int64_t*>(ws + p.off_keys),
+                                 sa::attn::key_tiles(a->B, a->T)};
+            e = sa::attn::launch_keys(f, bf, a->d, stream);
+        }
     }
     if (e != hipSuccess) return hip_fail(e, "recent attention backward launch");
     return SA_OK;

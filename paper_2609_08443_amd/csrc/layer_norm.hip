@@ -242,23 +242,10 @@ __global__ __launch_bounds__(kThreads) void norm_cols_kernel(const T* __restrict
     sums[((int64_t)blockIdx.y * 2 + 1) * D + c] = db;
 }
 
-// dgamma and dbeta: sums over the parts, in order; 32 columns a workgroup, parts over 8 threads each
+// dgamma and dbeta: sums over the parts, in order
 __global__ __launch_bounds__(kThreads) void norm_sum_kernel(const float* __restrict__ sums, int n, int D,
                                                             float* __restrict__ dgamma, float* __restrict__ dbeta) {
-    __shared__ float acc[8][33];
-    const int c = blockIdx.x * 32 + threadIdx.x % 32, p = threadIdx.x / 32;
-    float s = 0.f;
-    if (c < 2 * D)
-        for (int i = p; i < n; i += 8) s += sums[(int64_t)i * 2 * D + c];
-    acc[p][threadIdx.x % 32] = s;
-    __syncthreads();
-    if (p == 0 && c < 2 * D) {
-        s = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s += acc[i][threadIdx.x];
-        if (c < D) dgamma[c] = s;
-        else dbeta[c - D] = s;
-    }
+    vec::sum_parts(sums, n, 2 * (int64_t)D, [&](int64_t c, float s) { (c < D ? dgamma[c] : dbeta[c - D]) = s; });
 }
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -295,7 +282,7 @@ template <typename T>
 int64_t bwd_parts(int64_t N, int D) {
     const int rows = rows_at_once<T>(D);
     if (rows == 0) return std::min<int64_t>(std::max<int64_t>(N, 1), 64);
-    return std::max<int64_t>(1, std::min<int64_t>(cdiv(N, rows), 2 * (int64_t)device_cus()));
+    return std::max<int64_t>(1, std::min<int64_t>(cdiv(N, rows), 4 * (int64_t)device_cus()));
 }
 
 template <typename T>
@@ -339,7 +326,7 @@ hipError_t norm_bwd(const NormArgs& a, hipStream_t stream) {
         });
     }
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)cdiv(2 * (int64_t)a.D, 32)), dim3(kThreads), 0, stream, a.sums,
+    hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)cdiv(2 * (int64_t)a.D, vec::kSumColumns)), dim3(kThreads), 0, stream, a.sums,
                        (int)parts, a.D, a.dgamma, a.dbeta);
     return hipGetLastError();
 }

@@ -112,19 +112,7 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const T* __restrict__
 
 template <typename TO>
 __global__ __launch_bounds__(kThreads) void bias_sum_kernel(const float* __restrict__ sums, int n, int C, TO* __restrict__ db) {
-    __shared__ float acc[8][33];
-    const int c = blockIdx.x * 32 + threadIdx.x % 32, p = threadIdx.x / 32;
-    float s = 0.f;
-    if (c < C)
-        for (int i = p; i < n; i += 8) s += sums[(int64_t)i * C + c];
-    acc[p][threadIdx.x % 32] = s;
-    __syncthreads();
-    if (p == 0 && c < C) {
-        s = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s += acc[i][threadIdx.x];
-        vec::store(db + c, s);
-    }
+    vec::sum_parts(sums, n, C, [&](int64_t c, float s) { vec::store(db + c, s); });
 }
 
 // n values (a multiple of 4), each the sum of its parts [splits][n] in order
@@ -152,7 +140,7 @@ hipError_t act_bwd(const ActBwd& a, hipStream_t stream) {
                        reinterpret_cast<const T*>(a.pre), a.N, a.F, a.act, reinterpret_cast<T*>(a.dz), a.db ? a.sums : nullptr);
     if (a.db) {
         const int C = a.act == SA_ACT_SWIGLU ? 2 * a.F : a.F;
-        const dim3 g((unsigned)cdiv(C, 32));
+        const dim3 g((unsigned)cdiv(C, vec::kSumColumns));
         if (a.db_bf16)
             hipLaunchKernelGGL(bias_sum_kernel<uint16_t>, g, dim3(kThreads), 0, stream, a.sums, (int)parts, C,
                                reinterpret_cast<uint16_t*>(a.db));

@@ -22,7 +22,9 @@ struct Product {
     int32_t splits = 1, per = 0x7fffffff;
 };
 bool product_supported(const Product& p);
-hipError_t launch_product(const Product& p, hipStream_t stream, int shape);
+// the splits that take least time, the sum of their results included, for plain fp32 results
+void choose_splits(Product* p);
+hipError_t launch_product(const Product& p, hipStream_t stream);
 
 }  // namespace linear
 }  // namespace sa

@@ -503,11 +503,67 @@ bool product_supported(const Product& p) {
            cdiv(p.M, 64) * cdiv(p.N, 64) * p.splits < (int64_t(1) << 24);
 }
 
-int product_shapes() { return 6; }
+namespace {
 
-hipError_t launch_product(const Product& p, hipStream_t stream, int shape) {
+// Tile shapes: rows, columns, microseconds a slab of 64 k takes a compute unit at best, where its
+// workgroups wait for one slab after the other, and microseconds of writing a tile's results.
+// Measured on 8192 x 8192 x 8192, 40,000 x 1,024 x 4,096 and, for the waiting, 16 to 1,000 x 1,024 x 1,024.
+struct Shape {
+    int bm, bn;
+    double busy, alone, results;
+    bool rows_ok;   // takes an A that is contiguous along its rows
+};
+constexpr Shape kShapes[] = {{256, 256, 1.79, 1.56, 5.0, true}, {192, 256, 1.36, 1.28, 3.7, false},
+                             {128, 256, 1.02, 0.88, 2.5, true}, {256, 128, 1.02, 0.88, 2.5, true},
+                             {128, 128, 0.52, 0.76, 1.2, true}, {64, 64, 0.31, 0.52, 0.4, true}};
+constexpr int kNumShapes = sizeof(kShapes) / sizeof(kShapes[0]);
+
+// estimated time of a product: what the compute unit with the most tiles takes
+double estimate(const Product& p, const Shape& t) {
+    const int32_t slabs = (int32_t)std::min<int64_t>(p.per, cdiv(p.K, GBK));
+    const int64_t n = cdiv(cdiv(p.M, t.bm) * cdiv(p.N, t.bn) * p.splits, device_cus());
+    return std::max(n * t.busy, t.alone) * slabs + n * t.results;
+}
+int choose(const Product& p, double* time) {
+    int best = -1;
+    for (int i = 0; i < kNumShapes; ++i) {
+        if (p.a_k != 1 && !kShapes[i].rows_ok) continue;
+        const double e = estimate(p, kShapes[i]);
+        if (best < 0 || e < *time) {
+            best = i;
+            *time = e;
+        }
+    }
+    return best;
+}
+
+}  // namespace
+
+void choose_splits(Product* p) {
+    const int32_t slabs = (int32_t)cdiv(p->K, GBK);
+    double least = 0;
+    int32_t splits = 1, per = slabs;
+    for (int32_t s = 1; s <= 16 && s * 4 <= std::max(slabs, 4); ++s) {
+        p->per = (int32_t)cdiv(slabs, s);
+        p->splits = (int32_t)cdiv(slabs, p->per);
+        double e = 0;
+        choose(*p, &e);
+        // the parts written and added up, from what is behind the L2
+        if (p->splits > 1) e += 4.0 + p->splits * (double)p->M * p->N * 8 / 8e6;
+        if (s == 1 || e < least) {
+            least = e;
+            splits = p->splits;
+            per = p->per;
+        }
+    }
+    p->splits = splits;
+    p->per = per;
+}
+
+hipError_t launch_product(const Product& p, hipStream_t stream) {
     if (!product_supported(p)) return hipErrorInvalidValue;
-    switch (shape) {
+    double time = 0;
+    switch (choose(p, &time)) {
         case 0: return launch_t<256, 256, 2, 4, 2>(p, stream);
         case 1: return launch_t<192, 256, 2, 4, 2>(p, stream);
         case 2: return launch_t<128, 256, 2, 4, 3>(p, stream);

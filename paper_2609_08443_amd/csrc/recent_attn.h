@@ -39,6 +39,21 @@ struct Plan {
     int64_t tiles;
     int32_t min_units;        // fewest units a workgroup takes
 };
+// The index of the last of n + 1 ascending values, the first of them 0, that is at most x, but not the n-th: by
+// a whole wave, 64 of them at a time.
+__device__ inline int64_t last_at_most(const int64_t* v, int64_t n, int64_t x) {
+    const int lane = threadIdx.x & 63;
+    int64_t lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const uint64_t le = __builtin_amdgcn_ballot_w64(at < hi && v[at < hi ? at : lo] <= x);
+        const int64_t i = lo + (63 - __builtin_clzll(le | 1)) * step;
+        hi = i + step < hi ? i + step : hi;
+        lo = i;
+    }
+    return ((int64_t)__builtin_amdgcn_readfirstlane((int32_t)(lo >> 32)) << 32) |
+           (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)lo);
+}
 
 // The whole work is hk times the tiles' units, key head by key head, in equal pieces.
 __device__ inline int64_t pieces(const Plan& p, int32_t hk, int64_t grid, int64_t* total) {
@@ -49,15 +64,7 @@ __device__ inline int64_t pieces(const Plan& p, int32_t hk, int64_t grid, int64_
 }
 
 // the last tile that begins at or before a key head's unit
-__device__ inline int64_t tile_at(const Plan& p, int64_t unit) {
-    int64_t lo = 0, hi = p.tiles;
-    while (hi - lo > 1) {
-        const int64_t m = (lo + hi) / 2;
-        if (p.prefix[m] <= unit) lo = m;
-        else hi = m;
-    }
-    return lo;
-}
+__device__ inline int64_t tile_at(const Plan& p, int64_t unit) { return last_at_most(p.prefix, p.tiles, unit); }
 
 struct User {
     int64_t t0, tok0;   // first target, first token
@@ -319,9 +326,11 @@ struct KeysArgs {
     const float *lse, *delta;     // [N,h]
     void *dK, *dV;
     int64_t dk_t, dk_h, dv_t, dv_h;
-    int64_t tiles;                // key_tiles
+    const int64_t* prefix;        // [B + 2] tiles of kKeyTile keys before each user (B: the tokens behind the last one's)
+    int64_t most;                 // key_tiles
 };
-int64_t key_tiles(int64_t B, int64_t T);
+constexpr int kKeyTile = 128;
+int64_t key_tiles(int64_t B, int64_t T);   // no more tiles than this
 hipError_t launch_keys(const KeysArgs& f, bool bf16, int32_t d, hipStream_t stream);
 
 // The whole backward of users with at most fused_rows rows a key head (0: no instance)
@@ -341,7 +350,8 @@ int64_t fused_items(int64_t B, int64_t T, int32_t chunk);
 int64_t fused_slots(int64_t T, int32_t chunk);
 hipError_t launch_fused(const FusedArgs& f, bool bf16, int32_t d, hipStream_t stream);
 
-hipError_t launch_plan(const View& a, const RowsShape& s, int64_t tiles, TileRec* recs, int64_t* prefix,
+// keys: [B + 2], the keys' side's tiles, or null
+hipError_t launch_plan(const View& a, const RowsShape& s, int64_t tiles, TileRec* recs, int64_t* prefix, int64_t* keys,
                        hipStream_t stream);
 hipError_t launch_join(const RowsArgs& f, bool bf16, int32_t d, int32_t bq, bool bwd, hipStream_t stream);
 

@@ -15,10 +15,13 @@ namespace {
 
 constexpr int kPlanThreads = 1024;
 
+// Users' first rows are looked up in LDS where they fit
+constexpr int kUsersInLds = 4096;
+
 // tile t's record and its units
-__device__ int32_t plan_tile(const View& a, int32_t bq, int32_t unit, int64_t t, TileRec* rec) {
+__device__ int32_t plan_tile(const View& a, const int64_t* targets, int32_t bq, int32_t unit, int64_t t, TileRec* rec) {
     int64_t tile0;
-    const int64_t b = user_of_tile(a.targets, a.B, a.N, a.g, bq, t, &tile0);
+    const int64_t b = user_of_tile(targets, a.B, a.N, a.g, bq, t, &tile0);
     const User us = user_at(a, b);
     const int64_t row0 = (t - tile0) * bq, rows = (int64_t)us.n * a.g;
     rec->user = (int32_t)b;
@@ -60,30 +63,46 @@ __device__ inline int64_t scan(int64_t v, int64_t* sums) {
     return v;
 }
 
+// tiles of keys of user b
+__device__ int32_t plan_keys(const View& a, int64_t b) {
+    const User us = user_at(a, b);
+    if (b == a.B) return (int32_t)((a.T - us.tok0 + kKeyTile - 1) / kKeyTile) * (a.skip < 0);
+    return (int64_t)us.n * a.g <= a.skip ? 0 : (us.L + kKeyTile - 1) / kKeyTile;
+}
+
 // Few tiles: records and sums by one workgroup, a thread a tile.  Else every tile's units by the
-// grid first (into prefix[t + 1]), then their sums.
+// grid first (into prefix[t + 1]), then their sums.  A second workgroup of the sums does the keys'.
 enum PlanStep { kAll, kTiles, kSums };
 template <PlanStep STEP>
 __global__ __launch_bounds__(STEP == kTiles ? 256 : kPlanThreads) void plan_kernel(View a, int32_t bq, int32_t unit,
                                                                                     int64_t tiles, TileRec* recs,
-                                                                                    int64_t* prefix) {
+                                                                                    int64_t* prefix, int64_t* keys) {
     if constexpr (STEP == kTiles) {
         const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-        if (t < tiles) prefix[t + 1] = plan_tile(a, bq, unit, t, recs + t);
+        if (t < tiles) prefix[t + 1] = plan_tile(a, a.targets, bq, unit, t, recs + t);
     } else {
         __shared__ int64_t sums[kPlanThreads / 64];
         __shared__ int64_t carry;
+        __shared__ int64_t first[STEP == kAll ? kUsersInLds + 1 : 1];
+        const bool for_keys = blockIdx.x == 1;
+        int64_t* const to = for_keys ? keys : prefix;
+        const int64_t n = for_keys ? a.B + 1 : tiles;
+        const int64_t* targets = a.targets;
+        if (STEP == kAll && !for_keys && a.B <= kUsersInLds) {
+            for (int64_t b = threadIdx.x; b <= a.B; b += kPlanThreads) first[b] = a.targets[b];
+            targets = first;
+        }
         if (threadIdx.x == 0) {
             carry = 0;
-            prefix[0] = 0;
+            to[0] = 0;
         }
         __syncthreads();
-        for (int64_t t0 = 0; t0 < tiles; t0 += kPlanThreads) {
+        for (int64_t t0 = 0; t0 < n; t0 += kPlanThreads) {
             const int64_t t = t0 + threadIdx.x;
             int64_t v = 0;
-            if (t < tiles) v = STEP == kAll ? plan_tile(a, bq, unit, t, recs + t) : prefix[t + 1];
+            if (t < n) v = for_keys ? plan_keys(a, t) : STEP == kAll ? plan_tile(a, targets, bq, unit, t, recs + t) : prefix[t + 1];
             v = scan(v, sums) + carry;
-            if (t < tiles) prefix[t + 1] = v;
+            if (t < n) to[t + 1] = v;
             __syncthreads();
             if (threadIdx.x == kPlanThreads - 1) carry = v;
             __syncthreads();
@@ -91,9 +110,12 @@ __global__ __launch_bounds__(STEP == kTiles ? 256 : kPlanThreads) void plan_kern
     }
 }
 
-// Workgroup w: the tile that piece w's border cuts, if none before cuts it too.
+// Workgroup w: the tile that piece w's border cuts, if none before cuts it too.  Threads take a row's values
+// four at a time, and where there are few rows, every GROUPS-th piece, joined through LDS.
 template <typename T, int D, bool BWD>
 __global__ __launch_bounds__(256) void join_kernel(RowsArgs f, int32_t bq) {
+    constexpr int PER = D / 4;   // threads a row
+    __shared__ float acc[256][5];
     const View& a = f.a;
     int64_t X;
     const int64_t P = pieces(f.p, a.hk, f.grid, &X), W = f.p.prefix[f.p.tiles], w = blockIdx.x + 1;
@@ -101,40 +123,77 @@ __global__ __launch_bounds__(256) void join_kernel(RowsArgs f, int32_t bq) {
     const int64_t at = w * X / P, kv = at / W, tile = tile_at(f.p, at - kv * W);
     const int64_t t0 = kv * W + f.p.prefix[tile], t1 = kv * W + f.p.prefix[tile + 1];
     if (at <= t0 || (w - 1) * X / P > t0) return;
-    int64_t last = w;   // the last piece with a part of it
-    while (last + 1 < P && (last + 1) * X / P < t1) ++last;
+    // the last piece with a part of it: the one that its last unit is in, the largest p with p X <= (t1 - 1) P + P - 1
+    const int64_t last = min(((t1 - 1) * P + P - 1) / X, P - 1);
     const TileRec rec = f.p.recs[tile];
     const User us = user_at(a, rec.user);
     const int32_t rows = min(bq, us.n * a.g - rec.row0);
     const int64_t stride = (int64_t)bq * (D + 2);
     // piece w - 1 began the tile; piece v's part of a tile that it goes on with is at 2 v
-    const float* first = f.parts + (2 * (w - 1) + 1) * stride;
-    for (int32_t x = threadIdx.x; x < rows * (D / 4); x += 256) {
-        const int32_t r = x / (D / 4), d = 4 * (x % (D / 4));
+    const int32_t n = (int32_t)(last - w) + 2;
+    auto part_of = [&](int32_t i) { return f.parts + (i == 0 ? 2 * (w - 1) + 1 : 2 * (w + i - 1)) * stride; };
+    // threads side by side on one row's piece: as many groups of pieces as rows leave room for
+    int32_t groups = 256 / (rows * PER);
+    groups = groups < 1 ? 1 : groups;
+    const int32_t group = rows * PER >= 256 ? 0 : threadIdx.x / (rows * PER);
+    for (int32_t x = rows * PER >= 256 ? threadIdx.x : threadIdx.x % (rows * PER); x < rows * PER; x += 256) {
+        const int32_t r = x / PER, d = 4 * (x % PER);
         const int32_t row = rec.row0 + r;
         const int64_t target = us.t0 + row / a.g;
         const int32_t head = (int32_t)kv * a.g + row % a.g;
         float v[4] = {0.f, 0.f, 0.f, 0.f};
         float m = -__builtin_inff(), l = 0.f;
+        const bool in = group < groups;
+        if (groups == 1 && !in) return;
         if constexpr (!BWD) {
-            m = first[bq * D + r];
-            for (int64_t p = w; p <= last; ++p) m = fmaxf(m, f.parts[2 * p * stride + bq * D + r]);
+            if (in) {
+#pragma unroll 4
+                for (int32_t i = group; i < n; i += groups) m = fmaxf(m, part_of(i)[bq * D + r]);
+            }
         }
         const float ms = m == -__builtin_inff() ? 0.f : m;
-        auto add = [&](const float* part) {
-            const float4 o = *reinterpret_cast<const float4*>(part + r * D + d);
-            float fac = 1.f;
-            if constexpr (!BWD) {
-                fac = exp2_(part[bq * D + r] - ms);
-                l = __builtin_fmaf(part[bq * D + bq + r], fac, l);
+        if (in) {
+#pragma unroll 4
+            for (int32_t i = group; i < n; i += groups) {
+                const float* part = part_of(i);
+                const float4 o = *reinterpret_cast<const float4*>(part + r * D + d);
+                float fac = 1.f;
+                if constexpr (!BWD) {
+                    fac = exp2_(part[bq * D + r] - ms);
+                    l = __builtin_fmaf(part[bq * D + bq + r], fac, l);
+                }
+                v[0] = __builtin_fmaf(o.x, fac, v[0]);
+                v[1] = __builtin_fmaf(o.y, fac, v[1]);
+                v[2] = __builtin_fmaf(o.z, fac, v[2]);
+                v[3] = __builtin_fmaf(o.w, fac, v[3]);
             }
-            v[0] = __builtin_fmaf(o.x, fac, v[0]);
-            v[1] = __builtin_fmaf(o.y, fac, v[1]);
-            v[2] = __builtin_fmaf(o.z, fac, v[2]);
-            v[3] = __builtin_fmaf(o.w, fac, v[3]);
-        };
-        add(first);
-        for (int64_t p = w; p <= last; ++p) add(f.parts + 2 * p * stride);
+        }
+        if (groups > 1) {   // (all threads come here once)
+            float* mine = acc[threadIdx.x];
+            __shared__ float tops[256];
+            tops[threadIdx.x] = m;
+            __syncthreads();
+            float top = m;
+            if constexpr (!BWD) {
+                for (int32_t g = 0; g < groups; ++g) top = fmaxf(top, tops[g * rows * PER + x]);
+            }
+            const float fac = BWD || m == -__builtin_inff() ? (BWD ? 1.f : 0.f) : exp2_(m - top);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mine[e] = v[e] * fac;
+            mine[4] = l * fac;
+            __syncthreads();
+            if (group != 0) return;
+            m = top;
+            l = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = 0.f;
+            for (int32_t g = 0; g < groups; ++g) {
+                const float* o = acc[g * rows * PER + x];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += o[e];
+                l += o[4];
+            }
+        }
         const float inv = BWD ? a.scale : l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] *= inv;
@@ -155,14 +214,15 @@ hipError_t launch_join_t(const RowsArgs& f, int32_t bq, bool bwd, hipStream_t st
 
 }  // namespace
 
-hipError_t launch_plan(const View& a, const RowsShape& s, int64_t tiles, TileRec* recs, int64_t* prefix,
+hipError_t launch_plan(const View& a, const RowsShape& s, int64_t tiles, TileRec* recs, int64_t* prefix, int64_t* keys,
                        hipStream_t stream) {
+    const dim3 one(keys ? 2 : 1);
     if (tiles <= 4 * kPlanThreads) {
-        hipLaunchKernelGGL(plan_kernel<kAll>, dim3(1), dim3(kPlanThreads), 0, stream, a, s.bq, s.unit, tiles, recs, prefix);
+        hipLaunchKernelGGL(plan_kernel<kAll>, one, dim3(kPlanThreads), 0, stream, a, s.bq, s.unit, tiles, recs, prefix, keys);
     } else {
         hipLaunchKernelGGL(plan_kernel<kTiles>, dim3((unsigned)((tiles + 255) / 256)), dim3(256), 0, stream, a, s.bq,
-                           s.unit, tiles, recs, prefix);
-        hipLaunchKernelGGL(plan_kernel<kSums>, dim3(1), dim3(kPlanThreads), 0, stream, a, s.bq, s.unit, tiles, recs, prefix);
+                           s.unit, tiles, recs, prefix, keys);
+        hipLaunchKernelGGL(plan_kernel<kSums>, one, dim3(kPlanThreads), 0, stream, a, s.bq, s.unit, tiles, recs, prefix, keys);
     }
     return hipGetLastError();
 }

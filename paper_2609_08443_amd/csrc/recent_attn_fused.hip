@@ -39,11 +39,17 @@ struct FusedStats {
 // A user's chunks: tokens in 32s, dealt out evenly to as few chunks as hold them.  Chunks of users with
 // several are longer than chunk / 2 - 32 keys, so that their first keys, over that length, number them apart.
 __device__ inline int32_t chunks_of(int32_t L, int32_t chunk) { return (int32_t)(((int64_t)L + chunk - 1) / chunk); }
-__device__ inline int32_t chunk_begin(int32_t L, int32_t n, int32_t i) {
-    const int64_t u = ((int64_t)L + 31) / 32;
-    return (int32_t)min((int64_t)L, 32 * (u * i / n));
-}
-__device__ inline int64_t slot_of(int64_t first, int32_t chunk) { return first / (chunk / 2 - 32); }
+struct Chunks {
+    int32_t n, q, r;   // the first r of n have q + 1 32s, the others q
+    __device__ Chunks(int32_t L, int32_t chunk) {
+        n = chunks_of(L, chunk);
+        const int32_t u = (int32_t)(((int64_t)L + 31) / 32);
+        q = n > 0 ? u / n : 0;
+        r = n > 0 ? u % n : 0;
+    }
+    __device__ int32_t begin(int32_t i, int32_t L) const { return (int32_t)min((int64_t)L, 32 * ((int64_t)q * i + min(i, r))); }
+};
+__device__ inline int64_t slot_of(int64_t first, int32_t chunk) { return (uint32_t)first / (uint32_t)(chunk / 2 - 32); }
 
 // the transposed ds: [32 keys][32 rows] in LDS
 template <typename T>
@@ -102,10 +108,11 @@ __global__ __launch_bounds__(256, (FusedCfg<T, D>::PER_CU)) void fused_kernel(Fu
             us.n = 0;
             us.L = (int32_t)(a.T - us.tok0);
         }
-        const int32_t n_chunks = chunks_of(us.L, f.chunk), ci = (int32_t)(item - item0);
+        const Chunks chunks(us.L, f.chunk);
+        const int32_t n_chunks = chunks.n, ci = (int32_t)(item - item0);
         if (ci >= n_chunks || (int64_t)us.n * a.g > kFusedRows) continue;
         const int32_t rows = us.n * a.g;
-        const int32_t c0 = chunk_begin(us.L, n_chunks, ci), c1 = chunk_begin(us.L, n_chunks, ci + 1);
+        const int32_t c0 = chunks.begin(ci, us.L), c1 = chunks.begin(ci + 1, us.L);
         const int32_t first = (int32_t)us.tok0 + c0, last = (int32_t)us.tok0 + c1;   // the chunk's keys
         const T* Kp = reinterpret_cast<const T*>(a.K) + kv * a.k_h;
         const T* Vp = reinterpret_cast<const T*>(a.V) + kv * a.v_h;
@@ -190,7 +197,9 @@ __global__ __launch_bounds__(256, (FusedCfg<T, D>::PER_CU)) void fused_kernel(Fu
             for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = f32x16{};
             T* const kt = reinterpret_cast<T*>(ring + stage * C::TILE);
             if (rows > 0) {
-                wait_loads<0>();
+                // (the stores of the 32 keys before need not be done)
+                if (k0 == mine) wait_loads<0>();
+                else wait_loads<2 * C::LOADS>();
                 typename M::Frag kf, vf;
                 M::load_tile(kf, kt, lane);
                 M::load_tile(vf, vt, lane);
@@ -334,30 +343,32 @@ __global__ __launch_bounds__(256, (FusedCfg<T, D>::PER_CU)) void fused_kernel(Fu
     }
 }
 
-// dq of users with several chunks, or none
+// dq of users with several chunks, or none; a workgroup takes 256 / (D / 4) rows
 template <typename T, int D>
 __global__ __launch_bounds__(256) void fused_sum_kernel(FusedArgs f) {
     const View& a = f.a;
-    constexpr int kFusedRows = FusedCfg<T, D>::kFusedRows;
-    for (int64_t v = blockIdx.x; v < (a.B + 1) * a.hk; v += gridDim.x) {
-        const int64_t b = v / a.hk;
-        const int32_t kv = (int32_t)(v % a.hk);
+    constexpr int kFusedRows = FusedCfg<T, D>::kFusedRows, AT_ONCE = 256 / (D / 4);
+    constexpr int PARTS = kFusedRows / AT_ONCE;
+    for (int64_t v = blockIdx.x; v < (a.B + 1) * a.hk * PARTS; v += gridDim.x) {
+        const int64_t b = v / (a.hk * PARTS);
+        const int32_t kv = (int32_t)(v / PARTS % a.hk), part = (int32_t)(v % PARTS);
         const User us = user_at(a, b);
         const int64_t rows = (int64_t)us.n * a.g;
-        const int32_t n = b < a.B ? chunks_of(us.L, f.chunk) : 0;
-        if (n == 1 || (rows > kFusedRows && n > 0)) continue;
-        for (int64_t x = threadIdx.x; x < rows * (D / 4); x += 256) {
-            const int64_t r = x / (D / 4);
-            const int32_t d = 4 * (int32_t)(x % (D / 4));
+        const Chunks chunks(b < a.B ? us.L : 0, f.chunk);
+        if (chunks.n == 1 || (rows > kFusedRows && chunks.n > 0)) continue;
+        // (rows without chunks: any number of them)
+        for (int64_t r = part * AT_ONCE + threadIdx.x / (D / 4); r < rows; r += kFusedRows) {
+            const int32_t d = 4 * (threadIdx.x % (D / 4));
             const int64_t target = us.t0 + r / a.g;
             const int32_t head = kv * a.g + (int32_t)(r % a.g);
             int32_t lo, hi;
             seen(a, us, target, &lo, &hi);
             float y[4] = {0.f, 0.f, 0.f, 0.f};
             if (hi > lo) {
-                for (int32_t i = 0; i < n; ++i) {
-                    const int64_t first = us.tok0 + chunk_begin(us.L, n, i);
-                    const float4 p = *reinterpret_cast<const float4*>(f.parts + ((slot_of(first, f.chunk) * a.hk + kv) * kFusedRows + r) * D + d);
+#pragma unroll 4
+                for (int32_t i = 0; i < chunks.n; ++i) {
+                    const int64_t slot = slot_of(us.tok0 + chunks.begin(i, us.L), f.chunk);
+                    const float4 p = *reinterpret_cast<const float4*>(f.parts + ((slot * a.hk + kv) * kFusedRows + r) * D + d);
                     y[0] += p.x;
                     y[1] += p.y;
                     y[2] += p.z;
@@ -377,7 +388,8 @@ hipError_t launch_fused_t(const FusedArgs& f, hipStream_t stream) {
     if (f.a.T > 0)
         hipLaunchKernelGGL((fused_kernel<T, D>), dim3((unsigned)std::min(f.items * f.a.hk, most)), dim3(256), 0, stream, f);
     if (f.a.N > 0)
-        hipLaunchKernelGGL((fused_sum_kernel<T, D>), dim3((unsigned)std::min((f.a.B + 1) * f.a.hk, most)), dim3(256), 0, stream, f);
+        hipLaunchKernelGGL((fused_sum_kernel<T, D>),
+                           dim3((unsigned)std::min((f.a.B + 1) * f.a.hk * (FusedCfg<T, D>::kFusedRows * (D / 4) / 256), most)), dim3(256), 0, stream, f);
     return hipGetLastError();
 }
 
@@ -390,7 +402,7 @@ int32_t fused_rows(bool bf16, int32_t d) {
 int32_t fused_chunk(int64_t B, int64_t T, int32_t hk) {
     // enough chunks for the compute units, and few enough that their rows cost little
     const int64_t want = T * hk / (4 * (int64_t)device_cus());
-    return (int32_t)std::min<int64_t>(2048, std::max<int64_t>(256, want / 128 * 128));
+    return (int32_t)std::min<int64_t>(1152, std::max<int64_t>(256, want / 128 * 128));
 }
 int64_t fused_items(int64_t B, int64_t T, int32_t chunk) { return T / chunk + B + 1; }
 int64_t fused_slots(int64_t T, int32_t chunk) { return T / (chunk / 2 - 32) + 1; }

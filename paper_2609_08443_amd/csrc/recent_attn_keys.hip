@@ -5,6 +5,8 @@
 // key's scores in its own two lanes, from where p = exp(s - lse) goes into dV^T += dout^T p and
 // ds = p (dP - delta), times the cap's derivative, into dK^T += q^T ds.  Every sum is one
 // workgroup's, in the rows' order: nothing is added up in memory.
+#include <algorithm>
+
 #include "recent_attn.h"
 
 namespace sa {
@@ -12,7 +14,7 @@ namespace attn {
 
 namespace {
 
-constexpr int kKeys = 128, kRows = 32;
+constexpr int kKeys = kKeyTile, kRows = 32;
 
 template <typename T, int D>
 struct KeysCfg {
@@ -38,18 +40,17 @@ __global__ __launch_bounds__(256, (KeysCfg<T, D>::PER_CU)) void keys_kernel(Keys
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hl = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const float inv_cap = a.cap > 0.f ? a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e, to_exp = 2.f * kLog2e * inv_cap;
-    for (int64_t v = blockIdx.x; v < f.tiles * a.hk; v += gridDim.x) {
-        const int64_t id = xcd_range(v, f.tiles * a.hk), tile = id / a.hk;
+    const int64_t total = f.prefix[a.B + 1] * a.hk;
+    for (int64_t v = blockIdx.x; v < total; v += gridDim.x) {
+        const int64_t id = xcd_range(v, total), tile = id / a.hk;
         const int32_t kv = (int32_t)(id % a.hk);
-        int64_t tile0;
-        const int64_t b = user_of_tile_wave(a.offsets, a.B, a.T, 1, kKeys, tile, &tile0);
+        const int64_t b = last_at_most(f.prefix, a.B + 1, tile);
         User us = user_at(a, b);
         if (b == a.B) {   // tokens behind the last user's
             us.n = 0;
             us.L = (int32_t)(a.T - us.tok0);
         }
-        const int64_t first = (tile - tile0) * kKeys;
-        if (first >= us.L || (int64_t)us.n * a.g <= a.skip) continue;
+        const int64_t first = (tile - f.prefix[b]) * kKeys;
         const int32_t nk = (int32_t)min((int64_t)kKeys, us.L - first);
         const int64_t key0 = us.tok0 + first + 32 * w;   // the wave's first
         const int32_t mine = nk - 32 * w;                // how many it has
@@ -228,8 +229,8 @@ __global__ __launch_bounds__(256, (KeysCfg<T, D>::PER_CU)) void keys_kernel(Keys
 
 template <typename T, int D>
 hipError_t launch_keys_t(const KeysArgs& f, hipStream_t stream) {
-    const int64_t most = int64_t(1) << 22, n = f.tiles * f.a.hk;
-    hipLaunchKernelGGL((keys_kernel<T, D>), dim3((unsigned)(n < most ? n : most)), dim3(256), 0, stream, f);
+    const int64_t n = std::min(f.most * f.a.hk, (int64_t)device_cus() * KeysCfg<T, D>::PER_CU * 4);
+    hipLaunchKernelGGL((keys_kernel<T, D>), dim3((unsigned)n), dim3(256), 0, stream, f);
     return hipGetLastError();
 }
 

@@ -59,5 +59,39 @@ __device__ inline void store(T* p, int c, int D, const float* v) {
     }
 }
 
+// Column sums of parts [n][C] fp32, in a fixed order: workgroup b does columns 16 b .. 16 b + 15, four threads
+// side by side and 64 groups of them down the parts, whose sums are added up through LDS.  put(column, sum).
+constexpr int kSumColumns = 16;
+template <typename F>
+__device__ inline void sum_parts(const float* __restrict__ parts, int n, int64_t C, F put) {
+    __shared__ float acc[64][kSumColumns + 1];
+    const int64_t c = (int64_t)blockIdx.x * kSumColumns + 4 * (threadIdx.x & 3);
+    const int group = threadIdx.x >> 2;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if (c + 4 <= C && C % 4 == 0) {
+#pragma unroll 8
+        for (int i = group; i < n; i += 64) {
+            const float4 x = *reinterpret_cast<const float4*>(parts + i * C + c);
+            s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
+        }
+    } else {
+#pragma unroll 4
+        for (int i = group; i < n; i += 64)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < C) s[e] += parts[i * C + c + e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[group][4 * (threadIdx.x & 3) + e] = s[e];
+    __syncthreads();
+    // 16 threads a column, four groups each, then across them
+    const int col = threadIdx.x >> 4, g = threadIdx.x & 15;
+    float v = (acc[g][col] + acc[g + 16][col]) + (acc[g + 32][col] + acc[g + 48][col]);
+#pragma unroll
+    for (int o = 1; o < 16; o *= 2) v += __shfl_xor(v, o, 64);
+    const int64_t to = (int64_t)blockIdx.x * kSumColumns + col;
+    if (g == 0 && to < C) put(to, v);
+}
+
 }  // namespace vec
 }  // namespace sa

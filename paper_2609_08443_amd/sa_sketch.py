@@ -11,7 +11,10 @@ import ctypes
 import functools
 import math
 import os
+import struct
 from typing import Any, NamedTuple, Optional, Tuple
+
+import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsa_sketch.so")
@@ -49,22 +52,10 @@ class SAError(RuntimeError):
         super().__init__(f"{self.status_name}: {detail}")
 
 
-class _RecentAttn(ctypes.Structure):
-    """sa_recent_attn"""
-    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "K", "V")]
-                + [(n, ctypes.c_int64) for n in ("q_stride", "q_head_stride", "k_stride", "k_head_stride", "v_stride",
-                                                 "v_head_stride")]
-                + [(n, ctypes.c_void_p) for n in ("offsets", "targets", "ends", "slopes")]
-                + [(n, ctypes.c_int64) for n in ("B", "T", "N")]
-                + [(n, ctypes.c_int32) for n in ("h", "hk", "d", "window")]
-                + [("scale", ctypes.c_float), ("cap", ctypes.c_float), ("dtype", ctypes.c_int)])
-
-
-class _RecentAttnGrads(ctypes.Structure):
-    """sa_recent_attn_grads"""
-    _fields_ = ([(n, ctypes.c_void_p) for n in ("dq", "dK", "dV")]
-                + [(n, ctypes.c_int64) for n in ("dq_stride", "dq_head_stride", "dk_stride", "dk_head_stride", "dv_stride",
-                                                 "dv_head_stride")])
+# sa_recent_attn and sa_recent_attn_grads: three pointers, six strides; the first goes on with offsets, targets, ends
+# and slopes, B, T and N, h, hk, d and window, scale and cap, dtype
+_RECENT_ATTN = struct.Struct("3P6q4P3q4i2fi4x")
+_RECENT_ATTN_GRADS = struct.Struct("3P6q")
 
 
 _lib = None
@@ -150,13 +141,12 @@ def lib() -> ctypes.CDLL:
     L.sa_stca_cached_fwd.restype = c.c_int
     L.sa_stca_cached_bwd.argtypes = cached + [vp, vp, vp, vp, vp, c.c_int, vp, sz, vp]
     L.sa_stca_cached_bwd.restype = c.c_int
-    recent = c.POINTER(_RecentAttn)
     for nm in ("sa_recent_attn_fwd_workspace_size", "sa_recent_attn_bwd_workspace_size"):
-        getattr(L, nm).argtypes = [recent]
+        getattr(L, nm).argtypes = [vp]
         getattr(L, nm).restype = sz
-    L.sa_recent_attn_fwd.argtypes = [recent, vp, vp, vp, sz, vp]
+    L.sa_recent_attn_fwd.argtypes = [vp, vp, vp, vp, sz, vp]
     L.sa_recent_attn_fwd.restype = c.c_int
-    L.sa_recent_attn_bwd.argtypes = [recent, vp, vp, vp, c.POINTER(_RecentAttnGrads), vp, sz, vp]
+    L.sa_recent_attn_bwd.argtypes = [vp, vp, vp, vp, vp, vp, sz, vp]
     L.sa_recent_attn_bwd.restype = c.c_int
     L.sa_layer_norm_fwd.argtypes = [vp, i64, vp, vp, i64, i32, f32, c.c_int, vp, vp, vp]
     L.sa_layer_norm_fwd.restype = c.c_int
@@ -191,7 +181,6 @@ def _check(rc: int):
 
 
 def _dtype_code(t) -> int:
-    import torch
     if t.dtype == torch.bfloat16:
         return SA_BF16
     if t.dtype == torch.float32:
@@ -204,7 +193,6 @@ def _ptr(t) -> Optional[int]:
 
 
 def _stream_handle(stream) -> Optional[int]:
-    import torch
     if stream is None:
         stream = torch.cuda.current_stream()
     return stream.cuda_stream or None
@@ -234,7 +222,6 @@ def fwd_chunk_tokens(B, T, H, M, d, dtype_code) -> int:
 
 
 def _workspace(nbytes, device, workspace):
-    import torch
     if nbytes == 0:
         return None, 0
     if workspace is None:
@@ -247,7 +234,6 @@ def _workspace(nbytes, device, workspace):
 def sketch_fwd(K, V, P, offsets, scale: Optional[float] = None, sketch=None, lse=None,
                want_lse: bool = True, workspace=None, stream=None):
     """sa_sketch_fwd on torch tensors.  Returns (sketch [B,H,M,d] fp32, lse [T,H] or None)."""
-    import torch
     T, H, d = K.shape
     M = P.shape[1]
     B = offsets.shape[0] - 1
@@ -282,7 +268,6 @@ def sketch_fwd_noalloc(K, V, P, offsets, scale: Optional[float] = None, sketch=N
     """sa_sketch_fwd_noalloc on torch tensors: the library's own device scratch
     array instead of a workspace.  The caller passes (or this allocates, before the
     call) the outputs.  Returns (sketch, lse or None)."""
-    import torch
     T, H, d = K.shape
     M = P.shape[1]
     B = offsets.shape[0] - 1
@@ -315,7 +300,6 @@ def sketch_fwd_tokenwise(K, V, P, offsets, scale: Optional[float] = None, sketch
                          want_lse: bool = True, workspace=None, stream=None):
     """sa_sketch_fwd_tokenwise on torch tensors (weights normalised over each user's
     tokens per prototype).  Returns (sketch [B,H,M,d] fp32, lse_m [B,H,M] or None)."""
-    import torch
     T, H, d = K.shape
     M = P.shape[1]
     B = offsets.shape[0] - 1
@@ -345,7 +329,6 @@ def sketch_fwd_tokenwise(K, V, P, offsets, scale: Optional[float] = None, sketch
 def sketch_bwd(K, V, P, offsets, dsketch, lse, scale: Optional[float] = None, dK=None,
                dV=None, dP=None, workspace=None, stream=None) -> Tuple:
     """sa_sketch_bwd on torch tensors.  dsketch: [B,R,H,M,d].  Returns (dK, dV, dP)."""
-    import torch
     T, H, d = K.shape
     M = P.shape[1]
     B = offsets.shape[0] - 1
@@ -383,7 +366,6 @@ def layer_bwd_workspace_size(B, T, H, M, d, dtype_code, R) -> int:
 
 
 def _layer_inputs(X, P, Wq, Wk, offsets):
-    import torch
     T, H, d = X.shape
     M = P.shape[1]
     B = offsets.shape[0] - 1
@@ -400,7 +382,6 @@ def layer_fwd(X, P, Wq, Wk, offsets, scale: Optional[float] = None, sketch=None,
               want_lse: bool = True, workspace=None, stream=None):
     """sa_layer_fwd on torch tensors: one SA layer with its projections (K = X W_K,
     Q = P W_Q, the history X aggregated).  Returns (sketch [B,H,M,d] fp32, lse [T,H] or None)."""
-    import torch
     B, T, H, M, d, dev, code = _layer_inputs(X, P, Wq, Wk, offsets)
     if scale is None:
         scale = 1.0 / math.sqrt(d)
@@ -422,7 +403,6 @@ def layer_fwd(X, P, Wq, Wk, offsets, scale: Optional[float] = None, sketch=None,
 def layer_bwd(X, P, Wq, Wk, offsets, dsketch, lse, scale: Optional[float] = None, workspace=None,
               stream=None) -> Tuple:
     """sa_layer_bwd on torch tensors.  dsketch: [B,R,H,M,d].  Returns (dX, dP, dWq, dWk), fp32."""
-    import torch
     B, T, H, M, d, dev, code = _layer_inputs(X, P, Wq, Wk, offsets)
     R = dsketch.shape[1]
     _require(dsketch, "dsketch", (B, R, H, M, d), torch.float32, dev)
@@ -452,7 +432,6 @@ def block_saved_size(B, T, H, M, d, n_layers, dtype_code) -> int:
 def block_saved_buffer(X, P, Wq, offsets):
     """A device buffer for the training forward's intermediates (sa_block_fwd's
     `saved`), sized for these inputs."""
-    import torch
     T, H, d = X.shape
     n = block_saved_size(offsets.shape[0] - 1, T, H, P.shape[1], d, Wq.shape[0], _dtype_code(X))
     return torch.empty(max(n, 1), dtype=torch.uint8, device=X.device)
@@ -466,7 +445,6 @@ def block_saved_views(saved, B, T, H, M, d, n_layers, dtype_code) -> list:
     dict per layer: "Q" and "Pp" [B,H,M,d] (fp32, and the input dtype for P'),
     "lse" [T,H], and "state" [B,H,M,d] for layers after the first.  The first
     layer's Q and P' are [H,M,d] (the shared prototypes' queries)."""
-    import torch
     out = []
     el_dt = torch.bfloat16 if dtype_code == SA_BF16 else torch.float32
     for l in range(n_layers):
@@ -505,7 +483,6 @@ def block_fwd(X, P, Wq, Wk, ln, W1, W3, W2, offsets, scale: Optional[float] = No
     """sa_block_fwd on torch tensors: stacked SA with len(Wq) layers.
     With `saved` (from block_saved_buffer) the intermediates are kept there for
     block_bwd.  Returns (out [B,H,M,d] fp32, lse [n_layers,T,H] or None)."""
-    import torch
     T, H, d = X.shape
     M = P.shape[1]
     B = offsets.shape[0] - 1
@@ -548,7 +525,6 @@ def block_bwd(X, P, Wq, Wk, ln, W1, W3, W2, offsets, dout, scale: Optional[float
     forward is then not replayed), or None.
     Returns a dict of fp32 tensors dX, dP, dWq, dWk, dln, dW1, dW3, dW2 (shapes of
     the inputs)."""
-    import torch
     T, H, d = X.shape
     M = P.shape[1]
     B = offsets.shape[0] - 1
@@ -593,7 +569,6 @@ def stca_bwd_workspace_size(B, R, k, D, h, dtype_code) -> int:
 
 
 def _stca_check(Xs, q, Wq, Wk, Wv):
-    import torch
     B, k, D = Xs.shape
     R = q.shape[1]
     dev, dt = Xs.device, Xs.dtype
@@ -659,7 +634,6 @@ def cache_slot_bytes(k: int, D: int, fmt: str) -> int:
 
 def sketch_cache(n_slots: int, k: int, D: int, fmt: str = "fp8", device="cuda") -> SketchCache:
     """An empty cache of n_slots slots on `device`."""
-    import torch
     nbytes = cache_slot_bytes(k, D, fmt)
     if nbytes == 0:
         raise SAError(1, lib().sa_last_error().decode())
@@ -675,7 +649,6 @@ def _cache_format(fmt) -> int:
 
 def _cache_args(cache: SketchCache, slots):
     """(device, format code, n_slots, B) of a cache and the slots of a batch."""
-    import torch
     code = _cache_format(cache.fmt)
     dev = cache.data.device
     if dev.type != "cuda":
@@ -700,7 +673,6 @@ def _on_device(workspace, device):
 def _on(device, stream):
     """The tensors' device and, where given, the caller's stream as the current ones, so
     that what a call allocates belongs to the stream that it runs on."""
-    import torch
     if stream is not None:
         if stream.device != device:
             raise SAError(1, f"the stream is on {stream.device}, the tensors on {device}")
@@ -724,7 +696,6 @@ _AS_IT_IS = _AsItIs()
 def _handle(device, stream) -> Optional[int]:
     """The stream's handle; of the device's current stream without making an object of it
     (0.2 us instead of 2.7, of calls of ten)."""
-    import torch
     if stream is not None:
         return stream.cuda_stream or None
     return torch._C._cuda_getCurrentRawStream(device.index) or None
@@ -733,7 +704,6 @@ def _handle(device, stream) -> Optional[int]:
 def cache_write(cache: SketchCache, Xs, slots, rows=None, stream=None) -> None:
     """sa_cache_write on torch tensors: sketches Xs [B,k,D] (bf16 or fp32) into the slots
     [B] int64 of the cache; rows [B] int32 are their valid rows (None: all k)."""
-    import torch
     dev, fmt, n_slots, B = _cache_args(cache, slots)
     code = _dtype_code(Xs)
     _require(Xs, "Xs", (B, cache.k, cache.D), Xs.dtype, dev)
@@ -748,7 +718,6 @@ def cache_write(cache: SketchCache, Xs, slots, rows=None, stream=None) -> None:
 def cache_read(cache: SketchCache, slots, dtype=None, out=None, stream=None):
     """sa_cache_read on torch tensors: [B,k,D] in `dtype` (or out's; bf16 by default) of
     the slots [B], zeros past each one's rows and for slots outside the cache."""
-    import torch
     dev, fmt, n_slots, B = _cache_args(cache, slots)
     if dtype is None:
         dtype = torch.bfloat16 if out is None else out.dtype
@@ -786,7 +755,6 @@ def stca_cached_fwd(cache: SketchCache, slots, q, Wq, Wk, Wv, h: int, scale: Opt
     """sa_stca_cached_fwd on torch tensors: stca_fwd with each user's sketch read from its
     slot [B] int64 of the cache.  Returns (out [B,R,D] in out_dtype (or out's; fp32 by
     default), lse [B,R,h] or None)."""
-    import torch
     dev, fmt, n_slots, B, R, code = _cached_check(cache, slots, q, Wq, Wk, Wv)
     k, D = cache.k, cache.D
     if h < 1:
@@ -813,7 +781,6 @@ def stca_cached_bwd(cache: SketchCache, slots, q, Wq, Wk, Wv, h: int, dout, scal
                     workspace=None, stream=None):
     """sa_stca_cached_bwd on torch tensors: dict of the gradients dq, dWq, dWk, dWv in
     dout's dtype (the cached sketches are constants)."""
-    import torch
     dev, fmt, n_slots, B, R, code = _cached_check(cache, slots, q, Wq, Wk, Wv)
     k, D = cache.k, cache.D
     _require(dout, "dout", (B, R, D), dout.dtype, dev)
@@ -835,49 +802,89 @@ def stca_cached_bwd(cache: SketchCache, slots, q, Wq, Wk, Wv, h: int, dout, scal
     return g
 
 
+def _is(t, name, shape, dtype, device):
+    """_require, with its reasons looked for only where something is wrong (calls of ten
+    microseconds check eight tensors)."""
+    if t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
+        _require(t, name, shape, dtype, device)
+
+
+_DTYPE_CODES = {torch.bfloat16: SA_BF16, torch.float32: SA_FP32}
+
+
+def _gpu_code(t, name):
+    """The dtype code of a tensor on a GPU, and its device."""
+    dev = t.device
+    if dev.type != "cuda":
+        raise SAError(1, f"{name} is on {dev}, expected a GPU")
+    code = _DTYPE_CODES.get(t.dtype)
+    return (_dtype_code(t) if code is None else code), dev
+
+
+@functools.lru_cache(maxsize=4096)
+def _bytes_of(name, device_index, *args) -> int:
+    """A workspace's size; the library's answer depends on the sizes and the device."""
+    return int(getattr(lib(), name)(*args))
+
+
+def _buffer(nbytes, device, workspace):
+    """A call's workspace: the caller's, or one of its own."""
+    if workspace is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    _workspace(nbytes, device, _on_device(workspace, device))
+    return workspace
+
+
+def _bytes_given(ws) -> int:
+    return 0 if ws is None else ws.numel() * ws.element_size()
+
+
 def _heads_view(t, name, shape, dtype, device):
     """(elements from row to row, from head to head) of a [rows, heads, d] tensor whose heads
     may lie in wider rows, as slices of one projection do."""
-    if t.shape != tuple(shape):
-        raise SAError(1, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.dtype != dtype:
-        raise SAError(1, f"{name} has dtype {t.dtype}, expected {dtype}")
-    if t.device != device:
-        raise SAError(1, f"{name} is on {t.device}, expected {device}")
-    n, heads, d = shape
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
+        raise SAError(1, f"{name} is {tuple(t.shape)} {t.dtype} on {t.device}, expected {tuple(shape)} {dtype} on {device}")
     row, head, one = t.stride()
-    if one != 1 and d > 1:
+    if one != 1 and shape[2] > 1:
         raise SAError(1, f"{name}: the values of a head must lie together")
     # (strides along dimensions of one say nothing)
-    return (row if n > 1 else 0), (head if heads > 1 else 0)
+    return (row if shape[0] > 1 else 0), (head if shape[1] > 1 else 0)
 
 
 def _recent_args(q, K, V, offsets, targets, ends, window, slopes, scale, cap):
-    """(device, the call's sa_recent_attn) of a batch."""
-    import torch
-    dev, dt = q.device, q.dtype
-    if dev.type != "cuda":
-        raise SAError(1, f"q is on {dev}, expected a GPU")
+    """(device, sizes, the call's sa_recent_attn as bytes) of a batch."""
     if q.dim() != 3 or K.dim() != 3:
         raise SAError(1, f"q and K have shapes {tuple(q.shape)} and {tuple(K.shape)}, expected [N, h, d] and [T, hk, d]")
+    code, dev = _gpu_code(q, "q")
+    dt = q.dtype
     N, h, d = q.shape
-    T, hk = K.shape[:2]
-    code = _dtype_code(q)
-    strides = (*_heads_view(q, "q", (N, h, d), dt, dev), *_heads_view(K, "K", (T, hk, d), dt, dev),
-               *_heads_view(V, "V", (T, hk, d), dt, dev))
+    T, hk, _ = K.shape
+    sq, sk, sv = (_heads_view(q, "q", (N, h, d), dt, dev), _heads_view(K, "K", (T, hk, d), dt, dev),
+                  _heads_view(V, "V", (T, hk, d), dt, dev))
     if offsets.dim() != 1 or offsets.shape[0] < 1:
         raise SAError(1, f"offsets has shape {tuple(offsets.shape)}, expected [B + 1]")
     B = offsets.shape[0] - 1
-    _require(offsets, "offsets", (B + 1,), torch.int64, dev)
-    _require(targets, "targets", (B + 1,), torch.int64, dev)
+    _is(offsets, "offsets", (B + 1,), torch.int64, dev)
+    _is(targets, "targets", (B + 1,), torch.int64, dev)
     if ends is not None:
-        _require(ends, "ends", (N,), torch.int32, dev)
+        _is(ends, "ends", (N,), torch.int32, dev)
     if slopes is not None:
-        _require(slopes, "slopes", (h,), torch.float32, dev)
+        _is(slopes, "slopes", (h,), torch.float32, dev)
     if scale is None:
-        scale = 1.0 / math.sqrt(max(d, 1))
-    return dev, _RecentAttn(_ptr(q), _ptr(K), _ptr(V), *strides, _ptr(offsets), _ptr(targets), _ptr(ends), _ptr(slopes),
-                            B, T, N, h, hk, d, window, scale, cap, code)
+        scale = d ** -0.5 if d else 1.0
+    try:
+        args = _RECENT_ATTN.pack(q.data_ptr(), K.data_ptr(), V.data_ptr(), *sq, *sk, *sv, offsets.data_ptr(),
+                                 targets.data_ptr(), 0 if ends is None else ends.data_ptr(),
+                                 0 if slopes is None else slopes.data_ptr(), B, T, N, h, hk, d, window, scale, cap, code)
+    except (struct.error, OverflowError) as e:
+        raise SAError(1, f"window, scale or cap: {e}") from None
+    return dev, (B, T, N, h, hk, d, code), args
+
+
+def _recent_bytes(name, dev, sizes) -> int:
+    B, T, N, h, hk, d, code = sizes
+    return _bytes_of(name, dev.index, _RECENT_ATTN.pack(0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, B, T, N, h, hk, d, 0, 1.0, 0.0,
+                                                        code))
 
 
 def recent_attn_fwd(q, K, V, offsets, targets, ends=None, window: int = 0, slopes=None, scale: Optional[float] = None,
@@ -887,15 +894,16 @@ def recent_attn_fwd(q, K, V, offsets, targets, ends=None, window: int = 0, slope
     `offsets` [B+1] say; `ends` [N] int32 and `window` limit what a target sees, `slopes` [h]
     prefer nearer tokens, `cap` bounds the scores.  Returns (out [N,h,d] in q's dtype, lse
     [N,h] fp32 or None)."""
-    import torch
-    dev, a = _recent_args(q, K, V, offsets, targets, ends, window, slopes, scale, cap)
+    dev, sizes, args = _recent_args(q, K, V, offsets, targets, ends, window, slopes, scale, cap)
+    N, h, d = sizes[2], sizes[3], sizes[5]
     with _on(dev, stream):
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-        _require(out, "out", q.shape, q.dtype, dev)
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=dev) if want_lse else None
-        ws, nbytes = _workspace(int(lib().sa_recent_attn_fwd_workspace_size(a)), dev, _on_device(workspace, dev))
-        rc = lib().sa_recent_attn_fwd(a, _ptr(out), _ptr(lse), _ptr(ws), nbytes, _handle(dev, stream))
+            out = torch.empty((N, h, d), dtype=q.dtype, device=dev)
+        else:
+            _is(out, "out", (N, h, d), q.dtype, dev)
+        lse = torch.empty((N, h), dtype=torch.float32, device=dev) if want_lse else None
+        ws = _buffer(_recent_bytes("sa_recent_attn_fwd_workspace_size", dev, sizes), dev, workspace)
+        rc = _lib.sa_recent_attn_fwd(args, out.data_ptr(), _ptr(lse), _ptr(ws), _bytes_given(ws), _handle(dev, stream))
     _check(rc)
     return out, lse
 
@@ -905,31 +913,31 @@ def recent_attn_bwd(q, K, V, offsets, targets, out, lse, dout, ends=None, window
                     stream=None):
     """sa_recent_attn_bwd on torch tensors: dict of the gradients dq, dK, dV in q's dtype, from
     the forward's out and lse.  dq, dK and dV may be given, as views of wider rows too."""
-    import torch
-    dev, a = _recent_args(q, K, V, offsets, targets, ends, window, slopes, scale, cap)
-    _require(out, "out", q.shape, q.dtype, dev)
-    _require(dout, "dout", q.shape, q.dtype, dev)
-    _require(lse, "lse", q.shape[:2], torch.float32, dev)
+    dev, sizes, args = _recent_args(q, K, V, offsets, targets, ends, window, slopes, scale, cap)
+    _, T, N, h, hk, d, _ = sizes
+    dt = q.dtype
+    _is(out, "out", (N, h, d), dt, dev)
+    _is(dout, "dout", (N, h, d), dt, dev)
+    _is(lse, "lse", (N, h), torch.float32, dev)
     with _on(dev, stream):
-        g, strides = {}, []
-        for name, t, like in (("dq", dq, q), ("dK", dK, K), ("dV", dV, V)):
-            g[name] = torch.empty(like.shape, dtype=q.dtype, device=dev) if t is None else t
-            strides += _heads_view(g[name], name, like.shape, q.dtype, dev)
-        ws, nbytes = _workspace(int(lib().sa_recent_attn_bwd_workspace_size(a)), dev, _on_device(workspace, dev))
-        rc = lib().sa_recent_attn_bwd(a, _ptr(out), _ptr(lse), _ptr(dout),
-                                      _RecentAttnGrads(_ptr(g["dq"]), _ptr(g["dK"]), _ptr(g["dV"]), *strides), _ptr(ws),
-                                      nbytes, _handle(dev, stream))
+        dq = torch.empty((N, h, d), dtype=dt, device=dev) if dq is None else dq
+        dK = torch.empty((T, hk, d), dtype=dt, device=dev) if dK is None else dK
+        dV = torch.empty((T, hk, d), dtype=dt, device=dev) if dV is None else dV
+        grads = _RECENT_ATTN_GRADS.pack(dq.data_ptr(), dK.data_ptr(), dV.data_ptr(), *_heads_view(dq, "dq", (N, h, d), dt, dev),
+                                        *_heads_view(dK, "dK", (T, hk, d), dt, dev),
+                                        *_heads_view(dV, "dV", (T, hk, d), dt, dev))
+        ws = _buffer(_recent_bytes("sa_recent_attn_bwd_workspace_size", dev, sizes), dev, workspace)
+        rc = _lib.sa_recent_attn_bwd(args, out.data_ptr(), lse.data_ptr(), dout.data_ptr(), grads, _ptr(ws), _bytes_given(ws),
+                                     _handle(dev, stream))
     _check(rc)
-    return g
+    return {"dq": dq, "dK": dK, "dV": dV}
 
 
-def _rows_view(t, name, width=None):
+def _rows_view(t, name):
     """(rows, width, elements from row to row) of a [rows, width] tensor whose rows may lie in
     wider ones."""
-    if t.dim() != 2 or (width is not None and t.shape[1] != width):
-        raise SAError(1, f"{name} has shape {tuple(t.shape)}, expected [rows, {'width' if width is None else width}]")
-    if t.device.type != "cuda":
-        raise SAError(1, f"{name} is on {t.device}, expected a GPU")
+    if t.dim() != 2:
+        raise SAError(1, f"{name} has shape {tuple(t.shape)}, expected [rows, width]")
     n, D = t.shape
     row, one = t.stride()
     if one != 1 and D > 1:
@@ -941,19 +949,19 @@ def layer_norm_fwd(x, gamma, beta, eps: float = 1e-5, y=None, want_stats: bool =
     """sa_layer_norm_fwd on torch tensors: rows x [N,D] (a view of wider rows is fine) with
     weights gamma, beta [D].  Returns (y [N,D], stats [N,2] fp32: mean and 1 / sqrt(var + eps),
     or None)."""
-    import torch
     N, D, ld = _rows_view(x, "x")
-    dev, dt = x.device, x.dtype
-    code = _dtype_code(x)
-    _require(gamma, "gamma", (D,), dt, dev)
-    _require(beta, "beta", (D,), dt, dev)
+    code, dev = _gpu_code(x, "x")
+    dt = x.dtype
+    _is(gamma, "gamma", (D,), dt, dev)
+    _is(beta, "beta", (D,), dt, dev)
     with _on(dev, stream):
         if y is None:
             y = torch.empty((N, D), dtype=dt, device=dev)
-        _require(y, "y", (N, D), dt, dev)
+        else:
+            _is(y, "y", (N, D), dt, dev)
         stats = torch.empty((N, 2), dtype=torch.float32, device=dev) if want_stats else None
-        rc = lib().sa_layer_norm_fwd(_ptr(x), ld, _ptr(gamma), _ptr(beta), N, D, float(eps), code, _ptr(y), _ptr(stats),
-                                     _handle(dev, stream))
+        rc = lib().sa_layer_norm_fwd(x.data_ptr(), ld, gamma.data_ptr(), beta.data_ptr(), N, D, eps, code, y.data_ptr(),
+                                     _ptr(stats), _handle(dev, stream))
     _check(rc)
     return y, stats
 
@@ -961,40 +969,40 @@ def layer_norm_fwd(x, gamma, beta, eps: float = 1e-5, y=None, want_stats: bool =
 def layer_norm_bwd(x, gamma, stats, dy, dx=None, workspace=None, stream=None):
     """sa_layer_norm_bwd on torch tensors: dict of dx [N,D] in x's dtype and dgamma, dbeta [D]
     fp32, from the forward's stats."""
-    import torch
     N, D, ld = _rows_view(x, "x")
-    dev, dt = x.device, x.dtype
-    code = _dtype_code(x)
-    _require(gamma, "gamma", (D,), dt, dev)
-    _require(stats, "stats", (N, 2), torch.float32, dev)
-    _require(dy, "dy", (N, D), dt, dev)
+    code, dev = _gpu_code(x, "x")
+    dt = x.dtype
+    _is(gamma, "gamma", (D,), dt, dev)
+    _is(stats, "stats", (N, 2), torch.float32, dev)
+    _is(dy, "dy", (N, D), dt, dev)
     with _on(dev, stream):
-        g = {"dx": torch.empty((N, D), dtype=dt, device=dev) if dx is None else dx,
-             "dgamma": torch.empty(D, dtype=torch.float32, device=dev),
-             "dbeta": torch.empty(D, dtype=torch.float32, device=dev)}
-        _require(g["dx"], "dx", (N, D), dt, dev)
-        ws, nbytes = _workspace(int(lib().sa_layer_norm_bwd_workspace_size(N, D, code)), dev, _on_device(workspace, dev))
-        rc = lib().sa_layer_norm_bwd(_ptr(x), ld, _ptr(gamma), _ptr(stats), _ptr(dy), N, D, code, _ptr(g["dx"]),
-                                     _ptr(g["dgamma"]), _ptr(g["dbeta"]), _ptr(ws), nbytes, _handle(dev, stream))
+        if dx is None:
+            dx = torch.empty((N, D), dtype=dt, device=dev)
+        else:
+            _is(dx, "dx", (N, D), dt, dev)
+        dgamma = torch.empty(D, dtype=torch.float32, device=dev)
+        dbeta = torch.empty(D, dtype=torch.float32, device=dev)
+        ws = _buffer(_bytes_of("sa_layer_norm_bwd_workspace_size", dev.index, N, D, code), dev, workspace)
+        rc = _lib.sa_layer_norm_bwd(x.data_ptr(), ld, gamma.data_ptr(), stats.data_ptr(), dy.data_ptr(), N, D, code,
+                                    dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), _ptr(ws), _bytes_given(ws),
+                                    _handle(dev, stream))
     _check(rc)
-    return g
-
-
-def _activation(act) -> int:
-    if act not in ACTIVATIONS:
-        raise SAError(1, f"activation {act!r}, expected one of {tuple(ACTIVATIONS)}")
-    return ACTIVATIONS[act]
+    return {"dx": dx, "dgamma": dgamma, "dbeta": dbeta}
 
 
 def _linear_args(x, W, act):
     """(N, K, F, x's row stride, W's columns, activation, dtype code, device) of a linear layer."""
     N, K, ld = _rows_view(x, "x")
-    code = _activation(act)
-    if W.dim() != 2 or (act == "swiglu" and W.shape[1] % 2):
-        raise SAError(1, f"W has shape {tuple(W.shape)}, expected [{K}, {'2 F' if act == 'swiglu' else 'F'}]")
+    acode = ACTIVATIONS.get(act)
+    if acode is None:
+        raise SAError(1, f"activation {act!r}, expected one of {tuple(ACTIVATIONS)}")
+    code, dev = _gpu_code(x, "x")
+    gated = act == "swiglu"
+    if W.dim() != 2 or (gated and W.shape[1] % 2):
+        raise SAError(1, f"W has shape {tuple(W.shape)}, expected [{K}, {'2 F' if gated else 'F'}]")
     C = W.shape[1]
-    _require(W, "W", (K, C), x.dtype, x.device)
-    return N, K, C // 2 if act == "swiglu" else C, ld, C, code, _dtype_code(x), x.device
+    _is(W, "W", (K, C), x.dtype, dev)
+    return N, K, C // 2 if gated else C, ld, C, acode, code, dev
 
 
 def linear_fwd(x, W, bias=None, act: str = "none", residual=None, y=None, want_pre: bool = False, workspace=None,
@@ -1002,21 +1010,21 @@ def linear_fwd(x, W, bias=None, act: str = "none", residual=None, y=None, want_p
     """sa_linear_fwd on torch tensors: y = act(x W + bias) + residual, x [N,K] (a view of wider
     rows is fine), W [K,F], or [K,2F] for act "swiglu" (the gated half first).  Returns (y [N,F],
     pre [N, W's columns], what the backward needs of an activation, or None)."""
-    import torch
     N, K, F, ld, C, acode, code, dev = _linear_args(x, W, act)
     dt = x.dtype
     if bias is not None:
-        _require(bias, "bias", (C,), dt, dev)
+        _is(bias, "bias", (C,), dt, dev)
     if residual is not None:
-        _require(residual, "residual", (N, F), dt, dev)
+        _is(residual, "residual", (N, F), dt, dev)
     with _on(dev, stream):
         if y is None:
             y = torch.empty((N, F), dtype=dt, device=dev)
-        _require(y, "y", (N, F), dt, dev)
+        else:
+            _is(y, "y", (N, F), dt, dev)
         pre = torch.empty((N, C), dtype=dt, device=dev) if want_pre else None
-        ws, nbytes = _workspace(int(lib().sa_linear_fwd_workspace_size(N, K, F, acode, code)), dev, _on_device(workspace, dev))
-        rc = lib().sa_linear_fwd(_ptr(x), ld, _ptr(W), _ptr(bias), _ptr(residual), N, K, F, acode, code, _ptr(y), _ptr(pre),
-                                 _ptr(ws), nbytes, _handle(dev, stream))
+        ws = _buffer(_bytes_of("sa_linear_fwd_workspace_size", dev.index, N, K, F, acode, code), dev, workspace)
+        rc = _lib.sa_linear_fwd(x.data_ptr(), ld, W.data_ptr(), _ptr(bias), _ptr(residual), N, K, F, acode, code, y.data_ptr(),
+                                _ptr(pre), _ptr(ws), _bytes_given(ws), _handle(dev, stream))
     _check(rc)
     return y, pre
 
@@ -1025,22 +1033,24 @@ def linear_bwd(x, W, dy, bias: bool = False, act: str = "none", pre=None, weight
     """sa_linear_bwd on torch tensors: dict of the gradients dx [N,K] in x's dtype, dW and, with
     bias, db in weight_dtype (x's by default), from the forward's `pre` (act "none" needs none).
     The residual's gradient is dy."""
-    import torch
     N, K, F, ld, C, acode, code, dev = _linear_args(x, W, act)
     dt = x.dtype
-    _require(dy, "dy", (N, F), dt, dev)
-    if act != "none":
-        if pre is None:
-            raise SAError(1, f"activation {act!r} needs the forward's pre")
-        _require(pre, "pre", (N, C), dt, dev)
+    _is(dy, "dy", (N, F), dt, dev)
+    if act == "none":
+        pre = None
+    elif pre is None:
+        raise SAError(1, f"activation {act!r} needs the forward's pre")
+    else:
+        _is(pre, "pre", (N, C), dt, dev)
     with _on(dev, stream):
-        wdt = dict(dtype=dt if weight_dtype is None else weight_dtype, device=dev)
-        g = {"dx": torch.empty((N, K), dtype=dt, device=dev), "dW": torch.empty((K, C), **wdt)}
+        wdt = dt if weight_dtype is None else weight_dtype
+        g = {"dx": torch.empty((N, K), dtype=dt, device=dev), "dW": torch.empty((K, C), dtype=wdt, device=dev)}
         if bias:
-            g["db"] = torch.empty(C, **wdt)
-        ws, nbytes = _workspace(int(lib().sa_linear_bwd_workspace_size(N, K, F, acode, code)), dev, _on_device(workspace, dev))
-        rc = lib().sa_linear_bwd(_ptr(x), ld, _ptr(W), _ptr(pre), _ptr(dy), N, K, F, acode, code, _ptr(g["dx"]), _ptr(g["dW"]),
-                                 _ptr(g.get("db")), _dtype_code(g["dW"]), _ptr(ws), nbytes, _handle(dev, stream))
+            g["db"] = torch.empty(C, dtype=wdt, device=dev)
+        ws = _buffer(_bytes_of("sa_linear_bwd_workspace_size", dev.index, N, K, F, acode, code), dev, workspace)
+        rc = _lib.sa_linear_bwd(x.data_ptr(), ld, W.data_ptr(), _ptr(pre), dy.data_ptr(), N, K, F, acode, code,
+                                g["dx"].data_ptr(), g["dW"].data_ptr(), _ptr(g.get("db")), _dtype_code(g["dW"]), _ptr(ws),
+                                _bytes_given(ws), _handle(dev, stream))
     _check(rc)
     return g
 
@@ -1054,7 +1064,6 @@ def gemm_bf16(A, a_strides, B, b_strides, C, c_strides, M, N, K, batch, alpha=1.
     """sa_gemm_bf16 on torch tensors: A, B bf16 and C (fp32 or bf16) device
     tensors addressed by (z, row, col) element strides a_strides = (a_z, a_m, a_k),
     b_strides = (b_z, b_k, b_n), c_strides = (c_z, c_m).  Returns C."""
-    import torch
     for name, t in (("A", A), ("B", B)):
         if t.dtype != torch.bfloat16 or not t.is_cuda:
             raise SAError(1, f"{name} must be a bf16 device tensor")
@@ -1091,7 +1100,6 @@ def kernel_times(max_kernels: int = 32) -> dict:
 def build_worklist(offsets, T: int, H: int, chunk_tokens: int, max_items: Optional[int] = None,
                    stream=None):
     """sa_build_worklist: returns the items as an int32 tensor [n_items, 8] on the device."""
-    import torch
     B = offsets.shape[0] - 1
     if max_items is None:
         max_items = (H * T + chunk_tokens - 1) // chunk_tokens + H * B
