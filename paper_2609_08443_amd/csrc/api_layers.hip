@@ -27,7 +27,8 @@ struct AttnPlan {
     sa::attn::RowsShape shape;
     int64_t tiles = 0;
     int32_t grid = 1;
-    size_t off_recs = 0, off_prefix = 0, off_keys = 0, off_parts = 0, off_delta = 0, total = 0;
+    bool plan_inline = false;
+    size_t off_recs = 0, off_prefix = 0, off_keys = 0, off_begun = 0, off_parts = 0, off_delta = 0, total = 0;
 };
 
 AttnPlan plan_attn(const sa_recent_attn& a, bool bwd) {
@@ -61,9 +62,14 @@ AttnPlan plan_attn(const sa_recent_attn& a, bool bwd) {
             return p;
         }
     }
+    // few tiles: the kernel plans for itself, a launch less, where that is quick (a thread goes over the ends of a
+    // tile's targets)
+    p.plan_inline = !bwd && p.tiles <= sa::attn::kInlineTiles && (!a.ends || a.N <= 4 * a.B);
+    // (room for the plan either way: the size goes by sizes alone)
     p.off_recs = carve(sizeof(sa::attn::TileRec) * (size_t)p.tiles);
     p.off_prefix = carve(sizeof(int64_t) * ((size_t)p.tiles + 1));
     p.off_parts = carve(sizeof(float) * 2 * (size_t)p.grid * p.shape.bq * (a.d + 2));
+    p.off_begun = carve(sizeof(sa::attn::Begun) * (size_t)p.grid);
     if (bwd) p.off_keys = carve(sizeof(int64_t) * ((size_t)a.B + 2));
     if (bwd) p.off_delta = carve(sizeof(float) * (size_t)a.N * a.h);
     p.total = off;
@@ -127,15 +133,17 @@ sa::attn::RowsArgs rows_args(const sa::attn::View& v, const AttnPlan& p, uint8_t
     sa::attn::RowsArgs f{};
     f.a = v;
     f.p = {reinterpret_cast<const sa::attn::TileRec*>(ws + p.off_recs), reinterpret_cast<const int64_t*>(ws + p.off_prefix),
-           p.tiles, 1};
+           p.tiles, p.shape.bq, p.shape.unit};
     f.parts = reinterpret_cast<float*>(ws + p.off_parts);
+    f.begun = reinterpret_cast<sa::attn::Begun*>(ws + p.off_begun);
+    f.plan_inline = p.plan_inline;
     f.grid = p.grid;
     return f;
 }
 
 hipError_t run_plan(const sa::attn::RowsArgs& f, const AttnPlan& p, bool bwd, uint8_t* ws, hipStream_t stream) {
     sa::ProfScope ps("recent_attn_plan", stream);
-    return sa::attn::launch_plan(f.a, p.shape, p.tiles, reinterpret_cast<sa::attn::TileRec*>(ws + p.off_recs),
+    return sa::attn::launch_plan(f.a, f.p, reinterpret_cast<sa::attn::TileRec*>(ws + p.off_recs),
                                  reinterpret_cast<int64_t*>(ws + p.off_prefix),
                                  bwd ? reinterpret_cast<int64_t*>(ws + p.off_keys) : nullptr, stream);
 }
@@ -148,7 +156,7 @@ hipError_t run_rows(const sa::attn::RowsArgs& f, const AttnPlan& p, const sa_rec
     }
     if (e == hipSuccess) {
         sa::ProfScope ps("recent_attn_join", stream);
-        e = sa::attn::launch_join(f, bf, a.d, p.shape.bq, bwd, stream);
+        e = sa::attn::launch_join(f, bf, a.d, bwd, stream);
     }
     return e;
 }
@@ -411,7 +419,7 @@ sa_status sa_recent_attn_fwd(const sa_recent_attn* a, void* out, float* lse, voi
     sa::attn::RowsArgs f = rows_args(v, p, ws);
     f.out = out;
     f.lse = lse;
-    hipError_t e = run_plan(f, p, false, ws, stream);
+    hipError_t e = p.plan_inline ? hipSuccess : run_plan(f, p, false, ws, stream);
     if (e == hipSuccess) e = run_rows(f, p, *a, false, stream);
     if (e != hipSuccess) return hip_fail(e, "recent attention launch");
     return SA_OK;

@@ -37,8 +37,26 @@ struct Plan {
     const TileRec* recs;      // [tiles]
     const int64_t* prefix;    // [tiles + 1] units before each tile (at least one a tile with rows)
     int64_t tiles;
-    int32_t min_units;        // fewest units a workgroup takes
+    int32_t bq, unit;         // rows of a tile, keys of a unit
 };
+// Few tiles: every workgroup of the kernel makes the plan for itself, in LDS
+constexpr int kInlineTiles = 512;
+struct InlinePlan {
+    TileRec recs[kInlineTiles];
+    int64_t prefix[kInlineTiles + 1];
+    int64_t sums[4];
+};
+// A piece that begins a tile and does not end it: what the join has to know
+struct Begun {
+    int64_t t0;             // the user's first target
+    int32_t n, kv;          // pieces of the tile (0: nothing begun), its key head
+    int32_t row0, rows;     // its first row, and how many
+};
+// A value that all lanes have, in scalar registers
+__device__ inline int32_t uniform(int32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ inline int64_t uniform(int64_t v) {
+    return ((int64_t)uniform((int32_t)(v >> 32)) << 32) | (uint32_t)uniform((int32_t)v);
+}
 // The index of the last of n + 1 ascending values, the first of them 0, that is at most x, but not the n-th: by
 // a whole wave, 64 of them at a time.
 __device__ inline int64_t last_at_most(const int64_t* v, int64_t n, int64_t x) {
@@ -51,16 +69,14 @@ __device__ inline int64_t last_at_most(const int64_t* v, int64_t n, int64_t x) {
         hi = i + step < hi ? i + step : hi;
         lo = i;
     }
-    return ((int64_t)__builtin_amdgcn_readfirstlane((int32_t)(lo >> 32)) << 32) |
-           (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)lo);
+    return uniform(lo);
 }
 
 // The whole work is hk times the tiles' units, key head by key head, in equal pieces.
 __device__ inline int64_t pieces(const Plan& p, int32_t hk, int64_t grid, int64_t* total) {
-    const int64_t X = p.prefix[p.tiles] * hk;
+    const int64_t X = uniform(p.prefix[p.tiles]) * hk;
     *total = X;
-    const int64_t most = X / p.min_units;
-    return most < 1 ? 1 : most < grid ? most : grid;
+    return X < 1 ? 1 : X < grid ? X : grid;
 }
 
 // the last tile that begins at or before a key head's unit
@@ -112,7 +128,7 @@ __device__ inline int64_t user_of_tile_wave(const int64_t* first, int64_t B, int
         hi = n + step < hi ? n + step : hi;
         lo = n;
     }
-    lo = ((int64_t)__builtin_amdgcn_readfirstlane((int32_t)(lo >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)lo);
+    lo = uniform(lo);
     *tile0 = first_tile(first, lo, most, per, size);
     return lo;
 }
@@ -135,6 +151,36 @@ __device__ inline float swap_halves(float v, float (*f)(float, float)) {
 }
 __device__ inline float add_(float a, float b) { return a + b; }
 __device__ inline float max_(float a, float b) { return fmaxf(a, b); }
+
+// Tile t's record and its units; `targets` are a.targets or a copy of them
+__device__ inline int32_t plan_tile(const View& a, const int64_t* targets, int32_t bq, int32_t unit, int64_t t, TileRec* rec) {
+    int64_t tile0;
+    const int64_t b = user_of_tile(targets, a.B, a.N, a.g, bq, t, &tile0);
+    const User us = user_at(a, b);
+    const int64_t row0 = (t - tile0) * bq, rows = (int64_t)us.n * a.g;
+    rec->user = (int32_t)b;
+    rec->row0 = (int32_t)row0;
+    rec->klo = rec->khi = (int32_t)us.tok0;
+    if (row0 >= rows || rows <= a.skip) return 0;
+    int32_t lo = us.L, hi = 0;
+    if (!a.ends) {
+        seen(a, us, 0, &lo, &hi);
+    } else {
+        const int64_t i1 = us.t0 + (min(row0 + bq, rows) - 1) / a.g;
+        for (int64_t i = us.t0 + row0 / a.g; i <= i1; ++i) {
+            int32_t l, h;
+            seen(a, us, i, &l, &h);
+            if (h > l) {
+                lo = min(lo, l);
+                hi = max(hi, h);
+            }
+        }
+    }
+    if (hi <= lo) return 1;
+    rec->klo += lo;
+    rec->khi += hi;
+    return (hi - lo + unit - 1) / unit;
+}
 
 // Products of a 32-row tile in LDS, [32][D] of T, 16-byte chunks swizzled within each row, with
 // operands that hold 32 columns one a lane (l % 32; k over the halves).
@@ -310,7 +356,9 @@ struct RowsArgs {
     float* delta;            // backward: <dout, out> of every row, written
     int64_t dq_t, dq_h;
     float* parts;            // [2 grid][bq][d + 2]: results of pieces that are not whole tiles
+    Begun* begun;            // [grid]
     int32_t grid;
+    bool plan_inline;        // p.recs and p.prefix are the kernel's own
 };
 struct RowsShape {
     int32_t bq, unit, per_cu;   // rows of a tile, keys of a unit, workgroups a CU holds
@@ -351,9 +399,8 @@ int64_t fused_slots(int64_t T, int32_t chunk);
 hipError_t launch_fused(const FusedArgs& f, bool bf16, int32_t d, hipStream_t stream);
 
 // keys: [B + 2], the keys' side's tiles, or null
-hipError_t launch_plan(const View& a, const RowsShape& s, int64_t tiles, TileRec* recs, int64_t* prefix, int64_t* keys,
-                       hipStream_t stream);
-hipError_t launch_join(const RowsArgs& f, bool bf16, int32_t d, int32_t bq, bool bwd, hipStream_t stream);
+hipError_t launch_plan(const View& a, const Plan& p, TileRec* recs, int64_t* prefix, int64_t* keys, hipStream_t stream);
+hipError_t launch_join(const RowsArgs& f, bool bf16, int32_t d, bool bwd, hipStream_t stream);
 
 }  // namespace attn
 }  // namespace sa

@@ -18,36 +18,6 @@ constexpr int kPlanThreads = 1024;
 // Users' first rows are looked up in LDS where they fit
 constexpr int kUsersInLds = 4096;
 
-// tile t's record and its units
-__device__ int32_t plan_tile(const View& a, const int64_t* targets, int32_t bq, int32_t unit, int64_t t, TileRec* rec) {
-    int64_t tile0;
-    const int64_t b = user_of_tile(targets, a.B, a.N, a.g, bq, t, &tile0);
-    const User us = user_at(a, b);
-    const int64_t row0 = (t - tile0) * bq, rows = (int64_t)us.n * a.g;
-    rec->user = (int32_t)b;
-    rec->row0 = (int32_t)row0;
-    rec->klo = rec->khi = (int32_t)us.tok0;
-    if (row0 >= rows || rows <= a.skip) return 0;
-    int32_t lo = us.L, hi = 0;
-    if (!a.ends) {
-        seen(a, us, 0, &lo, &hi);
-    } else {
-        const int64_t i1 = us.t0 + (min(row0 + bq, rows) - 1) / a.g;
-        for (int64_t i = us.t0 + row0 / a.g; i <= i1; ++i) {
-            int32_t l, h;
-            seen(a, us, i, &l, &h);
-            if (h > l) {
-                lo = min(lo, l);
-                hi = max(hi, h);
-            }
-        }
-    }
-    if (hi <= lo) return 1;
-    rec->klo += lo;
-    rec->khi += hi;
-    return (hi - lo + unit - 1) / unit;
-}
-
 // Inclusive sums over the workgroup's threads
 __device__ inline int64_t scan(int64_t v, int64_t* sums) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -110,37 +80,30 @@ __global__ __launch_bounds__(STEP == kTiles ? 256 : kPlanThreads) void plan_kern
     }
 }
 
-// Workgroup w: the tile that piece w's border cuts, if none before cuts it too.  Threads take a row's values
-// four at a time, and where there are few rows, every GROUPS-th piece, joined through LDS.
+// Workgroup w: the tile that piece w began and others went on with.  Threads take a row's values
+// four at a time, and where there are few rows, every `groups`-th piece, joined through LDS.
 template <typename T, int D, bool BWD>
-__global__ __launch_bounds__(256) void join_kernel(RowsArgs f, int32_t bq) {
+__global__ __launch_bounds__(256) void join_kernel(RowsArgs f) {
     constexpr int PER = D / 4;   // threads a row
     __shared__ float acc[256][5];
     const View& a = f.a;
-    int64_t X;
-    const int64_t P = pieces(f.p, a.hk, f.grid, &X), W = f.p.prefix[f.p.tiles], w = blockIdx.x + 1;
-    if (w >= P) return;
-    const int64_t at = w * X / P, kv = at / W, tile = tile_at(f.p, at - kv * W);
-    const int64_t t0 = kv * W + f.p.prefix[tile], t1 = kv * W + f.p.prefix[tile + 1];
-    if (at <= t0 || (w - 1) * X / P > t0) return;
-    // the last piece with a part of it: the one that its last unit is in, the largest p with p X <= (t1 - 1) P + P - 1
-    const int64_t last = min(((t1 - 1) * P + P - 1) / X, P - 1);
-    const TileRec rec = f.p.recs[tile];
-    const User us = user_at(a, rec.user);
-    const int32_t rows = min(bq, us.n * a.g - rec.row0);
+    const int32_t bq = f.p.bq;
+    const int64_t w = blockIdx.x;
+    const Begun tile = f.begun[w];
+    const int32_t n = tile.n, rows = tile.rows;
+    if (n < 2) return;
     const int64_t stride = (int64_t)bq * (D + 2);
-    // piece w - 1 began the tile; piece v's part of a tile that it goes on with is at 2 v
-    const int32_t n = (int32_t)(last - w) + 2;
-    auto part_of = [&](int32_t i) { return f.parts + (i == 0 ? 2 * (w - 1) + 1 : 2 * (w + i - 1)) * stride; };
+    // what piece w began is at 2 w + 1; piece v's part of a tile that it goes on with at 2 v
+    auto part_of = [&](int32_t i) { return f.parts + (i == 0 ? 2 * w + 1 : 2 * (w + i)) * stride; };
     // threads side by side on one row's piece: as many groups of pieces as rows leave room for
     int32_t groups = 256 / (rows * PER);
     groups = groups < 1 ? 1 : groups;
     const int32_t group = rows * PER >= 256 ? 0 : threadIdx.x / (rows * PER);
     for (int32_t x = rows * PER >= 256 ? threadIdx.x : threadIdx.x % (rows * PER); x < rows * PER; x += 256) {
         const int32_t r = x / PER, d = 4 * (x % PER);
-        const int32_t row = rec.row0 + r;
-        const int64_t target = us.t0 + row / a.g;
-        const int32_t head = (int32_t)kv * a.g + row % a.g;
+        const int32_t row = tile.row0 + r;
+        const int64_t target = tile.t0 + row / a.g;
+        const int32_t head = tile.kv * a.g + row % a.g;
         float v[4] = {0.f, 0.f, 0.f, 0.f};
         float m = -__builtin_inff(), l = 0.f;
         const bool in = group < groups;
@@ -205,32 +168,32 @@ __global__ __launch_bounds__(256) void join_kernel(RowsArgs f, int32_t bq) {
 }
 
 template <typename T, int D>
-hipError_t launch_join_t(const RowsArgs& f, int32_t bq, bool bwd, hipStream_t stream) {
+hipError_t launch_join_t(const RowsArgs& f, bool bwd, hipStream_t stream) {
     const dim3 grid((unsigned)(f.grid - 1));
-    if (bwd) hipLaunchKernelGGL((join_kernel<T, D, true>), grid, dim3(256), 0, stream, f, bq);
-    else hipLaunchKernelGGL((join_kernel<T, D, false>), grid, dim3(256), 0, stream, f, bq);
+    if (bwd) hipLaunchKernelGGL((join_kernel<T, D, true>), grid, dim3(256), 0, stream, f);
+    else hipLaunchKernelGGL((join_kernel<T, D, false>), grid, dim3(256), 0, stream, f);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_plan(const View& a, const RowsShape& s, int64_t tiles, TileRec* recs, int64_t* prefix, int64_t* keys,
-                       hipStream_t stream) {
+hipError_t launch_plan(const View& a, const Plan& p, TileRec* recs, int64_t* prefix, int64_t* keys, hipStream_t stream) {
     const dim3 one(keys ? 2 : 1);
+    const int64_t tiles = p.tiles;
     if (tiles <= 4 * kPlanThreads) {
-        hipLaunchKernelGGL(plan_kernel<kAll>, one, dim3(kPlanThreads), 0, stream, a, s.bq, s.unit, tiles, recs, prefix, keys);
+        hipLaunchKernelGGL(plan_kernel<kAll>, one, dim3(kPlanThreads), 0, stream, a, p.bq, p.unit, tiles, recs, prefix, keys);
     } else {
-        hipLaunchKernelGGL(plan_kernel<kTiles>, dim3((unsigned)((tiles + 255) / 256)), dim3(256), 0, stream, a, s.bq,
-                           s.unit, tiles, recs, prefix, keys);
-        hipLaunchKernelGGL(plan_kernel<kSums>, one, dim3(kPlanThreads), 0, stream, a, s.bq, s.unit, tiles, recs, prefix, keys);
+        hipLaunchKernelGGL(plan_kernel<kTiles>, dim3((unsigned)((tiles + 255) / 256)), dim3(256), 0, stream, a, p.bq,
+                           p.unit, tiles, recs, prefix, keys);
+        hipLaunchKernelGGL(plan_kernel<kSums>, one, dim3(kPlanThreads), 0, stream, a, p.bq, p.unit, tiles, recs, prefix, keys);
     }
     return hipGetLastError();
 }
 
-hipError_t launch_join(const RowsArgs& f, bool bf16, int32_t d, int32_t bq, bool bwd, hipStream_t stream) {
+hipError_t launch_join(const RowsArgs& f, bool bf16, int32_t d, bool bwd, hipStream_t stream) {
     if (f.grid < 2) return hipSuccess;
-    if (bf16) return d == 64 ? launch_join_t<uint16_t, 64>(f, bq, bwd, stream) : launch_join_t<uint16_t, 128>(f, bq, bwd, stream);
-    return d == 64 ? launch_join_t<float, 64>(f, bq, bwd, stream) : launch_join_t<float, 128>(f, bq, bwd, stream);
+    if (bf16) return d == 64 ? launch_join_t<uint16_t, 64>(f, bwd, stream) : launch_join_t<uint16_t, 128>(f, bwd, stream);
+    return d == 64 ? launch_join_t<float, 64>(f, bwd, stream) : launch_join_t<float, 128>(f, bwd, stream);
 }
 
 }  // namespace attn

@@ -19,7 +19,7 @@ template <typename T, int D, bool WIDE, bool BWD>
 struct RowsCfg {
     static constexpr int EL = sizeof(T);
     static constexpr int BQ = WIDE ? 128 : 32;
-    static constexpr int NT = WIDE && EL == 2 ? 2 : 1;   // tiles of 32 keys a wave takes at a time
+    static constexpr int NT = WIDE && EL == 2 && !BWD ? 2 : 1;   // tiles of 32 keys a wave takes at a time
     static constexpr int UNIT = WIDE ? 32 * NT : 128;
     static constexpr int TILE = 32 * D * EL;
     static constexpr int STAGE = 2 * NT * TILE;          // keys and values
@@ -30,9 +30,36 @@ struct RowsCfg {
     static constexpr int LDS = RING > JOIN ? RING : JOIN;
     static constexpr int LOADS = STAGE / (WIDE ? 4 : 1) / 1024;   // a wave's loads of a unit
     static constexpr int BY_LDS = 160 * 1024 / LDS;
-    static constexpr int PER_CU = BY_LDS < (D == 64 && EL == 2 ? 3 : 2) ? BY_LDS : (D == 64 && EL == 2 ? 3 : 2);
+    static constexpr int BY_REGISTERS = D == 64 && EL == 2 ? 3 : EL == 4 && D == 128 ? 1 : 2;
+    static constexpr int PER_CU = BY_LDS < BY_REGISTERS ? BY_LDS : BY_REGISTERS;
     static_assert(PER_CU >= 1 && LDS <= 160 * 1024, "LDS");
 };
+
+// The plan of at most kInlineTiles tiles, by one workgroup; `scratch`: B + 1 values of LDS
+__device__ inline void make_plan(const View& a, const Plan& p, InlinePlan* own, int64_t* scratch) {
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    for (int64_t b = tid; b <= a.B; b += 256) scratch[b] = a.targets[b];
+    __syncthreads();
+    int64_t c[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int t = 2 * tid + i;
+        c[i] = t < p.tiles ? plan_tile(a, scratch, p.bq, p.unit, t, &own->recs[t]) : 0;
+    }
+    int64_t v = c[0] + c[1];
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+        const int64_t o = __shfl_up(v, s, 64);
+        if (lane >= s) v += o;
+    }
+    if (lane == 63) own->sums[w] = v;
+    __syncthreads();
+    for (int i = 0; i < w; ++i) v += own->sums[i];
+    own->prefix[2 * tid + 1] = v - c[1];
+    own->prefix[2 * tid + 2] = v;
+    if (tid == 0) own->prefix[0] = 0;
+    __syncthreads();
+}
 
 template <typename T, int D, bool WIDE, bool BWD>
 __global__ __launch_bounds__(256, (RowsCfg<T, D, WIDE, BWD>::PER_CU)) void rows_kernel(RowsArgs f) {
@@ -44,24 +71,35 @@ __global__ __launch_bounds__(256, (RowsCfg<T, D, WIDE, BWD>::PER_CU)) void rows_
     const View& a = f.a;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hl = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    __shared__ __attribute__((aligned(16))) InlinePlan own;
+    Plan plan = f.p;
+    if (f.plan_inline) {
+        make_plan(a, plan, &own, reinterpret_cast<int64_t*>(smem));
+        plan.recs = own.recs;
+        plan.prefix = own.prefix;
+    }
     int64_t X;
-    const int64_t P = pieces(f.p, a.hk, f.grid, &X);
-    if (blockIdx.x >= P) return;
-    const int64_t id = xcd_range(blockIdx.x, P), W = f.p.prefix[f.p.tiles];
+    const int64_t P = pieces(plan, a.hk, f.grid, &X);
+    if (blockIdx.x >= P) {
+        if (tid == 0) f.begun[blockIdx.x].n = 0;
+        return;
+    }
+    const int64_t id = xcd_range(blockIdx.x, P), W = X / a.hk;
+    if (tid == 0) f.begun[id].n = 0;
     int64_t at = id * X / P;
     const int64_t end = (id + 1) * X / P;
     int32_t kv = (int32_t)(at / W);
     int64_t rem = at - kv * W;   // of the key head's units
-    int64_t tile = tile_at(f.p, rem);
+    int64_t tile = tile_at(plan, rem);
     const T* Kp = reinterpret_cast<const T*>(a.K);
     const T* Vp = reinterpret_cast<const T*>(a.V);
     uint8_t* const ring = smem + (WIDE ? 0 : w * C::STAGES * C::STAGE);
     const float cap2 = a.cap * kLog2e, inv_cap = a.cap > 0.f ? a.scale / a.cap : 0.f, to_exp = 2.f * kLog2e * inv_cap;
 
     while (at < end) {
-        const int64_t first = f.p.prefix[tile], cost = f.p.prefix[tile + 1] - first;
-        if (rem >= f.p.prefix[tile + 1]) {   // (a tile without rows has no units)
-            if (++tile == f.p.tiles) {
+        const int64_t first = uniform(plan.prefix[tile]), cost = uniform(plan.prefix[tile + 1]) - first;
+        if (rem >= first + cost) {   // (a tile without rows has no units)
+            if (++tile == plan.tiles) {
                 tile = 0;
                 rem = 0;
                 ++kv;
@@ -69,7 +107,8 @@ __global__ __launch_bounds__(256, (RowsCfg<T, D, WIDE, BWD>::PER_CU)) void rows_
             continue;
         }
         const int64_t k0 = rem - first, k1 = min(cost, k0 + (end - at));
-        const TileRec rec = f.p.recs[tile];
+        TileRec rec = plan.recs[tile];
+        rec = {uniform(rec.user), uniform(rec.row0), uniform(rec.klo), uniform(rec.khi)};
         const User us = user_at(a, rec.user);
         const int32_t nrows = us.n * a.g;
         // the lane's row
@@ -269,6 +308,11 @@ __global__ __launch_bounds__(256, (RowsCfg<T, D, WIDE, BWD>::PER_CU)) void rows_
 
         // results
         const bool is_whole = k0 == 0 && k1 == cost;
+        if (k0 == 0 && !is_whole && tid == 0) {
+            // the last piece with a part of the tile is the one that its last unit is in
+            const int64_t t1 = kv * W + first + cost, last = min((t1 * P - 1) / X, P - 1);
+            f.begun[id] = {us.t0, (int32_t)(last - id) + 1, kv, rec.row0, min(C::BQ, nrows - rec.row0)};
+        }
         float* part = f.parts + (2 * id + (k0 == 0 ? 1 : 0)) * C::BQ * (D + 2);
         if constexpr (!BWD) l = swap_halves(l, add_);
         if constexpr (WIDE) {
