@@ -141,6 +141,18 @@ __device__ __forceinline__ void add4(const uint16_t* p, int left, float* v) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] += __uint_as_float((uint32_t)x.v[e] << 16);
 }
+__device__ __forceinline__ void put4(uint16_t* p, int left, const float* v) {
+    const uint2 x = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    if (left >= 4) {
+        __builtin_memcpy(p, &x, 8);
+    } else {
+        Four y;
+        __builtin_memcpy(&y, &x, 8);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) p[e] = y.v[e];
+    }
+}
 struct __attribute__((packed, aligned(2))) Eight {
     uint16_t v[8];
 };
@@ -429,12 +441,129 @@ __global__ __launch_bounds__(64 * PM * PN, (Cfg<BM, BN, PM, PN, NS>::PER_CU * PM
     }
 }
 
+// Few rows: 32 rows by 32 columns a workgroup (swiglu: 32 of each half), its eight waves each every eighth slab
+// of k, all of whose loads are on their way at once, and their sums added up through LDS in order.  A tile of the
+// other kernel goes through its slabs one after the other: 16 rows of 1,024 by 1,024 columns take it 12.4 us.
+constexpr int kFewStages = 2;
+// B_KC: B's columns come straight into registers, like x's rows.
+template <bool B_KC, int OUT>
+__global__ __launch_bounds__(512, 2) void few_rows_kernel(Args g) {
+    constexpr bool GATED = OUT == kGated;
+    constexpr int FN = GATED ? 2 : 1, SLAB = GBK * 32 * 2;   // bytes of 64 k by 32 columns
+    constexpr int RING = B_KC ? 0 : 8 * kFewStages * FN * SLAB, SUMS = 8 * FN * 16 * 64 * 4;
+    __shared__ __attribute__((aligned(16))) uint8_t smem[RING > SUMS ? RING : SUMS];
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hl = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n0 = blockIdx.x * 32, m0 = blockIdx.y * 32;
+    const int slabs = (g.K + GBK - 1) / GBK;
+    uint8_t* const ring = smem + w * kFewStages * FN * SLAB;
+    const uint16_t* const xp = g.A + (int64_t)min(m0 + l32, g.M - 1) * g.a_m;
+    const uint16_t* const bp = B_KC ? g.B + (int64_t)min(n0 + l32, g.N - 1) * g.b_n : nullptr;
+    struct X {
+        uint4 v[4], b[B_KC ? 4 : 1];
+    };
+    auto load_x = [&](X& x, int kt) __attribute__((always_inline)) {
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            const int k = kt * GBK + 16 * ks + 8 * hl;
+            x.v[ks] = k < g.K ? *reinterpret_cast<const uint4*>(xp + k) : make_uint4(0, 0, 0, 0);
+            if constexpr (B_KC) x.b[ks] = k < g.K ? *reinterpret_cast<const uint4*>(bp + k) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    // W's slab as it lies in memory, [64 k][32], chunks permuted within a row
+    auto issue = [&](int kt, int stage) __attribute__((always_inline)) {
+#pragma unroll
+        for (int f = 0; f < FN; ++f)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int k = 16 * q + (lane >> 2), chunk = (lane & 3) ^ ((k >> 2) & 3);
+                const int half = GATED ? g.nb / 2 : g.nb, col = min(n0 + 8 * chunk, half - 8) + f * half;
+                const uint16_t* from = g.B + (int64_t)(kt * GBK + k) * g.b_k + col;
+                dma16(kt * GBK + k < g.K ? reinterpret_cast<const char*>(from) : reinterpret_cast<const char*>(kZeros),
+                      ring + (stage * FN + f) * SLAB + q * 1024);
+            }
+    };
+    f32x16 acc[FN];
+#pragma unroll
+    for (int f = 0; f < FN; ++f) acc[f] = f32x16{};
+    X x, xn;
+    int stage = 0;
+    if (w < slabs) {
+        load_x(x, w);
+        if constexpr (!B_KC) issue(w, 0);
+    }
+    for (int kt = w; kt < slabs; kt += 8) {
+        if (kt + 8 < slabs) load_x(xn, kt + 8);
+        if constexpr (B_KC) {
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+                acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x.b[ks]),
+                                                                 __builtin_bit_cast(bf16x8, x.v[ks]), acc[0], 0, 0, 0);
+            x = xn;
+            continue;
+        }
+        if (kt + 8 < slabs) {
+            issue(kt + 8, stage ^ 1);
+            wait_loads<4 + 4 * FN>();
+        } else {
+            wait_loads<0>();
+        }
+#pragma unroll
+        for (int f = 0; f < FN; ++f) {
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            typedef __attribute__((address_space(3))) short lds_short;
+            lds_short* base = (lds_short*)(ring + (stage * FN + f) * SLAB);
+            const int s = lane & 15, gr = (lane >> 4) & 1, col = 16 * gr + 4 * (s & 3);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+                const int k = 16 * ks + 8 * hl + (s >> 2);
+                lds_short* p = base + k * 32 + 8 * ((col >> 3) ^ ((k >> 2) & 3)) + (col & 7);
+                lds_short* q = base + (k + 4) * 32 + 8 * ((col >> 3) ^ (((k + 4) >> 2) & 3)) + (col & 7);
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)q);
+                acc[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)),
+                    __builtin_bit_cast(bf16x8, x.v[ks]), acc[f], 0, 0, 0);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        x = xn;
+        stage ^= 1;
+    }
+    // [wave][half][register][lane]
+    __syncthreads();
+    float* const part = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int f = 0; f < FN; ++f)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) part[((w * FN + f) * 16 + r) * 64 + lane] = acc[f][r];
+    __syncthreads();
+    const int q = tid >> 6, n = n0 + 8 * q + 4 * hl, m = m0 + l32;
+    if (q >= 4 || m >= g.M || n >= g.F) return;
+    float z[4], u[4] = {0.f, 0.f, 0.f, 0.f};
+    auto sum = [&](float* v, int f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[e] += part[((i * FN + f) * 16 + 4 * q + e) * 64 + lane];
+        }
+        if (g.bias) add4(g.bias + f * g.F + n, g.F - n, v);
+        if (g.pre) put4(g.pre + (int64_t)m * g.N + f * g.F + n, g.F - n, v);
+    };
+    sum(z, 0);
+    if constexpr (GATED) sum(u, 1);
+    const int64_t o = (int64_t)m * g.F + n;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = activate<false>(z[e], u[e], GATED ? SA_ACT_SWIGLU : OUT >= kEpi ? OUT - kEpi : SA_ACT_NONE);
+    if (g.res) add4(g.res + o, g.F - n, z);
+    put4(reinterpret_cast<uint16_t*>(g.y) + o, g.F - n, z);
+}
+
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-template <int BM, int BN, int PM, int PN, int NS>
-hipError_t launch_t(const Product& p, hipStream_t stream) {
-    using C = Cfg<BM, BN, PM, PN, NS>;
+Args args_of(const Product& p, int bm, int bn) {
     Args g;
     g.A = reinterpret_cast<const uint16_t*>(p.A);
     g.B = reinterpret_cast<const uint16_t*>(p.B);
@@ -443,8 +572,8 @@ hipError_t launch_t(const Product& p, hipStream_t stream) {
     g.ma = p.ma; g.nb = p.nb;
     const bool gated = p.epi && p.epi->act == SA_ACT_SWIGLU;
     g.F = gated ? p.N / 2 : p.N;
-    g.tm = (int32_t)cdiv(p.M, BM);
-    g.tn = (int32_t)(gated ? cdiv(g.F, BN / 2) : cdiv(p.N, BN));
+    g.tm = (int32_t)cdiv(p.M, bm);
+    g.tn = (int32_t)(gated ? cdiv(g.F, bn / 2) : cdiv(p.N, bn));
     g.splits = p.splits;
     g.per = p.per;
     g.y = p.y;
@@ -452,6 +581,30 @@ hipError_t launch_t(const Product& p, hipStream_t stream) {
     g.res = p.epi ? reinterpret_cast<const uint16_t*>(p.epi->res) : nullptr;
     g.pre = p.epi ? reinterpret_cast<uint16_t*>(p.epi->pre) : nullptr;
     g.act = p.epi ? p.epi->act : SA_ACT_NONE;
+    return g;
+}
+
+hipError_t launch_few_rows(const Product& p, hipStream_t stream) {
+    const Args g = args_of(p, 32, 64);
+    const dim3 grid((unsigned)cdiv(g.F, 32), (unsigned)cdiv(p.M, 32));
+#define SA_RUN(OUT) hipLaunchKernelGGL((few_rows_kernel<false, OUT>), grid, dim3(512), 0, stream, g)
+    if (p.b_k == 1) hipLaunchKernelGGL((few_rows_kernel<true, kBf16>), grid, dim3(512), 0, stream, g);
+    else switch (g.act) {
+        case SA_ACT_RELU: SA_RUN(kEpi + SA_ACT_RELU); break;
+        case SA_ACT_GELU: SA_RUN(kEpi + SA_ACT_GELU); break;
+        case SA_ACT_SILU: SA_RUN(kEpi + SA_ACT_SILU); break;
+        case SA_ACT_SWIGLU: SA_RUN(kGated); break;
+        default: SA_RUN(kEpi + SA_ACT_NONE);
+    }
+#undef SA_RUN
+    return hipGetLastError();
+}
+
+template <int BM, int BN, int PM, int PN, int NS>
+hipError_t launch_t(const Product& p, hipStream_t stream) {
+    using C = Cfg<BM, BN, PM, PN, NS>;
+    const Args g = args_of(p, BM, BN);
+    const bool gated = g.act == SA_ACT_SWIGLU;
     const dim3 grid((unsigned)std::min<int64_t>((int64_t)g.tm * g.tn * g.splits, (int64_t)device_cus() * C::PER_CU));
     const bool a_kc = p.a_k == 1, b_kc = p.b_k == 1;
 #define SA_RUN(AK, BK, OUT) \
@@ -563,7 +716,14 @@ void choose_splits(Product* p) {
 hipError_t launch_product(const Product& p, hipStream_t stream) {
     if (!product_supported(p)) return hipErrorInvalidValue;
     double time = 0;
-    switch (choose(p, &time)) {
+    const int shape = choose(p, &time);
+    // few rows (a tile of 64 by 64 columns, k = 1024, takes 13 us, 4 of which are not its slabs'): 16, 64, 256 rows by
+    // 1,024 columns 4.2, 5.2, 5.9 us, 128 by 4,096 9.1; 64 and 256 by 1,024 with k = 4096 12.0 and 13.8 (tiles: 40)
+    if (p.a_k == 1 && p.splits == 1) {
+        const int64_t n = cdiv(cdiv(p.N, 32) * cdiv(p.M, 32), device_cus());
+        if (2.6 + 1.6 * n * cdiv(p.K, 8 * GBK) < 4.0 + time) return launch_few_rows(p, stream);
+    }
+    switch (shape) {
         case 0: return launch_t<256, 256, 2, 4, 2>(p, stream);
         case 1: return launch_t<192, 256, 2, 4, 2>(p, stream);
         case 2: return launch_t<128, 256, 2, 4, 3>(p, stream);
