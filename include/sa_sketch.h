@@ -663,8 +663,9 @@ typedef enum {
     SA_ACT_SWIGLU = 4 /* W and bias have 2 F columns: y = silu(z[:, :F]) * z[:, F:] */
 } sa_activation;
 
-/* Bytes of workspace that sa_linear_fwd needs for this shape (0 is possible). */
-size_t sa_linear_fwd_workspace_size(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype);
+/* Bytes of workspace that sa_linear_fwd needs for this shape (0 is possible): rows of x and W that
+ * are no multiple of 16 bytes may be copied there. */
+size_t sa_linear_fwd_workspace_size(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype, int64_t x_stride);
 
 /*
  * A linear layer with bias, activation and residual after its product: the projections, the
@@ -688,8 +689,8 @@ sa_status sa_linear_fwd(const void* x, int64_t x_stride, const void* W, const vo
                         int32_t K, int32_t F, sa_activation act, sa_dtype dtype, void* y, void* pre, void* workspace,
                         size_t workspace_bytes, void* stream);
 
-/* Bytes of workspace that sa_linear_bwd needs for this shape (0 is possible). */
-size_t sa_linear_bwd_workspace_size(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype);
+/* Bytes of workspace that sa_linear_bwd needs for this shape. */
+size_t sa_linear_bwd_workspace_size(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype, int64_t x_stride);
 
 /*
  * Backward of sa_linear_fwd: with dz = dy act'(pre),

@@ -184,40 +184,96 @@ sa_status check_linear(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dt
     return SA_OK;
 }
 
-// the bf16 products of a layer;
-sa::linear::Product fwd_product(const void* x, int64_t x_ld, const void* W, int64_t N, int32_t K, int32_t C,
-                                const sa::linear::Epilogue* epi, void* y) {
-    return {x, W, x_ld, 1, C, 1, (int32_t)N, C, K, 0, C, y, true, epi};
-}
-sa::linear::Product dx_product(const void* dz, const void* W, int64_t N, int32_t K, int32_t C, void* dx) {
-    return {dz, W, C, 1, 1, C, (int32_t)N, K, C, 0, 0, dx, true, nullptr};
-}
-sa::linear::Product dw_product(const void* x, int64_t x_ld, const void* dz, int64_t N, int32_t K, int32_t C, void* dW, bool bf) {
-    return {x, dz, 1, x_ld, C, 1, K, C, (int32_t)N, K, C, dW, bf, nullptr};
-}
+// A layer's products on tiles of 16-byte pieces (linear_gemm.hip), where x, W or dz have rows that are no whole
+// pieces over copies of them with zeros up to the next; small ones in such sizes, and small ones in single
+// precision, on the general product (layer.hip).
+int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+constexpr double kPadTime = 3.0, kPadRate = 4e6;                // us; bytes written a us, read ones not counted
+double general_time(double flops, bool epilogue) { return (epilogue ? 10.0 : 6.0) + flops / 60e6; }
 
-// z in fp32, where the product has no epilogue and z does not fit into the result
-size_t linear_fwd_workspace(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype) {
-    return dtype == SA_FP32 && act != SA_ACT_SWIGLU ? 0 : 4 * (size_t)N * columns(F, act);
+struct LinearFwdPlan {
+    bool tiles = false, pad_x = false, pad_w = false;
+    int64_t Kp = 0, Fp = 0;                  // padded k, columns of y
+    size_t off_x = 0, off_w = 0, total = 0;  // copies; or z in fp32, from the start
+};
+LinearFwdPlan plan_linear_fwd(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype, int64_t x_ld) {
+    LinearFwdPlan p;
+    const bool bf = dtype == SA_BF16;
+    const int64_t el = bf ? 2 : 4, piece = 16 / el, halves = act == SA_ACT_SWIGLU ? 2 : 1;
+    p.Kp = round_up(K, piece);
+    p.Fp = round_up(F, piece);
+    p.pad_x = p.Kp != K || x_ld % piece != 0;
+    p.pad_w = p.Kp != K || p.Fp != F;
+    sa::linear::Epilogue epi{nullptr, nullptr, (int)act, nullptr};
+    sa::linear::Product prod{bf, nullptr, nullptr, p.pad_x ? p.Kp : x_ld, 1, halves * p.Fp, 1, (int32_t)N, columns(F, act),
+                             (int32_t)p.Kp, 0, (int32_t)(halves * p.Fp), nullptr, bf, &epi};
+    double time = 0;
+    if (sa::linear::product_supported(prod)) {
+        time = sa::linear::product_time(prod);
+        if (p.pad_x) time += kPadTime + el * N * p.Kp / kPadRate;
+        if (p.pad_w) time += kPadTime + el * p.Kp * halves * p.Fp / kPadRate;
+        p.tiles = (bf && !p.pad_x && !p.pad_w) || time < general_time(2.0 * N * K * columns(F, act), true);
+    }
+    if (!p.tiles) {   // z in fp32, where it does not fit into the result
+        p.total = bf || act == SA_ACT_SWIGLU ? 4 * (size_t)N * columns(F, act) : 0;
+        return p;
+    }
+    if (p.pad_x) p.total = align_up(el * N * p.Kp, 256);
+    p.off_w = p.total;
+    if (p.pad_w) p.total += el * p.Kp * halves * p.Fp;
+    return p;
 }
 
 struct LinearBwdPlan {
+    bool dx_tiles = false, dw_tiles = false, pad_z = false, pad_w = false, pad_x = false;
+    int64_t Kp = 0, Cp = 0;
     int32_t splits = 1, per = 0x7fffffff;   // dW's sum over the rows
-    size_t off_dz = 0, off_sums = 0, off_parts = 0, total = 0;
+    size_t off_dz = 0, off_w = 0, off_x = 0, off_sums = 0, off_parts = 0, total = 0;
 };
-LinearBwdPlan plan_linear_bwd(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype) {
+LinearBwdPlan plan_linear_bwd(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype, int64_t x_ld) {
     LinearBwdPlan p;
-    const size_t el = dtype == SA_BF16 ? 2 : 4, C = columns(F, act);
-    p.off_sums = act == SA_ACT_NONE ? 0 : align_up(el * (size_t)N * C, 256);
-    p.off_parts = align_up(p.off_sums + 4 * (size_t)sa::linear::act_bwd_parts(N, F, dtype == SA_BF16) * C, 256);
-    p.total = p.off_parts;
-    if (dtype == SA_BF16) {
-        sa::linear::Product prod = dw_product(nullptr, K, nullptr, N, K, columns(F, act), nullptr, false);
-        sa::linear::choose_splits(&prod);
-        p.splits = prod.splits;
-        p.per = prod.per;
-        if (p.splits > 1) p.total += 4 * (size_t)p.splits * K * C;
+    const bool bf = dtype == SA_BF16;
+    const int64_t el = bf ? 2 : 4, piece = 16 / el;
+    const int32_t C = columns(F, act);
+    const double flops = 2.0 * N * K * C;
+    p.Kp = round_up(K, piece);
+    p.Cp = round_up(C, piece);
+    p.pad_w = p.Cp != C;
+    p.pad_x = p.Kp != K || x_ld % piece != 0;
+    p.pad_z = p.Cp != C;   // (SA_ACT_NONE: a copy of dy; else dz is written so)
+    const double z_time = act == SA_ACT_NONE && p.pad_z ? kPadTime + el * N * p.Cp / kPadRate : 0;
+    sa::linear::Product dx{bf, nullptr, nullptr, p.Cp, 1, 1, p.Cp, (int32_t)N, K, (int32_t)p.Cp, 0, 0, nullptr, bf, nullptr};
+    if (N > 0 && sa::linear::product_supported(dx)) {
+        const double time = sa::linear::product_time(dx) + z_time + (p.pad_w ? kPadTime + el * K * p.Cp / kPadRate : 0);
+        p.dx_tiles = (bf && !p.pad_z) || time < general_time(flops, false);
     }
+    sa::linear::Product dw{bf, nullptr, nullptr, 1, p.pad_x ? p.Kp : x_ld, p.Cp, 1, K, C, (int32_t)N, (int32_t)p.Kp, (int32_t)p.Cp,
+                           nullptr, false, nullptr};
+    if (N > 0 && sa::linear::product_supported(dw)) {
+        sa::linear::choose_splits(&dw);
+        const double time = sa::linear::product_time(dw) + (dw.splits > 1 ? 4.0 + dw.splits * (double)K * C / 1e6 : 0) + z_time +
+                            (p.pad_x ? kPadTime + el * N * p.Kp / kPadRate : 0);
+        p.dw_tiles = (bf && !p.pad_z && !p.pad_x) || time < general_time(flops, false);
+        if (p.dw_tiles) {
+            p.splits = dw.splits;
+            p.per = dw.per;
+        }
+    }
+    p.pad_z = p.pad_z && (p.dx_tiles || p.dw_tiles);
+    p.pad_w = p.pad_w && p.dx_tiles;
+    p.pad_x = p.pad_x && p.dw_tiles;
+    size_t off = 0;
+    auto carve = [&](size_t bytes) {
+        const size_t o = off;
+        off = align_up(off + bytes, 256);
+        return o;
+    };
+    if (act != SA_ACT_NONE || p.pad_z) p.off_dz = carve(el * N * (p.pad_z ? p.Cp : C));
+    if (p.pad_w) p.off_w = carve(el * K * p.Cp);
+    if (p.pad_x) p.off_x = carve(el * N * p.Kp);
+    p.off_sums = carve(4 * (size_t)sa::linear::act_bwd_parts(N, F, bf) * C);
+    if (p.splits > 1) p.off_parts = carve(4 * (size_t)p.splits * K * C);
+    p.total = off;
     return p;
 }
 
@@ -295,8 +351,10 @@ sa_status sa_layer_norm_bwd(const void* x, int64_t x_stride, const void* gamma, 
     return SA_OK;
 }
 
-size_t sa_linear_fwd_workspace_size(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype) {
-    return check_linear(N, K, F, act, dtype) == SA_OK ? linear_fwd_workspace(N, K, F, act, dtype) : 0;
+size_t sa_linear_fwd_workspace_size(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype, int64_t x_stride) {
+    if (x_stride == 0) x_stride = K;
+    if (check_linear(N, K, F, act, dtype) != SA_OK || x_stride < 0 || N == 0) return 0;
+    return plan_linear_fwd(N, K, F, act, dtype, x_stride).total;
 }
 
 sa_status sa_linear_fwd(const void* x, int64_t x_stride, const void* W, const void* bias, const void* residual, int64_t N,
@@ -311,33 +369,44 @@ sa_status sa_linear_fwd(const void* x, int64_t x_stride, const void* W, const vo
     if (!x || !W || !y) return api_fail(SA_ERR_INVALID_ARG, "null pointer argument");
     if (!aligned16(x) || !aligned16(W) || !aligned16(bias) || !aligned16(residual) || !aligned16(y) || !aligned16(pre))
         return api_fail(SA_ERR_INVALID_ARG, "tensor arguments must be 16-byte aligned");
-    const size_t need = linear_fwd_workspace(N, K, F, act, dtype);
-    if (need > 0) {
-        st = check_workspace(workspace, workspace_bytes, need);
+    const LinearFwdPlan p = plan_linear_fwd(N, K, F, act, dtype, x_stride);
+    if (p.total > 0) {
+        st = check_workspace(workspace, workspace_bytes, p.total);
         if (st != SA_OK) return st;
     }
+    uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
     hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
     const bool bf = dtype == SA_BF16;
-    const int32_t C = columns(F, act);
-    float* z = reinterpret_cast<float*>(need > 0 ? workspace : y);
-    sa::ProfScope ps("linear_fwd", stream);
+    const int32_t C = columns(F, act), halves = act == SA_ACT_SWIGLU ? 2 : 1;
     const sa::linear::Epilogue epi{bias, residual, (int)act, pre};
-    const sa::linear::Product prod = fwd_product(x, x_stride, W, N, K, C, &epi, y);
-    hipError_t e;
-    if (bf && sa::linear::product_supported(prod)) {
-        e = sa::linear::launch_product(prod, stream);
-        if (e != hipSuccess) return hip_fail(e, "linear layer launch");
-        return SA_OK;
+    sa::ProfScope ps("linear_fwd", stream);
+    hipError_t e = hipSuccess;
+    if (p.tiles) {
+        const void *xs = x, *Ws = W;
+        if (p.pad_x) {
+            xs = ws + p.off_x;
+            e = sa::linear::launch_pad(x, x_stride, N, K, 1, ws + p.off_x, N, (int32_t)p.Kp, bf, stream);
+        }
+        if (e == hipSuccess && p.pad_w) {
+            Ws = ws + p.off_w;
+            e = sa::linear::launch_pad(W, C, K, F, halves, ws + p.off_w, p.Kp, (int32_t)p.Fp, bf, stream);
+        }
+        if (e == hipSuccess)
+            e = sa::linear::launch_product({bf, xs, Ws, p.pad_x ? p.Kp : x_stride, 1, halves * p.Fp, 1, (int32_t)N, C, (int32_t)p.Kp,
+                                            0, (int32_t)(halves * p.Fp), y, bf, &epi}, stream);
+    } else {
+        float* z = reinterpret_cast<float*>(p.total > 0 ? workspace : y);
+        e = sa::launch_gemm({x, bf, 0, x_stride, 1, W, bf, 0, C, 1, z, false, 0, C, (int32_t)N, C, K, 1, 1.f, false}, stream);
+        if (e == hipSuccess) e = sa::linear::launch_epilogue(z, epi, N, F, bf, y, stream);
     }
-    e = sa::launch_gemm({x, bf, 0, x_stride, 1, W, bf, 0, C, 1, z, false, 0, C, (int32_t)N, C, K, 1, 1.f, false}, stream);
-    if (e == hipSuccess)
-        e = sa::linear::launch_epilogue(z, {bias, residual, (int)act, pre}, N, F, bf, y, stream);
     if (e != hipSuccess) return hip_fail(e, "linear layer launch");
     return SA_OK;
 }
 
-size_t sa_linear_bwd_workspace_size(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype) {
-    return check_linear(N, K, F, act, dtype) == SA_OK ? plan_linear_bwd(N, K, F, act, dtype).total : 0;
+size_t sa_linear_bwd_workspace_size(int64_t N, int32_t K, int32_t F, sa_activation act, sa_dtype dtype, int64_t x_stride) {
+    if (x_stride == 0) x_stride = K;
+    if (check_linear(N, K, F, act, dtype) != SA_OK || x_stride < 0) return 0;
+    return plan_linear_bwd(N, K, F, act, dtype, x_stride).total;
 }
 
 sa_status sa_linear_bwd(const void* x, int64_t x_stride, const void* W, const void* pre, const void* dy, int64_t N,
@@ -357,40 +426,50 @@ sa_status sa_linear_bwd(const void* x, int64_t x_stride, const void* W, const vo
     if (!aligned16(x) || !aligned16(W) || !aligned16(pre) || !aligned16(dy) || !aligned16(dx) || !aligned16(dW) ||
         !aligned16(dbias))
         return api_fail(SA_ERR_INVALID_ARG, "tensor arguments must be 16-byte aligned");
-    const LinearBwdPlan p = plan_linear_bwd(N, K, F, act, dtype);
+    const LinearBwdPlan p = plan_linear_bwd(N, K, F, act, dtype, x_stride);
     st = check_workspace(workspace, workspace_bytes, p.total);
     if (st != SA_OK) return st;
     uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
     hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
     const bool bf = dtype == SA_BF16, wb = weight_dtype == SA_BF16;
-    const int32_t C = columns(F, act);
+    const int32_t C = columns(F, act), z_ld = (int32_t)(p.pad_z ? p.Cp : C);
     hipError_t e = hipSuccess;
-    const void* dz = act == SA_ACT_NONE ? dy : ws + p.off_dz;
+    const void* dz = act == SA_ACT_NONE && !p.pad_z ? dy : ws + p.off_dz;
     if (act != SA_ACT_NONE || dbias) {
         sa::ProfScope ps("linear_act_bwd", stream);
-        e = sa::linear::launch_act_bwd({dy, pre, N, F, (int)act, ws + p.off_dz, dbias, wb, reinterpret_cast<float*>(ws + p.off_sums)},
-                                       bf, stream);
+        e = sa::linear::launch_act_bwd({dy, pre, N, F, (int)act, ws + p.off_dz, z_ld, dbias, wb,
+                                        reinterpret_cast<float*>(ws + p.off_sums)}, bf, stream);
     }
-    if (e == hipSuccess && dx) {
+    if (e == hipSuccess && act == SA_ACT_NONE && p.pad_z)
+        e = sa::linear::launch_pad(dy, C, N, C, 1, ws + p.off_dz, N, z_ld, bf, stream);
+    if (e == hipSuccess && dx && N > 0) {
         sa::ProfScope ps("linear_dx", stream);
-        const sa::linear::Product prod = dx_product(dz, W, N, K, C, dx);
-        if (bf && sa::linear::product_supported(prod)) e = sa::linear::launch_product(prod, stream);
-        else e = sa::launch_gemm({dz, bf, 0, C, 1, W, bf, 0, 1, C, dx, bf, 0, K, (int32_t)N, K, C, 1, 1.f, false}, stream);
+        const void* Ws = W;
+        if (p.pad_w) {
+            Ws = ws + p.off_w;
+            e = sa::linear::launch_pad(W, C, K, C, 1, ws + p.off_w, K, (int32_t)p.Cp, bf, stream);
+        }
+        if (e == hipSuccess && p.dx_tiles)
+            e = sa::linear::launch_product({bf, dz, Ws, z_ld, 1, 1, p.Cp, (int32_t)N, K, (int32_t)p.Cp, 0, 0, dx, bf, nullptr}, stream);
+        else if (e == hipSuccess)
+            e = sa::launch_gemm({dz, bf, 0, z_ld, 1, W, bf, 0, 1, C, dx, bf, 0, K, (int32_t)N, K, C, 1, 1.f, false}, stream);
     }
     if (e == hipSuccess && dW) {
         sa::ProfScope ps("linear_dw", stream);
-        sa::linear::Product prod = dw_product(x, x_stride, dz, N, K, C, dW, wb);
-        if (p.splits > 1) {
-            prod.y = ws + p.off_parts;
-            prod.y_bf16 = false;
-            prod.splits = p.splits;
-            prod.per = p.per;
+        const void* xs = x;
+        if (p.pad_x) {
+            xs = ws + p.off_x;
+            e = sa::linear::launch_pad(x, x_stride, N, K, 1, ws + p.off_x, N, (int32_t)p.Kp, bf, stream);
         }
-        if (bf && sa::linear::product_supported(prod)) {
-            e = sa::linear::launch_product(prod, stream);
+        void* const to = p.splits > 1 ? ws + p.off_parts : dW;
+        if (e == hipSuccess && p.dw_tiles) {
+            e = sa::linear::launch_product({bf, xs, dz, 1, p.pad_x ? p.Kp : x_stride, z_ld, 1, K, C, (int32_t)N, (int32_t)p.Kp, z_ld, to,
+                                            p.splits == 1 && wb, nullptr, p.splits, p.per}, stream);
             if (e == hipSuccess && p.splits > 1)
-                e = sa::linear::launch_sum_splits(reinterpret_cast<const float*>(ws + p.off_parts), p.splits, (int64_t)K * C, dW, wb, stream);
-        } else e = sa::launch_gemm({x, bf, 0, 1, x_stride, dz, bf, 0, C, 1, dW, wb, 0, C, K, C, (int32_t)N, 1, 1.f, false}, stream);
+                e = sa::linear::launch_sum_splits(reinterpret_cast<const float*>(to), p.splits, (int64_t)K * C, dW, wb, stream);
+        } else if (e == hipSuccess) {
+            e = sa::launch_gemm({x, bf, 0, 1, x_stride, dz, bf, 0, z_ld, 1, dW, wb, 0, C, K, C, (int32_t)N, 1, 1.f, false}, stream);
+        }
     }
     if (e != hipSuccess) return hip_fail(e, "linear layer backward launch");
     return SA_OK;

@@ -67,8 +67,12 @@ struct Epilogue {
 // y [N][F] of z fp32; y may be z (fp32, no swiglu)
 hipError_t launch_epilogue(const float* z, const Epilogue& e, int64_t N, int32_t F, bool bf16, void* y, hipStream_t stream);
 
-// n values (a multiple of 4), each the sum of its parts [splits][n] in order
+// n values, each the sum of its parts [splits][n] in order
 hipError_t launch_sum_splits(const float* parts, int32_t splits, int64_t n, void* to, bool bf16, hipStream_t stream);
+
+// to [rows][halves to_width] = from [rows_in][halves width], ld values from row to row, zeros where `from` has none
+hipError_t launch_pad(const void* from, int64_t ld, int64_t rows_in, int32_t width, int32_t halves, void* to, int64_t rows,
+                      int32_t to_width, bool bf16, hipStream_t stream);
 
 // dz = dy act'(pre) (not written for SA_ACT_NONE), and its column sums db, through sums
 // [act_bwd_parts][columns]
@@ -77,7 +81,8 @@ struct ActBwd {
     int64_t N;
     int32_t F;
     int act;
-    void* dz;
+    void* dz;         // rows of dz_ld values, zeros past the columns
+    int32_t dz_ld;
     void* db;   // or null
     bool db_bf16;
     float* sums;

@@ -62,7 +62,8 @@ __global__ __launch_bounds__(kThreads) void epilogue_kernel(const float* z, cons
 constexpr int kAcross = 32, kDown = kThreads / kAcross;
 template <typename T>
 __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const T* __restrict__ dy, const T* __restrict__ pre, int64_t N,
-                                                           int F, int act, T* __restrict__ dz, float* __restrict__ sums) {
+                                                           int F, int act, T* __restrict__ dz, int dz_ld,
+                                                           float* __restrict__ sums) {
     constexpr int V = vec::Piece<T>::N;
     __shared__ float part[kDown][kAcross * V];
     const int tx = threadIdx.x % kAcross, ty = threadIdx.x / kAcross, c = (blockIdx.x * kAcross + tx) * V;
@@ -83,8 +84,11 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const T* __restrict__
                     d2[e] = 0.f;
                     g[e] = activate_bwd<sizeof(T) == 4>(a[e], gated ? b[e] : 0.f, g[e], act, &d2[e]);
                 }
-                vec::store<V>(dz + row * C, c, F, g);
-                if (gated) vec::store<V>(dz + row * C + F, c, F, d2);
+                T* to = dz + row * dz_ld;
+                vec::store<V>(to, c, F, g);
+                if (gated) vec::store<V>(to + F, c, F, d2);
+                if (c + V >= F)
+                    for (int i = C; i < dz_ld; ++i) vec::store(to + i, 0.f);
             }
             if (sums) {
 #pragma unroll
@@ -115,11 +119,20 @@ __global__ __launch_bounds__(kThreads) void bias_sum_kernel(const float* __restr
     vec::sum_parts(sums, n, C, [&](int64_t c, float s) { vec::store(db + c, s); });
 }
 
-// n values (a multiple of 4), each the sum of its parts [splits][n] in order
+// n values, each the sum of its parts [splits][n] in order
 template <typename TO>
 __global__ __launch_bounds__(kThreads) void sum_splits_kernel(const float* __restrict__ parts, int splits, int64_t n,
                                                               TO* __restrict__ to) {
+    const bool fours = n % 4 == 0;
     for (int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * kThreads * 4) {
+        if (!fours) {
+            for (int64_t k = i; k < n && k < i + 4; ++k) {
+                float v = parts[k];
+                for (int p = 1; p < splits; ++p) v += parts[p * n + k];
+                vec::store(to + k, v);
+            }
+            continue;
+        }
         float4 v = *reinterpret_cast<const float4*>(parts + i);
         for (int p = 1; p < splits; ++p) {
             const float4 x = *reinterpret_cast<const float4*>(parts + p * n + i);
@@ -132,12 +145,31 @@ __global__ __launch_bounds__(kThreads) void sum_splits_kernel(const float* __res
 }
 
 template <typename T>
+__global__ __launch_bounds__(kThreads) void pad_kernel(const T* __restrict__ from, int64_t ld, int64_t rows_in, int width,
+                                                       int halves, T* __restrict__ to, int64_t rows, int to_width) {
+    constexpr int V = vec::Piece<T>::N;   // (to_width is a multiple of V)
+    const int64_t per = (int64_t)halves * (to_width / V), n = rows * per;
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) {
+        const int64_t row = i / per;
+        const int at = (int)(i % per) * V, half = at / to_width, c = at % to_width;
+        float v[V];
+        if (row < rows_in) {
+            vec::load<V>(from + row * ld + (int64_t)half * width, c, width, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = 0.f;
+        }
+        vec::store<V>(to + i * V, 0, V, v);
+    }
+}
+
+template <typename T>
 hipError_t act_bwd(const ActBwd& a, hipStream_t stream) {
     constexpr int V = vec::Piece<T>::N;
     const int64_t parts = act_bwd_parts(a.N, a.F, sizeof(T) == 2);
     const dim3 grid((unsigned)cdiv(a.F, kAcross * V), (unsigned)parts);
     hipLaunchKernelGGL(act_bwd_kernel<T>, grid, dim3(kThreads), 0, stream, reinterpret_cast<const T*>(a.dy),
-                       reinterpret_cast<const T*>(a.pre), a.N, a.F, a.act, reinterpret_cast<T*>(a.dz), a.db ? a.sums : nullptr);
+                       reinterpret_cast<const T*>(a.pre), a.N, a.F, a.act, reinterpret_cast<T*>(a.dz), a.dz_ld, a.db ? a.sums : nullptr);
     if (a.db) {
         const int C = a.act == SA_ACT_SWIGLU ? 2 * a.F : a.F;
         const dim3 g((unsigned)cdiv(C, vec::kSumColumns));
@@ -160,6 +192,18 @@ int64_t act_bwd_parts(int64_t N, int32_t F, bool bf16) {
 
 hipError_t launch_act_bwd(const ActBwd& a, bool bf16, hipStream_t stream) {
     return bf16 ? act_bwd<uint16_t>(a, stream) : act_bwd<float>(a, stream);
+}
+
+hipError_t launch_pad(const void* from, int64_t ld, int64_t rows_in, int32_t width, int32_t halves, void* to, int64_t rows,
+                      int32_t to_width, bool bf16, hipStream_t stream) {
+    const dim3 grid((unsigned)std::min<int64_t>(cdiv(rows * halves * (to_width / (bf16 ? 8 : 4)), kThreads), 1 << 20));
+    if (bf16)
+        hipLaunchKernelGGL(pad_kernel<uint16_t>, grid, dim3(kThreads), 0, stream, reinterpret_cast<const uint16_t*>(from), ld,
+                           rows_in, width, halves, reinterpret_cast<uint16_t*>(to), rows, to_width);
+    else
+        hipLaunchKernelGGL(pad_kernel<float>, grid, dim3(kThreads), 0, stream, reinterpret_cast<const float*>(from), ld, rows_in,
+                           width, halves, reinterpret_cast<float*>(to), rows, to_width);
+    return hipGetLastError();
 }
 
 hipError_t launch_sum_splits(const float* parts, int32_t splits, int64_t n, void* to, bool bf16, hipStream_t stream) {

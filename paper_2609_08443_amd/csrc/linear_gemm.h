@@ -1,4 +1,4 @@
-// The linear layer's bf16 products (linear_gemm.hip).
+// The linear layer's products (linear_gemm.hip).
 #pragma once
 
 #include "linear.h"
@@ -6,16 +6,17 @@
 namespace sa {
 namespace linear {
 
-// y(m, n) = sum_k A(m, k) B(k, n), with A[m a_m + k a_k], B[k b_k + n b_n] bf16, each contiguous along
-// k or along its other index, M x N x K.  Results bf16 through an epilogue (A k-contiguous, B
+// y(m, n) = sum_k A(m, k) B(k, n), with A[m a_m + k a_k], B[k b_k + n b_n] in bf16 or fp32, each
+// contiguous along k or along its other index, M x N x K.  Results in the same type through an epilogue (A k-contiguous, B
 // n-contiguous; swiglu: N = 2 F columns of B give F of y), or plain bf16 or fp32 [M][N]; with splits > 1
 // the sum over k in that many parts of `per` slabs of 64, fp32, each [M][N].
 struct Product {
+    bool bf16;
     const void *A, *B;
     int64_t a_m, a_k, b_k, b_n;
     int32_t M, N, K;
-    int32_t ma, nb;   // A's rows and B's columns in memory where it is contiguous along them (multiples of 8; swiglu:
-                      // nb / 2 columns of each half)
+    int32_t ma, nb;   // A's rows and B's columns in memory where it is contiguous along them (whole 16-byte pieces;
+                      // swiglu: nb / 2 columns of each half)
     void* y;
     bool y_bf16;
     const Epilogue* epi;   // or null
@@ -25,6 +26,8 @@ bool product_supported(const Product& p);
 // the splits that take least time, the sum of their results included, for plain fp32 results
 void choose_splits(Product* p);
 hipError_t launch_product(const Product& p, hipStream_t stream);
+// its estimated time, in microseconds (not that of the sum of splits)
+double product_time(const Product& p);
 
 }  // namespace linear
 }  // namespace sa

@@ -1,12 +1,12 @@
-// Products of a linear layer on the matrix cores, bf16 with fp32 sums:
+// Products of a linear layer on the matrix cores, bf16 with fp32 sums or fp32 throughout:
 //
 //   y = act(x W + b) + residual   (A = x, B = W, epilogue on the results where they are)
 //   dx = dz W^T   (B k-contiguous),   dW = x^T dz   (A and B contiguous along their rows, any K)
 //
-// A wave takes (32 FM) x (32 FN) outputs as FM x FN v_mfma_f32_32x32x16_bf16 of W's columns by x's rows: a
-// lane then holds four consecutive columns of a row, where the epilogue is done; the results go through a
-// wave's own part of LDS and out in whole rows.  k goes by in slabs of 64, STAGES of both operands in LDS,
-// loaded straight into it STAGES - 1 slabs ahead; the first slabs of a workgroup's next tile are on their
+// A wave takes (32 FM) x (32 FN) outputs as FM x FN products of W's columns by x's rows (32x32x16 bf16, 32x32x2
+// fp32): a lane then holds four consecutive columns of a row, where the epilogue is done; results in bf16 go
+// through a wave's own part of LDS and out in whole rows.  k goes by in slabs of 128 bytes (64 bf16, 32 fp32),
+// STAGES of both operands in LDS, loaded straight into it STAGES - 1 slabs ahead; the first slabs of a workgroup's next tile are on their
 // way while the results of the last one are written.
 #include "linear_gemm.h"
 
@@ -23,46 +23,48 @@ using namespace tile;
 
 __device__ __attribute__((aligned(16))) const uint32_t kZeros[4] = {0, 0, 0, 0};
 
+template <typename T>
 struct Args {
-    const uint16_t *A, *B;
+    const T *A, *B;
     int64_t a_m, a_k, b_k, b_n;
     int32_t M, N, K, F;     // F: columns of y, N those of pre
     int32_t ma, nb;         // rows of A, columns of B to load, where they are contiguous along them
     int32_t tm, tn, splits, per;
     void* y;
-    const uint16_t *bias, *res;
-    uint16_t* pre;
+    const T *bias, *res;
+    T* pre;
     int32_t act;
 };
+// k of a slab
+template <typename T>
+constexpr int kSlab = 128 / sizeof(T);
 
 // what becomes of the results
-enum Out { kF32, kBf16, kGated, kEpi };   // kEpi + activation: one instance each, without branches at every value
+enum Out { kF32, kPlain, kGated, kEpi };   // kF32: plain, and parts of k; kPlain: in T; kEpi + activation: an instance each
 
 // Loads of an operand's slabs, R rows.  k-contiguous: load q of a slab fills LDS rows 8 q .. 8 q + 7, lane l
-// row 8 q + l / 8 and the chunk whose swizzled position is l % 8.
-template <int R, int WAVES, bool KC, bool GATED>
+// row 8 q + l / 8 and the 16-byte chunk whose swizzled position is l % 8.
+template <typename T, int R, int WAVES, bool KC, bool GATED>
 struct Operand;
-template <int R, int WAVES, bool GATED>
-struct Operand<R, WAVES, true, GATED> {
-    static constexpr int Q = R / 8 / WAVES;
+template <typename T, int R, int WAVES, bool GATED>
+struct Operand<T, R, WAVES, true, GATED> {
+    static constexpr int Q = R / 8 / WAVES, EL = sizeof(T);
     const char* base;
     uint32_t off[Q];
-    int64_t step;
     int chunk_k[Q];
-    __device__ __forceinline__ void init(const uint16_t* p, int64_t s_row, int64_t, int row0, int nrows, int w, int lane) {
+    __device__ __forceinline__ void init(const T* p, int64_t s_row, int64_t, int row0, int nrows, int w, int lane) {
         base = reinterpret_cast<const char*>(p + (int64_t)row0 * s_row);
-        step = 2 * GBK;
 #pragma unroll
         for (int i = 0; i < Q; ++i) {
             const int row = 8 * (w + WAVES * i) + (lane >> 3), c = (lane & 7) ^ swz_x<64>(row);
-            off[i] = (uint32_t)min(row, nrows - 1 - row0) * (uint32_t)(2 * s_row) + 16u * c;
-            chunk_k[i] = 8 * c;
+            off[i] = (uint32_t)min(row, nrows - 1 - row0) * (uint32_t)(EL * s_row) + 16u * c;
+            chunk_k[i] = 16 / EL * c;
         }
     }
-    // slab kt, `left` of its k in the operand (64 or more: all)
+    // slab kt, `left` of its k in the operand (all, or a multiple of a chunk's)
     __device__ __forceinline__ void issue(int kt, int left, uint8_t* lds, int w) const {
-        const char* p = base + kt * step;
-        if (left >= GBK) {
+        const char* p = base + (int64_t)kt * 128;
+        if (left >= kSlab<T>) {
 #pragma unroll
             for (int i = 0; i < Q; ++i) dma16(p, off[i], lds + (w + WAVES * i) * 1024);
         } else {
@@ -72,36 +74,37 @@ struct Operand<R, WAVES, true, GATED> {
         }
     }
 };
-// Contiguous along its rows: as it lies in memory, [64 k][R], chunks permuted within a row of LDS by
-// tr_swizzle.  GATED: column c of the tile is column 32 (c / 64) + c % 32 of one half of the matrix,
-// the second for odd c / 32.
-template <int R, int WAVES, bool GATED>
-struct Operand<R, WAVES, false, GATED> {
-    static constexpr int Q = R / 8 / WAVES, LPR = R / 8;
+// Contiguous along its rows: as it lies in memory, [k of the slab][R], bf16 with its chunks permuted within a
+// row of LDS by tr_swizzle.  GATED: column c of the tile is column 32 (c / 64) + c % 32 of one half of the
+// matrix, the second for odd c / 32.
+template <typename T, int R, int WAVES, bool GATED>
+struct Operand<T, R, WAVES, false, GATED> {
+    static constexpr int EL = sizeof(T), PER = 16 / EL, LPR = R / PER, Q = R / 8 / WAVES;
     const char* base;
     uint32_t off[Q];
     int64_t step;
     int row_k[Q];
-    __device__ __forceinline__ void init(const uint16_t* p, int64_t, int64_t s_k, int col0, int ncols, int w, int lane) {
+    __device__ __forceinline__ void init(const T* p, int64_t, int64_t s_k, int col0, int ncols, int w, int lane) {
         base = reinterpret_cast<const char*>(p);
-        step = 2 * GBK * s_k;
+        step = EL * kSlab<T> * s_k;
 #pragma unroll
         for (int i = 0; i < Q; ++i) {
-            const int idx = (w + WAVES * i) * 64 + lane, k = idx / LPR, c = 8 * ((idx % LPR) ^ tr_swizzle(k, LPR));
+            const int idx = (w + WAVES * i) * 64 + lane, k = idx / LPR, pos = idx % LPR;
+            const int c = PER * (EL == 2 ? pos ^ tr_swizzle(k, LPR) : pos);
             int col;
             if constexpr (GATED) {
                 const int half = ncols / 2;
-                col = min(col0 / 2 + 32 * (c / 64) + c % 32, half - 8) + ((c / 32) & 1) * half;
+                col = min(col0 / 2 + 32 * (c / 64) + c % 32, half - PER) + ((c / 32) & 1) * half;
             } else {
-                col = min(col0 + c, ncols - 8);
+                col = min(col0 + c, ncols - PER);
             }
-            off[i] = (uint32_t)k * (uint32_t)(2 * s_k) + 2u * (uint32_t)col;
+            off[i] = (uint32_t)k * (uint32_t)(EL * s_k) + EL * (uint32_t)col;
             row_k[i] = k;
         }
     }
     __device__ __forceinline__ void issue(int kt, int left, uint8_t* lds, int w) const {
         const char* p = base + kt * step;
-        if (left >= GBK) {
+        if (left >= kSlab<T>) {
 #pragma unroll
             for (int i = 0; i < Q; ++i) dma16(p, off[i], lds + (w + WAVES * i) * 1024);
         } else {
@@ -112,14 +115,55 @@ struct Operand<R, WAVES, false, GATED> {
     }
 };
 
+// Fragments of a slab, 32 rows or columns from `first` and a quarter of its k, and their product.
+template <typename T>
+struct Mul;
+template <>
+struct Mul<uint16_t> {
+    typedef bf16x8 Frag;
+    template <int R, bool KC>
+    __device__ __forceinline__ static Frag read(const uint8_t* lds, int first, int ks, int lane) {
+        return lt_frag<R, KC>(lds, first, ks, lane);
+    }
+    __device__ __forceinline__ static f32x16 add(const Frag& a, const Frag& b, const f32x16& c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+};
+template <>
+struct Mul<float> {
+    struct Frag {
+        float v[4];   // k = 8 ks + 4 (l / 32) + e
+    };
+    template <int R, bool KC>
+    __device__ __forceinline__ static Frag read(const uint8_t* lds, int first, int ks, int lane) {
+        const int l32 = lane & 31, hl = lane >> 5;
+        const float* p = reinterpret_cast<const float*>(lds);
+        Frag f;
+        if constexpr (KC) {
+            const int row = first + l32;
+            const float4 x = *reinterpret_cast<const float4*>(p + row * 32 + 4 * ((2 * ks + hl) ^ swz_x<64>(row)));
+            f.v[0] = x.x; f.v[1] = x.y; f.v[2] = x.z; f.v[3] = x.w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f.v[e] = p[(8 * ks + 4 * hl + e) * R + first + l32];
+        }
+        return f;
+    }
+    __device__ __forceinline__ static f32x16 add(const Frag& a, const Frag& b, f32x16 c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[e], b.v[e], c, 0, 0, 0);
+        return c;
+    }
+};
+
 // BM x BN outputs by PM x PN waves, NS stages
 template <int BM, int BN, int PM, int PN, int NS>
 struct Cfg {
     static constexpr int WAVES = PM * PN, THREADS = 64 * WAVES;
     static constexpr int FM = BM / PM / 32, FN = BN / PN / 32;   // 32 x 32 products of a wave
-    static constexpr int A_BYTES = BM * GBK * 2, STAGE = (BM + BN) * GBK * 2, LDS = NS * STAGE;
+    static constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128, LDS = NS * STAGE;
     static constexpr int LOADS = (BM + BN) / 8 / WAVES;           // a wave's of a slab
-    static constexpr int OUT_BYTES = 32 * 32 * FN * 2;            // a wave's 32 rows of results
+    static constexpr int OUT_BYTES = 32 * 32 * FN * 2;            // a wave's 32 rows of results in bf16
     static constexpr int PER_CU = 160 * 1024 / LDS > 2 ? 2 : 160 * 1024 / LDS;
     static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && FM >= 1 && FN >= 1, "whole loads and products");
     static_assert(WAVES * OUT_BYTES <= STAGE, "results go through a stage");
@@ -153,6 +197,22 @@ __device__ __forceinline__ void put4(uint16_t* p, int left, const float* v) {
             if (e < left) p[e] = y.v[e];
     }
 }
+__device__ __forceinline__ void add4(const float* p, int left, float* v) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += e < left ? p[e] : 0.f;
+}
+struct __attribute__((packed, aligned(4))) FourF {
+    float v[4];
+};
+__device__ __forceinline__ void put4(float* p, int left, const float* v) {
+    if (left >= 4) {
+        __builtin_memcpy(p, v, 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) p[e] = v[e];
+    }
+}
 struct __attribute__((packed, aligned(2))) Eight {
     uint16_t v[8];
 };
@@ -167,10 +227,6 @@ __device__ __forceinline__ void put8(uint16_t* p, int left, const uint4& x) {
             if (e < left) p[e] = y.v[e];
     }
 }
-struct __attribute__((packed, aligned(4))) FourF {
-    float v[4];
-};
-
 // A wave's 32 rows of 32 NF columns through LDS: lane (row l32) puts columns 32 i + 8 q + 4 hl .. + 3, and takes
 // eight of a row, 4 NF lanes side by side.  16-byte chunks are permuted within a row so that rows spread over
 // the banks.
@@ -196,19 +252,21 @@ struct Rows {
     }
 };
 
-template <int BM, int BN, int PM, int PN, int NS, bool A_KC, bool B_KC, int OUT>
-__global__ __launch_bounds__(64 * PM * PN, (Cfg<BM, BN, PM, PN, NS>::PER_CU * PM * PN / 4)) void product_kernel(Args g) {
+template <typename T, int BM, int BN, int PM, int PN, int NS, bool A_KC, bool B_KC, int OUT>
+__global__ __launch_bounds__(64 * PM * PN, (Cfg<BM, BN, PM, PN, NS>::PER_CU * PM * PN / 4)) void product_kernel(Args<T> g) {
     using C = Cfg<BM, BN, PM, PN, NS>;
-    constexpr bool GATED = OUT == kGated;
+    using M = Mul<T>;
+    constexpr bool GATED = OUT == kGated, EXACT = sizeof(T) == 4;
+    constexpr bool ROWS = sizeof(T) == 2 && OUT != kF32;   // results through LDS
     static_assert(!GATED || C::FN == 2, "a wave holds both halves of its columns");
     __shared__ __attribute__((aligned(16))) uint8_t smem[C::LDS];
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hl = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w % PM, wn = w / PM;
     const int total = g.tm * g.tn * g.splits;   // (the host: fewer than 2^24)
-    const int slabs = (g.K + GBK - 1) / GBK;
+    const int slabs = (g.K + kSlab<T> - 1) / kSlab<T>;
 
-    Operand<BM, C::WAVES, A_KC, false> oa;
-    Operand<BN, C::WAVES, B_KC, GATED> ob;
+    Operand<T, BM, C::WAVES, A_KC, false> oa;
+    Operand<T, BN, C::WAVES, B_KC, GATED> ob;
     struct Place {
         int m0, n0, s0, nk;   // first row, column, slab, and the slabs
         int64_t part;
@@ -233,7 +291,7 @@ __global__ __launch_bounds__(64 * PM * PN, (Cfg<BM, BN, PM, PN, NS>::PER_CU * PM
     };
     auto issue = [&](int kt, int stage) __attribute__((always_inline)) {
         uint8_t* st = smem + stage * C::STAGE;
-        const int left = g.K - kt * GBK;
+        const int left = g.K - kt * kSlab<T>;
         oa.issue(kt, left, st, w);
         ob.issue(kt, left, st + C::A_BYTES, w);
     };
@@ -248,23 +306,22 @@ __global__ __launch_bounds__(64 * PM * PN, (Cfg<BM, BN, PM, PN, NS>::PER_CU * PM
     auto mul = [&](int stage) __attribute__((always_inline)) {
         const uint8_t* As = smem + stage * C::STAGE;
         const uint8_t* Bs = As + C::A_BYTES;
-        bf16x8 a[2][C::FM], b[2][C::FN];
-        auto rd = [&](int ks, bf16x8(&ao)[C::FM], bf16x8(&bo)[C::FN]) __attribute__((always_inline)) {
+        typename M::Frag a[2][C::FM], b[2][C::FN];
+        auto rd = [&](int ks, typename M::Frag(&ao)[C::FM], typename M::Frag(&bo)[C::FN]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < C::FN; ++i) bo[i] = lt_frag<BN, B_KC>(Bs, 32 * (C::FN * wn + i), ks, lane);
+            for (int i = 0; i < C::FN; ++i) bo[i] = M::template read<BN, B_KC>(Bs, 32 * (C::FN * wn + i), ks, lane);
 #pragma unroll
-            for (int j = 0; j < C::FM; ++j) ao[j] = lt_frag<BM, A_KC>(As, 32 * (C::FM * wm + j), ks, lane);
+            for (int j = 0; j < C::FM; ++j) ao[j] = M::template read<BM, A_KC>(As, 32 * (C::FM * wm + j), ks, lane);
         };
         rd(0, a[0], b[0]);
 #pragma unroll
-        for (int ks = 0; ks < GBK / 16; ++ks) {
-            if (ks + 1 < GBK / 16) rd(ks + 1, a[(ks + 1) & 1], b[(ks + 1) & 1]);
+        for (int ks = 0; ks < 4; ++ks) {
+            if (ks + 1 < 4) rd(ks + 1, a[(ks + 1) & 1], b[(ks + 1) & 1]);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < C::FM; ++j)
 #pragma unroll
-                for (int i = 0; i < C::FN; ++i)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[ks & 1][i], a[ks & 1][j], acc[i][j], 0, 0, 0);
+                for (int i = 0; i < C::FN; ++i) acc[i][j] = M::add(b[ks & 1][i], a[ks & 1][j], acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -272,122 +329,77 @@ __global__ __launch_bounds__(64 * PM * PN, (Cfg<BM, BN, PM, PN, NS>::PER_CU * PM
     auto write = [&](const Place& p, uint8_t* lds) __attribute__((always_inline)) {
         const Rows<C::FN> wide{lds + w * C::OUT_BYTES};
         const Rows<1> narrow{lds + w * C::OUT_BYTES};
+        // columns n of block i and quarter q, and how many of the matrix there are from there on
+        const int nw = GATED ? p.n0 / 2 + 32 * wn : p.n0 + 32 * C::FN * wn;
+        auto col = [&](int i, int q) __attribute__((always_inline)) { return nw + (GATED ? 0 : 32 * i) + 8 * q + 4 * hl; };
 #pragma unroll
         for (int j = 0; j < C::FM; ++j) {
             const int m0 = p.m0 + 32 * (C::FM * wm + j), m = m0 + l32;
-            if constexpr (OUT == kF32) {
-                if (m >= g.M) continue;
+            const bool row = m < g.M;
+            auto four = [&](int i, int q, float* z) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[e] = acc[i][j][4 * q + e];
+            };
+            if (OUT >= kGated && g.bias) {
 #pragma unroll
                 for (int i = 0; i < C::FN; ++i)
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const int n = p.n0 + 32 * (C::FN * wn + i) + 8 * q + 4 * hl;
-                        float* to = reinterpret_cast<float*>(g.y) + p.part + (int64_t)m * g.N + n;
-                        if (n + 4 <= g.N) {
-                            FourF x{{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]}};
-                            __builtin_memcpy(to, &x, 16);
-                        } else {
+                        float z[4];
+                        four(i, q, z);
+                        add4(g.bias + (GATED ? i * g.F : 0) + col(i, q), g.F - col(i, q), z);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (n + e < g.N) to[e] = acc[i][j][4 * q + e];
-                        }
+                        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = z[e];
                     }
-            } else if constexpr (GATED) {
-                const int nw = p.n0 / 2 + 32 * wn;   // the wave's first column of each half
-                if (g.bias) {
+            }
+            if (OUT >= kGated && g.pre) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < C::FN; ++i)
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const int n = nw + 8 * q + 4 * hl;
-                            float z[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) z[e] = acc[i][j][4 * q + e];
-                            add4(g.bias + i * g.F + n, g.F - n, z);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = z[e];
-                        }
-                }
-                if (g.pre) {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            float z[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) z[e] = acc[i][j][4 * q + e];
-                            wide.put(l32, i, q, hl, z);
-                        }
+                    for (int q = 0; q < 4; ++q) {
+                        float z[4];
+                        four(i, q, z);
+                        if constexpr (ROWS) wide.put(l32, i, q, hl, z);
+                        else if (row) put4(g.pre + (int64_t)m * g.N + (GATED ? i * g.F : 0) + col(i, q), g.F - col(i, q), z);
+                    }
+                if constexpr (ROWS)
                     wide.take(lane, [&](int r, int c, const uint4& x) __attribute__((always_inline)) {
-                        const int n = nw + c % 32;
-                        if (m0 + r < g.M && n < g.F) put8(g.pre + (int64_t)(m0 + r) * g.N + c / 32 * g.F + n, g.F - n, x);
+                        const int n = nw + (GATED ? c % 32 : c);
+                        if (m0 + r < g.M && n < g.F) put8(g.pre + (int64_t)(m0 + r) * g.N + (GATED ? c / 32 * g.F : 0) + n, g.F - n, x);
                     });
-                }
+            }
+#pragma unroll
+            for (int i = 0; i < (GATED ? 1 : C::FN); ++i)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int n = nw + 8 * q + 4 * hl;
+                    const int n = col(i, q);
                     float z[4];
+                    four(i, q, z);
+                    if constexpr (GATED) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) z[e] = activate<false>(acc[0][j][4 * q + e], acc[1][j][4 * q + e], SA_ACT_SWIGLU);
-                    if (g.res && m < g.M) add4(g.res + (int64_t)m * g.F + n, g.F - n, z);
-                    narrow.put(l32, 0, q, hl, z);
+                        for (int e = 0; e < 4; ++e) z[e] = activate<EXACT>(z[e], acc[C::FN - 1][j][4 * q + e], SA_ACT_SWIGLU);
+                    } else if constexpr (OUT > kEpi) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) z[e] = activate<EXACT>(z[e], 0.f, OUT - kEpi);
+                    }
+                    const int64_t o = (int64_t)m * g.F + n;
+                    if (OUT >= kGated && g.res && row) add4(g.res + o, g.F - n, z);
+                    if constexpr (ROWS) {
+                        if constexpr (GATED) narrow.put(l32, 0, q, hl, z);
+                        else wide.put(l32, i, q, hl, z);
+                    } else if constexpr (OUT == kF32) {
+                        if (row) put4(reinterpret_cast<float*>(g.y) + p.part + o, g.F - n, z);
+                    } else {
+                        if (row) put4(reinterpret_cast<T*>(g.y) + o, g.F - n, z);
+                    }
                 }
-                narrow.take(lane, [&](int r, int c, const uint4& x) __attribute__((always_inline)) {
+            if constexpr (ROWS) {
+                auto out = [&](int r, int c, const uint4& x) __attribute__((always_inline)) {
                     const int n = nw + c;
                     if (m0 + r < g.M && n < g.F) put8(reinterpret_cast<uint16_t*>(g.y) + (int64_t)(m0 + r) * g.F + n, g.F - n, x);
-                });
-            } else {
-                const int nw = p.n0 + 32 * C::FN * wn;
-                auto out = [&](uint16_t* to) __attribute__((always_inline)) {
-                    wide.take(lane, [&](int r, int c, const uint4& x) __attribute__((always_inline)) {
-                        const int n = nw + c;
-                        if (m0 + r < g.M && n < g.N) put8(to + (int64_t)(m0 + r) * g.N + n, g.N - n, x);
-                    });
                 };
-                if (OUT >= kEpi && g.bias) {
-#pragma unroll
-                    for (int i = 0; i < C::FN; ++i)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const int n = nw + 32 * i + 8 * q + 4 * hl;
-                            float z[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) z[e] = acc[i][j][4 * q + e];
-                            add4(g.bias + n, g.N - n, z);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = z[e];
-                        }
-                }
-                if (OUT >= kEpi && g.pre) {
-#pragma unroll
-                    for (int i = 0; i < C::FN; ++i)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            float z[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) z[e] = acc[i][j][4 * q + e];
-                            wide.put(l32, i, q, hl, z);
-                        }
-                    out(g.pre);
-                }
-#pragma unroll
-                for (int i = 0; i < C::FN; ++i)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int n = nw + 32 * i + 8 * q + 4 * hl;
-                        float z[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) z[e] = acc[i][j][4 * q + e];
-                        if constexpr (OUT >= kEpi) {
-                            if constexpr (OUT != kEpi + SA_ACT_NONE) {
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) z[e] = activate<false>(z[e], 0.f, OUT - kEpi);
-                            }
-                            if (g.res && m < g.M) add4(g.res + (int64_t)m * g.N + n, g.N - n, z);
-                        }
-                        wide.put(l32, i, q, hl, z);
-                    }
-                out(reinterpret_cast<uint16_t*>(g.y));
+                if constexpr (GATED) narrow.take(lane, out);
+                else wide.take(lane, out);
             }
         }
     };
@@ -427,14 +439,14 @@ __global__ __launch_bounds__(64 * PM * PN, (Cfg<BM, BN, PM, PN, NS>::PER_CU * PM
         if (NS > 2 && loaded == NS - 1) wait_loads<(NS - 2) * C::LOADS>();
         else wait_loads<0>();
         if (++kt == p.nk) {
-            if (OUT != kF32) barrier();   // every wave is done with the stage that the results go through
+            if (ROWS) barrier();   // every wave is done with the stage that the results go through
             write(p, smem + stage * C::STAGE);
             v += gridDim.x;
             if (v >= total) break;
             p = place(v);
             kt = 0;
             zero();
-            if (OUT != kF32) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (ROWS) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
         stage = stage == NS - 1 ? 0 : stage + 1;
         barrier();
@@ -447,7 +459,7 @@ __global__ __launch_bounds__(64 * PM * PN, (Cfg<BM, BN, PM, PN, NS>::PER_CU * PM
 constexpr int kFewStages = 2;
 // B_KC: B's columns come straight into registers, like x's rows.
 template <bool B_KC, int OUT>
-__global__ __launch_bounds__(512, 2) void few_rows_kernel(Args g) {
+__global__ __launch_bounds__(512, 2) void few_rows_kernel(Args<uint16_t> g) {
     constexpr bool GATED = OUT == kGated;
     constexpr int FN = GATED ? 2 : 1, SLAB = GBK * 32 * 2;   // bytes of 64 k by 32 columns
     constexpr int RING = B_KC ? 0 : 8 * kFewStages * FN * SLAB, SUMS = 8 * FN * 16 * 64 * 4;
@@ -493,8 +505,8 @@ __global__ __launch_bounds__(512, 2) void few_rows_kernel(Args g) {
         if constexpr (!B_KC) issue(w, 0);
     }
     for (int kt = w; kt < slabs; kt += 8) {
-        if (kt + 8 < slabs) load_x(xn, kt + 8);
         if constexpr (B_KC) {
+            if (kt + 8 < slabs) load_x(xn, kt + 8);
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks)
                 acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x.b[ks]),
@@ -502,9 +514,11 @@ __global__ __launch_bounds__(512, 2) void few_rows_kernel(Args g) {
             x = xn;
             continue;
         }
+        // (counted: W's loads alone, which are always as many; x's next are on their way after the wait)
         if (kt + 8 < slabs) {
             issue(kt + 8, stage ^ 1);
-            wait_loads<4 + 4 * FN>();
+            wait_loads<4 * FN>();
+            load_x(xn, kt + 8);
         } else {
             wait_loads<0>();
         }
@@ -555,7 +569,7 @@ __global__ __launch_bounds__(512, 2) void few_rows_kernel(Args g) {
     if constexpr (GATED) sum(u, 1);
     const int64_t o = (int64_t)m * g.F + n;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = activate<false>(z[e], u[e], GATED ? SA_ACT_SWIGLU : OUT >= kEpi ? OUT - kEpi : SA_ACT_NONE);
+    for (int e = 0; e < 4; ++e) z[e] = activate<false>(z[e], u[e], GATED ? SA_ACT_SWIGLU : OUT > kEpi ? OUT - kEpi : SA_ACT_NONE);
     if (g.res) add4(g.res + o, g.F - n, z);
     put4(reinterpret_cast<uint16_t*>(g.y) + o, g.F - n, z);
 }
@@ -563,10 +577,11 @@ __global__ __launch_bounds__(512, 2) void few_rows_kernel(Args g) {
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-Args args_of(const Product& p, int bm, int bn) {
-    Args g;
-    g.A = reinterpret_cast<const uint16_t*>(p.A);
-    g.B = reinterpret_cast<const uint16_t*>(p.B);
+template <typename T>
+Args<T> args_of(const Product& p, int bm, int bn) {
+    Args<T> g;
+    g.A = reinterpret_cast<const T*>(p.A);
+    g.B = reinterpret_cast<const T*>(p.B);
     g.a_m = p.a_m; g.a_k = p.a_k; g.b_k = p.b_k; g.b_n = p.b_n;
     g.M = p.M; g.N = p.N; g.K = p.K;
     g.ma = p.ma; g.nb = p.nb;
@@ -577,18 +592,18 @@ Args args_of(const Product& p, int bm, int bn) {
     g.splits = p.splits;
     g.per = p.per;
     g.y = p.y;
-    g.bias = p.epi ? reinterpret_cast<const uint16_t*>(p.epi->bias) : nullptr;
-    g.res = p.epi ? reinterpret_cast<const uint16_t*>(p.epi->res) : nullptr;
-    g.pre = p.epi ? reinterpret_cast<uint16_t*>(p.epi->pre) : nullptr;
+    g.bias = p.epi ? reinterpret_cast<const T*>(p.epi->bias) : nullptr;
+    g.res = p.epi ? reinterpret_cast<const T*>(p.epi->res) : nullptr;
+    g.pre = p.epi ? reinterpret_cast<T*>(p.epi->pre) : nullptr;
     g.act = p.epi ? p.epi->act : SA_ACT_NONE;
     return g;
 }
 
 hipError_t launch_few_rows(const Product& p, hipStream_t stream) {
-    const Args g = args_of(p, 32, 64);
+    const Args<uint16_t> g = args_of<uint16_t>(p, 32, 64);
     const dim3 grid((unsigned)cdiv(g.F, 32), (unsigned)cdiv(p.M, 32));
 #define SA_RUN(OUT) hipLaunchKernelGGL((few_rows_kernel<false, OUT>), grid, dim3(512), 0, stream, g)
-    if (p.b_k == 1) hipLaunchKernelGGL((few_rows_kernel<true, kBf16>), grid, dim3(512), 0, stream, g);
+    if (p.b_k == 1) hipLaunchKernelGGL((few_rows_kernel<true, kPlain>), grid, dim3(512), 0, stream, g);
     else switch (g.act) {
         case SA_ACT_RELU: SA_RUN(kEpi + SA_ACT_RELU); break;
         case SA_ACT_GELU: SA_RUN(kEpi + SA_ACT_GELU); break;
@@ -600,15 +615,15 @@ hipError_t launch_few_rows(const Product& p, hipStream_t stream) {
     return hipGetLastError();
 }
 
-template <int BM, int BN, int PM, int PN, int NS>
+template <typename T, int BM, int BN, int PM, int PN, int NS>
 hipError_t launch_t(const Product& p, hipStream_t stream) {
     using C = Cfg<BM, BN, PM, PN, NS>;
-    const Args g = args_of(p, BM, BN);
+    const Args<T> g = args_of<T>(p, BM, BN);
     const bool gated = g.act == SA_ACT_SWIGLU;
     const dim3 grid((unsigned)std::min<int64_t>((int64_t)g.tm * g.tn * g.splits, (int64_t)device_cus() * C::PER_CU));
     const bool a_kc = p.a_k == 1, b_kc = p.b_k == 1;
 #define SA_RUN(AK, BK, OUT) \
-    hipLaunchKernelGGL((product_kernel<BM, BN, PM, PN, NS, AK, BK, OUT>), grid, dim3(C::THREADS), 0, stream, g)
+    hipLaunchKernelGGL((product_kernel<T, BM, BN, PM, PN, NS, AK, BK, OUT>), grid, dim3(C::THREADS), 0, stream, g)
     if (p.epi) {
         if (gated) {
             if constexpr (C::FN == 2) SA_RUN(true, false, kGated);
@@ -622,13 +637,13 @@ hipError_t launch_t(const Product& p, hipStream_t stream) {
             }
         }
     } else if (a_kc && b_kc) {
-        SA_RUN(true, true, kBf16);
-    } else if constexpr (BM % 64 != 0 || BM == 192) {   // (rows of LDS that tr_swizzle permutes: powers of two)
+        SA_RUN(true, true, kPlain);
+    } else if constexpr (BM == 192) {   // (rows of LDS that tr_swizzle permutes: powers of two)
         return hipErrorInvalidValue;
-    } else if (p.y_bf16) {
-        SA_RUN(false, false, kBf16);
-    } else {
+    } else if (sizeof(T) == 4 || !p.y_bf16) {
         SA_RUN(false, false, kF32);
+    } else {
+        if constexpr (sizeof(T) == 2) SA_RUN(false, false, kPlain);
     }
 #undef SA_RUN
     return hipGetLastError();
@@ -638,19 +653,20 @@ hipError_t launch_t(const Product& p, hipStream_t stream) {
 
 bool product_supported(const Product& p) {
     const bool a_kc = p.a_k == 1, b_kc = p.b_k == 1;
+    const int64_t el = p.bf16 ? 2 : 4, piece = 16 / el;
     if (!al16(p.A) || !al16(p.B) || p.M < 1 || p.N < 1 || p.K < 1) return false;
-    if ((a_kc ? p.a_m : p.a_k) % 8 != 0 || (b_kc ? p.b_n : p.b_k) % 8 != 0) return false;
-    if ((a_kc || b_kc) && p.K % 8 != 0) return false;
-    if (!a_kc && (p.a_m != 1 || p.ma % 8 != 0 || p.ma < 8)) return false;
-    if (!b_kc && (p.b_n != 1 || p.nb % 8 != 0 || p.nb < 8)) return false;
+    if ((a_kc ? p.a_m : p.a_k) % piece != 0 || (b_kc ? p.b_n : p.b_k) % piece != 0) return false;
+    if ((a_kc || b_kc) && p.K % piece != 0) return false;
+    if (!a_kc && (p.a_m != 1 || p.ma % piece != 0 || p.ma < piece)) return false;
+    if (!b_kc && (p.b_n != 1 || p.nb % piece != 0 || p.nb < piece)) return false;
     if (p.epi) {
-        if (!a_kc || b_kc || (p.epi->act == SA_ACT_SWIGLU && p.nb % 16 != 0)) return false;
-    } else if (a_kc != b_kc || (a_kc && !p.y_bf16)) {
+        if (!a_kc || b_kc || (p.epi->act == SA_ACT_SWIGLU && p.nb % (2 * piece) != 0)) return false;
+    } else if (a_kc != b_kc || (a_kc && p.bf16 != p.y_bf16)) {
         return false;
     }
-    // a lane's offsets within a tile's slab are 32-bit bytes: 256 rows, or 64 k and all columns
-    auto fits = [](bool kc, int64_t rows, int64_t s_row, int64_t s_k) {
-        return kc ? 256 * s_row * 2 + 128 < (int64_t(1) << 32) : 64 * s_k * 2 + 2 * rows < (int64_t(1) << 32);
+    // a lane's offsets within a tile's slab are 32-bit bytes: 256 rows, or a slab's k and all columns
+    auto fits = [&](bool kc, int64_t rows, int64_t s_row, int64_t s_k) {
+        return kc ? 256 * s_row * el + 128 < (int64_t(1) << 32) : (128 / el) * s_k * el + el * rows < (int64_t(1) << 32);
     };
     return fits(a_kc, p.ma, p.a_m, p.a_k) && fits(b_kc, p.nb, p.b_n, p.b_k) &&
            cdiv(p.M, 64) * cdiv(p.N, 64) * p.splits < (int64_t(1) << 24);
@@ -661,6 +677,7 @@ namespace {
 // Tile shapes: rows, columns, microseconds a slab of 64 k takes a compute unit at best, where its
 // workgroups wait for one slab after the other, and microseconds of writing a tile's results.
 // Measured on 8192 x 8192 x 8192, 40,000 x 1,024 x 4,096 and, for the waiting, 16 to 1,000 x 1,024 x 1,024.
+// fp32: slabs of 32 k, sixteen times the matrix instructions' time.
 struct Shape {
     int bm, bn;
     double busy, alone, results;
@@ -669,19 +686,21 @@ struct Shape {
 constexpr Shape kShapes[] = {{256, 256, 1.79, 1.56, 5.0, true}, {192, 256, 1.36, 1.28, 3.7, false},
                              {128, 256, 1.02, 0.88, 2.5, true}, {256, 128, 1.02, 0.88, 2.5, true},
                              {128, 128, 0.52, 0.76, 1.2, true}, {64, 64, 0.31, 0.52, 0.4, true}};
-constexpr int kNumShapes = sizeof(kShapes) / sizeof(kShapes[0]);
+constexpr Shape kShapes32[] = {{128, 128, 3.1, 3.1, 2.4, true}, {64, 64, 0.8, 0.8, 0.6, true}};
+constexpr int kNumShapes = sizeof(kShapes) / sizeof(kShapes[0]), kNumShapes32 = sizeof(kShapes32) / sizeof(kShapes32[0]);
 
 // estimated time of a product: what the compute unit with the most tiles takes
 double estimate(const Product& p, const Shape& t) {
-    const int32_t slabs = (int32_t)std::min<int64_t>(p.per, cdiv(p.K, GBK));
+    const int32_t slabs = (int32_t)std::min<int64_t>(p.per, cdiv(p.K, p.bf16 ? 64 : 32));
     const int64_t n = cdiv(cdiv(p.M, t.bm) * cdiv(p.N, t.bn) * p.splits, device_cus());
     return std::max(n * t.busy, t.alone) * slabs + n * t.results;
 }
 int choose(const Product& p, double* time) {
     int best = -1;
-    for (int i = 0; i < kNumShapes; ++i) {
-        if (p.a_k != 1 && !kShapes[i].rows_ok) continue;
-        const double e = estimate(p, kShapes[i]);
+    const Shape* shapes = p.bf16 ? kShapes : kShapes32;
+    for (int i = 0; i < (p.bf16 ? kNumShapes : kNumShapes32); ++i) {
+        if (p.a_k != 1 && !shapes[i].rows_ok) continue;
+        const double e = estimate(p, shapes[i]);
         if (best < 0 || e < *time) {
             best = i;
             *time = e;
@@ -693,7 +712,7 @@ int choose(const Product& p, double* time) {
 }  // namespace
 
 void choose_splits(Product* p) {
-    const int32_t slabs = (int32_t)cdiv(p->K, GBK);
+    const int32_t slabs = (int32_t)cdiv(p->K, p->bf16 ? 64 : 32);
     double least = 0;
     int32_t splits = 1, per = slabs;
     for (int32_t s = 1; s <= 16 && s * 4 <= std::max(slabs, 4); ++s) {
@@ -713,23 +732,38 @@ void choose_splits(Product* p) {
     p->per = per;
 }
 
+namespace {
+
+// few rows (a tile of 64 by 64 columns, k = 1024, takes 13 us, 4 of which are not its slabs'): 16, 64, 256 rows by
+// 1,024 columns 4.2, 5.2, 5.9 us, 128 by 4,096 9.1; 64 and 256 by 1,024 with k = 4096 12.0 and 13.8 (tiles: 40)
+double few_rows_time(const Product& p) {
+    if (!p.bf16 || p.a_k != 1 || p.splits != 1) return 1e30;
+    const int64_t n = cdiv(cdiv(p.N, 32) * cdiv(p.M, 32), device_cus());
+    return 2.6 + 1.6 * n * cdiv(p.K, 8 * GBK);
+}
+
+}  // namespace
+
+double product_time(const Product& p) {
+    double time = 0;
+    choose(p, &time);
+    return std::min(4.0 + time, few_rows_time(p));
+}
+
 hipError_t launch_product(const Product& p, hipStream_t stream) {
     if (!product_supported(p)) return hipErrorInvalidValue;
     double time = 0;
     const int shape = choose(p, &time);
-    // few rows (a tile of 64 by 64 columns, k = 1024, takes 13 us, 4 of which are not its slabs'): 16, 64, 256 rows by
-    // 1,024 columns 4.2, 5.2, 5.9 us, 128 by 4,096 9.1; 64 and 256 by 1,024 with k = 4096 12.0 and 13.8 (tiles: 40)
-    if (p.a_k == 1 && p.splits == 1) {
-        const int64_t n = cdiv(cdiv(p.N, 32) * cdiv(p.M, 32), device_cus());
-        if (2.6 + 1.6 * n * cdiv(p.K, 8 * GBK) < 4.0 + time) return launch_few_rows(p, stream);
-    }
+    if (!p.bf16)
+        return shape == 0 ? launch_t<float, 128, 128, 2, 2, 2>(p, stream) : launch_t<float, 64, 64, 2, 1, 4>(p, stream);
+    if (few_rows_time(p) < 4.0 + time) return launch_few_rows(p, stream);
     switch (shape) {
-        case 0: return launch_t<256, 256, 2, 4, 2>(p, stream);
-        case 1: return launch_t<192, 256, 2, 4, 2>(p, stream);
-        case 2: return launch_t<128, 256, 2, 4, 3>(p, stream);
-        case 3: return launch_t<256, 128, 4, 2, 3>(p, stream);
-        case 4: return launch_t<128, 128, 4, 2, 2>(p, stream);
-        default: return launch_t<64, 64, 2, 1, 4>(p, stream);
+        case 0: return launch_t<uint16_t, 256, 256, 2, 4, 2>(p, stream);
+        case 1: return launch_t<uint16_t, 192, 256, 2, 4, 2>(p, stream);
+        case 2: return launch_t<uint16_t, 128, 256, 2, 4, 3>(p, stream);
+        case 3: return launch_t<uint16_t, 256, 128, 4, 2, 3>(p, stream);
+        case 4: return launch_t<uint16_t, 128, 128, 4, 2, 2>(p, stream);
+        default: return launch_t<uint16_t, 64, 64, 2, 1, 4>(p, stream);
     }
 }
 

@@ -155,7 +155,7 @@ def lib() -> ctypes.CDLL:
     L.sa_layer_norm_bwd.argtypes = [vp, i64, vp, vp, vp, i64, i32, c.c_int, vp, vp, vp, vp, sz, vp]
     L.sa_layer_norm_bwd.restype = c.c_int
     for nm in ("sa_linear_fwd_workspace_size", "sa_linear_bwd_workspace_size"):
-        getattr(L, nm).argtypes = [i64, i32, i32, c.c_int, c.c_int]
+        getattr(L, nm).argtypes = [i64, i32, i32, c.c_int, c.c_int, i64]
         getattr(L, nm).restype = sz
     L.sa_linear_fwd.argtypes = [vp, i64, vp, vp, vp, i64, i32, i32, c.c_int, c.c_int, vp, vp, vp, sz, vp]
     L.sa_linear_fwd.restype = c.c_int
@@ -1022,7 +1022,7 @@ def linear_fwd(x, W, bias=None, act: str = "none", residual=None, y=None, want_p
         else:
             _is(y, "y", (N, F), dt, dev)
         pre = torch.empty((N, C), dtype=dt, device=dev) if want_pre else None
-        ws = _buffer(_bytes_of("sa_linear_fwd_workspace_size", dev.index, N, K, F, acode, code), dev, workspace)
+        ws = _buffer(_bytes_of("sa_linear_fwd_workspace_size", dev.index, N, K, F, acode, code, ld), dev, workspace)
         rc = _lib.sa_linear_fwd(x.data_ptr(), ld, W.data_ptr(), _ptr(bias), _ptr(residual), N, K, F, acode, code, y.data_ptr(),
                                 _ptr(pre), _ptr(ws), _bytes_given(ws), _handle(dev, stream))
     _check(rc)
@@ -1047,7 +1047,7 @@ def linear_bwd(x, W, dy, bias: bool = False, act: str = "none", pre=None, weight
         g = {"dx": torch.empty((N, K), dtype=dt, device=dev), "dW": torch.empty((K, C), dtype=wdt, device=dev)}
         if bias:
             g["db"] = torch.empty(C, dtype=wdt, device=dev)
-        ws = _buffer(_bytes_of("sa_linear_bwd_workspace_size", dev.index, N, K, F, acode, code), dev, workspace)
+        ws = _buffer(_bytes_of("sa_linear_bwd_workspace_size", dev.index, N, K, F, acode, code, ld), dev, workspace)
         rc = _lib.sa_linear_bwd(x.data_ptr(), ld, W.data_ptr(), _ptr(pre), dy.data_ptr(), N, K, F, acode, code,
                                 g["dx"].data_ptr(), g["dW"].data_ptr(), _ptr(g.get("db")), _dtype_code(g["dW"]), _ptr(ws),
                                 _bytes_given(ws), _handle(dev, stream))

@@ -113,7 +113,9 @@ def test_norm_without_rows(sa):
 
 
 LINEAR = [(1, 1, 1), (1, 64, 64), (1, 1024, 1024), (2, 256, 512), (5, 200, 331), (64, 64, 64), (100, 128, 96), (130, 72, 40),
-          (257, 320, 264), (300, 512, 1024), (1000, 63, 65), (77, 1030, 128), (16, 192, 8), (3, 4096, 24)]
+          (257, 320, 264), (300, 512, 1024), (1000, 63, 65), (77, 1030, 128), (16, 192, 8), (3, 4096, 24),
+          # sizes that run on copies padded to whole pieces, and tiles whose last rows, columns and k end inside
+          (96, 1024, 256), (200, 1096, 600), (700, 1001, 903), (1300, 999, 640), (900, 640, 1111)]
 ACTS = ["none", "relu", "gelu", "silu", "swiglu"]
 
 
