@@ -11,6 +11,7 @@
 #include "linear_gemm.h"
 
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm_tiles.h"
 
@@ -121,10 +122,12 @@ struct Mul;
 template <>
 struct Mul<uint16_t> {
     typedef bf16x8 Frag;
+    static constexpr int STEPS = 1;
     template <int R, bool KC>
     __device__ __forceinline__ static Frag read(const uint8_t* lds, int first, int ks, int lane) {
         return lt_frag<R, KC>(lds, first, ks, lane);
     }
+    template <int STEP>
     __device__ __forceinline__ static f32x16 add(const Frag& a, const Frag& b, const f32x16& c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     }
@@ -132,8 +135,9 @@ struct Mul<uint16_t> {
 template <>
 struct Mul<float> {
     struct Frag {
-        float v[4];   // k = 8 ks + 4 (l / 32) + e
+        float v[4];   // k = 8 ks + 4 (l / 32) + step
     };
+    static constexpr int STEPS = 4;
     template <int R, bool KC>
     __device__ __forceinline__ static Frag read(const uint8_t* lds, int first, int ks, int lane) {
         const int l32 = lane & 31, hl = lane >> 5;
@@ -149,10 +153,9 @@ struct Mul<float> {
         }
         return f;
     }
-    __device__ __forceinline__ static f32x16 add(const Frag& a, const Frag& b, f32x16 c) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[e], b.v[e], c, 0, 0, 0);
-        return c;
+    template <int STEP>
+    __device__ __forceinline__ static f32x16 add(const Frag& a, const Frag& b, const f32x16& c) {
+        return __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[STEP], b.v[STEP], c, 0, 0, 0);
     }
 };
 
@@ -318,10 +321,19 @@ __global__ __launch_bounds__(64 * PM * PN, (Cfg<BM, BN, PM, PN, NS>::PER_CU * PM
         for (int ks = 0; ks < 4; ++ks) {
             if (ks + 1 < 4) rd(ks + 1, a[(ks + 1) & 1], b[(ks + 1) & 1]);
             __builtin_amdgcn_sched_barrier(0);
+            auto step = [&](auto e) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < C::FM; ++j)
+                for (int j = 0; j < C::FM; ++j)
 #pragma unroll
-                for (int i = 0; i < C::FN; ++i) acc[i][j] = M::add(b[ks & 1][i], a[ks & 1][j], acc[i][j]);
+                    for (int i = 0; i < C::FN; ++i)
+                        acc[i][j] = M::template add<decltype(e)::value>(b[ks & 1][i], a[ks & 1][j], acc[i][j]);
+            };
+            step(std::integral_constant<int, 0>{});
+            if constexpr (M::STEPS == 4) {
+                step(std::integral_constant<int, 1>{});
+                step(std::integral_constant<int, 2>{});
+                step(std::integral_constant<int, 3>{});
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -686,7 +698,7 @@ struct Shape {
 constexpr Shape kShapes[] = {{256, 256, 1.79, 1.56, 5.0, true}, {192, 256, 1.36, 1.28, 3.7, false},
                              {128, 256, 1.02, 0.88, 2.5, true}, {256, 128, 1.02, 0.88, 2.5, true},
                              {128, 128, 0.52, 0.76, 1.2, true}, {64, 64, 0.31, 0.52, 0.4, true}};
-constexpr Shape kShapes32[] = {{128, 128, 3.1, 3.1, 2.4, true}, {64, 64, 0.8, 0.8, 0.6, true}};
+constexpr Shape kShapes32[] = {{128, 128, 1.89, 2.1, 2.4, true}, {64, 64, 0.72, 0.62, 0.6, true}};
 constexpr int kNumShapes = sizeof(kShapes) / sizeof(kShapes[0]), kNumShapes32 = sizeof(kShapes32) / sizeof(kShapes32[0]);
 
 // estimated time of a product: what the compute unit with the most tiles takes
