@@ -11,6 +11,7 @@
 #include <algorithm>
 
 #include "recent_attn.h"
+#include "reduce_ops.h"
 
 namespace sa {
 namespace attn {
@@ -221,6 +222,24 @@ __global__ __launch_bounds__(256, (FusedCfg<T, D>::PER_CU)) void fused_kernel(Fu
                     f32x16 s = f32x16{}, ds = f32x16{};
                     M::with_rows(s, qt, kf, lane);
                     M::with_rows(ds, dt, vf, lane);
+                    // Rows whose tokens are all here: delta from their own p and dP.  (<dout, out> has the rounding
+                    // of out, as far off as ds's own where few tokens share a result.)
+                    if (__builtin_amdgcn_ballot_w64(live && lo >= k0 && hi <= kn)) {
+                        float pd[16];
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int row = 32 * t + srow(r, hl);
+                            float x = a.cap > 0.f ? capped<T>(s[r], to_exp, inv_cap, cap2, nullptr) : s[r] * (a.scale * kLog2e);
+                            x = __builtin_fmaf(st.slope2[row], (float)(key + 1 - st.hi[row]), x);
+                            const bool in = key >= st.lo[row] && key < st.hi[row];
+                            pd[r] = in ? exp2_(x - st.lse2[row]) * ds[r] : 0.f;
+                        }
+                        // (lanes 2 r, 2 r + 1 of each half: the sum of register r's row)
+                        const float sum = half_sum16(pd, l32);
+                        const int row = 32 * t + srow(l32 >> 1, hl);
+                        if ((lane & 1) == 0 && st.hi[row] > st.lo[row] && st.lo[row] >= k0 && st.hi[row] <= kn) st.delta[row] = sum;
+                        wave_lds_order();
+                    }
                     float cc = a.scale * kLog2e;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
