@@ -144,6 +144,47 @@ __device__ inline void seen(const View& a, const User& u, int64_t i, int32_t* lo
     *lo = a.window > 0 && e > a.window ? e - a.window : 0;
 }
 
+// Whether any of n times 16 bytes of values is no number, from the largest of their sizes
+template <typename T, int N>
+__device__ inline bool any_bad(const uint4 (&x)[N]) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    if constexpr (sizeof(T) == 2) {
+        u16x2 top = {0, 0};
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[e] & 0x7fff7fffu));
+        }
+        return top.x >= 0x7f80u || top.y >= 0x7f80u;
+    } else {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = max(top, v[e] & 0x7fffffffu);
+        }
+        return top >= 0x7f800000u;
+    }
+}
+
+// Zeros for those of 16 bytes of values that are no numbers; whether there were any.  In a product whose other
+// factor is 0 for a row that does not see the value, it would be a NaN all the same.
+template <typename T>
+__device__ inline bool zero_bad(uint4& x) {
+    uint32_t v[4] = {x.x, x.y, x.z, x.w};
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const bool hi = (v[e] & 0x7f800000u) == 0x7f800000u, lo = sizeof(T) == 2 && (v[e] & 0x7f80u) == 0x7f80u;
+        bad = bad || hi || lo;
+        v[e] = sizeof(T) == 4 ? (hi ? 0u : v[e]) : v[e] & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
+    }
+    x = make_uint4(v[0], v[1], v[2], v[3]);
+    return bad;
+}
+
 __device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ inline float swap_halves(float v, float (*f)(float, float)) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -242,6 +283,15 @@ struct Tile32<uint16_t, D> {
             for (int h2 = 0; h2 < 2; ++h2)
                 c[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_tr_tokens<D>(tile, lane, i, h2), p.v[h2], c[i], 0, 0, 0);
     }
+    __device__ static bool finite(const Frag& f) {
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            uint4 x = __builtin_bit_cast(uint4, f.v[i]);
+            bad = zero_bad<uint16_t>(x) || bad;
+        }
+        return !bad;
+    }
     // values 4 j .. 4 j + 3 of a row
     __device__ static void store4(uint16_t* p, const float* v) {
         *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
@@ -302,6 +352,15 @@ struct Tile32<float, D> {
                 c[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(tile[at(row, 8 * i + (l32 >> 2)) + (l32 & 3)], p.v[r], c[i], 0, 0, 0);
         }
     }
+    __device__ static bool finite(const Frag& f) {
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+            uint4 x = __builtin_bit_cast(uint4, f.v[i]);
+            bad = zero_bad<float>(x) || bad;
+        }
+        return !bad;
+    }
     __device__ static void store4(float* p, const float* v) {
         *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
     }
@@ -333,6 +392,20 @@ __device__ inline float dot_of(const float* a, const float* b, int n) {
     return s;
 }
 
+// whether n values in memory, whole 16 bytes of them, are numbers
+template <typename T>
+__device__ inline bool all_finite(const T* a, int n) {
+    bool bad = false;
+    for (int i = 0; i < n; i += 16 / (int)sizeof(T)) {
+        uint4 x = *reinterpret_cast<const uint4*>(a + i);
+        bad = zero_bad<T>(x) || bad;
+    }
+    return !bad;
+}
+__device__ inline float to_float(uint16_t x) { return bf16_lo(x); }
+__device__ inline float to_float(float x) { return x; }
+__device__ inline bool is_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+
 // A capped score (in units of log 2) and, for the backward, the cap's derivative:
 //   cap tanh(x / cap) = cap (1 - 2 / (1 + exp(2 x / cap))).
 // That form's error is of the order of cap 2^-24 whatever x is; single precision takes tanh itself,
@@ -353,7 +426,7 @@ struct RowsArgs {
     void* out;               // forward: [N,h,d]; else dq, at dq_t, dq_h
     float* lse;              // [N,h]; the backward's input
     const void *o, *dout;    // backward: [N,h,d]
-    float* delta;            // backward: <dout, out> of every row, written
+    float* delta;            // backward: <dout, out> of every row, written; no number where q has any that is none
     int64_t dq_t, dq_h;
     float* parts;            // [2 grid][bq][d + 2]: results of pieces that are not whole tiles
     Begun* begun;            // [grid]
@@ -366,6 +439,14 @@ struct RowsShape {
 RowsShape rows_shape(bool bf16, int32_t d, bool wide, bool bwd);
 hipError_t launch_rows_fwd(const RowsArgs& f, bool bf16, int32_t d, bool wide, hipStream_t stream);
 hipError_t launch_rows_dq(const RowsArgs& f, bool bf16, int32_t d, bool wide, hipStream_t stream);
+
+// A row's log-sum-exp in units of log 2 for exp2(s - lse2), on the keys' side: +inf where it has no weights; a NaN
+// where q, dout or what it sees hold what is no number (its statistics say so), and so are its gradients.
+// Both kinds' q and dout are taken as zeros.
+__device__ inline float row_lse2(bool live, float lse, float delta) {
+    if (!live || lse == -__builtin_inff()) return __builtin_inff();
+    return is_finite(lse) && is_finite(delta) ? lse * kLog2e : __builtin_nanf("");
+}
 
 // The keys' side of the backward
 struct KeysArgs {

@@ -156,7 +156,7 @@ __global__ __launch_bounds__(256, (FusedCfg<T, D>::PER_CU)) void fused_kernel(Fu
             }
             // statistics, four threads a row (of 64)
             const int r = tid >> 2, part = tid & 3;
-            float lse2 = __builtin_inff(), delta = 0.f, slope2 = 0.f;
+            float lse = 0.f, delta = 0.f, slope2 = 0.f;
             int32_t lo = 0, hi = 0;
             if (r < rows) {
                 const int64_t target = us.t0 + r / a.g;
@@ -169,13 +169,15 @@ __global__ __launch_bounds__(256, (FusedCfg<T, D>::PER_CU)) void fused_kernel(Fu
                     const T* op = reinterpret_cast<const T*>(f.o) + o * D + part * (D / 4);
                     const T* dp = reinterpret_cast<const T*>(f.dout) + o * D + part * (D / 4);
                     delta = dot_of(op, dp, D / 4);
-                    const float lse = f.lse[o];
-                    if (lse != -__builtin_inff()) lse2 = lse * kLog2e;
+                    lse = f.lse[o];
+                    const T* qp = reinterpret_cast<const T*>(a.q) + target * a.q_t + head * a.q_h + part * (D / 4);
+                    if (!all_finite(qp, D / 4)) delta = __builtin_nanf("");
                     if (a.slopes) slope2 = a.slopes[head] * kLog2e;
                 }
             }
             delta += __shfl_xor(delta, 1, 64);
             delta += __shfl_xor(delta, 2, 64);
+            const float lse2 = row_lse2(hi > lo, lse, delta);
             if (part == 0) {
                 st.lse2[r] = lse2;
                 st.delta[r] = delta;
@@ -183,8 +185,14 @@ __global__ __launch_bounds__(256, (FusedCfg<T, D>::PER_CU)) void fused_kernel(Fu
                 st.lo[r] = lo;
                 st.hi[r] = hi;
             }
+            // rows without weights, or with no numbers: zeros too
+            if (__syncthreads_or(hi > lo && !(lse2 < __builtin_inff()))) {
+                for (int x = tid; x < kFusedRows * M::CHUNKS; x += 256)
+                    if (!(st.lse2[x / M::CHUNKS] < __builtin_inff()))
+                        reinterpret_cast<uint4*>(rows_q)[x] = reinterpret_cast<uint4*>(rows_d)[x] = make_uint4(0, 0, 0, 0);
+                __syncthreads();
+            }
         }
-        __syncthreads();
 
         f32x16 dq[kTiles][D / 32];
 #pragma unroll
@@ -222,6 +230,7 @@ __global__ __launch_bounds__(256, (FusedCfg<T, D>::PER_CU)) void fused_kernel(Fu
                     f32x16 s = f32x16{}, ds = f32x16{};
                     M::with_rows(s, qt, kf, lane);
                     M::with_rows(ds, dt, vf, lane);
+                    const uint64_t bad = __builtin_amdgcn_ballot_w64(!is_finite(s[0]));   // 0 times what is no number is none
                     // Rows whose tokens are all here: delta from their own p and dP.  (<dout, out> has the rounding
                     // of out, as far off as ds's own where few tokens share a result.)
                     if (__builtin_amdgcn_ballot_w64(live && lo >= k0 && hi <= kn)) {
@@ -266,15 +275,6 @@ __global__ __launch_bounds__(256, (FusedCfg<T, D>::PER_CU)) void fused_kernel(Fu
                         }
                         cc = 1.f;
                     }
-                    if (!whole) {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const int row = 32 * t + srow(r, hl);
-                            const bool in = key >= st.lo[row] && key < st.hi[row] && key < last;
-                            s[r] = in ? s[r] : -__builtin_inff();
-                            ds[r] = in ? ds[r] : 0.f;
-                        }
-                    }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const float4 ls = *reinterpret_cast<const float4*>(&st.lse2[32 * t + 8 * j + 4 * hl]);
@@ -283,6 +283,22 @@ __global__ __launch_bounds__(256, (FusedCfg<T, D>::PER_CU)) void fused_kernel(Fu
                         for (int e = 0; e < 4; ++e) {
                             s[4 * j + e] = exp2_(__builtin_fmaf(s[4 * j + e], cc, -lv[e]));
                             ds[4 * j + e] *= s[4 * j + e];
+                        }
+                    }
+                    if (!whole) {   // (after the product: lse2 may be no number)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int row = 32 * t + srow(r, hl);
+                            const bool in = key >= st.lo[row] && key < st.hi[row] && key < last;
+                            s[r] = in ? s[r] : 0.f;
+                            ds[r] = in ? ds[r] : 0.f;
+                        }
+                        // (rows that see a key that is no number have it from the scores, kf's)
+#pragma unroll
+                        for (int i = 0; bad && i < C::LOADS; ++i) {
+                            uint4* const x = reinterpret_cast<uint4*>(kt) + i * 64 + (anew(tid) & 63);
+                            uint4 y = *x;
+                            if (zero_bad<T>(y)) *x = y;
                         }
                     }
                     Turn<T>::put(turn, ds, l32, hl);

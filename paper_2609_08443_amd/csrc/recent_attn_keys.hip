@@ -102,8 +102,8 @@ __global__ __launch_bounds__(256, (KeysCfg<T, D>::PER_CU)) void keys_kernel(Keys
             s.hi += (int32_t)us.tok0;
             const int64_t o = target * a.h + head;
             const float lse = f.lse[o];
-            s.lse2 = s.hi > s.lo && lse != -__builtin_inff() ? lse * kLog2e : __builtin_inff();
             s.delta = s.hi > s.lo ? f.delta[o] : 0.f;
+            s.lse2 = row_lse2(s.hi > s.lo, lse, s.delta);
             s.slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.f;
             return s;
         };
@@ -120,8 +120,9 @@ __global__ __launch_bounds__(256, (KeysCfg<T, D>::PER_CU)) void keys_kernel(Keys
             T* dt = reinterpret_cast<T*>(smem + stage * C::STAGE + C::TILE);
             const RowStats& st = stats[stage];
             const int32_t lo = st.lo[l32], hi = st.hi[l32];
-            const uint32_t dead = (uint32_t)__builtin_amdgcn_ballot_w64(hi <= lo);
-            if (dead) {   // rows that see nothing: zeros, whatever they hold (the same in every wave)
+            const uint32_t dead = (uint32_t)__builtin_amdgcn_ballot_w64(!(st.lse2[l32] < __builtin_inff()));
+            if (dead) {   // rows without weights, or with some that are no numbers: zeros, whatever they hold (the same
+                          // in every wave)
                 for (int x = tid; x < kRows * M::CHUNKS; x += 256)
                     if ((dead >> (x / M::CHUNKS)) & 1u) {
                         reinterpret_cast<uint4*>(qt)[x] = make_uint4(0, 0, 0, 0);
@@ -165,16 +166,6 @@ __global__ __launch_bounds__(256, (KeysCfg<T, D>::PER_CU)) void keys_kernel(Keys
                 }
                 cc = 1.f;
             }
-            if (!whole) {
-                const int32_t key = k0 + l32;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int row = srow(r, hl);
-                    const bool in = key >= st.lo[row] && key < st.hi[row];
-                    s[r] = in ? s[r] : -__builtin_inff();
-                    ds[r] = in ? ds[r] : 0.f;
-                }
-            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float4 ls = *reinterpret_cast<const float4*>(&st.lse2[8 * j + 4 * hl]);
@@ -183,6 +174,16 @@ __global__ __launch_bounds__(256, (KeysCfg<T, D>::PER_CU)) void keys_kernel(Keys
                 for (int e = 0; e < 4; ++e) {
                     s[4 * j + e] = exp2_(__builtin_fmaf(s[4 * j + e], cc, -lv[e]));
                     ds[4 * j + e] *= s[4 * j + e];
+                }
+            }
+            if (!whole) {   // (after the product: lse2 may be no number)
+                const int32_t key = k0 + l32;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int row = srow(r, hl);
+                    const bool in = key >= st.lo[row] && key < st.hi[row];
+                    s[r] = in ? s[r] : 0.f;
+                    ds[r] = in ? ds[r] : 0.f;
                 }
             }
             M::with_cols(dv, dt, M::cols(s), lane);

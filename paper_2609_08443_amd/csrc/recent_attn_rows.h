@@ -72,6 +72,7 @@ __global__ __launch_bounds__(256, (RowsCfg<T, D, WIDE, BWD>::PER_CU)) void rows_
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hl = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     __shared__ __attribute__((aligned(16))) InlinePlan own;
+    __shared__ int2 sees[WIDE ? 4 : 1];   // the keys that all rows of a wave see
     Plan plan = f.p;
     if (f.plan_inline) {
         make_plan(a, plan, &own, reinterpret_cast<int64_t*>(smem));
@@ -146,7 +147,7 @@ __global__ __launch_bounds__(256, (RowsCfg<T, D, WIDE, BWD>::PER_CU)) void rows_
             M::load(df, reinterpret_cast<const T*>(f.dout) + o, live, hl);
             Frag of;
             M::load(of, reinterpret_cast<const T*>(f.o) + o, live, hl);
-            delta = swap_halves(M::dot(df, of), add_);
+            delta = swap_halves(M::dot(df, of) + (M::finite(qf) ? 0.f : __builtin_nanf("")), add_);
             lse2 = live ? f.lse[target * a.h + head] * kLog2e : __builtin_inff();
             if (lse2 == -__builtin_inff()) lse2 = __builtin_inff();
             if (k0 == 0 && ok && hl == 0 && (WIDE || w == 0)) f.delta[target * a.h + head] = delta;
@@ -172,9 +173,28 @@ __global__ __launch_bounds__(256, (RowsCfg<T, D, WIDE, BWD>::PER_CU)) void rows_
         };
 
         f32x16 acc[D / 32];
+        float m, l;   // l: this half's part
+        // Where some row does not see all of a unit's keys, its factor of theirs is 0, but 0 times what is no number
+        // is a NaN.  So such values of the second product's tile (V; K for BWD) are made zeros there, by the lanes that
+        // loaded them, and the rows that see one have it from the loop that follows the units.  A wave with a ring of
+        // its own does that as it masks; tiles of 128 rows take the piece a second time, if a result is no number.
+        bool careful = false;
+        auto clean = [&](int stage) __attribute__((always_inline)) {
+            constexpr int Q = C::LOADS / 2;
+            uint4* const at = reinterpret_cast<uint4*>(ring + stage * C::STAGE + (BWD ? 0 : NT * C::TILE)) + (WIDE ? w * 64 : 0) + lane;
+            uint4 x[Q];
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
-        float m = -__builtin_inff(), l = 0.f;   // l: this half's part
+            for (int i = 0; i < Q; ++i) x[i] = at[(WIDE ? 4 * i : i) * 64];
+            if (any_bad<T>(x)) {
+                if (!WIDE) careful = true;
+#pragma unroll
+                for (int i = 0; i < Q; ++i) {
+                    zero_bad<T>(x[i]);
+                    at[(WIDE ? 4 * i : i) * 64] = x[i];
+                }
+            }
+            if (WIDE) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        };
 
         auto multiply = [&](int64_t u, int stage) __attribute__((always_inline)) {
             const T* kt = reinterpret_cast<const T*>(ring + stage * C::STAGE);
@@ -231,6 +251,7 @@ __global__ __launch_bounds__(256, (RowsCfg<T, D, WIDE, BWD>::PER_CU)) void rows_
                         if (BWD) ds[t][r] = in ? ds[t][r] : 0.f;
                     }
                 }
+                if constexpr (!WIDE) clean(stage);
             }
             if constexpr (BWD) {
 #pragma unroll
@@ -270,10 +291,23 @@ __global__ __launch_bounds__(256, (RowsCfg<T, D, WIDE, BWD>::PER_CU)) void rows_
             }
         };
 
+        auto begin = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
+            m = -__builtin_inff();
+            l = 0.f;
+        };
+        int32_t tile_lo = all_lo, tile_hi = all_hi;   // the keys that all rows of the tile see
+        auto part_of = [&](int64_t u) {
+            const int32_t key0 = klo + first_key(u);
+            return key0 < tile_lo || key0 + 32 * NT > tile_hi;
+        };
+        begin();
         if constexpr (WIDE) {
-            if (nkeys > 0) {
+            while (nkeys > 0) {
                 issue(k0, 0);
                 wait_loads<0>();
+                if (careful && part_of(k0)) clean(0);
                 barrier();
                 for (int64_t u = k0; u < k1; ++u) {
                     const int st = (int)(u - k0) & 1;
@@ -285,8 +319,23 @@ __global__ __launch_bounds__(256, (RowsCfg<T, D, WIDE, BWD>::PER_CU)) void rows_
                         if (u + 1 < k1) issue(u + 1, 0);
                     }
                     wait_loads<0>();
+                    if (careful && u + 1 < k1 && part_of(u + 1)) clean(C::STAGES == 2 ? st ^ 1 : 0);
                     barrier();
                 }
+                bool bad = false;
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) bad = bad || !is_finite(acc[i][r]);
+                if (careful || !__syncthreads_or(bad)) break;
+                careful = true;
+                if (lane == 0) sees[w] = make_int2(all_lo, all_hi);
+                __syncthreads();
+                for (int i = 0; i < 4; ++i) {
+                    tile_lo = max(tile_lo, uniform(sees[i].x));
+                    tile_hi = min(tile_hi, uniform(sees[i].y));
+                }
+                begin();
             }
         } else {
             if (k0 < k1 && first_key(k0) < nkeys) issue(k0, 0);
@@ -303,6 +352,32 @@ __global__ __launch_bounds__(256, (RowsCfg<T, D, WIDE, BWD>::PER_CU)) void rows_
                 multiply(u, st);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before it is written again
                 if (C::STAGES == 1 && more) issue(u + 1, 0);
+            }
+        }
+
+        if (__builtin_amdgcn_ballot_w64(careful)) {
+            for (int64_t u = k0; u < k1; ++u) {
+                const int32_t key0 = klo + first_key(u);
+                if (!part_of(u)) continue;
+                for (int32_t key = max(key0, any_lo); key < min(key0 + 32 * NT, any_hi); ++key) {
+                    const T* x = BWD ? Kp + (int64_t)key * a.k_t + kv * a.k_h : Vp + (int64_t)key * a.v_t + kv * a.v_h;
+                    const bool in = live && key >= lo && key < hi;
+                    if constexpr (BWD) {
+                        const float nan = in && !all_finite(x, D) ? __builtin_nanf("") : 0.f;
+#pragma unroll
+                        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) acc[i][r] += nan;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) {
+                                const float v = to_float(x[32 * i + srow(r, hl)]);
+                                acc[i][r] += in && !is_finite(v) ? v : 0.f;
+                            }
+                    }
+                }
             }
         }
 

@@ -151,3 +151,116 @@ def test_forward(sa, dtype, d, name):
 def test_backward(sa, dtype, d, name):
     print(f"bwd {name} d={d} {dtype}", flush=True)
     check_bwd(sa, Batch(d=d, dtype=dtype, **CASES[name]))
+
+
+# ---------------------------------------------------------------- what is no number stays with those who see it
+
+BAD = [float("nan"), float("inf"), float("-inf")]
+
+
+def spoilt(b, where, at, value):
+    """The batch with one value of K, V, q or dout set."""
+    t = {"K": b.K, "V": b.V, "q": b.q, "dout": b.dout}[where]
+    t[at] = value
+    if where in "KV":
+        b.kv = torch.stack([b.K, b.V], 1).cuda()
+    return b
+
+
+@pytest.mark.parametrize("cap", [0.0, 4.0])
+@pytest.mark.parametrize("targets", [[3, 5], [150, 40]])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("where", ["K", "V"])
+def test_forward_of_tokens_that_are_no_numbers(sa, where, dtype, targets, cap):
+    """Targets whose window leaves such a token out, and other users, have the results that they have without it."""
+    case = dict(tokens=[300, 70], targets=targets, h=4, hk=2, d=64, dtype=dtype, ends="random", window=200, cap=cap)
+    good = Batch(**case)
+    args, kw = good.device()
+    ref, rlse = sa.recent_attn_fwd(*args, **kw)
+    user = np.repeat([0, 1], targets)
+    for value in BAD:
+        for token in (0, 31, 150, 299):
+            b = spoilt(Batch(**case), where, (token, 1, 5), value)
+            args, kw = b.device()
+            out, lse = sa.recent_attn_fwd(*args, **kw)
+            e = np.minimum(b.ends, np.array([300, 70])[user])
+            sees = (user == 0) & (token < e) & (token >= np.maximum(0, e - 200))
+            clean = torch.from_numpy(~sees).cuda()
+            assert torch.equal(out[clean], ref[clean]) and torch.equal(lse[clean], rlse[clean]), (value, token)
+            assert torch.equal(out[:, :2], ref[:, :2])          # the heads that read key head 0
+            if where == "V" and sees.any():
+                hit = out[~clean][:, 2:]
+                assert not torch.isfinite(hit[:, :, 5]).any(), (value, token)
+                rest = [d for d in range(64) if d != 5]
+                assert torch.equal(hit[:, :, rest], ref[~clean][:, 2:][:, :, rest])
+
+
+@pytest.mark.parametrize("cap", [0.0, 4.0])
+@pytest.mark.parametrize("targets", [[3, 5], [150, 40]])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("where", ["K", "V", "q", "dout"])
+def test_backward_of_what_is_no_number(sa, where, dtype, targets, cap):
+    """Gradients of targets and tokens that have nothing to do with it are as they are without it."""
+    case = dict(tokens=[300, 70], targets=targets, h=4, hk=2, d=64, dtype=dtype, ends="random", window=200, cap=cap)
+    user = np.repeat([0, 1], targets)
+
+    def grads(b):
+        args, kw = b.device()
+        out, lse = sa.recent_attn_fwd(*args, **kw)
+        return sa.recent_attn_bwd(*args, out, lse, b.dout.cuda(), **kw)
+
+    ref = grads(Batch(**case))
+    tok_user = np.repeat([0, 1], [300, 70])
+    for value in BAD:
+        for at in (0, 2):
+            b = Batch(**case)
+            e = np.minimum(b.ends, np.array([300, 70])[user])
+            lo = np.maximum(0, e - 200)
+            if where in "KV":
+                token = (0, 31, 250)[at]
+                g = grads(spoilt(b, where, (token, 1, 5), value))
+                rows = (user == 0) & (token < e) & (token >= lo)      # targets that see the token
+            else:
+                g = grads(spoilt(b, where, (at, 3, 5), value))        # query head 3 of one target
+                rows = np.arange(len(user)) == at
+            # tokens that such a target sees
+            j = np.concatenate([np.arange(300), np.arange(70)])
+            toks = np.array([any(user[i] == tok_user[t] and lo[i] <= j[t] < e[i] for i in np.flatnonzero(rows))
+                             for t in range(370)])
+            if where in "KV":
+                toks[token] = True
+            rows, toks = torch.from_numpy(rows).cuda(), torch.from_numpy(toks).cuda()
+            assert torch.equal(g["dq"][~rows], ref["dq"][~rows]), (value, at)
+            assert torch.equal(g["dK"][~toks], ref["dK"][~toks]), (value, at)
+            assert torch.equal(g["dV"][~toks], ref["dV"][~toks]), (value, at)
+            assert torch.equal(g["dK"][:, 0], ref["dK"][:, 0]) and torch.equal(g["dV"][:, 0], ref["dV"][:, 0])
+
+
+@pytest.mark.parametrize("targets", [[3, 5], [150, 40]])
+def test_padding_that_is_no_number(sa, targets):
+    """Targets that see nothing and rows and tokens behind the last user's may hold anything."""
+    case = dict(tokens=[300, 70], targets=targets, h=4, hk=2, d=64, dtype="bf16", ends="random", tail=(33, 20))
+
+    def run(fill):
+        b = Batch(**case)
+        n = sum(targets)
+        b.ends[1] = 0
+        for t in (b.q, b.dout):
+            t[1] = fill
+            t[n:] = fill
+        b.K[370:] = fill
+        b.V[370:] = fill
+        b.kv = torch.stack([b.K, b.V], 1).cuda()
+        args, kw = b.device()
+        out, lse = sa.recent_attn_fwd(*args, **kw)
+        return out, lse, sa.recent_attn_bwd(*args, out, lse, b.dout.cuda(), **kw)
+
+    out, lse, g = run(1.0)
+    for fill in BAD:
+        o, l, h = run(fill)
+        assert torch.equal(o, out) and torch.equal(l, lse)
+        for k in g:
+            assert torch.equal(h[k], g[k]), k
+    n = sum(targets)
+    assert not out[n:].any() and torch.isneginf(lse[n:]).all() and not g["dq"][n:].any()
+    assert not g["dK"][370:].any() and not g["dV"][370:].any()
