@@ -106,6 +106,13 @@ sa_status check_strides(const char* name, int64_t* row, int64_t* head, int32_t h
     return SA_OK;
 }
 
+// a gradient's rows and heads may not lie on each other
+sa_status check_apart(const char* name, int64_t row, int64_t head, int64_t rows, int32_t heads, int32_t d) {
+    const bool apart = (heads == 1 || head >= d) && (rows <= 1 || row >= d) &&
+                       (rows <= 1 || heads == 1 || row >= (heads - 1) * head + d || head >= (rows - 1) * row + d);
+    return apart ? SA_OK : api_fail(SA_ERR_INVALID_ARG, "%s: rows and heads lie on each other", name);
+}
+
 sa_status attn_view(const sa_recent_attn& a, sa::attn::View* v) {
     const bool bf = a.dtype == SA_BF16;
     *v = {a.q, a.K, a.V, a.offsets, a.targets, a.ends, a.slopes, a.B, a.T, a.N, a.h, a.hk, a.h / a.hk, a.window, a.scale,
@@ -214,8 +221,8 @@ LinearFwdPlan plan_linear_fwd(int64_t N, int32_t K, int32_t F, sa_activation act
         if (p.pad_w) time += kPadTime + el * p.Kp * halves * p.Fp / kPadRate;
         p.tiles = (bf && !p.pad_x && !p.pad_w) || time < general_time(2.0 * N * K * columns(F, act), true);
     }
-    if (!p.tiles) {   // z in fp32, where it does not fit into the result
-        p.total = bf || act == SA_ACT_SWIGLU ? 4 * (size_t)N * columns(F, act) : 0;
+    if (!p.tiles) {   // z in fp32 (not in y's place, where the residual may be)
+        p.total = 4 * (size_t)N * columns(F, act);
         return p;
     }
     if (p.pad_x) p.total = align_up(el * N * p.Kp, 256);
@@ -395,7 +402,7 @@ sa_status sa_linear_fwd(const void* x, int64_t x_stride, const void* W, const vo
             e = sa::linear::launch_product({bf, xs, Ws, p.pad_x ? p.Kp : x_stride, 1, halves * p.Fp, 1, (int32_t)N, C, (int32_t)p.Kp,
                                             0, (int32_t)(halves * p.Fp), y, bf, &epi}, stream);
     } else {
-        float* z = reinterpret_cast<float*>(p.total > 0 ? workspace : y);
+        float* z = reinterpret_cast<float*>(workspace);
         e = sa::launch_gemm({x, bf, 0, x_stride, 1, W, bf, 0, C, 1, z, false, 0, C, (int32_t)N, C, K, 1, 1.f, false}, stream);
         if (e == hipSuccess) e = sa::linear::launch_epilogue(z, epi, N, F, bf, y, stream);
     }
@@ -523,6 +530,9 @@ sa_status sa_recent_attn_bwd(const sa_recent_attn* a, const void* out, const flo
     st = check_strides("dq", &gr.dq_stride, &gr.dq_head_stride, a->h, a->d, bf);
     if (st == SA_OK) st = check_strides("dK", &gr.dk_stride, &gr.dk_head_stride, a->hk, a->d, bf);
     if (st == SA_OK) st = check_strides("dV", &gr.dv_stride, &gr.dv_head_stride, a->hk, a->d, bf);
+    if (st == SA_OK) st = check_apart("dq", gr.dq_stride, gr.dq_head_stride, a->N, a->h, a->d);
+    if (st == SA_OK) st = check_apart("dK", gr.dk_stride, gr.dk_head_stride, a->T, a->hk, a->d);
+    if (st == SA_OK) st = check_apart("dV", gr.dv_stride, gr.dv_head_stride, a->T, a->hk, a->d);
     if (st != SA_OK) return st;
     if ((a->N > 0 && (!out || !lse || !dout || !gr.dq)) || (a->T > 0 && (!gr.dK || !gr.dV)))
         return api_fail(SA_ERR_INVALID_ARG, "null pointer argument");

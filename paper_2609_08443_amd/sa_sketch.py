@@ -847,6 +847,8 @@ def _heads_view(t, name, shape, dtype, device):
     row, head, one = t.stride()
     if one != 1 and shape[2] > 1:
         raise SAError(1, f"{name}: the values of a head must lie together")
+    if (row == 0 and shape[0] > 1) or (head == 0 and shape[1] > 1):
+        raise SAError(1, f"{name}: rows and heads of an expanded tensor lie on each other; make it contiguous")
     # (strides along dimensions of one say nothing)
     return (row if shape[0] > 1 else 0), (head if shape[1] > 1 else 0)
 
@@ -942,6 +944,8 @@ def _rows_view(t, name):
     row, one = t.stride()
     if one != 1 and D > 1:
         raise SAError(1, f"{name}: the values of a row must lie together")
+    if row == 0 and n > 1:
+        raise SAError(1, f"{name}: the rows of an expanded tensor lie on each other; make it contiguous")
     return n, D, (row if n > 1 else D)
 
 

@@ -160,3 +160,76 @@ def test_linear_backward(sa, N, K, F, act, dtype):
             within(got[k], ref[k], off[k] + half * np.abs(ref[k]), k)
     got = sa.linear_bwd(x.cuda(), W.cuda(), dy.cuda(), act=act, pre=None if act == "none" else pre.cuda())
     assert set(got) == {"dx", "dW"}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("act", ["none", "gelu", "swiglu"])
+@pytest.mark.parametrize("N,K,F", [(1, 64, 64), (5, 200, 331), (64, 64, 64), (300, 512, 1024), (700, 1001, 903), (1000, 63, 65)])
+def test_linear_result_in_the_residuals_place(sa, N, K, F, act, dtype):
+    C = 2 * F if act == "swiglu" else F
+    x, W, res = values(dtype, (N, K), 1).cuda(), values(dtype, (K, C), 2, K ** -0.5).cuda(), values(dtype, (N, F), 4).cuda()
+    y, _ = sa.linear_fwd(x, W, act=act, residual=res)
+    out = res.clone()
+    got, _ = sa.linear_fwd(x, W, act=act, residual=out, y=out)
+    assert got is out and torch.equal(out, y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("N,K,F,extra", [(1, 64, 64, 8), (5, 200, 331, 3), (130, 256, 512, 64), (300, 512, 128, 5), (257, 72, 1000, 8)])
+def test_linear_of_strided_rows(sa, N, K, F, extra, dtype):
+    wide = values(dtype, (N, K + extra), 1).cuda()
+    x, W, dy = wide[:, :K], values(dtype, (K, F), 2, K ** -0.5).cuda(), values(dtype, (N, F), 3).cuda()
+    close = x.contiguous()
+    y, _ = sa.linear_fwd(x, W)
+    ry, _, ey, _ = ol.linear_fwd(f8(close.cpu()), f8(W.cpu()), None, "none", None, dtype)
+    within(y, ry, ey, "y")
+    got = sa.linear_bwd(x, W, dy, bias=True)
+    ref, off = ol.linear_bwd(f8(close.cpu()), f8(W.cpu()), None, f8(dy.cpu()), "none", dtype)
+    for k in got:
+        within(got[k], ref[k], off[k] + HALF[dtype] * np.abs(ref[k]), k)
+
+
+def test_linear_without_rows(sa):
+    for act in ACTS:
+        x, W = torch.empty(0, 64, device="cuda"), torch.ones(64, 64, device="cuda")
+        F = 32 if act == "swiglu" else 64
+        y, pre = sa.linear_fwd(x, W, act=act, want_pre=True)
+        assert y.shape == (0, F) and pre.shape == (0, 64)
+        g = sa.linear_bwd(x, W, y, bias=True, act=act, pre=pre)
+        assert g["dx"].shape == (0, 64) and not g["dW"].any() and not g["db"].any()
+
+
+def test_linear_rows_that_are_no_numbers(sa):
+    """A row's NaN or infinity stays in its row, forward and in dx, on copies with padding too."""
+    for N, K, F in ((300, 512, 256), (300, 333, 199), (40, 1000, 64)):
+        x, W, dy = values("bf16", (N, K), 1).cuda(), values("bf16", (K, F), 2).cuda(), values("bf16", (N, F), 3).cuda()
+        y, _ = sa.linear_fwd(x, W)
+        dx = sa.linear_bwd(x, W, dy)["dx"]
+        for bad in (float("nan"), float("inf")):
+            z, dz = x.clone(), dy.clone()
+            z[7, K - 1], dz[7, F - 1] = bad, bad
+            got, _ = sa.linear_fwd(z, W)
+            gx = sa.linear_bwd(x, W, dz)["dx"]
+            for a, b in ((got, y), (gx, dx)):
+                assert torch.equal(a[:7], b[:7]) and torch.equal(a[8:], b[8:])
+                assert not torch.isfinite(a[7]).any()
+
+
+def test_bad_tensors_are_refused(sa):
+    from paper_2609_08443_amd.sa_sketch import SAError
+    x, W = torch.zeros(4, 64, device="cuda"), torch.zeros(64, 64, device="cuda")
+    one = torch.ones(64, device="cuda")
+    stats = torch.zeros(4, 2, device="cuda")
+    for call in (lambda: sa.linear_fwd(x[:1].expand(4, -1), W), lambda: sa.linear_fwd(x.t(), W),
+                 lambda: sa.linear_fwd(x, W.t()), lambda: sa.linear_fwd(x, W.bfloat16()), lambda: sa.linear_fwd(x, W, act="tanh"),
+                 lambda: sa.linear_fwd(x, W, bias=one[:63]), lambda: sa.linear_fwd(x, W, residual=x[:3]),
+                 lambda: sa.linear_fwd(x.half(), W.half()), lambda: sa.linear_fwd(x, W.cpu()),
+                 lambda: sa.linear_fwd(x, W[:, :63].contiguous(), act="swiglu"), lambda: sa.linear_fwd(x[:, 1:33], W[:32]),
+                 lambda: sa.linear_bwd(x, W, x, act="relu"), lambda: sa.linear_bwd(x, W, x, weight_dtype=torch.bfloat16),
+                 lambda: sa.linear_bwd(x, W, x, workspace=torch.empty(1, dtype=torch.uint8, device="cuda")),
+                 lambda: sa.layer_norm_fwd(x[:1].expand(4, -1), one, one), lambda: sa.layer_norm_fwd(x, one[:3], one),
+                 lambda: sa.layer_norm_fwd(x, one, one, eps=-1.0), lambda: sa.layer_norm_fwd(x[0], one, one),
+                 lambda: sa.layer_norm_bwd(x, one, stats[:3], x), lambda: sa.layer_norm_bwd(x, one, stats, x.t().contiguous()),
+                 lambda: sa.layer_norm_bwd(x, one, stats, x, workspace=torch.empty(1, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(SAError):
+            call()

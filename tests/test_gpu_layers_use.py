@@ -1,0 +1,397 @@
+"""GPU tests of the recent attention, layer norm and linear layers as a program uses them: together,
+in graphs, on streams, with workspaces and strided tensors of its own, for many users and long caches."""
+import numpy as np
+import pytest
+
+from oracle import layers as ol
+from oracle import recent as orec
+from oracle.recent import HALF
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def sa():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2609_08443_amd import sa_sketch
+    sa_sketch.lib()
+    return sa_sketch
+
+
+def f8(t):
+    return t.detach().double().cpu().numpy()
+
+
+def within(got, ref, off, what):
+    got = f8(got)
+    assert np.array_equal(np.isneginf(got), np.isneginf(ref)), what
+    fin = np.isfinite(ref)
+    worst = np.max(np.abs(got[fin] - ref[fin]) / np.maximum(off[fin], 1e-30), initial=0.0)
+    assert worst <= 1.0, f"{what}: {worst:.3g} of the bound"
+
+
+def values(dtype, shape, seed, scale=1.0, mean=0.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * scale + mean).to(DT[dtype]).cuda()
+
+
+def csr(counts):
+    return torch.from_numpy(np.concatenate([[0], np.cumsum(counts)]).astype(np.int64)).cuda()
+
+
+# ---------------------------------------------------------------- a layer of them
+
+class Layer:
+    """Norm, projections, attention of targets over recent tokens, output projection with residual,
+    norm and gated feed-forward network with residual."""
+
+    def __init__(self, dtype, tokens, targets, Dm=192, h=4, hk=2, d=64, F=160):
+        self.dtype, self.h, self.hk, self.d = dtype, h, hk, d
+        self.offsets, self.targets = csr(tokens), csr(targets)
+        T, N = sum(tokens), sum(targets)
+        self.T, self.N = T, N
+        v = lambda *s, **k: values(dtype, s, **k)  # noqa: E731
+        self.p = dict(x=v(T, Dm, seed=1), t=v(N, Dm, seed=2), g1=v(Dm, seed=3, scale=0.1, mean=1.0), b1=v(Dm, seed=4, scale=0.1),
+                      Wkv=v(Dm, 2 * hk * d, seed=5, scale=Dm ** -0.5), Wq=v(Dm, h * d, seed=6, scale=Dm ** -0.5),
+                      Wo=v(h * d, Dm, seed=7, scale=(h * d) ** -0.5), g2=v(Dm, seed=8, scale=0.1, mean=1.0),
+                      b2=v(Dm, seed=9, scale=0.1), Wu=v(Dm, 2 * F, seed=10, scale=Dm ** -0.5),
+                      bu=v(2 * F, seed=11, scale=0.1), Wd=v(F, Dm, seed=12, scale=F ** -0.5))
+        n = np.repeat(tokens, targets)
+        self.ends = torch.from_numpy((n - np.arange(N) % 3).clip(0).astype(np.int32)).cuda()
+        self.slopes = torch.tensor([0.5 ** (i + 1) for i in range(h)], device="cuda")
+        self.kw = dict(ends=self.ends, window=90, slopes=self.slopes, cap=6.0)
+        self.dy = v(N, Dm, seed=13)
+
+    def forward(self, sa):
+        p, s = self.p, {}
+        s["xn"], s["xs"] = sa.layer_norm_fwd(p["x"], p["g1"], p["b1"])
+        s["tn"], s["ts"] = sa.layer_norm_fwd(p["t"], p["g1"], p["b1"])
+        s["kv"], _ = sa.linear_fwd(s["xn"], p["Wkv"])
+        s["q"], _ = sa.linear_fwd(s["tn"], p["Wq"])
+        kv = s["kv"].view(self.T, 2, self.hk, self.d)
+        s["o"], s["lse"] = sa.recent_attn_fwd(s["q"].view(self.N, self.h, self.d), kv[:, 0], kv[:, 1], self.offsets, self.targets,
+                                              **self.kw)
+        s["r"], _ = sa.linear_fwd(s["o"].view(self.N, -1), p["Wo"], residual=p["t"])
+        s["rn"], s["rs"] = sa.layer_norm_fwd(s["r"], p["g2"], p["b2"])
+        s["f"], s["pre"] = sa.linear_fwd(s["rn"], p["Wu"], bias=p["bu"], act="swiglu", want_pre=True)
+        s["y"], _ = sa.linear_fwd(s["f"], p["Wd"], residual=s["r"])
+        return s
+
+    def backward(self, sa, s):
+        p, g = self.p, {}
+        a = sa.linear_bwd(s["f"], p["Wd"], self.dy, weight_dtype=torch.float32)
+        b = sa.linear_bwd(s["rn"], p["Wu"], a["dx"], bias=True, act="swiglu", pre=s["pre"], weight_dtype=torch.float32)
+        c = sa.layer_norm_bwd(s["r"], p["g2"], s["rs"], b["dx"])
+        dr = c["dx"] + self.dy
+        e = sa.linear_bwd(s["o"].view(self.N, -1), p["Wo"], dr, weight_dtype=torch.float32)
+        kv = s["kv"].view(self.T, 2, self.hk, self.d)
+        dkv = torch.full_like(s["kv"], 7.0)
+        d4 = dkv.view(kv.shape)
+        q = s["q"].view(self.N, self.h, self.d)
+        at = sa.recent_attn_bwd(q, kv[:, 0], kv[:, 1], self.offsets, self.targets, s["o"], s["lse"], e["dx"].view(q.shape),
+                                dK=d4[:, 0], dV=d4[:, 1], **self.kw)
+        k = sa.linear_bwd(s["xn"], p["Wkv"], dkv, weight_dtype=torch.float32)
+        m = sa.linear_bwd(s["tn"], p["Wq"], at["dq"].view(self.N, -1), weight_dtype=torch.float32)
+        nx = sa.layer_norm_bwd(p["x"], p["g1"], s["xs"], k["dx"])
+        nt = sa.layer_norm_bwd(p["t"], p["g1"], s["ts"], m["dx"])
+        g.update(Wd=a["dW"], Wu=b["dW"], bu=b["db"], g2=c["dgamma"], b2=c["dbeta"], Wo=e["dW"], Wkv=k["dW"], Wq=m["dW"],
+                 x=nx["dx"], t=nt["dx"] + dr, g1=nx["dgamma"] + nt["dgamma"], b1=nx["dbeta"] + nt["dbeta"])
+        return g
+
+    def plain(self):
+        """y and the gradients in float64 on the CPU, by autograd."""
+        p = {k: v.detach().double().cpu().requires_grad_() for k, v in self.p.items()}
+        norm = torch.nn.functional.layer_norm
+        D = p["x"].shape[1]
+        xn, tn = norm(p["x"], (D,), p["g1"], p["b1"]), norm(p["t"], (D,), p["g1"], p["b1"])
+        kv = (xn @ p["Wkv"]).view(self.T, 2, self.hk, self.d)
+        q = (tn @ p["Wq"]).view(self.N, self.h, self.d)
+        off, tg, ends = self.offsets.tolist(), self.targets.tolist(), self.ends.tolist()
+        rows = []
+        for b in range(len(off) - 1):
+            for i in range(tg[b], tg[b + 1]):
+                e = min(ends[i], off[b + 1] - off[b])
+                lo = max(0, e - 90)
+                if e == 0:
+                    rows.append(torch.zeros(self.h * self.d, dtype=torch.float64))
+                    continue
+                K, V = kv[off[b] + lo:off[b] + e, 0], kv[off[b] + lo:off[b] + e, 1]
+                g = self.h // self.hk
+                K, V = K.repeat_interleave(g, 1), V.repeat_interleave(g, 1)
+                s = 6.0 * torch.tanh((K * q[i]).sum(2) * self.d ** -0.5 / 6.0)
+                s = s - self.slopes.double().cpu() * (e - 1 - torch.arange(lo, e, dtype=torch.float64))[:, None]
+                rows.append((torch.softmax(s, 0)[:, :, None] * V).sum(0).reshape(-1))
+        r = torch.stack(rows) @ p["Wo"] + p["t"]
+        z = norm(r, (D,), p["g2"], p["b2"]) @ p["Wu"] + p["bu"]
+        F = z.shape[1] // 2
+        y = torch.nn.functional.silu(z[:, :F]) * z[:, F:] @ p["Wd"] + r
+        (y * self.dy.double().cpu()).sum().backward()
+        return y.detach(), {k: v.grad for k, v in p.items()}
+
+
+TOKENS, TARGETS = [100, 0, 257, 33, 3], [3, 2, 40, 1, 0]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_a_layer_of_them(sa, dtype):
+    """Off by no more than a dozen stages in a row may be: fp32, sums of at most 320 terms and a gain of at most 2 a
+    stage, 12 * 2 * 320 * 2^-23 < 1e-3 of the norm; bf16, each stage rounds its result (and some a factor) by at most
+    2^-8, 2 * 12 * 2^-8 < 0.1."""
+    a = Layer(dtype, TOKENS, TARGETS)
+    s = a.forward(sa)
+    g = a.backward(sa, s)
+    y, ref = a.plain()
+    tol = 1e-3 if dtype == "fp32" else 0.1
+    rel = lambda got, want: float((got.double().cpu() - want).norm() / want.norm())  # noqa: E731
+    assert rel(s["y"], y) < tol
+    assert set(g) == set(ref)
+    for k in ref:
+        assert rel(g[k], ref[k]) < tol, k
+
+
+# ---------------------------------------------------------------- graphs, streams, workspaces
+
+def same(a, b):
+    return all(torch.equal(a[k], b[k]) for k in a if a[k] is not None)
+
+
+@pytest.mark.parametrize("targets", [TARGETS, [300, 2, 150, 70, 0]])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_layer_in_a_graph(sa, dtype, targets):
+    """Forward and backward captured and replayed on new values, eager calls between; the same bits as eagerly."""
+    a = Layer(dtype, TOKENS, targets)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        a.backward(sa, a.forward(sa))
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s = a.forward(sa)
+        g = a.backward(sa, s)
+    for i in range(4):
+        a.p["x"].copy_(values(dtype, tuple(a.p["x"].shape), 100 + i))
+        a.dy.copy_(values(dtype, tuple(a.dy.shape), 200 + i))
+        if i == 2:
+            a.ends.copy_(torch.flip(a.ends, [0]))
+        es = a.forward(sa)
+        eg = a.backward(sa, es)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(es, s) and same(eg, g), i
+
+
+def attn_case(dtype="bf16", tokens=(700, 31, 1500, 4), targets=(30, 3, 200, 1), h=4, hk=2, d=64, seed=0):
+    T, N = sum(tokens), sum(targets)
+    kv = values(dtype, (T, 2, hk, d), seed + 1)
+    return (values(dtype, (N, h, d), seed), kv[:, 0], kv[:, 1], csr(tokens), csr(targets)), values(dtype, (N, h, d), seed + 2)
+
+
+def test_two_graphs_share_a_workspace(sa):
+    cases = [attn_case(seed=10), attn_case(tokens=(64, 2000), targets=(1, 1), seed=20)]
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+    graphs, outs, eager = [], [], []
+    for args, dout in cases:
+        out, lse = sa.recent_attn_fwd(*args)
+        eager.append((out, lse, sa.recent_attn_bwd(*args, out, lse, dout)))
+    for args, dout in cases:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out, lse = sa.recent_attn_fwd(*args, workspace=ws)
+            outs.append((out, lse, sa.recent_attn_bwd(*args, out, lse, dout, workspace=ws)))
+        graphs.append(graph)
+    for order in ([0, 1], [1, 0], [0, 0, 1], [1, 1, 0]):
+        for t in outs:
+            t[0].fill_(3.0)
+        ws.fill_(0xff)
+        for i in order:
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        for got, want in zip(outs, eager):
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and same(got[2], want[2])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_the_same_bits_again_and_on_other_streams(sa, dtype):
+    args, dout = attn_case(dtype)
+    x, W, dy = values(dtype, (700, 512), 5), values(dtype, (512, 1000), 6, 0.05), values(dtype, (700, 1000), 7)
+    gamma = values(dtype, (512,), 8)
+
+    def run(stream=None):
+        out, lse = sa.recent_attn_fwd(*args, stream=stream)
+        y, pre = sa.linear_fwd(x, W, act="silu", want_pre=True, stream=stream)
+        n, st = sa.layer_norm_fwd(x, gamma, gamma, stream=stream)
+        return dict(out=out, lse=lse, y=y, pre=pre, n=n, st=st, **sa.recent_attn_bwd(*args, out, lse, dout, stream=stream),
+                    **sa.linear_bwd(x, W, dy, bias=True, act="silu", pre=pre, stream=stream),
+                    **{f"n{k}": v for k, v in sa.layer_norm_bwd(x, gamma, st, n, stream=stream).items()})
+
+    ref = run()
+    assert same(ref, run())
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    got = [run(s) for s in (a, b, a, b)]      # two at once
+    with torch.cuda.stream(a):
+        got.append(run())
+    torch.cuda.synchronize()
+    assert all(same(ref, g) for g in got)
+
+
+def test_workspaces_of_the_caller(sa):
+    """As large as asked for, larger, with anything in it; too small ones are refused."""
+    args, dout = attn_case()
+    q, K = args[0], args[1]
+    out, lse = sa.recent_attn_fwd(*args)
+    g = sa.recent_attn_bwd(*args, out, lse, dout)
+    pack = sa._RECENT_ATTN.pack(*[0] * 13, 4, K.shape[0], q.shape[0], 4, 2, 64, 0, 1.0, 0.0, sa.SA_BF16)
+    nf, nb = sa.lib().sa_recent_attn_fwd_workspace_size(pack), sa.lib().sa_recent_attn_bwd_workspace_size(pack)
+    for fill in (0, 0xff, 0x7f):
+        for more in (0, 4096):
+            wf = torch.full((nf + more + 16,), fill, dtype=torch.uint8, device="cuda")
+            wb = torch.full((nb + more + 16,), fill, dtype=torch.uint8, device="cuda")
+            o, z = sa.recent_attn_fwd(*args, workspace=wf[:nf + more])
+            assert torch.equal(o, out) and torch.equal(z, lse)
+            assert same(g, sa.recent_attn_bwd(*args, out, lse, dout, workspace=wb[:nb + more]))
+            assert (wf[nf:] == fill).all() and (wb[nb:] == fill).all()
+    for n, call in ((nf, lambda w: sa.recent_attn_fwd(*args, workspace=w)),
+                    (nb, lambda w: sa.recent_attn_bwd(*args, out, lse, dout, workspace=w))):
+        with pytest.raises(sa.SAError):
+            call(torch.empty(n - 1, dtype=torch.uint8, device="cuda"))
+        with pytest.raises(sa.SAError):
+            call(torch.empty(n + 8, dtype=torch.uint8, device="cuda")[8:])
+        with pytest.raises(sa.SAError):
+            call(torch.empty(n, dtype=torch.uint8))
+
+
+# ---------------------------------------------------------------- strides, many users, long caches
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tokens", [[40, 0, 7], [300, 129]])
+def test_tokens_over_themselves_in_one_projection(sa, dtype, d, tokens):
+    """q, K and V are parts of a projection's rows, their gradients parts of its gradient's; every token
+    sees itself and those before it."""
+    h, hk = 4, 2
+    T = sum(tokens)
+    qkv = values(dtype, (T, (h + 2 * hk) * d + 24), 3)
+    cut = lambda t: (t[:, 8:8 + h * d].view(T, h, d), t[:, 8 + h * d:8 + (h + hk) * d].view(T, hk, d),  # noqa: E731
+                     t[:, 8 + (h + hk) * d:8 + (h + 2 * hk) * d].view(T, hk, d))
+    off = csr(tokens)
+    ends = torch.cat([torch.arange(1, n + 1, dtype=torch.int32) for n in tokens]).cuda()
+    dout = values(dtype, (T, h, d), 4)
+    q, K, V = cut(qkv)
+    out, lse = sa.recent_attn_fwd(q, K, V, off, off, ends=ends)
+    n = lambda t: f8(t)  # noqa: E731
+    oargs = (n(q), n(K), n(V), off.cpu().numpy(), off.cpu().numpy())
+    ro, rl, eo, el = orec.fwd(*oargs, ends=ends.cpu().numpy(), dtype=dtype)
+    within(out, ro, eo, "out")
+    within(lse, rl, el, "lse")
+    grad = torch.full_like(qkv, 5.0)
+    dq, dK, dV = cut(grad)
+    ref, e = orec.bwd(*oargs, f8(dout), ends=ends.cpu().numpy(), dtype=dtype)
+    ro, rl = torch.from_numpy(ro).to(DT[dtype]).cuda(), torch.from_numpy(rl.astype(np.float32)).cuda()
+    g = sa.recent_attn_bwd(q, K, V, off, off, ro, rl, dout, ends=ends, dq=dq, dK=dK, dV=dV)
+    for k in ref:
+        within(g[k], ref[k], e[k], k)
+    assert (grad[:, :8] == 5.0).all() and (grad[:, 8 + (h + 2 * hk) * d:] == 5.0).all()
+
+
+@pytest.mark.parametrize("B,most,per", [(700, 90, 3), (5000, 20, 2), (600, 40, 130)])
+def test_many_users(sa, B, most, per):
+    """More tiles than a kernel plans by itself, than a thread of the plan holds, users of every kind side by side."""
+    rng = np.random.default_rng(B)
+    tokens, targets = rng.integers(0, most, B), rng.integers(0, per + 1, B)
+    if per > 100:
+        targets[rng.random(B) < 0.9] = 1
+        tokens[B // 2], targets[B // 3] = 9000, 700
+    T, N, h, hk, d = int(tokens.sum()), int(targets.sum()), 2, 1, 64
+    kv = values("bf16", (T, 2, hk, d), 1)
+    q, dout = values("bf16", (N, h, d), 2), values("bf16", (N, h, d), 3)
+    ends = torch.from_numpy(rng.integers(0, np.repeat(tokens, targets) + 1).astype(np.int32)).cuda()
+    off, tg = csr(tokens), csr(targets)
+    oargs = (f8(q), f8(kv[:, 0]), f8(kv[:, 1]), off.cpu().numpy(), tg.cpu().numpy())
+    ro, rl, eo, el = orec.fwd(*oargs, ends=ends.cpu().numpy())
+    out, lse = sa.recent_attn_fwd(q, kv[:, 0], kv[:, 1], off, tg, ends=ends)
+    within(out, ro, eo, "out")
+    within(lse, rl, el, "lse")
+    ref, e = orec.bwd(*oargs, f8(dout), ends=ends.cpu().numpy())
+    given = torch.from_numpy(ro).bfloat16().cuda(), torch.from_numpy(rl.astype(np.float32)).cuda()
+    g = sa.recent_attn_bwd(q, kv[:, 0], kv[:, 1], off, tg, *given, dout, ends=ends)
+    for k in ref:
+        within(g[k], ref[k], e[k], k)
+
+
+@pytest.mark.parametrize("targets", [1, 70])
+def test_offsets_past_32_bits(sa, targets):
+    """9 M tokens, 2.3 G values: a window at the end of a history of nearly all, and the user behind it."""
+    T, h, hk, d, last, window = 9_000_000, 4, 2, 64, 1000, 500
+    kv = torch.empty(T, 2, hk, d, dtype=torch.bfloat16, device="cuda").fill_(float("nan"))
+    tail = last + window
+    kv[-tail:] = values("bf16", (tail, 2, hk, d), 1)
+    N = 2 * targets
+    q, dout = values("bf16", (N, h, d), 2), values("bf16", (N, h, d), 3)
+    off, tg = csr([T - last, last]), csr([targets, targets])
+    kw = dict(window=window)
+    oargs = (f8(q), f8(kv[-tail:, 0]), f8(kv[-tail:, 1]), np.array([0, window, tail]), tg.cpu().numpy())
+    ro, rl, eo, el = orec.fwd(*oargs, window=window)
+    out, lse = sa.recent_attn_fwd(q, kv[:, 0], kv[:, 1], off, tg, **kw)
+    within(out, ro, eo, "out")
+    within(lse, rl, el, "lse")
+    ref, e = orec.bwd(*oargs, f8(dout), window=window)
+    dkv = torch.empty_like(kv).fill_(9.0)
+    given = torch.from_numpy(ro).bfloat16().cuda(), torch.from_numpy(rl.astype(np.float32)).cuda()
+    g = sa.recent_attn_bwd(q, kv[:, 0], kv[:, 1], off, tg, *given, dout, dK=dkv[:, 0], dV=dkv[:, 1], **kw)
+    within(g["dq"], ref["dq"], e["dq"], "dq")
+    within(dkv[-tail:, 0], ref["dK"], e["dK"], "dK")
+    within(dkv[-tail:, 1], ref["dV"], e["dV"], "dV")
+    assert not dkv[:-tail].any()
+
+
+def test_norm_and_linear_of_many_values(sa):
+    """More than 2^31 values: the rows at the end."""
+    N, D = 1_200_000, 2048
+    x = torch.empty(N, D, dtype=torch.bfloat16, device="cuda").fill_(1.0)
+    end = values("bf16", (300, D), 1)
+    x[-300:] = end
+    gamma, beta = values("bf16", (D,), 2), values("bf16", (D,), 3)
+    y, st = sa.layer_norm_fwd(x, gamma, beta)
+    ry, rs, ey, es = ol.norm_fwd(f8(end), f8(gamma), f8(beta), 1e-5, "bf16")
+    within(y[-300:], ry, ey, "y")
+    within(st[-300:], rs, es, "stats")
+    assert torch.equal(y[0], beta) and torch.equal(y[N // 2], beta)
+    W = values("bf16", (D, 64), 4, D ** -0.5)
+    z, _ = sa.linear_fwd(x, W)
+    rz, _, ez, _ = ol.linear_fwd(f8(end), f8(W), None, "none", None, "bf16")
+    within(z[-300:], rz, ez, "z")
+    dz = values("bf16", (N, 64), 5)
+    dz[:-300] = 0
+    g = sa.linear_bwd(x, W, dz)
+    ref, off = ol.linear_bwd(f8(end), f8(W), None, f8(dz[-300:]), "none", "bf16")
+    for k in ("dx", "dW"):
+        got = g[k][-300:] if k == "dx" else g[k]
+        within(got, ref[k], off[k] + HALF["bf16"] * np.abs(ref[k]), k)
+    assert not g["dx"][:-300].any()
+
+
+def test_refusals_leave_tensors_alone(sa):
+    args, dout = attn_case()
+    q, K, V, off, tg = args
+    out, lse = sa.recent_attn_fwd(*args)
+    dK = torch.full((K.shape[0], 2, 64), 4.0, dtype=torch.bfloat16, device="cuda")
+    for call in (lambda: sa.recent_attn_fwd(q, K, V[:-1], off, tg, out=out), lambda: sa.recent_attn_fwd(*args, window=-1, out=out),
+                 lambda: sa.recent_attn_fwd(*args, cap=-1.0, out=out), lambda: sa.recent_attn_fwd(*args, scale=0.0, out=out),
+                 lambda: sa.recent_attn_fwd(q[:, :, :32], K[:, :, :32], V[:, :, :32], off, tg),
+                 lambda: sa.recent_attn_fwd(q[:, :3], K, V, off, tg), lambda: sa.recent_attn_fwd(q.float(), K, V, off, tg),
+                 lambda: sa.recent_attn_fwd(q, K, V, off.cpu(), tg), lambda: sa.recent_attn_fwd(*args, out=out[:, :, ::2]),
+                 lambda: sa.recent_attn_fwd(q, K[:, :1].expand(-1, 2, -1), V, off, tg),
+                 lambda: sa.recent_attn_bwd(*args, out, lse, dout, dK=dK[:, :1].expand(-1, 2, -1)),
+                 lambda: sa.recent_attn_bwd(*args, out, lse, dout[:1].expand_as(dout), dK=dK),
+                 lambda: sa.recent_attn_bwd(*args, out, lse[:-1], dout, dK=dK)):
+        before = out.clone()
+        with pytest.raises(sa.SAError):
+            call()
+        assert torch.equal(out, before) and (dK == 4.0).all()
