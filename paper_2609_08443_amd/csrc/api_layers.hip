@@ -35,8 +35,11 @@ AttnPlan plan_attn(const sa_recent_attn& a, bool bwd) {
     AttnPlan p;
     const bool bf = a.dtype == SA_BF16;
     const int64_t g = a.h / a.hk, rows = a.N * g;
-    // tiles of 128 rows where users have that many on average
-    p.wide = rows > 48 * a.B;
+    // Tiles of 128 rows where users have many on average.  bf16, 16 users of 10,000 tokens, 16 heads of 64, the forward
+    // in us, tiles of 32 and of 128 rows: 40 rows 145, 162; 64 rows 146, 164; 80 rows 358, 172; 64 users of 1,000: 32 rows
+    // 55, 70; 40 rows 91, 75.  fp32, 16 users of 2,000 tokens, 4 heads of 64: 128 rows 73, 79; 200 rows 136, 110; heads
+    // of 128, the forward 128 rows 102, 138; 600 rows 469, 545; dq 64 rows 102, 148; 96 rows 152, 154; 128 rows 170, 160.
+    p.wide = rows > (bf ? 48 : bwd ? 64 : 128) * a.B && (bf || a.d == 64 || bwd);
     p.shape = sa::attn::rows_shape(bf, a.d, p.wide, bwd);
     p.tiles = rows / p.shape.bq + a.B + 1;
     // no more workgroups than units of work

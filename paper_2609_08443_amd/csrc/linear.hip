@@ -26,7 +26,7 @@ int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void epilogue_kernel(const float* z, const T* __restrict__ bias,
-                                                            const T* __restrict__ res, int64_t N, int F, int act,
+                                                            const T* res, int64_t N, int F, int act,
                                                             T* __restrict__ pre, T* y) {
     constexpr int V = vec::Piece<T>::N;
     const int64_t per = (F + V - 1) / V, n = N * per;
