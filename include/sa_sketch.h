@@ -553,7 +553,8 @@ sa_status sa_stca_cached_bwd(const void* cache, const int32_t* cache_rows, int64
  *   targets          [B+1] int64 CSR offsets of the users' targets, offsets [B+1] of their tokens
  *   ends             [N] int32 or NULL;  slopes [h] fp32, or NULL for none
  *   B, T, N, h, hk, d    h a multiple of hk, d in {64, 128}
- *   window           tokens, >= 0;  cap >= 0, finite (0: none);  scale finite and > 0
+ *   window           tokens, >= 0;  cap >= 0 (0: none), scale > 0; both, and scale / cap, finite
+ *                    and below 2^126
  *
  * Targets behind the last user's (from targets[B] on) see nothing; tokens behind the last
  * user's (from offsets[B] on) are seen by none.  A NaN or infinity in a token reaches the
@@ -604,8 +605,9 @@ typedef struct {
  *
  *   out, lse     what sa_recent_attn_fwd wrote for the same inputs
  *   dout         [N,h,d] (dtype), packed
- *   grads        dq, dK, dV (dtype), overwritten; zeros for targets that see nothing and for
- *                tokens that no target sees, those behind the last user's too
+ *   grads        dq, dK, dV (dtype), overwritten, their rows and heads apart; zeros for targets
+ *                that see nothing and for tokens that no target sees, those behind the last
+ *                user's too
  *
  * A target that sees nothing adds nothing, whatever its q and dout hold.  bf16 mode rounds
  * the softmax weights, their gradients and the results to bf16 and sums in fp32.  N = 0 and
@@ -677,7 +679,7 @@ size_t sa_linear_fwd_workspace_size(int64_t N, int32_t K, int32_t F, sa_activati
  *   x         [N,K] (dtype), x_stride elements from row to row (0: K)
  *   W         [K,C] (dtype), row = input feature, C = F (swiglu: 2 F);  bias [C] (dtype) or NULL
  *   residual  [N,F] (dtype), packed, or NULL
- *   y         output [N,F] (dtype), packed; it may be residual
+ *   y         output [N,F] (dtype), packed; it may be residual, but not x or W
  *   pre       output [N,C] (dtype), packed: z, for the backward, or NULL
  *
  * Sums in fp32, y and z rounded once each (y from the unrounded z).  N = 0 is a no-op; K, F >= 1.
@@ -702,7 +704,7 @@ size_t sa_linear_bwd_workspace_size(int64_t N, int32_t K, int32_t F, sa_activati
  *   pre              what the forward wrote; NULL for SA_ACT_NONE, which has no need of it
  *   dy               [N,F] (dtype), packed
  *   dx, dW, dbias    outputs [N,K], [K,C], [C], packed; dx in dtype, dW and dbias in weight_dtype:
- *                    SA_FP32, or SA_BF16 with dtype SA_BF16.  NULL: not wanted
+ *                    SA_FP32, or SA_BF16 with dtype SA_BF16.  NULL: not wanted.  None may be an input
  *
  * bf16 mode rounds dz to bf16 before the products (dbias sums it unrounded).  All outputs are
  * overwritten; N = 0 leaves zeros in dW and dbias.

@@ -88,6 +88,9 @@ sa_status check_attn_sizes(const sa_recent_attn* a) {
     if (a->h % a->hk != 0) return api_fail(SA_ERR_INVALID_ARG, "h=%d is not a multiple of hk=%d", a->h, a->hk);
     if (!(std::isfinite(a->scale) && a->scale > 0.f)) return api_fail(SA_ERR_INVALID_ARG, "scale must be finite and > 0");
     if (!(std::isfinite(a->cap) && a->cap >= 0.f)) return api_fail(SA_ERR_INVALID_ARG, "cap must be finite and >= 0");
+    // (the kernels take both in units of log 2)
+    if (!std::isfinite(4.f * a->scale) || !std::isfinite(4.f * a->cap) || (a->cap > 0.f && !std::isfinite(4.f * (a->scale / a->cap))))
+        return api_fail(SA_ERR_UNSUPPORTED, "scale, cap or scale / cap is beyond the supported range");
     if (a->d != 64 && a->d != 128) return api_fail(SA_ERR_UNSUPPORTED, "d must be 64 or 128 (got %d)", a->d);
     constexpr int64_t k31 = int64_t(1) << 31;
     if (a->h > 65536) return api_fail(SA_ERR_UNSUPPORTED, "h must be <= 65536 (got %d)", a->h);
@@ -377,6 +380,7 @@ sa_status sa_linear_fwd(const void* x, int64_t x_stride, const void* W, const vo
     if (x_stride < 0) return api_fail(SA_ERR_INVALID_ARG, "x_stride must be >= 0");
     if (N == 0) return SA_OK;
     if (!x || !W || !y) return api_fail(SA_ERR_INVALID_ARG, "null pointer argument");
+    if (y == x || y == W || y == pre || pre == x || pre == W) return api_fail(SA_ERR_INVALID_ARG, "y and pre may not be each other, x or W");
     if (!aligned16(x) || !aligned16(W) || !aligned16(bias) || !aligned16(residual) || !aligned16(y) || !aligned16(pre))
         return api_fail(SA_ERR_INVALID_ARG, "tensor arguments must be 16-byte aligned");
     const LinearFwdPlan p = plan_linear_fwd(N, K, F, act, dtype, x_stride);
@@ -436,6 +440,8 @@ sa_status sa_linear_bwd(const void* x, int64_t x_stride, const void* W, const vo
     if (!aligned16(x) || !aligned16(W) || !aligned16(pre) || !aligned16(dy) || !aligned16(dx) || !aligned16(dW) ||
         !aligned16(dbias))
         return api_fail(SA_ERR_INVALID_ARG, "tensor arguments must be 16-byte aligned");
+    if (dx && (dx == dy || dx == x || dx == W || dx == pre))
+        return api_fail(SA_ERR_INVALID_ARG, "dx may not be an input");
     const LinearBwdPlan p = plan_linear_bwd(N, K, F, act, dtype, x_stride);
     st = check_workspace(workspace, workspace_bytes, p.total);
     if (st != SA_OK) return st;

@@ -202,7 +202,7 @@ __device__ inline int32_t plan_tile(const View& a, const int64_t* targets, int32
     rec->user = (int32_t)b;
     rec->row0 = (int32_t)row0;
     rec->klo = rec->khi = (int32_t)us.tok0;
-    if (row0 >= rows || rows <= a.skip) return 0;
+    if (row0 < 0 || row0 >= rows || rows <= a.skip) return 0;   // (< 0: offsets that begin past 0)
     int32_t lo = us.L, hi = 0;
     if (!a.ends) {
         seen(a, us, 0, &lo, &hi);

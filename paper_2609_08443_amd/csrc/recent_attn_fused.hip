@@ -115,7 +115,7 @@ __global__ __launch_bounds__(256, (FusedCfg<T, D>::PER_CU)) void fused_kernel(Fu
         }
         const Chunks chunks(us.L, f.chunk);
         const int32_t n_chunks = chunks.n, ci = (int32_t)(item - item0);
-        if (ci >= n_chunks || (int64_t)us.n * a.g > kFusedRows) continue;
+        if (ci < 0 || ci >= n_chunks || (int64_t)us.n * a.g > kFusedRows) continue;   // (< 0: offsets that begin past 0)
         const int32_t rows = us.n * a.g;
         const int32_t c0 = chunks.begin(ci, us.L), c1 = chunks.begin(ci + 1, us.L);
         const int32_t first = (int32_t)us.tok0 + c0, last = (int32_t)us.tok0 + c1;   // the chunk's keys

@@ -31,6 +31,7 @@ BAD_RECENT = [
     (dict(q=A + 8), INVALID), (dict(K=A + 2), INVALID), (dict(V=A + 4), INVALID), (dict(offsets=A + 8), INVALID),
     (dict(targets=A + 8), INVALID), (dict(ends=A + 4), INVALID), (dict(slopes=A + 4), INVALID),
     (dict(qs=(132, 64)), INVALID), (dict(ks=(128, 4)), INVALID), (dict(vs=(-128, 64)), INVALID), (dict(vs=(128, -64)), INVALID),
+    (dict(scale=3e38), UNSUPPORTED), (dict(cap=3e38), UNSUPPORTED), (dict(cap=1e-39), UNSUPPORTED),
     (dict(ks=(1 << 24, 64)), UNSUPPORTED), (dict(qs=(128, 1 << 23)), UNSUPPORTED),
 ]
 
@@ -132,12 +133,12 @@ def test_layer_norm_bwd_rejects_bad_arguments(kw, code):
     assert norm_bwd(**kw) == code and sa.lib().sa_last_error().decode() != ""
 
 
-def linear_fwd(x=A, ld=0, W=A, bias=None, residual=None, N=3, K=64, F=64, act=0, dtype=sa.SA_BF16, y=A, pre=None, ws=A,
+def linear_fwd(x=A, ld=0, W=2 * A, bias=None, residual=None, N=3, K=64, F=64, act=0, dtype=sa.SA_BF16, y=3 * A, pre=None, ws=A,
                wsb=1 << 50):
     return sa.lib().sa_linear_fwd(x, ld, W, bias, residual, N, K, F, act, dtype, y, pre, ws, wsb, None)
 
 
-def linear_bwd(x=A, ld=0, W=A, pre=A, dy=A, N=3, K=64, F=64, act=0, dtype=sa.SA_BF16, dx=A, dW=A, db=A, wdt=sa.SA_FP32, ws=A,
+def linear_bwd(x=A, ld=0, W=2 * A, pre=3 * A, dy=4 * A, N=3, K=64, F=64, act=0, dtype=sa.SA_BF16, dx=5 * A, dW=6 * A, db=A, wdt=sa.SA_FP32, ws=A,
                wsb=1 << 50):
     return sa.lib().sa_linear_bwd(x, ld, W, pre, dy, N, K, F, act, dtype, dx, dW, db, wdt, ws, wsb, None)
 
@@ -150,6 +151,7 @@ LINEAR_SIZES = [(dict(N=-1), INVALID), (dict(K=0), INVALID), (dict(F=0), INVALID
 
 @pytest.mark.parametrize("kw,code", LINEAR_SIZES + [
     (dict(x=None), INVALID), (dict(W=None), INVALID), (dict(y=None), INVALID), (dict(x=A + 2), INVALID), (dict(W=A + 8), INVALID),
+    (dict(y=A), INVALID), (dict(y=2 * A), INVALID), (dict(pre=3 * A), INVALID), (dict(pre=A), INVALID),
     (dict(bias=A + 2), INVALID), (dict(residual=A + 8), INVALID), (dict(y=A + 4), INVALID), (dict(pre=A + 4), INVALID),
     (dict(K=63, ws=None), WORKSPACE), (dict(K=63, wsb=1), WORKSPACE), (dict(K=63, ws=A + 8), WORKSPACE)])
 def test_linear_fwd_rejects_bad_arguments(kw, code):
@@ -158,6 +160,7 @@ def test_linear_fwd_rejects_bad_arguments(kw, code):
 
 @pytest.mark.parametrize("kw,code", LINEAR_SIZES + [
     (dict(x=None), INVALID), (dict(W=None), INVALID), (dict(dy=None), INVALID), (dict(act=1, pre=None), INVALID),
+    (dict(dx=A), INVALID), (dict(dx=2 * A), INVALID), (dict(dx=3 * A), INVALID), (dict(dx=4 * A), INVALID),
     (dict(dx=A + 8), INVALID), (dict(dW=A + 4), INVALID), (dict(db=A + 4), INVALID), (dict(pre=A + 2, act=2), INVALID),
     (dict(wdt=4), INVALID), (dict(dtype=sa.SA_FP32, wdt=sa.SA_BF16), UNSUPPORTED), (dict(ws=None), WORKSPACE),
     (dict(wsb=1), WORKSPACE), (dict(ws=A + 8), WORKSPACE)])

@@ -395,3 +395,52 @@ def test_refusals_leave_tensors_alone(sa):
         with pytest.raises(sa.SAError):
             call()
         assert torch.equal(out, before) and (dK == 4.0).all()
+
+
+@pytest.mark.parametrize("tokens,targets", [([5, 300, 400], [7, 100, 160]), ([300, 5, 2], [200, 9, 0]), ([-9, 300, 1 << 40], [-3, 90, 1 << 40]),
+                                            ([100, 100, 100], [50, 50, 50])])
+@pytest.mark.parametrize("per", [1, 90])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_malformed_offsets_stay_inside(sa, dtype, per, tokens, targets):
+    """Offsets that begin past 0, fall, or reach behind the tensors: any values, but nothing outside of the results."""
+    T, N, h, hk, d = 350, 2 * per, 4, 2, 64
+    offsets, tg = (torch.tensor(v, dtype=torch.int64, device="cuda") for v in (tokens, targets))
+    kv, q, dout = values(dtype, (T, 2, hk, d), 1), values(dtype, (N, h, d), 2), values(dtype, (N, h, d), 3)
+    big = lambda n: torch.full((n + 64, h, d), 9.0, dtype=DT[dtype], device="cuda")  # noqa: E731
+    o, dq, dkv = big(N), big(N), torch.full((T + 64, 2, hk, d), 9.0, dtype=DT[dtype], device="cuda")
+    _, lse = sa.recent_attn_fwd(q, kv[:, 0], kv[:, 1], offsets, tg, out=o[32:32 + N])
+    lse = torch.zeros_like(lse)
+    sa.recent_attn_bwd(q, kv[:, 0], kv[:, 1], offsets, tg, torch.zeros_like(q), lse, dout, dq=dq[32:32 + N], dK=dkv[32:32 + T, 0],
+                       dV=dkv[32:32 + T, 1])
+    torch.cuda.synchronize()
+    for t, n in ((o, N), (dq, N), (dkv, T)):
+        assert (t[:32] == 9.0).all() and (t[32 + n:] == 9.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("N,K,F", [(3, 1 << 20, 24), (40, (1 << 20) - 3, 5), (3, 24, 1 << 20), (70, 9, (1 << 20) - 1)])
+def test_linear_of_the_widest(sa, dtype, N, K, F):
+    x, W, dy = values(dtype, (N, K), 1), values(dtype, (K, F), 2, K ** -0.5), values(dtype, (N, F), 3)
+    y, _ = sa.linear_fwd(x, W)
+    ry, _, ey, _ = ol.linear_fwd(f8(x), f8(W), None, "none", None, dtype)
+    within(y, ry, ey, "y")
+    got = sa.linear_bwd(x, W, dy, bias=True)
+    ref, off = ol.linear_bwd(f8(x), f8(W), None, f8(dy), "none", dtype)
+    for k in got:
+        within(got[k], ref[k], off[k] + HALF[dtype] * np.abs(ref[k]), k)
+
+
+def test_norm_of_the_widest(sa):
+    """2^24 values a row: off by what sums of so many can be (a tree's log2 of them, 24 roundings and the lanes' own 256)."""
+    D = 1 << 24
+    x, gamma, beta, dy = values("fp32", (2, D), 1), values("fp32", (D,), 2, 0.1, 1.0), values("fp32", (D,), 3), values("fp32", (2, D), 4)
+    y, st = sa.layer_norm_fwd(x, gamma, beta)
+    g = sa.layer_norm_bwd(x, gamma, st, dy)
+    X, G = x.double(), gamma.double()
+    xh = (X - X.mean(1, keepdim=True)) / torch.sqrt(X.var(1, unbiased=False, keepdim=True) + 1e-5)
+    assert (y - (xh * G + beta.double())).abs().max() < 1e-4
+    d = dy.double()
+    e = d * G
+    dx = (e - e.mean(1, keepdim=True) - xh * (e * xh).mean(1, keepdim=True)) / torch.sqrt(X.var(1, unbiased=False, keepdim=True) + 1e-5)
+    assert (g["dx"] - dx).abs().max() < 1e-4
+    assert (g["dgamma"] - (d * xh).sum(0)).abs().max() < 1e-4 and (g["dbeta"] - d.sum(0)).abs().max() < 1e-5
