@@ -439,7 +439,8 @@ int32_t fused_rows(bool bf16, int32_t d) {
 }
 
 int32_t fused_chunk(int64_t B, int64_t T, int32_t hk) {
-    // enough chunks for the compute units, and few enough that their rows cost little
+    // Enough chunks for the compute units, and few enough that their rows cost little (16 users of 10,000 tokens, 16
+    // heads of 64, 40 targets: at most 576 keys 358 us, 1,152 337, 2,304 343).
     const int64_t want = T * hk / (4 * (int64_t)device_cus());
     return (int32_t)std::min<int64_t>(1152, std::max<int64_t>(256, want / 128 * 128));
 }
