@@ -1,12 +1,12 @@
 // The keys' and values' gradients of the attention over recent histories.
 //
 // A workgroup holds 128 keys of one user and key head, 32 a wave and one a lane of each half, and
-// takes all rows that may see them, 32 at a time through LDS: S = q K^T and dP = dout V^T leave a
+// takes all rows that may see them, 64 at a time through LDS (fp32: 32): S = q K^T and dP = dout V^T leave a
 // key's scores in its own two lanes, from where p = exp(s - lse) goes into dV^T += dout^T p and
 // ds = p (dP - delta), times the cap's derivative, into dK^T += q^T ds.  Every sum is one
 // workgroup's, in the rows' order: nothing is added up in memory.  16 users of 300 targets and
-// 4,000 tokens, 8 heads of 64, take 178 us, 79 GFLOP: four products of 32 rows between two
-// barriers, and 8 waves a CU.
+// 4,000 tokens, 8 heads of 64, take 153 us, 79 GFLOP: 8 waves a CU, whose softmax and products
+// share the SIMDs two by two.
 #include <algorithm>
 
 #include "recent_attn.h"
@@ -16,13 +16,15 @@ namespace attn {
 
 namespace {
 
-constexpr int kKeys = kKeyTile, kRows = 32;
+constexpr int kKeys = kKeyTile, kMostRows = 64;
 
 template <typename T, int D>
 struct KeysCfg {
-    static constexpr int EL = sizeof(T), TILE = kRows * D * EL;
-    static constexpr int STAGE = 2 * TILE;   // q and dout
-    static constexpr int LOADS = TILE / 1024 / 4;   // a wave's, of each
+    static constexpr int EL = sizeof(T), TILE = 32 * D * EL;
+    // tiles of rows between two barriers (two for one: 176 us to 153 at D = 64 in the case above, 497 to 389 at D = 128)
+    static constexpr int RT = EL == 2 ? 2 : 1, ROWS = 32 * RT;
+    static constexpr int STAGE = 2 * RT * TILE;                  // q and dout
+    static constexpr int LOADS = RT * TILE / 1024 / 4;           // a wave's, of each
     // (one workgroup more a CU spills 51 and 111 registers: 16 users of 300 targets and 4,000 tokens, 8 heads, 278 us
     // for 185 at D = 64, 752 for 519 at D = 128)
     static constexpr int PER_CU = EL == 2 && D == 64 ? 2 : 1;
@@ -30,15 +32,15 @@ struct KeysCfg {
 
 // a row's statistics in LDS
 struct RowStats {
-    float lse2[kRows], delta[kRows], slope2[kRows];
-    int32_t lo[kRows], hi[kRows];   // absolute; hi = lo: sees nothing
+    float lse2[kMostRows], delta[kMostRows], slope2[kMostRows];
+    int32_t lo[kMostRows], hi[kMostRows];   // absolute; hi = lo: sees nothing
 };
 
 template <typename T, int D>
 __global__ __launch_bounds__(256, (KeysCfg<T, D>::PER_CU)) void keys_kernel(KeysArgs f) {
     using C = KeysCfg<T, D>;
     using M = Tile32<T, D>;
-    __shared__ __attribute__((aligned(16))) uint8_t smem[2 * C::STAGE];   // 4 tiles: one a wave for its results
+    __shared__ __attribute__((aligned(16))) uint8_t smem[2 * C::STAGE];   // 4 tiles or more: one a wave for its results
     __shared__ __attribute__((aligned(16))) RowStats stats[2];
     const View& a = f.a;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hl = lane >> 5;
@@ -66,18 +68,18 @@ __global__ __launch_bounds__(256, (KeysCfg<T, D>::PER_CU)) void keys_kernel(Keys
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = f32x16{};
 
-        const int32_t rows = us.n * a.g, units = (rows + kRows - 1) / kRows;
+        const int32_t rows = us.n * a.g, units = (rows + C::ROWS - 1) / C::ROWS;
         const T* qp = reinterpret_cast<const T*>(a.q) + us.t0 * a.q_t + (int64_t)kv * a.g * a.q_h;
         const T* dp = reinterpret_cast<const T*>(f.dout) + (us.t0 * a.h + (int64_t)kv * a.g) * D;
         auto issue = [&](int32_t u, int stage) __attribute__((always_inline)) {
             uint8_t* to = smem + stage * C::STAGE;
-            const int32_t r0 = u * kRows, t0 = r0 / a.g;
+            const int32_t r0 = u * C::ROWS, t0 = r0 / a.g;
             const char* qb = reinterpret_cast<const char*>(qp + (int64_t)t0 * a.q_t);
             const char* db = reinterpret_cast<const char*>(dp + (int64_t)t0 * a.h * D);
 #pragma unroll
             for (int i = 0; i < C::LOADS; ++i) {
                 const int q = w + 4 * i, pos = q * 64 + lane, r = pos / M::CHUNKS;
-                const uint32_t chunk = 16u * M::chunk_at(r, pos % M::CHUNKS);
+                const uint32_t chunk = 16u * M::chunk_at(r & 31, pos % M::CHUNKS);
                 const uint32_t row = (uint32_t)min(r0 + r, rows - 1);
                 uint32_t t = row, gi = 0;
                 if (a.g > 1) {
@@ -86,17 +88,17 @@ __global__ __launch_bounds__(256, (KeysCfg<T, D>::PER_CU)) void keys_kernel(Keys
                 }
                 t -= (uint32_t)t0;
                 dma16(qb, t * (uint32_t)(a.q_t * C::EL) + gi * (uint32_t)(a.q_h * C::EL) + chunk, to + q * 1024);
-                dma16(db, (t * (uint32_t)a.h + gi) * (uint32_t)(D * C::EL) + chunk, to + C::TILE + q * 1024);
+                dma16(db, (t * (uint32_t)a.h + gi) * (uint32_t)(D * C::EL) + chunk, to + C::RT * C::TILE + q * 1024);
             }
         };
-        // the statistics of unit u's rows, by the first 32 threads
+        // the statistics of unit u's rows, by the first threads
         struct Stat {
             float lse2, delta, slope2;
             int32_t lo, hi;
         };
         auto stat = [&](int32_t u) {
             Stat s;
-            const int32_t row = u * kRows + l32;
+            const int32_t row = u * C::ROWS + lane;
             const bool in = row < rows;
             const int64_t target = us.t0 + (in ? row / a.g : 0);
             const int32_t head = kv * a.g + (in ? row % a.g : 0);
@@ -113,101 +115,107 @@ __global__ __launch_bounds__(256, (KeysCfg<T, D>::PER_CU)) void keys_kernel(Keys
         };
         auto put = [&](const Stat& s, int stage) {
             RowStats& st = stats[stage];
-            st.lse2[l32] = s.lse2;
-            st.delta[l32] = s.delta;
-            st.slope2[l32] = s.slope2;
-            st.lo[l32] = s.lo;
-            st.hi[l32] = s.hi;
+            st.lse2[lane] = s.lse2;
+            st.delta[lane] = s.delta;
+            st.slope2[lane] = s.slope2;
+            st.lo[lane] = s.lo;
+            st.hi[lane] = s.hi;
         };
         auto multiply = [&](int stage) __attribute__((always_inline)) {
-            T* qt = reinterpret_cast<T*>(smem + stage * C::STAGE);
-            T* dt = reinterpret_cast<T*>(smem + stage * C::STAGE + C::TILE);
+            T* const q0 = reinterpret_cast<T*>(smem + stage * C::STAGE);
+            T* const d0 = reinterpret_cast<T*>(smem + stage * C::STAGE + C::RT * C::TILE);
             const RowStats& st = stats[stage];
-            const int32_t lo = st.lo[l32], hi = st.hi[l32];
-            const uint32_t dead = (uint32_t)__builtin_amdgcn_ballot_w64(!(st.lse2[l32] < __builtin_inff()));
+            const uint64_t dead = __builtin_amdgcn_ballot_w64(lane < C::ROWS && !(st.lse2[lane % C::ROWS] < __builtin_inff()));
             if (dead) {   // rows without weights, or with some that are no numbers: zeros, whatever they hold (the same
                           // in every wave)
-                for (int x = tid; x < kRows * M::CHUNKS; x += 256)
+                for (int x = tid; x < C::ROWS * M::CHUNKS; x += 256)
                     if ((dead >> (x / M::CHUNKS)) & 1u) {
-                        reinterpret_cast<uint4*>(qt)[x] = make_uint4(0, 0, 0, 0);
-                        reinterpret_cast<uint4*>(dt)[x] = make_uint4(0, 0, 0, 0);
+                        reinterpret_cast<uint4*>(q0)[x] = make_uint4(0, 0, 0, 0);
+                        reinterpret_cast<uint4*>(d0)[x] = make_uint4(0, 0, 0, 0);
                     }
                 lds_barrier();
             }
             if (mine <= 0) return;
             const int32_t k0 = (int32_t)key0, kn = k0 + min(mine, 32);
-            const bool live = hi > lo;
-            if (!__builtin_amdgcn_ballot_w64(live && lo < kn && hi > k0)) return;
-            const bool whole = __builtin_amdgcn_ballot_w64(live && (lo > k0 || hi < kn)) == 0;
-            f32x16 s = f32x16{}, ds = f32x16{};
-            M::with_rows(s, qt, kf, lane);
-            M::with_rows(ds, dt, vf, lane);
-            float cc = a.scale * kLog2e;
-            float slope[16];
-            const bool cap = a.cap > 0.f;
+#pragma unroll 1
+            for (int t = 0; t < C::RT; ++t) {
+                const T* const qt = q0 + t * 32 * D;
+                const T* const dt = d0 + t * 32 * D;
+                const int r0 = 32 * t;
+                const int32_t lo = st.lo[r0 + l32], hi = st.hi[r0 + l32];
+                const bool live = hi > lo;
+                if (!__builtin_amdgcn_ballot_w64(live && lo < kn && hi > k0)) continue;
+                const bool whole = __builtin_amdgcn_ballot_w64(live && (lo > k0 || hi < kn)) == 0;
+                f32x16 s = f32x16{}, ds = f32x16{};
+                M::with_rows(s, qt, kf, lane);
+                M::with_rows(ds, dt, vf, lane);
+                float cc = a.scale * kLog2e;
+                float slope[16];
+                const bool cap = a.cap > 0.f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float4 de = *reinterpret_cast<const float4*>(&st.delta[8 * j + 4 * hl]);
-                ds[4 * j] -= de.x;
-                ds[4 * j + 1] -= de.y;
-                ds[4 * j + 2] -= de.z;
-                ds[4 * j + 3] -= de.w;
-            }
-            if (cap) {
-                cc = 1.f;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[r] = capped<T>(s[r], to_exp, inv_cap, cap2, &slope[r]);
-                    ds[r] *= slope[r];
+                for (int j = 0; j < 4; ++j) {
+                    const float4 de = *reinterpret_cast<const float4*>(&st.delta[r0 + 8 * j + 4 * hl]);
+                    ds[4 * j] -= de.x;
+                    ds[4 * j + 1] -= de.y;
+                    ds[4 * j + 2] -= de.z;
+                    ds[4 * j + 3] -= de.w;
                 }
-            }
-            if (a.slopes) {
-                const int32_t key = k0 + l32;
+                if (cap) {
+                    cc = 1.f;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int row = srow(r, hl);
-                    s[r] = __builtin_fmaf(s[r], cc, st.slope2[row] * (float)(key + 1 - st.hi[row]));
+                    for (int r = 0; r < 16; ++r) {
+                        s[r] = capped<T>(s[r], to_exp, inv_cap, cap2, &slope[r]);
+                        ds[r] *= slope[r];
+                    }
                 }
-                cc = 1.f;
-            }
+                if (a.slopes) {
+                    const int32_t key = k0 + l32;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float4 ls = *reinterpret_cast<const float4*>(&st.lse2[8 * j + 4 * hl]);
-                const float lv[4] = {ls.x, ls.y, ls.z, ls.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[4 * j + e] = exp2_(__builtin_fmaf(s[4 * j + e], cc, -lv[e]));
-                    ds[4 * j + e] *= s[4 * j + e];
+                    for (int r = 0; r < 16; ++r) {
+                        const int row = r0 + srow(r, hl);
+                        s[r] = __builtin_fmaf(s[r], cc, st.slope2[row] * (float)(key + 1 - st.hi[row]));
+                    }
+                    cc = 1.f;
                 }
-            }
-            if (!whole) {   // (after the product: lse2 may be no number)
-                const int32_t key = k0 + l32;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int row = srow(r, hl);
-                    const bool in = key >= st.lo[row] && key < st.hi[row];
-                    s[r] = in ? s[r] : 0.f;
-                    ds[r] = in ? ds[r] : 0.f;
+                for (int j = 0; j < 4; ++j) {
+                    const float4 ls = *reinterpret_cast<const float4*>(&st.lse2[r0 + 8 * j + 4 * hl]);
+                    const float lv[4] = {ls.x, ls.y, ls.z, ls.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[4 * j + e] = exp2_(__builtin_fmaf(s[4 * j + e], cc, -lv[e]));
+                        ds[4 * j + e] *= s[4 * j + e];
+                    }
                 }
+                if (!whole) {   // (after the product: lse2 may be no number)
+                    const int32_t key = k0 + l32;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int row = r0 + srow(r, hl);
+                        const bool in = key >= st.lo[row] && key < st.hi[row];
+                        s[r] = in ? s[r] : 0.f;
+                        ds[r] = in ? ds[r] : 0.f;
+                    }
+                }
+                M::with_cols(dv, dt, M::cols(s), lane);
+                M::with_cols(dk, qt, M::cols(ds), lane);
             }
-            M::with_cols(dv, dt, M::cols(s), lane);
-            M::with_cols(dk, qt, M::cols(ds), lane);
         };
 
         if (units > 0) {
             lds_barrier();   // the last tile's rows are read
             issue(0, 0);
-            if (tid < 32) put(stat(0), 0);
+            if (tid < C::ROWS) put(stat(0), 0);
             wait_loads<0>();
             lds_barrier();
             for (int32_t u = 0; u < units; ++u) {
                 Stat next;
                 if (u + 1 < units) {
-                    if (tid < 32) next = stat(u + 1);
+                    if (tid < C::ROWS) next = stat(u + 1);
                     issue(u + 1, (u + 1) & 1);
                 }
                 multiply(u & 1);
-                if (u + 1 < units && tid < 32) put(next, (u + 1) & 1);
+                if (u + 1 < units && tid < C::ROWS) put(next, (u + 1) & 1);
                 wait_loads<0>();
                 lds_barrier();
             }
