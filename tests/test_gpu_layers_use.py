@@ -444,3 +444,19 @@ def test_norm_of_the_widest(sa):
     dx = (e - e.mean(1, keepdim=True) - xh * (e * xh).mean(1, keepdim=True)) / torch.sqrt(X.var(1, unbiased=False, keepdim=True) + 1e-5)
     assert (g["dx"] - dx).abs().max() < 1e-4
     assert (g["dgamma"] - (d * xh).sum(0)).abs().max() < 1e-4 and (g["dbeta"] - d.sum(0)).abs().max() < 1e-5
+
+
+@pytest.mark.parametrize("tokens,targets", [([0, 0], [2, 3]), ([5, 200], [0, 0]), ([0], [0]), ([], []), ([0, 0], [70, 130]), ([1], [1])])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_without_tokens_or_targets(sa, dtype, tokens, targets):
+    T, N, h, hk, d = sum(tokens), sum(targets), 4, 2, 64
+    kv, q, dout = values(dtype, (T, 2, hk, d), 1), values(dtype, (N, h, d), 2), values(dtype, (N, h, d), 3)
+    off, tg = csr(tokens), csr(targets)
+    out, lse = sa.recent_attn_fwd(q, kv[:, 0], kv[:, 1], off, tg)
+    dkv = torch.full_like(kv, 9.0)
+    g = sa.recent_attn_bwd(q, kv[:, 0], kv[:, 1], off, tg, out, lse, dout, dK=dkv[:, 0], dV=dkv[:, 1])
+    if T == 1:   # one token: its value, and its gradient the sum of two values below 16, rounded once
+        assert torch.equal(out, kv[:, 1].repeat_interleave(2, 1))
+        within(g["dV"], f8(dout).reshape(1, hk, 2, d).sum(2), np.full((1, hk, d), 32 * HALF[dtype]), "dV")
+        return
+    assert not out.any() and torch.isneginf(lse).all() and not g["dq"].any() and not dkv.any()
